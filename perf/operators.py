@@ -251,7 +251,8 @@ def prepare(case, seed):
     seq = per(logp) / (per(counted).clamp(min=1) if case["average"] else 1)
     s["ref_logp"] = (seq + (1.0 if case["average"] else 3.0) * rand(len(lengths))).float() if case["ref"] else None
     s.update(pair_loss=torch.empty(case["pairs"], device="cuda"), seq_logp=torch.empty(len(lengths), device="cuda"),
-             row_logp=torch.empty(rows, device="cuda"), row_lse=torch.empty(rows, device="cuda"))
+             row_logp=torch.empty(rows, device="cuda"),
+             workspace=torch.empty(4 * rows + 16 * case["pairs"] + 1024, device="cuda"))
     return s
 
 
@@ -291,7 +292,7 @@ def _own_distill(s):
 def _own_preference(s):
     c = s["case"]
     _package().glr_preference_loss(s["logits"], s["tokens"], s["offsets"], loss=s["loss"], pair_loss=s["pair_loss"],
-                                   seq_logp=s["seq_logp"], row_logp=s["row_logp"], row_lse=s["row_lse"],
+                                   seq_logp=s["seq_logp"], row_logp=s["row_logp"], workspace=s["workspace"],
                                    dlogits=s["dlogits"], ref_logp=s["ref_logp"], kind=c["kind"], beta=c["beta"],
                                    smoothing=c["smoothing"], average=c["average"])
     return {"loss": s["loss"], "pair_loss": s["pair_loss"], "seq_logp": s["seq_logp"], "row_logp": s["row_logp"],
