@@ -361,6 +361,179 @@ int glr_test_expire_wait(glr_handle* h, int32_t polls, void* stream);
 int glr_select_noalloc(int32_t m_prime, int32_t n_prime, int32_t r, const float* U, const float* Mbar,
                        uint64_t seed, int64_t t, float* lambda_out, int32_t* J_out, void* stream);
 
+/* ---- operators around the step ----------------------------------------------------------- */
+
+/* What makes the gradients that a step takes: the layers' products with their epilogues and
+ * gradients, and the losses on the logits of the last layer, each with the gradient that the
+ * backward pass starts from.  They hold no state: the caller owns every buffer, all work is enqueued
+ * on `stream` without synchronisation, nothing is allocated, and a call may be captured into a
+ * graph.  Common to all of them:
+ *   - Matrices are row-major with unit column stride; ld* is the row stride in elements (at least
+ *     the number of columns; any value and any element-aligned address).  dtype is GLR_F32 or
+ *     GLR_BF16.  Sums, statistics and epilogues are fp32; a bf16 result is rounded once.
+ *   - Sizes may be zero where that leaves nothing to do.  Outputs must not overlap inputs or each
+ *     other unless a description says so.
+ *   - The same call gives the same bits: every sum has a fixed order.
+ *   - Errors: GLR_EINVAL (message in glr_last_error(NULL)), GLR_ECUDA.  glr_operator_status reports
+ *     a bounded device wait that gave up.                                                       */
+
+#define GLR_ACT_NONE      0
+#define GLR_ACT_RELU      1   /* max(z, 0); its slope at 0 is 0                                 */
+#define GLR_ACT_GELU      2   /* z Phi(z) with the error function                              */
+#define GLR_ACT_GELU_TANH 3   /* 0.5 z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3)))              */
+#define GLR_ACT_SILU      4   /* z / (1 + exp(-z))                                             */
+
+/* A linear layer, Z = X W^T + b, Y = act(Z) + R: W (n x k) is the layer matrix as glr_create takes
+ * it (m = n, n = k there).  bias (n, of dtype), residual (rows x n) and preact (receives Z as dtype,
+ * for the backward pass) may be null.  residual may be Y itself.                                */
+typedef struct glr_linear_args {
+    int64_t rows, n, k;
+    const void* X; int64_t ldx;
+    const void* W; int64_t ldw;
+    void* Y; int64_t ldy;
+    const void* bias;
+    const void* residual; int64_t ldr;
+    void* preact; int64_t ldp;
+    int32_t dtype;
+    int32_t act;
+} glr_linear_args;
+int glr_linear(const glr_linear_args* a, void* stream);
+
+/* The gradient of a layer's input, with the activation below it: G = dZ W + residual (the gradient
+ * that reaches X past this layer; may be null), dX = G act'(preact), where preact (rows x k) is the
+ * pre-activation whose activation X is (null: act must be GLR_ACT_NONE, dX = G).  grad_out (null:
+ * not wanted) receives G, the gradient of X itself.  dZ is rows x n, W n x k, dX rows x k.
+ * residual may be dX or grad_out itself.                                                        */
+typedef struct glr_linear_grad_input_args {
+    int64_t rows, n, k;
+    const void* dZ; int64_t lddz;
+    const void* W; int64_t ldw;
+    void* dX; int64_t lddx;
+    const void* residual; int64_t ldr;
+    const void* preact; int64_t ldp;
+    void* grad_out; int64_t ldg;
+    int32_t dtype;
+    int32_t act;
+} glr_linear_grad_input_args;
+int glr_linear_grad_input(const glr_linear_grad_input_args* a, void* stream);
+
+/* Every node's gradient of a layer's weights and bias.  The rows of dZ (nodes * rows x n) and X
+ * (nodes * rows x k) are the nodes' one after the other, `rows` each: dW[i] = dZ_i^T X_i (n x k,
+ * contiguous, grad_dtype: what glr_step takes as G[i]) and, when db is not null, db[i] = the column
+ * sums of dZ_i (n, grad_dtype).  dW and db are host arrays of `nodes` device pointers.  rows = 0
+ * writes zeros.  1 <= nodes <= GLR_MAX_NODES.                                                   */
+typedef struct glr_linear_grad_weight_args {
+    int64_t nodes, rows, n, k;
+    const void* dZ; int64_t lddz;
+    const void* X; int64_t ldx;
+    void* const* dW;
+    void* const* db;
+    int32_t dtype;
+    int32_t grad_dtype;
+} glr_linear_grad_weight_args;
+int glr_linear_grad_weight(const glr_linear_grad_weight_args* a, void* stream);
+
+/* Losses.  logits is rows x vocab.  weight[t] (null: 1 / rows each) is row t's share of the loss;
+ * a row of weight 0 does not count: its logits are not read (they may be NaN), its outputs and its
+ * gradient are zero.  A row whose logits are all -infinity leaves no distribution and counts as if
+ * its weight were 0.  Logits of -infinity are entries ruled out: probability and gradient zero.
+ * dlogits (rows x vocab of dtype) may be null (no gradient is formed) or logits itself with the
+ * same ld.  Indices (ids, labels, tokens, offsets) are int32, or int64 where index64 is 1.  A row
+ * of logits is at most GLR_MAX_LOGIT_BYTES long.                                                 */
+#define GLR_MAX_LOGIT_BYTES 1572864
+
+/* Distillation from a teacher's top logits.  Row t of teacher (rows x topk, teacher_dtype) holds
+ * the teacher's logits a_k at the ids of row t of ids (ld = ld_ids); an id outside [0, vocab) is an
+ * absent entry, and the same id given twice is two entries.  With q = softmax_k(a / tau) over the
+ * present entries, p = softmax(z / tau) and p1 = softmax(z) over the vocabulary:
+ *   row_loss = soft sum_k q_k (log q_k - log p[id_k]) + hard (-log p1[label])
+ *   loss     = sum_t weight_t row_loss_t
+ *   dlogits  = weight (soft / tau (p - sum_k q_k e_{id_k}) + hard (p1 - e_label))
+ * labels null or a label outside [0, vocab): no hard term for the row.  No present entry (or only
+ * teacher logits of -infinity): no soft term.  topk <= GLR_MAX_TOPK; tau > 0.                     */
+#define GLR_MAX_TOPK 1024
+typedef struct glr_distill_args {
+    int64_t rows, vocab, topk;
+    const void* logits; int64_t ld_logits;
+    const void* teacher; int64_t ld_teacher;
+    const void* ids; int64_t ld_ids;
+    const void* labels;
+    const float* weight;
+    float* loss;
+    float* row_loss;
+    void* dlogits; int64_t ld_dlogits;
+    int32_t dtype, teacher_dtype, ids_index64, labels_index64;
+    float temperature, soft, hard;
+    int32_t reserved;
+} glr_distill_args;
+int glr_distill_loss(const glr_distill_args* a, void* stream);
+
+/* The clipped policy loss with a KL term, token by token.  With logp = log softmax(z / tau)[token],
+ * ratio = exp(logp - old_logp) and e = ref_logp - logp:
+ *   row_loss = -min(ratio A, clip(ratio, 1 - clip_low, 1 + clip_high) A) + kl (exp(e) - e - 1)
+ *   loss     = sum_t weight_t row_loss_t
+ *   dlogits  = weight (d row_loss / d logp) (e_token - p) / tau
+ * where the clipped branch has slope 0 (beyond 1 + clip_high for A > 0, below 1 - clip_low
+ * otherwise).  A token outside [0, vocab) makes its row not count.  ref_logp null: no KL term.
+ * logp (rows) receives the log-probabilities, row_loss (rows) the rows' losses.                   */
+typedef struct glr_policy_args {
+    int64_t rows, vocab;
+    const void* logits; int64_t ld_logits;
+    const void* tokens;
+    const float* old_logp;
+    const float* advantage;
+    const float* ref_logp;
+    const float* weight;
+    float* loss;
+    float* row_loss;
+    float* logp;
+    void* dlogits; int64_t ld_dlogits;
+    int32_t dtype, index64;
+    float temperature, clip_low, clip_high, kl;
+} glr_policy_args;
+int glr_policy_loss(const glr_policy_args* a, void* stream);
+
+/* A preference loss on pairs of answers.  Sequence s (0 <= s < 2 pairs) is the rows offsets[s] ..
+ * offsets[s + 1] of logits; 2 p is pair p's chosen answer and 2 p + 1 the rejected one.  tokens[t]
+ * is the token that row t predicts; one outside [0, vocab) does not count (a prompt, padding).  With
+ * row_logp = log softmax(z)[token] (0 where it does not count), seq_logp the sum over a sequence
+ * (its mean over the tokens that count when average is 1; 0 for none) and
+ * h = (seq_logp - ref_logp)_chosen - (seq_logp - ref_logp)_rejected (ref_logp null: 0):
+ *   GLR_PREF_SIGMOID  pair_loss = -(1 - smoothing) log sigmoid(beta h) - smoothing log sigmoid(-beta h)
+ *   GLR_PREF_IPO      pair_loss = (h - 1 / (2 beta))^2
+ *   loss = sum_p weight_p pair_loss_p (weight null: 1 / pairs each; a pair of weight 0 adds nothing
+ *   and gets a zero gradient)
+ *   dlogits = (d loss / d seq_logp) (d seq_logp / d row_logp) (e_token - softmax(z))
+ * Rows in no sequence get a zero gradient; offsets are clamped to [0, rows].  The weights here are the
+ * pairs', and a row whose token does not count is not read.  workspace: at least
+ * GLR_PREFERENCE_WORKSPACE(rows, pairs) bytes of device memory, 16-byte aligned, for this call only. */
+#define GLR_PREF_SIGMOID 0
+#define GLR_PREF_IPO     1
+#define GLR_PREFERENCE_WORKSPACE(rows, pairs) (16 * (int64_t)(rows) + 64 * (int64_t)(pairs) + 4096)
+typedef struct glr_preference_args {
+    int64_t rows, vocab, pairs;
+    const void* logits; int64_t ld_logits;
+    const void* tokens;
+    const void* offsets;
+    const float* ref_logp;
+    const float* weight;
+    float* loss;
+    float* pair_loss;
+    float* seq_logp;
+    float* row_logp;
+    void* dlogits; int64_t ld_dlogits;
+    void* workspace; int64_t workspace_bytes;
+    int32_t dtype, tokens_index64, offsets_index64, kind;
+    float beta, smoothing;
+    int32_t average, reserved;
+} glr_preference_args;
+int glr_preference_loss(const glr_preference_args* a, void* stream);
+
+/* GLR_ETIMEOUT when a bounded wait inside an operator's kernel has given up on the current device
+ * since the library was loaded (*gave_up such events; that call's outputs are not valid), else
+ * GLR_OK.  Synchronises the device.  gave_up may be null.                                         */
+int glr_operator_status(int32_t* gave_up);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,7 +21,9 @@ from ._lib import (GLR_ADAM, GLR_ADAMW, GLR_ALG3, GLR_ALG4, GLR_AMSGRAD, GLR_BF1
 __all__ = ["GlrError", "make_schedule", "glr_create", "glr_destroy", "glr_step", "glr_step_group",
            "glr_step_group_host", "glr_step_host", "glr_save", "glr_load", "glr_refresh", "glr_get_stats", "glr_last_error", "glr_get_error", "glr_get_selection",
            "glr_get_basis", "glr_set_basis", "glr_force_selection", "glr_test_expire_wait", "glr_profile_enable",
-           "glr_profile_read", "glr_select_noalloc", "GreedyLore", "load"]
+           "glr_profile_read", "glr_select_noalloc", "GreedyLore", "load", "glr_linear", "glr_linear_grad_input",
+           "glr_linear_grad_weight", "glr_distill_loss", "glr_policy_loss", "glr_preference_loss",
+           "glr_operator_status"]
 
 
 class GlrError(RuntimeError):
@@ -326,3 +328,7 @@ class GreedyLore:
             self.close()
         except Exception:
             pass
+
+
+from .operators import (glr_distill_loss, glr_linear, glr_linear_grad_input, glr_linear_grad_weight,  # noqa: E402
+                        glr_operator_status, glr_policy_loss, glr_preference_loss)

@@ -18,6 +18,10 @@ GLR_ALG3, GLR_ALG4 = 0, 1
 GLR_MSGD, GLR_ADAM, GLR_AMSGRAD, GLR_ADAMW, GLR_GALORE_ADAM = 0, 1, 2, 3, 4
 GLR_F32, GLR_BF16 = 0, 1
 GLR_MAX_NODES = 64
+GLR_ACT_NONE, GLR_ACT_RELU, GLR_ACT_GELU, GLR_ACT_GELU_TANH, GLR_ACT_SILU = 0, 1, 2, 3, 4
+GLR_PREF_SIGMOID, GLR_PREF_IPO = 0, 1
+GLR_MAX_LOGIT_BYTES = 1572864
+GLR_MAX_TOPK = 1024
 
 _c_void_pp = ctypes.POINTER(ctypes.c_void_p)
 _c_float_p = ctypes.c_void_p     # device/host float buffers are passed as raw addresses
@@ -73,6 +77,34 @@ class GlrDpExchange(ctypes.Structure):
     ]
 
 
+def _struct(name, doc, wide, narrow):
+    """A mirror of one of glr.h's operator argument structs: its 8-byte fields, then its 4-byte ones."""
+    fields = [(f.rstrip("*"), ctypes.c_void_p if f.endswith("*") else ctypes.c_int64) for f in wide.split()]
+    fields += [(f.rstrip("."), ctypes.c_float if f.endswith(".") else ctypes.c_int32) for f in narrow.split()]
+    return type(name, (ctypes.Structure,), {"_fields_": fields, "__doc__": doc})
+
+
+# "name*" is an address, "name" an int64 among the 8-byte fields; "name." a float, "name" an int32 among the rest
+GlrLinearArgs = _struct("GlrLinearArgs", "glr_linear_args",
+                        "rows n k X* ldx W* ldw Y* ldy bias* residual* ldr preact* ldp", "dtype act")
+GlrLinearGradInputArgs = _struct("GlrLinearGradInputArgs", "glr_linear_grad_input_args",
+                                 "rows n k dZ* lddz W* ldw dX* lddx residual* ldr preact* ldp grad_out* ldg",
+                                 "dtype act")
+GlrLinearGradWeightArgs = _struct("GlrLinearGradWeightArgs", "glr_linear_grad_weight_args",
+                                  "nodes rows n k dZ* lddz X* ldx dW* db*", "dtype grad_dtype")
+GlrDistillArgs = _struct("GlrDistillArgs", "glr_distill_args",
+                         "rows vocab topk logits* ld_logits teacher* ld_teacher ids* ld_ids labels* weight* loss* "
+                         "row_loss* dlogits* ld_dlogits",
+                         "dtype teacher_dtype ids_index64 labels_index64 temperature. soft. hard. reserved")
+GlrPolicyArgs = _struct("GlrPolicyArgs", "glr_policy_args",
+                        "rows vocab logits* ld_logits tokens* old_logp* advantage* ref_logp* weight* loss* row_loss* "
+                        "logp* dlogits* ld_dlogits",
+                        "dtype index64 temperature. clip_low. clip_high. kl.")
+GlrPreferenceArgs = _struct("GlrPreferenceArgs", "glr_preference_args",
+                            "rows vocab pairs logits* ld_logits tokens* offsets* ref_logp* weight* loss* pair_loss* "
+                            "seq_logp* row_logp* dlogits* ld_dlogits workspace* workspace_bytes",
+                            "dtype tokens_index64 offsets_index64 kind beta. smoothing. average reserved")
+
 GLR_PHASES = 7
 PHASE_NAMES = ["prev_project", "compose", "lambda", "select", "project", "update", "refresh"]
 
@@ -117,6 +149,13 @@ _SIGNATURES = {
     "glr_select_noalloc": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
                                           ctypes.c_void_p, ctypes.c_uint64, ctypes.c_int64, ctypes.c_void_p,
                                           ctypes.c_void_p, ctypes.c_void_p]),
+    "glr_linear": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p]),
+    "glr_linear_grad_input": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p]),
+    "glr_linear_grad_weight": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p]),
+    "glr_distill_loss": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p]),
+    "glr_policy_loss": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p]),
+    "glr_preference_loss": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p]),
+    "glr_operator_status": (ctypes.c_int, [ctypes.POINTER(ctypes.c_int32)]),
 }
 
 _lib = None

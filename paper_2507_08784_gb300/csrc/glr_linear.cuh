@@ -1,0 +1,72 @@
+// Arguments of the linear layers' kernels, as the entry points (glr_operators.cu) fill them.
+#pragma once
+
+#include "glr_internal.cuh"
+
+namespace glr {
+namespace linear {
+
+// What the epilogue makes of an element acc of the product:
+//   kForward    z = acc + bias; aux <- z; out <- act(z) + add
+//   kGradInput  g = acc + add; aux <- g; out <- g act'(pre)
+//   kGradWeight out[node] <- acc
+enum Mode : int { kForward = 0, kGradInput = 1, kGradWeight = 2 };
+
+// out(i, j) = epilogue(sum_p A(i, p) B(j, p)), i < M, j < N, p < K, for every node (batch) b: A and B
+// move on by sAb and sBb elements.  A(i, p) = A[i sAi + p sAp], one of sAi and sAp being 1; B alike.
+struct Product {
+    int mode, dtype, out_dtype, act;
+    int64_t M, N, K;
+    int nodes;
+    const void* A; int64_t sAi, sAp, sAb;
+    const void* B; int64_t sBj, sBp, sBb;
+    void* out; int64_t ldo;
+    const void* bias;
+    const void* add; int64_t ldadd;
+    const void* pre; int64_t ldpre;
+    void* aux; int64_t ldaux;
+    void* outs[GLR_MAX_NODES];              // kGradWeight: each node's M x N result, contiguous
+    int* err;
+};
+
+// Any strides, sizes and alignment.
+cudaError_t product(const Product& p, cudaStream_t st);
+
+// sums[b][j] = sum over the rows of node b of x(i, j), x rows x n in rows of ldx
+struct ColumnSums {
+    int64_t rows, n;
+    int nodes, dtype, out_dtype;
+    const void* x; int64_t ldx;
+    void* sums[GLR_MAX_NODES];
+};
+cudaError_t column_sums(const ColumnSums& c, cudaStream_t st);
+
+// The activations and their slopes (GLR_ACT_*).
+__device__ __forceinline__ float act_value(float z, int act) {
+    switch (act) {
+        case GLR_ACT_RELU: return z <= 0.f ? 0.f : z;            // a NaN stays one
+        case GLR_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.7071067811865476f));
+        case GLR_ACT_GELU_TANH: return 0.5f * z * (1.f + tanhf(0.7978845608028654f * (z + 0.044715f * z * z * z)));
+        case GLR_ACT_SILU: return z / (1.f + expf(-z));
+        default: return z;
+    }
+}
+__device__ __forceinline__ float act_slope(float z, int act) {
+    switch (act) {
+        case GLR_ACT_RELU: return z <= 0.f ? 0.f : z > 0.f ? 1.f : z;
+        case GLR_ACT_GELU:
+            return 0.5f * (1.f + erff(z * 0.7071067811865476f)) + z * (0.3989422804014327f * expf(-0.5f * z * z));
+        case GLR_ACT_GELU_TANH: {
+            const float t = tanhf(0.7978845608028654f * (z + 0.044715f * z * z * z));
+            return 0.5f * (1.f + t) + 0.5f * z * (1.f - t * t) * 0.7978845608028654f * (1.f + 3.f * 0.044715f * z * z);
+        }
+        case GLR_ACT_SILU: {
+            const float p = 1.f / (1.f + expf(-z));
+            return p * (1.f + z * (1.f - p));
+        }
+        default: return 1.f;
+    }
+}
+
+}  // namespace linear
+}  // namespace glr
