@@ -29,8 +29,12 @@ struct Product {
     int* err;
 };
 
-// Any strides, sizes and alignment.
 cudaError_t product(const Product& p, cudaStream_t st);
+// Any strides, sizes, alignment and types (k_linear.cu).
+cudaError_t any_product(const Product& p, cudaStream_t st);
+// bf16 operands whose rows begin on 16 bytes: tcgen05 (k_linear_tc.cu).
+bool tc_ok(const Product& p);
+cudaError_t tc_product(const Product& p, cudaStream_t st);
 
 // sums[b][j] = sum over the rows of node b of x(i, j), x rows x n in rows of ldx
 struct ColumnSums {

@@ -100,8 +100,11 @@ __device__ __forceinline__ void slab_mma(float (&acc)[2][4][4], const __nv_bfloa
             for (int n = 0; n < 4; ++n) mma_bf16(acc[m][n], fa[m], fb[n]);
     }
 }
-__device__ __forceinline__ void slab_mma(float (&acc)[2][4][4], const float* a, const float* b, int g, int t) {
+// fp32: the tensor core truncates its sums, which would add up over a long contraction; a slab's products
+// are summed there by themselves and join the total in a rounded addition.
+__device__ __forceinline__ void slab_mma(float (&total)[2][4][4], const float* a, const float* b, int g, int t) {
     constexpr int P = Traits<float>::kPitch;
+    float acc[2][4][4] = {};
 #pragma unroll
     for (int k = 0; k < kSlab; k += 8) {
         uint32_t ah[2][4], al[2][4], bh[4][2], bl[4][2];
@@ -126,6 +129,12 @@ __device__ __forceinline__ void slab_mma(float (&acc)[2][4][4], const float* a, 
                 mma_tf32(acc[m][n], ah[m], bh[n]);
             }
     }
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) total[m][n][q] += acc[m][n][q];
 }
 
 __device__ __forceinline__ void finish(const Product& p, int node, int64_t i, int64_t j, float acc) {
@@ -212,6 +221,10 @@ bool wide_ok(const void* base, int64_t row_stride, int64_t node_stride, int64_t 
 
 cudaError_t product(const Product& p, cudaStream_t st) {
     if (p.M == 0 || p.N == 0) return cudaSuccess;
+    return tc_ok(p) ? tc_product(p, st) : any_product(p, st);
+}
+
+cudaError_t any_product(const Product& p, cudaStream_t st) {
     const int64_t es = p.dtype == GLR_BF16 ? 2 : 4;
     const int64_t tiles = ((p.M + kTile - 1) / kTile) * ((p.N + kTile - 1) / kTile);
     if (tiles > 0x7fffffff) return cudaErrorInvalidValue;
