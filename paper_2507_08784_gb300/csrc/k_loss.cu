@@ -5,17 +5,29 @@
 // log p_v = (z_v - m) / tau - log s and p_v = exp((z_v - m) / tau) / s.  Everything is formed from
 // z - m, so logits of the type's lowest value and of -infinity need no special case: m is taken as 0
 // where every logit is -infinity (then s = 0: the row leaves no distribution), and a NaN reaches s.
+//
+// The rows kernel reads a row once and writes its gradient once.  A row, or with a cluster of C CTAs a
+// C-th of it, lies in a slot of shared memory: filled by a bulk copy while earlier rows are worked on,
+// reduced by the consumer warps, overwritten by its own gradient and written back by a bulk copy.  The
+// CTAs of a cluster exchange (m, s) over distributed shared memory.  So it is bound by HBM as long as a
+// row's arithmetic (two exponentials and about eight instructions a logit) is shorter than its copies.
 #include <math_constants.h>
 
+#include <algorithm>
+
 #include "glr_loss.cuh"
+#include "glr_ptx.cuh"
 
 namespace glr {
 namespace loss {
 
 namespace {
 
+using tc::mbar_expect_tx;
+using tc::mbar_init;
+using tc::smem_u32;
+
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
@@ -27,189 +39,578 @@ __device__ __forceinline__ float load(const __nv_bfloat16* p) { return __bfloat1
 __device__ __forceinline__ void store(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
-// Maximum, and sums of exp at two temperatures (s1: temperature 1, for a hard term beside tau != 1).
-struct Stat { float m, s, s1; };
-// Teacher: maximum, sum of e = exp((a - m) / tau), sums of e a and e (z_id - the row's maximum).
-struct Top { float m, s, a, z; };
+// Two fp32 values in one register pair.
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t exp2_2(uint64_t v) {
+    float a, b;
+    unpack2(v, a, b);
+    return pack2(exp2_fast(a), exp2_fast(b));
+}
 
-// exp2((a - m) c) for a <= m, with exp of -infinity against -infinity counted as 1 (its sum is 0)
+// Sixteen bytes of logits as pairs, and back.
+template <class T> struct Vec;
+template <> struct Vec<__nv_bfloat16> {
+    static constexpr int kElems = 8;
+    static __device__ __forceinline__ void get(const uint4& u, uint64_t (&v)[4]) {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = pack2(__uint_as_float(w[q] << 16), __uint_as_float(w[q] & 0xffff0000u));
+    }
+    static __device__ __forceinline__ float top(const uint4& u) {
+        auto h = [](uint32_t x) { return *reinterpret_cast<const __nv_bfloat162*>(&x); };
+        const __nv_bfloat162 m = __hmax2(__hmax2(h(u.x), h(u.y)), __hmax2(h(u.z), h(u.w)));
+        return fmaxf(__low2float(m), __high2float(m));
+    }
+    static __device__ __forceinline__ uint4 put(const uint64_t (&v)[4]) {
+        uint32_t w[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            float a, b;
+            unpack2(v[q], a, b);
+            const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+            w[q] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+template <> struct Vec<float> {
+    static constexpr int kElems = 4;
+    static __device__ __forceinline__ void get(const uint4& u, uint64_t (&v)[2]) {
+        v[0] = pack2(__uint_as_float(u.x), __uint_as_float(u.y));
+        v[1] = pack2(__uint_as_float(u.z), __uint_as_float(u.w));
+    }
+    static __device__ __forceinline__ float top(const uint4& u) {
+        return fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
+    }
+    static __device__ __forceinline__ uint4 put(const uint64_t (&v)[2]) {
+        float a, b, c, d;
+        unpack2(v[0], a, b);
+        unpack2(v[1], c, d);
+        return make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
+    }
+};
+
+// exp2((a - m) c) for a <= m, with -infinity against -infinity counted as 1 (its sum is 0)
 __device__ __forceinline__ float shrink(float a, float m, float c) {
     return a == -CUDART_INF_F ? 1.f : exp2_fast((a - m) * c);
 }
-__device__ __forceinline__ Stat merge(const Stat& x, const Stat& y, float c) {
+// Maximum, and sums of exp at two temperatures (s1: temperature 1, for a hard term beside tau != 1).
+struct Stat { float m, s, s1; };
+__device__ __forceinline__ Stat merge(const Stat& x, const Stat& y, float c, bool two) {
     Stat r;
     r.m = fmaxf(x.m, y.m);
     r.s = x.s * shrink(x.m, r.m, c) + y.s * shrink(y.m, r.m, c);
-    r.s1 = x.s1 * shrink(x.m, r.m, kLog2e) + y.s1 * shrink(y.m, r.m, kLog2e);
+    r.s1 = two ? x.s1 * shrink(x.m, r.m, kLog2e) + y.s1 * shrink(y.m, r.m, kLog2e) : 0.f;
     return r;
 }
+// Teacher: maximum, sums of e = exp((a - m) / tau) and of e (a - m).
+struct Top { float m, s, a; };
 __device__ __forceinline__ Top merge(const Top& x, const Top& y, float c) {
     Top r;
     r.m = fmaxf(x.m, y.m);
     const float fx = shrink(x.m, r.m, c), fy = shrink(y.m, r.m, c);
     r.s = x.s * fx + y.s * fy;
-    r.a = x.a * fx + y.a * fy;
-    r.z = x.z * fx + y.z * fy;
+    r.a = (x.s == 0.f ? 0.f : (x.a + x.s * (x.m - r.m)) * fx) + (y.s == 0.f ? 0.f : (y.a + y.s * (y.m - r.m)) * fy);
     return r;
 }
-__device__ __forceinline__ Stat shuffle(const Stat& x, int d) {
-    return {__shfl_xor_sync(~0u, x.m, d), __shfl_xor_sync(~0u, x.s, d), __shfl_xor_sync(~0u, x.s1, d)};
+
+constexpr int kMaxWarps = 16;               // consumer warps
+constexpr int kMaxSlots = 4;
+constexpr int kMaxCluster = 8;
+constexpr int kEntries = 4;                 // teacher entries a thread: topk <= 4 x threads
+
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0;
 }
-__device__ __forceinline__ Top shuffle(const Top& x, int d) {
-    return {__shfl_xor_sync(~0u, x.m, d), __shfl_xor_sync(~0u, x.s, d), __shfl_xor_sync(~0u, x.a, d),
-            __shfl_xor_sync(~0u, x.z, d)};
+// Bounded wait.  One that gives up raises the CTA's abort flag and counts; from then on every wait of the
+// CTA returns at once, so that its threads still meet at their barriers and leave together.
+__device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, volatile int* abort, int* err) {
+    for (int it = 0; it < 16000000; ++it) {
+        if (try_wait(bar, parity)) return;
+        if (it >= 64) {
+            if (*abort) return;
+            __nanosleep(64);
+        }
+    }
+    if (atomicExch(const_cast<int*>(abort), 1) == 0) atomicAdd(err, 1);
 }
-// The block's merge, in a fixed order, to every thread.
-template <class S>
-__device__ S block_merge(S x, float c, S* scratch) {
-    for (int d = 16; d; d >>= 1) x = merge(x, shuffle(x, d), c);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = x;
-    __syncthreads();
-    S r = scratch[0];
-    for (int w = 1; w < (int)(blockDim.x >> 5); ++w) r = merge(r, scratch[w], c);
+__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
+}
+__device__ __forceinline__ void bar_consumers(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
+__device__ __forceinline__ bool bar_any(bool p, int threads) {
+    uint32_t r;
+    asm volatile("{ .reg .pred a, b; setp.ne.u32 a, %1, 0; bar.red.or.pred b, 1, %2, a; selp.u32 %0, 1, 0, b; }"
+                 : "=r"(r) : "r"(static_cast<uint32_t>(p)), "r"(threads) : "memory");
+    return r != 0;
+}
+
+// What a row needs beside its logits, and whether it counts.
+struct Side {
+    float w, adv, old, ref;
+    int64_t tok;
+    bool live;
+};
+template <int K>
+__device__ __forceinline__ Side side_of(const RowArgs& a, int64_t row, bool full) {
+    Side s{};
+    s.tok = -1;
+    s.w = K == kLogProb ? 1.f : a.weight ? a.weight[row] : a.share;
+    if (K != kDistill || a.labels.p) {
+        s.tok = K == kDistill ? a.labels.at(row) : a.tokens.at(row);
+        if (s.tok < 0 || s.tok >= a.vocab) s.tok = -1;
+    }
+    s.live = s.w != 0.f && (K == kDistill || s.tok >= 0);
+    if (K == kPolicy && full) {
+        s.adv = a.advantage[row];
+        s.old = a.old_logp[row];
+        if (a.ref_logp) s.ref = a.ref_logp[row];
+    }
+    return s;
+}
+// The 16-byte vectors of a row between its unaligned ends, and this CTA's share of them.
+struct Span {
+    int head, tail;                          // elements before and after the vectors
+    int v0, v1;                              // vectors [v0, v1) are this CTA's
+    int elems;                               // in all the vectors
+};
+template <class T>
+__device__ __forceinline__ Span span_of(const T* z, int vocab, int rank, int csize) {
+    constexpr int E = Vec<T>::kElems;
+    Span s;
+    s.head = static_cast<int>((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / static_cast<int>(sizeof(T));
+    s.head = s.head < vocab ? s.head : vocab;
+    const int n = (vocab - s.head) / E, per = (n + csize - 1) / csize;
+    s.elems = n * E;
+    s.tail = vocab - s.head - s.elems;
+    s.v0 = min(rank * per, n);
+    s.v1 = min(s.v0 + per, n);
+    return s;
+}
+
+constexpr int64_t kSlotMax = 68 * 1024;     // of a row a CTA, so that three slots fit
+constexpr int64_t kRingMax = 208 * 1024;
+
+template <int K, class T>
+__global__ void __launch_bounds__(kMaxWarps * 32 + 32) rows_kernel(const __grid_constant__ RowArgs a) {
+    chain_begin();
+    constexpr int E = Vec<T>::kElems, P = E / 2;
+    extern __shared__ __align__(128) uint8_t slots[];
+    __shared__ __align__(8) uint64_t full_bar[kMaxSlots], done_bar[kMaxSlots], x_bar[2];
+    // by the row's parity: a warp may be a row ahead of one that still reads
+    __shared__ Stat stat_s[2][kMaxWarps], cluster_s[2][kMaxCluster];
+    __shared__ Top top_s[2][K == kDistill ? kMaxWarps : 1];
+    __shared__ float zq_s[K == kDistill ? kMaxWarps : 1];
+    __shared__ int32_t id_s[K == kDistill ? GLR_MAX_TOPK + 1 : 1];
+    __shared__ float q_s[K == kDistill ? GLR_MAX_TOPK + 1 : 1];
+    __shared__ int32_t edge_s[16];
+    __shared__ int abort_flag;
+    const int nt = blockDim.x - 32, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, nw = nt >> 5;
+    const int C = a.cluster, S = a.slots, V = static_cast<int>(a.vocab);
+    uint32_t rank = 0;
+    if (C > 1) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    const int64_t first = blockIdx.x / C, step = gridDim.x / C;
+    volatile int* abort = &abort_flag;
+    if (tid == 0) {
+        abort_flag = 0;
+        for (int q = 0; q < S; ++q) { mbar_init(smem_u32(&full_bar[q]), 1); mbar_init(smem_u32(&done_bar[q]), nw); }
+        mbar_init(smem_u32(&x_bar[0]), C);
+        mbar_init(smem_u32(&x_bar[1]), C);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    if (C > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    const bool grad = K != kLogProb && a.dz != nullptr;
+
+    if (warp == nw) {
+        // producer: fills the slots, writes them back, fills them again
+        if (lane == 0) {
+            bool live = first < a.rows && side_of<K>(a, first, false).live;      // whether the next row to fill is read
+            auto fill = [&](int64_t row, int s) {
+                const T* z = static_cast<const T*>(a.z) + row * a.ldz;
+                const Span sp = span_of(z, V, rank, C);
+                const uint32_t bytes = live ? static_cast<uint32_t>(sp.v1 - sp.v0) * 16u : 0u;
+                const uint32_t bar = smem_u32(&full_bar[s]);
+                mbar_expect_tx(bar, bytes);
+                if (bytes)
+                    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                                 ::"r"(smem_u32(slots + static_cast<size_t>(s) * a.slot_bytes)), "l"(z + sp.head + static_cast<int64_t>(sp.v0) * E),
+                                 "r"(bytes), "r"(bar) : "memory");
+                live = row + step < a.rows && side_of<K>(a, row + step, false).live;
+            };
+            int64_t next = first;
+            for (int s = 0; s < S && next < a.rows; ++s, next += step) fill(next, s);
+            int s = 0;
+            uint32_t use = 0, last = 0;
+            for (int64_t row = first; row < a.rows; row += step) {
+                wait(smem_u32(&done_bar[s]), use, abort, a.err);
+                if (grad) {
+                    const T* z = static_cast<const T*>(a.z) + row * a.ldz;
+                    T* dz = static_cast<T*>(a.dz) + row * a.lddz;
+                    const Span sp = span_of(z, V, rank, C);
+                    if (sp.v1 > sp.v0 && ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0)
+                        asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
+                                     ::"l"(dz + sp.head + static_cast<int64_t>(sp.v0) * E), "r"(smem_u32(slots + static_cast<size_t>(s) * a.slot_bytes)),
+                                     "r"(static_cast<uint32_t>(sp.v1 - sp.v0) * 16u) : "memory");
+                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                }
+                if (next < a.rows) {
+                    if (grad) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    fill(next, s);
+                    next += step;
+                    last = (last & ~(1u << s)) | ((use ^ 1u) << s);
+                }
+                if (++s == S) { s = 0; use ^= 1u; }
+            }
+            if (grad) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+            if (*abort)                               // let the copies already issued land
+                for (int q = 0; q < S; ++q)
+                    if (first + q * step < a.rows)
+                        for (int it = 0; it < 4000000 && !try_wait(smem_u32(&full_bar[q]), (last >> q) & 1u); ++it) __nanosleep(64);
+        }
+        __syncwarp();
+    } else {
+        const float c = a.inv_tau * kLog2e;
+        const bool two = K == kDistill && a.labels.p && a.hard != 0.f && a.inv_tau != 1.f;
+        const uint64_t c2 = pack2(c, c), l2 = pack2(kLog2e, kLog2e);
+        int s = 0, par = 0;
+        uint32_t use = 0, xuse = 0;
+        Side side{};
+        int32_t id[kEntries];
+        float av[kEntries];
+        float edge = 0.f;
+        // Row data of `row`, ahead of their use: everything but what lies in the slot.
+        auto ahead = [&](int64_t row) {
+            side = side_of<K>(a, row, true);
+            if (K == kDistill) {
+#pragma unroll
+                for (int u = 0; u < kEntries; ++u) {
+                    const int k = tid + u * nt;
+                    id[u] = -1;
+                    av[u] = -CUDART_INF_F;
+                    if (k < a.topk && side.live) {
+                        const int64_t v = a.ids.at(row * a.ldi + k), at = row * a.ldt + k;
+                        if (v >= 0 && v < V) {
+                            id[u] = static_cast<int32_t>(v);
+                            av[u] = a.teacher_bf16 ? load(static_cast<const __nv_bfloat16*>(a.teacher) + at)
+                                                   : static_cast<const float*>(a.teacher)[at];
+                        }
+                    }
+                }
+            }
+            const T* z = static_cast<const T*>(a.z) + row * a.ldz;
+            const Span sp = span_of(z, V, rank, C);
+            // the unaligned ends, an element a thread: the head with the first CTA, the tail with the last
+            edge = -CUDART_INF_F;
+            if (side.live && rank == 0 && tid < sp.head) edge = load(z + tid);
+            if (side.live && rank == C - 1 && tid >= 8 && tid < 8 + sp.tail) edge = load(z + sp.head + sp.elems + tid - 8);
+        };
+        if (first < a.rows) ahead(first);
+        for (int64_t row = first; row < a.rows; row += step) {
+            const T* z = static_cast<const T*>(a.z) + row * a.ldz;
+            T* dz = grad ? static_cast<T*>(a.dz) + row * a.lddz : nullptr;
+            const Span sp = span_of(z, V, rank, C);
+            const int nv = sp.v1 - sp.v0;
+            uint4* slot = reinterpret_cast<uint4*>(slots + static_cast<size_t>(s) * a.slot_bytes);
+            const Side now = side;
+            bool counts = now.live;
+            int32_t eid[kEntries];
+            float ea[kEntries], ez[kEntries];
+            const float e0 = edge;
+            // logits at the listed ids: read here, before any CTA of the cluster overwrites them (dz may be z)
+            float zt = 0.f;
+            if (counts && now.tok >= 0) zt = load(z + now.tok);
+            if (K == kDistill) {
+#pragma unroll
+                for (int u = 0; u < kEntries; ++u) {
+                    eid[u] = id[u];
+                    ea[u] = av[u];
+                    ez[u] = eid[u] >= 0 ? load(z + eid[u]) : 0.f;
+                }
+            }
+            if (row + step < a.rows) ahead(row + step);
+
+            wait(smem_u32(&full_bar[s]), use, abort, a.err);
+            // ---- statistics
+            Stat st{-CUDART_INF_F, 0.f, 0.f};
+            if (counts) {
+                uint64_t s2 = 0, t2 = 0;               // pairs of partial sums
+                float m = e0, r = m == -CUDART_INF_F ? 0.f : m;
+                st.s = exp2_fast((e0 - r) * c);
+                st.s1 = exp2_fast((e0 - r) * kLog2e);
+                if (m == -CUDART_INF_F) st.s = st.s1 = 0.f;
+                for (int v = tid; v < nv; v += nt) {
+                    const uint4 u = slot[v];
+                    const float top = Vec<T>::top(u);
+                    if (top > m) {
+                        const float f = shrink(m, top, c);
+                        s2 = mul2(s2, pack2(f, f));
+                        st.s *= f;
+                        if (two) {
+                            const float f1 = shrink(m, top, kLog2e);
+                            t2 = mul2(t2, pack2(f1, f1));
+                            st.s1 *= f1;
+                        }
+                        m = r = top;
+                    }
+                    uint64_t x[P];
+                    Vec<T>::get(u, x);
+                    const uint64_t nr = pack2(-r, -r);
+#pragma unroll
+                    for (int q = 0; q < P; ++q) {
+                        const uint64_t d = add2(x[q], nr);
+                        s2 = add2(s2, exp2_2(mul2(d, c2)));
+                        if (two) t2 = add2(t2, exp2_2(mul2(d, l2)));
+                    }
+                }
+                float x, y;
+                unpack2(s2, x, y);
+                st.s += x + y;
+                unpack2(t2, x, y);
+                st.s1 += x + y;
+                st.m = m;
+            }
+            Top tp{-CUDART_INF_F, 0.f, 0.f};
+            if (K == kDistill) {
+#pragma unroll
+                for (int u = 0; u < kEntries; ++u)     // an entry that the teacher rules out leaves the sums as they are
+                    if (ea[u] != -CUDART_INF_F) tp = merge(tp, Top{ea[u], 1.f, 0.f}, c);
+            }
+#pragma unroll
+            for (int d = 16; d; d >>= 1) {
+                st = merge(st, Stat{__shfl_xor_sync(~0u, st.m, d), __shfl_xor_sync(~0u, st.s, d), two ? __shfl_xor_sync(~0u, st.s1, d) : 0.f}, c, two);
+                if (K == kDistill && warp * 32 < a.topk)
+                    tp = merge(tp, Top{__shfl_xor_sync(~0u, tp.m, d), __shfl_xor_sync(~0u, tp.s, d), __shfl_xor_sync(~0u, tp.a, d)}, c);
+            }
+            if (lane == 0) {
+                stat_s[par][warp] = st;
+                if (K == kDistill) top_s[par][warp] = tp;
+            }
+            bar_consumers(nt);
+            st = lane < nw ? stat_s[par][lane] : Stat{-CUDART_INF_F, 0.f, 0.f};
+            if (K == kDistill) tp = lane < nw ? top_s[par][lane] : Top{-CUDART_INF_F, 0.f, 0.f};
+#pragma unroll
+            for (int d = kMaxWarps / 2; d; d >>= 1) {
+                st = merge(st, Stat{__shfl_xor_sync(~0u, st.m, d), __shfl_xor_sync(~0u, st.s, d), two ? __shfl_xor_sync(~0u, st.s1, d) : 0.f}, c, two);
+                if (K == kDistill)
+                    tp = merge(tp, Top{__shfl_xor_sync(~0u, tp.m, d), __shfl_xor_sync(~0u, tp.s, d), __shfl_xor_sync(~0u, tp.a, d)}, c);
+            }
+            // lanes 0 .. 15 and 16 .. 31 hold the sums of two groups of warps; the second one is empty
+            st.m = __shfl_sync(~0u, st.m, 0); st.s = __shfl_sync(~0u, st.s, 0); st.s1 = __shfl_sync(~0u, st.s1, 0);
+            if (K == kDistill) { tp.m = __shfl_sync(~0u, tp.m, 0); tp.s = __shfl_sync(~0u, tp.s, 0); tp.a = __shfl_sync(~0u, tp.a, 0); }
+            if (C > 1) {
+                if (warp == 0 && lane < C) {
+                    const uint32_t to = peer_addr(smem_u32(&cluster_s[par][rank]), lane);
+                    asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0+4], %2;\n\tst.shared::cluster.f32 [%0+8], %3;"
+                                 ::"r"(to), "f"(st.m), "f"(st.s), "f"(st.s1) : "memory");
+                    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(peer_addr(smem_u32(&x_bar[par]), lane)) : "memory");
+                }
+                wait(smem_u32(&x_bar[par]), xuse, abort, a.err);
+                st = cluster_s[par][0];
+                for (int q = 1; q < C; ++q) st = merge(st, cluster_s[par][q], c, two);
+            }
+            if (st.s == 0.f) counts = false;
+            if (!two) st.s1 = st.s;
+
+            // ---- the row's loss and the factors of its gradient: dense exp2((z - m) c) + dense1 exp2((z - m) log2 e),
+            // less what is listed at single ids
+            const float ln_s = logf(st.s);
+            float dense = 0.f, dense1 = 0.f, at_tok = 0.f;
+            int n = 0, top = 0;                        // listed entries; the label is the last, past `top` teacher's
+            if (K == kDistill) {
+                const bool soft = counts && tp.s != 0.f, hard = counts && now.tok >= 0 && a.hard != 0.f;
+                const float f = now.w * a.soft * a.inv_tau;
+                if (soft) { dense = f / st.s; n = top = a.topk; }
+                const float inv = 1.f / tp.s;
+                float zq = 0.f;
+#pragma unroll
+                for (int u = 0; u < kEntries; ++u) {
+                    const int k = tid + u * nt;
+                    if (k < n) {
+                        const float e = ea[u] == -CUDART_INF_F ? 0.f : exp2_fast((ea[u] - tp.m) * c) * inv;
+                        id_s[k] = eid[u];
+                        q_s[k] = f * e;
+                        if (e != 0.f) zq += e * (ez[u] - st.m);
+                    }
+                }
+                if (warp * 32 < a.topk) {
+#pragma unroll
+                    for (int d = 16; d; d >>= 1) zq += __shfl_xor_sync(~0u, zq, d);
+                }
+                if (lane == 0) zq_s[warp] = zq;
+                if (hard) {
+                    at_tok = now.w * a.hard;
+                    dense1 = at_tok / st.s1;
+                    if (tid == 0) { id_s[n] = static_cast<int32_t>(now.tok); q_s[n] = at_tok; }
+                    ++n;
+                    if (!two) { dense += dense1; dense1 = 0.f; }
+                }
+                bar_consumers(nt);
+                if (tid == 0 && rank == 0) {
+                    float loss = 0.f;
+                    if (soft) {
+                        float z_sum = 0.f;
+                        for (int w = 0; w < nw && w * 32 < a.topk; ++w) z_sum += zq_s[w];
+                        loss = a.soft * ((tp.a * inv * a.inv_tau - logf(tp.s)) - (z_sum * a.inv_tau - ln_s));
+                    }
+                    if (hard) loss += a.hard * (logf(st.s1) - (zt - st.m));
+                    a.row_loss[row] = loss;
+                }
+            } else {
+                const float lp = counts ? (zt - st.m) * a.inv_tau - ln_s : 0.f;
+                if (K == kPolicy) {
+                    float loss = 0.f, slope = 0.f;
+                    if (counts) {
+                        const float A = now.adv, ratio = expf(lp - now.old);
+                        loss = -fminf(ratio * A, fminf(fmaxf(ratio, a.clip_lo), a.clip_hi) * A);
+                        if (isnan(ratio * A)) loss = ratio * A;
+                        slope = (A > 0.f ? ratio > a.clip_hi : ratio < a.clip_lo) ? 0.f : -A * ratio;
+                        if (a.ref_logp) {
+                            const float e = expm1f(now.ref - lp);
+                            loss += a.kl * (e - (now.ref - lp));
+                            slope -= a.kl * e;
+                        }
+                    }
+                    at_tok = -slope * now.w * a.inv_tau;
+                    dense = counts ? at_tok / st.s : 0.f;
+                    if (tid == 0 && rank == 0) { a.row_loss[row] = loss; a.logp[row] = lp; }
+                } else if (tid == 0 && rank == 0) {
+                    a.logp[row] = lp;
+                    a.lse[row] = counts ? st.m + ln_s : CUDART_INF_F;
+                    a.coef[row] = 0.f;
+                }
+            }
+
+            // ---- the gradient, over the logits
+            if (grad) {
+                auto at = [&](float x) {
+                    const float d = x - st.m;
+                    float g = dense * exp2_fast(d * c);
+                    if (two) g += dense1 * exp2_fast(d * kLog2e);
+                    return g;
+                };
+                const uint64_t nm = pack2(-st.m, -st.m), dd = pack2(dense, dense), dd1 = pack2(dense1, dense1);
+                if (counts) {
+                    for (int v = tid; v < nv; v += nt) {
+                        uint64_t x[P];
+                        Vec<T>::get(slot[v], x);
+#pragma unroll
+                        for (int q = 0; q < P; ++q) {
+                            const uint64_t d = add2(x[q], nm);
+                            x[q] = mul2(dd, exp2_2(mul2(d, c2)));
+                            if (two) x[q] = fma2(dd1, exp2_2(mul2(d, l2)), x[q]);
+                        }
+                        slot[v] = Vec<T>::put(x);
+                    }
+                } else {
+                    for (int v = tid; v < nv; v += nt) slot[v] = make_uint4(0, 0, 0, 0);
+                }
+                if (rank == 0 && tid < sp.head) store(dz + tid, counts ? at(e0) : 0.f);
+                if (rank == C - 1 && tid >= 8 && tid < 8 + sp.tail) store(dz + sp.head + sp.elems + tid - 8, counts ? at(e0) : 0.f);
+                // where an id lies: in this CTA's part of the slot, at an end that this CTA writes, or elsewhere
+                T* mine = reinterpret_cast<T*>(slot);
+                auto place = [&](int32_t v, int& in_slot, int& at_edge) {
+                    const int b = v - sp.head - sp.v0 * E;
+                    in_slot = v >= sp.head && b >= 0 && b < nv * E ? b : -1;
+                    at_edge = rank == 0 && v < sp.head ? v : rank == C - 1 && v >= sp.head + sp.elems ? 8 + v - sp.head - sp.elems : -1;
+                };
+                if (K == kPolicy && counts) {
+                    int b, e;
+                    place(static_cast<int32_t>(now.tok), b, e);
+                    if (b >= 0 && tid == (b / E) % nt) store(mine + b, at(zt) - at_tok);
+                    if (e >= 0 && tid == e) store(dz + now.tok, at(zt) - at_tok);
+                }
+                if (K == kDistill && n > 0) {
+                    // each listed entry marks its place; where all find their own mark no id is listed twice
+                    bar_consumers(nt);
+                    int b[kEntries + 1], e[kEntries + 1], who[kEntries + 1];
+                    float zz[kEntries + 1];
+#pragma unroll
+                    for (int u = 0; u <= kEntries; ++u) {
+                        const bool is_tok = u == kEntries;
+                        const int k = is_tok ? (tid == 0 ? top : n) : tid + u * nt;
+                        who[u] = -1;
+                        b[u] = e[u] = -1;
+                        zz[u] = is_tok ? zt : ez[u < kEntries ? u : 0];
+                        if (is_tok ? k < n : k < top) {
+                            const int32_t v = id_s[k];
+                            if (v >= 0) {
+                                place(v, b[u], e[u]);
+                                if (b[u] >= 0 || e[u] >= 0) who[u] = k;
+                                if (b[u] >= 0) *reinterpret_cast<uint16_t*>(mine + b[u]) = static_cast<uint16_t>(k);
+                                if (e[u] >= 0) edge_s[e[u]] = k;
+                            }
+                        }
+                    }
+                    bar_consumers(nt);
+                    bool twice = false;
+#pragma unroll
+                    for (int u = 0; u <= kEntries; ++u) {
+                        if (b[u] >= 0) twice |= *reinterpret_cast<const uint16_t*>(mine + b[u]) != who[u];
+                        if (e[u] >= 0) twice |= edge_s[e[u]] != who[u];
+                    }
+                    twice = bar_any(twice, nt);
+#pragma unroll
+                    for (int u = 0; u <= kEntries; ++u) {
+                        if (who[u] < 0) continue;
+                        float g = q_s[who[u]];
+                        if (twice) {
+                            g = 0.f;
+                            const int32_t v = id_s[who[u]];
+                            for (int j = 0; j < n; ++j) g += id_s[j] == v ? q_s[j] : 0.f;
+                        }
+                        if (b[u] >= 0) store(mine + b[u], at(zz[u]) - g);
+                        else store(dz + id_s[who[u]], at(zz[u]) - g);
+                    }
+                }
+                if (((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) != 0) {
+                    // the gradient's rows lie otherwise on 16 bytes than the logits': element by element
+                    bar_consumers(nt);
+                    T* to = dz + sp.head + static_cast<int64_t>(sp.v0) * E;
+                    for (int q = tid; q < nv * E; q += nt) to[q] = mine[q];
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            }
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(smem_u32(&done_bar[s]));
+            if (++s == S) { s = 0; use ^= 1u; }
+            if (par) xuse ^= 1u;
+            par ^= 1;
+        }
+    }
+    // no CTA of a cluster leaves while another may still write to its shared memory
+    if (C > 1) {
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
 }
 
 constexpr int kThreads = 512;
-
-// One CTA a row, the row read twice (statistics, gradient).
-template <int K, class T>
-__global__ void __launch_bounds__(kThreads) rows_kernel(const RowArgs a) {
-    chain_begin();
-    __shared__ Stat stat_s[kThreads / 32];
-    __shared__ Top top_s[kThreads / 32];
-    __shared__ int32_t id_s[GLR_MAX_TOPK + 1];
-    __shared__ float q_s[GLR_MAX_TOPK + 1];
-    const float c = a.inv_tau * kLog2e;
-    const int tid = threadIdx.x;
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const T* z = static_cast<const T*>(a.z) + row * a.ldz;
-        T* dz = a.dz ? static_cast<T*>(a.dz) + row * a.lddz : nullptr;
-        const float w = a.weight ? a.weight[row] : a.share;
-        int64_t tok = -1;
-        if (K != kDistill) tok = a.tokens.at(row);
-        else if (a.labels.p) tok = a.labels.at(row);
-        const bool has_tok = tok >= 0 && tok < a.vocab;
-        bool counts = K == kDistill ? w != 0.f : K == kPolicy ? has_tok && w != 0.f : has_tok;
-        Stat st{-CUDART_INF_F, 0.f, 0.f};
-        if (counts) {
-            for (int64_t v = tid; v < a.vocab; v += kThreads) {
-                const float x = load(z + v);
-                const float m = fmaxf(st.m, x), r = m == -CUDART_INF_F ? 0.f : m;
-                st.s = st.s * shrink(st.m, m, c) + exp2_fast((x - r) * c);
-                if (K == kDistill) st.s1 = st.s1 * shrink(st.m, m, kLog2e) + exp2_fast((x - r) * kLog2e);
-                st.m = m;
-            }
-        }
-        st = block_merge(st, c, stat_s);
-        if (st.s == 0.f) counts = false;
-        const float ln_s = logf(st.s);
-        float dense = 0.f, dense1 = 0.f;     // factors of exp2((z - m) c) and exp2((z - m) log2 e)
-        int n = 0;                            // entries subtracted at their ids
-        if (K == kDistill) {
-            Top tp{-CUDART_INF_F, 0.f, 0.f, 0.f};
-            float aval[GLR_MAX_TOPK / kThreads];
-#pragma unroll
-            for (int u = 0; u < GLR_MAX_TOPK / kThreads; ++u) {
-                const int k = tid + u * kThreads;
-                int64_t id = -1;
-                aval[u] = -CUDART_INF_F;
-                if (k < a.topk) {
-                    id = a.ids.at(row * a.ldi + k);
-                    if (id >= a.vocab) id = -1;
-                    if (id >= 0 && counts) {
-                        const int64_t at = row * a.ldt + k;
-                        aval[u] = a.teacher_bf16 ? load(static_cast<const __nv_bfloat16*>(a.teacher) + at)
-                                                 : static_cast<const float*>(a.teacher)[at];
-                        // an entry ruled out by the teacher leaves the sums as they are
-                        if (aval[u] != -CUDART_INF_F) tp = merge(tp, Top{aval[u], 1.f, aval[u], load(z + id) - st.m}, c);
-                    }
-                    id_s[k] = static_cast<int32_t>(id);
-                }
-            }
-            tp = block_merge(tp, c, top_s);
-            const bool soft = counts && tp.s != 0.f, hard = counts && has_tok && a.labels.p;
-            float loss = 0.f;
-            if (soft) {
-                const float ln_st = logf(tp.s), inv = 1.f / tp.s;
-                loss = a.soft * (((tp.a * inv - tp.m) * a.inv_tau - ln_st) - (tp.z * inv * a.inv_tau - ln_s));
-                dense = w * a.soft * a.inv_tau / st.s;
-            }
-#pragma unroll
-            for (int u = 0; u < GLR_MAX_TOPK / kThreads; ++u) {
-                const int k = tid + u * kThreads;
-                if (k < a.topk) q_s[k] = soft ? w * a.soft * a.inv_tau * shrink(aval[u], tp.m, c) / tp.s : 0.f;
-                if (k < a.topk && aval[u] == -CUDART_INF_F) q_s[k] = 0.f;
-            }
-            n = soft ? a.topk : 0;
-            if (hard) {
-                loss += a.hard * -((load(z + tok) - st.m) - logf(st.s1));
-                dense1 = w * a.hard / st.s1;
-                if (tid == 0) { id_s[n] = static_cast<int32_t>(tok); q_s[n] = w * a.hard; }
-                ++n;
-            }
-            if (tid == 0) a.row_loss[row] = loss;
-        } else {
-            const float lp = counts ? (load(z + tok) - st.m) * a.inv_tau - ln_s : 0.f;
-            if (K == kPolicy) {
-                float loss = 0.f, slope = 0.f;
-                if (counts) {
-                    const float A = a.advantage[row], ratio = expf(lp - a.old_logp[row]);
-                    loss = -fminf(ratio * A, fminf(fmaxf(ratio, a.clip_lo), a.clip_hi) * A);
-                    if (isnan(ratio * A)) loss = ratio * A;
-                    slope = (A > 0.f ? ratio > a.clip_hi : ratio < a.clip_lo) ? 0.f : -A * ratio;
-                    if (a.ref_logp) {
-                        const float e = expm1f(a.ref_logp[row] - lp);
-                        loss += a.kl * (e - (a.ref_logp[row] - lp));
-                        slope -= a.kl * e;
-                    }
-                }
-                const float coef = slope * w * a.inv_tau;
-                dense = counts ? -coef / st.s : 0.f;
-                if (counts) { n = 1; if (tid == 0) { id_s[0] = static_cast<int32_t>(tok); q_s[0] = -coef; } }
-                if (tid == 0) { a.row_loss[row] = loss; a.logp[row] = lp; }
-            } else if (tid == 0) {
-                a.logp[row] = lp;
-                a.lse[row] = counts ? st.m + ln_s : CUDART_INF_F;
-                a.coef[row] = 0.f;
-            }
-        }
-        if (K != kLogProb && dz) {
-            __syncthreads();
-            // the gradients at the listed ids are formed before the row is overwritten (dz may be z)
-            float mine[GLR_MAX_TOPK / kThreads + 1];
-#pragma unroll
-            for (int u = 0; u <= GLR_MAX_TOPK / kThreads; ++u) {
-                const int k = tid + u * kThreads;
-                mine[u] = 0.f;
-                if (k < n && id_s[k] >= 0) {
-                    const float x = load(z + id_s[k]);
-                    float g = 0.f;
-                    for (int j = 0; j < n; ++j) g += id_s[j] == id_s[k] ? q_s[j] : 0.f;
-                    mine[u] = dense * exp2_fast((x - st.m) * c) + dense1 * exp2_fast((x - st.m) * kLog2e) - g;
-                }
-            }
-            __syncthreads();
-            for (int64_t v = tid; v < a.vocab; v += kThreads) {
-                float g = 0.f;
-                if (counts) {
-                    const float x = load(z + v) - st.m;
-                    g = dense * exp2_fast(x * c);
-                    if (K == kDistill && dense1 != 0.f) g += dense1 * exp2_fast(x * kLog2e);
-                }
-                store(dz + v, g);
-            }
-            __syncthreads();
-#pragma unroll
-            for (int u = 0; u <= GLR_MAX_TOPK / kThreads; ++u) {
-                const int k = tid + u * kThreads;
-                if (k < n && id_s[k] >= 0) store(dz + id_s[k], mine[u]);
-            }
-            __syncthreads();
-        }
-    }
-}
 
 // Sums of a sequence's log-probabilities in 64 bits, thread by thread and then up the same tree.
 __device__ double block_sum(double x, double* scratch) {
@@ -308,12 +709,38 @@ __global__ void __launch_bounds__(kTotalThreads) total_kernel(const float* x, co
     if (threadIdx.x == 0) *out = static_cast<float>(s);
 }
 
+// Shape of a launch: how many CTAs share a row, their slots and threads.
 template <int K>
-cudaError_t rows_launch(const RowArgs& a, int dtype, cudaStream_t st) {
+cudaError_t rows_launch(RowArgs a, int dtype, cudaStream_t st) {
     if (a.rows == 0) return cudaSuccess;
-    const int grid = static_cast<int>(a.rows < 152 * 4 ? a.rows : 152 * 4);
-    return dtype == GLR_BF16 ? launch_chain(rows_kernel<K, __nv_bfloat16>, grid, kThreads, 0, st, a)
-                             : launch_chain(rows_kernel<K, float>, grid, kThreads, 0, st, a);
+    const int64_t es = dtype == GLR_BF16 ? 2 : 4, row_bytes = a.vocab * es;
+    int dev = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return e;
+    int C = 1;
+    while (C < kMaxCluster && row_bytes / C > kSlotMax) C *= 2;
+    // few rows: more CTAs a row, as long as each has 8 KiB of it
+    while (C < kMaxCluster && a.rows * C * 2 <= sms && row_bytes / (2 * C) >= 8192) C *= 2;
+    a.cluster = C;
+    a.slot_bytes = static_cast<uint32_t>(((row_bytes + 15) / 16 + C - 1) / C * 16);
+    a.slots = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(3, kRingMax / a.slot_bytes)));
+    const size_t smem = static_cast<size_t>(a.slots) * a.slot_bytes;
+    // CTAs an SM: as many as the slots leave room for, with about 512 consumer threads between them
+    int per_sm = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(8, kRingMax / static_cast<int64_t>(smem))));
+    const int warps = std::max(K == kDistill && a.topk > 512 ? 8 : 4, 16 / per_sm);
+    const int64_t groups = std::min<int64_t>(a.rows, std::max<int64_t>(1, static_cast<int64_t>(sms) * per_sm / C));
+    auto kernel = dtype == GLR_BF16 ? rows_kernel<K, __nv_bfloat16> : rows_kernel<K, float>;
+    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kRingMax))) != cudaSuccess) return e;
+    cudaLaunchAttribute attr[2]{};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = C; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = static_cast<unsigned>(groups * C); cfg.blockDim = warps * 32 + 32; cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
 }  // namespace
