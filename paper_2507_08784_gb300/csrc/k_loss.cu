@@ -34,6 +34,12 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// Natural logarithm by the hardware's of base 2: within 2^-22 absolute near 1, 2^-22 relative elsewhere.
+__device__ __forceinline__ float log_fast(float x) {
+    float y;
+    asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y * 0.6931471805599453f;
+}
 __device__ __forceinline__ float load(const float* p) { return *p; }
 __device__ __forceinline__ float load(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ void store(float* p, float v) { *p = v; }
@@ -132,11 +138,12 @@ __device__ __forceinline__ float warp_sum(float x) {
 }
 // The merge of a warp's lanes, in a fixed order, to all of them: one maximum, every lane's sums taken to it,
 // and their sum.  A NaN does not show in a maximum; it stays in the sums.
-__device__ __forceinline__ Stat warp_merge(Stat x, float c, bool two) {
+template <bool TWO>
+__device__ __forceinline__ Stat warp_merge(Stat x, float c) {
     Stat r;
     r.m = warp_max(x.m);
     r.s = warp_sum(x.s * shrink(x.m, r.m, c));
-    r.s1 = two ? warp_sum(x.s1 * shrink(x.m, r.m, kLog2e)) : 0.f;
+    r.s1 = TWO ? warp_sum(x.s1 * shrink(x.m, r.m, kLog2e)) : 0.f;
     return r;
 }
 __device__ __forceinline__ Top warp_merge(Top x, float c) {
@@ -154,17 +161,22 @@ constexpr int kMaxCluster = 8;
 constexpr int kEntries = 2;                 // teacher entries a thread: topk <= 2 x threads
 constexpr int kHeld = 8;                    // 16-byte vectors of a slot whose exponentials a thread keeps in registers
 
-__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
+// `peers`: what other CTAs of the cluster wrote before they arrived is to be seen.
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity, bool peers) {
     uint32_t done;
-    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
-                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    if (peers)
+        asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+                     : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    else
+        asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+                     : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
 // Bounded wait.  One that gives up raises the CTA's abort flag and counts; from then on every wait of the
 // CTA returns at once, so that its threads still meet at their barriers and leave together.
-__device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, volatile int* abort, int* err) {
+__device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, bool peers, volatile int* abort, int* err) {
     for (int it = 0; it < 16000000; ++it) {
-        if (try_wait(bar, parity)) return;
+        if (try_wait(bar, parity, peers)) return;
         if (it >= 64) {
             if (*abort) return;
             __nanosleep(64);
@@ -218,50 +230,62 @@ __device__ __forceinline__ bool is_live(const RowArgs& a, const Side& s) {
     return s.w != 0.f && (K == kDistill || token_of<K>(a, s) >= 0);
 }
 // The 16-byte vectors of a row between its unaligned ends, and this CTA's share of them.
-struct Span {
-    int head, tail;                          // elements before and after the vectors
-    int v0, v1;                              // vectors [v0, v1) are this CTA's
-    int elems;                               // in all the vectors
+struct __align__(16) Span {
+    int head, elems;                         // elements before the vectors, and in them
+    int v0, nv;                              // vectors [v0, v0 + nv) are this CTA's
 };
 template <class T>
-__device__ __forceinline__ Span span_of(const T* z, int vocab, int rank, int csize) {
+__device__ __forceinline__ Span span_of(const T* z, int vocab, int rank, int shift) {
     constexpr int E = Vec<T>::kElems;
     Span s;
     s.head = static_cast<int>((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / static_cast<int>(sizeof(T));
     s.head = s.head < vocab ? s.head : vocab;
-    const int n = (vocab - s.head) / E, per = (n + csize - 1) / csize;
+    const int n = (vocab - s.head) / E, per = (n + (1 << shift) - 1) >> shift;
     s.elems = n * E;
-    s.tail = vocab - s.head - s.elems;
     s.v0 = min(rank * per, n);
-    s.v1 = min(s.v0 + per, n);
+    s.nv = min(s.v0 + per, n) - s.v0;
     return s;
 }
+// What one thread prepares for all of them, a row ahead.
+struct __align__(16) Row {
+    Span span;
+    float w, adv, old, ref;
+    float zt;                                // the logit at the row's token or label
+    int32_t tok;                             // -1: none
+    int live, pad;
+};
 
 constexpr int64_t kSlotMax = kMaxWarps * 32 * kHeld * 16;    // of a row a CTA: 64 KiB, three slots fit
 constexpr int64_t kRingMax = 208 * 1024;
 
 // HELD: a slot has at most kHeld vectors a thread, and the exponentials of the statistics stay in registers
-// for the gradient; else (rows of more than eight such slots) they are formed again.
-template <int K, class T, bool HELD>
+// for the gradient; else (rows of more than eight such slots) they are formed again.  TWO: a hard term beside
+// tau != 1, so that the sums are kept at two temperatures.
+//
+// A row is a chain of short steps between three barriers, and what every warp does for itself in it is paid
+// sixteen times over: so one thread prepares the row data for all, another one copies, only the warps that
+// hold teacher entries look at them, and whatever comes from memory is asked for a row before it is used.
+template <int K, class T, bool HELD, bool TWO>
 __global__ void __launch_bounds__(kMaxWarps * 32) rows_kernel(const __grid_constant__ RowArgs a) {
     chain_begin();
     constexpr int E = Vec<T>::kElems, P = E / 2;
     constexpr int kKeep = HELD && K != kLogProb ? kHeld : 1;
+    constexpr bool D = K == kDistill;
     extern __shared__ __align__(128) uint8_t slots[];
     __shared__ __align__(8) uint64_t full_bar[kMaxSlots], x_bar[2];
     // by the row's parity: a warp may be a row ahead of one that still reads
+    __shared__ Row row_s[2];
     __shared__ Stat stat_s[2][kMaxWarps], cluster_s[2][kMaxCluster];
-    __shared__ Top top_s[2][K == kDistill ? kMaxWarps : 1];
-    __shared__ float zq_s[K == kDistill ? kMaxWarps : 1];
-    __shared__ int32_t id_s[K == kDistill ? GLR_MAX_TOPK + 1 : 1];
-    __shared__ float q_s[K == kDistill ? GLR_MAX_TOPK + 1 : 1];
-    __shared__ int32_t edge_s[16];
+    __shared__ Top top_s[2][D ? kMaxWarps : 1];
+    __shared__ float zq_s[D ? kMaxWarps : 1];
+    __shared__ int32_t id_s[D ? GLR_MAX_TOPK + 1 : 1];
+    __shared__ float q_s[D ? GLR_MAX_TOPK + 1 : 1];
     __shared__ int abort_flag;
     const int nt = blockDim.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, nw = nt >> 5;
-    const int C = a.cluster, S = a.slots, V = static_cast<int>(a.vocab);
+    const int C = 1 << a.cluster_shift, S = a.slots, V = static_cast<int>(a.vocab);
     uint32_t rank = 0;
     if (C > 1) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-    const int64_t first = blockIdx.x / C, step = gridDim.x / C;
+    const int64_t first = blockIdx.x >> a.cluster_shift, step = gridDim.x >> a.cluster_shift;
     volatile int* abort = &abort_flag;
     if (tid == 0) {
         abort_flag = 0;
@@ -273,17 +297,21 @@ __global__ void __launch_bounds__(kMaxWarps * 32) rows_kernel(const __grid_const
     __syncthreads();
     if (C > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     const bool grad = K != kLogProb && a.dz != nullptr;
+    const float c = a.inv_tau * kLog2e;
+    const uint64_t c2 = pack2(c, c), l2 = pack2(kLog2e, kLog2e);
+    auto logits = [&](int64_t row) { return static_cast<const T*>(a.z) + row * a.ldz; };
 
-    // Thread 0 fills the slots, and writes them back once every thread is done with a row.
+    // The copying thread fills the slots, and writes them back once every thread is done with a row.
+    const bool copier = tid == (nw >> 1) * 32;
     int64_t next = first;
     Side ask{};                                       // the next row to fill: whether it is read
     int fs = 0;
     uint32_t filled = 0, fill_par = 0;                // per slot (bit q): filled at all, parity of the last fill
     auto fill = [&]() {
         if (next >= a.rows) return;
-        const T* z = static_cast<const T*>(a.z) + next * a.ldz;
-        const Span sp = span_of(z, V, rank, C);
-        const uint32_t bytes = is_live<K>(a, ask) ? static_cast<uint32_t>(sp.v1 - sp.v0) * 16u : 0u;
+        const T* z = logits(next);
+        const Span sp = span_of(z, V, rank, a.cluster_shift);
+        const uint32_t bytes = is_live<K>(a, ask) ? static_cast<uint32_t>(sp.nv) * 16u : 0u;
         const uint32_t bar = smem_u32(&full_bar[fs]);
         mbar_expect_tx(bar, bytes);
         if (bytes)
@@ -296,75 +324,97 @@ __global__ void __launch_bounds__(kMaxWarps * 32) rows_kernel(const __grid_const
         next += step;
         if (next < a.rows) ask = side_at<K>(a, next, false);
     };
-    // with a gradient the slot of the row before is filled while this one's is written back (S = 1: its own)
-    if (tid == 0) {
+    // with a gradient the slot of the row before is filled in the middle of this one (S = 1: its own, at the end)
+    if (copier) {
         if (first < a.rows) ask = side_at<K>(a, first, false);
         for (int q = 0; q < (grad && S > 1 ? S - 1 : S); ++q) fill();
     }
+    // The preparing thread: `side` holds the row after the one in progress, the logit at its token is on the way.
+    const bool preparer = tid == (nw - 1) * 32;
+    Side side{};
+    T zt_raw{};
+    auto look_up = [&](int64_t row) {                 // side is that row's: its token's logit
+        const int32_t tok = K != kDistill || a.labels.p ? token_of<K>(a, side) : -1;
+        if (tok >= 0 && is_live<K>(a, side)) zt_raw = logits(row)[tok];
+    };
+    auto prepare = [&](int64_t row, Row& r) {
+        r.span = span_of(logits(row), V, rank, a.cluster_shift);
+        r.w = side.w; r.adv = side.adv; r.old = side.old; r.ref = side.ref;
+        r.tok = K != kDistill || a.labels.p ? token_of<K>(a, side) : -1;
+        r.live = is_live<K>(a, side);
+        r.zt = load(&zt_raw);
+    };
+    Side after{};                                     // and the row after that
+    if (preparer && first < a.rows) {
+        side = side_at<K>(a, first, true);
+        look_up(first);
+        prepare(first, row_s[0]);
+        if (first + step < a.rows) side = side_at<K>(a, first + step, true);
+    }
+    // Teacher entries, 32 kEntries a warp: entry k = warp 32 kEntries + 32 u + lane.
+    const int k0 = warp * 32 * kEntries + lane;
+    const bool entries = D && warp * 32 * kEntries < a.topk;
+    Word id[kEntries];
+    float av[kEntries];                               // bf16 teacher logits as their bits
+    auto ask_entries = [&](int64_t row) {
+#pragma unroll
+        for (int u = 0; u < kEntries; ++u) {
+            const int k = k0 + 32 * u;
+            if (k < a.topk) {
+                id[u] = word_at(a.ids, row * a.ldi + k);
+                const int64_t at = row * a.ldt + k;
+                av[u] = a.teacher_bf16 ? __uint_as_float(static_cast<const uint16_t*>(a.teacher)[at]) : static_cast<const float*>(a.teacher)[at];
+            }
+        }
+    };
+    if (entries && first < a.rows) ask_entries(first);
+    __syncthreads();
 
-    const float c = a.inv_tau * kLog2e;
-    const bool two = K == kDistill && a.labels.p && a.hard != 0.f && a.inv_tau != 1.f;
-    const uint64_t c2 = pack2(c, c), l2 = pack2(kLog2e, kLog2e);
     int s = 0, par = 0;
     uint32_t use = 0, xuse = 0;
-    Side side{};
-    Word id[kEntries];
-    float av[kEntries];                                // bf16 teacher logits as their bits
-    T edge;
-    // Row data of `row`, ahead of their use: everything but what lies in the slot.
-    auto ahead = [&](int64_t row) {
-        side = side_at<K>(a, row, true);
-        if (K == kDistill) {
-#pragma unroll
-            for (int u = 0; u < kEntries; ++u) {
-                const int k = tid + u * nt;
-                if (k < a.topk) {
-                    id[u] = word_at(a.ids, row * a.ldi + k);
-                    const int64_t at = row * a.ldt + k;
-                    av[u] = a.teacher_bf16 ? __uint_as_float(static_cast<const uint16_t*>(a.teacher)[at])
-                                           : static_cast<const float*>(a.teacher)[at];
-                }
-            }
-        }
-        const T* z = static_cast<const T*>(a.z) + row * a.ldz;
-        const Span sp = span_of(z, V, rank, C);
-        // the unaligned ends, an element a thread: the head with the first CTA, the tail with the last
-        if (rank == 0 && tid < sp.head) edge = z[tid];
-        if (rank == C - 1 && tid >= 8 && tid < 8 + sp.tail) edge = z[sp.head + sp.elems + tid - 8];
-    };
-    if (first < a.rows) ahead(first);
     for (int64_t row = first; row < a.rows; row += step) {
-        const T* z = static_cast<const T*>(a.z) + row * a.ldz;
-        T* dz = grad ? static_cast<T*>(a.dz) + row * a.lddz : nullptr;
-        const Span sp = span_of(z, V, rank, C);
-        const int nv = sp.v1 - sp.v0;
-        const bool same = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0;
+        const Row now = row_s[par];
+        const Span sp = now.span;
+        const int nv = sp.nv;
+        bool counts = now.live;
         uint4* slot = reinterpret_cast<uint4*>(slots + static_cast<size_t>(s) * a.slot_bytes);
-        const Side now = side;
-        bool counts = is_live<K>(a, now);
-        const int32_t tok = K != kDistill || a.labels.p ? token_of<K>(a, now) : -1;
+        const bool more = row + step < a.rows;
+        // ---- ask for what comes from memory.  Logits of this row are read here, before any CTA of the cluster
+        // overwrites them (dz may be z)
         int32_t eid[kEntries];
-        float ea[kEntries], ez[kEntries];
-        const bool has_edge = (rank == 0 && tid < sp.head) || (rank == C - 1 && tid >= 8 && tid < 8 + sp.tail);
-        const float e0 = counts && has_edge ? load(&edge) : -CUDART_INF_F;
-        // logits at the listed ids: read here, before any CTA of the cluster overwrites them (dz may be z)
-        float zt = 0.f;
-        if (counts && tok >= 0) zt = load(z + tok);
-        if (K == kDistill) {
+        float ea[kEntries];
+        T ez_raw[kEntries];                           // widened where they are used
+        if (entries) {
+            const T* z = logits(row);
 #pragma unroll
             for (int u = 0; u < kEntries; ++u) {
-                eid[u] = counts && tid + u * nt < a.topk ? index_of(id[u], a.ids.wide, V) : -1;
+                const int k = k0 + 32 * u;
+                eid[u] = counts && k < a.topk ? index_of(id[u], a.ids.wide, V) : -1;
                 ea[u] = eid[u] < 0 ? -CUDART_INF_F : a.teacher_bf16 ? __uint_as_float(__float_as_uint(av[u]) << 16) : av[u];
-                ez[u] = eid[u] >= 0 ? load(z + eid[u]) : 0.f;
+                if (eid[u] >= 0) ez_raw[u] = z[eid[u]];
+                if (k < a.topk) id_s[k] = eid[u];
             }
+            if (more) ask_entries(row + step);
         }
-        if (row + step < a.rows) ahead(row + step);
+        const bool hard = D && counts && now.tok >= 0 && a.hard != 0.f;
+        if (D && tid == 0) id_s[a.topk] = hard ? now.tok : -1;
+        // the unaligned ends, an element a thread: the head with the first CTA, the tail with the last
+        T edge{};
+        int at_end = -1;                              // this thread's element of the ends
+        if (warp == 0) {
+            if (rank == 0 && lane < sp.head) at_end = lane;
+            if (rank == C - 1 && lane >= 8 && lane < 8 + V - sp.head - sp.elems) at_end = sp.head + sp.elems + lane - 8;
+            if (counts && at_end >= 0) edge = logits(row)[at_end];
+        }
+        if (preparer && more) {
+            look_up(row + step);
+            if (row + 2 * step < a.rows) after = side_at<K>(a, row + 2 * step, true);
+        }
 
-        wait(smem_u32(&full_bar[s]), use, abort, a.err);
+        wait(smem_u32(&full_bar[s]), use, false, abort, a.err);
         // ---- statistics
-        Stat st{e0, 0.f, 0.f};
+        Stat st{-CUDART_INF_F, 0.f, 0.f};
         uint64_t kept[kKeep][P];
-        float ref = 0.f;                          // what this thread's exponentials are relative to
         if (counts && HELD) {
             uint4 u[kHeld];
 #pragma unroll
@@ -373,7 +423,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) rows_kernel(const __grid_const
                 u[q] = v < nv ? slot[v] : Vec<T>::none();
                 st.m = fmaxf(st.m, Vec<T>::top(u[q]));
             }
-            ref = st.m == -CUDART_INF_F ? 0.f : st.m;
+            const float ref = st.m == -CUDART_INF_F ? 0.f : st.m;
             const uint64_t nr = pack2(-ref, -ref);
             uint64_t s2[2] = {0, 0}, t2[2] = {0, 0};
 #pragma unroll
@@ -384,21 +434,19 @@ __global__ void __launch_bounds__(kMaxWarps * 32) rows_kernel(const __grid_const
                 for (int i = 0; i < P; ++i) {
                     const uint64_t d = add2(x[i], nr), e = exp2_2(mul2(d, c2));
                     s2[i & 1] = add2(s2[i & 1], e);
-                    if (two) t2[i & 1] = add2(t2[i & 1], exp2_2(mul2(d, l2)));
+                    if (TWO) t2[i & 1] = add2(t2[i & 1], exp2_2(mul2(d, l2)));
                     if (kKeep > 1) kept[q][i] = e;
                 }
             }
             float x, y;
             unpack2(add2(s2[0], s2[1]), x, y);
-            st.s = x + y + exp2_fast((e0 - ref) * c);
-            if (two) {
-                unpack2(add2(t2[0], t2[1]), x, y);
-                st.s1 = x + y + exp2_fast((e0 - ref) * kLog2e);
-            }
+            st.s = x + y;
+            unpack2(add2(t2[0], t2[1]), x, y);
+            st.s1 = x + y;
         } else if (counts) {
             uint64_t s2 = 0, t2 = 0;
             for (int v = tid; v < nv; v += nt) st.m = fmaxf(st.m, Vec<T>::top(slot[v]));
-            ref = st.m == -CUDART_INF_F ? 0.f : st.m;
+            const float ref = st.m == -CUDART_INF_F ? 0.f : st.m;
             const uint64_t nr = pack2(-ref, -ref);
             for (int v = tid; v < nv; v += nt) {
                 uint64_t x[P];
@@ -407,21 +455,26 @@ __global__ void __launch_bounds__(kMaxWarps * 32) rows_kernel(const __grid_const
                 for (int i = 0; i < P; ++i) {
                     const uint64_t d = add2(x[i], nr);
                     s2 = add2(s2, exp2_2(mul2(d, c2)));
-                    if (two) t2 = add2(t2, exp2_2(mul2(d, l2)));
+                    if (TWO) t2 = add2(t2, exp2_2(mul2(d, l2)));
                 }
             }
             float x, y;
             unpack2(s2, x, y);
-            st.s = x + y + exp2_fast((e0 - ref) * c);
-            if (two) {
-                unpack2(t2, x, y);
-                st.s1 = x + y + exp2_fast((e0 - ref) * kLog2e);
-            }
+            st.s = x + y;
+            unpack2(t2, x, y);
+            st.s1 = x + y;
         }
-        const float m_own = st.m;
-        st = warp_merge(st, c, two);
+        const float m_own = st.m;                     // what this thread's exponentials are relative to
+        const float e0 = load(&edge);
+        if (warp == 0 && counts && at_end >= 0) {     // one more element
+            const float m = fmaxf(st.m, e0), r = m == -CUDART_INF_F ? 0.f : m;
+            st.s = st.s * shrink(st.m, m, c) + exp2_fast((e0 - r) * c);
+            if (TWO) st.s1 = st.s1 * shrink(st.m, m, kLog2e) + exp2_fast((e0 - r) * kLog2e);
+            st.m = m;
+        }
+        st = warp_merge<TWO>(st, c);
         Top tp{-CUDART_INF_F, 0.f, 0.f};
-        if (K == kDistill && warp * 32 < a.topk) {
+        if (entries) {
 #pragma unroll
             for (int u = 0; u < kEntries; ++u) tp.m = fmaxf(tp.m, ea[u]);
 #pragma unroll
@@ -433,81 +486,76 @@ __global__ void __launch_bounds__(kMaxWarps * 32) rows_kernel(const __grid_const
                 }
             tp = warp_merge(tp, c);
         }
-        if (nw > 1) {
-            if (lane == 0) {
-                stat_s[par][warp] = st;
-                if (K == kDistill) top_s[par][warp] = tp;
-            }
-            __syncthreads();
+        if (lane == 0) {
+            stat_s[par][warp] = st;
+            if (entries) top_s[par][warp] = tp;
         }
-        if (nw > 1) {
-            st = warp_merge(lane < nw ? stat_s[par][lane] : Stat{-CUDART_INF_F, 0.f, 0.f}, c, two);
-            if (K == kDistill && a.topk > 32) tp = warp_merge(lane < nw ? top_s[par][lane] : Top{-CUDART_INF_F, 0.f, 0.f}, c);
-            else if (K == kDistill) tp = top_s[par][0];
+        __syncthreads();
+        if (copier && grad && S > 1) {                 // the slot of the row before has been written back by now
+            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            fill();
+        }
+        if (nw > 1) st = warp_merge<TWO>(lane < nw ? stat_s[par][lane] : Stat{-CUDART_INF_F, 0.f, 0.f}, c);
+        if (C > 1 && warp == 0 && lane < C) {
+            const uint32_t to = peer_addr(smem_u32(&cluster_s[par][rank]), lane);
+            asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0+4], %2;\n\tst.shared::cluster.f32 [%0+8], %3;"
+                         ::"r"(to), "f"(st.m), "f"(st.s), "f"(st.s1) : "memory");
+            asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(peer_addr(smem_u32(&x_bar[par]), lane)) : "memory");
+        }
+        // ---- while the peers' sums come in: the teacher's sums, and whether an id is listed twice
+        const int top = a.topk, n = D && counts ? top + 1 : 0;
+        bool twice = false;
+        if (D && counts) {
+            if (top > 32 * kEntries) tp = warp_merge(lane * 32 * kEntries < top ? top_s[par][lane & (kMaxWarps - 1)] : Top{-CUDART_INF_F, 0.f, 0.f}, c);
+            else if (top > 0) tp = top_s[par][0];
+            if (grad) {
+                // entry k against the earlier ones: 2^dup_shift threads an entry
+                const int parts = 1 << a.dup_shift;
+                for (int k = tid >> a.dup_shift; k < n; k += nt >> a.dup_shift) {
+                    const int32_t v = id_s[k];
+                    for (int j = tid & (parts - 1); j < k; j += parts) twice |= id_s[j] == v && v >= 0;
+                }
+            }
         }
         if (C > 1) {
-            if (warp == 0 && lane < C) {
-                const uint32_t to = peer_addr(smem_u32(&cluster_s[par][rank]), lane);
-                asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0+4], %2;\n\tst.shared::cluster.f32 [%0+8], %3;"
-                             ::"r"(to), "f"(st.m), "f"(st.s), "f"(st.s1) : "memory");
-                asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(peer_addr(smem_u32(&x_bar[par]), lane)) : "memory");
-            }
-            wait(smem_u32(&x_bar[par]), xuse, abort, a.err);
-            st = warp_merge(lane < C ? cluster_s[par][lane] : Stat{-CUDART_INF_F, 0.f, 0.f}, c, two);
+            wait(smem_u32(&x_bar[par]), xuse, true, abort, a.err);
+            st = warp_merge<TWO>(lane < C ? cluster_s[par][lane] : Stat{-CUDART_INF_F, 0.f, 0.f}, c);
         }
         if (st.s == 0.f) counts = false;
-        if (!two) st.s1 = st.s;
+        if (!TWO) st.s1 = st.s;
 
         // ---- the row's loss and the factors of its gradient: dense exp2((z - m) c) + dense1 exp2((z - m) log2 e),
         // less what is listed at single ids
-        const float ln_s = logf(st.s);
-        float dense = 0.f, dense1 = 0.f, at_tok = 0.f;
-        int n = 0, top = 0;                        // listed entries; the label is the last, past `top` teacher's
+        const float inv_s = __fdividef(1.f, st.s), zt = now.zt;
+        float dense = 0.f, dense1 = 0.f, at_tok = 0.f, q[kEntries] = {};
         if (K == kDistill) {
-            const bool soft = counts && tp.s != 0.f, hard = counts && tok >= 0 && a.hard != 0.f;
-            const float f = now.w * a.soft * a.inv_tau;
-            if (soft) { dense = f / st.s; n = top = a.topk; }
-            const float inv = 1.f / tp.s;
-            float zq = 0.f;
-#pragma unroll
-            for (int u = 0; u < kEntries; ++u) {
-                const int k = tid + u * nt;
-                if (k < n) {
-                    const float e = ea[u] == -CUDART_INF_F ? 0.f : exp2_fast((ea[u] - tp.m) * c) * inv;
-                    id_s[k] = eid[u];
-                    q_s[k] = f * e;
-                    if (e != 0.f) zq += e * (ez[u] - st.m);
-                }
-            }
-            if (warp * 32 < a.topk) {
-#pragma unroll
-                for (int d = 16; d; d >>= 1) zq += __shfl_xor_sync(~0u, zq, d);
-            }
-            if (lane == 0) zq_s[warp] = zq;
-            if (hard) {
+            const bool soft = counts && tp.s != 0.f;
+            const float f = now.w * a.soft * a.inv_tau, inv = 1.f / tp.s;
+            if (soft) dense = f * inv_s;
+            if (hard && counts) {
                 at_tok = now.w * a.hard;
                 dense1 = at_tok / st.s1;
-                if (tid == 0) { id_s[n] = tok; q_s[n] = at_tok; }
-                ++n;
-                if (!two) { dense += dense1; dense1 = 0.f; }
+                if (!TWO) { dense += dense1; dense1 = 0.f; }
             }
-            __syncthreads();
-            if (tid == 0 && rank == 0) {
-                float loss = 0.f;
-                if (soft) {
-                    float z_sum = 0.f;
-                    for (int w = 0; w < nw && w * 32 < a.topk; ++w) z_sum += zq_s[w];
-                    loss = a.soft * ((tp.a * inv * a.inv_tau - logf(tp.s)) - (z_sum * a.inv_tau - ln_s));
+            if (entries) {
+                float zq = 0.f;
+#pragma unroll
+                for (int u = 0; u < kEntries; ++u) {
+                    const float e = !soft || ea[u] == -CUDART_INF_F ? 0.f : exp2_fast((ea[u] - tp.m) * c) * inv;
+                    q[u] = f * e;
+                    if (k0 + 32 * u < top) q_s[k0 + 32 * u] = q[u];
+                    if (e != 0.f) zq += e * (load(&ez_raw[u]) - st.m);
                 }
-                if (hard) loss += a.hard * (logf(st.s1) - (zt - st.m));
-                a.row_loss[row] = loss;
+                zq = warp_sum(zq);
+                if (lane == 0) zq_s[warp] = zq;
             }
+            if (tid == 0) q_s[top] = at_tok;
         } else {
-            const float lp = counts ? (zt - st.m) * a.inv_tau - ln_s : 0.f;
+            const float lp = counts ? (zt - st.m) * a.inv_tau - log_fast(st.s) : 0.f;
             if (K == kPolicy) {
                 float loss = 0.f, slope = 0.f;
                 if (counts) {
-                    const float A = now.adv, ratio = expf(lp - now.old);
+                    const float A = now.adv, ratio = exp2_fast((lp - now.old) * kLog2e);
                     loss = -fminf(ratio * A, fminf(fmaxf(ratio, a.clip_lo), a.clip_hi) * A);
                     if (isnan(ratio * A)) loss = ratio * A;
                     slope = (A > 0.f ? ratio > a.clip_hi : ratio < a.clip_lo) ? 0.f : -A * ratio;
@@ -518,42 +566,50 @@ __global__ void __launch_bounds__(kMaxWarps * 32) rows_kernel(const __grid_const
                     }
                 }
                 at_tok = -slope * now.w * a.inv_tau;
-                dense = counts ? at_tok / st.s : 0.f;
+                dense = counts ? at_tok * inv_s : 0.f;
                 if (tid == 0 && rank == 0) { a.row_loss[row] = loss; a.logp[row] = lp; }
             } else if (tid == 0 && rank == 0) {
                 a.logp[row] = lp;
-                a.lse[row] = counts ? st.m + ln_s : CUDART_INF_F;
+                a.lse[row] = counts ? st.m + log_fast(st.s) : CUDART_INF_F;
                 a.coef[row] = 0.f;
             }
         }
 
         // ---- the gradient, over the logits
+        T* mine = reinterpret_cast<T*>(slot);
+        auto at = [&](float x) {
+            const float d = x - st.m;
+            float g = dense * exp2_fast(d * c);
+            if (TWO) g += dense1 * exp2_fast(d * kLog2e);
+            return g;
+        };
+        // the place of an id in this CTA's part of the row, or negative
+        auto place = [&](int32_t v) {
+            const int b = v - sp.head - sp.v0 * E;
+            return b < nv * E ? b : -1;
+        };
+        auto row_of = [&]() { return static_cast<T*>(a.dz) + row * a.lddz; };
+        auto is_end = [&](int32_t v) { return (rank == 0 && v < sp.head) || (rank == C - 1 && v >= sp.head + sp.elems); };
         if (grad) {
-            auto at = [&](float x) {
-                const float d = x - st.m;
-                float g = dense * exp2_fast(d * c);
-                if (two) g += dense1 * exp2_fast(d * kLog2e);
-                return g;
-            };
-            const uint64_t nm = pack2(-st.m, -st.m), dd = pack2(dense, dense), dd1 = pack2(dense1, dense1);
             if (counts && HELD) {
                 const float f = dense * shrink(m_own, st.m, c);
-                const uint64_t ff = pack2(f, f);
+                const uint64_t ff = pack2(f, f), nm = pack2(-st.m, -st.m), dd1 = pack2(dense1, dense1);
 #pragma unroll
-                for (int q = 0; q < kKeep; ++q) {
-                    const int v = tid + q * nt;
+                for (int j = 0; j < kKeep; ++j) {
+                    const int v = tid + j * nt;
                     if (v < nv) {
                         uint64_t x[P];
-                        if (two) Vec<T>::get(slot[v], x);
+                        if (TWO) Vec<T>::get(slot[v], x);
 #pragma unroll
                         for (int i = 0; i < P; ++i) {
-                            const uint64_t g = mul2(ff, kept[q][i]);
-                            x[i] = two ? fma2(dd1, exp2_2(mul2(add2(x[i], nm), l2)), g) : g;
+                            const uint64_t g = mul2(ff, kept[j][i]);
+                            x[i] = TWO ? fma2(dd1, exp2_2(mul2(add2(x[i], nm), l2)), g) : g;
                         }
                         slot[v] = Vec<T>::put(x);
                     }
                 }
             } else if (counts) {
+                const uint64_t nm = pack2(-st.m, -st.m), dd = pack2(dense, dense), dd1 = pack2(dense1, dense1);
                 for (int v = tid; v < nv; v += nt) {
                     uint64_t x[P];
                     Vec<T>::get(slot[v], x);
@@ -561,101 +617,94 @@ __global__ void __launch_bounds__(kMaxWarps * 32) rows_kernel(const __grid_const
                     for (int i = 0; i < P; ++i) {
                         const uint64_t d = add2(x[i], nm);
                         x[i] = mul2(dd, exp2_2(mul2(d, c2)));
-                        if (two) x[i] = fma2(dd1, exp2_2(mul2(d, l2)), x[i]);
+                        if (TWO) x[i] = fma2(dd1, exp2_2(mul2(d, l2)), x[i]);
                     }
                     slot[v] = Vec<T>::put(x);
                 }
             } else {
                 for (int v = tid; v < nv; v += nt) slot[v] = make_uint4(0, 0, 0, 0);
             }
-            if (rank == 0 && tid < sp.head) store(dz + tid, counts ? at(e0) : 0.f);
-            if (rank == C - 1 && tid >= 8 && tid < 8 + sp.tail) store(dz + sp.head + sp.elems + tid - 8, counts ? at(e0) : 0.f);
-            // where an id lies: in this CTA's part of the slot, at an end that this CTA writes, or elsewhere
-            T* mine = reinterpret_cast<T*>(slot);
-            auto place = [&](int32_t v, int& in_slot, int& at_edge) {
-                const int b = v - sp.head - sp.v0 * E;
-                in_slot = v >= sp.head && b >= 0 && b < nv * E ? b : -1;
-                at_edge = rank == 0 && v < sp.head ? v : rank == C - 1 && v >= sp.head + sp.elems ? 8 + v - sp.head - sp.elems : -1;
-            };
-            if (K == kPolicy && counts) {
-                int b, e;
-                place(tok, b, e);
-                if (b >= 0 && tid == (b / E) % nt) store(mine + b, at(zt) - at_tok);
-                if (e >= 0 && tid == e) store(dz + tok, at(zt) - at_tok);
+            if (at_end >= 0) {
+                float g = counts ? at(e0) : 0.f;
+                if (K == kPolicy && counts && at_end == now.tok) g -= at_tok;
+                store(row_of() + at_end, g);
             }
-            if (K == kDistill && n > 0) {
-                // each listed entry marks its place; where all find their own mark no id is listed twice
-                __syncthreads();
-                int b[kEntries + 1], e[kEntries + 1], who[kEntries + 1];
-                float zz[kEntries + 1];
+            if (K == kPolicy && counts) {              // by the thread that wrote the token's vector
+                const int b = place(now.tok);
+                int v = b / E;
+                if (HELD) {
 #pragma unroll
-                for (int u = 0; u <= kEntries; ++u) {
-                    const bool is_tok = u == kEntries;
-                    const int k = is_tok ? (tid == 0 ? top : n) : tid + u * nt;
-                    who[u] = -1;
-                    b[u] = e[u] = -1;
-                    zz[u] = is_tok ? zt : ez[u < kEntries ? u : 0];
-                    if (is_tok ? k < n : k < top) {
-                        const int32_t v = id_s[k];
-                        if (v >= 0) {
-                            place(v, b[u], e[u]);
-                            if (b[u] >= 0 || e[u] >= 0) who[u] = k;
-                            if (b[u] >= 0) *reinterpret_cast<uint16_t*>(mine + b[u]) = static_cast<uint16_t>(k);
-                            if (e[u] >= 0) edge_s[e[u]] = k;
-                        }
-                    }
+                    for (int j = 1; j < kHeld; ++j) v -= v >= nt ? nt : 0;
+                } else {
+                    v %= nt;
                 }
-                __syncthreads();
-                bool twice = false;
-#pragma unroll
-                for (int u = 0; u <= kEntries; ++u) {
-                    if (b[u] >= 0) twice |= *reinterpret_cast<const uint16_t*>(mine + b[u]) != who[u];
-                    if (e[u] >= 0) twice |= edge_s[e[u]] != who[u];
+                if (b >= 0 && v == tid) store(mine + b, at(zt) - at_tok);
+            }
+        }
+        if (K == kDistill) {
+            // every thread's part of the gradient is written before single entries are: the slot's, and the ends'
+            twice = __syncthreads_or(twice);
+            if (tid == 0 && rank == 0) {
+                float loss = 0.f;
+                if (counts && tp.s != 0.f) {
+                    float z_sum = 0.f;
+                    for (int w = 0; w * 32 * kEntries < top; ++w) z_sum += zq_s[w];
+                    loss = a.soft * ((tp.a / tp.s * a.inv_tau - log_fast(tp.s)) - (z_sum * a.inv_tau - log_fast(st.s)));
                 }
-                twice = __syncthreads_or(twice);
-#pragma unroll
-                for (int u = 0; u <= kEntries; ++u) {
-                    if (who[u] < 0) continue;
-                    float g = q_s[who[u]];
+                if (hard && counts) loss += a.hard * (log_fast(st.s1) - (zt - st.m));
+                a.row_loss[row] = loss;
+            }
+            if (grad && counts && (entries || tid == 0)) {
+                auto single = [&](int32_t v, float g, float z) {
+                    if (v < 0) return;
+                    const int b = place(v);
+                    if (b < 0 && !is_end(v)) return;
                     if (twice) {
                         g = 0.f;
-                        const int32_t v = id_s[who[u]];
                         for (int j = 0; j < n; ++j) g += id_s[j] == v ? q_s[j] : 0.f;
                     }
-                    if (b[u] >= 0) store(mine + b[u], at(zz[u]) - g);
-                    else store(dz + id_s[who[u]], at(zz[u]) - g);
+                    store(b >= 0 ? mine + b : row_of() + v, at(z) - g);
+                };
+                if (entries) {
+#pragma unroll
+                    for (int u = 0; u < kEntries; ++u) single(eid[u], q[u], load(&ez_raw[u]));
                 }
+                if (tid == 0 && hard) single(now.tok, at_tok, zt);
             }
-            if (!same) {
-                // the gradient's rows lie otherwise on 16 bytes than the logits': element by element
-                __syncthreads();
-                T* to = dz + sp.head + static_cast<int64_t>(sp.v0) * E;
-                for (int q = tid; q < nv * E; q += nt) to[q] = mine[q];
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+        const bool same = grad && ((reinterpret_cast<uintptr_t>(logits(row)) ^ reinterpret_cast<uintptr_t>(row_of())) & 15) == 0;
+        if (grad && !same) {
+            // the gradient's rows lie otherwise on 16 bytes than the logits': element by element
+            __syncthreads();
+            T* to = row_of() + sp.head + static_cast<int64_t>(sp.v0) * E;
+            for (int j = tid; j < nv * E; j += nt) to[j] = mine[j];
+        }
+        if (preparer && more) {
+            prepare(row + step, row_s[par ^ 1]);
+            side = after;
         }
         __syncthreads();
-        if (tid == 0) {
+        if (copier) {
             if (grad) {
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    // all threads' writes, before the copy reads them
                 if (nv > 0 && same)
                     asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
-                                 ::"l"(dz + sp.head + static_cast<int64_t>(sp.v0) * E), "r"(smem_u32(slot)), "r"(static_cast<uint32_t>(nv) * 16u) : "memory");
+                                 ::"l"(row_of() + sp.head + static_cast<int64_t>(sp.v0) * E), "r"(smem_u32(slot)), "r"(static_cast<uint32_t>(nv) * 16u) : "memory");
                 asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                if (S > 1) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-                else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                if (S == 1) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
             }
-            fill();
+            if (!grad || S == 1) fill();
         }
         if (++s == S) { s = 0; use ^= 1u; }
         if (par) xuse ^= 1u;
         par ^= 1;
     }
-    if (tid == 0) {
+    if (copier) {
         if (grad) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         if (*abort)                                   // let the copies already issued land
             for (int q = 0; q < S; ++q)
                 if (filled >> q & 1u)
-                    for (int it = 0; it < 4000000 && !try_wait(smem_u32(&full_bar[q]), fill_par >> q & 1u); ++it) __nanosleep(64);
+                    for (int it = 0; it < 4000000 && !try_wait(smem_u32(&full_bar[q]), fill_par >> q & 1u, false); ++it) __nanosleep(64);
     }
     // no CTA of a cluster leaves while another may still write to its shared memory
     if (C > 1) {
@@ -777,17 +826,27 @@ cudaError_t rows_launch(RowArgs a, int dtype, cudaStream_t st) {
     while (C < kMaxCluster && (vecs + C - 1) / C * 16 > kSlotMax) C *= 2;
     // few rows: more CTAs a row, as long as each has 4 KiB of it
     while (C < kMaxCluster && a.rows * C * 2 <= sms && row_bytes / (2 * C) >= 4096) C *= 2;
-    a.cluster = C;
+    a.cluster_shift = C == 1 ? 0 : C == 2 ? 1 : C == 4 ? 2 : 3;
     a.slot_bytes = static_cast<uint32_t>((vecs + C - 1) / C * 16);
     a.slots = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(3, kRingMax / a.slot_bytes)));
     const size_t smem = static_cast<size_t>(a.slots) * a.slot_bytes;
     const bool held = a.slot_bytes <= kSlotMax;
     int warps = held ? static_cast<int>((a.slot_bytes / 16 + 32 * kHeld - 1) / (32 * kHeld)) : kMaxWarps;
-    if (K == kDistill) warps = std::max(warps, (a.topk + 32 * kEntries - 1) / (32 * kEntries));
+    if (K == kDistill) {
+        warps = std::max(warps, (a.topk + 32 * kEntries - 1) / (32 * kEntries));
+        a.dup_shift = 0;                          // threads an entry in the search for ids listed twice
+        while ((a.topk + 1) << (a.dup_shift + 1) <= warps * 32) ++a.dup_shift;
+    }
     const int per_sm = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({16, kRingMax / static_cast<int64_t>(smem + 1024), 16 / warps})));
     const int64_t groups = std::min<int64_t>(a.rows, std::max<int64_t>(1, static_cast<int64_t>(sms) * per_sm / C));
-    auto kernel = dtype == GLR_BF16 ? (held ? rows_kernel<K, __nv_bfloat16, true> : rows_kernel<K, __nv_bfloat16, false>)
-                                    : (held ? rows_kernel<K, float, true> : rows_kernel<K, float, false>);
+    const bool two = K == kDistill && a.labels.p && a.hard != 0.f && a.inv_tau != 1.f;
+    auto pick = [&](auto t) {
+        using T = decltype(t);
+        constexpr bool D = K == kDistill;
+        return held ? (two ? rows_kernel<K, T, true, D> : rows_kernel<K, T, true, false>)
+                    : (two ? rows_kernel<K, T, false, D> : rows_kernel<K, T, false, false>);
+    };
+    auto kernel = dtype == GLR_BF16 ? pick(__nv_bfloat16()) : pick(float());
     if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kRingMax))) != cudaSuccess) return e;
     cudaLaunchAttribute attr[2]{};
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
