@@ -8,9 +8,9 @@
 //
 // The rows kernel reads a row once and writes its gradient once.  A row, or with a cluster of C CTAs a
 // C-th of it, lies in a slot of shared memory: filled by a bulk copy while earlier rows are worked on,
-// reduced by all warps, overwritten by its own gradient and written back by a bulk copy.  The
-// CTAs of a cluster exchange (m, s) over distributed shared memory.  So it is bound by HBM as long as a
-// row's arithmetic (two exponentials and about eight instructions a logit) is shorter than its copies.
+// reduced by the worker warps, overwritten by its own gradient and written back by a bulk copy.  The
+// CTAs of a cluster exchange (m, s) over distributed shared memory.  A service warp does everything else,
+// rows ahead or behind the workers: row data, copies, teacher entries, losses, single entries.
 #include <math_constants.h>
 
 #include <algorithm>
@@ -77,6 +77,13 @@ __device__ __forceinline__ uint64_t exp2_2(uint64_t v) {
 template <class T> struct Vec;
 template <> struct Vec<__nv_bfloat16> {
     static constexpr int kElems = 8;
+    using Mark = uint16_t;
+    static __device__ __forceinline__ void scatter(__nv_bfloat16* p, const uint4& u) {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        uint16_t* h = reinterpret_cast<uint16_t*>(p);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) { h[2 * q] = static_cast<uint16_t>(w[q]); h[2 * q + 1] = static_cast<uint16_t>(w[q] >> 16); }
+    }
     static __device__ __forceinline__ uint4 none() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
     static __device__ __forceinline__ void get(const uint4& u, uint64_t (&v)[4]) {
         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
@@ -102,6 +109,10 @@ template <> struct Vec<__nv_bfloat16> {
 };
 template <> struct Vec<float> {
     static constexpr int kElems = 4;
+    using Mark = uint32_t;
+    static __device__ __forceinline__ void scatter(float* p, const uint4& u) {
+        p[0] = __uint_as_float(u.x); p[1] = __uint_as_float(u.y); p[2] = __uint_as_float(u.z); p[3] = __uint_as_float(u.w);
+    }
     static __device__ __forceinline__ uint4 none() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
     static __device__ __forceinline__ void get(const uint4& u, uint64_t (&v)[2]) {
         v[0] = pack2(__uint_as_float(u.x), __uint_as_float(u.y));
@@ -140,7 +151,7 @@ __device__ __forceinline__ float warp_sum(float x) {
 // and their sum.  A NaN does not show in a maximum; it stays in the sums.
 template <bool TWO>
 __device__ __forceinline__ Stat warp_merge(Stat x, float c) {
-    Stat r;
+    Stat r{};
     r.m = warp_max(x.m);
     r.s = warp_sum(x.s * shrink(x.m, r.m, c));
     r.s1 = TWO ? warp_sum(x.s1 * shrink(x.m, r.m, kLog2e)) : 0.f;
@@ -155,11 +166,10 @@ __device__ __forceinline__ Top warp_merge(Top x, float c) {
     return r;
 }
 
-constexpr int kMaxWarps = 16;
-constexpr int kMaxSlots = 4;
+constexpr int kWorkers = 15;                // warps on a row at most; one more is the service warp
+constexpr int kMaxSlots = 3;
 constexpr int kMaxCluster = 8;
-constexpr int kEntries = 2;                 // teacher entries a thread: topk <= 2 x threads
-constexpr int kHeld = 8;                    // 16-byte vectors of a slot whose exponentials a thread keeps in registers
+constexpr int kHeld = 9;                    // 16-byte vectors of a slot whose exponentials a thread keeps in registers
 
 // `peers`: what other CTAs of the cluster wrote before they arrived is to be seen.
 __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity, bool peers) {
@@ -189,8 +199,8 @@ __device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
-// What a row needs beside its logits.  It is loaded a row ahead and looked at only then: an index stays as its
-// two words, and nothing is compared or converted on the way, which would wait for memory.
+// What a row needs beside its logits.  It is asked for well before it is looked at: an index stays as its two
+// words, and nothing is compared or converted on the way, which would wait for memory.
 struct Word { int32_t lo, hi; };
 __device__ __forceinline__ Word word_at(const Index& x, int64_t i) {
     if (x.wide) {
@@ -208,13 +218,13 @@ struct Side {
     Word tok;
 };
 template <int K>
-__device__ __forceinline__ Side side_at(const RowArgs& a, int64_t row, bool full) {
+__device__ __forceinline__ Side side_at(const RowArgs& a, int64_t row) {
     Side s{};
     s.w = K == kLogProb ? 1.f : a.weight ? a.weight[row] : a.share;
     s.tok = {-1, 0};
     if (K != kDistill) s.tok = word_at(a.tokens, row);
-    else if (a.labels.p && full) s.tok = word_at(a.labels, row);
-    if (K == kPolicy && full) {
+    else if (a.labels.p) s.tok = word_at(a.labels, row);
+    if (K == kPolicy) {
         s.adv = a.advantage[row];
         s.old = a.old_logp[row];
         if (a.ref_logp) s.ref = a.ref_logp[row];
@@ -246,42 +256,85 @@ __device__ __forceinline__ Span span_of(const T* z, int vocab, int rank, int shi
     s.nv = min(s.v0 + per, n) - s.v0;
     return s;
 }
-// What one thread prepares for all of them, a row ahead.
+// A row's data, prepared three rows ahead.
 struct __align__(16) Row {
     Span span;
     float w, adv, old, ref;
-    float zt;                                // the logit at the row's token or label
-    int32_t tok;                             // -1: none
-    int live, pad;
+    int32_t tok;                             // the row's token or label, -1: none
+    int live, same, pad;                     // same: logits and gradient lie alike on 16 bytes
 };
+// What the workers need of a row beside its sums: the logit at its token, and whether the teacher has entries.
+struct Pub { float zt; int soft; };
+// A row's loss and the factors of its gradient: dense exp2((z - m) c) + dense1 exp2((z - m) log2 e), less at_tok at
+// the token (distillation: and what the teacher's entries take).
+struct Coef { float dense, dense1, at_tok, loss, lp; };
 
-constexpr int64_t kSlotMax = kMaxWarps * 32 * kHeld * 16;    // of a row a CTA: 64 KiB, three slots fit
-constexpr int64_t kRingMax = 208 * 1024;
+template <int K, bool TWO>
+__device__ __forceinline__ Coef coef_of(const RowArgs& a, const Row& r, const Stat& st, const Pub& pub, bool counts) {
+    Coef k{};
+    if (K == kDistill) {
+        if (counts && pub.soft) k.dense = r.w * a.soft * a.inv_tau * __fdividef(1.f, st.s);
+        if (counts && r.tok >= 0 && a.hard != 0.f) {
+            k.at_tok = r.w * a.hard;
+            k.dense1 = k.at_tok * __fdividef(1.f, st.s1);
+            if (!TWO) { k.dense += k.dense1; k.dense1 = 0.f; }
+        }
+        return k;
+    }
+    if (!counts) return k;
+    k.lp = (pub.zt - st.m) * a.inv_tau - log_fast(st.s);
+    if (K == kPolicy) {
+        const float A = r.adv, ratio = exp2_fast((k.lp - r.old) * kLog2e);
+        k.loss = -fminf(ratio * A, fminf(fmaxf(ratio, a.clip_lo), a.clip_hi) * A);
+        if (isnan(ratio * A)) k.loss = ratio * A;
+        float slope = (A > 0.f ? ratio > a.clip_hi : ratio < a.clip_lo) ? 0.f : -A * ratio;
+        if (a.ref_logp) {
+            const float e = expm1f(r.ref - k.lp);
+            k.loss += a.kl * (e - (r.ref - k.lp));
+            slope -= a.kl * e;
+        }
+        k.at_tok = -slope * r.w * a.inv_tau;
+        k.dense = k.at_tok * __fdividef(1.f, st.s);
+    }
+    return k;
+}
 
-// HELD: a slot has at most kHeld vectors a thread, and the exponentials of the statistics stay in registers
-// for the gradient; else (rows of more than eight such slots) they are formed again.  TWO: a hard term beside
-// tau != 1, so that the sums are kept at two temperatures.
+constexpr int64_t kSlotMax = kWorkers * 32 * kHeld * 16;     // of a row a CTA: 67.5 KiB, three slots fit
+constexpr int64_t kRingMax = 196 * 1024;
+
+// HELD: a slot has at most kHeld vectors a worker thread, and the exponentials of the statistics stay in
+// registers for the gradient; else (rows of more than eight such slots) they are formed again.  TWO: a hard
+// term beside tau != 1, so that the sums are kept at two temperatures.
 //
-// A row is a chain of short steps between three barriers, and what every warp does for itself in it is paid
-// sixteen times over: so one thread prepares the row data for all, another one copies, only the warps that
-// hold teacher entries look at them, and whatever comes from memory is asked for a row before it is used.
+// A worker's row is: wait for the slot, sums, one barrier, the merge of all warps' sums (and of the cluster's
+// CTAs), the gradient into the slot.  What each of up to fifteen warps would do for itself is paid that many
+// times over, and a load's latency in this chain is lost to all of them, so the service warp does the rest:
+//   1 the teacher's softmax, the ends' sums and the token's logit of row i, before the workers' barrier
+//   2 the fill of a slot whose row has been written back
+//   3 the loads of row i + 1's entries and logits, and the data of row i + 3
+//   4 the loss of row i, once its sums are there
+//   5 single entries of row i's gradient, once the workers have written theirs, and its write-back
 template <int K, class T, bool HELD, bool TWO>
-__global__ void __launch_bounds__(kMaxWarps * 32) rows_kernel(const __grid_constant__ RowArgs a) {
+__global__ void __launch_bounds__((kWorkers + 1) * 32) rows_kernel(const __grid_constant__ RowArgs a) {
     chain_begin();
     constexpr int E = Vec<T>::kElems, P = E / 2;
     constexpr int kKeep = HELD && K != kLogProb ? kHeld : 1;
     constexpr bool D = K == kDistill;
+    constexpr int kList = D ? GLR_MAX_TOPK + 1 : 1;   // entries subtracted at single ids; the token is the last
     extern __shared__ __align__(128) uint8_t slots[];
-    __shared__ __align__(8) uint64_t full_bar[kMaxSlots], x_bar[2];
-    // by the row's parity: a warp may be a row ahead of one that still reads
-    __shared__ Row row_s[2];
-    __shared__ Stat stat_s[2][kMaxWarps], cluster_s[2][kMaxCluster];
-    __shared__ Top top_s[2][D ? kMaxWarps : 1];
-    __shared__ float zq_s[D ? kMaxWarps : 1];
-    __shared__ int32_t id_s[D ? GLR_MAX_TOPK + 1 : 1];
-    __shared__ float q_s[D ? GLR_MAX_TOPK + 1 : 1];
+    __shared__ __align__(8) uint64_t full_bar[kMaxSlots], x_bar[2], fin_bar, dense_bar;
+    // by the row's parity, or (row_s) its number modulo four: who writes them again has passed a barrier that
+    // all readers have reached
+    __shared__ Row row_s[4];
+    __shared__ Stat stat_s[2][kWorkers + 1], fin_s[2];
+    __shared__ __align__(16) float4 cluster_s[2][kMaxCluster];
+    __shared__ Pub pub_s[2];
+    __shared__ float end_s[2][16], zt_s[2];
+    __shared__ int32_t id_s[2][kList];
+    __shared__ float a_s[2][kList], z_s[2][kList], q_s[kList];
+    __shared__ int32_t mark_s[16];
     __shared__ int abort_flag;
-    const int nt = blockDim.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, nw = nt >> 5;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, nw = (blockDim.x >> 5) - 1, nt = nw * 32;
     const int C = 1 << a.cluster_shift, S = a.slots, V = static_cast<int>(a.vocab);
     uint32_t rank = 0;
     if (C > 1) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -290,421 +343,383 @@ __global__ void __launch_bounds__(kMaxWarps * 32) rows_kernel(const __grid_const
     if (tid == 0) {
         abort_flag = 0;
         for (int q = 0; q < S; ++q) mbar_init(smem_u32(&full_bar[q]), 1);
-        mbar_init(smem_u32(&x_bar[0]), C);
-        mbar_init(smem_u32(&x_bar[1]), C);
+        mbar_init(smem_u32(&x_bar[0]), 1);
+        mbar_init(smem_u32(&x_bar[1]), 1);
+        mbar_init(smem_u32(&fin_bar), 1);
+        mbar_init(smem_u32(&dense_bar), nw);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    __syncthreads();
-    if (C > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     const bool grad = K != kLogProb && a.dz != nullptr;
     const float c = a.inv_tau * kLog2e;
     const uint64_t c2 = pack2(c, c), l2 = pack2(kLog2e, kLog2e);
     auto logits = [&](int64_t row) { return static_cast<const T*>(a.z) + row * a.ldz; };
-
-    // The copying thread fills the slots, and writes them back once every thread is done with a row.
-    const bool copier = tid == (nw >> 1) * 32;
-    int64_t next = first;
-    Side ask{};                                       // the next row to fill: whether it is read
-    int fs = 0;
-    uint32_t filled = 0, fill_par = 0;                // per slot (bit q): filled at all, parity of the last fill
-    auto fill = [&]() {
-        if (next >= a.rows) return;
-        const T* z = logits(next);
-        const Span sp = span_of(z, V, rank, a.cluster_shift);
-        const uint32_t bytes = is_live<K>(a, ask) ? static_cast<uint32_t>(sp.nv) * 16u : 0u;
-        const uint32_t bar = smem_u32(&full_bar[fs]);
-        mbar_expect_tx(bar, bytes);
-        if (bytes)
-            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                         ::"r"(smem_u32(slots + static_cast<size_t>(fs) * a.slot_bytes)), "l"(z + sp.head + static_cast<int64_t>(sp.v0) * E),
-                         "r"(bytes), "r"(bar) : "memory");
-        fill_par = filled >> fs & 1u ? fill_par ^ 1u << fs : fill_par;
-        filled |= 1u << fs;
-        if (++fs == S) fs = 0;
-        next += step;
-        if (next < a.rows) ask = side_at<K>(a, next, false);
-    };
-    // with a gradient the slot of the row before is filled in the middle of this one (S = 1: its own, at the end)
-    if (copier) {
-        if (first < a.rows) ask = side_at<K>(a, first, false);
-        for (int q = 0; q < (grad && S > 1 ? S - 1 : S); ++q) fill();
-    }
-    // The preparing thread: `side` holds the row after the one in progress, the logit at its token is on the way.
-    const bool preparer = tid == (nw - 1) * 32;
-    Side side{};
-    T zt_raw{};
-    auto look_up = [&](int64_t row) {                 // side is that row's: its token's logit
-        const int32_t tok = K != kDistill || a.labels.p ? token_of<K>(a, side) : -1;
-        if (tok >= 0 && is_live<K>(a, side)) zt_raw = logits(row)[tok];
-    };
-    auto prepare = [&](int64_t row, Row& r) {
+    auto gradient = [&](int64_t row) { return static_cast<T*>(a.dz) + row * a.lddz; };
+    auto prepare = [&](int64_t row, int it, const Side& side) {
+        Row r{};
         r.span = span_of(logits(row), V, rank, a.cluster_shift);
         r.w = side.w; r.adv = side.adv; r.old = side.old; r.ref = side.ref;
-        r.tok = K != kDistill || a.labels.p ? token_of<K>(a, side) : -1;
+        r.tok = !D || a.labels.p ? token_of<K>(a, side) : -1;
         r.live = is_live<K>(a, side);
-        r.zt = load(&zt_raw);
+        r.same = ((reinterpret_cast<uintptr_t>(logits(row)) ^ reinterpret_cast<uintptr_t>(gradient(row))) & 15) == 0;
+        row_s[it & 3] = r;
     };
-    Side after{};                                     // and the row after that
-    if (preparer && first < a.rows) {
-        side = side_at<K>(a, first, true);
-        look_up(first);
-        prepare(first, row_s[0]);
-        if (first + step < a.rows) side = side_at<K>(a, first + step, true);
-    }
-    // Teacher entries, 32 kEntries a warp: entry k = warp 32 kEntries + 32 u + lane.
-    const int k0 = warp * 32 * kEntries + lane;
-    const bool entries = D && warp * 32 * kEntries < a.topk;
-    Word id[kEntries];
-    float av[kEntries];                               // bf16 teacher logits as their bits
-    auto ask_entries = [&](int64_t row) {
-#pragma unroll
-        for (int u = 0; u < kEntries; ++u) {
-            const int k = k0 + 32 * u;
-            if (k < a.topk) {
-                id[u] = word_at(a.ids, row * a.ldi + k);
-                const int64_t at = row * a.ldt + k;
-                av[u] = a.teacher_bf16 ? __uint_as_float(static_cast<const uint16_t*>(a.teacher)[at]) : static_cast<const float*>(a.teacher)[at];
-            }
-        }
-    };
-    if (entries && first < a.rows) ask_entries(first);
+    if (warp == nw && lane < 3 && first + lane * step < a.rows) prepare(first + lane * step, lane, side_at<K>(a, first + lane * step));
     __syncthreads();
+    if (C > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 
-    int s = 0, par = 0;
+    int s = 0, it = 0;
     uint32_t use = 0, xuse = 0;
-    for (int64_t row = first; row < a.rows; row += step) {
-        const Row now = row_s[par];
-        const Span sp = now.span;
-        const int nv = sp.nv;
-        bool counts = now.live;
-        uint4* slot = reinterpret_cast<uint4*>(slots + static_cast<size_t>(s) * a.slot_bytes);
-        const bool more = row + step < a.rows;
-        // ---- ask for what comes from memory.  Logits of this row are read here, before any CTA of the cluster
-        // overwrites them (dz may be z)
-        int32_t eid[kEntries];
-        float ea[kEntries];
-        T ez_raw[kEntries];                           // widened where they are used
-        if (entries) {
+    if (warp == nw) {
+        int fs = 0, fills = 0;
+        uint32_t fill_par = 0;                        // bit q: parity of slot q's last fill
+        auto fill = [&]() {                           // lane 0
+            const int64_t row = first + fills * step;
+            if (row >= a.rows) return;
+            const Row& r = row_s[fills & 3];
+            const uint32_t bytes = r.live ? static_cast<uint32_t>(r.span.nv) * 16u : 0u;
+            const uint32_t bar = smem_u32(&full_bar[fs]);
+            mbar_expect_tx(bar, bytes);
+            if (bytes)
+                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                             ::"r"(smem_u32(slots + static_cast<size_t>(fs) * a.slot_bytes)), "l"(logits(row) + r.span.head + static_cast<int64_t>(r.span.v0) * E),
+                             "r"(bytes), "r"(bar) : "memory");
+            if (fills >= S) fill_par ^= 1u << fs;
+            if (++fs == S) fs = 0;
+            ++fills;
+        };
+        // the element of the ends that this lane owns, or -1: the head with the first CTA, the tail with the last
+        auto end_of = [&](const Span& sp) {
+            const int tail = V - sp.head - sp.elems;
+            return rank == 0 && lane < sp.head ? lane : rank == C - 1 && lane >= 8 && lane < 8 + tail ? sp.head + sp.elems + lane - 8 : -1;
+        };
+        // 3: what comes from memory for a row, into shared memory.  (A row is only overwritten by its gradient
+        // once all CTAs of a cluster have sent its sums, which they do after this.)
+        auto stage = [&](int64_t row, int q) {
+            const Row& r = row_s[q & 3];
             const T* z = logits(row);
-#pragma unroll
-            for (int u = 0; u < kEntries; ++u) {
-                const int k = k0 + 32 * u;
-                eid[u] = counts && k < a.topk ? index_of(id[u], a.ids.wide, V) : -1;
-                ea[u] = eid[u] < 0 ? -CUDART_INF_F : a.teacher_bf16 ? __uint_as_float(__float_as_uint(av[u]) << 16) : av[u];
-                if (eid[u] >= 0) ez_raw[u] = z[eid[u]];
-                if (k < a.topk) id_s[k] = eid[u];
-            }
-            if (more) ask_entries(row + step);
-        }
-        const bool hard = D && counts && now.tok >= 0 && a.hard != 0.f;
-        if (D && tid == 0) id_s[a.topk] = hard ? now.tok : -1;
-        // the unaligned ends, an element a thread: the head with the first CTA, the tail with the last
-        T edge{};
-        int at_end = -1;                              // this thread's element of the ends
-        if (warp == 0) {
-            if (rank == 0 && lane < sp.head) at_end = lane;
-            if (rank == C - 1 && lane >= 8 && lane < 8 + V - sp.head - sp.elems) at_end = sp.head + sp.elems + lane - 8;
-            if (counts && at_end >= 0) edge = logits(row)[at_end];
-        }
-        if (preparer && more) {
-            look_up(row + step);
-            if (row + 2 * step < a.rows) after = side_at<K>(a, row + 2 * step, true);
-        }
-
-        wait(smem_u32(&full_bar[s]), use, false, abort, a.err);
-        // ---- statistics
-        Stat st{-CUDART_INF_F, 0.f, 0.f};
-        uint64_t kept[kKeep][P];
-        if (counts && HELD) {
-            uint4 u[kHeld];
-#pragma unroll
-            for (int q = 0; q < kHeld; ++q) {
-                const int v = tid + q * nt;
-                u[q] = v < nv ? slot[v] : Vec<T>::none();
-                st.m = fmaxf(st.m, Vec<T>::top(u[q]));
-            }
-            const float ref = st.m == -CUDART_INF_F ? 0.f : st.m;
-            const uint64_t nr = pack2(-ref, -ref);
-            uint64_t s2[2] = {0, 0}, t2[2] = {0, 0};
-#pragma unroll
-            for (int q = 0; q < kHeld; ++q) {
-                uint64_t x[P];
-                Vec<T>::get(u[q], x);
-#pragma unroll
-                for (int i = 0; i < P; ++i) {
-                    const uint64_t d = add2(x[i], nr), e = exp2_2(mul2(d, c2));
-                    s2[i & 1] = add2(s2[i & 1], e);
-                    if (TWO) t2[i & 1] = add2(t2[i & 1], exp2_2(mul2(d, l2)));
-                    if (kKeep > 1) kept[q][i] = e;
+            const int p = q & 1;
+            if (!r.live) return;
+            const int e = end_of(r.span);
+            const T ends = z[max(e, 0)], zt = z[max(r.tok, 0)];
+            if (D) {
+                for (int k = lane; k < a.topk; k += 32) {
+                    const int32_t id = index_of(word_at(a.ids, row * a.ldi + k), a.ids.wide, V);
+                    const int64_t at = row * a.ldt + k;
+                    const float t = a.teacher_bf16 ? load(static_cast<const __nv_bfloat16*>(a.teacher) + at) : static_cast<const float*>(a.teacher)[at];
+                    id_s[p][k] = id;
+                    a_s[p][k] = id < 0 ? -CUDART_INF_F : t;
+                    z_s[p][k] = load(z + max(id, 0));
+                }
+                const int64_t ahead = row + step < a.rows ? row + step : row;
+                for (int k = lane; k < a.topk; k += 32) {
+                    asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const char*>(a.ids.p) + (ahead * a.ldi + k) * (a.ids.wide ? 8 : 4)));
+                    asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const char*>(a.teacher) + (ahead * a.ldt + k) * (a.teacher_bf16 ? 2 : 4)));
                 }
             }
-            float x, y;
-            unpack2(add2(s2[0], s2[1]), x, y);
-            st.s = x + y;
-            unpack2(add2(t2[0], t2[1]), x, y);
-            st.s1 = x + y;
-        } else if (counts) {
-            uint64_t s2 = 0, t2 = 0;
-            for (int v = tid; v < nv; v += nt) st.m = fmaxf(st.m, Vec<T>::top(slot[v]));
-            const float ref = st.m == -CUDART_INF_F ? 0.f : st.m;
-            const uint64_t nr = pack2(-ref, -ref);
-            for (int v = tid; v < nv; v += nt) {
-                uint64_t x[P];
-                Vec<T>::get(slot[v], x);
-#pragma unroll
-                for (int i = 0; i < P; ++i) {
-                    const uint64_t d = add2(x[i], nr);
-                    s2 = add2(s2, exp2_2(mul2(d, c2)));
-                    if (TWO) t2 = add2(t2, exp2_2(mul2(d, l2)));
-                }
+            if (lane < 16) end_s[p][lane] = e >= 0 ? load(&ends) : -CUDART_INF_F;
+            if (lane == 0) {
+                zt_s[p] = load(&zt);
+                if (D) id_s[p][a.topk] = a.hard != 0.f ? r.tok : -1;
             }
-            float x, y;
-            unpack2(s2, x, y);
-            st.s = x + y;
-            unpack2(t2, x, y);
-            st.s1 = x + y;
-        }
-        const float m_own = st.m;                     // what this thread's exponentials are relative to
-        const float e0 = load(&edge);
-        if (warp == 0 && counts && at_end >= 0) {     // one more element
-            const float m = fmaxf(st.m, e0), r = m == -CUDART_INF_F ? 0.f : m;
-            st.s = st.s * shrink(st.m, m, c) + exp2_fast((e0 - r) * c);
-            if (TWO) st.s1 = st.s1 * shrink(st.m, m, kLog2e) + exp2_fast((e0 - r) * kLog2e);
-            st.m = m;
-        }
-        st = warp_merge<TWO>(st, c);
-        Top tp{-CUDART_INF_F, 0.f, 0.f};
-        if (entries) {
-#pragma unroll
-            for (int u = 0; u < kEntries; ++u) tp.m = fmaxf(tp.m, ea[u]);
-#pragma unroll
-            for (int u = 0; u < kEntries; ++u)     // an entry that the teacher rules out leaves the sums as they are
-                if (ea[u] != -CUDART_INF_F) {
-                    const float e = shrink(ea[u], tp.m, c);
-                    tp.s += e;
-                    tp.a += e * (ea[u] - tp.m);
-                }
-            tp = warp_merge(tp, c);
-        }
-        if (lane == 0) {
-            stat_s[par][warp] = st;
-            if (entries) top_s[par][warp] = tp;
-        }
-        __syncthreads();
-        if (copier && grad && S > 1) {                 // the slot of the row before has been written back by now
-            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-            fill();
-        }
-        if (nw > 1) st = warp_merge<TWO>(lane < nw ? stat_s[par][lane] : Stat{-CUDART_INF_F, 0.f, 0.f}, c);
-        if (C > 1 && warp == 0 && lane < C) {
-            const uint32_t to = peer_addr(smem_u32(&cluster_s[par][rank]), lane);
-            asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0+4], %2;\n\tst.shared::cluster.f32 [%0+8], %3;"
-                         ::"r"(to), "f"(st.m), "f"(st.s), "f"(st.s1) : "memory");
-            asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(peer_addr(smem_u32(&x_bar[par]), lane)) : "memory");
-        }
-        // ---- while the peers' sums come in: the teacher's sums, and whether an id is listed twice
-        const int top = a.topk, n = D && counts ? top + 1 : 0;
-        bool twice = false;
-        if (D && counts) {
-            if (top > 32 * kEntries) tp = warp_merge(lane * 32 * kEntries < top ? top_s[par][lane & (kMaxWarps - 1)] : Top{-CUDART_INF_F, 0.f, 0.f}, c);
-            else if (top > 0) tp = top_s[par][0];
-            if (grad) {
-                // entry k against the earlier ones: 2^dup_shift threads an entry
-                const int parts = 1 << a.dup_shift;
-                for (int k = tid >> a.dup_shift; k < n; k += nt >> a.dup_shift) {
-                    const int32_t v = id_s[k];
-                    for (int j = tid & (parts - 1); j < k; j += parts) twice |= id_s[j] == v && v >= 0;
-                }
+        };
+        if (lane == 0)
+            for (int q = 0; q < (grad && S > 1 ? S - 1 : S); ++q) fill();
+        if (first < a.rows) stage(first, 0);
+        __syncwarp();
+        for (int64_t row = first; row < a.rows; row += step, ++it) {
+            const Row now = row_s[it & 3];
+            const int par = it & 1, top = a.topk;
+            const uint32_t ph = static_cast<uint32_t>(par);                // fin_bar and dense_bar: a phase a row
+            bool counts = now.live;
+            // ---- 1
+            const int e = end_of(now.span);
+            const float e0 = counts && lane < 16 ? end_s[par][lane] : -CUDART_INF_F;
+            Stat st{e0, 0.f, 0.f};
+            if (e0 != -CUDART_INF_F) {                // exp of the one element against itself (a NaN stays one)
+                st.s = exp2_fast((e0 - e0) * c);
+                st.s1 = exp2_fast((e0 - e0) * kLog2e);
             }
-        }
-        if (C > 1) {
-            wait(smem_u32(&x_bar[par]), xuse, true, abort, a.err);
-            st = warp_merge<TWO>(lane < C ? cluster_s[par][lane] : Stat{-CUDART_INF_F, 0.f, 0.f}, c);
-        }
-        if (st.s == 0.f) counts = false;
-        if (!TWO) st.s1 = st.s;
-
-        // ---- the row's loss and the factors of its gradient: dense exp2((z - m) c) + dense1 exp2((z - m) log2 e),
-        // less what is listed at single ids
-        const float inv_s = __fdividef(1.f, st.s), zt = now.zt;
-        float dense = 0.f, dense1 = 0.f, at_tok = 0.f, q[kEntries] = {};
-        if (K == kDistill) {
-            const bool soft = counts && tp.s != 0.f;
-            const float f = now.w * a.soft * a.inv_tau, inv = 1.f / tp.s;
-            if (soft) dense = f * inv_s;
-            if (hard && counts) {
-                at_tok = now.w * a.hard;
-                dense1 = at_tok / st.s1;
-                if (!TWO) { dense += dense1; dense1 = 0.f; }
+            st = warp_merge<TWO>(st, c);
+            Top tp{-CUDART_INF_F, 0.f, 0.f};
+            if (D && counts) {
+                for (int k = lane; k < top; k += 32) tp.m = fmaxf(tp.m, a_s[par][k]);
+                for (int k = lane; k < top; k += 32) {
+                    const float x = a_s[par][k];
+                    if (x != -CUDART_INF_F) {         // an entry that the teacher rules out leaves the sums as they are
+                        const float w = shrink(x, tp.m, c);
+                        tp.s += w;
+                        tp.a += w * (x - tp.m);
+                    }
+                }
+                tp = warp_merge(tp, c);
             }
-            if (entries) {
+            const Pub pub{counts ? zt_s[par] : 0.f, D && tp.s != 0.f};
+            if (lane == 0) {
+                stat_s[par][nw] = st;
+                pub_s[par] = pub;
+                if (C > 1) mbar_expect_tx(smem_u32(&x_bar[par]), 16u * C);
+            }
+            __syncwarp();
+            asm volatile("bar.arrive 1, %0;" ::"r"(nt + 32) : "memory");
+            // ---- 2
+            if (lane == 0 && grad && S > 1) {
+                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                fill();
+            }
+            // ---- 3
+            const int64_t later = row + 3 * step;
+            Side side{};
+            if (lane == 0) side = side_at<K>(a, later < a.rows ? later : row);
+            if (row + step < a.rows) stage(row + step, it + 1);
+            if (lane == 0 && later < a.rows) prepare(later, it + 3, side);
+            __syncwarp();
+            // ---- 4
+            wait(smem_u32(&fin_bar), ph, false, abort, a.err);
+            st = fin_s[par];
+            if (st.s == 0.f) counts = false;
+            const Coef k = coef_of<K, TWO>(a, now, st, pub, counts);
+            if (D) {
+                const float f = now.w * a.soft * a.inv_tau, inv = 1.f / tp.s;
+                const bool soft = counts && pub.soft;
                 float zq = 0.f;
-#pragma unroll
-                for (int u = 0; u < kEntries; ++u) {
-                    const float e = !soft || ea[u] == -CUDART_INF_F ? 0.f : exp2_fast((ea[u] - tp.m) * c) * inv;
-                    q[u] = f * e;
-                    if (k0 + 32 * u < top) q_s[k0 + 32 * u] = q[u];
-                    if (e != 0.f) zq += e * (load(&ez_raw[u]) - st.m);
+                for (int j = lane; j < top; j += 32) {
+                    const float x = a_s[par][j], w = !soft || x == -CUDART_INF_F ? 0.f : exp2_fast((x - tp.m) * c) * inv;
+                    q_s[j] = f * w;
+                    if (w != 0.f) zq += w * (z_s[par][j] - st.m);
                 }
                 zq = warp_sum(zq);
-                if (lane == 0) zq_s[warp] = zq;
-            }
-            if (tid == 0) q_s[top] = at_tok;
-        } else {
-            const float lp = counts ? (zt - st.m) * a.inv_tau - log_fast(st.s) : 0.f;
-            if (K == kPolicy) {
-                float loss = 0.f, slope = 0.f;
-                if (counts) {
-                    const float A = now.adv, ratio = exp2_fast((lp - now.old) * kLog2e);
-                    loss = -fminf(ratio * A, fminf(fmaxf(ratio, a.clip_lo), a.clip_hi) * A);
-                    if (isnan(ratio * A)) loss = ratio * A;
-                    slope = (A > 0.f ? ratio > a.clip_hi : ratio < a.clip_lo) ? 0.f : -A * ratio;
-                    if (a.ref_logp) {
-                        const float e = expm1f(now.ref - lp);
-                        loss += a.kl * (e - (now.ref - lp));
-                        slope -= a.kl * e;
-                    }
+                if (lane == 0) {
+                    q_s[top] = k.at_tok;
+                    float loss = 0.f;
+                    if (soft) loss = a.soft * ((tp.a * inv * a.inv_tau - log_fast(tp.s)) - (zq * a.inv_tau - log_fast(st.s)));
+                    if (counts && now.tok >= 0 && a.hard != 0.f) loss += a.hard * (log_fast(st.s1) - (pub.zt - st.m));
+                    if (rank == 0) a.row_loss[row] = loss;
                 }
-                at_tok = -slope * now.w * a.inv_tau;
-                dense = counts ? at_tok * inv_s : 0.f;
-                if (tid == 0 && rank == 0) { a.row_loss[row] = loss; a.logp[row] = lp; }
-            } else if (tid == 0 && rank == 0) {
-                a.logp[row] = lp;
-                a.lse[row] = counts ? st.m + log_fast(st.s) : CUDART_INF_F;
-                a.coef[row] = 0.f;
+            } else if (lane == 0 && rank == 0) {
+                a.logp[row] = k.lp;
+                if (K == kPolicy) {
+                    a.row_loss[row] = k.loss;
+                } else {
+                    a.lse[row] = counts ? st.m + log_fast(st.s) : CUDART_INF_F;
+                    a.coef[row] = 0.f;
+                }
             }
-        }
-
-        // ---- the gradient, over the logits
-        T* mine = reinterpret_cast<T*>(slot);
-        auto at = [&](float x) {
-            const float d = x - st.m;
-            float g = dense * exp2_fast(d * c);
-            if (TWO) g += dense1 * exp2_fast(d * kLog2e);
-            return g;
-        };
-        // the place of an id in this CTA's part of the row, or negative
-        auto place = [&](int32_t v) {
-            const int b = v - sp.head - sp.v0 * E;
-            return b < nv * E ? b : -1;
-        };
-        auto row_of = [&]() { return static_cast<T*>(a.dz) + row * a.lddz; };
-        auto is_end = [&](int32_t v) { return (rank == 0 && v < sp.head) || (rank == C - 1 && v >= sp.head + sp.elems); };
-        if (grad) {
-            if (counts && HELD) {
-                const float f = dense * shrink(m_own, st.m, c);
-                const uint64_t ff = pack2(f, f), nm = pack2(-st.m, -st.m), dd1 = pack2(dense1, dense1);
-#pragma unroll
-                for (int j = 0; j < kKeep; ++j) {
-                    const int v = tid + j * nt;
-                    if (v < nv) {
-                        uint64_t x[P];
-                        if (TWO) Vec<T>::get(slot[v], x);
-#pragma unroll
-                        for (int i = 0; i < P; ++i) {
-                            const uint64_t g = mul2(ff, kept[j][i]);
-                            x[i] = TWO ? fma2(dd1, exp2_2(mul2(add2(x[i], nm), l2)), g) : g;
+            // ---- 5
+            wait(smem_u32(&dense_bar), ph, false, abort, a.err);
+            if (grad) {
+                uint8_t* slot = slots + static_cast<size_t>(s) * a.slot_bytes;
+                T* body = gradient(row) + now.span.head + static_cast<int64_t>(now.span.v0) * E;
+                T* mine = now.same ? reinterpret_cast<T*>(slot) : body;
+                auto at = [&](float x) {
+                    const float d = x - st.m;
+                    float g = k.dense * exp2_fast(d * c);
+                    if (TWO) g += k.dense1 * exp2_fast(d * kLog2e);
+                    return g;
+                };
+                // the place of an id in this CTA's part of the row, or negative; its end that this CTA owns, or negative
+                auto place = [&](int32_t v) {
+                    const int b = v - now.span.head - now.span.v0 * E;
+                    return b < now.span.nv * E ? b : -1;
+                };
+                auto at_end = [&](int32_t v) {
+                    return rank == 0 && v < now.span.head ? v : rank == C - 1 && v >= now.span.head + now.span.elems ? 8 + v - now.span.head - now.span.elems : -1;
+                };
+                if (e >= 0) store(gradient(row) + e, counts ? at(e0) : 0.f);
+                __syncwarp();
+                if (!D && counts && lane == 0) {
+                    if (place(now.tok) >= 0) store(mine + place(now.tok), at(pub.zt) - k.at_tok);
+                    else if (at_end(now.tok) >= 0) store(gradient(row) + now.tok, at(pub.zt) - k.at_tok);
+                }
+                if (D && counts) {
+                    // Entries mark their places in the slot (or an end's) with their number.  One that finds another's
+                    // mark there shares its id: it flags the mark, and the flagged mark's owner adds up all of that id.
+                    using M = typename Vec<T>::Mark;
+                    constexpr int kFlag = 1 << 14;
+                    auto id_at = [&](int j) { return id_s[par][j]; };
+                    auto mark_of = [&](int32_t v, int j, int op) {          // op 0: write j, 1: read, 2: flag
+                        const int b = place(v), x = b < 0 ? at_end(v) : -1;
+                        M* m = reinterpret_cast<M*>(slot) + (b >= 0 ? b : 0);
+                        if (b < 0 && x < 0) return -1;
+                        if (op == 0) { if (b >= 0) *m = static_cast<M>(j); else mark_s[x] = j; return j; }
+                        const int r = b >= 0 ? static_cast<int>(*m) : mark_s[x];
+                        if (op == 2) { if (b >= 0) *m = static_cast<M>(r | kFlag); else mark_s[x] = r | kFlag; }
+                        return r;
+                    };
+                    for (int j = lane; j <= top; j += 32) if (id_at(j) >= 0) mark_of(id_at(j), j, 0);
+                    __syncwarp();
+                    bool twice = false;
+                    for (int j = lane; j <= top; j += 32) {
+                        if (id_at(j) < 0) continue;
+                        const int r = mark_of(id_at(j), j, 1);
+                        if (r >= 0 && (r & (kFlag - 1)) != j) { mark_of(id_at(j), j, 2); twice = true; }
+                    }
+                    twice = __any_sync(~0u, twice);
+                    __syncwarp();
+                    for (int j = lane; j <= top; j += 32) {
+                        const int32_t v = id_at(j);
+                        const int r = v >= 0 ? mark_of(v, j, 1) : -1;
+                        if (r < 0 || (r & (kFlag - 1)) != j) continue;
+                        float g = q_s[j];
+                        if (twice && (r & kFlag)) {
+                            g = 0.f;
+                            for (int i = 0; i <= top; ++i) g += id_at(i) == v ? q_s[i] : 0.f;
                         }
-                        slot[v] = Vec<T>::put(x);
+                        const float x = j < top ? z_s[par][j] : pub.zt;
+                        store(place(v) >= 0 ? mine + place(v) : gradient(row) + v, at(x) - g);
                     }
                 }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    // the workers' writes and these, before the copy reads them
+                __syncwarp();
+                if (lane == 0) {
+                    if (now.span.nv > 0 && now.same)
+                        asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
+                                     ::"l"(body), "r"(smem_u32(slot)), "r"(static_cast<uint32_t>(now.span.nv) * 16u) : "memory");
+                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    if (S == 1) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                }
+            }
+            if (lane == 0 && (!grad || S == 1)) fill();
+            __syncwarp();
+            if (++s == S) s = 0;
+        }
+        if (lane == 0) {
+            if (grad) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+            if (*abort)                               // let the copies already issued land
+                for (int q = 0; q < S; ++q)
+                    if (q < fills)
+                        for (int i = 0; i < 4000000 && !try_wait(smem_u32(&full_bar[q]), fill_par >> q & 1u, false); ++i) __nanosleep(64);
+        }
+    } else {
+        for (int64_t row = first; row < a.rows; row += step, ++it) {
+            const int par = it & 1;
+            const Row now = row_s[it & 3];
+            const int nv = now.span.nv;
+            bool counts = now.live;
+            uint4* slot = reinterpret_cast<uint4*>(slots + static_cast<size_t>(s) * a.slot_bytes);
+            wait(smem_u32(&full_bar[s]), use, false, abort, a.err);
+            // ---- statistics
+            Stat st{-CUDART_INF_F, 0.f, 0.f};
+            uint64_t kept[kKeep][P];
+            if (counts && HELD) {
+                uint4 u[kHeld];
+#pragma unroll
+                for (int q = 0; q < kHeld; ++q) {
+                    const int v = tid + q * nt;
+                    u[q] = v < nv ? slot[v] : Vec<T>::none();
+                    st.m = fmaxf(st.m, Vec<T>::top(u[q]));
+                }
+                const float ref = st.m == -CUDART_INF_F ? 0.f : st.m;
+                const uint64_t nr = pack2(-ref, -ref);
+                uint64_t s2[2] = {0, 0}, t2[2] = {0, 0};
+#pragma unroll
+                for (int q = 0; q < kHeld; ++q) {
+                    uint64_t x[P];
+                    Vec<T>::get(u[q], x);
+#pragma unroll
+                    for (int i = 0; i < P; ++i) {
+                        const uint64_t d = add2(x[i], nr), e = exp2_2(mul2(d, c2));
+                        s2[i & 1] = add2(s2[i & 1], e);
+                        if (TWO) t2[i & 1] = add2(t2[i & 1], exp2_2(mul2(d, l2)));
+                        if (kKeep > 1) kept[q][i] = e;
+                    }
+                }
+                float x, y;
+                unpack2(add2(s2[0], s2[1]), x, y);
+                st.s = x + y;
+                unpack2(add2(t2[0], t2[1]), x, y);
+                st.s1 = x + y;
             } else if (counts) {
-                const uint64_t nm = pack2(-st.m, -st.m), dd = pack2(dense, dense), dd1 = pack2(dense1, dense1);
+                uint64_t s2 = 0, t2 = 0;
+                for (int v = tid; v < nv; v += nt) st.m = fmaxf(st.m, Vec<T>::top(slot[v]));
+                const float ref = st.m == -CUDART_INF_F ? 0.f : st.m;
+                const uint64_t nr = pack2(-ref, -ref);
                 for (int v = tid; v < nv; v += nt) {
                     uint64_t x[P];
                     Vec<T>::get(slot[v], x);
 #pragma unroll
                     for (int i = 0; i < P; ++i) {
-                        const uint64_t d = add2(x[i], nm);
-                        x[i] = mul2(dd, exp2_2(mul2(d, c2)));
-                        if (TWO) x[i] = fma2(dd1, exp2_2(mul2(d, l2)), x[i]);
+                        const uint64_t d = add2(x[i], nr);
+                        s2 = add2(s2, exp2_2(mul2(d, c2)));
+                        if (TWO) t2 = add2(t2, exp2_2(mul2(d, l2)));
                     }
-                    slot[v] = Vec<T>::put(x);
                 }
-            } else {
-                for (int v = tid; v < nv; v += nt) slot[v] = make_uint4(0, 0, 0, 0);
+                float x, y;
+                unpack2(s2, x, y);
+                st.s = x + y;
+                unpack2(t2, x, y);
+                st.s1 = x + y;
             }
-            if (at_end >= 0) {
-                float g = counts ? at(e0) : 0.f;
-                if (K == kPolicy && counts && at_end == now.tok) g -= at_tok;
-                store(row_of() + at_end, g);
+            const float m_own = st.m;                 // what this thread's exponentials are relative to
+            st = warp_merge<TWO>(st, c);
+            if (lane == 0) stat_s[par][warp] = st;
+            __syncwarp();
+            asm volatile("bar.sync 1, %0;" ::"r"(nt + 32) : "memory");
+            st = warp_merge<TWO>(lane <= nw ? stat_s[par][lane] : Stat{-CUDART_INF_F, 0.f, 0.f}, c);
+            const Pub pub = pub_s[par];
+            if (C > 1) {
+                // the sums go to the peers with the signal that they are there, in one store each
+                if (warp == 0 && lane < C)
+                    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
+                                 ::"r"(peer_addr(smem_u32(&cluster_s[par][rank]), lane)), "f"(st.m), "f"(st.s), "f"(st.s1), "f"(0.f),
+                                   "r"(peer_addr(smem_u32(&x_bar[par]), lane)) : "memory");
+                wait(smem_u32(&x_bar[par]), xuse, true, abort, a.err);
+                const float4 x = lane < C ? cluster_s[par][lane] : make_float4(-CUDART_INF_F, 0.f, 0.f, 0.f);
+                st = warp_merge<TWO>(Stat{x.x, x.y, x.z}, c);
             }
-            if (K == kPolicy && counts) {              // by the thread that wrote the token's vector
-                const int b = place(now.tok);
-                int v = b / E;
-                if (HELD) {
-#pragma unroll
-                    for (int j = 1; j < kHeld; ++j) v -= v >= nt ? nt : 0;
-                } else {
-                    v %= nt;
-                }
-                if (b >= 0 && v == tid) store(mine + b, at(zt) - at_tok);
+            if (!TWO) st.s1 = st.s;
+            if (tid == 0) {
+                fin_s[par] = st;
+                tc::mbar_arrive(smem_u32(&fin_bar));
             }
-        }
-        if (K == kDistill) {
-            // every thread's part of the gradient is written before single entries are: the slot's, and the ends'
-            twice = __syncthreads_or(twice);
-            if (tid == 0 && rank == 0) {
-                float loss = 0.f;
-                if (counts && tp.s != 0.f) {
-                    float z_sum = 0.f;
-                    for (int w = 0; w * 32 * kEntries < top; ++w) z_sum += zq_s[w];
-                    loss = a.soft * ((tp.a / tp.s * a.inv_tau - log_fast(tp.s)) - (z_sum * a.inv_tau - log_fast(st.s)));
-                }
-                if (hard && counts) loss += a.hard * (log_fast(st.s1) - (zt - st.m));
-                a.row_loss[row] = loss;
-            }
-            if (grad && counts && (entries || tid == 0)) {
-                auto single = [&](int32_t v, float g, float z) {
-                    if (v < 0) return;
-                    const int b = place(v);
-                    if (b < 0 && !is_end(v)) return;
-                    if (twice) {
-                        g = 0.f;
-                        for (int j = 0; j < n; ++j) g += id_s[j] == v ? q_s[j] : 0.f;
-                    }
-                    store(b >= 0 ? mine + b : row_of() + v, at(z) - g);
-                };
-                if (entries) {
-#pragma unroll
-                    for (int u = 0; u < kEntries; ++u) single(eid[u], q[u], load(&ez_raw[u]));
-                }
-                if (tid == 0 && hard) single(now.tok, at_tok, zt);
-            }
-        }
-        const bool same = grad && ((reinterpret_cast<uintptr_t>(logits(row)) ^ reinterpret_cast<uintptr_t>(row_of())) & 15) == 0;
-        if (grad && !same) {
-            // the gradient's rows lie otherwise on 16 bytes than the logits': element by element
-            __syncthreads();
-            T* to = row_of() + sp.head + static_cast<int64_t>(sp.v0) * E;
-            for (int j = tid; j < nv * E; j += nt) to[j] = mine[j];
-        }
-        if (preparer && more) {
-            prepare(row + step, row_s[par ^ 1]);
-            side = after;
-        }
-        __syncthreads();
-        if (copier) {
+            if (st.s == 0.f) counts = false;
+            // ---- the gradient
             if (grad) {
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    // all threads' writes, before the copy reads them
-                if (nv > 0 && same)
-                    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
-                                 ::"l"(row_of() + sp.head + static_cast<int64_t>(sp.v0) * E), "r"(smem_u32(slot)), "r"(static_cast<uint32_t>(nv) * 16u) : "memory");
-                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                if (S == 1) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                const Coef k = coef_of<K, TWO>(a, now, st, pub, counts);
+                const uint64_t nm = pack2(-st.m, -st.m), dd1 = pack2(k.dense1, k.dense1);
+                T* body = gradient(row) + now.span.head + static_cast<int64_t>(now.span.v0) * E;
+                auto put = [&](int v, const uint4& u) {
+                    if (now.same) slot[v] = u;
+                    else Vec<T>::scatter(body + v * E, u);     // the gradient's rows lie otherwise on 16 bytes
+                };
+                if (counts && HELD) {
+                    const float f = k.dense * shrink(m_own, st.m, c);
+                    const uint64_t ff = pack2(f, f);
+#pragma unroll
+                    for (int j = 0; j < kKeep; ++j) {
+                        const int v = tid + j * nt;
+                        if (v < nv) {
+                            uint64_t x[P];
+                            if (TWO) Vec<T>::get(slot[v], x);
+#pragma unroll
+                            for (int i = 0; i < P; ++i) {
+                                const uint64_t g = mul2(ff, kept[j][i]);
+                                x[i] = TWO ? fma2(dd1, exp2_2(mul2(add2(x[i], nm), l2)), g) : g;
+                            }
+                            put(v, Vec<T>::put(x));
+                        }
+                    }
+                } else if (counts) {
+                    const uint64_t dd = pack2(k.dense, k.dense);
+                    for (int v = tid; v < nv; v += nt) {
+                        uint64_t x[P];
+                        Vec<T>::get(slot[v], x);
+#pragma unroll
+                        for (int i = 0; i < P; ++i) {
+                            const uint64_t d = add2(x[i], nm);
+                            x[i] = mul2(dd, exp2_2(mul2(d, c2)));
+                            if (TWO) x[i] = fma2(dd1, exp2_2(mul2(d, l2)), x[i]);
+                        }
+                        put(v, Vec<T>::put(x));
+                    }
+                } else {
+                    for (int v = tid; v < nv; v += nt) put(v, make_uint4(0, 0, 0, 0));
+                }
             }
-            if (!grad || S == 1) fill();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(smem_u32(&dense_bar));
+            if (++s == S) { s = 0; use ^= 1u; }
+            if (par) xuse ^= 1u;
         }
-        if (++s == S) { s = 0; use ^= 1u; }
-        if (par) xuse ^= 1u;
-        par ^= 1;
-    }
-    if (copier) {
-        if (grad) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-        if (*abort)                                   // let the copies already issued land
-            for (int q = 0; q < S; ++q)
-                if (filled >> q & 1u)
-                    for (int it = 0; it < 4000000 && !try_wait(smem_u32(&full_bar[q]), fill_par >> q & 1u, false); ++it) __nanosleep(64);
     }
     // no CTA of a cluster leaves while another may still write to its shared memory
     if (C > 1) {
@@ -831,14 +846,7 @@ cudaError_t rows_launch(RowArgs a, int dtype, cudaStream_t st) {
     a.slots = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(3, kRingMax / a.slot_bytes)));
     const size_t smem = static_cast<size_t>(a.slots) * a.slot_bytes;
     const bool held = a.slot_bytes <= kSlotMax;
-    int warps = held ? static_cast<int>((a.slot_bytes / 16 + 32 * kHeld - 1) / (32 * kHeld)) : kMaxWarps;
-    if (K == kDistill) {
-        warps = std::max(warps, (a.topk + 32 * kEntries - 1) / (32 * kEntries));
-        a.dup_shift = 0;                          // threads an entry in the search for ids listed twice
-        while ((a.topk + 1) << (a.dup_shift + 1) <= warps * 32) ++a.dup_shift;
-    }
-    const int per_sm = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({16, kRingMax / static_cast<int64_t>(smem + 1024), 16 / warps})));
-    const int64_t groups = std::min<int64_t>(a.rows, std::max<int64_t>(1, static_cast<int64_t>(sms) * per_sm / C));
+    const int workers = held ? static_cast<int>((a.slot_bytes / 16 + 32 * kHeld - 1) / (32 * kHeld)) : kWorkers;
     const bool two = K == kDistill && a.labels.p && a.hard != 0.f && a.inv_tau != 1.f;
     auto pick = [&](auto t) {
         using T = decltype(t);
@@ -854,8 +862,19 @@ cudaError_t rows_launch(RowArgs a, int dtype, cudaStream_t st) {
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = C; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = static_cast<unsigned>(groups * C); cfg.blockDim = warps * 32; cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cfg.blockDim = (workers + 1) * 32; cfg.dynamicSmemBytes = smem; cfg.stream = st;
     cfg.attrs = attr; cfg.numAttrs = 2;
+    // as many groups of CTAs as run at once, each with its share of the rows
+    int64_t groups = a.rows;
+    if (a.rows * C > sms) {
+        int per = 0;
+        cfg.gridDim = C;
+        if (C > 1) e = cudaOccupancyMaxActiveClusters(&per, kernel, &cfg);
+        else if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, (workers + 1) * 32, smem)) == cudaSuccess) per *= sms;
+        if (e != cudaSuccess) return e;
+        groups = std::min<int64_t>(groups, std::max(per, 1));
+    }
+    cfg.gridDim = static_cast<unsigned>(groups * C);
     return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
