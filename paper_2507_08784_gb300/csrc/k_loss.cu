@@ -300,7 +300,7 @@ __device__ __forceinline__ Coef coef_of(const RowArgs& a, const Row& r, const St
 }
 
 constexpr int64_t kSlotMax = kWorkers * 32 * kHeld * 16;     // of a row a CTA: 67.5 KiB, three slots fit
-constexpr int64_t kRingMax = 196 * 1024;
+constexpr int64_t kRingMax = 193 * 1024;               // beside up to 34 KiB of the service warp's
 
 // HELD: a slot has at most kHeld vectors a worker thread, and the exponentials of the statistics stay in
 // registers for the gradient; else (rows of more than eight such slots) they are formed again.  TWO: a hard
@@ -309,11 +309,12 @@ constexpr int64_t kRingMax = 196 * 1024;
 // A worker's row is: wait for the slot, sums, one barrier, the merge of all warps' sums (and of the cluster's
 // CTAs), the gradient into the slot.  What each of up to fifteen warps would do for itself is paid that many
 // times over, and a load's latency in this chain is lost to all of them, so the service warp does the rest:
-//   1 the teacher's softmax, the ends' sums and the token's logit of row i, before the workers' barrier
-//   2 the fill of a slot whose row has been written back
-//   3 the loads of row i + 1's entries and logits, and the data of row i + 3
-//   4 the loss of row i, once its sums are there
-//   5 single entries of row i's gradient, once the workers have written theirs, and its write-back
+//   1 asks for the logits of row i + 1 that single entries need, the teacher's entries of row i + 2 and the
+//     data of row i + 3
+//   2 the ends' sums and the token's logit of row i, before the workers' barrier
+//   3 the loss of row i, once its sums are there, and the fill of the slot whose row has been written back
+//   4 single entries of row i's gradient, once the workers have written theirs, and its write-back
+//   5 puts down what was asked for, and the teacher's softmax of row i + 2
 template <int K, class T, bool HELD, bool TWO>
 __global__ void __launch_bounds__((kWorkers + 1) * 32) rows_kernel(const __grid_constant__ RowArgs a) {
     chain_begin();
@@ -330,8 +331,10 @@ __global__ void __launch_bounds__((kWorkers + 1) * 32) rows_kernel(const __grid_
     __shared__ __align__(16) float4 cluster_s[2][kMaxCluster];
     __shared__ Pub pub_s[2];
     __shared__ float end_s[2][16], zt_s[2];
-    __shared__ int32_t id_s[2][kList];
-    __shared__ float a_s[2][kList], z_s[2][kList], q_s[kList];
+    __shared__ int32_t id_s[3][kList];                // by the row's number modulo three: ids, and their q (0: none)
+    __shared__ float q_s[3][kList], z_s[2][kList];
+    __shared__ float teach_s[3];                      // sum of q log q; NaN-free only where soft_s
+    __shared__ int32_t soft_s[3];
     __shared__ int32_t mark_s[16];
     __shared__ int abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, nw = (blockDim.x >> 5) - 1, nt = nw * 32;
@@ -392,68 +395,116 @@ __global__ void __launch_bounds__((kWorkers + 1) * 32) rows_kernel(const __grid_
             const int tail = V - sp.head - sp.elems;
             return rank == 0 && lane < sp.head ? lane : rank == C - 1 && lane >= 8 && lane < 8 + tail ? sp.head + sp.elems + lane - 8 : -1;
         };
-        // 3: what comes from memory for a row, into shared memory.  (A row is only overwritten by its gradient
-        // once all CTAs of a cluster have sent its sums, which they do after this.)
-        auto stage = [&](int64_t row, int q) {
-            const Row& r = row_s[q & 3];
-            const T* z = logits(row);
-            const int p = q & 1;
-            if (!r.live) return;
-            const int e = end_of(r.span);
-            const T ends = z[max(e, 0)], zt = z[max(r.tok, 0)];
-            if (D) {
-                for (int k = lane; k < a.topk; k += 32) {
-                    const int32_t id = index_of(word_at(a.ids, row * a.ldi + k), a.ids.wide, V);
-                    const int64_t at = row * a.ldt + k;
-                    const float t = a.teacher_bf16 ? load(static_cast<const __nv_bfloat16*>(a.teacher) + at) : static_cast<const float*>(a.teacher)[at];
-                    id_s[p][k] = id;
-                    a_s[p][k] = id < 0 ? -CUDART_INF_F : t;
-                    z_s[p][k] = load(z + max(id, 0));
+        // The teacher's entries k, k + 32 of a row, as they lie in memory (lanes past the end: the last one).
+        struct Entry { Word id; float a; };
+        auto entry_at = [&](int64_t row, int k) {
+            k = min(k, a.topk - 1);
+            const int64_t at = row * a.ldt + k;
+            return Entry{word_at(a.ids, row * a.ldi + k),
+                         a.teacher_bf16 ? __uint_as_float(static_cast<const uint16_t*>(a.teacher)[at]) : static_cast<const float*>(a.teacher)[at]};
+        };
+        // Their softmax into q_s, ids into id_s: entries of the first two lots from registers, others from memory.
+        auto teacher = [&](int64_t row, int slot3, bool live, const Entry (&held)[2]) {
+            float m = -CUDART_INF_F;
+            auto take = [&](int k, const Entry& x) {
+                const int32_t id = live ? index_of(x.id, a.ids.wide, V) : -1;
+                const float t = id < 0 ? -CUDART_INF_F : a.teacher_bf16 ? __uint_as_float(__float_as_uint(x.a) << 16) : x.a;
+                id_s[slot3][k] = id;
+                q_s[slot3][k] = t;
+                m = fmaxf(m, t);
+            };
+            if (lane < a.topk) take(lane, held[0]);
+            if (lane + 32 < a.topk) take(lane + 32, held[1]);
+#pragma unroll 2
+            for (int k = lane + 64; k < a.topk; k += 32) take(k, entry_at(row, k));
+            m = warp_max(m);
+            float sum = 0.f, ta = 0.f;
+            for (int k = lane; k < a.topk; k += 32) {
+                const float t = q_s[slot3][k];
+                float w = 0.f;
+                if (t != -CUDART_INF_F) {             // an entry that the teacher rules out leaves the sums as they are
+                    w = exp2_fast((t - m) * c);
+                    sum += w;
+                    ta += w * (t - m);
                 }
-                const int64_t ahead = row + step < a.rows ? row + step : row;
-                for (int k = lane; k < a.topk; k += 32) {
-                    asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const char*>(a.ids.p) + (ahead * a.ldi + k) * (a.ids.wide ? 8 : 4)));
-                    asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const char*>(a.teacher) + (ahead * a.ldt + k) * (a.teacher_bf16 ? 2 : 4)));
-                }
+                q_s[slot3][k] = w;
             }
-            if (lane < 16) end_s[p][lane] = e >= 0 ? load(&ends) : -CUDART_INF_F;
+            sum = warp_sum(sum);
+            ta = warp_sum(ta);
+            const float inv = sum != 0.f ? 1.f / sum : 0.f;
+            for (int k = lane; k < a.topk; k += 32) q_s[slot3][k] *= inv;
             if (lane == 0) {
-                zt_s[p] = load(&zt);
-                if (D) id_s[p][a.topk] = a.hard != 0.f ? r.tok : -1;
+                teach_s[slot3] = ta * inv * a.inv_tau - log_fast(sum);
+                soft_s[slot3] = sum != 0.f;
+            }
+        };
+        auto row_live = [&](int q) { return row_s[q & 3].live != 0; };
+        // Puts down the logits at a row's ends and token.
+        auto put_ends = [&](int q, int e, const T& ends, const T& zt) {
+            if (lane < 16) end_s[q & 1][lane] = e >= 0 ? load(&ends) : -CUDART_INF_F;
+            if (lane == 0) {
+                zt_s[q & 1] = load(&zt);
+                if (D) id_s[q % 3][a.topk] = row_live(q) && a.hard != 0.f ? row_s[q & 3].tok : -1;
             }
         };
         if (lane == 0)
             for (int q = 0; q < (grad && S > 1 ? S - 1 : S); ++q) fill();
-        if (first < a.rows) stage(first, 0);
+        if (first < a.rows) {
+            if (D && a.topk > 0)
+                for (int q = 0; q < 2 && first + q * step < a.rows; ++q) {
+                    const Entry held[2] = {entry_at(first + q * step, lane), entry_at(first + q * step, lane + 32)};
+                    teacher(first + q * step, q, row_live(q), held);
+                }
+            else if (D && lane < 3) soft_s[lane] = 0;
+            __syncwarp();
+            const Row& r = row_s[0];
+            const T* z = logits(first);
+            const int e = end_of(r.span);
+            const T ends = z[max(e, 0)], zt = z[max(r.tok, 0)];
+            if (D)
+                for (int k = lane; k < a.topk; k += 32) z_s[0][k] = load(z + max(id_s[0][k], 0));
+            put_ends(0, e, ends, zt);
+        }
         __syncwarp();
+        int t0 = 0;                                   // it modulo 3
         for (int64_t row = first; row < a.rows; row += step, ++it) {
             const Row now = row_s[it & 3];
-            const int par = it & 1, top = a.topk;
+            const int par = it & 1, top = a.topk, t1 = t0 == 2 ? 0 : t0 + 1, t2 = t1 == 2 ? 0 : t1 + 1;
             const uint32_t ph = static_cast<uint32_t>(par);                // fin_bar and dense_bar: a phase a row
             bool counts = now.live;
-            // ---- 1
-            const int e = end_of(now.span);
-            const float e0 = counts && lane < 16 ? end_s[par][lane] : -CUDART_INF_F;
-            Stat st{e0, 0.f, 0.f};
-            if (e0 != -CUDART_INF_F) {                // exp of the one element against itself (a NaN stays one)
-                st.s = exp2_fast((e0 - e0) * c);
-                st.s1 = exp2_fast((e0 - e0) * kLog2e);
-            }
-            st = warp_merge<TWO>(st, c);
-            Top tp{-CUDART_INF_F, 0.f, 0.f};
-            if (D && counts) {
-                for (int k = lane; k < top; k += 32) tp.m = fmaxf(tp.m, a_s[par][k]);
-                for (int k = lane; k < top; k += 32) {
-                    const float x = a_s[par][k];
-                    if (x != -CUDART_INF_F) {         // an entry that the teacher rules out leaves the sums as they are
-                        const float w = shrink(x, tp.m, c);
-                        tp.s += w;
-                        tp.a += w * (x - tp.m);
-                    }
+            // ---- 1.  (A row is only overwritten by its gradient once all CTAs of a cluster have sent its sums, which
+            // they do after this warp has met their workers' barrier.)
+            const bool more = row + step < a.rows, more2 = row + 2 * step < a.rows, more3 = row + 3 * step < a.rows;
+            const Row& after = row_s[more ? (it + 1) & 3 : it & 3];
+            const T* za = logits(more ? row + step : row);
+            const int ea = end_of(after.span);
+            const T ends_raw = za[max(ea, 0)], zt_raw = za[max(after.tok, 0)];
+            T z_raw[2];
+            Entry held[2];
+            if (D && top > 0) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int k = min(lane + 32 * u, top - 1);
+                    z_raw[u] = za[max(id_s[more ? t1 : t0][k], 0)];
+                    held[u] = entry_at(more2 ? row + 2 * step : row, k);
                 }
-                tp = warp_merge(tp, c);
             }
-            const Pub pub{counts ? zt_s[par] : 0.f, D && tp.s != 0.f};
+            Side side{};
+            if (lane == 0) side = side_at<K>(a, more3 ? row + 3 * step : row);
+            // ---- 2
+            const int e = end_of(now.span);
+            Stat st{-CUDART_INF_F, 0.f, 0.f};
+            float e0 = -CUDART_INF_F;
+            if (now.span.head + now.span.elems < V || now.span.head) {
+                e0 = counts && lane < 16 ? end_s[par][lane] : -CUDART_INF_F;
+                if (e0 != -CUDART_INF_F) {            // exp of the one element against itself (a NaN stays one)
+                    st.m = e0;
+                    st.s = exp2_fast((e0 - e0) * c);
+                    st.s1 = exp2_fast((e0 - e0) * kLog2e);
+                }
+                st = warp_merge<TWO>(st, c);
+            }
+            const Pub pub{counts ? zt_s[par] : 0.f, D && counts && soft_s[t0]};
             if (lane == 0) {
                 stat_s[par][nw] = st;
                 pub_s[par] = pub;
@@ -461,39 +512,25 @@ __global__ void __launch_bounds__((kWorkers + 1) * 32) rows_kernel(const __grid_
             }
             __syncwarp();
             asm volatile("bar.arrive 1, %0;" ::"r"(nt + 32) : "memory");
-            // ---- 2
-            if (lane == 0 && grad && S > 1) {
-                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                fill();
-            }
             // ---- 3
-            const int64_t later = row + 3 * step;
-            Side side{};
-            if (lane == 0) side = side_at<K>(a, later < a.rows ? later : row);
-            if (row + step < a.rows) stage(row + step, it + 1);
-            if (lane == 0 && later < a.rows) prepare(later, it + 3, side);
-            __syncwarp();
-            // ---- 4
             wait(smem_u32(&fin_bar), ph, false, abort, a.err);
             st = fin_s[par];
             if (st.s == 0.f) counts = false;
             const Coef k = coef_of<K, TWO>(a, now, st, pub, counts);
             if (D) {
-                const float f = now.w * a.soft * a.inv_tau, inv = 1.f / tp.s;
                 const bool soft = counts && pub.soft;
                 float zq = 0.f;
-                for (int j = lane; j < top; j += 32) {
-                    const float x = a_s[par][j], w = !soft || x == -CUDART_INF_F ? 0.f : exp2_fast((x - tp.m) * c) * inv;
-                    q_s[j] = f * w;
-                    if (w != 0.f) zq += w * (z_s[par][j] - st.m);
-                }
+                if (soft)
+                    for (int j = lane; j < top; j += 32) {
+                        const float w = q_s[t0][j];
+                        if (w != 0.f) zq += w * (z_s[par][j] - st.m);
+                    }
                 zq = warp_sum(zq);
-                if (lane == 0) {
-                    q_s[top] = k.at_tok;
+                if (lane == 0 && rank == 0) {
                     float loss = 0.f;
-                    if (soft) loss = a.soft * ((tp.a * inv * a.inv_tau - log_fast(tp.s)) - (zq * a.inv_tau - log_fast(st.s)));
+                    if (soft) loss = a.soft * (teach_s[t0] - (zq * a.inv_tau - log_fast(st.s)));
                     if (counts && now.tok >= 0 && a.hard != 0.f) loss += a.hard * (log_fast(st.s1) - (pub.zt - st.m));
-                    if (rank == 0) a.row_loss[row] = loss;
+                    a.row_loss[row] = loss;
                 }
             } else if (lane == 0 && rank == 0) {
                 a.logp[row] = k.lp;
@@ -504,7 +541,11 @@ __global__ void __launch_bounds__((kWorkers + 1) * 32) rows_kernel(const __grid_
                     a.coef[row] = 0.f;
                 }
             }
-            // ---- 5
+            if (lane == 0 && grad && S > 1) {
+                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                fill();
+            }
+            // ---- 4
             wait(smem_u32(&dense_bar), ph, false, abort, a.err);
             if (grad) {
                 uint8_t* slot = slots + static_cast<size_t>(s) * a.slot_bytes;
@@ -516,56 +557,63 @@ __global__ void __launch_bounds__((kWorkers + 1) * 32) rows_kernel(const __grid_
                     if (TWO) g += k.dense1 * exp2_fast(d * kLog2e);
                     return g;
                 };
-                // the place of an id in this CTA's part of the row, or negative; its end that this CTA owns, or negative
+                // where an id lies: its place in this CTA's part of the row; -2 - i: the end i that this CTA owns; -1: elsewhere
                 auto place = [&](int32_t v) {
                     const int b = v - now.span.head - now.span.v0 * E;
-                    return b < now.span.nv * E ? b : -1;
-                };
-                auto at_end = [&](int32_t v) {
-                    return rank == 0 && v < now.span.head ? v : rank == C - 1 && v >= now.span.head + now.span.elems ? 8 + v - now.span.head - now.span.elems : -1;
+                    if (v < now.span.head) return rank == 0 ? -2 - v : -1;
+                    if (v >= now.span.head + now.span.elems) return rank == C - 1 ? -10 - (v - now.span.head - now.span.elems) : -1;
+                    return b < now.span.nv * E ? max(b, -1) : -1;
                 };
                 if (e >= 0) store(gradient(row) + e, counts ? at(e0) : 0.f);
                 __syncwarp();
                 if (!D && counts && lane == 0) {
-                    if (place(now.tok) >= 0) store(mine + place(now.tok), at(pub.zt) - k.at_tok);
-                    else if (at_end(now.tok) >= 0) store(gradient(row) + now.tok, at(pub.zt) - k.at_tok);
+                    const int b = place(now.tok);
+                    if (b != -1) store(b >= 0 ? mine + b : gradient(row) + now.tok, at(pub.zt) - k.at_tok);
                 }
                 if (D && counts) {
                     // Entries mark their places in the slot (or an end's) with their number.  One that finds another's
                     // mark there shares its id: it flags the mark, and the flagged mark's owner adds up all of that id.
                     using M = typename Vec<T>::Mark;
                     constexpr int kFlag = 1 << 14;
-                    auto id_at = [&](int j) { return id_s[par][j]; };
-                    auto mark_of = [&](int32_t v, int j, int op) {          // op 0: write j, 1: read, 2: flag
-                        const int b = place(v), x = b < 0 ? at_end(v) : -1;
-                        M* m = reinterpret_cast<M*>(slot) + (b >= 0 ? b : 0);
-                        if (b < 0 && x < 0) return -1;
-                        if (op == 0) { if (b >= 0) *m = static_cast<M>(j); else mark_s[x] = j; return j; }
-                        const int r = b >= 0 ? static_cast<int>(*m) : mark_s[x];
-                        if (op == 2) { if (b >= 0) *m = static_cast<M>(r | kFlag); else mark_s[x] = r | kFlag; }
-                        return r;
-                    };
-                    for (int j = lane; j <= top; j += 32) if (id_at(j) >= 0) mark_of(id_at(j), j, 0);
-                    __syncwarp();
-                    bool twice = false;
+                    const float f = now.w * a.soft * a.inv_tau;
+                    const int32_t* ids = id_s[t0];
+                    M* marks = reinterpret_cast<M*>(slot);
+                    auto value = [&](int j) { return j < top ? (pub.soft ? f * q_s[t0][j] : 0.f) : k.at_tok; };
+#pragma unroll 2
                     for (int j = lane; j <= top; j += 32) {
-                        if (id_at(j) < 0) continue;
-                        const int r = mark_of(id_at(j), j, 1);
-                        if (r >= 0 && (r & (kFlag - 1)) != j) { mark_of(id_at(j), j, 2); twice = true; }
+                        const int b = ids[j] >= 0 ? place(ids[j]) : -1;
+                        if (b >= 0) marks[b] = static_cast<M>(j);
+                        else if (b != -1) mark_s[-2 - b] = j;
                     }
-                    twice = __any_sync(~0u, twice);
                     __syncwarp();
+                    uint64_t lost = 0;                // bit u: entry lane + 32 u found another's mark
+#pragma unroll 2
                     for (int j = lane; j <= top; j += 32) {
-                        const int32_t v = id_at(j);
-                        const int r = v >= 0 ? mark_of(v, j, 1) : -1;
-                        if (r < 0 || (r & (kFlag - 1)) != j) continue;
-                        float g = q_s[j];
-                        if (twice && (r & kFlag)) {
-                            g = 0.f;
-                            for (int i = 0; i <= top; ++i) g += id_at(i) == v ? q_s[i] : 0.f;
+                        const int b = ids[j] >= 0 ? place(ids[j]) : -1;
+                        const int r = b >= 0 ? static_cast<int>(marks[b]) : b != -1 ? mark_s[-2 - b] : j;
+                        if ((r & (kFlag - 1)) != j) {
+                            lost |= uint64_t(1) << (j >> 5);
+                            if (b >= 0) marks[b] = static_cast<M>(r | kFlag);
+                            else mark_s[-2 - b] = r | kFlag;
                         }
-                        const float x = j < top ? z_s[par][j] : pub.zt;
-                        store(place(v) >= 0 ? mine + place(v) : gradient(row) + v, at(x) - g);
+                    }
+                    const bool twice = __any_sync(~0u, lost != 0);
+                    __syncwarp();
+#pragma unroll 2
+                    for (int j = lane; j <= top; j += 32) {
+                        const int32_t v = ids[j];
+                        const int b = v >= 0 ? place(v) : -1;
+                        if (b == -1) continue;
+                        float g = value(j);
+                        if (twice) {
+                            if (lost >> (j >> 5) & 1) continue;
+                            const int r = b >= 0 ? static_cast<int>(marks[b]) : mark_s[-2 - b];
+                            if (r & kFlag) {
+                                g = 0.f;
+                                for (int i = 0; i <= top; ++i) g += ids[i] == v ? value(i) : 0.f;
+                            }
+                        }
+                        store(b >= 0 ? mine + b : gradient(row) + v, at(j < top ? z_s[par][j] : pub.zt) - g);
                     }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    // the workers' writes and these, before the copy reads them
@@ -578,8 +626,23 @@ __global__ void __launch_bounds__((kWorkers + 1) * 32) rows_kernel(const __grid_
                     if (S == 1) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                 }
             }
-            if (lane == 0 && (!grad || S == 1)) fill();
             __syncwarp();
+            // ---- 5
+            if (more) {
+                put_ends(it + 1, ea, ends_raw, zt_raw);
+                if (D) {
+                    if (lane < top) z_s[par ^ 1][lane] = load(&z_raw[0]);
+                    if (lane + 32 < top) z_s[par ^ 1][lane + 32] = load(&z_raw[1]);
+                    for (int j = lane + 64; j < top; j += 32) z_s[par ^ 1][j] = load(za + max(id_s[t1][j], 0));
+                }
+            }
+            if (D && top > 0 && more2) teacher(row + 2 * step, t2, row_live(it + 2), held);
+            if (lane == 0) {
+                if (more3) prepare(row + 3 * step, it + 3, side);
+                if (!grad || S == 1) fill();          // without a gradient S rows ahead: the row just prepared
+            }
+            __syncwarp();
+            t0 = t1;
             if (++s == S) s = 0;
         }
         if (lane == 0) {

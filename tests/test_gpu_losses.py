@@ -440,3 +440,38 @@ def test_results_do_not_depend_on_the_launch():
         a = _run_distill(z, teacher, ids, labels, weight, 2.0, 1.0, 0.5)
         b = _run_distill(z, teacher, ids, labels, weight, 2.0, 1.0, 0.5)
         assert torch.equal(a[0], b[0]) and torch.equal(a[2], b[2])
+
+
+@pytest.mark.parametrize("vocab,rows", [(37, 9000), (2048, 5003), (8191, 3001), (32768, 1500), (65536, 700), (131071, 400)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_many_rows_a_group(vocab, rows, dt):
+    """Many more rows than the GPU takes at once: every row against 64-bit sums over all of them, with a gradient
+    and without one."""
+    dt = DT[dt]
+    gen = torch.Generator().manual_seed(17)
+    z = _logits(rows, vocab, dt, gen)
+    ids = torch.randint(0, vocab, (rows, 5), generator=gen).cuda()
+    teacher, labels = torch.randn(rows, 5, generator=gen).cuda(), torch.randint(0, vocab, (rows,), generator=gen).cuda()
+    weight = torch.ones(rows)
+    weight[::3] = 0
+    zc = z.clone()
+    loss, row, d = _run_distill(z, teacher, ids, labels, weight.cuda(), 2.0, 1.0, 0.5)
+    f_loss, f_row, _ = _run_distill(zc, teacher, ids, labels, weight.cuda(), 2.0, 1.0, 0.5, grad=False)
+    _, p_row, p_logp, _ = _run_policy(zc, labels, torch.zeros(rows, device="cuda"), torch.ones(rows, device="cuda"), None,
+                                      weight.cuda(), grad=False)
+    assert torch.equal(row, f_row) and torch.equal(loss, f_loss)
+    rel, q = _rel(zc[:50].float().cpu()) * 2, torch.softmax(teacher.double() / 2.0, 1)
+    for at in range(0, rows, 256):
+        part = slice(at, min(rows, at + 256))
+        x = zc[part].double()
+        lp, lp1 = torch.log_softmax(x / 2.0, 1), torch.log_softmax(x, 1).gather(1, labels[part, None])[:, 0]
+        want = (q[part] * (q[part].log() - lp.gather(1, ids[part]))).sum(1) - 0.5 * lp1
+        live = (weight[part] != 0).cuda()
+        assert ((row[part].double() - torch.where(live, want, 0)).abs() <= 8 * rel * (1 + want.abs())).all(), at
+        assert ((p_logp[part].double() - torch.where(live, lp1, 0)).abs() <= 8 * rel * (1 + lp1.abs())).all(), at
+        g = (0.5 * lp.exp() + 0.5 * torch.softmax(x, 1)).scatter_add_(1, ids[part], -0.5 * q[part])
+        g.scatter_add_(1, labels[part, None], torch.full((g.shape[0], 1), -0.5, device="cuda", dtype=torch.float64))
+        g = torch.where(live[:, None], g, 0)
+        tol = 16 * rel * (g.abs() + lp.exp() + torch.softmax(x, 1) + 1e-6) + (2.0 ** -8 * g.abs() if dt == torch.bfloat16 else 0)
+        tol.scatter_add_(1, ids[part], 16 * rel * q[part]).scatter_add_(1, labels[part, None], torch.full((g.shape[0], 1), 16 * rel, device="cuda").double())
+        assert ((d[part].double() - g).abs() <= tol).all(), at
