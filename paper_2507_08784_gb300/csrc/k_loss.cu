@@ -9,8 +9,8 @@
 // The rows kernel reads a row once and writes its gradient once.  A row, or with a cluster of C CTAs a
 // C-th of it, lies in a slot of shared memory: filled by a bulk copy while earlier rows are worked on,
 // reduced by the worker warps, overwritten by its own gradient and written back by a bulk copy.  The
-// CTAs of a cluster exchange (m, s) over distributed shared memory.  A service warp does everything else,
-// rows ahead or behind the workers: row data, copies, teacher entries, losses, single entries.
+// CTAs of a cluster exchange (m, s) over distributed shared memory.  Two service warps do everything else,
+// taking rows in turn: row data, copies, teacher entries, losses, single entries.
 #include <math_constants.h>
 
 #include <algorithm>
@@ -166,10 +166,10 @@ __device__ __forceinline__ Top warp_merge(Top x, float c) {
     return r;
 }
 
-constexpr int kWorkers = 15;                // warps on a row at most; one more is the service warp
+constexpr int kWorkers = 14;                // warps on a row at most; two more are service warps
 constexpr int kMaxSlots = 3;
 constexpr int kMaxCluster = 8;
-constexpr int kHeld = 9;                    // 16-byte vectors of a slot whose exponentials a thread keeps in registers
+constexpr int kHeld = 10;                   // 16-byte vectors of a slot whose exponentials a thread keeps in registers
 
 // `peers`: what other CTAs of the cluster wrote before they arrived is to be seen.
 __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity, bool peers) {
@@ -256,7 +256,7 @@ __device__ __forceinline__ Span span_of(const T* z, int vocab, int rank, int shi
     s.nv = min(s.v0 + per, n) - s.v0;
     return s;
 }
-// A row's data, prepared three rows ahead.
+// A row's data, prepared four rows ahead.
 struct __align__(16) Row {
     Span span;
     float w, adv, old, ref;
@@ -299,31 +299,34 @@ __device__ __forceinline__ Coef coef_of(const RowArgs& a, const Row& r, const St
     return k;
 }
 
-constexpr int64_t kSlotMax = kWorkers * 32 * kHeld * 16;     // of a row a CTA: 67.5 KiB, three slots fit
-constexpr int64_t kRingMax = 193 * 1024;               // beside up to 34 KiB of the service warp's
+constexpr int64_t kSlotMax = kWorkers * 32 * kHeld * 16;     // of a row a CTA: 70 KiB
+constexpr int64_t kRingMax = 196 * 1024;                     // three slots of 64 KiB and some bytes
 
 // HELD: a slot has at most kHeld vectors a worker thread, and the exponentials of the statistics stay in
 // registers for the gradient; else (rows of more than eight such slots) they are formed again.  TWO: a hard
 // term beside tau != 1, so that the sums are kept at two temperatures.
 //
 // A worker's row is: wait for the slot, sums, one barrier, the merge of all warps' sums (and of the cluster's
-// CTAs), the gradient into the slot.  What each of up to fifteen warps would do for itself is paid that many
-// times over, and a load's latency in this chain is lost to all of them, so the service warp does the rest:
-//   1 asks for the logits of row i + 1 that single entries need, the teacher's entries of row i + 2 and the
-//     data of row i + 3
+// CTAs), the gradient into the slot.  What each of up to fourteen warps would do for itself is paid that many
+// times over, and a load's latency in this chain is lost to all of them, so the service warps do the rest, each
+// for every second row i:
+//   1 asks for the ends, the token's logit and the teacher's entries of row i + 2, and for the data of rows
+//     i + 3 and i + 4
 //   2 the ends' sums and the token's logit of row i, before the workers' barrier
-//   3 the loss of row i, once its sums are there, and the fill of the slot whose row has been written back
-//   4 single entries of row i's gradient, once the workers have written theirs, and its write-back
-//   5 puts down what was asked for, and the teacher's softmax of row i + 2
+//   3 the loss of row i, once its sums are there
+//   4 single entries of row i's gradient, once the workers have written theirs, its write-back, and the fill of
+//     its slot with row i + S (S slots)
+//   5 puts down what was asked for, with the teacher's softmax
+// Their code is run once a row by one warp, so that it is bound by instruction fetch: its loops are kept rolled.
 template <int K, class T, bool HELD, bool TWO>
-__global__ void __launch_bounds__((kWorkers + 1) * 32) rows_kernel(const __grid_constant__ RowArgs a) {
+__global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_constant__ RowArgs a) {
     chain_begin();
     constexpr int E = Vec<T>::kElems, P = E / 2;
     constexpr int kKeep = HELD && K != kLogProb ? kHeld : 1;
     constexpr bool D = K == kDistill;
     constexpr int kList = D ? GLR_MAX_TOPK + 1 : 1;   // entries subtracted at single ids; the token is the last
     extern __shared__ __align__(128) uint8_t slots[];
-    __shared__ __align__(8) uint64_t full_bar[kMaxSlots], x_bar[2], fin_bar, dense_bar;
+    __shared__ __align__(8) uint64_t full_bar[kMaxSlots], x_bar[2], fin_bar[2], dense_bar[2];
     // by the row's parity, or (row_s) its number modulo four: who writes them again has passed a barrier that
     // all readers have reached
     __shared__ Row row_s[4];
@@ -331,13 +334,10 @@ __global__ void __launch_bounds__((kWorkers + 1) * 32) rows_kernel(const __grid_
     __shared__ __align__(16) float4 cluster_s[2][kMaxCluster];
     __shared__ Pub pub_s[2];
     __shared__ float end_s[2][16], zt_s[2];
-    __shared__ int32_t id_s[3][kList];                // by the row's number modulo three: ids, and their q (0: none)
-    __shared__ float q_s[3][kList], z_s[2][kList];
-    __shared__ float teach_s[3];                      // sum of q log q; NaN-free only where soft_s
-    __shared__ int32_t soft_s[3];
-    __shared__ int32_t mark_s[16];
+    __shared__ int32_t id_s[2][kList], mark_s[2][16];
+    __shared__ float q_s[2][kList], z_s[2][kList];
     __shared__ int abort_flag;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, nw = (blockDim.x >> 5) - 1, nt = nw * 32;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, nw = (blockDim.x >> 5) - 2, nt = nw * 32;
     const int C = 1 << a.cluster_shift, S = a.slots, V = static_cast<int>(a.vocab);
     uint32_t rank = 0;
     if (C > 1) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -346,10 +346,11 @@ __global__ void __launch_bounds__((kWorkers + 1) * 32) rows_kernel(const __grid_
     if (tid == 0) {
         abort_flag = 0;
         for (int q = 0; q < S; ++q) mbar_init(smem_u32(&full_bar[q]), 1);
-        mbar_init(smem_u32(&x_bar[0]), 1);
-        mbar_init(smem_u32(&x_bar[1]), 1);
-        mbar_init(smem_u32(&fin_bar), 1);
-        mbar_init(smem_u32(&dense_bar), nw);
+        for (int q = 0; q < 2; ++q) {
+            mbar_init(smem_u32(&x_bar[q]), 1);
+            mbar_init(smem_u32(&fin_bar[q]), 1);
+            mbar_init(smem_u32(&dense_bar[q]), nw);
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     const bool grad = K != kLogProb && a.dz != nullptr;
@@ -366,137 +367,133 @@ __global__ void __launch_bounds__((kWorkers + 1) * 32) rows_kernel(const __grid_
         r.same = ((reinterpret_cast<uintptr_t>(logits(row)) ^ reinterpret_cast<uintptr_t>(gradient(row))) & 15) == 0;
         row_s[it & 3] = r;
     };
-    if (warp == nw && lane < 3 && first + lane * step < a.rows) prepare(first + lane * step, lane, side_at<K>(a, first + lane * step));
+    if (warp == nw && lane < 4 && first + lane * step < a.rows) prepare(first + lane * step, lane, side_at<K>(a, first + lane * step));
     __syncthreads();
     if (C > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 
     int s = 0, it = 0;
     uint32_t use = 0, xuse = 0;
-    if (warp == nw) {
-        int fs = 0, fills = 0;
-        uint32_t fill_par = 0;                        // bit q: parity of slot q's last fill
-        auto fill = [&]() {                           // lane 0
-            const int64_t row = first + fills * step;
-            if (row >= a.rows) return;
-            const Row& r = row_s[fills & 3];
-            const uint32_t bytes = r.live ? static_cast<uint32_t>(r.span.nv) * 16u : 0u;
-            const uint32_t bar = smem_u32(&full_bar[fs]);
+    if (warp >= nw) {
+        const int sv = warp - nw;                     // rows sv, sv + 2, ..: their parity
+        auto fill = [&](int64_t row, int i, const Span& sp, bool live) {      // lane 0
+            const int q = i % S;
+            const uint32_t bytes = live ? static_cast<uint32_t>(sp.nv) * 16u : 0u, bar = smem_u32(&full_bar[q]);
             mbar_expect_tx(bar, bytes);
             if (bytes)
                 asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                             ::"r"(smem_u32(slots + static_cast<size_t>(fs) * a.slot_bytes)), "l"(logits(row) + r.span.head + static_cast<int64_t>(r.span.v0) * E),
+                             ::"r"(smem_u32(slots + static_cast<size_t>(q) * a.slot_bytes)), "l"(logits(row) + sp.head + static_cast<int64_t>(sp.v0) * E),
                              "r"(bytes), "r"(bar) : "memory");
-            if (fills >= S) fill_par ^= 1u << fs;
-            if (++fs == S) fs = 0;
-            ++fills;
         };
+        int filled = -1;                              // the last row that this warp filled a slot with
+        if (sv == 0 && lane == 0)
+            for (int q = 0; q < S; ++q)
+                if (first + q * step < a.rows) { fill(first + q * step, q, row_s[q].span, row_s[q].live); filled = q; }
         // the element of the ends that this lane owns, or -1: the head with the first CTA, the tail with the last
         auto end_of = [&](const Span& sp) {
             const int tail = V - sp.head - sp.elems;
             return rank == 0 && lane < sp.head ? lane : rank == C - 1 && lane >= 8 && lane < 8 + tail ? sp.head + sp.elems + lane - 8 : -1;
         };
-        // The teacher's entries k, k + 32 of a row, as they lie in memory (lanes past the end: the last one).
-        struct Entry { Word id; float a; };
-        auto entry_at = [&](int64_t row, int k) {
+        // What is asked for: the teacher's entries lane and lane + 32 as they lie in memory, and two logits.
+        struct Asked { Word id[2]; float a[2]; T end, zt; int e; };
+        auto entry = [&](int64_t row, int k, Word& id, float& t) {
             k = min(k, a.topk - 1);
             const int64_t at = row * a.ldt + k;
-            return Entry{word_at(a.ids, row * a.ldi + k),
-                         a.teacher_bf16 ? __uint_as_float(static_cast<const uint16_t*>(a.teacher)[at]) : static_cast<const float*>(a.teacher)[at]};
+            id = word_at(a.ids, row * a.ldi + k);
+            t = a.teacher_bf16 ? __uint_as_float(static_cast<const uint16_t*>(a.teacher)[at]) : static_cast<const float*>(a.teacher)[at];
         };
-        // Their softmax into q_s, ids into id_s: entries of the first two lots from registers, others from memory.
-        auto teacher = [&](int64_t row, int slot3, bool live, const Entry (&held)[2]) {
+        auto ask = [&](int64_t row, const Row& r, Asked& x) {
+            const T* z = logits(row);
+            x.e = end_of(r.span);
+            x.end = z[max(x.e, 0)];
+            x.zt = z[max(r.tok, 0)];
+            if (D && a.topk > 0) {
+                entry(row, lane, x.id[0], x.a[0]);
+                entry(row, lane + 32, x.id[1], x.a[1]);
+            }
+        };
+        float teach = 0.f;                            // sum of q log q of the row put down last
+        bool soft_next = false;
+        // ... and put down: ids, their q, their logits.  (A row is only overwritten by its gradient once all CTAs of
+        // a cluster have sent its sums, which they do after this warp has met their workers' barrier.)
+        auto put = [&](int64_t row, const Row& r, const Asked& x) {
+            if (lane < 16) end_s[sv][lane] = x.e >= 0 ? load(&x.end) : -CUDART_INF_F;
+            if (lane == 0) zt_s[sv] = load(&x.zt);
+            if (!D) return;
+            if (lane == 0) id_s[sv][a.topk] = r.live && a.hard != 0.f ? r.tok : -1;
             float m = -CUDART_INF_F;
-            auto take = [&](int k, const Entry& x) {
-                const int32_t id = live ? index_of(x.id, a.ids.wide, V) : -1;
-                const float t = id < 0 ? -CUDART_INF_F : a.teacher_bf16 ? __uint_as_float(__float_as_uint(x.a) << 16) : x.a;
-                id_s[slot3][k] = id;
-                q_s[slot3][k] = t;
+            auto take = [&](int k, const Word& word, float bits) {
+                const int32_t id = r.live ? index_of(word, a.ids.wide, V) : -1;
+                const float t = id < 0 ? -CUDART_INF_F : a.teacher_bf16 ? __uint_as_float(__float_as_uint(bits) << 16) : bits;
+                id_s[sv][k] = id;
+                q_s[sv][k] = t;
                 m = fmaxf(m, t);
             };
-            if (lane < a.topk) take(lane, held[0]);
-            if (lane + 32 < a.topk) take(lane + 32, held[1]);
-#pragma unroll 2
-            for (int k = lane + 64; k < a.topk; k += 32) take(k, entry_at(row, k));
+            if (lane < a.topk) take(lane, x.id[0], x.a[0]);
+            if (lane + 32 < a.topk) take(lane + 32, x.id[1], x.a[1]);
+#pragma unroll 1
+            for (int k = lane + 64; k < a.topk; k += 32) {
+                Word id;
+                float t;
+                entry(row, k, id, t);
+                take(k, id, t);
+            }
+            const T* z = logits(row);
+            const T z0 = z[lane < a.topk ? max(id_s[sv][lane], 0) : 0], z1 = z[lane + 32 < a.topk ? max(id_s[sv][lane + 32], 0) : 0];
             m = warp_max(m);
             float sum = 0.f, ta = 0.f;
+#pragma unroll 1
             for (int k = lane; k < a.topk; k += 32) {
-                const float t = q_s[slot3][k];
+                const float t = q_s[sv][k];
                 float w = 0.f;
                 if (t != -CUDART_INF_F) {             // an entry that the teacher rules out leaves the sums as they are
                     w = exp2_fast((t - m) * c);
                     sum += w;
                     ta += w * (t - m);
                 }
-                q_s[slot3][k] = w;
+                q_s[sv][k] = w;
             }
             sum = warp_sum(sum);
             ta = warp_sum(ta);
             const float inv = sum != 0.f ? 1.f / sum : 0.f;
-            for (int k = lane; k < a.topk; k += 32) q_s[slot3][k] *= inv;
-            if (lane == 0) {
-                teach_s[slot3] = ta * inv * a.inv_tau - log_fast(sum);
-                soft_s[slot3] = sum != 0.f;
-            }
+            teach = ta * inv * a.inv_tau - log_fast(sum);
+            soft_next = sum != 0.f;
+#pragma unroll 1
+            for (int k = lane; k < a.topk; k += 32) q_s[sv][k] *= inv;
+            if (lane < a.topk) z_s[sv][lane] = load(&z0);
+            if (lane + 32 < a.topk) z_s[sv][lane + 32] = load(&z1);
+#pragma unroll 4
+            for (int k = lane + 64; k < a.topk; k += 32) z_s[sv][k] = load(z + max(id_s[sv][k], 0));
         };
-        auto row_live = [&](int q) { return row_s[q & 3].live != 0; };
-        // Puts down the logits at a row's ends and token.
-        auto put_ends = [&](int q, int e, const T& ends, const T& zt) {
-            if (lane < 16) end_s[q & 1][lane] = e >= 0 ? load(&ends) : -CUDART_INF_F;
-            if (lane == 0) {
-                zt_s[q & 1] = load(&zt);
-                if (D) id_s[q % 3][a.topk] = row_live(q) && a.hard != 0.f ? row_s[q & 3].tok : -1;
-            }
-        };
-        if (lane == 0)
-            for (int q = 0; q < (grad && S > 1 ? S - 1 : S); ++q) fill();
-        if (first < a.rows) {
-            if (D && a.topk > 0)
-                for (int q = 0; q < 2 && first + q * step < a.rows; ++q) {
-                    const Entry held[2] = {entry_at(first + q * step, lane), entry_at(first + q * step, lane + 32)};
-                    teacher(first + q * step, q, row_live(q), held);
-                }
-            else if (D && lane < 3) soft_s[lane] = 0;
-            __syncwarp();
-            const Row& r = row_s[0];
-            const T* z = logits(first);
-            const int e = end_of(r.span);
-            const T ends = z[max(e, 0)], zt = z[max(r.tok, 0)];
-            if (D)
-                for (int k = lane; k < a.topk; k += 32) z_s[0][k] = load(z + max(id_s[0][k], 0));
-            put_ends(0, e, ends, zt);
+        const int64_t step2 = 2 * step;
+        if (first + sv * step < a.rows) {
+            Asked x;
+            ask(first + sv * step, row_s[sv], x);
+            put(first + sv * step, row_s[sv], x);
         }
         __syncwarp();
-        int t0 = 0;                                   // it modulo 3
-        for (int64_t row = first; row < a.rows; row += step, ++it) {
+        it = sv;
+        for (int64_t row = first + sv * step; row < a.rows; row += step2, it += 2) {
             const Row now = row_s[it & 3];
-            const int par = it & 1, top = a.topk, t1 = t0 == 2 ? 0 : t0 + 1, t2 = t1 == 2 ? 0 : t1 + 1;
-            const uint32_t ph = static_cast<uint32_t>(par);                // fin_bar and dense_bar: a phase a row
+            const int top = a.topk;
+            const uint32_t ph = static_cast<uint32_t>(it >> 1) & 1u;
             bool counts = now.live;
-            // ---- 1.  (A row is only overwritten by its gradient once all CTAs of a cluster have sent its sums, which
-            // they do after this warp has met their workers' barrier.)
-            const bool more = row + step < a.rows, more2 = row + 2 * step < a.rows, more3 = row + 3 * step < a.rows;
-            const Row& after = row_s[more ? (it + 1) & 3 : it & 3];
-            const T* za = logits(more ? row + step : row);
-            const int ea = end_of(after.span);
-            const T ends_raw = za[max(ea, 0)], zt_raw = za[max(after.tok, 0)];
-            T z_raw[2];
-            Entry held[2];
-            if (D && top > 0) {
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int k = min(lane + 32 * u, top - 1);
-                    z_raw[u] = za[max(id_s[more ? t1 : t0][k], 0)];
-                    held[u] = entry_at(more2 ? row + 2 * step : row, k);
-                }
+            const float tq = teach;
+            // ---- 1
+            const bool more = row + step2 < a.rows, more4 = row + 4 * step < a.rows;
+            const int64_t row_f = row + S * step;
+            Asked asked;
+            ask(more ? row + step2 : row, row_s[(more ? it + 2 : it) & 3], asked);
+            Side side{}, side_f{};
+            if (lane == 0) {
+                side = side_at<K>(a, more4 ? row + 4 * step : row);
+                side_f = side_at<K>(a, row_f < a.rows ? row_f : row);
             }
-            Side side{};
-            if (lane == 0) side = side_at<K>(a, more3 ? row + 3 * step : row);
             // ---- 2
             const int e = end_of(now.span);
             Stat st{-CUDART_INF_F, 0.f, 0.f};
             float e0 = -CUDART_INF_F;
             if (now.span.head + now.span.elems < V || now.span.head) {
-                e0 = counts && lane < 16 ? end_s[par][lane] : -CUDART_INF_F;
+                e0 = counts && lane < 16 ? end_s[sv][lane] : -CUDART_INF_F;
                 if (e0 != -CUDART_INF_F) {            // exp of the one element against itself (a NaN stays one)
                     st.m = e0;
                     st.s = exp2_fast((e0 - e0) * c);
@@ -504,31 +501,34 @@ __global__ void __launch_bounds__((kWorkers + 1) * 32) rows_kernel(const __grid_
                 }
                 st = warp_merge<TWO>(st, c);
             }
-            const Pub pub{counts ? zt_s[par] : 0.f, D && counts && soft_s[t0]};
+            const Pub pub{counts ? zt_s[sv] : 0.f, D && counts && soft_next};
             if (lane == 0) {
-                stat_s[par][nw] = st;
-                pub_s[par] = pub;
-                if (C > 1) mbar_expect_tx(smem_u32(&x_bar[par]), 16u * C);
+                stat_s[sv][nw] = st;
+                pub_s[sv] = pub;
+                if (C > 1) mbar_expect_tx(smem_u32(&x_bar[sv]), 16u * C);
             }
             __syncwarp();
-            asm volatile("bar.arrive 1, %0;" ::"r"(nt + 32) : "memory");
+            if (sv) asm volatile("bar.arrive 2, %0;" ::"r"(nt + 32) : "memory");
+            else asm volatile("bar.arrive 1, %0;" ::"r"(nt + 32) : "memory");
             // ---- 3
-            wait(smem_u32(&fin_bar), ph, false, abort, a.err);
-            st = fin_s[par];
+            wait(smem_u32(&fin_bar[sv]), ph, false, abort, a.err);
+            st = fin_s[sv];
             if (st.s == 0.f) counts = false;
             const Coef k = coef_of<K, TWO>(a, now, st, pub, counts);
             if (D) {
                 const bool soft = counts && pub.soft;
                 float zq = 0.f;
-                if (soft)
+                if (soft) {
+#pragma unroll 1
                     for (int j = lane; j < top; j += 32) {
-                        const float w = q_s[t0][j];
-                        if (w != 0.f) zq += w * (z_s[par][j] - st.m);
+                        const float w = q_s[sv][j];
+                        if (w != 0.f) zq += w * (z_s[sv][j] - st.m);
                     }
-                zq = warp_sum(zq);
+                    zq = warp_sum(zq);
+                }
                 if (lane == 0 && rank == 0) {
                     float loss = 0.f;
-                    if (soft) loss = a.soft * (teach_s[t0] - (zq * a.inv_tau - log_fast(st.s)));
+                    if (soft) loss = a.soft * (tq - (zq * a.inv_tau - log_fast(st.s)));
                     if (counts && now.tok >= 0 && a.hard != 0.f) loss += a.hard * (log_fast(st.s1) - (pub.zt - st.m));
                     a.row_loss[row] = loss;
                 }
@@ -541,14 +541,10 @@ __global__ void __launch_bounds__((kWorkers + 1) * 32) rows_kernel(const __grid_
                     a.coef[row] = 0.f;
                 }
             }
-            if (lane == 0 && grad && S > 1) {
-                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                fill();
-            }
             // ---- 4
-            wait(smem_u32(&dense_bar), ph, false, abort, a.err);
+            wait(smem_u32(&dense_bar[sv]), ph, false, abort, a.err);
             if (grad) {
-                uint8_t* slot = slots + static_cast<size_t>(s) * a.slot_bytes;
+                uint8_t* slot = slots + static_cast<size_t>(it % S) * a.slot_bytes;
                 T* body = gradient(row) + now.span.head + static_cast<int64_t>(now.span.v0) * E;
                 T* mine = now.same ? reinterpret_cast<T*>(slot) : body;
                 auto at = [&](float x) {
@@ -576,44 +572,46 @@ __global__ void __launch_bounds__((kWorkers + 1) * 32) rows_kernel(const __grid_
                     using M = typename Vec<T>::Mark;
                     constexpr int kFlag = 1 << 14;
                     const float f = now.w * a.soft * a.inv_tau;
-                    const int32_t* ids = id_s[t0];
+                    const int32_t* ids = id_s[sv];
                     M* marks = reinterpret_cast<M*>(slot);
-                    auto value = [&](int j) { return j < top ? (pub.soft ? f * q_s[t0][j] : 0.f) : k.at_tok; };
-#pragma unroll 2
-                    for (int j = lane; j <= top; j += 32) {
+                    auto value = [&](int j) { return j < top ? (pub.soft ? f * q_s[sv][j] : 0.f) : k.at_tok; };
+                    const int n = id_s[sv][top] >= 0 ? top + 1 : top;
+#pragma unroll 1
+                    for (int j = lane; j < n; j += 32) {
                         const int b = ids[j] >= 0 ? place(ids[j]) : -1;
                         if (b >= 0) marks[b] = static_cast<M>(j);
-                        else if (b != -1) mark_s[-2 - b] = j;
+                        else if (b != -1) mark_s[sv][-2 - b] = j;
                     }
                     __syncwarp();
                     uint64_t lost = 0;                // bit u: entry lane + 32 u found another's mark
-#pragma unroll 2
-                    for (int j = lane; j <= top; j += 32) {
+#pragma unroll 1
+                    for (int j = lane; j < n; j += 32) {
                         const int b = ids[j] >= 0 ? place(ids[j]) : -1;
-                        const int r = b >= 0 ? static_cast<int>(marks[b]) : b != -1 ? mark_s[-2 - b] : j;
+                        const int r = b >= 0 ? static_cast<int>(marks[b]) : b != -1 ? mark_s[sv][-2 - b] : j;
                         if ((r & (kFlag - 1)) != j) {
                             lost |= uint64_t(1) << (j >> 5);
                             if (b >= 0) marks[b] = static_cast<M>(r | kFlag);
-                            else mark_s[-2 - b] = r | kFlag;
+                            else mark_s[sv][-2 - b] = r | kFlag;
                         }
                     }
                     const bool twice = __any_sync(~0u, lost != 0);
                     __syncwarp();
-#pragma unroll 2
-                    for (int j = lane; j <= top; j += 32) {
+#pragma unroll 1
+                    for (int j = lane; j < n; j += 32) {
                         const int32_t v = ids[j];
                         const int b = v >= 0 ? place(v) : -1;
                         if (b == -1) continue;
                         float g = value(j);
                         if (twice) {
                             if (lost >> (j >> 5) & 1) continue;
-                            const int r = b >= 0 ? static_cast<int>(marks[b]) : mark_s[-2 - b];
+                            const int r = b >= 0 ? static_cast<int>(marks[b]) : mark_s[sv][-2 - b];
                             if (r & kFlag) {
                                 g = 0.f;
-                                for (int i = 0; i <= top; ++i) g += ids[i] == v ? value(i) : 0.f;
+#pragma unroll 1
+                                for (int i = 0; i < n; ++i) g += ids[i] == v ? value(i) : 0.f;
                             }
                         }
-                        store(b >= 0 ? mine + b : gradient(row) + v, at(j < top ? z_s[par][j] : pub.zt) - g);
+                        store(b >= 0 ? mine + b : gradient(row) + v, at(j < top ? z_s[sv][j] : pub.zt) - g);
                     }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    // the workers' writes and these, before the copy reads them
@@ -623,34 +621,26 @@ __global__ void __launch_bounds__((kWorkers + 1) * 32) rows_kernel(const __grid_
                         asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
                                      ::"l"(body), "r"(smem_u32(slot)), "r"(static_cast<uint32_t>(now.span.nv) * 16u) : "memory");
                     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                    if (S == 1) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                 }
             }
             __syncwarp();
-            // ---- 5
-            if (more) {
-                put_ends(it + 1, ea, ends_raw, zt_raw);
-                if (D) {
-                    if (lane < top) z_s[par ^ 1][lane] = load(&z_raw[0]);
-                    if (lane + 32 < top) z_s[par ^ 1][lane + 32] = load(&z_raw[1]);
-                    for (int j = lane + 64; j < top; j += 32) z_s[par ^ 1][j] = load(za + max(id_s[t1][j], 0));
-                }
-            }
-            if (D && top > 0 && more2) teacher(row + 2 * step, t2, row_live(it + 2), held);
+            // ---- 5, and the slot's next row once it has been read
+            if (more) put(row + step2, row_s[(it + 2) & 3], asked);
             if (lane == 0) {
-                if (more3) prepare(row + 3 * step, it + 3, side);
-                if (!grad || S == 1) fill();          // without a gradient S rows ahead: the row just prepared
+                if (row_f < a.rows) {
+                    if (grad) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    fill(row_f, it + S, span_of(logits(row_f), V, rank, a.cluster_shift), is_live<K>(a, side_f));
+                    filled = it + S;
+                }
+                if (more4) prepare(row + 4 * step, it + 4, side);
             }
             __syncwarp();
-            t0 = t1;
-            if (++s == S) s = 0;
         }
         if (lane == 0) {
             if (grad) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-            if (*abort)                               // let the copies already issued land
-                for (int q = 0; q < S; ++q)
-                    if (q < fills)
-                        for (int i = 0; i < 4000000 && !try_wait(smem_u32(&full_bar[q]), fill_par >> q & 1u, false); ++i) __nanosleep(64);
+            if (*abort)                               // let the copies that this warp issued land
+                for (int i = max(filled - 3, 0); i <= filled; ++i)
+                    for (int q = 0; q < 1000000 && !try_wait(smem_u32(&full_bar[i % S]), static_cast<uint32_t>(i / S) & 1u, false); ++q) __nanosleep(64);
         }
     } else {
         for (int64_t row = first; row < a.rows; row += step, ++it) {
@@ -716,7 +706,8 @@ __global__ void __launch_bounds__((kWorkers + 1) * 32) rows_kernel(const __grid_
             st = warp_merge<TWO>(st, c);
             if (lane == 0) stat_s[par][warp] = st;
             __syncwarp();
-            asm volatile("bar.sync 1, %0;" ::"r"(nt + 32) : "memory");
+            if (par) asm volatile("bar.sync 2, %0;" ::"r"(nt + 32) : "memory");
+            else asm volatile("bar.sync 1, %0;" ::"r"(nt + 32) : "memory");
             st = warp_merge<TWO>(lane <= nw ? stat_s[par][lane] : Stat{-CUDART_INF_F, 0.f, 0.f}, c);
             const Pub pub = pub_s[par];
             if (C > 1) {
@@ -732,7 +723,7 @@ __global__ void __launch_bounds__((kWorkers + 1) * 32) rows_kernel(const __grid_
             if (!TWO) st.s1 = st.s;
             if (tid == 0) {
                 fin_s[par] = st;
-                tc::mbar_arrive(smem_u32(&fin_bar));
+                tc::mbar_arrive(smem_u32(&fin_bar[par]));
             }
             if (st.s == 0.f) counts = false;
             // ---- the gradient
@@ -779,7 +770,7 @@ __global__ void __launch_bounds__((kWorkers + 1) * 32) rows_kernel(const __grid_
                 }
             }
             __syncwarp();
-            if (lane == 0) tc::mbar_arrive(smem_u32(&dense_bar));
+            if (lane == 0) tc::mbar_arrive(smem_u32(&dense_bar[par]));
             if (++s == S) { s = 0; use ^= 1u; }
             if (par) xuse ^= 1u;
         }
@@ -793,22 +784,29 @@ __global__ void __launch_bounds__((kWorkers + 1) * 32) rows_kernel(const __grid_
 
 constexpr int kThreads = 512;
 
-// Sums of a sequence's log-probabilities in 64 bits, thread by thread and then up the same tree.
-__device__ double block_sum(double x, double* scratch) {
-    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
+// Sums as pairs of floats, the second one the rounding errors of the first (64-bit arithmetic runs at a
+// hundredth of the rate here): thread by thread, then up a tree, in a fixed order.
+struct Pair { float hi, lo; };
+__device__ __forceinline__ Pair plus(const Pair& x, const Pair& y) {
+    const float s = x.hi + y.hi, b = s - x.hi, err = (x.hi - (s - b)) + (y.hi - b);
+    return {s, isfinite(s) ? err + x.lo + y.lo : 0.f};
+}
+__device__ Pair block_sum(Pair x, Pair* scratch) {
+    for (int d = 16; d; d >>= 1) x = plus(x, Pair{__shfl_xor_sync(~0u, x.hi, d), __shfl_xor_sync(~0u, x.lo, d)});
     __syncthreads();
     if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = x;
     __syncthreads();
-    double r = 0;
-    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) r += scratch[w];
-    return r;
+    const int lane = threadIdx.x & 31;
+    x = lane < static_cast<int>(blockDim.x >> 5) ? scratch[lane] : Pair{0.f, 0.f};
+    for (int d = 16; d; d >>= 1) x = plus(x, Pair{__shfl_xor_sync(~0u, x.hi, d), __shfl_xor_sync(~0u, x.lo, d)});
+    return x;
 }
 
 constexpr int kPairThreads = 256;
 // One CTA a pair.
 __global__ void __launch_bounds__(kPairThreads) pairs_kernel(const PairArgs a) {
     chain_begin();
-    __shared__ double scratch[kPairThreads / 32];
+    __shared__ Pair scratch[kPairThreads / 32];
     const int64_t p = blockIdx.x;
     int64_t at[2][2];
     float seq[2], share[2];
@@ -817,19 +815,21 @@ __global__ void __launch_bounds__(kPairThreads) pairs_kernel(const PairArgs a) {
         b = b < 0 ? 0 : b > a.rows ? a.rows : b;
         e = e < b ? b : e > a.rows ? a.rows : e;
         at[h][0] = b; at[h][1] = e;
-        double sum = 0, cnt = 0;
+        Pair sum{0.f, 0.f};
+        int cnt = 0;
         for (int64_t t = b + threadIdx.x; t < e; t += kPairThreads) {
-            sum += a.row_logp[t];
+            sum = plus(sum, Pair{a.row_logp[t], 0.f});
             cnt += a.lse[t] != CUDART_INF_F;
         }
         sum = block_sum(sum, scratch);
         share[h] = 1.f;
+        seq[h] = sum.hi + sum.lo;
         if (a.average) {
-            cnt = block_sum(cnt, scratch);
-            share[h] = static_cast<float>(1.0 / (cnt < 1 ? 1 : cnt));
-            sum /= cnt < 1 ? 1 : cnt;
+            // (the number of tokens, exactly: its two halves as floats)
+            const Pair n = block_sum(Pair{static_cast<float>(cnt), 0.f}, scratch);
+            share[h] = 1.f / fmaxf(n.hi + n.lo, 1.f);
+            seq[h] = seq[h] / fmaxf(n.hi + n.lo, 1.f);
         }
-        seq[h] = static_cast<float>(sum);
     }
     const float w = a.weight ? a.weight[p] : a.share;
     const float h = (seq[0] - (a.ref_logp ? a.ref_logp[2 * p] : 0.f)) - (seq[1] - (a.ref_logp ? a.ref_logp[2 * p + 1] : 0.f));
@@ -880,14 +880,17 @@ constexpr int kTotalThreads = 1024;
 __global__ void __launch_bounds__(kTotalThreads) total_kernel(const float* x, const float* weight, float share, int64_t n,
                                                               float* out) {
     chain_begin();
-    __shared__ double scratch[kTotalThreads / 32];
-    double s = 0;
+    __shared__ Pair scratch[kTotalThreads / 32];
+    Pair s{0.f, 0.f};
     for (int64_t i = threadIdx.x; i < n; i += kTotalThreads) {
-        const float w = weight ? weight[i] : share;
-        if (w != 0.f) s += static_cast<double>(w) * x[i];
+        const float w = weight ? weight[i] : share, v = x[i];
+        if (w != 0.f) {
+            const float p = w * v;
+            s = plus(s, Pair{p, isfinite(p) ? fmaf(w, v, -p) : 0.f});
+        }
     }
     s = block_sum(s, scratch);
-    if (threadIdx.x == 0) *out = static_cast<float>(s);
+    if (threadIdx.x == 0) *out = s.hi + s.lo;
 }
 
 // Shape of a launch: how many CTAs share a row, their slots and threads.
@@ -925,7 +928,7 @@ cudaError_t rows_launch(RowArgs a, int dtype, cudaStream_t st) {
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = C; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.blockDim = (workers + 1) * 32; cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cfg.blockDim = (workers + 2) * 32; cfg.dynamicSmemBytes = smem; cfg.stream = st;
     cfg.attrs = attr; cfg.numAttrs = 2;
     // as many groups of CTAs as run at once, each with its share of the rows
     int64_t groups = a.rows;
@@ -933,7 +936,7 @@ cudaError_t rows_launch(RowArgs a, int dtype, cudaStream_t st) {
         int per = 0;
         cfg.gridDim = C;
         if (C > 1) e = cudaOccupancyMaxActiveClusters(&per, kernel, &cfg);
-        else if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, (workers + 1) * 32, smem)) == cudaSuccess) per *= sms;
+        else if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, (workers + 2) * 32, smem)) == cudaSuccess) per *= sms;
         if (e != cudaSuccess) return e;
         groups = std::min<int64_t>(groups, std::max(per, 1));
     }
