@@ -439,7 +439,7 @@ int glr_linear_grad_weight(const glr_linear_grad_weight_args* a, void* stream);
  * its weight were 0.  Logits of -infinity are entries ruled out: probability and gradient zero.
  * dlogits (rows x vocab of dtype) may be null (no gradient is formed) or logits itself with the
  * same ld.  Indices (ids, labels, tokens, offsets) are int32, or int64 where index64 is 1.  A row
- * of logits is at most GLR_MAX_LOGIT_BYTES long.                                                 */
+ * of logits is at most GLR_MAX_LOGIT_BYTES long, and there are at most 2^24 rows.                 */
 #define GLR_MAX_LOGIT_BYTES 1572864
 
 /* Distillation from a teacher's top logits.  Row t of teacher (rows x topk, teacher_dtype) holds

@@ -59,13 +59,13 @@ bool vector_ok(const void* p, int64_t n, int64_t bytes) {
 }
 bool optional_ok(const void* p, int64_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 
-constexpr int64_t kMaxRows = int64_t(1) << 40;
+constexpr int64_t kMaxRows = int64_t(1) << 24;
 
 // The checks all losses share.
 int check_logits(const char* who, int64_t rows, int64_t vocab, const void* z, int64_t ldz, void* dz, int64_t lddz,
                  const float* weight, float* loss, int dtype) {
     if (!dtype_ok(dtype)) return refuse("%s: unknown dtype %d", who, dtype);
-    if (rows < 0 || rows > kMaxRows) return refuse("%s: need 0 <= rows <= 2^40", who);
+    if (rows < 0 || rows > kMaxRows) return refuse("%s: need 0 <= rows <= 2^24", who);
     if (vocab < 1 || vocab > GLR_MAX_LOGIT_BYTES || vocab * bytes_of(dtype) > GLR_MAX_LOGIT_BYTES)
         return refuse("%s: need vocab >= 1 and rows of logits of at most %d bytes", who, GLR_MAX_LOGIT_BYTES);
     if (!matrix_ok(z, ldz, rows, vocab, dtype)) return refuse("%s: logits null, misaligned or with ld < vocab", who);

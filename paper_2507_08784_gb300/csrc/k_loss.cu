@@ -782,7 +782,7 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
     }
 }
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 256;
 
 // Sums as pairs of floats, the second one the rounding errors of the first (64-bit arithmetic runs at a
 // hundredth of the rate here): thread by thread, then up a tree, in a fixed order.
@@ -857,22 +857,67 @@ __global__ void __launch_bounds__(kPairThreads) pairs_kernel(const PairArgs a) {
     }
 }
 
+// Sixteen bytes past the caches' keeping: the second and last read of a row, and its gradient.
+__device__ __forceinline__ uint4 load_last(const void* p) {
+    uint4 u;
+    asm volatile("ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
+    return u;
+}
+__device__ __forceinline__ void store_last(void* p, const uint4& u) {
+    asm volatile("st.global.cs.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(u.x), "r"(u.y), "r"(u.z), "r"(u.w) : "memory");
+}
+
+// dz = coef (e_token - exp(z - lse)): the second pass over a preference batch's rows, a piece of a row a CTA.  Rows are taken from the last one back: the sums' pass ended there, and the L2 still holds some
+// 100 MB of it.  Bound by HBM: one read, one write.
+constexpr int kPieceVecs = 4;
 template <class T>
-__global__ void __launch_bounds__(kThreads) grad_kernel(const RowArgs a) {
+__global__ void __launch_bounds__(kThreads) grad_kernel(const RowArgs a, int pieces) {
     chain_begin();
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const T* z = static_cast<const T*>(a.z) + row * a.ldz;
-        T* dz = static_cast<T*>(a.dz) + row * a.lddz;
-        const float coef = a.coef[row], lse = a.lse[row];
-        const int64_t tok = coef == 0.f ? -1 : a.tokens.at(row);
-        for (int64_t v = threadIdx.x; v < a.vocab; v += kThreads) {
-            float g = 0.f;
-            if (coef != 0.f) {
-                const float p = exp2_fast((load(z + v) - lse) * kLog2e);
-                g = v == tok ? coef - coef * p : -coef * p;
+    constexpr int E = Vec<T>::kElems, P = E / 2;
+    const int64_t row = a.rows - 1 - blockIdx.x / pieces;
+    const int piece = static_cast<int>(blockIdx.x % pieces), V = static_cast<int>(a.vocab), tid = threadIdx.x;
+    const T* z = static_cast<const T*>(a.z) + row * a.ldz;
+    T* dz = static_cast<T*>(a.dz) + row * a.lddz;
+    const float coef = a.coef[row], lse = a.lse[row];
+    const int32_t tok = index_of(word_at(a.tokens, row), a.tokens.wide, V);
+    const bool zero = coef == 0.f;
+    auto at = [&](float x, int v) {
+        const float g = -coef * exp2_fast((x - lse) * kLog2e);
+        return v == tok ? g + coef : g;
+    };
+    const Span sp = span_of(z, V, 0, 0);
+    if (piece == 0) {                                 // the unaligned ends
+        const int v = tid < sp.head ? tid : tid >= 32 && tid < 32 + V - sp.head - sp.elems ? sp.head + sp.elems + tid - 32 : -1;
+        if (v >= 0) store(dz + v, zero ? 0.f : at(load(z + v), v));
+    }
+    const bool same = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0;
+    const int v0 = piece * (kThreads * kPieceVecs) + tid;
+    uint4 u[kPieceVecs];
+    if (!zero) {
+#pragma unroll
+        for (int q = 0; q < kPieceVecs; ++q)
+            if (v0 + q * kThreads < sp.nv) u[q] = load_last(z + sp.head + static_cast<int64_t>(v0 + q * kThreads) * E);
+    }
+    const uint64_t nl = pack2(-lse, -lse), l2 = pack2(kLog2e, kLog2e), nc = pack2(-coef, -coef);
+#pragma unroll
+    for (int q = 0; q < kPieceVecs; ++q) {
+        const int v = v0 + q * kThreads, b = tok - sp.head - v * E;
+        if (v >= sp.nv) break;
+        uint4 r = make_uint4(0, 0, 0, 0);
+        if (!zero) {
+            uint64_t x[P];
+            Vec<T>::get(u[q], x);
+#pragma unroll
+            for (int i = 0; i < P; ++i) x[i] = mul2(nc, exp2_2(mul2(add2(x[i], nl), l2)));
+            if (tok >= 0 && b >= 0 && b < E) {
+#pragma unroll
+                for (int i = 0; i < P; ++i) x[i] = add2(x[i], pack2(b == 2 * i ? coef : 0.f, b == 2 * i + 1 ? coef : 0.f));
             }
-            store(dz + v, g);
+            r = Vec<T>::put(x);
         }
+        T* to = dz + sp.head + static_cast<int64_t>(v) * E;
+        if (same) store_last(to, r);
+        else Vec<T>::scatter(to, r);
     }
 }
 
@@ -957,9 +1002,11 @@ cudaError_t pairs(const PairArgs& a, cudaStream_t st) {
 
 cudaError_t log_prob_grad(const RowArgs& a, int dtype, cudaStream_t st) {
     if (a.rows == 0) return cudaSuccess;
-    const int grid = static_cast<int>(a.rows < 152 * 4 ? a.rows : 152 * 4);
-    return dtype == GLR_BF16 ? launch_chain(grad_kernel<__nv_bfloat16>, grid, kThreads, 0, st, a)
-                             : launch_chain(grad_kernel<float>, grid, kThreads, 0, st, a);
+    const int64_t vecs = a.vocab * (dtype == GLR_BF16 ? 2 : 4) / 16, per = kThreads * kPieceVecs;
+    const int pieces = static_cast<int>(std::max<int64_t>(1, (vecs + per - 1) / per));
+    const unsigned grid = static_cast<unsigned>(a.rows * pieces);
+    return dtype == GLR_BF16 ? launch_chain(grad_kernel<__nv_bfloat16>, grid, kThreads, 0, st, a, pieces)
+                             : launch_chain(grad_kernel<float>, grid, kThreads, 0, st, a, pieces);
 }
 
 cudaError_t total(const float* x, const float* weight, float share, int64_t n, float* out, cudaStream_t st) {
