@@ -1,6 +1,8 @@
 // Products of linear layers with their epilogues, for any sizes, strides and alignment: 64 x 64 output
-// tiles by four warps, operand slabs of 32 contraction elements through registers into shared memory, two
-// slabs deep.  bf16 operands go through mma.sync.m16n8k16; fp32 ones through m16n8k8 in the 3xTF32 form
+// tiles by four warps, operand slabs of 32 contraction elements through registers (two slabs ahead) into shared
+// memory.  Where the tiles leave SMs idle a cluster of up to eight CTAs shares a tile's contraction; their partial
+// tiles are added over distributed shared memory in the order of the contraction, each CTA finishing its rows.
+// Bound by the loads' latency in the chain of slabs at these sizes.  bf16 operands go through mma.sync.m16n8k16; fp32 ones through m16n8k8 in the 3xTF32 form
 // (x = hi + lo, a b ~ hi hi + hi lo + lo hi, a few 2^-21 relative a product), accumulated in fp32.
 #include "glr_linear.cuh"
 
@@ -155,12 +157,26 @@ __device__ __forceinline__ void finish(const Product& p, int node, int64_t i, in
     }
 }
 
+__device__ __forceinline__ float peer_load(const float* p, uint32_t rank) {
+    uint32_t addr;
+    float v;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(static_cast<uint32_t>(__cvta_generic_to_shared(p))), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
 template <class T>
 __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant__ Product p, bool wide_a, bool wide_b) {
     chain_begin();
-    constexpr int P = Traits<T>::kPitch;
-    __shared__ __align__(16) T sa[2][kTile * P], sb[2][kTile * P];
-    const int node = blockIdx.z;
+    constexpr int P = Traits<T>::kPitch, kPart = kTile + 1;
+    constexpr int kSmem = 4 * kTile * P * static_cast<int>(sizeof(T)) > kTile * kPart * 4 ? 4 * kTile * P * static_cast<int>(sizeof(T)) : kTile * kPart * 4;
+    __shared__ __align__(16) uint8_t smem[kSmem];
+    T (*sa)[kTile * P] = reinterpret_cast<T (*)[kTile * P]>(smem);
+    T (*sb)[kTile * P] = sa + 2;
+    const int node = blockIdx.z, splits = gridDim.y, split = blockIdx.y;     // the splits of a tile are one cluster
     const int64_t tiles_n = (p.N + kTile - 1) / kTile;
     const int64_t i0 = blockIdx.x / tiles_n * kTile, j0 = blockIdx.x % tiles_n * kTile;
     const T* A = static_cast<const T*>(p.A) + node * p.sAb;
@@ -168,48 +184,121 @@ __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant
     const int warp = threadIdx.x >> 5, g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
     const int wm = (warp >> 1) * 32, wn = (warp & 1) * 32;
     float acc[2][4][4] = {};
-    Slab<T> ra, rb;
-    const int64_t slabs = (p.K + kSlab - 1) / kSlab;
-    if (slabs > 0) {
-        ra.load(A, p.sAi, p.sAp, i0, 0, p.M, p.K, wide_a);
-        rb.load(B, p.sBj, p.sBp, j0, 0, p.N, p.K, wide_b);
-    }
-    for (int64_t s = 0; s < slabs; ++s) {
-        const int buf = s & 1;
-        ra.store(sa[buf], p.sAp == 1);
-        rb.store(sb[buf], p.sBp == 1);
+    Slab<T> ra[2], rb[2];
+    const int64_t all = (p.K + kSlab - 1) / kSlab, first = all * split / splits, last = all * (split + 1) / splits;
+    auto fetch = [&](int q, int64_t s) {
+        if (s >= last) return;
+        ra[q].load(A, p.sAi, p.sAp, i0, s * kSlab, p.M, p.K, wide_a);
+        rb[q].load(B, p.sBj, p.sBp, j0, s * kSlab, p.N, p.K, wide_b);
+    };
+    auto work = [&](int q, int64_t s) {
+        ra[q].store(sa[q], p.sAp == 1);
+        rb[q].store(sb[q], p.sBp == 1);
         __syncthreads();
-        if (s + 1 < slabs) {
-            ra.load(A, p.sAi, p.sAp, i0, (s + 1) * kSlab, p.M, p.K, wide_a);
-            rb.load(B, p.sBj, p.sBp, j0, (s + 1) * kSlab, p.N, p.K, wide_b);
-        }
-        slab_mma(acc, sa[buf] + wm * P, sb[buf] + wn * P, g, t);
+        fetch(q, s + 2);
+        slab_mma(acc, sa[q] + wm * P, sb[q] + wn * P, g, t);
+    };
+    fetch(0, first);
+    fetch(1, first + 1);
+    for (int64_t s = first; s < last; s += 2) {
+        work(0, s);
+        if (s + 1 < last) work(1, s + 1);
     }
+    if (splits == 1) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    finish(p, node, i0 + wm + 16 * m + g + 8 * (q >> 1), j0 + wn + 8 * n + 2 * t + (q & 1), acc[m][n][q]);
+        return;
+    }
+    float* part = reinterpret_cast<float*>(smem);
+    __syncthreads();                                  // every warp is done with the slabs
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int n = 0; n < 4; ++n)
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                finish(p, node, i0 + wm + 16 * m + g + 8 * (q >> 1), j0 + wn + 8 * n + 2 * t + (q & 1), acc[m][n][q]);
+                part[(wm + 16 * m + g + 8 * (q >> 1)) * kPart + wn + 8 * n + 2 * t + (q & 1)] = acc[m][n][q];
+    cluster_sync();
+    const int rows = kTile / splits;                  // this CTA's rows of the tile
+    for (int e = threadIdx.x; e < rows * kTile; e += kThreads) {
+        const int i = split * rows + e / kTile, j = e % kTile;
+        if (i0 + i >= p.M || j0 + j >= p.N) continue;
+        float v = 0.f;
+        for (int q = 0; q < splits; ++q) v += peer_load(part + i * kPart + j, q);
+        finish(p, node, i0 + i, j0 + j, v);
+    }
+    cluster_sync();                                   // the peers are done with this CTA's shared memory
 }
 
-// 32 columns a CTA, eight rows of threads down them; the eight sums are added in order.
-constexpr int kSumCols = 32, kSumRows = 8;
-__global__ void __launch_bounds__(kSumCols * kSumRows) column_sums_kernel(const __grid_constant__ ColumnSums c) {
+// Column sums: 64 columns a CTA, eight neighbouring ones (16 bytes of bf16) a thread and 32 rows of threads; a
+// cluster of up to eight CTAs shares the rows where the columns leave SMs idle.  Added in a fixed order: down a
+// thread's rows, up the rows of threads, over the cluster's CTAs.  Bound by HBM.
+constexpr int kSumCols = 64, kSumThreads = 256, kSumLanes = kSumThreads / (kSumCols / 8);
+template <class T>
+__global__ void __launch_bounds__(kSumThreads) column_sums_kernel(const __grid_constant__ ColumnSums c, bool wide) {
     chain_begin();
-    __shared__ float part[kSumRows][kSumCols];
-    const int node = blockIdx.y, tx = threadIdx.x % kSumCols, ty = threadIdx.x / kSumCols;
-    const int64_t j = static_cast<int64_t>(blockIdx.x) * kSumCols + tx;
-    float s = 0.f;
-    if (j < c.n)
-        for (int64_t i = ty; i < c.rows; i += kSumRows) s += get(c.x, (node * c.rows + i) * c.ldx + j, c.dtype);
-    part[ty][tx] = s;
-    __syncthreads();
-    if (ty == 0 && j < c.n) {
-        for (int y = 1; y < kSumRows; ++y) s += part[y][tx];
-        put(c.sums[node], j, c.out_dtype, s);
+    __shared__ float part[kSumLanes][kSumCols + 1];
+    __shared__ float sums[kSumCols];
+    const int node = blockIdx.z, splits = gridDim.y, split = blockIdx.y;
+    const int col = threadIdx.x % (kSumCols / 8) * 8, lane = threadIdx.x / (kSumCols / 8);
+    const int64_t j = static_cast<int64_t>(blockIdx.x) * kSumCols + col;
+    const int left = static_cast<int>(c.n - j < 8 ? c.n - j : 8);
+    const int64_t r0 = c.rows * split / splits, r1 = c.rows * (split + 1) / splits;
+    const T* x = static_cast<const T*>(c.x) + node * c.rows * c.ldx + j;
+    float s[8] = {};
+    if (left > 0) {
+        constexpr int kVec = Traits<T>::kVec;
+#pragma unroll 4
+        for (int64_t i = r0 + lane; i < r1; i += kSumLanes) {
+            T v[8];
+            if (wide && left == 8) {
+#pragma unroll
+                for (int e = 0; e < 8; e += kVec) *reinterpret_cast<uint4*>(v + e) = *reinterpret_cast<const uint4*>(x + i * c.ldx + e);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = e < left ? x[i * c.ldx + e] : T(0.f);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[e] += to_f(v[e]);
+        }
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) part[lane][col + e] = s[e];
+    __syncthreads();
+    const int64_t k = static_cast<int64_t>(blockIdx.x) * kSumCols + threadIdx.x;
+    if (threadIdx.x < kSumCols) {
+        float v = 0.f;
+        for (int q = 0; q < kSumLanes; ++q) v += part[q][threadIdx.x];
+        sums[threadIdx.x] = v;
+        if (splits == 1 && k < c.n) put(c.sums[node], k, c.out_dtype, v);
+    }
+    if (splits == 1) return;
+    cluster_sync();
+    if (split == 0 && threadIdx.x < kSumCols && k < c.n) {
+        float v = 0.f;
+        for (int q = 0; q < splits; ++q) v += peer_load(sums + threadIdx.x, q);
+        put(c.sums[node], k, c.out_dtype, v);
+    }
+    cluster_sync();
+}
+
+// launch_chain with clusters of 1 x splits CTAs.
+template <class... Q, class... A>
+cudaError_t launch_clusters(void (*kernel)(Q...), dim3 grid, int threads, int splits, cudaStream_t st, const A&... args) {
+    cudaLaunchAttribute attr[2]{};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 1; attr[1].val.clusterDim.y = splits; attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid; cfg.blockDim = threads; cfg.stream = st;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 // Sixteen-byte loads: the base, the row stride and the nodes' stride on 16 bytes.
@@ -229,16 +318,25 @@ cudaError_t any_product(const Product& p, cudaStream_t st) {
     const int64_t tiles = ((p.M + kTile - 1) / kTile) * ((p.N + kTile - 1) / kTile);
     if (tiles > 0x7fffffff) return cudaErrorInvalidValue;
     const bool wa = wide_ok(p.A, p.sAp == 1 ? p.sAi : p.sAp, p.sAb, es), wb = wide_ok(p.B, p.sBp == 1 ? p.sBj : p.sBp, p.sBb, es);
-    const dim3 grid(static_cast<unsigned>(tiles), 1, p.nodes);
-    return p.dtype == GLR_BF16 ? launch_chain(product_kernel<__nv_bfloat16>, grid, kThreads, 0, st, p, wa, wb)
-                               : launch_chain(product_kernel<float>, grid, kThreads, 0, st, p, wa, wb);
+    // CTAs a tile: as many as fill the SMs twice, as long as each keeps four slabs
+    const int64_t slabs = (p.K + kSlab - 1) / kSlab;
+    int splits = 1;
+    while (splits < 8 && tiles * p.nodes * splits < 152 && slabs >= 8 * splits) splits *= 2;
+    const dim3 grid(static_cast<unsigned>(tiles), splits, p.nodes);
+    return p.dtype == GLR_BF16 ? launch_clusters(product_kernel<__nv_bfloat16>, grid, kThreads, splits, st, p, wa, wb)
+                               : launch_clusters(product_kernel<float>, grid, kThreads, splits, st, p, wa, wb);
 }
 
 cudaError_t column_sums(const ColumnSums& c, cudaStream_t st) {
     if (c.n == 0) return cudaSuccess;
     const int64_t blocks = (c.n + kSumCols - 1) / kSumCols;
     if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-    return launch_chain(column_sums_kernel, dim3(static_cast<unsigned>(blocks), c.nodes), kSumCols * kSumRows, 0, st, c);
+    int splits = 1;
+    while (splits < 8 && blocks * c.nodes * splits < 304 && c.rows >= 256 * splits) splits *= 2;
+    const bool wide = wide_ok(c.x, c.ldx, c.rows * c.ldx, c.dtype == GLR_BF16 ? 2 : 4);
+    const dim3 grid(static_cast<unsigned>(blocks), splits, c.nodes);
+    return c.dtype == GLR_BF16 ? launch_clusters(column_sums_kernel<__nv_bfloat16>, grid, kSumThreads, splits, st, c, wide)
+                               : launch_clusters(column_sums_kernel<float>, grid, kSumThreads, splits, st, c, wide);
 }
 
 }  // namespace linear
