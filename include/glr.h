@@ -394,10 +394,16 @@ typedef struct glr_linear_args {
     const void* bias;
     const void* residual; int64_t ldr;
     void* preact; int64_t ldp;
+    void* workspace; int64_t workspace_bytes;
     int32_t dtype;
     int32_t act;
 } glr_linear_args;
 int glr_linear(const glr_linear_args* a, void* stream);
+/* The bytes of workspace (device memory, 16-byte aligned, for one call at a time) with which a call
+ * with these arguments is fastest: fp32 matrices, and ones whose rows do not begin on 16 bytes, are
+ * first laid out for the tensor cores where the product is large.  0: none.  A call with less (or a null
+ * workspace) is slower, and right.  The two gradients below have the same.                        */
+int glr_linear_workspace(const glr_linear_args* a, int64_t* bytes);
 
 /* The gradient of a layer's input, with the activation below it: G = dZ W + residual (the gradient
  * that reaches X past this layer; may be null), dX = G act'(preact), where preact (rows x k) is the
@@ -412,10 +418,12 @@ typedef struct glr_linear_grad_input_args {
     const void* residual; int64_t ldr;
     const void* preact; int64_t ldp;
     void* grad_out; int64_t ldg;
+    void* workspace; int64_t workspace_bytes;
     int32_t dtype;
     int32_t act;
 } glr_linear_grad_input_args;
 int glr_linear_grad_input(const glr_linear_grad_input_args* a, void* stream);
+int glr_linear_grad_input_workspace(const glr_linear_grad_input_args* a, int64_t* bytes);
 
 /* Every node's gradient of a layer's weights and bias.  The rows of dZ (nodes * rows x n) and X
  * (nodes * rows x k) are the nodes' one after the other, `rows` each: dW[i] = dZ_i^T X_i (n x k,
@@ -428,10 +436,12 @@ typedef struct glr_linear_grad_weight_args {
     const void* X; int64_t ldx;
     void* const* dW;
     void* const* db;
+    void* workspace; int64_t workspace_bytes;
     int32_t dtype;
     int32_t grad_dtype;
 } glr_linear_grad_weight_args;
 int glr_linear_grad_weight(const glr_linear_grad_weight_args* a, void* stream);
+int glr_linear_grad_weight_workspace(const glr_linear_grad_weight_args* a, int64_t* bytes);
 
 /* Losses.  logits is rows x vocab.  weight[t] (null: 1 / rows each) is row t's share of the loss;
  * a row of weight 0 does not count: its logits are not read (they may be NaN), its outputs and its

@@ -86,12 +86,14 @@ def _struct(name, doc, wide, narrow):
 
 # "name*" is an address, "name" an int64 among the 8-byte fields; "name." a float, "name" an int32 among the rest
 GlrLinearArgs = _struct("GlrLinearArgs", "glr_linear_args",
-                        "rows n k X* ldx W* ldw Y* ldy bias* residual* ldr preact* ldp", "dtype act")
+                        "rows n k X* ldx W* ldw Y* ldy bias* residual* ldr preact* ldp workspace* "
+                        "workspace_bytes", "dtype act")
 GlrLinearGradInputArgs = _struct("GlrLinearGradInputArgs", "glr_linear_grad_input_args",
-                                 "rows n k dZ* lddz W* ldw dX* lddx residual* ldr preact* ldp grad_out* ldg",
+                                 "rows n k dZ* lddz W* ldw dX* lddx residual* ldr preact* ldp grad_out* ldg workspace* "
+                                 "workspace_bytes",
                                  "dtype act")
 GlrLinearGradWeightArgs = _struct("GlrLinearGradWeightArgs", "glr_linear_grad_weight_args",
-                                  "nodes rows n k dZ* lddz X* ldx dW* db*", "dtype grad_dtype")
+                                  "nodes rows n k dZ* lddz X* ldx dW* db* workspace* workspace_bytes", "dtype grad_dtype")
 GlrDistillArgs = _struct("GlrDistillArgs", "glr_distill_args",
                          "rows vocab topk logits* ld_logits teacher* ld_teacher ids* ld_ids labels* weight* loss* "
                          "row_loss* dlogits* ld_dlogits",
@@ -150,6 +152,9 @@ _SIGNATURES = {
                                           ctypes.c_void_p, ctypes.c_uint64, ctypes.c_int64, ctypes.c_void_p,
                                           ctypes.c_void_p, ctypes.c_void_p]),
     "glr_linear": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p]),
+    "glr_linear_workspace": (ctypes.c_int, [ctypes.c_void_p, ctypes.POINTER(ctypes.c_int64)]),
+    "glr_linear_grad_input_workspace": (ctypes.c_int, [ctypes.c_void_p, ctypes.POINTER(ctypes.c_int64)]),
+    "glr_linear_grad_weight_workspace": (ctypes.c_int, [ctypes.c_void_p, ctypes.POINTER(ctypes.c_int64)]),
     "glr_linear_grad_input": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p]),
     "glr_linear_grad_weight": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p]),
     "glr_distill_loss": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p]),

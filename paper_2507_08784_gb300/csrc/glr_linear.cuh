@@ -29,12 +29,19 @@ struct Product {
     int* err;
 };
 
-cudaError_t product(const Product& p, cudaStream_t st);
-// Any strides, sizes, alignment and types (k_linear.cu).
+// tcgen05 (k_linear_tc.cu): whether it takes the product, and the workspace that the packed operands need.
+struct TcPlan {
+    bool ok, pack_a, pack_b;
+    int planes;
+    int64_t bytes_a, bytes_b;
+    int64_t bytes() const { return ok ? bytes_a + bytes_b : 0; }
+};
+TcPlan tc_plan(const Product& p);
+cudaError_t tc_product(const Product& p, const TcPlan& plan, void* workspace, cudaStream_t st);
+// Any strides, sizes, alignment and types, without workspace (k_linear.cu).
 cudaError_t any_product(const Product& p, cudaStream_t st);
-// bf16 operands whose rows begin on 16 bytes: tcgen05 (k_linear_tc.cu).
-bool tc_ok(const Product& p);
-cudaError_t tc_product(const Product& p, cudaStream_t st);
+// The one of the two that the sizes, the alignment and the workspace given call for.
+cudaError_t product(const Product& p, void* workspace, int64_t workspace_bytes, cudaStream_t st);
 
 // sums[b][j] = sum over the rows of node b of x(i, j), x rows x n in rows of ldx
 struct ColumnSums {

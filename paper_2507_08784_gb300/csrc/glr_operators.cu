@@ -92,8 +92,10 @@ bool flag(int v) { return v == 0 || v == 1; }
 
 using namespace glr;
 
-extern "C" int glr_linear(const glr_linear_args* a, void* stream) {
-    const char* who = "glr_linear";
+namespace {
+
+// The checks and the product of a call.
+int linear_product(const char* who, const glr_linear_args* a, linear::Product& p) {
     if (!a) return refuse("%s: null arguments", who);
     if (int rc = check_layer(who, a->rows, a->n, a->k, a->dtype, a->act)) return rc;
     if (!matrix_ok(a->X, a->ldx, a->rows, a->k, a->dtype) || !matrix_ok(a->W, a->ldw, a->n, a->k, a->dtype))
@@ -106,19 +108,17 @@ extern "C" int glr_linear(const glr_linear_args* a, void* stream) {
         return refuse("%s: preact misaligned or with ld < n", who);
     if (a->residual && a->residual == a->Y && a->rows > 1 && a->ldr != a->ldy)
         return refuse("%s: residual in place of Y needs the same ld", who);
-    linear::Product p{};
+    p = linear::Product{};
     p.mode = linear::kForward; p.dtype = p.out_dtype = a->dtype; p.act = a->act;
     p.M = a->rows; p.N = a->n; p.K = a->k; p.nodes = 1;
     p.A = a->X; p.sAi = a->ldx; p.sAp = 1;
     p.B = a->W; p.sBj = a->ldw; p.sBp = 1;
     p.out = a->Y; p.ldo = a->ldy; p.bias = a->bias;
     p.add = a->residual; p.ldadd = a->ldr; p.aux = a->preact; p.ldaux = a->ldp;
-    if (!(p.err = gave_up_counter())) return launched(who, cudaErrorNoDevice);
-    return launched(who, linear::product(p, static_cast<cudaStream_t>(stream)));
+    return GLR_OK;
 }
 
-extern "C" int glr_linear_grad_input(const glr_linear_grad_input_args* a, void* stream) {
-    const char* who = "glr_linear_grad_input";
+int grad_input_product(const char* who, const glr_linear_grad_input_args* a, linear::Product& p) {
     if (!a) return refuse("%s: null arguments", who);
     if (int rc = check_layer(who, a->rows, a->n, a->k, a->dtype, a->act)) return rc;
     if (!matrix_ok(a->dZ, a->lddz, a->rows, a->n, a->dtype)) return refuse("%s: dZ null, misaligned or with ld < n", who);
@@ -132,7 +132,7 @@ extern "C" int glr_linear_grad_input(const glr_linear_grad_input_args* a, void* 
     if (a->residual && a->rows > 1 &&
         ((a->residual == a->dX && a->ldr != a->lddx) || (a->residual == a->grad_out && a->ldr != a->ldg)))
         return refuse("%s: residual in place of an output needs the same ld", who);
-    linear::Product p{};
+    p = linear::Product{};
     p.mode = linear::kGradInput; p.dtype = p.out_dtype = a->dtype; p.act = a->act;
     p.M = a->rows; p.N = a->k; p.K = a->n; p.nodes = 1;
     p.A = a->dZ; p.sAi = a->lddz; p.sAp = 1;
@@ -141,12 +141,10 @@ extern "C" int glr_linear_grad_input(const glr_linear_grad_input_args* a, void* 
     p.add = a->residual; p.ldadd = a->ldr;
     if (a->act != GLR_ACT_NONE) { p.pre = a->preact; p.ldpre = a->ldp; }
     p.aux = a->grad_out; p.ldaux = a->ldg;
-    if (!(p.err = gave_up_counter())) return launched(who, cudaErrorNoDevice);
-    return launched(who, linear::product(p, static_cast<cudaStream_t>(stream)));
+    return GLR_OK;
 }
 
-extern "C" int glr_linear_grad_weight(const glr_linear_grad_weight_args* a, void* stream) {
-    const char* who = "glr_linear_grad_weight";
+int grad_weight_product(const char* who, const glr_linear_grad_weight_args* a, linear::Product& p) {
     if (!a) return refuse("%s: null arguments", who);
     if (int rc = check_layer(who, a->rows, a->n, a->k, a->dtype, GLR_ACT_NONE)) return rc;
     if (!dtype_ok(a->grad_dtype)) return refuse("%s: unknown grad_dtype %d", who, a->grad_dtype);
@@ -160,20 +158,66 @@ extern "C" int glr_linear_grad_weight(const glr_linear_grad_weight_args* a, void
         if (!vector_ok(a->dW[i], a->n * a->k, gs)) return refuse("%s: dW[%d] is null or misaligned", who, (int)i);
         if (a->db && !vector_ok(a->db[i], a->n, gs)) return refuse("%s: db[%d] is null or misaligned", who, (int)i);
     }
-    linear::Product p{};
+    p = linear::Product{};
     p.mode = linear::kGradWeight; p.dtype = a->dtype; p.out_dtype = a->grad_dtype;
     p.M = a->n; p.N = a->k; p.K = a->rows; p.nodes = static_cast<int>(a->nodes);
     p.A = a->dZ; p.sAi = 1; p.sAp = a->lddz; p.sAb = a->rows * a->lddz;
     p.B = a->X; p.sBj = 1; p.sBp = a->ldx; p.sBb = a->rows * a->ldx;
+    for (int64_t i = 0; i < a->nodes; ++i) p.outs[i] = a->dW[i];
+    return GLR_OK;
+}
+
+int run_product(const char* who, linear::Product& p, void* workspace, int64_t bytes, cudaStream_t st) {
+    if (reinterpret_cast<uintptr_t>(workspace) % 16) return refuse("%s: workspace is not 16-byte aligned", who);
+    if (!(p.err = gave_up_counter())) return launched(who, cudaErrorNoDevice);
+    return launched(who, linear::product(p, workspace, bytes, st));
+}
+int product_workspace(int rc, const linear::Product& p, int64_t* bytes) {
+    if (rc == GLR_OK) *bytes = linear::tc_plan(p).bytes();
+    return rc;
+}
+
+}  // namespace
+
+extern "C" int glr_linear(const glr_linear_args* a, void* stream) {
+    linear::Product p;
+    const int rc = linear_product("glr_linear", a, p);
+    return rc ? rc : run_product("glr_linear", p, a->workspace, a->workspace_bytes, static_cast<cudaStream_t>(stream));
+}
+extern "C" int glr_linear_workspace(const glr_linear_args* a, int64_t* bytes) {
+    linear::Product p;
+    if (!bytes) return refuse("%s: bytes is null", "glr_linear_workspace");
+    return product_workspace(linear_product("glr_linear_workspace", a, p), p, bytes);
+}
+
+extern "C" int glr_linear_grad_input(const glr_linear_grad_input_args* a, void* stream) {
+    linear::Product p;
+    const int rc = grad_input_product("glr_linear_grad_input", a, p);
+    return rc ? rc : run_product("glr_linear_grad_input", p, a->workspace, a->workspace_bytes, static_cast<cudaStream_t>(stream));
+}
+extern "C" int glr_linear_grad_input_workspace(const glr_linear_grad_input_args* a, int64_t* bytes) {
+    linear::Product p;
+    if (!bytes) return refuse("%s: bytes is null", "glr_linear_grad_input_workspace");
+    return product_workspace(grad_input_product("glr_linear_grad_input_workspace", a, p), p, bytes);
+}
+
+extern "C" int glr_linear_grad_weight(const glr_linear_grad_weight_args* a, void* stream) {
+    const char* who = "glr_linear_grad_weight";
+    linear::Product p;
+    if (int rc = grad_weight_product(who, a, p)) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (int rc = run_product(who, p, a->workspace, a->workspace_bytes, st)) return rc;
+    if (!a->db) return GLR_OK;
     linear::ColumnSums c{};
     c.rows = a->rows; c.n = a->n; c.nodes = p.nodes; c.dtype = a->dtype; c.out_dtype = a->grad_dtype;
     c.x = a->dZ; c.ldx = a->lddz;
-    for (int64_t i = 0; i < a->nodes; ++i) { p.outs[i] = a->dW[i]; if (a->db) c.sums[i] = a->db[i]; }
-    if (!(p.err = gave_up_counter())) return launched(who, cudaErrorNoDevice);
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    cudaError_t e = linear::product(p, st);
-    if (e == cudaSuccess && a->db) e = linear::column_sums(c, st);
-    return launched(who, e);
+    for (int64_t i = 0; i < a->nodes; ++i) c.sums[i] = a->db[i];
+    return launched(who, linear::column_sums(c, st));
+}
+extern "C" int glr_linear_grad_weight_workspace(const glr_linear_grad_weight_args* a, int64_t* bytes) {
+    linear::Product p;
+    if (!bytes) return refuse("%s: bytes is null", "glr_linear_grad_weight_workspace");
+    return product_workspace(grad_weight_product("glr_linear_grad_weight_workspace", a, p), p, bytes);
 }
 
 extern "C" int glr_distill_loss(const glr_distill_args* a, void* stream) {

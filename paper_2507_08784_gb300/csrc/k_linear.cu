@@ -81,9 +81,19 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
 
-// The warp's 32 x 32 part of the tile, one slab.
-__device__ __forceinline__ void slab_mma(float (&acc)[2][4][4], const __nv_bfloat16* a, const __nv_bfloat16* b, int g, int t) {
+// The warp's 32 x 32 part of the tile, one slab.  The tensor cores truncate their sums, which would add up over a
+// long contraction: a slab's products are summed there by themselves and join the total in rounded additions.
+__device__ __forceinline__ void join(float (&total)[2][4][4], const float (&acc)[2][4][4]) {
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) total[m][n][q] += acc[m][n][q];
+}
+__device__ __forceinline__ void slab_mma(float (&total)[2][4][4], const __nv_bfloat16* a, const __nv_bfloat16* b, int g, int t) {
     constexpr int P = Traits<__nv_bfloat16>::kPitch;
+    float acc[2][4][4] = {};
     auto at = [](const __nv_bfloat16* s, int row, int col) { return *reinterpret_cast<const uint32_t*>(s + row * P + col); };
 #pragma unroll
     for (int k = 0; k < kSlab; k += 16) {
@@ -101,9 +111,8 @@ __device__ __forceinline__ void slab_mma(float (&acc)[2][4][4], const __nv_bfloa
 #pragma unroll
             for (int n = 0; n < 4; ++n) mma_bf16(acc[m][n], fa[m], fb[n]);
     }
+    join(total, acc);
 }
-// fp32: the tensor core truncates its sums, which would add up over a long contraction; a slab's products
-// are summed there by themselves and join the total in a rounded addition.
 __device__ __forceinline__ void slab_mma(float (&total)[2][4][4], const float* a, const float* b, int g, int t) {
     constexpr int P = Traits<float>::kPitch;
     float acc[2][4][4] = {};
@@ -131,12 +140,7 @@ __device__ __forceinline__ void slab_mma(float (&total)[2][4][4], const float* a
                 mma_tf32(acc[m][n], ah[m], bh[n]);
             }
     }
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int n = 0; n < 4; ++n)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) total[m][n][q] += acc[m][n][q];
+    join(total, acc);
 }
 
 __device__ __forceinline__ void finish(const Product& p, int node, int64_t i, int64_t j, float acc) {
@@ -308,9 +312,11 @@ bool wide_ok(const void* base, int64_t row_stride, int64_t node_stride, int64_t 
 
 }  // namespace
 
-cudaError_t product(const Product& p, cudaStream_t st) {
+cudaError_t product(const Product& p, void* workspace, int64_t workspace_bytes, cudaStream_t st) {
     if (p.M == 0 || p.N == 0) return cudaSuccess;
-    return tc_ok(p) ? tc_product(p, st) : any_product(p, st);
+    const TcPlan plan = tc_plan(p);
+    const bool fits = plan.bytes() == 0 || (workspace && workspace_bytes >= plan.bytes());
+    return plan.ok && fits ? tc_product(p, plan, workspace, st) : any_product(p, st);
 }
 
 cudaError_t any_product(const Product& p, cudaStream_t st) {

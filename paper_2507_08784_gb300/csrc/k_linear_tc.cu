@@ -1,15 +1,23 @@
 // Products of linear layers on the fifth-generation tensor cores: out = epilogue(A B^T) for bf16 operands
 // whose rows lie on 16 bytes, either operand contiguous along the contraction ("K-major") or along its own
 // index ("MN-major"), so that the forward product, the input's gradient and the weights' gradients all read
-// their matrices as they are.
+// their matrices as they are.  Matrices that lie otherwise are copied into rows on 16 bytes first, and fp32
+// ones into three bf16 planes x = hi + mid + lo (24 bits): their product is the sum of the six plane products
+// above 2^-24, one after the other in the same accumulator.
 //
-// One persistent kernel: a CTA (CG = 1) or a pair of CTAs on two SMs (CG = 2) takes 128 CG x BN output
+// tc_product_kernel, persistent: a CTA (CG = 1) or a pair of CTAs on two SMs (CG = 2) takes 128 CG x BN output
 // tiles in turn.  One warp copies operand slabs of 64 contraction elements (128-byte swizzle) into a ring of
 // shared-memory stages, one thread issues tcgen05.mma.kind::f16 (of the pair's first CTA: each CTA holds its
 // 128 rows of A and half of B's, and the result's rows stay in their CTA's tensor memory), and eight warps
 // bring the finished accumulator through the epilogue while the next tile's products run into the other half
 // of tensor memory.  Stages are handed over on mbarriers; every wait is bounded: a CTA that gives up counts
 // the event, lets its copies land, frees tensor memory and returns.
+// tc_split_kernel, for few tiles: a cluster of up to eight CTAs shares a 128 x 64 tile's contraction, and adds
+// its partial tiles over distributed shared memory in the order of the contraction.
+//
+// The tensor cores truncate their fp32 sums (about 2^-25 of the sum for every 16 elements, always the same
+// way), which over a long contraction is far above fp32 rounding: where the result is fp32 (PROMOTE), and in
+// tc_split_kernel, the sums of 256 contraction elements join the total in rounded additions by the epilogue warps.
 //
 // What bounds it: the tensor pipe for contractions of about 1000 and more; below that the epilogue, which
 // each thread does on a row of the tile, 16 bytes a load or store.
@@ -30,7 +38,8 @@ using tc::mbar_expect_tx;
 using tc::mbar_init;
 using tc::smem_u32;
 
-constexpr int kEpiWarps = 8, kProducer = 8, kIssuer = 9, kThreads = 320;
+constexpr int epi_warps(bool promote) { return promote ? 16 : 8; }     // ... of 64 or 128 columns each
+constexpr int threads_of(int epi) { return (epi + 2) * 32; }
 constexpr int kSlab = 64;                       // contraction elements a stage: one 128-byte swizzle row of bf16
 constexpr int kMaxStages = 8;
 constexpr size_t kRingBytes = 208 * 1024;
@@ -40,6 +49,8 @@ struct TcArgs {
     Product p;
     CUtensorMap mapA, mapB;
     int tiles_m, tiles_n, tiles, slabs, stages;
+    int planes;                                 // 1, or 3: a slab of the contraction is six products of planes
+    int chunk;                                  // slabs whose sums are kept in tensor memory (PROMOTE)
     int wide;                                   // 16-byte accesses: bit 0 out, 1 bias, 2 add, 3 pre, 4 aux
 };
 
@@ -77,15 +88,6 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int
     }
     if (atomicExch(const_cast<int*>(abort), 1) == 0) atomicAdd(err, 1);
     return false;
-}
-template <int CG>
-__device__ __forceinline__ void load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
-    if (CG == 1)
-        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
-    else
-        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];"
-                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
 template <int CG>
 __device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
@@ -133,8 +135,31 @@ __device__ __forceinline__ void tmem_load32(uint32_t ta, float (&v)[32]) {
     for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(u[j]);
 }
 
-// Eight bf16 at p (n of them in range), widened.
-__device__ __forceinline__ void get8(const void* base, int64_t at, int n, bool wide, float (&v)[8]) {
+__device__ __forceinline__ void tmem_store32(uint32_t ta, const float* v) {
+    uint32_t u[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) u[j] = __float_as_uint(v[j]);
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+                 ::"r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]),
+                   "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(u[16]), "r"(u[17]), "r"(u[18]), "r"(u[19]),
+                   "r"(u[20]), "r"(u[21]), "r"(u[22]), "r"(u[23]), "r"(u[24]), "r"(u[25]), "r"(u[26]), "r"(u[27]), "r"(u[28]), "r"(u[29]),
+                   "r"(u[30]), "r"(u[31]), "r"(ta) : "memory");
+}
+
+// Eight elements at p (n of them in range), widened.
+__device__ __forceinline__ void get8(const void* base, int64_t at, int n, bool wide, int dtype, float (&v)[8]) {
+    if (dtype == GLR_F32) {
+        const float* p = static_cast<const float*>(base) + at;
+        if (wide && n == 8) {
+            const float4 x = *reinterpret_cast<const float4*>(p), y = *reinterpret_cast<const float4*>(p + 4);
+            v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = e < n ? p[e] : 0.f;
+        }
+        return;
+    }
     const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(base) + at;
     if (wide && n == 8) {
         const uint4 u = *reinterpret_cast<const uint4*>(p);
@@ -194,40 +219,41 @@ __device__ __forceinline__ void act8(float (&v)[8], int act) {
 // The epilogue on eight neighbouring columns of a row (i, j): acc in v.
 __device__ __forceinline__ void epilogue8(const TcArgs& a, int node, int64_t i, int64_t j, float (&v)[8]) {
     const Product& p = a.p;
+    const int dt = p.out_dtype;                 // but in kGradWeight also the inputs' type
     const int n = static_cast<int>(p.N - j < 8 ? p.N - j : 8);
     if (p.mode == kGradWeight) {
-        put8(p.outs[node], i * p.N + j, n, a.wide & 1, p.out_dtype, v);
+        put8(p.outs[node], i * p.N + j, n, a.wide & 1, dt, v);
         return;
     }
     float x[8];
     if (p.mode == kForward) {
         if (p.bias) {
-            get8(p.bias, j, n, a.wide & 2, x);
+            get8(p.bias, j, n, a.wide & 2, dt, x);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] += x[e];
         }
-        if (p.aux) put8(p.aux, i * p.ldaux + j, n, a.wide & 16, GLR_BF16, v);
+        if (p.aux) put8(p.aux, i * p.ldaux + j, n, a.wide & 16, dt, v);
         act8<false>(v, p.act);
         if (p.add) {
-            get8(p.add, i * p.ldadd + j, n, a.wide & 4, x);
+            get8(p.add, i * p.ldadd + j, n, a.wide & 4, dt, x);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] += x[e];
         }
     } else {
         if (p.add) {
-            get8(p.add, i * p.ldadd + j, n, a.wide & 4, x);
+            get8(p.add, i * p.ldadd + j, n, a.wide & 4, dt, x);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] += x[e];
         }
-        if (p.aux) put8(p.aux, i * p.ldaux + j, n, a.wide & 16, GLR_BF16, v);
+        if (p.aux) put8(p.aux, i * p.ldaux + j, n, a.wide & 16, dt, v);
         if (p.pre) {
-            get8(p.pre, i * p.ldpre + j, n, a.wide & 8, x);
+            get8(p.pre, i * p.ldpre + j, n, a.wide & 8, dt, x);
             act8<true>(x, p.act);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] *= x[e];
         }
     }
-    put8(p.out, i * p.ldo + j, n, a.wide & 1, GLR_BF16, v);
+    put8(p.out, i * p.ldo + j, n, a.wide & 1, dt, v);
 }
 
 struct Tile { int node, m, n; };
@@ -243,9 +269,41 @@ __device__ __forceinline__ Tile tile_at(const TcArgs& a, int t) {
     return r;
 }
 
+// The planes of A and B in the six products of a slab, the smallest first.
+__device__ __forceinline__ int plane_a(int pair) { return pair == 0 ? 2 : pair == 2 || pair == 3 ? 1 : 0; }
+__device__ __forceinline__ int plane_b(int pair) { return pair == 1 ? 2 : pair == 2 || pair == 4 ? 1 : 0; }
+
+// The tile copies of stage k (slab k, or product k mod 6 of slab k / 6) of rows m0.. of A and n0.. of B.
+template <int CG, int BB, bool MNA, bool MNB>
+__device__ __forceinline__ void load_stage(const TcArgs& a, int k, int m0, int n0, int node, uint32_t st, uint32_t bar) {
+    const int slab = a.planes == 3 ? k / 6 : k, pair = a.planes == 3 ? k - 6 * slab : 0;
+    const int pa = a.planes == 3 ? plane_a(pair) : 0, pb = a.planes == 3 ? plane_b(pair) : 0, x = slab * kSlab;
+    if (MNA) {
+        for (int c = 0; c < 2; ++c) load_3d<CG>(st + c * 8192, &a.mapA, m0 + 64 * c, x, node + a.p.nodes * pa, bar);
+    } else {
+        load_3d<CG>(st, &a.mapA, x, m0, pa, bar);
+    }
+    if (MNB) {
+        for (int c = 0; c < BB / 64; ++c) load_3d<CG>(st + 16384 + c * 8192, &a.mapB, n0 + 64 * c, x, node + a.p.nodes * pb, bar);
+    } else {
+        load_3d<CG>(st + 16384, &a.mapB, x, n0, pb, bar);
+    }
+}
+// ... and its MMAs, sixteen contraction elements each.
 template <int BN, int CG, bool MNA, bool MNB>
-__global__ void __launch_bounds__(kThreads, 1) tc_product_kernel(const __grid_constant__ TcArgs a) {
+__device__ __forceinline__ void mma_stage(uint32_t d, uint32_t st, bool add) {
+    constexpr uint32_t id = (1u << 4) | (1u << 7) | (1u << 10) | (MNA ? 1u << 15 : 0u) | (MNB ? 1u << 16 : 0u) |
+                            (static_cast<uint32_t>(BN >> 3) << 17) | (static_cast<uint32_t>(8 * CG) << 24);
+#pragma unroll
+    for (int kk = 0; kk < kSlab / 16; ++kk)
+        mma_f16<CG>(d, operand_desc(st + (MNA ? 2048 : 32) * kk, MNA, 8192),
+                    operand_desc(st + 16384 + (MNB ? 2048 : 32) * kk, MNB, 8192), id, (add || kk) ? 1u : 0u);
+}
+
+template <int BN, int CG, bool MNA, bool MNB, bool PROMOTE>
+__global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_kernel(const __grid_constant__ TcArgs a) {
     chain_begin();
+    constexpr int kEpiWarps = epi_warps(PROMOTE), kProducer = kEpiWarps, kIssuer = kEpiWarps + 1, kSpan = BN / (kEpiWarps / 4);
     constexpr uint32_t SB = stage_bytes<BN, CG>(), BB = BN / CG;     // bytes a stage, rows of B in this CTA
     constexpr uint32_t kCols = 2 * BN;                               // two accumulators of BN columns
     extern __shared__ uint8_t dyn_smem[];
@@ -293,17 +351,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_product_kernel(const __grid_co
                     uint32_t bar = smem_u32(&full_bar[s]);
                     if (rank == 0) mbar_expect_tx(bar, SB * CG);
                     else bar = peer_addr(bar, 0);
-                    if (MNA) {
-                        for (int c = 0; c < 2; ++c) load_3d<CG>(st + c * 8192, &a.mapA, m0 + 64 * c, k * kSlab, tl.node, bar);
-                    } else {
-                        load_2d<CG>(st, &a.mapA, k * kSlab, m0, bar);
-                    }
-                    if (MNB) {
-                        for (int c = 0; c < static_cast<int>(BB) / 64; ++c)
-                            load_3d<CG>(st + 16384 + c * 8192, &a.mapB, n0 + 64 * c, k * kSlab, tl.node, bar);
-                    } else {
-                        load_2d<CG>(st + 16384, &a.mapB, k * kSlab, n0, bar);
-                    }
+                    load_stage<CG, static_cast<int>(BB), MNA, MNB>(a, k, m0, n0, tl.node, st, bar);
                     issued |= 1u << s;
                     last = (last & ~(1u << s)) | (use << s);
                     if (++s == S) { s = 0; use ^= 1u; }
@@ -317,57 +365,86 @@ __global__ void __launch_bounds__(kThreads, 1) tc_product_kernel(const __grid_co
         __syncwarp();
     } else if (warp == kIssuer) {
         if (lane == 0 && rank == 0) {
-            constexpr uint32_t id = (1u << 4) | (1u << 7) | (1u << 10) | (MNA ? 1u << 15 : 0u) | (MNB ? 1u << 16 : 0u) |
-                                    (static_cast<uint32_t>(BN >> 3) << 17) | (static_cast<uint32_t>(8 * CG) << 24);
             int s = 0, b = 0;
             uint32_t use = 0, tuse[2] = {0, 0};
             bool ok = true;
             for (int t = first; t < a.tiles && ok; t += step) {
-                if (!(ok = wait(smem_u32(&tempty_bar[b]), tuse[b] ^ 1u, abort, err))) break;
-                fence_after();
-                const uint32_t d = tmem + static_cast<uint32_t>(b * BN);
-                for (int k = 0; k < a.slabs; ++k) {
-                    if (!(ok = wait(smem_u32(&full_bar[s]), use, abort, err))) break;
+                for (int k0 = 0; k0 < a.slabs && ok; k0 += PROMOTE ? a.chunk : a.slabs) {
+                    if (!(ok = wait(smem_u32(&tempty_bar[b]), tuse[b] ^ 1u, abort, err))) break;
                     fence_after();
-                    const uint32_t st = smem_u32(ring + static_cast<size_t>(s) * SB);
-#pragma unroll
-                    for (int kk = 0; kk < kSlab / 16; ++kk)
-                        mma_f16<CG>(d, operand_desc(st + (MNA ? 2048 : 32) * kk, MNA, 8192),
-                                    operand_desc(st + 16384 + (MNB ? 2048 : 32) * kk, MNB, 8192), id, (k | kk) ? 1u : 0u);
-                    commit<CG>(smem_u32(&empty_bar[s]));
-                    if (++s == S) { s = 0; use ^= 1u; }
+                    const uint32_t d = tmem + static_cast<uint32_t>(b * BN);
+                    const int k1 = PROMOTE ? min(k0 + a.chunk, a.slabs) : a.slabs;
+                    for (int k = k0; k < k1; ++k) {
+                        if (!(ok = wait(smem_u32(&full_bar[s]), use, abort, err))) break;
+                        fence_after();
+                        mma_stage<BN, CG, MNA, MNB>(d, smem_u32(ring + static_cast<size_t>(s) * SB), k > k0);
+                        commit<CG>(smem_u32(&empty_bar[s]));
+                        if (++s == S) { s = 0; use ^= 1u; }
+                    }
+                    if (!ok) break;
+                    commit<CG>(smem_u32(&tfull_bar[b]));
+                    tuse[b] ^= 1u;
+                    b ^= 1;
                 }
-                if (!ok) break;
-                commit<CG>(smem_u32(&tfull_bar[b]));
-                tuse[b] ^= 1u;
-                b ^= 1;
             }
         }
         __syncwarp();
     } else {
-        // warp w: tensor-memory lanes 32 (w mod 4) .. + 31, columns of half w / 4
+        // warp w: tensor-memory lanes 32 (w mod 4) .. + 31, the w / 4-th kSpan columns
         uint32_t tuse[2] = {0, 0};
         int b = 0;
-        const int quad = warp & 3, c0 = (warp >> 2) * (BN / 2);
+        const int quad = warp & 3, c0 = (warp >> 2) * kSpan;
+        auto hand_back = [&]() {
+            fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                const uint32_t bar = smem_u32(&tempty_bar[b]);
+                asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(peer_addr(bar, 0)) : "memory");
+            }
+        };
         for (int t = first; t < a.tiles; t += step) {
             const Tile tl = tile_at(a, t);
-            const bool ok = wait(smem_u32(&tfull_bar[b]), tuse[b], abort, err);
-            if (!__all_sync(0xffffffffu, ok)) break;
-            fence_after();
+            if (PROMOTE) {
+                // the chunks' sums are added up in registers, and put back into the last one's columns
+                float sum[kSpan];
+#pragma unroll
+                for (int e = 0; e < kSpan; ++e) sum[e] = 0.f;
+                bool ok = true;
+                for (int k0 = 0; k0 < a.slabs; k0 += a.chunk) {
+                    ok = wait(smem_u32(&tfull_bar[b]), tuse[b], abort, err);
+                    if (!(ok = __all_sync(0xffffffffu, ok))) break;
+                    fence_after();
+                    const uint32_t ta = tmem + static_cast<uint32_t>(b * BN + c0) + (static_cast<uint32_t>(32 * quad) << 16);
+#pragma unroll
+                    for (int c = 0; c < kSpan; c += 32) {
+                        float v[32];
+                        tmem_load32(ta + static_cast<uint32_t>(c), v);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) sum[c + e] += v[e];
+                    }
+                    if (k0 + a.chunk < a.slabs) {
+                        hand_back();
+                        tuse[b] ^= 1u;
+                        b ^= 1;
+                    }
+                }
+                if (!ok) break;
+                const uint32_t ta = tmem + static_cast<uint32_t>(b * BN + c0) + (static_cast<uint32_t>(32 * quad) << 16);
+#pragma unroll
+                for (int c = 0; c < kSpan; c += 32) tmem_store32(ta + static_cast<uint32_t>(c), sum + c);
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+            } else {
+                const bool ok = wait(smem_u32(&tfull_bar[b]), tuse[b], abort, err);
+                if (!__all_sync(0xffffffffu, ok)) break;
+                fence_after();
+            }
             const int64_t i = static_cast<int64_t>(tl.m * CG + static_cast<int>(rank)) * 128 + 32 * quad + lane;
             const uint32_t ta = tmem + static_cast<uint32_t>(b * BN + c0) + (static_cast<uint32_t>(32 * quad) << 16);
 #pragma unroll 1
-            for (int c = 0; c < BN / 2; c += 32) {
+            for (int c = 0; c < kSpan; c += 32) {
                 float v[32];
                 tmem_load32(ta + static_cast<uint32_t>(c), v);
-                if (c + 32 >= BN / 2) {              // the last of this warp's columns: hand the accumulator back
-                    fence_before();
-                    __syncwarp();
-                    if (lane == 0) {
-                        const uint32_t bar = smem_u32(&tempty_bar[b]);
-                        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(CG == 1 ? peer_addr(bar, cluster_rank()) : peer_addr(bar, 0)) : "memory");
-                    }
-                }
+                if (c + 32 >= kSpan) hand_back();   // the last of this warp's columns
                 const int64_t j = static_cast<int64_t>(tl.n) * BN + c0 + c;
                 if (i < a.p.M) {
 #pragma unroll
@@ -393,88 +470,313 @@ __global__ void __launch_bounds__(kThreads, 1) tc_product_kernel(const __grid_co
     }
 }
 
+// ------------------------------------------------------------------------------------------
+// Few tiles: 128 x 64 of them, a cluster of CTAs each.  CTA q of a cluster takes its q-th of the stages, sums them
+// in chunks, leaves its partial tile in shared memory (where the ring was) and finishes its part of the rows.
+// ------------------------------------------------------------------------------------------
+constexpr int kSplitN = 64, kSplitPitch = kSplitN + 4;
+template <bool MNA, bool MNB>
+__global__ void __launch_bounds__(threads_of(8), 1) tc_split_kernel(const __grid_constant__ TcArgs a) {
+    chain_begin();
+    constexpr int kEpiWarps = 8, kProducer = 8, kIssuer = 9, kThreads = threads_of(8);
+    constexpr uint32_t SB = stage_bytes<kSplitN, 1>(), kCols = 2 * kSplitN;
+    extern __shared__ uint8_t dyn_smem[];
+    uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dyn_smem) + 1023) & ~uintptr_t(1023));
+    __shared__ __align__(8) uint64_t full_bar[kMaxStages], empty_bar[kMaxStages], tfull_bar[2], tempty_bar[2];
+    __shared__ uint32_t tmem_base;
+    __shared__ int abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, S = a.stages;
+    const int splits = gridDim.y, split = blockIdx.y;
+    const int k_first = static_cast<int>(static_cast<int64_t>(a.slabs) * split / splits);
+    const int k_last = static_cast<int>(static_cast<int64_t>(a.slabs) * (split + 1) / splits);
+    volatile int* abort = &abort_flag;
+    int* err = a.p.err;
+    if (threadIdx.x == 0) {
+        abort_flag = 0;
+        for (int q = 0; q < S; ++q) { mbar_init(smem_u32(&full_bar[q]), 1); mbar_init(smem_u32(&empty_bar[q]), 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&tfull_bar[b]), 1); mbar_init(smem_u32(&tempty_bar[b]), kEpiWarps); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kIssuer) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "r"(kCols));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = tmem_base;
+    const Tile tl = tile_at(a, blockIdx.x);
+    float sum[kSplitN / 2];
+#pragma unroll
+    for (int e = 0; e < kSplitN / 2; ++e) sum[e] = 0.f;
+    if (warp == kProducer) {
+        if (lane == 0) {
+            uint32_t issued = 0, last = 0;
+            int s = 0;
+            uint32_t use = 0;
+            bool ok = true;
+            for (int k = k_first; k < k_last; ++k) {
+                if (!(ok = wait(smem_u32(&empty_bar[s]), use ^ 1u, abort, err))) break;
+                const uint32_t bar = smem_u32(&full_bar[s]);
+                mbar_expect_tx(bar, SB);
+                load_stage<1, kSplitN, MNA, MNB>(a, k, tl.m * 128, tl.n * kSplitN, tl.node, smem_u32(ring + static_cast<size_t>(s) * SB), bar);
+                issued |= 1u << s;
+                last = (last & ~(1u << s)) | (use << s);
+                if (++s == S) { s = 0; use ^= 1u; }
+            }
+            if (!ok)                                 // let the copies already issued land
+                for (int q = 0; q < S; ++q)
+                    if (issued & (1u << q))
+                        for (int it = 0; it < 4000000 && !try_wait(smem_u32(&full_bar[q]), (last >> q) & 1u); ++it) __nanosleep(64);
+        }
+        __syncwarp();
+    } else if (warp == kIssuer) {
+        if (lane == 0) {
+            int s = 0, b = 0;
+            uint32_t use = 0, tuse[2] = {0, 0};
+            bool ok = true;
+            for (int k0 = k_first; k0 < k_last && ok; k0 += a.chunk) {
+                if (!(ok = wait(smem_u32(&tempty_bar[b]), tuse[b] ^ 1u, abort, err))) break;
+                fence_after();
+                for (int k = k0; k < min(k0 + a.chunk, k_last); ++k) {
+                    if (!(ok = wait(smem_u32(&full_bar[s]), use, abort, err))) break;
+                    fence_after();
+                    mma_stage<kSplitN, 1, MNA, MNB>(tmem + static_cast<uint32_t>(b * kSplitN), smem_u32(ring + static_cast<size_t>(s) * SB), k > k0);
+                    commit<1>(smem_u32(&empty_bar[s]));
+                    if (++s == S) { s = 0; use ^= 1u; }
+                }
+                if (!ok) break;
+                commit<1>(smem_u32(&tfull_bar[b]));
+                tuse[b] ^= 1u;
+                b ^= 1;
+            }
+        }
+        __syncwarp();
+    } else {
+        uint32_t tuse[2] = {0, 0};
+        int b = 0;
+        for (int k0 = k_first; k0 < k_last; k0 += a.chunk) {
+            const bool ok = wait(smem_u32(&tfull_bar[b]), tuse[b], abort, err);
+            if (!__all_sync(0xffffffffu, ok)) break;
+            fence_after();
+            float v[32];
+            tmem_load32(tmem + static_cast<uint32_t>(b * kSplitN + (warp >> 2) * 32) + (static_cast<uint32_t>(32 * (warp & 3)) << 16), v);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) sum[e] += v[e];
+            fence_before();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(smem_u32(&tempty_bar[b]));
+            tuse[b] ^= 1u;
+            b ^= 1;
+        }
+    }
+    fence_before();
+    __syncthreads();                                 // every stage has been read: the last products are done
+    float* part = reinterpret_cast<float*>(ring);
+    if (warp < kEpiWarps) {
+        float* to = part + (32 * (warp & 3) + lane) * kSplitPitch + (warp >> 2) * 32;
+#pragma unroll
+        for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(to + e) = make_float4(sum[e], sum[e + 1], sum[e + 2], sum[e + 3]);
+    }
+    __syncthreads();
+    if (splits > 1) cluster_sync();
+    const int rows = 128 / splits;                   // this CTA's rows of the tile, eight columns a thread
+    for (int e = threadIdx.x; e < rows * (kSplitN / 8); e += kThreads) {
+        const int r = split * rows + e / (kSplitN / 8), c = e % (kSplitN / 8) * 8;
+        const int64_t i = static_cast<int64_t>(tl.m) * 128 + r, j = static_cast<int64_t>(tl.n) * kSplitN + c;
+        if (i >= a.p.M || j >= a.p.N) continue;
+        float v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = 0.f;
+        for (int q = 0; q < splits; ++q) {
+            const uint32_t from = peer_addr(smem_u32(part + r * kSplitPitch + c), q);
+#pragma unroll
+            for (int h = 0; h < 8; h += 4) {
+                float x[4];
+                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                             : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]) : "r"(from + 4 * h) : "memory");
+#pragma unroll
+                for (int y = 0; y < 4; ++y) v[h + y] += x[y];
+            }
+        }
+        epilogue8(a, tl.node, i, j, v);
+    }
+    if (splits > 1) cluster_sync();                  // the peers are done with this CTA's shared memory
+    else __syncthreads();
+    if (warp == kIssuer) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols));
+    }
+}
+
+// Rows of `cols` elements, ld apart, as `planes` bf16 matrices in rows of ldp (a multiple of eight), one after the
+// other: x = hi + mid + lo, each the bf16 nearest to what is left.  Bound by HBM.
+constexpr int kPackThreads = 256;
+template <class T>
+__global__ void __launch_bounds__(kPackThreads) pack_kernel(const T* x, int64_t rows, int64_t cols, int64_t ld, bool wide,
+                                                            __nv_bfloat16* to, int64_t ldp, int planes) {
+    chain_begin();
+    const int64_t per = ldp / 8, total = rows * per;
+    for (int64_t g = static_cast<int64_t>(blockIdx.x) * kPackThreads + threadIdx.x; g < total; g += static_cast<int64_t>(gridDim.x) * kPackThreads) {
+        const int64_t i = g / per, j = (g - i * per) * 8;
+        const int n = static_cast<int>(cols - j < 8 ? cols - j : 8);
+        float v[8];
+        get8(x, i * ld + j, n, wide, sizeof(T) == 2 ? GLR_BF16 : GLR_F32, v);
+        for (int p = 0; p < planes; ++p) {
+            uint32_t w[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * q], v[2 * q + 1]);
+                // what would round up to infinity is cut off instead
+                if (isinf(__low2float(h)) && isfinite(v[2 * q])) h.x = __float2bfloat16_rz(v[2 * q]);
+                if (isinf(__high2float(h)) && isfinite(v[2 * q + 1])) h.y = __float2bfloat16_rz(v[2 * q + 1]);
+                w[q] = *reinterpret_cast<const uint32_t*>(&h);
+                // an infinity or NaN is the first plane's alone
+                v[2 * q] = isfinite(v[2 * q]) ? v[2 * q] - __low2float(h) : 0.f;
+                v[2 * q + 1] = isfinite(v[2 * q + 1]) ? v[2 * q + 1] - __high2float(h) : 0.f;
+            }
+            *reinterpret_cast<uint4*>(to + (p * rows + i) * ldp + j) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+}
+
 bool on16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
+// An operand as its storage: `rows` rows of `cols` contiguous elements ld apart (all nodes' rows together).
+struct Storage { int64_t rows, cols, ld; };
+Storage storage(int64_t si, int64_t sp, int64_t ni, int64_t np, int nodes) {
+    return sp == 1 ? Storage{ni, np, si} : Storage{np * nodes, ni, sp};
+}
+int64_t up8(int64_t x) { return (x + 7) / 8 * 8; }
+
 // The tile copies of an operand X(i, p): rows of 64 contraction elements (K-major), or 64 x 64 blocks of
-// (index, contraction) per node (MN-major).
-bool operand_map(CUtensorMap* map, const void* x, int64_t si, int64_t sp, int64_t sb, int64_t ni, int64_t np, int nodes, uint32_t rows) {
-    // a stride along a single row is never used; the copies only want it to be valid
-    if (ni == 1 && sp == 1) si = (np + 7) / 8 * 8;
-    if (np == 1 && sp != 1) sp = (ni + 7) / 8 * 8;
+// (index, contraction) per node (MN-major); planes one after the other.
+bool operand_map(CUtensorMap* map, const void* x, int64_t si, int64_t sp, int64_t sb, int64_t ni, int64_t np, int nodes, int planes,
+                 uint32_t rows) {
+    // a stride along a single row or plane is never used; the copies only want it to be valid
+    if (ni == 1 && sp == 1) si = up8(np);
+    if (np == 1 && sp != 1) sp = up8(ni);
     if (sp == 1) {
-        const uint64_t dims[2] = {static_cast<uint64_t>(np), static_cast<uint64_t>(ni)}, str[1] = {static_cast<uint64_t>(si) * 2};
-        const uint32_t box[2] = {kSlab, rows};
-        return host::encode_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, 2, dims, str, box, CU_TENSOR_MAP_SWIZZLE_128B);
+        const uint64_t dims[3] = {static_cast<uint64_t>(np), static_cast<uint64_t>(ni), static_cast<uint64_t>(planes)};
+        const uint64_t str[2] = {static_cast<uint64_t>(si) * 2, static_cast<uint64_t>(si * ni) * 2};
+        const uint32_t box[3] = {kSlab, rows, 1};
+        return host::encode_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, 3, dims, str, box, CU_TENSOR_MAP_SWIZZLE_128B);
     }
-    const uint64_t dims[3] = {static_cast<uint64_t>(ni), static_cast<uint64_t>(np), static_cast<uint64_t>(nodes)};
-    const uint64_t str[2] = {static_cast<uint64_t>(sp) * 2, static_cast<uint64_t>(nodes > 1 ? sb : sp) * 2};
+    const uint64_t dims[3] = {static_cast<uint64_t>(ni), static_cast<uint64_t>(np), static_cast<uint64_t>(nodes * planes)};
+    const uint64_t str[2] = {static_cast<uint64_t>(sp) * 2, static_cast<uint64_t>(nodes * planes > 1 ? sb : sp) * 2};
     const uint32_t box[3] = {64, kSlab, 1};
     return host::encode_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, 3, dims, str, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-template <int BN, int CG, bool MNA, bool MNB>
-cudaError_t launch(TcArgs& a, cudaStream_t st) {
-    constexpr uint32_t SB = stage_bytes<BN, CG>();
-    a.stages = std::min<int>(kMaxStages, static_cast<int>(kRingBytes / SB));
-    const size_t smem = std::max<size_t>(static_cast<size_t>(a.stages) * SB + 1024, 120 * 1024);
-    auto kernel = tc_product_kernel<BN, CG, MNA, MNB>;
+template <class Kernel>
+cudaError_t launch(Kernel kernel, const TcArgs& a, dim3 grid, dim3 cluster, int threads, size_t smem, cudaStream_t st) {
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
-    int dev = 0, sms = 0;
-    if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
-    if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
     cudaLaunchAttribute attr[2]{};
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = CG; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    attr[1].val.clusterDim.x = cluster.x; attr[1].val.clusterDim.y = cluster.y; attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = static_cast<unsigned>(std::min(a.tiles, sms / CG) * CG);
-    cfg.blockDim = kThreads; cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cfg.gridDim = grid; cfg.blockDim = threads; cfg.dynamicSmemBytes = smem; cfg.stream = st;
     cfg.attrs = attr; cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kernel, a);
 }
-template <int BN, int CG>
-cudaError_t launch_major(TcArgs& a, bool mna, bool mnb, cudaStream_t st) {
-    if (mna) return mnb ? launch<BN, CG, true, true>(a, st) : launch<BN, CG, true, false>(a, st);
-    return mnb ? launch<BN, CG, false, true>(a, st) : launch<BN, CG, false, false>(a, st);
+template <bool MNA, bool MNB>
+cudaError_t launch_major(TcArgs& a, bool promote, int splits, int sms, cudaStream_t st) {
+    const uint32_t sb = splits ? stage_bytes<kSplitN, 1>() : stage_bytes<256, 2>();
+    a.stages = std::min<int>(kMaxStages, static_cast<int>(kRingBytes / sb));
+    const size_t smem = std::max<size_t>(static_cast<size_t>(a.stages) * sb + 1024, 120 * 1024);
+    if (splits) return launch(tc_split_kernel<MNA, MNB>, a, dim3(static_cast<unsigned>(a.tiles), splits), dim3(1, splits), threads_of(8), smem, st);
+    const dim3 grid(static_cast<unsigned>(std::min(a.tiles, sms / 2) * 2));
+    return promote ? launch(tc_product_kernel<256, 2, MNA, MNB, true>, a, grid, dim3(2), threads_of(epi_warps(true)), smem, st)
+                   : launch(tc_product_kernel<256, 2, MNA, MNB, false>, a, grid, dim3(2), threads_of(epi_warps(false)), smem, st);
+}
+
+template <class T>
+cudaError_t pack(const void* x, const Storage& s, int planes, void* to, cudaStream_t st) {
+    const int64_t ldp = up8(s.cols), groups = (s.rows * (ldp / 8) + kPackThreads - 1) / kPackThreads;
+    const bool wide = on16(x) && s.ld * static_cast<int64_t>(sizeof(T)) % 16 == 0;
+    return launch_chain(pack_kernel<T>, static_cast<unsigned>(std::min<int64_t>(groups, 152 * 16)), kPackThreads, 0, st,
+                        static_cast<const T*>(x), s.rows, s.cols, s.ld, wide, static_cast<__nv_bfloat16*>(to), ldp, planes);
+}
+
+// Whether an operand's rows lie on 16 bytes as they are.
+bool lies_well(const void* x, int64_t si, int64_t sp, int64_t sb, int64_t ni, int64_t np, int nodes) {
+    const int64_t ld = sp == 1 ? si : sp, rows = sp == 1 ? ni : np;
+    return on16(x) && (rows == 1 || (ld % 8 == 0 && ld < (int64_t(1) << 36))) && (nodes == 1 || (sb % 8 == 0 && sb < (int64_t(1) << 36)));
 }
 
 }  // namespace
 
-bool tc_ok(const Product& p) {
-    auto operand = [&](const void* x, int64_t si, int64_t sp, int64_t sb, int64_t ni) {
-        const int64_t ld = sp == 1 ? si : sp, rows = sp == 1 ? ni : p.K;
-        return on16(x) && (rows == 1 || (ld % 8 == 0 && ld < (int64_t(1) << 36))) &&
-               (p.nodes == 1 || (sb % 8 == 0 && sb < (int64_t(1) << 36)));
-    };
-    return p.dtype == GLR_BF16 && p.K > 0 && p.M > 0 && p.N > 0 && operand(p.A, p.sAi, p.sAp, p.sAb, p.M) &&
-           operand(p.B, p.sBj, p.sBp, p.sBb, p.N);
+// Which operands a product has to have packed, and what that takes.
+TcPlan tc_plan(const Product& p) {
+    TcPlan t{};
+    if (p.K <= 0 || p.M <= 0 || p.N <= 0) return t;
+    if (p.nodes > 1 && (p.sAp == 1 || p.sBp == 1)) return t;     // (a single column: K-major, and those maps have no nodes)
+    t.planes = p.dtype == GLR_F32 ? 3 : 1;
+    t.pack_a = t.planes == 3 || !lies_well(p.A, p.sAi, p.sAp, p.sAb, p.M, p.K, p.nodes);
+    t.pack_b = t.planes == 3 || !lies_well(p.B, p.sBj, p.sBp, p.sBb, p.N, p.K, p.nodes);
+    const Storage a = storage(p.sAi, p.sAp, p.M, p.K, p.nodes), b = storage(p.sBj, p.sBp, p.N, p.K, p.nodes);
+    if (t.pack_a) t.bytes_a = (t.planes * a.rows * up8(a.cols) * 2 + 255) / 256 * 256;
+    if (t.pack_b) t.bytes_b = t.planes * b.rows * up8(b.cols) * 2;
+    // Packing reads both matrices once more and launches two kernels: it pays where the product itself is long and
+    // neither side is thin (measured at both ends: a 64-row product is faster unpacked).
+    const double flops = 2.0 * static_cast<double>(p.M) * static_cast<double>(p.N) * static_cast<double>(p.K) * p.nodes;
+    t.ok = !(t.pack_a || t.pack_b) || (p.M >= 128 && p.N >= 128 && flops >= 5e8);
+    return t;
 }
 
-cudaError_t tc_product(const Product& p, cudaStream_t st) {
+cudaError_t tc_product(const Product& p, const TcPlan& plan, void* workspace, cudaStream_t st) {
     TcArgs a{};
     a.p = p;
-    const bool mna = p.sAp != 1, mnb = p.sBp != 1;
-    const int BN = 256, CG = 2;
-    a.tiles_m = static_cast<int>((p.M + 128 * CG - 1) / (128 * CG));
-    a.tiles_n = static_cast<int>((p.N + BN - 1) / BN);
-    const int64_t tiles = static_cast<int64_t>(a.tiles_m) * a.tiles_n * p.nodes;
-    if (tiles > (1 << 30)) return cudaErrorInvalidValue;
-    a.tiles = static_cast<int>(tiles);
-    a.slabs = static_cast<int>((p.K + kSlab - 1) / kSlab);
-    const int64_t os = p.out_dtype == GLR_BF16 ? 2 : 4;
+    Product& q = a.p;
+    cudaError_t e = cudaSuccess;
+    auto packed = [&](const void*& x, int64_t& si, int64_t& sp, int64_t& sb, int64_t ni, uint8_t* to) {
+        const Storage s = storage(si, sp, ni, p.K, p.nodes);
+        e = plan.planes == 3 ? pack<float>(x, s, 3, to, st) : pack<__nv_bfloat16>(x, s, 1, to, st);
+        x = to;
+        (sp == 1 ? si : sp) = up8(s.cols);
+        sb = sp == 1 ? 0 : p.K * sp;
+    };
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    if (plan.pack_a) packed(q.A, q.sAi, q.sAp, q.sAb, p.M, ws);
+    if (e == cudaSuccess && plan.pack_b) packed(q.B, q.sBj, q.sBp, q.sBb, p.N, ws + plan.bytes_a);
+    if (e != cudaSuccess) return e;
+    int dev = 0, sms = 0;
+    if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
+    if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
+    const bool mna = q.sAp != 1, mnb = q.sBp != 1, promote = p.out_dtype == GLR_F32;
+    a.planes = plan.planes;
+    a.chunk = plan.planes == 3 ? 6 : 4;
+    const int64_t slabs = (p.K + kSlab - 1) / kSlab * (plan.planes == 3 ? 6 : 1);
+    if (slabs > (1 << 30)) return cudaErrorInvalidValue;
+    a.slabs = static_cast<int>(slabs);
+    // pairs' tiles of 256 x 256 where they fill most of the GPU, else 128 x 64 ones, shared by clusters
+    const int64_t big = ((p.M + 255) / 256) * ((p.N + 255) / 256) * p.nodes;
+    const int64_t small = ((p.M + 127) / 128) * ((p.N + kSplitN - 1) / kSplitN) * p.nodes;
+    int splits = 0;
+    if (big < sms / 4) {
+        splits = 1;
+        while (splits < 8 && small * splits * 2 <= sms && slabs >= 8 * splits) splits *= 2;
+    }
+    a.tiles_m = static_cast<int>((p.M + (splits ? 127 : 255)) / (splits ? 128 : 256));
+    a.tiles_n = static_cast<int>((p.N + (splits ? kSplitN : 256) - 1) / (splits ? kSplitN : 256));
+    if (std::max(big, small) > (1 << 30)) return cudaErrorInvalidValue;
+    a.tiles = static_cast<int>(splits ? small : big);
+    const int64_t os = p.out_dtype == GLR_BF16 ? 2 : 4, per16 = 16 / os;
     if (p.mode == kGradWeight) {
         a.wide = p.N * os % 16 == 0;
         for (int i = 0; i < p.nodes; ++i) a.wide = a.wide && on16(p.outs[i]);
     } else {
-        a.wide = (on16(p.out) && p.ldo % 8 == 0 ? 1 : 0) | (on16(p.bias) ? 2 : 0) | (on16(p.add) && p.ldadd % 8 == 0 ? 4 : 0) |
-                 (on16(p.pre) && p.ldpre % 8 == 0 ? 8 : 0) | (on16(p.aux) && p.ldaux % 8 == 0 ? 16 : 0);
+        a.wide = (on16(p.out) && p.ldo % per16 == 0 ? 1 : 0) | (on16(p.bias) ? 2 : 0) | (on16(p.add) && p.ldadd % per16 == 0 ? 4 : 0) |
+                 (on16(p.pre) && p.ldpre % per16 == 0 ? 8 : 0) | (on16(p.aux) && p.ldaux % per16 == 0 ? 16 : 0);
     }
-    if (!operand_map(&a.mapA, p.A, p.sAi, p.sAp, p.sAb, p.M, p.K, p.nodes, 128) ||
-        !operand_map(&a.mapB, p.B, p.sBj, p.sBp, p.sBb, p.N, p.K, p.nodes, BN / CG))
+    if (!operand_map(&a.mapA, q.A, q.sAi, q.sAp, q.sAb, p.M, p.K, p.nodes, a.planes, 128) ||
+        !operand_map(&a.mapB, q.B, q.sBj, q.sBp, q.sBb, p.N, p.K, p.nodes, a.planes, splits ? kSplitN : 128))
         return cudaErrorInvalidValue;
-    return launch_major<256, 2>(a, mna, mnb, st);
+    if (mna) return mnb ? launch_major<true, true>(a, promote, splits, sms, st) : launch_major<true, false>(a, promote, splits, sms, st);
+    return mnb ? launch_major<false, true>(a, promote, splits, sms, st) : launch_major<false, false>(a, promote, splits, sms, st);
 }
 
 }  // namespace linear

@@ -69,6 +69,28 @@ def _call(fn, args, stream) -> None:
         _check(rc)
 
 
+def _space(args, query, x: torch.Tensor, work: float, ragged: int, stream):
+    """The workspace that a product asks for (float32 or rows off 16 bytes, where it is large), from PyTorch's
+    allocator in the stream's own pool: its memory is reused in the order of the work that runs there."""
+    if (x.dtype == torch.bfloat16 and not ragged) or work < 5e8:
+        return None
+    need = ctypes.c_int64(0)
+    _check(query(ctypes.byref(args), ctypes.byref(need)))
+    if need.value == 0:
+        return None
+    space = _alloc(need.value, torch.uint8, x.device, stream)
+    args.workspace, args.workspace_bytes = space.data_ptr(), need.value
+    return space
+
+
+def _alloc(n: int, dtype, device, stream) -> torch.Tensor:
+    if stream is None:
+        return torch.empty(n, dtype=dtype, device=device)
+    own = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream_ptr(stream))
+    with torch.cuda.stream(own):
+        return torch.empty(n, dtype=dtype, device=device)
+
+
 def _activation(act: str) -> int:
     if act not in ACTIVATIONS:
         raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}")
@@ -88,8 +110,12 @@ def glr_linear(X: torch.Tensor, W: torch.Tensor, Y: torch.Tensor, *, bias: Optio
     y, ldy = _mat(Y, "Y", rows, n, dt)
     r, ldr = _mat(residual, "residual", rows, n, dt)
     p, ldp = _mat(preact, "preact", rows, n, dt)
-    _call(load().glr_linear, _lib.GlrLinearArgs(rows, n, k, x, ldx, w, ldw, y, ldy, _vec(bias, "bias", n, dt), r, ldr, p, ldp,
-                                                dtype, _activation(act)), stream)
+    lib = load()
+    args = _lib.GlrLinearArgs(rows, n, k, x, ldx, w, ldw, y, ldy, _vec(bias, "bias", n, dt), r, ldr, p, ldp, None, 0, dtype,
+                              _activation(act))
+    space = _space(args, lib.glr_linear_workspace, X, 2.0 * rows * n * k, ((x | w) & 15) | ((ldx | ldw) & 7), stream)
+    _call(lib.glr_linear, args, stream)
+    del space
 
 
 def glr_linear_grad_input(dZ: torch.Tensor, W: torch.Tensor, dX: torch.Tensor, *,
@@ -106,8 +132,12 @@ def glr_linear_grad_input(dZ: torch.Tensor, W: torch.Tensor, dX: torch.Tensor, *
     r, ldr = _mat(residual, "residual", rows, k, dt)
     p, ldp = _mat(preact, "preact", rows, k, dt)
     g, ldg = _mat(grad_out, "grad_out", rows, k, dt)
-    _call(load().glr_linear_grad_input, _lib.GlrLinearGradInputArgs(rows, n, k, z, lddz, w, ldw, x, lddx, r, ldr, p, ldp, g, ldg,
-                                                                    dtype, _activation(act)), stream)
+    lib = load()
+    args = _lib.GlrLinearGradInputArgs(rows, n, k, z, lddz, w, ldw, x, lddx, r, ldr, p, ldp, g, ldg, None, 0, dtype,
+                                       _activation(act))
+    space = _space(args, lib.glr_linear_grad_input_workspace, dZ, 2.0 * rows * n * k, ((z | w) & 15) | ((lddz | ldw) & 7), stream)
+    _call(lib.glr_linear_grad_input, args, stream)
+    del space
 
 
 def glr_linear_grad_weight(dZ: torch.Tensor, X: torch.Tensor, dW: Union[torch.Tensor, Sequence[torch.Tensor]], *,
@@ -135,9 +165,12 @@ def glr_linear_grad_weight(dZ: torch.Tensor, X: torch.Tensor, dW: Union[torch.Te
         wp[i] = _vec(g, f"dW[{i}]", n * k, gd)
     for i, g in enumerate(db or ()):
         bp[i] = _vec(g, f"db[{i}]", n, gd)
-    _call(load().glr_linear_grad_weight,
-          _lib.GlrLinearGradWeightArgs(nodes, rows // nodes, n, k, z, lddz, x, ldx, ctypes.addressof(wp),
-                                       None if db is None else ctypes.addressof(bp), dtype, grad_dtype), stream)
+    lib = load()
+    args = _lib.GlrLinearGradWeightArgs(nodes, rows // nodes, n, k, z, lddz, x, ldx, ctypes.addressof(wp),
+                                        None if db is None else ctypes.addressof(bp), None, 0, dtype, grad_dtype)
+    space = _space(args, lib.glr_linear_grad_weight_workspace, dZ, 2.0 * rows * n * k, ((z | x) & 15) | ((lddz | ldx) & 7), stream)
+    _call(lib.glr_linear_grad_weight, args, stream)
+    del space
 
 
 def glr_distill_loss(logits: torch.Tensor, teacher: torch.Tensor, ids: torch.Tensor, *, loss: torch.Tensor,
@@ -207,13 +240,7 @@ def glr_preference_loss(logits: torch.Tensor, tokens: torch.Tensor, offsets: tor
     o, owide = _index(offsets, "offsets", 2 * pairs + 1)
     need = 4 * rows + 16 * pairs + 1024
     if workspace is None:
-        # in the stream's own pool: its memory is reused in the order of the work that runs there
-        if stream is None:
-            workspace = torch.empty(need, device=logits.device)
-        else:
-            own = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream_ptr(stream))
-            with torch.cuda.stream(own):
-                workspace = torch.empty(need, device=logits.device)
+        workspace = _alloc(need, torch.float32, logits.device, stream)
     elif workspace.dtype != torch.float32 or not workspace.is_cuda or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous float32 CUDA tensor")
     _call(load().glr_preference_loss,

@@ -248,3 +248,90 @@ def test_results_are_reproducible():
         glr.glr_linear_grad_weight(dZ, X, a, db=da)
         glr.glr_linear_grad_weight(dZ, X, b, db=db)
         assert all(torch.equal(x, y) for x, y in zip(a + da, b + db))
+
+
+@pytest.mark.parametrize("nodes,rows,n,k", [(2, 64, 1, 64), (3, 40, 64, 1), (4, 7, 1, 1), (2, 1, 128, 192), (8, 1, 8, 8)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_grad_weight_of_single_columns_and_rows(nodes, rows, n, k, dt):
+    import paper_2507_08784_gb300 as glr
+    dt = DT[dt]
+    gen = torch.Generator().manual_seed(12)
+    dZ, X = _mat(nodes * rows, n, dt, gen), _mat(nodes * rows, k, dt, gen)
+    dW, db = [torch.empty(n, k, device="cuda") for _ in range(nodes)], [torch.empty(n, device="cuda") for _ in range(nodes)]
+    glr.glr_linear_grad_weight(dZ, X, dW, db=db)
+    for i in range(nodes):
+        a, b = (t[i * rows:(i + 1) * rows].cpu().double().T.contiguous() for t in (dZ, X))
+        _check(dW[i], a @ b.T, _sum_tol(a, b, rows, dt), torch.float32)
+        _check(db[i], a.sum(1), (rows + 8) * 2.0 ** -23 * a.abs().sum(1), torch.float32)
+
+
+LARGE = [(700, 640, 1111), (257, 2048, 1024), (2048, 300, 901), (4100, 256, 513), (130, 1000, 4096)]
+
+
+@pytest.mark.parametrize("rows,n,k", LARGE)
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("pad,shift", [(0, 0), (1, 3)])
+def test_large_products(rows, n, k, dt, pad, shift):
+    """Products large enough to be laid out for the tensor cores first (fp32, and rows off 16 bytes), with positive
+    inputs too, where a truncated sum would drift: every sum within 2^-20 of sum |a| |b|, which rounded additions
+    of up to 4100 products meet (their errors add up like their square root) and truncated ones do not."""
+    import paper_2507_08784_gb300 as glr
+    dt = DT[dt]
+    gen = torch.Generator().manual_seed(rows)
+    for positive in (False, True):
+        X, W, Z = _mat(rows, k, dt, gen, pad, shift), _mat(n, k, dt, gen, pad, shift), _mat(rows, n, dt, gen, pad, shift)
+        if positive:
+            X.abs_(), W.abs_(), Z.abs_()
+        Y, ybuf = _out(rows, n, dt, pad, shift)
+        dX, xbuf = _out(rows, k, dt, pad, shift)
+        dW = [torch.empty(n, k, device="cuda")]
+        glr.glr_linear(X, W, Y, act="relu")
+        glr.glr_linear_grad_input(Z, W, dX)
+        glr.glr_linear_grad_weight(Z, X, dW)
+        torch.cuda.synchronize()
+        x, w, z = X.double(), W.double(), Z.double()
+        for got, a, b in ((Y, x, w), (dX, z, w.T), (dW[0], z.T, x.T)):
+            want, size = a @ b.T, a.abs() @ b.abs().T
+            want = want.clamp(min=0) if got is Y else want
+            tol = 2.0 ** -20 * size + (2.0 ** -8 * want.abs() if got.dtype == torch.bfloat16 else 2.0 ** -22 * want.abs())
+            if got.dtype == torch.bfloat16:
+                tol += (a.shape[1] + 8) * 2.0 ** -23 * size       # bf16 results may be summed by truncation
+            assert ((got.double() - want).abs() <= tol).all(), (positive, float(((got.double() - want).abs() / size).max()))
+        assert _untouched(ybuf, Y) and _untouched(xbuf, dX)
+    glr.glr_operator_status()
+
+
+def test_large_products_without_workspace():
+    """The C entry point with no workspace takes another way to the same product."""
+    import ctypes
+    import paper_2507_08784_gb300 as glr
+    from paper_2507_08784_gb300 import _lib
+    gen = torch.Generator().manual_seed(3)
+    X, W, Y, Z = (_mat(*s, torch.float32, gen) for s in ((600, 900), (700, 900), (600, 700), (600, 700)))
+    args = _lib.GlrLinearArgs(600, 700, 900, X.data_ptr(), 900, W.data_ptr(), 900, Y.data_ptr(), 700, None, None, 0, None, 0, None, 0, 0, 0)
+    need = ctypes.c_int64(-1)
+    assert glr.load().glr_linear_workspace(ctypes.byref(args), ctypes.byref(need)) == 0 and need.value >= 3 * 2 * 1300 * 900
+    assert glr.load().glr_linear(ctypes.byref(args), torch.cuda.current_stream().cuda_stream) == 0
+    glr.glr_linear(X, W, Z)
+    torch.cuda.synchronize()
+    size, want = X.double().abs() @ W.double().abs().T, X.double() @ W.double().T
+    for got in (Y, Z):
+        assert ((got.double() - want).abs() <= 2.0 ** -19 * size).all()
+
+
+def test_infinities_survive_the_layout():
+    """fp32 matrices cut into planes: an infinity or a NaN stays in its row, and the type's extremes are finite."""
+    import paper_2507_08784_gb300 as glr
+    gen = torch.Generator().manual_seed(4)
+    X, W = _mat(300, 1500, torch.float32, gen), _mat(1200, 1500, torch.float32, gen)
+    Y, Z = torch.empty(300, 1200, device="cuda"), torch.empty(300, 1200, device="cuda")
+    glr.glr_linear(X, W, Y)
+    X[5, 7], X[90, 1400], X[200] = float("nan"), float("inf"), 0.0
+    X[200, 3] = 1.5e38
+    glr.glr_linear(X, W, Z)
+    assert torch.isnan(Z[5]).all() and not torch.isfinite(Z[90]).any()
+    keep = [i for i in range(300) if i not in (5, 90, 200)]
+    assert torch.equal(Z[keep], Y[keep])
+    small = W[:, 3].abs() < 2
+    want = 1.5e38 * W[:, 3].double()
+    assert ((Z[200].double() - want).abs()[small] <= 2.0 ** -19 * want.abs()[small]).all()
