@@ -17,10 +17,14 @@
 //
 // The tensor cores truncate their fp32 sums (about 2^-25 of the sum for every 16 elements, always the same
 // way), which over a long contraction is far above fp32 rounding: where the result is fp32 (PROMOTE), and in
-// tc_split_kernel, the sums of 256 contraction elements join the total in rounded additions by the epilogue warps.
+// tc_split_kernel, the sums of 256 contraction elements (64 of three planes) join the total in rounded additions by
+// the epilogue warps.
 //
-// What bounds it: the tensor pipe for contractions of about 1000 and more; below that the epilogue, which
-// each thread does on a row of the tile, 16 bytes a load or store.
+// What bounds it: the tensor pipe for contractions of about 1000 and more; below that the epilogue.  Tensor memory
+// gives a thread a row, whose aligned results it stores as they come (32 rows a store).  Where there is more to read
+// or write than that, or rows off 16 bytes, the epilogue warps turn 32 x 32 blocks round in shared memory, so that
+// four lanes share a row and an access covers whole sectors of eight (8192 x 4096 x 11008 with an activation and its
+// pre-activation 508 -> 496 us; without either 461 against 470 us, a stage of the ring less).
 #include <algorithm>
 
 #include "glr_host.cuh"
@@ -42,15 +46,19 @@ constexpr int epi_warps(bool promote) { return promote ? 16 : 8; }     // ... of
 constexpr int threads_of(int epi) { return (epi + 2) * 32; }
 constexpr int kSlab = 64;                       // contraction elements a stage: one 128-byte swizzle row of bf16
 constexpr int kMaxStages = 8;
-constexpr size_t kRingBytes = 208 * 1024;
+constexpr size_t kSmemBytes = 224 * 1024;       // of it the ring has what the epilogue warps' blocks leave
+constexpr int kBlockPitch = 36;                 // floats a row of a 32 x 32 block: no two lanes on a bank
+constexpr size_t kBlockBytes = 32 * kBlockPitch * 4;
 constexpr int kBand = 8;                        // tile rows walked together, so that a wave's operands share L2
 
 struct TcArgs {
     Product p;
     CUtensorMap mapA, mapB;
-    int tiles_m, tiles_n, tiles, slabs, stages;
+    int tiles_m, tiles_n, slabs, stages;
+    int tiles, whole;                           // tiles in all; from `whole` on they are halves of BN / 2 columns
     int planes;                                 // 1, or 3: a slab of the contraction is six products of planes
     int chunk;                                  // slabs whose sums are kept in tensor memory (PROMOTE)
+    int turned;                                 // whether the epilogue turns blocks round in shared memory
     int wide;                                   // 16-byte accesses: bit 0 out, 1 bias, 2 add, 3 pre, 4 aux
 };
 
@@ -217,16 +225,17 @@ __device__ __forceinline__ void act8(float (&v)[8], int act) {
 }
 
 // The epilogue on eight neighbouring columns of a row (i, j): acc in v.
+template <int MODE, int DT>
 __device__ __forceinline__ void epilogue8(const TcArgs& a, int node, int64_t i, int64_t j, float (&v)[8]) {
     const Product& p = a.p;
-    const int dt = p.out_dtype;                 // but in kGradWeight also the inputs' type
+    constexpr int dt = DT;                      // of the results, and but in kGradWeight of the inputs too
     const int n = static_cast<int>(p.N - j < 8 ? p.N - j : 8);
-    if (p.mode == kGradWeight) {
+    if (MODE == kGradWeight) {
         put8(p.outs[node], i * p.N + j, n, a.wide & 1, dt, v);
         return;
     }
     float x[8];
-    if (p.mode == kForward) {
+    if (MODE == kForward) {
         if (p.bias) {
             get8(p.bias, j, n, a.wide & 2, dt, x);
 #pragma unroll
@@ -256,16 +265,25 @@ __device__ __forceinline__ void epilogue8(const TcArgs& a, int node, int64_t i, 
     put8(p.out, i * p.ldo + j, n, a.wide & 1, dt, v);
 }
 
-struct Tile { int node, m, n; };
+// A tile: its node, rows 128 CG m .., columns n0 .. n0 + bn.
+struct Tile { int node, m, n0, bn; };
+template <int BN>
 __device__ __forceinline__ Tile tile_at(const TcArgs& a, int t) {
-    const int per = a.tiles_m * a.tiles_n;
     Tile r;
+    r.bn = BN;
+    int half = 0;
+    if (t >= a.whole) {                              // the last ones as halves, for twice as many CTAs
+        half = (t - a.whole) & 1;
+        t = a.whole + ((t - a.whole) >> 1);
+        r.bn = BN / 2;
+    }
+    const int per = a.tiles_m * a.tiles_n;
     r.node = t / per;
     t -= r.node * per;
     const int band = t / (kBand * a.tiles_n), in = t - band * kBand * a.tiles_n;
     const int h = min(kBand, a.tiles_m - band * kBand);
     r.m = band * kBand + in % h;
-    r.n = in / h;
+    r.n0 = in / h * BN + half * (BN / 2);
     return r;
 }
 
@@ -273,9 +291,10 @@ __device__ __forceinline__ Tile tile_at(const TcArgs& a, int t) {
 __device__ __forceinline__ int plane_a(int pair) { return pair == 0 ? 2 : pair == 2 || pair == 3 ? 1 : 0; }
 __device__ __forceinline__ int plane_b(int pair) { return pair == 1 ? 2 : pair == 2 || pair == 4 ? 1 : 0; }
 
-// The tile copies of stage k (slab k, or product k mod 6 of slab k / 6) of rows m0.. of A and n0.. of B.
-template <int CG, int BB, bool MNA, bool MNB>
-__device__ __forceinline__ void load_stage(const TcArgs& a, int k, int m0, int n0, int node, uint32_t st, uint32_t bar) {
+// The tile copies of stage k (slab k, or product k mod 6 of slab k / 6) of rows m0.. of A and `nb` 64-row pieces from
+// n0 on of B.
+template <int CG, bool MNA, bool MNB>
+__device__ __forceinline__ void load_stage(const TcArgs& a, int k, int m0, int n0, int nb, int node, uint32_t st, uint32_t bar) {
     const int slab = a.planes == 3 ? k / 6 : k, pair = a.planes == 3 ? k - 6 * slab : 0;
     const int pa = a.planes == 3 ? plane_a(pair) : 0, pb = a.planes == 3 ? plane_b(pair) : 0, x = slab * kSlab;
     if (MNA) {
@@ -283,31 +302,37 @@ __device__ __forceinline__ void load_stage(const TcArgs& a, int k, int m0, int n
     } else {
         load_3d<CG>(st, &a.mapA, x, m0, pa, bar);
     }
-    if (MNB) {
-        for (int c = 0; c < BB / 64; ++c) load_3d<CG>(st + 16384 + c * 8192, &a.mapB, n0 + 64 * c, x, node + a.p.nodes * pb, bar);
-    } else {
-        load_3d<CG>(st + 16384, &a.mapB, x, n0, pb, bar);
+    for (int c = 0; c < nb; ++c) {
+        if (MNB) load_3d<CG>(st + 16384 + c * 8192, &a.mapB, n0 + 64 * c, x, node + a.p.nodes * pb, bar);
+        else load_3d<CG>(st + 16384 + c * 8192, &a.mapB, x, n0 + 64 * c, pb, bar);
     }
 }
-// ... and its MMAs, sixteen contraction elements each.
-template <int BN, int CG, bool MNA, bool MNB>
-__device__ __forceinline__ void mma_stage(uint32_t d, uint32_t st, bool add) {
-    constexpr uint32_t id = (1u << 4) | (1u << 7) | (1u << 10) | (MNA ? 1u << 15 : 0u) | (MNB ? 1u << 16 : 0u) |
-                            (static_cast<uint32_t>(BN >> 3) << 17) | (static_cast<uint32_t>(8 * CG) << 24);
+// ... and its MMAs, sixteen contraction elements each, on `bn` columns.
+template <int CG, bool MNA, bool MNB>
+__device__ __forceinline__ void mma_stage(uint32_t d, uint32_t st, int bn, bool add) {
+    const uint32_t id = (1u << 4) | (1u << 7) | (1u << 10) | (MNA ? 1u << 15 : 0u) | (MNB ? 1u << 16 : 0u) |
+                        (static_cast<uint32_t>(bn >> 3) << 17) | (static_cast<uint32_t>(8 * CG) << 24);
 #pragma unroll
     for (int kk = 0; kk < kSlab / 16; ++kk)
         mma_f16<CG>(d, operand_desc(st + (MNA ? 2048 : 32) * kk, MNA, 8192),
                     operand_desc(st + 16384 + (MNB ? 2048 : 32) * kk, MNB, 8192), id, (add || kk) ? 1u : 0u);
 }
 
-template <int BN, int CG, bool MNA, bool MNB, bool PROMOTE>
+// How a mode's operands lie: the forward product's both along the contraction, ...
+constexpr bool mn_major_a(int mode) { return mode == kGradWeight; }
+constexpr bool mn_major_b(int mode) { return mode != kForward; }
+
+template <int BN, int CG, int MODE, bool PROMOTE>
 __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_kernel(const __grid_constant__ TcArgs a) {
     chain_begin();
+    constexpr bool MNA = mn_major_a(MODE), MNB = mn_major_b(MODE);
+    constexpr int DT = PROMOTE ? GLR_F32 : GLR_BF16;
     constexpr int kEpiWarps = epi_warps(PROMOTE), kProducer = kEpiWarps, kIssuer = kEpiWarps + 1, kSpan = BN / (kEpiWarps / 4);
-    constexpr uint32_t SB = stage_bytes<BN, CG>(), BB = BN / CG;     // bytes a stage, rows of B in this CTA
+    constexpr uint32_t SB = stage_bytes<BN, CG>();
     constexpr uint32_t kCols = 2 * BN;                               // two accumulators of BN columns
     extern __shared__ uint8_t dyn_smem[];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dyn_smem) + 1023) & ~uintptr_t(1023));
+    float* blocks = reinterpret_cast<float*>(ring + static_cast<size_t>(a.stages) * SB);
     __shared__ __align__(8) uint64_t full_bar[kMaxStages], empty_bar[kMaxStages], tfull_bar[2], tempty_bar[2];
     __shared__ uint32_t tmem_base;
     __shared__ int abort_flag;
@@ -343,15 +368,16 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
             uint32_t use = 0, issued = 0, last = 0;
             bool ok = true;
             for (int t = first; t < a.tiles && ok; t += step) {
-                const Tile tl = tile_at(a, t);
-                const int m0 = (tl.m * CG + static_cast<int>(rank)) * 128, n0 = tl.n * BN + static_cast<int>(rank) * static_cast<int>(BB);
+                const Tile tl = tile_at<BN>(a, t);
+                const int mine = tl.bn / CG;         // columns of the tile whose rows of B this CTA holds
+                const int m0 = (tl.m * CG + static_cast<int>(rank)) * 128, n0 = tl.n0 + static_cast<int>(rank) * mine;
                 for (int k = 0; k < a.slabs; ++k) {
                     if (!(ok = wait(smem_u32(&empty_bar[s]), use ^ 1u, abort, err))) break;
                     const uint32_t st = smem_u32(ring + static_cast<size_t>(s) * SB);
                     uint32_t bar = smem_u32(&full_bar[s]);
-                    if (rank == 0) mbar_expect_tx(bar, SB * CG);
+                    if (rank == 0) mbar_expect_tx(bar, static_cast<uint32_t>(16384 + mine * 128) * CG);
                     else bar = peer_addr(bar, 0);
-                    load_stage<CG, static_cast<int>(BB), MNA, MNB>(a, k, m0, n0, tl.node, st, bar);
+                    load_stage<CG, MNA, MNB>(a, k, m0, n0, mine / 64, tl.node, st, bar);
                     issued |= 1u << s;
                     last = (last & ~(1u << s)) | (use << s);
                     if (++s == S) { s = 0; use ^= 1u; }
@@ -369,6 +395,7 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
             uint32_t use = 0, tuse[2] = {0, 0};
             bool ok = true;
             for (int t = first; t < a.tiles && ok; t += step) {
+                const int bn = t < a.whole ? BN : BN / 2;
                 for (int k0 = 0; k0 < a.slabs && ok; k0 += PROMOTE ? a.chunk : a.slabs) {
                     if (!(ok = wait(smem_u32(&tempty_bar[b]), tuse[b] ^ 1u, abort, err))) break;
                     fence_after();
@@ -377,7 +404,7 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
                     for (int k = k0; k < k1; ++k) {
                         if (!(ok = wait(smem_u32(&full_bar[s]), use, abort, err))) break;
                         fence_after();
-                        mma_stage<BN, CG, MNA, MNB>(d, smem_u32(ring + static_cast<size_t>(s) * SB), k > k0);
+                        mma_stage<CG, MNA, MNB>(d, smem_u32(ring + static_cast<size_t>(s) * SB), bn, k > k0);
                         commit<CG>(smem_u32(&empty_bar[s]));
                         if (++s == S) { s = 0; use ^= 1u; }
                     }
@@ -393,7 +420,8 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
         // warp w: tensor-memory lanes 32 (w mod 4) .. + 31, the w / 4-th kSpan columns
         uint32_t tuse[2] = {0, 0};
         int b = 0;
-        const int quad = warp & 3, c0 = (warp >> 2) * kSpan;
+        const int quad = warp & 3;
+        float* block = blocks + warp * 32 * kBlockPitch;
         auto hand_back = [&]() {
             fence_before();
             __syncwarp();
@@ -403,7 +431,8 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
             }
         };
         for (int t = first; t < a.tiles; t += step) {
-            const Tile tl = tile_at(a, t);
+            const Tile tl = tile_at<BN>(a, t);
+            const int span = tl.bn == BN ? kSpan : kSpan / 2, c0 = (warp >> 2) * span;
             if (PROMOTE) {
                 // the chunks' sums are added up in registers, and put back into the last one's columns
                 float sum[kSpan];
@@ -417,6 +446,7 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
                     const uint32_t ta = tmem + static_cast<uint32_t>(b * BN + c0) + (static_cast<uint32_t>(32 * quad) << 16);
 #pragma unroll
                     for (int c = 0; c < kSpan; c += 32) {
+                        if (c >= span) break;
                         float v[32];
                         tmem_load32(ta + static_cast<uint32_t>(c), v);
 #pragma unroll
@@ -431,29 +461,50 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
                 if (!ok) break;
                 const uint32_t ta = tmem + static_cast<uint32_t>(b * BN + c0) + (static_cast<uint32_t>(32 * quad) << 16);
 #pragma unroll
-                for (int c = 0; c < kSpan; c += 32) tmem_store32(ta + static_cast<uint32_t>(c), sum + c);
+                for (int c = 0; c < kSpan; c += 32)
+                    if (c < span) tmem_store32(ta + static_cast<uint32_t>(c), sum + c);
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
             } else {
                 const bool ok = wait(smem_u32(&tfull_bar[b]), tuse[b], abort, err);
                 if (!__all_sync(0xffffffffu, ok)) break;
                 fence_after();
             }
-            const int64_t i = static_cast<int64_t>(tl.m * CG + static_cast<int>(rank)) * 128 + 32 * quad + lane;
+            const int64_t i0 = static_cast<int64_t>(tl.m * CG + static_cast<int>(rank)) * 128 + 32 * quad;
             const uint32_t ta = tmem + static_cast<uint32_t>(b * BN + c0) + (static_cast<uint32_t>(32 * quad) << 16);
 #pragma unroll 1
-            for (int c = 0; c < kSpan; c += 32) {
+            for (int c = 0; c < span; c += 32) {
                 float v[32];
                 tmem_load32(ta + static_cast<uint32_t>(c), v);
-                if (c + 32 >= kSpan) hand_back();   // the last of this warp's columns
-                const int64_t j = static_cast<int64_t>(tl.n) * BN + c0 + c;
-                if (i < a.p.M) {
+                if (c + 32 >= span) hand_back();     // the last of this warp's columns
+                if (!a.turned) {
+                    const int64_t j = static_cast<int64_t>(tl.n0) + c0 + c;
+                    if (i0 + lane < a.p.M) {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        float w[8];
+                        for (int q = 0; q < 4; ++q) {
+                            float w[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) w[e] = v[8 * q + e];
-                        if (j + 8 * q < a.p.N) epilogue8(a, tl.node, i, j + 8 * q, w);
+                            for (int e = 0; e < 8; ++e) w[e] = v[8 * q + e];
+                            if (j + 8 * q < a.p.N) epilogue8<MODE, DT>(a, tl.node, i0 + lane, j + 8 * q, w);
+                        }
                     }
+                    continue;
+                }
+                __syncwarp();
+#pragma unroll
+                for (int e = 0; e < 32; e += 4)
+                    *reinterpret_cast<float4*>(block + lane * kBlockPitch + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+                __syncwarp();
+                const int64_t j = static_cast<int64_t>(tl.n0) + c0 + c + (lane & 3) * 8;
+#pragma unroll 1
+                for (int q = 0; q < 4; ++q) {
+                    const int r = 8 * q + (lane >> 2);
+                    float w[8];
+#pragma unroll
+                    for (int h = 0; h < 8; h += 4) {
+                        const float4 x = *reinterpret_cast<const float4*>(block + r * kBlockPitch + (lane & 3) * 8 + h);
+                        w[h] = x.x; w[h + 1] = x.y; w[h + 2] = x.z; w[h + 3] = x.w;
+                    }
+                    if (i0 + r < a.p.M && j < a.p.N) epilogue8<MODE, DT>(a, tl.node, i0 + r, j, w);
                 }
             }
             tuse[b] ^= 1u;
@@ -475,9 +526,10 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
 // in chunks, leaves its partial tile in shared memory (where the ring was) and finishes its part of the rows.
 // ------------------------------------------------------------------------------------------
 constexpr int kSplitN = 64, kSplitPitch = kSplitN + 4;
-template <bool MNA, bool MNB>
+template <int MODE>
 __global__ void __launch_bounds__(threads_of(8), 1) tc_split_kernel(const __grid_constant__ TcArgs a) {
     chain_begin();
+    constexpr bool MNA = mn_major_a(MODE), MNB = mn_major_b(MODE);
     constexpr int kEpiWarps = 8, kProducer = 8, kIssuer = 9, kThreads = threads_of(8);
     constexpr uint32_t SB = stage_bytes<kSplitN, 1>(), kCols = 2 * kSplitN;
     extern __shared__ uint8_t dyn_smem[];
@@ -505,7 +557,7 @@ __global__ void __launch_bounds__(threads_of(8), 1) tc_split_kernel(const __grid
     __syncthreads();
     fence_after();
     const uint32_t tmem = tmem_base;
-    const Tile tl = tile_at(a, blockIdx.x);
+    const Tile tl = tile_at<kSplitN>(a, blockIdx.x);
     float sum[kSplitN / 2];
 #pragma unroll
     for (int e = 0; e < kSplitN / 2; ++e) sum[e] = 0.f;
@@ -519,7 +571,7 @@ __global__ void __launch_bounds__(threads_of(8), 1) tc_split_kernel(const __grid
                 if (!(ok = wait(smem_u32(&empty_bar[s]), use ^ 1u, abort, err))) break;
                 const uint32_t bar = smem_u32(&full_bar[s]);
                 mbar_expect_tx(bar, SB);
-                load_stage<1, kSplitN, MNA, MNB>(a, k, tl.m * 128, tl.n * kSplitN, tl.node, smem_u32(ring + static_cast<size_t>(s) * SB), bar);
+                load_stage<1, MNA, MNB>(a, k, tl.m * 128, tl.n0, 1, tl.node, smem_u32(ring + static_cast<size_t>(s) * SB), bar);
                 issued |= 1u << s;
                 last = (last & ~(1u << s)) | (use << s);
                 if (++s == S) { s = 0; use ^= 1u; }
@@ -541,7 +593,7 @@ __global__ void __launch_bounds__(threads_of(8), 1) tc_split_kernel(const __grid
                 for (int k = k0; k < min(k0 + a.chunk, k_last); ++k) {
                     if (!(ok = wait(smem_u32(&full_bar[s]), use, abort, err))) break;
                     fence_after();
-                    mma_stage<kSplitN, 1, MNA, MNB>(tmem + static_cast<uint32_t>(b * kSplitN), smem_u32(ring + static_cast<size_t>(s) * SB), k > k0);
+                    mma_stage<1, MNA, MNB>(tmem + static_cast<uint32_t>(b * kSplitN), smem_u32(ring + static_cast<size_t>(s) * SB), kSplitN, k > k0);
                     commit<1>(smem_u32(&empty_bar[s]));
                     if (++s == S) { s = 0; use ^= 1u; }
                 }
@@ -583,7 +635,7 @@ __global__ void __launch_bounds__(threads_of(8), 1) tc_split_kernel(const __grid
     const int rows = 128 / splits;                   // this CTA's rows of the tile, eight columns a thread
     for (int e = threadIdx.x; e < rows * (kSplitN / 8); e += kThreads) {
         const int r = split * rows + e / (kSplitN / 8), c = e % (kSplitN / 8) * 8;
-        const int64_t i = static_cast<int64_t>(tl.m) * 128 + r, j = static_cast<int64_t>(tl.n) * kSplitN + c;
+        const int64_t i = static_cast<int64_t>(tl.m) * 128 + r, j = static_cast<int64_t>(tl.n0) + c;
         if (i >= a.p.M || j >= a.p.N) continue;
         float v[8];
 #pragma unroll
@@ -599,7 +651,8 @@ __global__ void __launch_bounds__(threads_of(8), 1) tc_split_kernel(const __grid
                 for (int y = 0; y < 4; ++y) v[h + y] += x[y];
             }
         }
-        epilogue8(a, tl.node, i, j, v);
+        if (a.p.out_dtype == GLR_F32) epilogue8<MODE, GLR_F32>(a, tl.node, i, j, v);
+        else epilogue8<MODE, GLR_BF16>(a, tl.node, i, j, v);
     }
     if (splits > 1) cluster_sync();                  // the peers are done with this CTA's shared memory
     else __syncthreads();
@@ -682,15 +735,21 @@ cudaError_t launch(Kernel kernel, const TcArgs& a, dim3 grid, dim3 cluster, int 
     cfg.attrs = attr; cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kernel, a);
 }
-template <bool MNA, bool MNB>
-cudaError_t launch_major(TcArgs& a, bool promote, int splits, int sms, cudaStream_t st) {
-    const uint32_t sb = splits ? stage_bytes<kSplitN, 1>() : stage_bytes<256, 2>();
-    a.stages = std::min<int>(kMaxStages, static_cast<int>(kRingBytes / sb));
-    const size_t smem = std::max<size_t>(static_cast<size_t>(a.stages) * sb + 1024, 120 * 1024);
-    if (splits) return launch(tc_split_kernel<MNA, MNB>, a, dim3(static_cast<unsigned>(a.tiles), splits), dim3(1, splits), threads_of(8), smem, st);
+template <int MODE>
+cudaError_t launch_mode(TcArgs& a, bool promote, int splits, int sms, cudaStream_t st) {
+    if (splits) {
+        // half of an SM's shared memory: two CTAs an SM
+        a.stages = 4;
+        const size_t smem = a.stages * stage_bytes<kSplitN, 1>() + 1024;
+        return launch(tc_split_kernel<MODE>, a, dim3(static_cast<unsigned>(a.tiles), splits), dim3(1, splits), threads_of(8), smem, st);
+    }
+    const uint32_t sb = stage_bytes<256, 2>();
+    const size_t blocks = a.turned ? epi_warps(promote) * kBlockBytes : 0;
+    a.stages = std::min<int>(kMaxStages, static_cast<int>((kSmemBytes - 1024 - blocks) / sb));
+    const size_t smem = static_cast<size_t>(a.stages) * sb + 1024 + blocks;
     const dim3 grid(static_cast<unsigned>(std::min(a.tiles, sms / 2) * 2));
-    return promote ? launch(tc_product_kernel<256, 2, MNA, MNB, true>, a, grid, dim3(2), threads_of(epi_warps(true)), smem, st)
-                   : launch(tc_product_kernel<256, 2, MNA, MNB, false>, a, grid, dim3(2), threads_of(epi_warps(false)), smem, st);
+    return promote ? launch(tc_product_kernel<256, 2, MODE, true>, a, grid, dim3(2), threads_of(epi_warps(true)), smem, st)
+                   : launch(tc_product_kernel<256, 2, MODE, false>, a, grid, dim3(2), threads_of(epi_warps(false)), smem, st);
 }
 
 template <class T>
@@ -713,7 +772,8 @@ bool lies_well(const void* x, int64_t si, int64_t sp, int64_t sb, int64_t ni, in
 TcPlan tc_plan(const Product& p) {
     TcPlan t{};
     if (p.K <= 0 || p.M <= 0 || p.N <= 0) return t;
-    if (p.nodes > 1 && (p.sAp == 1 || p.sBp == 1)) return t;     // (a single column: K-major, and those maps have no nodes)
+    // (single columns may lie along the contraction in a mode that has them across it)
+    if ((p.sAp != 1) != mn_major_a(p.mode) || (p.sBp != 1) != mn_major_b(p.mode)) return t;
     t.planes = p.dtype == GLR_F32 ? 3 : 1;
     t.pack_a = t.planes == 3 || !lies_well(p.A, p.sAi, p.sAp, p.sAb, p.M, p.K, p.nodes);
     t.pack_b = t.planes == 3 || !lies_well(p.B, p.sBj, p.sBp, p.sBb, p.N, p.K, p.nodes);
@@ -746,24 +806,30 @@ cudaError_t tc_product(const Product& p, const TcPlan& plan, void* workspace, cu
     int dev = 0, sms = 0;
     if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
     if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
-    const bool mna = q.sAp != 1, mnb = q.sBp != 1, promote = p.out_dtype == GLR_F32;
+    const bool promote = p.out_dtype == GLR_F32;
     a.planes = plan.planes;
     a.chunk = plan.planes == 3 ? 6 : 4;
     const int64_t slabs = (p.K + kSlab - 1) / kSlab * (plan.planes == 3 ? 6 : 1);
     if (slabs > (1 << 30)) return cudaErrorInvalidValue;
     a.slabs = static_cast<int>(slabs);
-    // pairs' tiles of 256 x 256 where they fill most of the GPU, else 128 x 64 ones, shared by clusters
-    const int64_t big = ((p.M + 255) / 256) * ((p.N + 255) / 256) * p.nodes;
+    // Pairs' tiles of 256 x 256, or 128 x 64 ones shared by clusters: whichever is done first at 512 cycles a slab of a
+    // wave of pairs and 400 a slab of a small tile on an SM (measured: its 24 KiB from the L2).
+    const int64_t big = ((p.M + 255) / 256) * ((p.N + 255) / 256) * p.nodes, pairs = sms / 2;
     const int64_t small = ((p.M + 127) / 128) * ((p.N + kSplitN - 1) / kSplitN) * p.nodes;
     int splits = 0;
-    if (big < sms / 4) {
+    if (std::max<int64_t>(sms, small) * 400 < (big + pairs - 1) / pairs * sms * 512) {
         splits = 1;
-        while (splits < 8 && small * splits * 2 <= sms && slabs >= 8 * splits) splits *= 2;
+        while (splits < 8 && small * splits * 2 <= 2 * sms && slabs >= 8 * splits) splits *= 2;
     }
     a.tiles_m = static_cast<int>((p.M + (splits ? 127 : 255)) / (splits ? 128 : 256));
     a.tiles_n = static_cast<int>((p.N + (splits ? kSplitN : 256) - 1) / (splits ? kSplitN : 256));
     if (std::max(big, small) > (1 << 30)) return cudaErrorInvalidValue;
-    a.tiles = static_cast<int>(splits ? small : big);
+    a.tiles = a.whole = static_cast<int>(splits ? small : big);
+    if (!splits) {
+        // a last wave of at most half the pairs: half tiles, one for each of twice as many
+        const int rest = static_cast<int>(big % pairs);
+        if (rest > 0 && 2 * rest <= pairs) { a.whole -= rest; a.tiles += rest; }
+    }
     const int64_t os = p.out_dtype == GLR_BF16 ? 2 : 4, per16 = 16 / os;
     if (p.mode == kGradWeight) {
         a.wide = p.N * os % 16 == 0;
@@ -773,10 +839,12 @@ cudaError_t tc_product(const Product& p, const TcPlan& plan, void* workspace, cu
                  (on16(p.pre) && p.ldpre % per16 == 0 ? 8 : 0) | (on16(p.aux) && p.ldaux % per16 == 0 ? 16 : 0);
     }
     if (!operand_map(&a.mapA, q.A, q.sAi, q.sAp, q.sAb, p.M, p.K, p.nodes, a.planes, 128) ||
-        !operand_map(&a.mapB, q.B, q.sBj, q.sBp, q.sBb, p.N, p.K, p.nodes, a.planes, splits ? kSplitN : 128))
+        !operand_map(&a.mapB, q.B, q.sBj, q.sBp, q.sBb, p.N, p.K, p.nodes, a.planes, 64))
         return cudaErrorInvalidValue;
-    if (mna) return mnb ? launch_major<true, true>(a, promote, splits, sms, st) : launch_major<true, false>(a, promote, splits, sms, st);
-    return mnb ? launch_major<false, true>(a, promote, splits, sms, st) : launch_major<false, false>(a, promote, splits, sms, st);
+    a.turned = p.add || p.pre || p.aux || !(a.wide & 1);
+    return p.mode == kForward ? launch_mode<kForward>(a, promote, splits, sms, st)
+         : p.mode == kGradInput ? launch_mode<kGradInput>(a, promote, splits, sms, st)
+                                : launch_mode<kGradWeight>(a, promote, splits, sms, st);
 }
 
 }  // namespace linear
