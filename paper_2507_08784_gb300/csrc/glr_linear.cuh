@@ -52,27 +52,43 @@ struct ColumnSums {
 };
 cudaError_t column_sums(const ColumnSums& c, cudaStream_t st);
 
-// The activations and their slopes (GLR_ACT_*).
+// The activations and their slopes (GLR_ACT_*).  FAST, for results that are rounded to bf16: exponentials and
+// quotients by the hardware's approximations (a few 2^-22 relative), tanh u as 1 - 2 / (1 + exp(2 u)).
+template <bool FAST>
+__device__ __forceinline__ float exp_of(float x) { return FAST ? __expf(x) : expf(x); }
+template <bool FAST>
+__device__ __forceinline__ float over(float x, float y) { return FAST ? __fdividef(x, y) : x / y; }
+template <bool FAST>
+__device__ __forceinline__ float tanh_of(float u) {
+    // (beyond 40 the quotient's denominator would leave the range of the fast division)
+    return FAST ? 1.f - __fdividef(2.f, 1.f + __expf(2.f * fminf(u, 40.f))) : tanhf(u);
+}
+template <bool FAST>
+__device__ __forceinline__ float sigmoid_of(float z) {
+    return over<FAST>(1.f, 1.f + exp_of<FAST>(FAST ? fminf(-z, 80.f) : -z));
+}
+template <bool FAST>
 __device__ __forceinline__ float act_value(float z, int act) {
     switch (act) {
         case GLR_ACT_RELU: return z <= 0.f ? 0.f : z;            // a NaN stays one
         case GLR_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.7071067811865476f));
-        case GLR_ACT_GELU_TANH: return 0.5f * z * (1.f + tanhf(0.7978845608028654f * (z + 0.044715f * z * z * z)));
-        case GLR_ACT_SILU: return z / (1.f + expf(-z));
+        case GLR_ACT_GELU_TANH: return 0.5f * z * (1.f + tanh_of<FAST>(0.7978845608028654f * (z + 0.044715f * z * z * z)));
+        case GLR_ACT_SILU: return FAST ? z * sigmoid_of<FAST>(z) : z / (1.f + expf(-z));
         default: return z;
     }
 }
+template <bool FAST>
 __device__ __forceinline__ float act_slope(float z, int act) {
     switch (act) {
         case GLR_ACT_RELU: return z <= 0.f ? 0.f : z > 0.f ? 1.f : z;
         case GLR_ACT_GELU:
-            return 0.5f * (1.f + erff(z * 0.7071067811865476f)) + z * (0.3989422804014327f * expf(-0.5f * z * z));
+            return 0.5f * (1.f + erff(z * 0.7071067811865476f)) + z * (0.3989422804014327f * exp_of<FAST>(-0.5f * z * z));
         case GLR_ACT_GELU_TANH: {
-            const float t = tanhf(0.7978845608028654f * (z + 0.044715f * z * z * z));
+            const float t = tanh_of<FAST>(0.7978845608028654f * (z + 0.044715f * z * z * z));
             return 0.5f * (1.f + t) + 0.5f * z * (1.f - t * t) * 0.7978845608028654f * (1.f + 3.f * 0.044715f * z * z);
         }
         case GLR_ACT_SILU: {
-            const float p = 1.f / (1.f + expf(-z));
+            const float p = sigmoid_of<FAST>(z);
             return p * (1.f + z * (1.f - p));
         }
         default: return 1.f;

@@ -149,13 +149,13 @@ __device__ __forceinline__ void finish(const Product& p, int node, int64_t i, in
         put(p.outs[node], i * p.N + j, p.out_dtype, acc);
     } else if (p.mode == kForward) {
         const float z = p.bias ? acc + get(p.bias, j, p.dtype) : acc;
-        float y = act_value(z, p.act);
+        float y = act_value<false>(z, p.act);
         if (p.add) y += get(p.add, i * p.ldadd + j, p.dtype);
         if (p.aux) put(p.aux, i * p.ldaux + j, p.dtype, z);
         put(p.out, i * p.ldo + j, p.dtype, y);
     } else {
         const float g = p.add ? acc + get(p.add, i * p.ldadd + j, p.dtype) : acc;
-        const float d = p.pre ? g * act_slope(get(p.pre, i * p.ldpre + j, p.dtype), p.act) : g;
+        const float d = p.pre ? g * act_slope<false>(get(p.pre, i * p.ldpre + j, p.dtype), p.act) : g;
         if (p.aux) put(p.aux, i * p.ldaux + j, p.dtype, g);
         put(p.out, i * p.ldo + j, p.dtype, d);
     }

@@ -21,10 +21,8 @@
 // the epilogue warps.
 //
 // What bounds it: the tensor pipe for contractions of about 1000 and more; below that the epilogue.  Tensor memory
-// gives a thread a row, whose aligned results it stores as they come (32 rows a store).  Where there is more to read
-// or write than that, or rows off 16 bytes, the epilogue warps turn 32 x 32 blocks round in shared memory, so that
-// four lanes share a row and an access covers whole sectors of eight (8192 x 4096 x 11008 with an activation and its
-// pre-activation 508 -> 496 us; without either 461 against 470 us, a stage of the ring less).
+// gives a thread a row; the epilogue warps turn 32 x 32 blocks round in shared memory, so that four lanes share a
+// row and an access covers whole sectors of eight rows.
 #include <algorithm>
 
 #include "glr_host.cuh"
@@ -58,7 +56,6 @@ struct TcArgs {
     int tiles, whole;                           // tiles in all; from `whole` on they are halves of BN / 2 columns
     int planes;                                 // 1, or 3: a slab of the contraction is six products of planes
     int chunk;                                  // slabs whose sums are kept in tensor memory (PROMOTE)
-    int turned;                                 // whether the epilogue turns blocks round in shared memory
     int wide;                                   // 16-byte accesses: bit 0 out, 1 bias, 2 add, 3 pre, 4 aux
 };
 
@@ -208,12 +205,12 @@ __device__ __forceinline__ void put8(void* base, int64_t at, int n, bool wide, i
         for (int e = 0; e < 8; ++e) if (e < n) p[e] = __float2bfloat16_rn(v[e]);
     }
 }
-template <bool SLOPE>
+template <bool SLOPE, bool FAST>
 __device__ __forceinline__ void act8(float (&v)[8], int act) {
     switch (act) {                               // one branch for the eight
 #define GLR_ACT_CASE(A)                                                                               \
         case A:                                                                                       \
-            _Pragma("unroll") for (int e = 0; e < 8; ++e) v[e] = SLOPE ? act_slope(v[e], A) : act_value(v[e], A); \
+            _Pragma("unroll") for (int e = 0; e < 8; ++e) v[e] = SLOPE ? act_slope<FAST>(v[e], A) : act_value<FAST>(v[e], A); \
             break;
         GLR_ACT_CASE(GLR_ACT_RELU)
         GLR_ACT_CASE(GLR_ACT_GELU)
@@ -242,7 +239,7 @@ __device__ __forceinline__ void epilogue8(const TcArgs& a, int node, int64_t i, 
             for (int e = 0; e < 8; ++e) v[e] += x[e];
         }
         if (p.aux) put8(p.aux, i * p.ldaux + j, n, a.wide & 16, dt, v);
-        act8<false>(v, p.act);
+        act8<false, DT == GLR_BF16>(v, p.act);
         if (p.add) {
             get8(p.add, i * p.ldadd + j, n, a.wide & 4, dt, x);
 #pragma unroll
@@ -257,7 +254,7 @@ __device__ __forceinline__ void epilogue8(const TcArgs& a, int node, int64_t i, 
         if (p.aux) put8(p.aux, i * p.ldaux + j, n, a.wide & 16, dt, v);
         if (p.pre) {
             get8(p.pre, i * p.ldpre + j, n, a.wide & 8, dt, x);
-            act8<true>(x, p.act);
+            act8<true, DT == GLR_BF16>(x, p.act);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] *= x[e];
         }
@@ -476,19 +473,6 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
                 float v[32];
                 tmem_load32(ta + static_cast<uint32_t>(c), v);
                 if (c + 32 >= span) hand_back();     // the last of this warp's columns
-                if (!a.turned) {
-                    const int64_t j = static_cast<int64_t>(tl.n0) + c0 + c;
-                    if (i0 + lane < a.p.M) {
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            float w[8];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) w[e] = v[8 * q + e];
-                            if (j + 8 * q < a.p.N) epilogue8<MODE, DT>(a, tl.node, i0 + lane, j + 8 * q, w);
-                        }
-                    }
-                    continue;
-                }
                 __syncwarp();
 #pragma unroll
                 for (int e = 0; e < 32; e += 4)
@@ -744,7 +728,7 @@ cudaError_t launch_mode(TcArgs& a, bool promote, int splits, int sms, cudaStream
         return launch(tc_split_kernel<MODE>, a, dim3(static_cast<unsigned>(a.tiles), splits), dim3(1, splits), threads_of(8), smem, st);
     }
     const uint32_t sb = stage_bytes<256, 2>();
-    const size_t blocks = a.turned ? epi_warps(promote) * kBlockBytes : 0;
+    const size_t blocks = epi_warps(promote) * kBlockBytes;
     a.stages = std::min<int>(kMaxStages, static_cast<int>((kSmemBytes - 1024 - blocks) / sb));
     const size_t smem = static_cast<size_t>(a.stages) * sb + 1024 + blocks;
     const dim3 grid(static_cast<unsigned>(std::min(a.tiles, sms / 2) * 2));
@@ -841,7 +825,6 @@ cudaError_t tc_product(const Product& p, const TcPlan& plan, void* workspace, cu
     if (!operand_map(&a.mapA, q.A, q.sAi, q.sAp, q.sAb, p.M, p.K, p.nodes, a.planes, 128) ||
         !operand_map(&a.mapB, q.B, q.sBj, q.sBp, q.sBb, p.N, p.K, p.nodes, a.planes, 64))
         return cudaErrorInvalidValue;
-    a.turned = p.add || p.pre || p.aux || !(a.wide & 1);
     return p.mode == kForward ? launch_mode<kForward>(a, promote, splits, sms, st)
          : p.mode == kGradInput ? launch_mode<kGradInput>(a, promote, splits, sms, st)
                                 : launch_mode<kGradWeight>(a, promote, splits, sms, st);
