@@ -6,7 +6,7 @@
 // above 2^-24, one after the other in the same accumulator.
 //
 // tc_product_kernel, persistent: a CTA (CG = 1) or a pair of CTAs on two SMs (CG = 2) takes 128 CG x BN output
-// tiles in turn.  One warp copies operand slabs of 64 contraction elements (128-byte swizzle) into a ring of
+// tiles in turn.  Two warps copy operand slabs of 64 contraction elements (128-byte swizzle) into a ring of
 // shared-memory stages, one thread issues tcgen05.mma.kind::f16 (of the pair's first CTA: each CTA holds its
 // 128 rows of A and half of B's, and the result's rows stay in their CTA's tensor memory), and eight warps
 // bring the finished accumulator through the epilogue while the next tile's products run into the other half
@@ -41,7 +41,7 @@ using tc::mbar_init;
 using tc::smem_u32;
 
 constexpr int epi_warps(bool promote) { return promote ? 16 : 8; }     // ... of 64 or 128 columns each
-constexpr int threads_of(int epi) { return (epi + 2) * 32; }
+constexpr int threads_of(int epi) { return (epi + 3) * 32; }             // ... and two copying warps and the issuer
 constexpr int kSlab = 64;                       // contraction elements a stage: one 128-byte swizzle row of bf16
 constexpr int kMaxStages = 8;
 constexpr size_t kSmemBytes = 224 * 1024;       // of it the ring has what the epilogue warps' blocks leave
@@ -75,9 +75,12 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// (What these barriers hand over is read by tile copies, MMAs and tensor-memory loads, which their commits and
+// the tcgen05 fences order.  A wait that acquires for the cluster would clear the L1 each time, and an arrival
+// that releases for it would wait for the stores before it: together 690 cycles for the issuer's 512-cycle slab.)
 __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
     uint32_t done;
-    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
                  : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
@@ -118,13 +121,13 @@ __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint
         asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
                      ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(acc));
 }
-// Arrives on `bar` (of both CTAs of a pair) when the products issued so far are done.
+// Arrives on `bar` (of the CTAs of `mask`) when the products issued so far are done.
 template <int CG>
-__device__ __forceinline__ void commit(uint32_t bar) {
+__device__ __forceinline__ void commit(uint32_t bar, uint16_t mask = 1) {
     if (CG == 1) tc::mma_commit(bar);
     else
         asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                     ::"r"(bar), "h"(static_cast<uint16_t>(3)) : "memory");
+                     ::"r"(bar), "h"(mask) : "memory");
 }
 __device__ __forceinline__ void tmem_load32(uint32_t ta, float (&v)[32]) {
     uint32_t u[32];
@@ -288,20 +291,34 @@ __device__ __forceinline__ Tile tile_at(const TcArgs& a, int t) {
 __device__ __forceinline__ int plane_a(int pair) { return pair == 0 ? 2 : pair == 2 || pair == 3 ? 1 : 0; }
 __device__ __forceinline__ int plane_b(int pair) { return pair == 1 ? 2 : pair == 2 || pair == 4 ? 1 : 0; }
 
-// The tile copies of stage k (slab k, or product k mod 6 of slab k / 6) of rows m0.. of A and `nb` 64-row pieces from
-// n0 on of B.
-template <int CG, bool MNA, bool MNB>
-__device__ __forceinline__ void load_stage(const TcArgs& a, int k, int m0, int n0, int nb, int node, uint32_t st, uint32_t bar) {
-    const int slab = a.planes == 3 ? k / 6 : k, pair = a.planes == 3 ? k - 6 * slab : 0;
-    const int pa = a.planes == 3 ? plane_a(pair) : 0, pb = a.planes == 3 ? plane_b(pair) : 0, x = slab * kSlab;
+// The tile copies of stage k (slab k, or product k mod 6 of slab k / 6): rows m0.. of A, and `nb` 64-row pieces of B
+// from n0 on.
+template <int CG, bool MNA>
+__device__ __forceinline__ void load_a(const TcArgs& a, int k, int m0, int node, uint32_t st, uint32_t bar) {
+    int x = k * kSlab, z = node;
+    if (a.planes == 3) {
+        const int slab = k / 6;
+        x = slab * kSlab;
+        z += a.p.nodes * plane_a(k - 6 * slab);
+    }
     if (MNA) {
-        for (int c = 0; c < 2; ++c) load_3d<CG>(st + c * 8192, &a.mapA, m0 + 64 * c, x, node + a.p.nodes * pa, bar);
+        load_3d<CG>(st, &a.mapA, m0, x, z, bar);
+        load_3d<CG>(st + 8192, &a.mapA, m0 + 64, x, z, bar);
     } else {
-        load_3d<CG>(st, &a.mapA, x, m0, pa, bar);
+        load_3d<CG>(st, &a.mapA, x, m0, z, bar);
+    }
+}
+template <int CG, bool MNB>
+__device__ __forceinline__ void load_b(const TcArgs& a, int k, int n0, int nb, int node, uint32_t st, uint32_t bar) {
+    int x = k * kSlab, z = node;
+    if (a.planes == 3) {
+        const int slab = k / 6;
+        x = slab * kSlab;
+        z += a.p.nodes * plane_b(k - 6 * slab);
     }
     for (int c = 0; c < nb; ++c) {
-        if (MNB) load_3d<CG>(st + 16384 + c * 8192, &a.mapB, n0 + 64 * c, x, node + a.p.nodes * pb, bar);
-        else load_3d<CG>(st + 16384 + c * 8192, &a.mapB, x, n0 + 64 * c, pb, bar);
+        if (MNB) load_3d<CG>(st + 16384 + c * 8192, &a.mapB, n0 + 64 * c, x, z, bar);
+        else load_3d<CG>(st + 16384 + c * 8192, &a.mapB, x, n0 + 64 * c, z, bar);
     }
 }
 // ... and its MMAs, sixteen contraction elements each, on `bn` columns.
@@ -319,12 +336,13 @@ __device__ __forceinline__ void mma_stage(uint32_t d, uint32_t st, int bn, bool 
 constexpr bool mn_major_a(int mode) { return mode == kGradWeight; }
 constexpr bool mn_major_b(int mode) { return mode != kForward; }
 
-template <int BN, int CG, int MODE, bool PROMOTE>
+template <int BN, int MODE, bool PROMOTE>
 __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_kernel(const __grid_constant__ TcArgs a) {
     chain_begin();
+    constexpr int CG = 2;
     constexpr bool MNA = mn_major_a(MODE), MNB = mn_major_b(MODE);
     constexpr int DT = PROMOTE ? GLR_F32 : GLR_BF16;
-    constexpr int kEpiWarps = epi_warps(PROMOTE), kProducer = kEpiWarps, kIssuer = kEpiWarps + 1, kSpan = BN / (kEpiWarps / 4);
+    constexpr int kEpiWarps = epi_warps(PROMOTE), kCopyA = kEpiWarps, kCopyB = kEpiWarps + 1, kIssuer = kEpiWarps + 2, kSpan = BN / (kEpiWarps / 4);
     constexpr uint32_t SB = stage_bytes<BN, CG>();
     constexpr uint32_t kCols = 2 * BN;                               // two accumulators of BN columns
     extern __shared__ uint8_t dyn_smem[];
@@ -334,8 +352,9 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
     __shared__ uint32_t tmem_base;
     __shared__ int abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, S = a.stages;
-    const uint32_t rank = CG == 1 ? 0 : cluster_rank();
+    const uint32_t rank = cluster_rank();
     const int first = blockIdx.x / CG, step = gridDim.x / CG;
+    constexpr uint16_t both = 3;                      // the pair's CTAs
     volatile int* abort = &abort_flag;
     int* err = a.p.err;
     if (threadIdx.x == 0) {
@@ -345,22 +364,19 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kIssuer) {
-        if (CG == 1) {
-            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "r"(kCols));
-            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-        } else {
-            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "r"(kCols));
-            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
-        }
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "r"(kCols));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
     }
     fence_before();
     __syncthreads();
-    if (CG == 2) cluster_sync();
+    cluster_sync();
     fence_after();
     const uint32_t tmem = tmem_base;
 
-    if (warp == kProducer) {
+    if (warp == kCopyA || warp == kCopyB) {
+        // one warp copies A, one B: an issue of copies takes a good hundred cycles, and a slab's products 512
         if (lane == 0) {
+            const bool is_a = warp == kCopyA;
             int s = 0;
             uint32_t use = 0, issued = 0, last = 0;
             bool ok = true;
@@ -370,11 +386,13 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
                 const int m0 = (tl.m * CG + static_cast<int>(rank)) * 128, n0 = tl.n0 + static_cast<int>(rank) * mine;
                 for (int k = 0; k < a.slabs; ++k) {
                     if (!(ok = wait(smem_u32(&empty_bar[s]), use ^ 1u, abort, err))) break;
-                    const uint32_t st = smem_u32(ring + static_cast<size_t>(s) * SB);
-                    uint32_t bar = smem_u32(&full_bar[s]);
-                    if (rank == 0) mbar_expect_tx(bar, static_cast<uint32_t>(16384 + mine * 128) * CG);
-                    else bar = peer_addr(bar, 0);
-                    load_stage<CG, MNA, MNB>(a, k, m0, n0, mine / 64, tl.node, st, bar);
+                    const uint32_t st = smem_u32(ring + static_cast<size_t>(s) * SB), bar = peer_addr(smem_u32(&full_bar[s]), 0);
+                    if (is_a) {
+                        if (rank == 0) mbar_expect_tx(smem_u32(&full_bar[s]), static_cast<uint32_t>(16384 + mine * 128) * CG);
+                        load_a<CG, MNA>(a, k, m0, tl.node, st, bar);
+                    } else {
+                        load_b<CG, MNB>(a, k, n0, mine / 64, tl.node, st, bar);
+                    }
                     issued |= 1u << s;
                     last = (last & ~(1u << s)) | (use << s);
                     if (++s == S) { s = 0; use ^= 1u; }
@@ -402,11 +420,11 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
                         if (!(ok = wait(smem_u32(&full_bar[s]), use, abort, err))) break;
                         fence_after();
                         mma_stage<CG, MNA, MNB>(d, smem_u32(ring + static_cast<size_t>(s) * SB), bn, k > k0);
-                        commit<CG>(smem_u32(&empty_bar[s]));
+                        commit<CG>(smem_u32(&empty_bar[s]), both);
                         if (++s == S) { s = 0; use ^= 1u; }
                     }
                     if (!ok) break;
-                    commit<CG>(smem_u32(&tfull_bar[b]));
+                    commit<CG>(smem_u32(&tfull_bar[b]), both);
                     tuse[b] ^= 1u;
                     b ^= 1;
                 }
@@ -424,7 +442,7 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
             __syncwarp();
             if (lane == 0) {
                 const uint32_t bar = smem_u32(&tempty_bar[b]);
-                asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(peer_addr(bar, 0)) : "memory");
+                asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(peer_addr(bar, 0)) : "memory");
             }
         };
         for (int t = first; t < a.tiles; t += step) {
@@ -497,11 +515,10 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
     }
     fence_before();
     __syncthreads();
-    if (CG == 2) cluster_sync();                     // the pair's barriers and tensor memory are done with
+    cluster_sync();                                  // the cluster's barriers and tensor memory are done with
     if (warp == kIssuer) {
         fence_after();
-        if (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols));
-        else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols));
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols));
     }
 }
 
@@ -514,7 +531,7 @@ template <int MODE>
 __global__ void __launch_bounds__(threads_of(8), 1) tc_split_kernel(const __grid_constant__ TcArgs a) {
     chain_begin();
     constexpr bool MNA = mn_major_a(MODE), MNB = mn_major_b(MODE);
-    constexpr int kEpiWarps = 8, kProducer = 8, kIssuer = 9, kThreads = threads_of(8);
+    constexpr int kEpiWarps = 8, kCopyA = 8, kCopyB = 9, kIssuer = 10, kThreads = threads_of(8);
     constexpr uint32_t SB = stage_bytes<kSplitN, 1>(), kCols = 2 * kSplitN;
     extern __shared__ uint8_t dyn_smem[];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dyn_smem) + 1023) & ~uintptr_t(1023));
@@ -545,7 +562,7 @@ __global__ void __launch_bounds__(threads_of(8), 1) tc_split_kernel(const __grid
     float sum[kSplitN / 2];
 #pragma unroll
     for (int e = 0; e < kSplitN / 2; ++e) sum[e] = 0.f;
-    if (warp == kProducer) {
+    if (warp == kCopyA || warp == kCopyB) {
         if (lane == 0) {
             uint32_t issued = 0, last = 0;
             int s = 0;
@@ -553,9 +570,13 @@ __global__ void __launch_bounds__(threads_of(8), 1) tc_split_kernel(const __grid
             bool ok = true;
             for (int k = k_first; k < k_last; ++k) {
                 if (!(ok = wait(smem_u32(&empty_bar[s]), use ^ 1u, abort, err))) break;
-                const uint32_t bar = smem_u32(&full_bar[s]);
-                mbar_expect_tx(bar, SB);
-                load_stage<1, MNA, MNB>(a, k, tl.m * 128, tl.n0, 1, tl.node, smem_u32(ring + static_cast<size_t>(s) * SB), bar);
+                const uint32_t bar = smem_u32(&full_bar[s]), st = smem_u32(ring + static_cast<size_t>(s) * SB);
+                if (warp == kCopyA) {
+                    mbar_expect_tx(bar, SB);
+                    load_a<1, MNA>(a, k, tl.m * 128, tl.node, st, bar);
+                } else {
+                    load_b<1, MNB>(a, k, tl.n0, 1, tl.node, st, bar);
+                }
                 issued |= 1u << s;
                 last = (last & ~(1u << s)) | (use << s);
                 if (++s == S) { s = 0; use ^= 1u; }
@@ -732,8 +753,8 @@ cudaError_t launch_mode(TcArgs& a, bool promote, int splits, int sms, cudaStream
     a.stages = std::min<int>(kMaxStages, static_cast<int>((kSmemBytes - 1024 - blocks) / sb));
     const size_t smem = static_cast<size_t>(a.stages) * sb + 1024 + blocks;
     const dim3 grid(static_cast<unsigned>(std::min(a.tiles, sms / 2) * 2));
-    return promote ? launch(tc_product_kernel<256, 2, MODE, true>, a, grid, dim3(2), threads_of(epi_warps(true)), smem, st)
-                   : launch(tc_product_kernel<256, 2, MODE, false>, a, grid, dim3(2), threads_of(epi_warps(false)), smem, st);
+    return promote ? launch(tc_product_kernel<256, MODE, true>, a, grid, dim3(2), threads_of(epi_warps(true)), smem, st)
+                   : launch(tc_product_kernel<256, MODE, false>, a, grid, dim3(2), threads_of(epi_warps(false)), smem, st);
 }
 
 template <class T>
@@ -800,6 +821,7 @@ cudaError_t tc_product(const Product& p, const TcPlan& plan, void* workspace, cu
     // wave of pairs and 400 a slab of a small tile on an SM (measured: its 24 KiB from the L2).
     const int64_t big = ((p.M + 255) / 256) * ((p.N + 255) / 256) * p.nodes, pairs = sms / 2;
     const int64_t small = ((p.M + 127) / 128) * ((p.N + kSplitN - 1) / kSplitN) * p.nodes;
+    if (std::max(big, small) > (1 << 30)) return cudaErrorInvalidValue;
     int splits = 0;
     if (std::max<int64_t>(sms, small) * 400 < (big + pairs - 1) / pairs * sms * 512) {
         splits = 1;
@@ -807,7 +829,6 @@ cudaError_t tc_product(const Product& p, const TcPlan& plan, void* workspace, cu
     }
     a.tiles_m = static_cast<int>((p.M + (splits ? 127 : 255)) / (splits ? 128 : 256));
     a.tiles_n = static_cast<int>((p.N + (splits ? kSplitN : 256) - 1) / (splits ? kSplitN : 256));
-    if (std::max(big, small) > (1 << 30)) return cudaErrorInvalidValue;
     a.tiles = a.whole = static_cast<int>(splits ? small : big);
     if (!splits) {
         // a last wave of at most half the pairs: half tiles, one for each of twice as many
