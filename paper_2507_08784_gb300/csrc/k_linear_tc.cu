@@ -34,6 +34,7 @@ namespace linear {
 
 namespace {
 
+using tc::elect_one;
 using tc::fence_after;
 using tc::fence_before;
 using tc::mbar_expect_tx;
@@ -293,10 +294,10 @@ __device__ __forceinline__ int plane_b(int pair) { return pair == 1 ? 2 : pair =
 
 // The tile copies of stage k (slab k, or product k mod 6 of slab k / 6): rows m0.. of A, and `nb` 64-row pieces of B
 // from n0 on.
-template <int CG, bool MNA>
+template <int CG, bool MNA, bool PLANES>
 __device__ __forceinline__ void load_a(const TcArgs& a, int k, int m0, int node, uint32_t st, uint32_t bar) {
     int x = k * kSlab, z = node;
-    if (a.planes == 3) {
+    if (PLANES && a.planes == 3) {
         const int slab = k / 6;
         x = slab * kSlab;
         z += a.p.nodes * plane_a(k - 6 * slab);
@@ -308,10 +309,10 @@ __device__ __forceinline__ void load_a(const TcArgs& a, int k, int m0, int node,
         load_3d<CG>(st, &a.mapA, x, m0, z, bar);
     }
 }
-template <int CG, bool MNB>
+template <int CG, bool MNB, bool PLANES>
 __device__ __forceinline__ void load_b(const TcArgs& a, int k, int n0, int nb, int node, uint32_t st, uint32_t bar) {
     int x = k * kSlab, z = node;
-    if (a.planes == 3) {
+    if (PLANES && a.planes == 3) {
         const int slab = k / 6;
         x = slab * kSlab;
         z += a.p.nodes * plane_b(k - 6 * slab);
@@ -375,7 +376,7 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
 
     if (warp == kCopyA || warp == kCopyB) {
         // one warp copies A, one B: an issue of copies takes a good hundred cycles, and a slab's products 512
-        if (lane == 0) {
+        if (elect_one()) {
             const bool is_a = warp == kCopyA;
             int s = 0;
             uint32_t use = 0, issued = 0, last = 0;
@@ -389,9 +390,9 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
                     const uint32_t st = smem_u32(ring + static_cast<size_t>(s) * SB), bar = peer_addr(smem_u32(&full_bar[s]), 0);
                     if (is_a) {
                         if (rank == 0) mbar_expect_tx(smem_u32(&full_bar[s]), static_cast<uint32_t>(16384 + mine * 128) * CG);
-                        load_a<CG, MNA>(a, k, m0, tl.node, st, bar);
+                        load_a<CG, MNA, PROMOTE>(a, k, m0, tl.node, st, bar);
                     } else {
-                        load_b<CG, MNB>(a, k, n0, mine / 64, tl.node, st, bar);
+                        load_b<CG, MNB, PROMOTE>(a, k, n0, mine / 64, tl.node, st, bar);
                     }
                     issued |= 1u << s;
                     last = (last & ~(1u << s)) | (use << s);
@@ -405,7 +406,7 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
         }
         __syncwarp();
     } else if (warp == kIssuer) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0 && elect_one()) {
             int s = 0, b = 0;
             uint32_t use = 0, tuse[2] = {0, 0};
             bool ok = true;
@@ -563,7 +564,7 @@ __global__ void __launch_bounds__(threads_of(8), 1) tc_split_kernel(const __grid
 #pragma unroll
     for (int e = 0; e < kSplitN / 2; ++e) sum[e] = 0.f;
     if (warp == kCopyA || warp == kCopyB) {
-        if (lane == 0) {
+        if (elect_one()) {
             uint32_t issued = 0, last = 0;
             int s = 0;
             uint32_t use = 0;
@@ -573,9 +574,9 @@ __global__ void __launch_bounds__(threads_of(8), 1) tc_split_kernel(const __grid
                 const uint32_t bar = smem_u32(&full_bar[s]), st = smem_u32(ring + static_cast<size_t>(s) * SB);
                 if (warp == kCopyA) {
                     mbar_expect_tx(bar, SB);
-                    load_a<1, MNA>(a, k, tl.m * 128, tl.node, st, bar);
+                    load_a<1, MNA, true>(a, k, tl.m * 128, tl.node, st, bar);
                 } else {
-                    load_b<1, MNB>(a, k, tl.n0, 1, tl.node, st, bar);
+                    load_b<1, MNB, true>(a, k, tl.n0, 1, tl.node, st, bar);
                 }
                 issued |= 1u << s;
                 last = (last & ~(1u << s)) | (use << s);
@@ -588,7 +589,7 @@ __global__ void __launch_bounds__(threads_of(8), 1) tc_split_kernel(const __grid
         }
         __syncwarp();
     } else if (warp == kIssuer) {
-        if (lane == 0) {
+        if (elect_one()) {
             int s = 0, b = 0;
             uint32_t use = 0, tuse[2] = {0, 0};
             bool ok = true;
