@@ -239,6 +239,135 @@ __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant
     cluster_sync();                                   // the peers are done with this CTA's shared memory
 }
 
+// Few rows against a matrix along the contraction (one token's forward product): the matrix is read once, in 16-byte
+// loads, and the rows come from the L1 for every four of its rows.  A warp takes four results of each row, lanes along
+// the contraction, its next loads in flight under the present ones' products (fp32, rounded); `ways` warps of a CTA
+// share them where they would leave SMs without warps.  Lanes' sums are exchanged by halves and added up in a fixed
+// order.  More than eight rows: CTAs for each eight.  Bound by HBM to four rows, by the products beyond.
+// One row of 2048 x 2048 bf16 8.9 us with its launch (128 x 64 tensor-core tiles: 23), of 11008 x 4096 23 us (72), of
+// 4096 x 11008 25 us (54); eight rows of the three 11, 40, 40 us (25, 64, 46).
+constexpr int kRowsCols = 4, kRowsWarps = 8;
+__device__ __forceinline__ void widen(const uint4& u, float (&f)[8], const __nv_bfloat16*) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) { f[2 * q] = __uint_as_float(w[q] << 16); f[2 * q + 1] = __uint_as_float(w[q] & 0xffff0000u); }
+}
+__device__ __forceinline__ void widen(const uint4& u, float (&f)[4], const float*) {
+    f[0] = __uint_as_float(u.x); f[1] = __uint_as_float(u.y); f[2] = __uint_as_float(u.z); f[3] = __uint_as_float(u.w);
+}
+__device__ __forceinline__ uint4 load_once(const uint4* p) {
+    uint4 u;
+    asm("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
+    return u;
+}
+template <class T, int R>
+__global__ void __launch_bounds__(kRowsWarps * 32, 2) rows_kernel(const __grid_constant__ Product p, int ways) {
+    chain_begin();
+    constexpr int E = 16 / static_cast<int>(sizeof(T)), C = kRowsCols, U = R <= 2 ? 2 : 1, n = R * C;
+    __shared__ float part[kRowsWarps][n];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, groups = kRowsWarps / ways, way = warp % ways;
+    const int64_t j0 = (static_cast<int64_t>(blockIdx.x) * groups + warp / ways) * C;
+    const int64_t i0 = static_cast<int64_t>(blockIdx.y) * R;
+    const T* A = static_cast<const T*>(p.A);
+    const T* B = static_cast<const T*>(p.B);
+    const uint4 *a[R], *b[C];                         // rows past the ends: the last one once more
+#pragma unroll
+    for (int r = 0; r < R; ++r) a[r] = reinterpret_cast<const uint4*>(A + min(i0 + r, p.M - 1) * p.sAi);
+#pragma unroll
+    for (int c = 0; c < C; ++c) b[c] = reinterpret_cast<const uint4*>(B + min(j0 + c, p.N - 1) * p.sBj);
+    float sum[n];
+#pragma unroll
+    for (int q = 0; q < n; ++q) sum[q] = 0.f;
+    const int64_t nv = p.K / E;
+    const int step = 32 * ways;
+    constexpr bool EARLY = R < 8;       // eight rows' vectors would not fit the registers
+    uint4 next[U][C];
+    auto ask = [&](int64_t v) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int c = 0; c < C; ++c) next[u][c] = v + u * step < nv ? load_once(b[c] + v + u * step) : uint4{0, 0, 0, 0};
+    };
+    int64_t v = way * 32 + lane;
+    ask(v);
+    for (; v < nv; v += U * step) {
+        uint4 now[U][C], row[U][EARLY ? R : 1];
+        auto row_at = [&](int u, int r) { return v + u * step < nv ? __ldg(a[r] + v + u * step) : uint4{0, 0, 0, 0}; };
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) now[u][c] = next[u][c];
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (EARLY) row[u][r] = row_at(u, r);
+        }
+        ask(v + U * step);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float w[C][E];
+#pragma unroll
+            for (int c = 0; c < C; ++c) widen(now[u][c], w[c], B);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                float x[E];
+                widen(EARLY ? row[u][r] : row_at(u, r), x, A);
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) sum[r * C + c] = fmaf(x[e], w[c][e], sum[r * C + c]);
+            }
+        }
+    }
+    // the elements past the last whole vector: a lane each
+    if (const int64_t k = nv * E + lane; way == 0 && k < p.K) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                sum[r * C + c] = fmaf(to_f(reinterpret_cast<const T*>(a[r])[k]), to_f(reinterpret_cast<const T*>(b[c])[k]), sum[r * C + c]);
+    }
+    // lanes 32 q / n .. hold the total of sum q
+    int width = n;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+        const bool upper = lane & off;
+        if (width > 1) {
+            width >>= 1;
+#pragma unroll
+            for (int q = 0; q < n / 2; ++q)
+                if (q < width) {
+                    const float keep = upper ? sum[q + width] : sum[q], give = upper ? sum[q] : sum[q + width];
+                    sum[q] = keep + __shfl_xor_sync(0xffffffffu, give, off);
+                }
+        } else {
+            sum[0] += __shfl_xor_sync(0xffffffffu, sum[0], off);
+        }
+    }
+    if (lane % (32 / n) == 0) part[warp][lane / (32 / n)] = sum[0];
+    __syncthreads();
+    for (int e = threadIdx.x; e < groups * n; e += kRowsWarps * 32) {
+        const int g = e / n, q = e % n;
+        float v = 0.f;
+        for (int w = 0; w < ways; ++w) v += part[g * ways + w][q];
+        finish(p, 0, i0 + q / C, (static_cast<int64_t>(blockIdx.x) * groups + g) * C + q % C, v);
+    }
+}
+template <class T, int R>
+cudaError_t launch_rows(const Product& p, cudaStream_t st) {
+    // ways to share the contraction: up to 32 warps an SM, each with two loads of a row at least
+    constexpr int C = kRowsCols, E = 16 / static_cast<int>(sizeof(T));
+    int ways = 1;
+    while (ways < kRowsWarps && p.N / C * ways < 152 * 32 && p.K / E >= 128 * ways) ways *= 2;
+    const int64_t per = kRowsWarps / ways * C, blocks = (p.N + per - 1) / per;
+    if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
+    return launch_chain(rows_kernel<T, R>, dim3(static_cast<unsigned>(blocks), static_cast<unsigned>((p.M + R - 1) / R)),
+                        dim3(kRowsWarps * 32), 0, st, p, ways);
+}
+template <class T>
+cudaError_t few_rows(const Product& p, cudaStream_t st) {
+    return p.M == 1 ? launch_rows<T, 1>(p, st) : p.M == 2 ? launch_rows<T, 2>(p, st) : p.M <= 4 ? launch_rows<T, 4>(p, st) : launch_rows<T, 8>(p, st);
+}
+
 // Column sums: 64 columns a CTA, eight neighbouring ones (16 bytes of bf16) a thread and 32 rows of threads; a
 // cluster of up to eight CTAs shares the rows where the columns leave SMs idle.  Added in a fixed order: down a
 // thread's rows, up the rows of threads, over the cluster's CTAs.  Bound by HBM.
@@ -314,6 +443,13 @@ bool wide_ok(const void* base, int64_t row_stride, int64_t node_stride, int64_t 
 
 cudaError_t product(const Product& p, void* workspace, int64_t workspace_bytes, cudaStream_t st) {
     if (p.M == 0 || p.N == 0) return cudaSuccess;
+    // Few rows: the tensor cores' tiles cost the same from one row to 128 (bf16 4096 x 11008: 46 us, few_rows' 25 for one row,
+    // 40 for eight); fp32 ones go through any_product below 128 rows (11008 x 4096: 255 us, few_rows' 37 for one row,
+    // 132 for 24).
+    const int64_t es = p.dtype == GLR_BF16 ? 2 : 4;
+    if (p.mode == kForward && p.M <= (p.dtype == GLR_BF16 ? 8 : 24) && p.K > 0 && p.sAp == 1 && p.sBp == 1 && wide_ok(p.A, p.M == 1 ? 0 : p.sAi, 0, es) &&
+        wide_ok(p.B, p.N == 1 ? 0 : p.sBj, 0, es))
+        return p.dtype == GLR_BF16 ? few_rows<__nv_bfloat16>(p, st) : few_rows<float>(p, st);
     const TcPlan plan = tc_plan(p);
     const bool fits = plan.bytes() == 0 || (workspace && workspace_bytes >= plan.bytes());
     return plan.ok && fits ? tc_product(p, plan, workspace, st) : any_product(p, st);

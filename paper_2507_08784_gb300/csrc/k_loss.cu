@@ -385,7 +385,7 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
                              "r"(bytes), "r"(bar) : "memory");
         };
         int filled = -1;                              // the last row that this warp filled a slot with
-        if (sv == 0 && lane == 0)
+        if (sv == 0 && tc::elect_one())
             for (int q = 0; q < S; ++q)
                 if (first + q * step < a.rows) { fill(first + q * step, q, row_s[q].span, row_s[q].live); filled = q; }
         // the element of the ends that this lane owns, or -1: the head with the first CTA, the tail with the last
@@ -616,7 +616,7 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    // the workers' writes and these, before the copy reads them
                 __syncwarp();
-                if (lane == 0) {
+                if (tc::elect_one()) {
                     if (now.span.nv > 0 && now.same)
                         asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
                                      ::"l"(body), "r"(smem_u32(slot)), "r"(static_cast<uint32_t>(now.span.nv) * 16u) : "memory");
@@ -626,7 +626,7 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
             __syncwarp();
             // ---- 5, and the slot's next row once it has been read
             if (more) put(row + step2, row_s[(it + 2) & 3], asked);
-            if (lane == 0) {
+            if (tc::elect_one()) {
                 if (row_f < a.rows) {
                     if (grad) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                     fill(row_f, it + S, span_of(logits(row_f), V, rank, a.cluster_shift), is_live<K>(a, side_f));
@@ -636,7 +636,7 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
             }
             __syncwarp();
         }
-        if (lane == 0) {
+        if (tc::elect_one()) {
             if (grad) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
             if (*abort)                               // let the copies that this warp issued land
                 for (int i = max(filled - 3, 0); i <= filled; ++i)

@@ -335,3 +335,27 @@ def test_infinities_survive_the_layout():
     small = W[:, 3].abs() < 2
     want = 1.5e38 * W[:, 3].double()
     assert ((Z[200].double() - want).abs()[small] <= 2.0 ** -19 * want.abs()[small]).all()
+
+
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 7, 8, 9])
+@pytest.mark.parametrize("n,k", [(1, 8), (2, 3), (5, 1032), (63, 515), (64, 2048), (1001, 4100), (6000, 8193)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_few_rows(rows, n, k, dt):
+    """Rows on 16 bytes of any length, whose last vector is whole or not."""
+    import paper_2507_08784_gb300 as glr
+    dt = DT[dt]
+    gen = torch.Generator().manual_seed(rows + 7 * n + 13 * k)
+    pad = -k % 8 + 8
+    X, W = _mat(rows, k, dt, gen, pad), _mat(n, k, dt, gen, pad, scale=k ** -0.5)
+    b = torch.randn(n, generator=gen).to(dt).cuda()
+    R = _mat(rows, n, dt, gen, 1, 1)
+    Y, ybuf = _out(rows, n, dt, 3, 1)
+    P, pbuf = _out(rows, n, dt, 5, 2)
+    glr.glr_linear(X, W, Y, bias=b, act="silu", residual=R, preact=P)
+    Xc, Wc, Rc = X.cpu(), W.cpu(), R.cpu()
+    Z, want = ref.linear(Xc, Wc, b.cpu(), "silu", Rc)
+    tol = 1.2 * _sum_tol(Xc.double(), Wc.double(), k, dt) + 2.0 ** -21 * (Z.abs() + 1)
+    _check(Y, want, tol + 2.0 ** -22 * Rc.double().abs(), dt)
+    _check(P, Z, tol, dt)
+    assert _untouched(ybuf, Y) and _untouched(pbuf, P)
+    glr.glr_operator_status()
