@@ -43,8 +43,14 @@ def _check(rc: int, handle=None, group=()):
         raise GlrError(rc, msg.decode() if msg else "")
 
 
+# the current stream's address without a Stream object around it (0.4 us instead of 3, a quarter of a small call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream_ptr(stream) -> int:
     if stream is None:
+        if _raw_stream is not None:
+            return int(_raw_stream(torch.cuda.current_device()))
         stream = torch.cuda.current_stream()
     return int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
 
