@@ -135,8 +135,6 @@ __device__ __forceinline__ float shrink(float a, float m, float c) {
 }
 // Maximum, and sums of exp at two temperatures (s1: temperature 1, for a hard term beside tau != 1).
 struct Stat { float m, s, s1; };
-// Teacher: maximum, sums of e = exp((a - m) / tau) and of e (a - m).
-struct Top { float m, s, a; };
 __device__ __forceinline__ float warp_max(float x) {
     float r;
     asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
@@ -149,7 +147,7 @@ __device__ __forceinline__ float warp_sum(float x) {
 }
 // The merge of a warp's lanes, in a fixed order, to all of them: one maximum, every lane's sums taken to it,
 // and their sum.  A NaN does not show in a maximum; it stays in the sums.
-template <bool TWO>
+template <int TWO>
 __device__ __forceinline__ Stat warp_merge(Stat x, float c) {
     Stat r{};
     r.m = warp_max(x.m);
@@ -157,15 +155,6 @@ __device__ __forceinline__ Stat warp_merge(Stat x, float c) {
     r.s1 = TWO ? warp_sum(x.s1 * shrink(x.m, r.m, kLog2e)) : 0.f;
     return r;
 }
-__device__ __forceinline__ Top warp_merge(Top x, float c) {
-    Top r;
-    r.m = warp_max(x.m);
-    const float f = shrink(x.m, r.m, c);
-    r.s = warp_sum(x.s * f);
-    r.a = warp_sum(x.s == 0.f ? 0.f : (x.a + x.s * (x.m - r.m)) * f);
-    return r;
-}
-
 constexpr int kWorkers = 14;                // warps on a row at most; two more are service warps
 constexpr int kMaxSlots = 3;
 constexpr int kMaxCluster = 8;
@@ -269,7 +258,7 @@ struct Pub { float zt; int soft; };
 // the token (distillation: and what the teacher's entries take).
 struct Coef { float dense, dense1, at_tok, loss, lp; };
 
-template <int K, bool TWO>
+template <int K, int TWO>
 __device__ __forceinline__ Coef coef_of(const RowArgs& a, const Row& r, const Stat& st, const Pub& pub, bool counts) {
     Coef k{};
     if (K == kDistill) {
@@ -304,7 +293,9 @@ constexpr int64_t kRingMax = 196 * 1024;                     // three slots of 6
 
 // HELD: a slot has at most kHeld vectors a worker thread, and the exponentials of the statistics stay in
 // registers for the gradient; else (rows of more than eight such slots) they are formed again.  TWO: a hard
-// term beside tau != 1, so that the sums are kept at two temperatures.
+// term beside tau != 1, so that the sums are kept at two temperatures: kBoth takes two exponentials an element, and at
+// tau = 2 kSquares has the second as the square of the first (4096 rows
+// of 32768 bf16, 64 entries, a hard term: tau = 2 126 -> 109 us, tau = 3 126, tau = 1 103).
 //
 // A worker's row is: wait for the slot, sums, one barrier, the merge of all warps' sums (and of the cluster's
 // CTAs), the gradient into the slot.  What each of up to fourteen warps would do for itself is paid that many
@@ -318,7 +309,8 @@ constexpr int64_t kRingMax = 196 * 1024;                     // three slots of 6
 //     its slot with row i + S (S slots)
 //   5 puts down what was asked for, with the teacher's softmax
 // Their code is run once a row by one warp, so that it is bound by instruction fetch: its loops are kept rolled.
-template <int K, class T, bool HELD, bool TWO>
+constexpr int kBoth = 1, kSquares = 2;
+template <int K, class T, bool HELD, int TWO>
 __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_constant__ RowArgs a) {
     chain_begin();
     constexpr int E = Vec<T>::kElems, P = E / 2;
@@ -375,7 +367,7 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
     uint32_t use = 0, xuse = 0;
     if (warp >= nw) {
         const int sv = warp - nw;                     // rows sv, sv + 2, ..: their parity
-        auto fill = [&](int64_t row, int i, const Span& sp, bool live) {      // lane 0
+        auto fill = [&](int64_t row, int i, const Span& sp, bool live) {      // the elected lane
             const int q = i % S;
             const uint32_t bytes = live ? static_cast<uint32_t>(sp.nv) * 16u : 0u, bar = smem_u32(&full_bar[q]);
             mbar_expect_tx(bar, bytes);
@@ -484,7 +476,7 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
             Asked asked;
             ask(more ? row + step2 : row, row_s[(more ? it + 2 : it) & 3], asked);
             Side side{}, side_f{};
-            if (lane == 0) {
+            if (tc::elect_one()) {                    // (the lane that uses them: one mask's elections agree)
                 side = side_at<K>(a, more4 ? row + 4 * step : row);
                 side_f = side_at<K>(a, row_f < a.rows ? row_f : row);
             }
@@ -672,7 +664,7 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
                     for (int i = 0; i < P; ++i) {
                         const uint64_t d = add2(x[i], nr), e = exp2_2(mul2(d, c2));
                         s2[i & 1] = add2(s2[i & 1], e);
-                        if (TWO) t2[i & 1] = add2(t2[i & 1], exp2_2(mul2(d, l2)));
+                        if (TWO) t2[i & 1] = TWO == kSquares ? fma2(e, e, t2[i & 1]) : add2(t2[i & 1], exp2_2(mul2(d, l2)));
                         if (kKeep > 1) kept[q][i] = e;
                     }
                 }
@@ -691,9 +683,9 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
                     Vec<T>::get(slot[v], x);
 #pragma unroll
                     for (int i = 0; i < P; ++i) {
-                        const uint64_t d = add2(x[i], nr);
-                        s2 = add2(s2, exp2_2(mul2(d, c2)));
-                        if (TWO) t2 = add2(t2, exp2_2(mul2(d, l2)));
+                        const uint64_t d = add2(x[i], nr), e = exp2_2(mul2(d, c2));
+                        s2 = add2(s2, e);
+                        if (TWO) t2 = TWO == kSquares ? fma2(e, e, t2) : add2(t2, exp2_2(mul2(d, l2)));
                     }
                 }
                 float x, y;
@@ -738,16 +730,19 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
                 if (counts && HELD) {
                     const float f = k.dense * shrink(m_own, st.m, c);
                     const uint64_t ff = pack2(f, f);
+                    const float f1 = TWO == kSquares ? k.dense1 * shrink(m_own, st.m, kLog2e) : 0.f;
+                    const uint64_t ff1 = pack2(f1, f1);
 #pragma unroll
                     for (int j = 0; j < kKeep; ++j) {
                         const int v = tid + j * nt;
                         if (v < nv) {
                             uint64_t x[P];
-                            if (TWO) Vec<T>::get(slot[v], x);
+                            if (TWO == kBoth) Vec<T>::get(slot[v], x);
 #pragma unroll
                             for (int i = 0; i < P; ++i) {
-                                const uint64_t g = mul2(ff, kept[j][i]);
-                                x[i] = TWO ? fma2(dd1, exp2_2(mul2(add2(x[i], nm), l2)), g) : g;
+                                const uint64_t e = kept[j][i], g = mul2(ff, e);
+                                x[i] = TWO == kBoth ? fma2(dd1, exp2_2(mul2(add2(x[i], nm), l2)), g)
+                                     : TWO == kSquares ? mul2(fma2(ff1, e, ff), e) : g;
                             }
                             put(v, Vec<T>::put(x));
                         }
@@ -759,9 +754,8 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
                         Vec<T>::get(slot[v], x);
 #pragma unroll
                         for (int i = 0; i < P; ++i) {
-                            const uint64_t d = add2(x[i], nm);
-                            x[i] = mul2(dd, exp2_2(mul2(d, c2)));
-                            if (TWO) x[i] = fma2(dd1, exp2_2(mul2(d, l2)), x[i]);
+                            const uint64_t d = add2(x[i], nm), e = exp2_2(mul2(d, c2));
+                            x[i] = TWO == kBoth ? fma2(dd1, exp2_2(mul2(d, l2)), mul2(dd, e)) : TWO == kSquares ? mul2(fma2(dd1, e, dd), e) : mul2(dd, e);
                         }
                         put(v, Vec<T>::put(x));
                     }
@@ -958,12 +952,13 @@ cudaError_t rows_launch(RowArgs a, int dtype, cudaStream_t st) {
     const size_t smem = static_cast<size_t>(a.slots) * a.slot_bytes;
     const bool held = a.slot_bytes <= kSlotMax;
     const int workers = held ? static_cast<int>((a.slot_bytes / 16 + 32 * kHeld - 1) / (32 * kHeld)) : kWorkers;
-    const bool two = K == kDistill && a.labels.p && a.hard != 0.f && a.inv_tau != 1.f;
+    const int two = K != kDistill || !a.labels.p || a.hard == 0.f || a.inv_tau == 1.f ? 0 : a.inv_tau == 0.5f ? kSquares : kBoth;
     auto pick = [&](auto t) {
         using T = decltype(t);
         constexpr bool D = K == kDistill;
-        return held ? (two ? rows_kernel<K, T, true, D> : rows_kernel<K, T, true, false>)
-                    : (two ? rows_kernel<K, T, false, D> : rows_kernel<K, T, false, false>);
+        constexpr int B = D ? kBoth : 0, Q = D ? kSquares : 0;
+        return held ? (two == kBoth ? rows_kernel<K, T, true, B> : two ? rows_kernel<K, T, true, Q> : rows_kernel<K, T, true, 0>)
+                    : (two == kBoth ? rows_kernel<K, T, false, B> : two ? rows_kernel<K, T, false, Q> : rows_kernel<K, T, false, 0>);
     };
     auto kernel = dtype == GLR_BF16 ? pick(__nv_bfloat16()) : pick(float());
     if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kRingMax))) != cudaSuccess) return e;
