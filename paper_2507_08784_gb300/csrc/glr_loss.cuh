@@ -38,7 +38,7 @@ struct RowArgs {
     // log-probability pass: the row's log sum exp (+infinity: the row does not count) and a zero
     float* lse; float* coef;
     int* err;
-    int cluster_shift, slots; uint32_t slot_bytes;    // set by the launcher
+    int cluster_shift, slots, lists; uint32_t slot_bytes;    // set by the launcher
 };
 
 struct PairArgs {

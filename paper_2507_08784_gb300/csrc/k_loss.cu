@@ -14,6 +14,7 @@
 #include <math_constants.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "glr_loss.cuh"
 #include "glr_ptx.cuh"
@@ -155,7 +156,7 @@ __device__ __forceinline__ Stat warp_merge(Stat x, float c) {
     r.s1 = TWO ? warp_sum(x.s1 * shrink(x.m, r.m, kLog2e)) : 0.f;
     return r;
 }
-constexpr int kWorkers = 14;                // warps on a row at most; two more are service warps
+constexpr int kWorkers = 14;                // warps on a row at most; two more are service warps, one of which beside a teacher's
 constexpr int kMaxSlots = 3;
 constexpr int kMaxCluster = 8;
 constexpr int kHeld = 10;                   // 16-byte vectors of a slot whose exponentials a thread keeps in registers
@@ -288,8 +289,15 @@ __device__ __forceinline__ Coef coef_of(const RowArgs& a, const Row& r, const St
     return k;
 }
 
-constexpr int64_t kSlotMax = kWorkers * 32 * kHeld * 16;     // of a row a CTA: 70 KiB
+constexpr int64_t slot_max(int workers) { return int64_t(workers) * 32 * kHeld * 16; }   // of a row a CTA: 70 KiB
 constexpr int64_t kRingMax = 196 * 1024;                     // three slots of 64 KiB and some bytes
+constexpr int64_t kDynMax = 222 * 1024;                      // ... and a teacher's lists
+constexpr int kFewEntries = 64;
+constexpr int kMaxLists = 4;
+// A list: ids, q and logits of a row's entries, the label last, and whether the teacher has any and sum q log q.
+__host__ __device__ constexpr int list_words(int64_t topk) { return (3 * (static_cast<int>(topk) + 1) + 2 + 3) & ~3; }
+// FEW (at most 64 entries): the service warps see to the teacher's entries; else a warp of its own does.
+constexpr int most_workers(bool few) { return few ? kWorkers : kWorkers - 1; }
 
 // HELD: a slot has at most kHeld vectors a worker thread, and the exponentials of the statistics stay in
 // registers for the gradient; else (rows of more than eight such slots) they are formed again.  TWO: a hard
@@ -309,16 +317,20 @@ constexpr int64_t kRingMax = 196 * 1024;                     // three slots of 6
 //     its slot with row i + S (S slots)
 //   5 puts down what was asked for, with the teacher's softmax
 // Their code is run once a row by one warp, so that it is bound by instruction fetch: its loops are kept rolled.
+// With more than 64 entries (FEW false) the latter would not be done in time: a warp of its own sees to them, ahead by
+// up to four rows, and takes a worker's place (8192 rows of 131071 bf16, 128 entries: 917 -> 734 us; 4096 rows of 32768,
+// 128 entries 124 -> 108, 64 entries 96 -> 101 if it did it there too).
 constexpr int kBoth = 1, kSquares = 2;
-template <int K, class T, bool HELD, int TWO>
+template <int K, class T, bool HELD, int TWO, bool FEW>
 __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_constant__ RowArgs a) {
     chain_begin();
     constexpr int E = Vec<T>::kElems, P = E / 2;
     constexpr int kKeep = HELD && K != kLogProb ? kHeld : 1;
     constexpr bool D = K == kDistill;
-    constexpr int kList = D ? GLR_MAX_TOPK + 1 : 1;   // entries subtracted at single ids; the token is the last
+    constexpr bool TEACH = D && !FEW;
+    constexpr int kList = D && FEW ? kFewEntries + 1 : 1;     // entries subtracted at single ids; the token is the last
     extern __shared__ __align__(128) uint8_t slots[];
-    __shared__ __align__(8) uint64_t full_bar[kMaxSlots], x_bar[2], fin_bar[2], dense_bar[2];
+    __shared__ __align__(8) uint64_t full_bar[kMaxSlots], x_bar[2], fin_bar[2], dense_bar[2], list_bar[kMaxLists], read_bar[kMaxLists];
     // by the row's parity, or (row_s) its number modulo four: who writes them again has passed a barrier that
     // all readers have reached
     __shared__ Row row_s[4];
@@ -329,7 +341,7 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
     __shared__ int32_t id_s[2][kList], mark_s[2][16];
     __shared__ float q_s[2][kList], z_s[2][kList];
     __shared__ int abort_flag;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, nw = (blockDim.x >> 5) - 2, nt = nw * 32;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, nw = (blockDim.x >> 5) - (TEACH ? 3 : 2), nt = nw * 32;
     const int C = 1 << a.cluster_shift, S = a.slots, V = static_cast<int>(a.vocab);
     uint32_t rank = 0;
     if (C > 1) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -343,6 +355,8 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
             mbar_init(smem_u32(&fin_bar[q]), 1);
             mbar_init(smem_u32(&dense_bar[q]), nw);
         }
+        if (TEACH)
+            for (int q = 0; q < kMaxLists; ++q) { mbar_init(smem_u32(&list_bar[q]), 1); mbar_init(smem_u32(&read_bar[q]), 1); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     const bool grad = K != kLogProb && a.dz != nullptr;
@@ -363,9 +377,110 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
     __syncthreads();
     if (C > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 
+    // row i's list (i mod a.lists; a power of two of them)
+    auto list_of = [&](int i) {
+        return reinterpret_cast<int32_t*>(slots + static_cast<size_t>(S) * a.slot_bytes) + (i & (a.lists - 1)) * list_words(a.topk);
+    };
+    const int n1 = a.topk + 1;
     int s = 0, it = 0;
     uint32_t use = 0, xuse = 0;
-    if (warp >= nw) {
+    if (TEACH && warp == nw + 2) {
+        // The teacher's warp, as far ahead as there are lists: a row's entries are asked for a row earlier, and its
+        // list is given out a row later, when the logits at its first entries have come.
+        constexpr int kAhead = 4;                     // entries a lane asks for at a time
+        Word id[kAhead];
+        float ta[kAhead];
+        T zk[kAhead], zlast[kAhead];
+        Side side{};
+        auto entries = [&](int64_t row, int k0) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (k0 + 32 * u >= a.topk) break;
+                const int k = min(k0 + 32 * u + lane, a.topk - 1);
+                const int64_t at = row * a.ldt + k;
+                id[u] = word_at(a.ids, row * a.ldi + k);
+                ta[u] = a.teacher_bf16 ? __uint_as_float(static_cast<const uint16_t*>(a.teacher)[at]) : static_cast<const float*>(a.teacher)[at];
+            }
+        };
+        if (first < a.rows) {
+            side = side_at<K>(a, first);
+            entries(first, 0);
+        }
+        for (int64_t row = first; first < a.rows && row < a.rows + step; row += step, ++it) {
+            const bool ends_here = row >= a.rows;     // only the last row's list is left
+            int32_t* ids = list_of(it);
+            float *qs = reinterpret_cast<float*>(ids + n1), *zs = qs + n1, *ends = zs + n1;
+            const bool live = is_live<K>(a, side);
+            const int32_t label = live && a.labels.p && a.hard != 0.f ? token_of<K>(a, side) : -1;
+            float m = -CUDART_INF_F;
+            if (!ends_here) {
+                wait(smem_u32(&read_bar[it & (a.lists - 1)]), (static_cast<uint32_t>(it / a.lists) & 1u) ^ 1u, false, abort, a.err);
+                const T* z = logits(row);
+                auto take = [&](int k, int u) {
+                    const int32_t v = live && k < a.topk ? index_of(id[u], a.ids.wide, V) : -1;
+                    const float t = v < 0 ? -CUDART_INF_F : a.teacher_bf16 ? __uint_as_float(__float_as_uint(ta[u]) << 16) : ta[u];
+                    if (k < a.topk) { ids[k] = v; qs[k] = t; }
+                    m = fmaxf(m, t);
+                    return z[max(v, 0)];
+                };
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) {
+                    if (32 * u >= a.topk) break;
+                    zk[u] = take(32 * u + lane, u);
+                }
+#pragma unroll 1
+                for (int k0 = 32 * kAhead; k0 < a.topk; k0 += 32 * kAhead) {
+                    entries(row, k0);
+                    T zr[kAhead];
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u) {
+                        if (k0 + 32 * u >= a.topk) break;
+                        zr[u] = take(k0 + 32 * u + lane, u);
+                    }
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u)
+                        if (k0 + 32 * u + lane < a.topk) zs[k0 + 32 * u + lane] = load(&zr[u]);
+                }
+                const int64_t after = min(row + step, a.rows - 1);
+                side = side_at<K>(a, after);
+                entries(after, 0);
+            }
+            if (it > 0) {
+                float* zs_last = reinterpret_cast<float*>(list_of(it - 1) + 2 * n1);
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u)
+                    if (32 * u + lane < a.topk) zs_last[32 * u + lane] = load(&zlast[u]);
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(smem_u32(&list_bar[(it - 1) & (a.lists - 1)]));
+            }
+            if (ends_here) break;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) zlast[u] = zk[u];
+            m = warp_max(m);
+            float sum = 0.f, tsum = 0.f;
+#pragma unroll 1
+            for (int k = lane; k < a.topk; k += 32) {
+                const float t = qs[k];
+                float w = 0.f;
+                if (t != -CUDART_INF_F) {             // an entry that the teacher rules out leaves the sums as they are
+                    w = exp2_fast((t - m) * c);
+                    sum += w;
+                    tsum += w * (t - m);
+                }
+                qs[k] = w;
+            }
+            sum = warp_sum(sum);
+            tsum = warp_sum(tsum);
+            const float inv = sum != 0.f ? 1.f / sum : 0.f;
+#pragma unroll 1
+            for (int k = lane; k < a.topk; k += 32) qs[k] *= inv;
+            if (lane == 0) {
+                ids[a.topk] = label;
+                ends[0] = sum != 0.f ? 1.f : 0.f;
+                ends[1] = tsum * inv * a.inv_tau - log_fast(sum);
+            }
+        }
+    } else if (warp >= nw) {
         const int sv = warp - nw;                     // rows sv, sv + 2, ..: their parity
         auto fill = [&](int64_t row, int i, const Span& sp, bool live) {      // the elected lane
             const int q = i % S;
@@ -398,7 +513,7 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
             x.e = end_of(r.span);
             x.end = z[max(x.e, 0)];
             x.zt = z[max(r.tok, 0)];
-            if (D && a.topk > 0) {
+            if (D && FEW && a.topk > 0) {
                 entry(row, lane, x.id[0], x.a[0]);
                 entry(row, lane + 32, x.id[1], x.a[1]);
             }
@@ -410,7 +525,7 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
         auto put = [&](int64_t row, const Row& r, const Asked& x) {
             if (lane < 16) end_s[sv][lane] = x.e >= 0 ? load(&x.end) : -CUDART_INF_F;
             if (lane == 0) zt_s[sv] = load(&x.zt);
-            if (!D) return;
+            if (!D || TEACH) return;
             if (lane == 0) id_s[sv][a.topk] = r.live && a.hard != 0.f ? r.tok : -1;
             float m = -CUDART_INF_F;
             auto take = [&](int k, const Word& word, float bits) {
@@ -422,13 +537,6 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
             };
             if (lane < a.topk) take(lane, x.id[0], x.a[0]);
             if (lane + 32 < a.topk) take(lane + 32, x.id[1], x.a[1]);
-#pragma unroll 1
-            for (int k = lane + 64; k < a.topk; k += 32) {
-                Word id;
-                float t;
-                entry(row, k, id, t);
-                take(k, id, t);
-            }
             const T* z = logits(row);
             const T z0 = z[lane < a.topk ? max(id_s[sv][lane], 0) : 0], z1 = z[lane + 32 < a.topk ? max(id_s[sv][lane + 32], 0) : 0];
             m = warp_max(m);
@@ -453,8 +561,6 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
             for (int k = lane; k < a.topk; k += 32) q_s[sv][k] *= inv;
             if (lane < a.topk) z_s[sv][lane] = load(&z0);
             if (lane + 32 < a.topk) z_s[sv][lane + 32] = load(&z1);
-#pragma unroll 4
-            for (int k = lane + 64; k < a.topk; k += 32) z_s[sv][k] = load(z + max(id_s[sv][k], 0));
         };
         const int64_t step2 = 2 * step;
         if (first + sv * step < a.rows) {
@@ -469,7 +575,13 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
             const int top = a.topk;
             const uint32_t ph = static_cast<uint32_t>(it >> 1) & 1u;
             bool counts = now.live;
-            const float tq = teach;
+            const int32_t* ids = TEACH ? list_of(it) : id_s[sv];
+            const float *qs = TEACH ? reinterpret_cast<const float*>(ids + n1) : q_s[sv], *zs = TEACH ? qs + n1 : z_s[sv];
+            // (a row is only overwritten by its gradient once all CTAs of a cluster have sent its sums, which they do
+            // after the barrier below: the teacher's warp has read the row's logits by then)
+            if (TEACH) wait(smem_u32(&list_bar[it & (a.lists - 1)]), static_cast<uint32_t>(it / a.lists) & 1u, false, abort, a.err);
+            const float tq = TEACH ? zs[n1 + 1] : teach;
+            const bool soft_now = TEACH ? zs[n1] != 0.f : soft_next;
             // ---- 1
             const bool more = row + step2 < a.rows, more4 = row + 4 * step < a.rows;
             const int64_t row_f = row + S * step;
@@ -493,7 +605,7 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
                 }
                 st = warp_merge<TWO>(st, c);
             }
-            const Pub pub{counts ? zt_s[sv] : 0.f, D && counts && soft_next};
+            const Pub pub{counts ? zt_s[sv] : 0.f, D && counts && soft_now};
             if (lane == 0) {
                 stat_s[sv][nw] = st;
                 pub_s[sv] = pub;
@@ -513,8 +625,8 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
                 if (soft) {
 #pragma unroll 1
                     for (int j = lane; j < top; j += 32) {
-                        const float w = q_s[sv][j];
-                        if (w != 0.f) zq += w * (z_s[sv][j] - st.m);
+                        const float w = qs[j];
+                        if (w != 0.f) zq += w * (zs[j] - st.m);
                     }
                     zq = warp_sum(zq);
                 }
@@ -564,10 +676,9 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
                     using M = typename Vec<T>::Mark;
                     constexpr int kFlag = 1 << 14;
                     const float f = now.w * a.soft * a.inv_tau;
-                    const int32_t* ids = id_s[sv];
                     M* marks = reinterpret_cast<M*>(slot);
-                    auto value = [&](int j) { return j < top ? (pub.soft ? f * q_s[sv][j] : 0.f) : k.at_tok; };
-                    const int n = id_s[sv][top] >= 0 ? top + 1 : top;
+                    auto value = [&](int j) { return j < top ? (pub.soft ? f * qs[j] : 0.f) : k.at_tok; };
+                    const int n = ids[top] >= 0 ? top + 1 : top;
 #pragma unroll 1
                     for (int j = lane; j < n; j += 32) {
                         const int b = ids[j] >= 0 ? place(ids[j]) : -1;
@@ -603,7 +714,7 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
                                 for (int i = 0; i < n; ++i) g += ids[i] == v ? value(i) : 0.f;
                             }
                         }
-                        store(b >= 0 ? mine + b : gradient(row) + v, at(j < top ? z_s[sv][j] : pub.zt) - g);
+                        store(b >= 0 ? mine + b : gradient(row) + v, at(j < top ? zs[j] : pub.zt) - g);
                     }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    // the workers' writes and these, before the copy reads them
@@ -619,6 +730,7 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
             // ---- 5, and the slot's next row once it has been read
             if (more) put(row + step2, row_s[(it + 2) & 3], asked);
             if (tc::elect_one()) {
+                if (TEACH) tc::mbar_arrive(smem_u32(&read_bar[it & (a.lists - 1)]));
                 if (row_f < a.rows) {
                     if (grad) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                     fill(row_f, it + S, span_of(logits(row_f), V, rank, a.cluster_shift), is_live<K>(a, side_f));
@@ -943,32 +1055,42 @@ cudaError_t rows_launch(RowArgs a, int dtype, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     const int64_t vecs = (row_bytes + 15) / 16;
     int C = 1;
-    while (C < kMaxCluster && (vecs + C - 1) / C * 16 > kSlotMax) C *= 2;
+    const bool few = K != kDistill || a.topk <= kFewEntries;
+    const int most = most_workers(few);
+    while (C < kMaxCluster && (vecs + C - 1) / C * 16 > slot_max(most)) C *= 2;
     // few rows: more CTAs a row, as long as each has 4 KiB of it
     while (C < kMaxCluster && a.rows * C * 2 <= sms && row_bytes / (2 * C) >= 4096) C *= 2;
     a.cluster_shift = C == 1 ? 0 : C == 2 ? 1 : C == 4 ? 2 : 3;
     a.slot_bytes = static_cast<uint32_t>((vecs + C - 1) / C * 16);
-    a.slots = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(3, kRingMax / a.slot_bytes)));
-    const size_t smem = static_cast<size_t>(a.slots) * a.slot_bytes;
-    const bool held = a.slot_bytes <= kSlotMax;
-    const int workers = held ? static_cast<int>((a.slot_bytes / 16 + 32 * kHeld - 1) / (32 * kHeld)) : kWorkers;
+    // the teacher's lists: four, or two beside the longest slots
+    const int64_t list = few ? 0 : 4 * list_words(a.topk);
+    a.lists = kMaxLists;
+    if (a.lists * list + a.slot_bytes > kDynMax) a.lists = 2;
+    a.slots = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(3, std::min(kRingMax, kDynMax - a.lists * list) / a.slot_bytes)));
+    const size_t smem = static_cast<size_t>(a.slots) * a.slot_bytes + a.lists * list;
+    const bool held = a.slot_bytes <= slot_max(most);
+    const int workers = held ? static_cast<int>((a.slot_bytes / 16 + 32 * kHeld - 1) / (32 * kHeld)) : most, extra = few ? 2 : 3;
     const int two = K != kDistill || !a.labels.p || a.hard == 0.f || a.inv_tau == 1.f ? 0 : a.inv_tau == 0.5f ? kSquares : kBoth;
     auto pick = [&](auto t) {
         using T = decltype(t);
         constexpr bool D = K == kDistill;
         constexpr int B = D ? kBoth : 0, Q = D ? kSquares : 0;
-        return held ? (two == kBoth ? rows_kernel<K, T, true, B> : two ? rows_kernel<K, T, true, Q> : rows_kernel<K, T, true, 0>)
-                    : (two == kBoth ? rows_kernel<K, T, false, B> : two ? rows_kernel<K, T, false, Q> : rows_kernel<K, T, false, 0>);
+        auto of = [&](auto f) {
+            constexpr bool F = decltype(f)::value || !D;
+            return held ? (two == kBoth ? rows_kernel<K, T, true, B, F> : two ? rows_kernel<K, T, true, Q, F> : rows_kernel<K, T, true, 0, F>)
+                        : (two == kBoth ? rows_kernel<K, T, false, B, F> : two ? rows_kernel<K, T, false, Q, F> : rows_kernel<K, T, false, 0, F>);
+        };
+        return few ? of(std::true_type()) : of(std::false_type());
     };
     auto kernel = dtype == GLR_BF16 ? pick(__nv_bfloat16()) : pick(float());
-    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kRingMax))) != cudaSuccess) return e;
+    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kDynMax))) != cudaSuccess) return e;
     cudaLaunchAttribute attr[2]{};
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = C; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.blockDim = (workers + 2) * 32; cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cfg.blockDim = (workers + extra) * 32; cfg.dynamicSmemBytes = smem; cfg.stream = st;
     cfg.attrs = attr; cfg.numAttrs = 2;
     // as many groups of CTAs as run at once, each with its share of the rows
     int64_t groups = a.rows;
@@ -976,7 +1098,7 @@ cudaError_t rows_launch(RowArgs a, int dtype, cudaStream_t st) {
         int per = 0;
         cfg.gridDim = C;
         if (C > 1) e = cudaOccupancyMaxActiveClusters(&per, kernel, &cfg);
-        else if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, (workers + 2) * 32, smem)) == cudaSuccess) per *= sms;
+        else if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, (workers + extra) * 32, smem)) == cudaSuccess) per *= sms;
         if (e != cudaSuccess) return e;
         groups = std::min<int64_t>(groups, std::max(per, 1));
     }

@@ -475,3 +475,39 @@ def test_many_rows_a_group(vocab, rows, dt):
         tol = 16 * rel * (g.abs() + lp.exp() + torch.softmax(x, 1) + 1e-6) + (2.0 ** -8 * g.abs() if dt == torch.bfloat16 else 0)
         tol.scatter_add_(1, ids[part], 16 * rel * q[part]).scatter_add_(1, labels[part, None], torch.full((g.shape[0], 1), 16 * rel, device="cuda").double())
         assert ((d[part].double() - g).abs() <= tol).all(), at
+
+
+@pytest.mark.parametrize("vocab,rows,topk,tau", [(70, 5000, 65, 2.0), (2048, 3001, 100, 1.0), (8191, 1500, 128, 3.0), (32768, 700, 129, 2.0),
+                                                 (131071, 200, 257, 1.0), (131072, 300, 128, 2.0), (390001, 60, 1024, 1.5)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("inplace", [False, True])
+def test_many_entries_a_row(vocab, rows, topk, tau, dt, inplace):
+    """More of the teacher's entries than a warp's first loads, ids given twice among them, over many rows a group; the
+    last size leaves room for two rows' entries beside the row itself."""
+    dt = DT[dt]
+    gen = torch.Generator().manual_seed(23)
+    z = _logits(rows, vocab, dt, gen)
+    ids = torch.randint(0, vocab, (rows, topk), generator=gen)
+    ids[::2, 1] = ids[::2, topk - 1]
+    ids, labels = ids.int().cuda(), torch.randint(0, vocab, (rows,), generator=gen).cuda()
+    teacher, weight = torch.randn(rows, topk, generator=gen).cuda(), torch.ones(rows)
+    weight[::5] = 0
+    zc = z.clone()
+    loss, row, d = _run_distill(z, teacher, ids, labels, weight.cuda(), tau, 1.0, 0.5, inplace=inplace)
+    rel, q = _rel(zc[:50].float().cpu()) * 2, torch.softmax(teacher.double() / tau, 1)
+    wants = torch.zeros((), device="cuda", dtype=torch.float64)
+    for at in range(0, rows, 64):
+        part = slice(at, min(rows, at + 64))
+        x, k = zc[part].double(), ids[part].long()
+        lp, lp1 = torch.log_softmax(x / tau, 1), torch.log_softmax(x, 1).gather(1, labels[part, None])[:, 0]
+        live = (weight[part] != 0).cuda()
+        want = torch.where(live, (q[part] * (q[part].log() - lp.gather(1, k))).sum(1) - 0.5 * lp1, 0)
+        wants += want.sum()
+        assert ((row[part].double() - want).abs() <= 8 * rel * (1 + want.abs())).all(), at
+        g = (lp.exp() / tau + 0.5 * torch.softmax(x, 1)).scatter_add_(1, k, -q[part] / tau)
+        g.scatter_add_(1, labels[part, None], torch.full((g.shape[0], 1), -0.5, device="cuda", dtype=torch.float64))
+        g = torch.where(live[:, None], g, 0)
+        tol = 16 * rel * (g.abs() + lp.exp() + torch.softmax(x, 1) + 1e-6) + (2.0 ** -8 * g.abs() if dt == torch.bfloat16 else 0)
+        tol.scatter_add_(1, k, 16 * rel * q[part]).scatter_add_(1, labels[part, None], torch.full((g.shape[0], 1), 16 * rel, device="cuda").double())
+        assert ((d[part].double() - g).abs() <= tol).all(), at
+    assert abs(float(loss) - float(wants)) <= 8 * rel * (rows + abs(float(wants)))
