@@ -529,7 +529,7 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
 // ------------------------------------------------------------------------------------------
 constexpr int kSplitN = 64, kSplitPitch = kSplitN + 4;
 template <int MODE>
-__global__ void __launch_bounds__(threads_of(8), 1) tc_split_kernel(const __grid_constant__ TcArgs a) {
+__global__ void __launch_bounds__(threads_of(8), 2) tc_split_kernel(const __grid_constant__ TcArgs a) {
     chain_begin();
     constexpr bool MNA = mn_major_a(MODE), MNB = mn_major_b(MODE);
     constexpr int kEpiWarps = 8, kCopyA = 8, kCopyB = 9, kIssuer = 10, kThreads = threads_of(8);
