@@ -333,6 +333,17 @@ __device__ __forceinline__ void mma_stage(uint32_t d, uint32_t st, int bn, bool 
                     operand_desc(st + 16384 + (MNB ? 2048 : 32) * kk, MNB, 8192), id, (add || kk) ? 1u : 0u);
 }
 
+// A warp's columns of an accumulator have been read: its barrier, of the pair's first CTA `lead`.
+template <int CG>
+__device__ __forceinline__ void hand_back(uint32_t bar, uint32_t lead) {
+    fence_before();
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) {
+        if (CG == 1) tc::mbar_arrive(bar);
+        else asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(peer_addr(bar, lead)) : "memory");
+    }
+}
+
 // How a mode's operands lie: the forward product's both along the contraction, ...
 constexpr bool mn_major_a(int mode) { return mode == kGradWeight; }
 constexpr bool mn_major_b(int mode) { return mode != kForward; }
@@ -438,14 +449,7 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
         int b = 0;
         const int quad = warp & 3;
         float* block = blocks + warp * 32 * kBlockPitch;
-        auto hand_back = [&]() {
-            fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                const uint32_t bar = smem_u32(&tempty_bar[b]);
-                asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(peer_addr(bar, 0)) : "memory");
-            }
-        };
+        auto hand_back = [&]() { linear::hand_back<CG>(smem_u32(&tempty_bar[b]), 0); };
         for (int t = first; t < a.tiles; t += step) {
             const Tile tl = tile_at<BN>(a, t);
             const int span = tl.bn == BN ? kSpan : kSpan / 2, c0 = (warp >> 2) * span;
@@ -524,16 +528,19 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
 }
 
 // ------------------------------------------------------------------------------------------
-// Few tiles: 128 x 64 of them, a cluster of CTAs each.  CTA q of a cluster takes its q-th of the stages, sums them
-// in chunks, leaves its partial tile in shared memory (where the ring was) and finishes its part of the rows.
+// Few tiles: a cluster each, of CTAs with 128 x 64 of the result (CG = 1, two CTAs an SM) or of pairs with 256 x 256
+// (CG = 2).  The cluster's q-th CTA or pair takes the q-th part of the stages, sums them in chunks, leaves its partial
+// tile in shared memory (where the ring was) and finishes its part of the rows.
 // ------------------------------------------------------------------------------------------
-constexpr int kSplitN = 64, kSplitPitch = kSplitN + 4;
-template <int MODE>
-__global__ void __launch_bounds__(threads_of(8), 2) tc_split_kernel(const __grid_constant__ TcArgs a) {
+constexpr int kSplitN = 64;
+template <int MODE, int CG>
+__global__ void __launch_bounds__(threads_of(epi_warps(CG == 2)), CG == 2 ? 1 : 2) tc_split_kernel(const __grid_constant__ TcArgs a) {
     chain_begin();
     constexpr bool MNA = mn_major_a(MODE), MNB = mn_major_b(MODE);
-    constexpr int kEpiWarps = 8, kCopyA = 8, kCopyB = 9, kIssuer = 10, kThreads = threads_of(8);
-    constexpr uint32_t SB = stage_bytes<kSplitN, 1>(), kCols = 2 * kSplitN;
+    constexpr int BN = CG == 2 ? 256 : kSplitN, kPitch = BN + 4;
+    constexpr int kEpiWarps = epi_warps(CG == 2), kCopyA = kEpiWarps, kCopyB = kEpiWarps + 1, kIssuer = kEpiWarps + 2;
+    constexpr int kThreads = threads_of(kEpiWarps), kSpan = BN / (kEpiWarps / 4);
+    constexpr uint32_t SB = stage_bytes<BN, CG>(), kCols = 2 * BN;
     extern __shared__ uint8_t dyn_smem[];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dyn_smem) + 1023) & ~uintptr_t(1023));
     __shared__ __align__(8) uint64_t full_bar[kMaxStages], empty_bar[kMaxStages], tfull_bar[2], tempty_bar[2];
@@ -541,6 +548,7 @@ __global__ void __launch_bounds__(threads_of(8), 2) tc_split_kernel(const __grid
     __shared__ int abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, S = a.stages;
     const int splits = gridDim.y, split = blockIdx.y;
+    const uint32_t half = CG == 2 ? cluster_rank() & 1 : 0, lead = CG == 2 ? cluster_rank() & ~1u : 0;    // of the pair
     const int k_first = static_cast<int>(static_cast<int64_t>(a.slabs) * split / splits);
     const int k_last = static_cast<int>(static_cast<int64_t>(a.slabs) * (split + 1) / splits);
     volatile int* abort = &abort_flag;
@@ -548,21 +556,28 @@ __global__ void __launch_bounds__(threads_of(8), 2) tc_split_kernel(const __grid
     if (threadIdx.x == 0) {
         abort_flag = 0;
         for (int q = 0; q < S; ++q) { mbar_init(smem_u32(&full_bar[q]), 1); mbar_init(smem_u32(&empty_bar[q]), 1); }
-        for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&tfull_bar[b]), 1); mbar_init(smem_u32(&tempty_bar[b]), kEpiWarps); }
+        for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&tfull_bar[b]), 1); mbar_init(smem_u32(&tempty_bar[b]), kEpiWarps * CG); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kIssuer) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "r"(kCols));
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        if (CG == 1) {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "r"(kCols));
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "r"(kCols));
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+        }
     }
     fence_before();
     __syncthreads();
+    if (CG == 2) cluster_sync();
     fence_after();
     const uint32_t tmem = tmem_base;
-    const Tile tl = tile_at<kSplitN>(a, blockIdx.x);
-    float sum[kSplitN / 2];
+    const Tile tl = tile_at<BN>(a, blockIdx.x / CG);
+    const int m0 = (tl.m * CG + static_cast<int>(half)) * 128;
+    float sum[kSpan];
 #pragma unroll
-    for (int e = 0; e < kSplitN / 2; ++e) sum[e] = 0.f;
+    for (int e = 0; e < kSpan; ++e) sum[e] = 0.f;
     if (warp == kCopyA || warp == kCopyB) {
         if (elect_one()) {
             uint32_t issued = 0, last = 0;
@@ -571,25 +586,27 @@ __global__ void __launch_bounds__(threads_of(8), 2) tc_split_kernel(const __grid
             bool ok = true;
             for (int k = k_first; k < k_last; ++k) {
                 if (!(ok = wait(smem_u32(&empty_bar[s]), use ^ 1u, abort, err))) break;
-                const uint32_t bar = smem_u32(&full_bar[s]), st = smem_u32(ring + static_cast<size_t>(s) * SB);
+                const uint32_t own = smem_u32(&full_bar[s]), bar = CG == 2 ? peer_addr(own, lead) : own;
+                const uint32_t st = smem_u32(ring + static_cast<size_t>(s) * SB);
                 if (warp == kCopyA) {
-                    mbar_expect_tx(bar, SB);
-                    load_a<1, MNA, true>(a, k, tl.m * 128, tl.node, st, bar);
+                    if (half == 0) mbar_expect_tx(own, SB * CG);
+                    load_a<CG, MNA, true>(a, k, m0, tl.node, st, bar);
                 } else {
-                    load_b<1, MNB, true>(a, k, tl.n0, 1, tl.node, st, bar);
+                    load_b<CG, MNB, true>(a, k, tl.n0 + static_cast<int>(half) * (BN / CG), BN / CG / 64, tl.node, st, bar);
                 }
                 issued |= 1u << s;
                 last = (last & ~(1u << s)) | (use << s);
                 if (++s == S) { s = 0; use ^= 1u; }
             }
-            if (!ok)                                 // let the copies already issued land
+            if (!ok && half == 0)                    // let the copies already issued land
                 for (int q = 0; q < S; ++q)
                     if (issued & (1u << q))
                         for (int it = 0; it < 4000000 && !try_wait(smem_u32(&full_bar[q]), (last >> q) & 1u); ++it) __nanosleep(64);
         }
         __syncwarp();
     } else if (warp == kIssuer) {
-        if (elect_one()) {
+        if (half == 0 && elect_one()) {
+            const uint16_t pair = static_cast<uint16_t>(3u << lead);
             int s = 0, b = 0;
             uint32_t use = 0, tuse[2] = {0, 0};
             bool ok = true;
@@ -599,12 +616,12 @@ __global__ void __launch_bounds__(threads_of(8), 2) tc_split_kernel(const __grid
                 for (int k = k0; k < min(k0 + a.chunk, k_last); ++k) {
                     if (!(ok = wait(smem_u32(&full_bar[s]), use, abort, err))) break;
                     fence_after();
-                    mma_stage<1, MNA, MNB>(tmem + static_cast<uint32_t>(b * kSplitN), smem_u32(ring + static_cast<size_t>(s) * SB), kSplitN, k > k0);
-                    commit<1>(smem_u32(&empty_bar[s]));
+                    mma_stage<CG, MNA, MNB>(tmem + static_cast<uint32_t>(b * BN), smem_u32(ring + static_cast<size_t>(s) * SB), BN, k > k0);
+                    commit<CG>(smem_u32(&empty_bar[s]), pair);
                     if (++s == S) { s = 0; use ^= 1u; }
                 }
                 if (!ok) break;
-                commit<1>(smem_u32(&tfull_bar[b]));
+                commit<CG>(smem_u32(&tfull_bar[b]), pair);
                 tuse[b] ^= 1u;
                 b ^= 1;
             }
@@ -617,13 +634,14 @@ __global__ void __launch_bounds__(threads_of(8), 2) tc_split_kernel(const __grid
             const bool ok = wait(smem_u32(&tfull_bar[b]), tuse[b], abort, err);
             if (!__all_sync(0xffffffffu, ok)) break;
             fence_after();
-            float v[32];
-            tmem_load32(tmem + static_cast<uint32_t>(b * kSplitN + (warp >> 2) * 32) + (static_cast<uint32_t>(32 * (warp & 3)) << 16), v);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) sum[e] += v[e];
-            fence_before();
-            __syncwarp();
-            if (lane == 0) tc::mbar_arrive(smem_u32(&tempty_bar[b]));
+            for (int c = 0; c < kSpan; c += 32) {
+                float v[32];
+                tmem_load32(tmem + static_cast<uint32_t>(b * BN + (warp >> 2) * kSpan + c) + (static_cast<uint32_t>(32 * (warp & 3)) << 16), v);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) sum[c + e] += v[e];
+            }
+            hand_back<CG>(smem_u32(&tempty_bar[b]), lead);
             tuse[b] ^= 1u;
             b ^= 1;
         }
@@ -632,22 +650,22 @@ __global__ void __launch_bounds__(threads_of(8), 2) tc_split_kernel(const __grid
     __syncthreads();                                 // every stage has been read: the last products are done
     float* part = reinterpret_cast<float*>(ring);
     if (warp < kEpiWarps) {
-        float* to = part + (32 * (warp & 3) + lane) * kSplitPitch + (warp >> 2) * 32;
+        float* to = part + (32 * (warp & 3) + lane) * kPitch + (warp >> 2) * kSpan;
 #pragma unroll
-        for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(to + e) = make_float4(sum[e], sum[e + 1], sum[e + 2], sum[e + 3]);
+        for (int e = 0; e < kSpan; e += 4) *reinterpret_cast<float4*>(to + e) = make_float4(sum[e], sum[e + 1], sum[e + 2], sum[e + 3]);
     }
     __syncthreads();
-    if (splits > 1) cluster_sync();
+    if (CG == 2 || splits > 1) cluster_sync();
     const int rows = 128 / splits;                   // this CTA's rows of the tile, eight columns a thread
-    for (int e = threadIdx.x; e < rows * (kSplitN / 8); e += kThreads) {
-        const int r = split * rows + e / (kSplitN / 8), c = e % (kSplitN / 8) * 8;
-        const int64_t i = static_cast<int64_t>(tl.m) * 128 + r, j = static_cast<int64_t>(tl.n0) + c;
+    for (int e = threadIdx.x; e < rows * (BN / 8); e += kThreads) {
+        const int r = split * rows + e / (BN / 8), c = e % (BN / 8) * 8;
+        const int64_t i = static_cast<int64_t>(m0) + r, j = static_cast<int64_t>(tl.n0) + c;
         if (i >= a.p.M || j >= a.p.N) continue;
         float v[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] = 0.f;
         for (int q = 0; q < splits; ++q) {
-            const uint32_t from = peer_addr(smem_u32(part + r * kSplitPitch + c), q);
+            const uint32_t from = peer_addr(smem_u32(part + r * kPitch + c), half + CG * q);
 #pragma unroll
             for (int h = 0; h < 8; h += 4) {
                 float x[4];
@@ -660,11 +678,12 @@ __global__ void __launch_bounds__(threads_of(8), 2) tc_split_kernel(const __grid
         if (a.p.out_dtype == GLR_F32) epilogue8<MODE, GLR_F32>(a, tl.node, i, j, v);
         else epilogue8<MODE, GLR_BF16>(a, tl.node, i, j, v);
     }
-    if (splits > 1) cluster_sync();                  // the peers are done with this CTA's shared memory
+    if (CG == 2 || splits > 1) cluster_sync();       // the peers are done with this CTA's shared memory
     else __syncthreads();
     if (warp == kIssuer) {
         fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols));
+        if (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols));
+        else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols));
     }
 }
 
@@ -742,12 +761,17 @@ cudaError_t launch(Kernel kernel, const TcArgs& a, dim3 grid, dim3 cluster, int 
     return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 template <int MODE>
-cudaError_t launch_mode(TcArgs& a, bool promote, int splits, int sms, cudaStream_t st) {
-    if (splits) {
+cudaError_t launch_mode(TcArgs& a, bool promote, int splits, bool paired, int sms, cudaStream_t st) {
+    if (splits && !paired) {
         // half of an SM's shared memory: two CTAs an SM
         a.stages = 4;
         const size_t smem = a.stages * stage_bytes<kSplitN, 1>() + 1024;
-        return launch(tc_split_kernel<MODE>, a, dim3(static_cast<unsigned>(a.tiles), splits), dim3(1, splits), threads_of(8), smem, st);
+        return launch(tc_split_kernel<MODE, 1>, a, dim3(static_cast<unsigned>(a.tiles), splits), dim3(1, splits), threads_of(epi_warps(false)), smem, st);
+    }
+    if (splits) {
+        a.stages = 6;
+        const size_t smem = a.stages * stage_bytes<256, 2>() + 1024;
+        return launch(tc_split_kernel<MODE, 2>, a, dim3(static_cast<unsigned>(2 * a.tiles), splits), dim3(2, splits), threads_of(epi_warps(true)), smem, st);
     }
     const uint32_t sb = stage_bytes<256, 2>();
     const size_t blocks = epi_warps(promote) * kBlockBytes;
@@ -786,10 +810,11 @@ TcPlan tc_plan(const Product& p) {
     const Storage a = storage(p.sAi, p.sAp, p.M, p.K, p.nodes), b = storage(p.sBj, p.sBp, p.N, p.K, p.nodes);
     if (t.pack_a) t.bytes_a = (t.planes * a.rows * up8(a.cols) * 2 + 255) / 256 * 256;
     if (t.pack_b) t.bytes_b = t.planes * b.rows * up8(b.cols) * 2;
-    // Packing reads both matrices once more and launches two kernels: it pays where the product itself is long and
-    // neither side is thin (measured at both ends: a 64-row product is faster unpacked).
+    // Packing reads the matrices once more and launches a kernel for each: it pays where the product itself is long
+    // (bf16 rows off 16 bytes, 16 x 4096 x 4096: 76 us unpacked, 33 packed; 128 x 1500 x 1500 38 and 19; fp32 96 x 4096 x
+    // 4096 134 and 76; 64 x 1500 x 1500 unpacked 23 in either type, which is what packing it takes by itself).
     const double flops = 2.0 * static_cast<double>(p.M) * static_cast<double>(p.N) * static_cast<double>(p.K) * p.nodes;
-    t.ok = !(t.pack_a || t.pack_b) || (p.M >= 128 && p.N >= 128 && flops >= 5e8);
+    t.ok = !(t.pack_a || t.pack_b) || flops >= 5e8;
     return t;
 }
 
@@ -818,19 +843,28 @@ cudaError_t tc_product(const Product& p, const TcPlan& plan, void* workspace, cu
     const int64_t slabs = (p.K + kSlab - 1) / kSlab * (plan.planes == 3 ? 6 : 1);
     if (slabs > (1 << 30)) return cudaErrorInvalidValue;
     a.slabs = static_cast<int>(slabs);
-    // Pairs' tiles of 256 x 256, or 128 x 64 ones shared by clusters: whichever is done first at 512 cycles a slab of a
-    // wave of pairs and 400 a slab of a small tile on an SM (measured: its 24 KiB from the L2).
     const int64_t big = ((p.M + 255) / 256) * ((p.N + 255) / 256) * p.nodes, pairs = sms / 2;
     const int64_t small = ((p.M + 127) / 128) * ((p.N + kSplitN - 1) / kSplitN) * p.nodes;
     if (std::max(big, small) > (1 << 30)) return cudaErrorInvalidValue;
+    // One of three, by the cycles it takes (measured; a stage is a slab, or one of an fp32 slab's six products).
+    // 256 x 256 tiles, one after the other on every pair: 530 a stage, 650 with promoted sums.  The same tiles, two
+    // pairs sharing a contraction: 670 a stage, and more to begin and end with; 36 such clusters run at once on 152 SMs
+    // (four pairs to a tile: too few clusters at once, never the fastest).  128 x 64 tiles shared by one to eight CTAs: 420 a
+    // stage, 620 with two on an SM.  400 x 4096 x 4096 fp32: 176, 114 and 157 us; 1000 x 11008 x 2048 bf16: 56, 48 and 66; 200 x
+    // 4096 x 4096 bf16: 27, 27 and 23; 24 rows: 27, 25 and 19.
+    const auto waves = [](int64_t n, int64_t at_once) { return (n + at_once - 1) / at_once; };
+    int64_t best = 4000 + waves(big, pairs) * slabs * (promote ? 650 : 530);
     int splits = 0;
-    if (std::max<int64_t>(sms, small) * 400 < (big + pairs - 1) / pairs * sms * 512) {
-        splits = 1;
-        while (splits < 8 && small * splits * 2 <= 2 * sms && slabs >= 8 * splits) splits *= 2;
+    bool paired = false;
+    if (const int64_t t = 26000 + waves(big, sms * 36 / 152) * (slabs + 1) / 2 * 670; t < best && slabs >= 8) { best = t; splits = 2; paired = true; }
+    for (int q = 1; q <= 8 && (q == 1 || slabs >= 4 * q); q *= 2) {
+        const int64_t t = 2000 + waves(small * q, 2 * sms) * (6000 + waves(slabs, q) * (small * q > sms ? 620 : 420));
+        if (t < best) { best = t; splits = q; paired = false; }
     }
-    a.tiles_m = static_cast<int>((p.M + (splits ? 127 : 255)) / (splits ? 128 : 256));
-    a.tiles_n = static_cast<int>((p.N + (splits ? kSplitN : 256) - 1) / (splits ? kSplitN : 256));
-    a.tiles = a.whole = static_cast<int>(splits ? small : big);
+    const int bm = splits && !paired ? 128 : 256, bn = splits && !paired ? kSplitN : 256;
+    a.tiles_m = static_cast<int>((p.M + bm - 1) / bm);
+    a.tiles_n = static_cast<int>((p.N + bn - 1) / bn);
+    a.tiles = a.whole = static_cast<int>(splits && !paired ? small : big);
     if (!splits) {
         // a last wave of at most half the pairs: half tiles, one for each of twice as many
         const int rest = static_cast<int>(big % pairs);
@@ -847,9 +881,9 @@ cudaError_t tc_product(const Product& p, const TcPlan& plan, void* workspace, cu
     if (!operand_map(&a.mapA, q.A, q.sAi, q.sAp, q.sAb, p.M, p.K, p.nodes, a.planes, 128) ||
         !operand_map(&a.mapB, q.B, q.sBj, q.sBp, q.sBb, p.N, p.K, p.nodes, a.planes, 64))
         return cudaErrorInvalidValue;
-    return p.mode == kForward ? launch_mode<kForward>(a, promote, splits, sms, st)
-         : p.mode == kGradInput ? launch_mode<kGradInput>(a, promote, splits, sms, st)
-                                : launch_mode<kGradWeight>(a, promote, splits, sms, st);
+    return p.mode == kForward ? launch_mode<kForward>(a, promote, splits, paired, sms, st)
+         : p.mode == kGradInput ? launch_mode<kGradInput>(a, promote, splits, paired, sms, st)
+                                : launch_mode<kGradWeight>(a, promote, splits, paired, sms, st);
 }
 
 }  // namespace linear

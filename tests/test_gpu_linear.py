@@ -359,3 +359,11 @@ def test_few_rows(rows, n, k, dt):
     _check(P, Z, tol, dt)
     assert _untouched(ybuf, Y) and _untouched(pbuf, P)
     glr.glr_operator_status()
+
+
+@pytest.mark.parametrize("rows,n,k", [(1000, 2048, 8200), (1000, 8200, 2048), (8200, 1000, 2048), (20, 4100, 4097), (400, 1100, 2100)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("pad,shift", [(0, 0), (3, 1)])
+def test_long_contractions_of_few_tiles(rows, n, k, dt, pad, shift):
+    """Contractions that pairs of SMs or single ones share, of the product and of each gradient in turn."""
+    test_large_products(rows, n, k, dt, pad, shift)
