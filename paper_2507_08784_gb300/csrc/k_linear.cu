@@ -384,21 +384,31 @@ __global__ void __launch_bounds__(kSumThreads) column_sums_kernel(const __grid_c
     const int64_t r0 = c.rows * split / splits, r1 = c.rows * (split + 1) / splits;
     const T* x = static_cast<const T*>(c.x) + node * c.rows * c.ldx + j;
     float s[8] = {};
-    if (left > 0) {
-        constexpr int kVec = Traits<T>::kVec;
-#pragma unroll 4
-        for (int64_t i = r0 + lane; i < r1; i += kSumLanes) {
-            T v[8];
-            if (wide && left == 8) {
+    if (wide && left == 8) {
+        // loads of several rows at once, zero past the last one
+        constexpr int kPer = 8 / Traits<T>::kVec, kAhead = 8 / kPer;
+        for (int64_t i = r0 + lane; i < r1; i += kAhead * kSumLanes) {
+            uint4 u[kAhead][kPer];
 #pragma unroll
-                for (int e = 0; e < 8; e += kVec) *reinterpret_cast<uint4*>(v + e) = *reinterpret_cast<const uint4*>(x + i * c.ldx + e);
-            } else {
+            for (int q = 0; q < kAhead; ++q)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = e < left ? x[i * c.ldx + e] : T(0.f);
-            }
+                for (int h = 0; h < kPer; ++h)
+                    u[q][h] = i + q * kSumLanes < r1 ? load_once(reinterpret_cast<const uint4*>(x + (i + q * kSumLanes) * c.ldx) + h) : uint4{0, 0, 0, 0};
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[e] += to_f(v[e]);
+            for (int q = 0; q < kAhead; ++q)
+#pragma unroll
+                for (int h = 0; h < kPer; ++h) {
+                    float f[Traits<T>::kVec];
+                    widen(u[q][h], f, static_cast<const T*>(nullptr));
+#pragma unroll
+                    for (int e = 0; e < Traits<T>::kVec; ++e) s[h * Traits<T>::kVec + e] += f[e];
+                }
         }
+    } else if (left > 0) {
+        for (int64_t i = r0 + lane; i < r1; i += kSumLanes)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e < left) s[e] += to_f(x[i * c.ldx + e]);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) part[lane][col + e] = s[e];
