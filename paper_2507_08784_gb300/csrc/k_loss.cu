@@ -302,8 +302,8 @@ constexpr int most_workers(bool few) { return few ? kWorkers : kWorkers - 1; }
 // HELD: a slot has at most kHeld vectors a worker thread, and the exponentials of the statistics stay in
 // registers for the gradient; else (rows of more than eight such slots) they are formed again.  TWO: a hard
 // term beside tau != 1, so that the sums are kept at two temperatures: kBoth takes two exponentials an element, and at
-// tau = 2 kSquares has the second as the square of the first (4096 rows
-// of 32768 bf16, 64 entries, a hard term: tau = 2 126 -> 109 us, tau = 3 126, tau = 1 103).
+// tau = 2 or 4 the second is the first's square or fourth power (4096 rows
+// of 32768 bf16, 64 entries, a hard term: tau = 2 126 -> 109 us, tau = 4 126 -> 111, tau = 3 126, tau = 1 103).
 //
 // A worker's row is: wait for the slot, sums, one barrier, the merge of all warps' sums (and of the cluster's
 // CTAs), the gradient into the slot.  What each of up to fourteen warps would do for itself is paid that many
@@ -320,7 +320,18 @@ constexpr int most_workers(bool few) { return few ? kWorkers : kWorkers - 1; }
 // With more than 64 entries (FEW false) the latter would not be done in time: a warp of its own sees to them, ahead by
 // up to four rows, and takes a worker's place (8192 rows of 131071 bf16, 128 entries: 917 -> 734 us; 4096 rows of 32768,
 // 128 entries 124 -> 108, 64 entries 96 -> 101 if it did it there too).
-constexpr int kBoth = 1, kSquares = 2;
+constexpr int kBoth = 1, kSquares = 2, kFourths = 3;
+// s + e^tau, and f e + f1 e^tau
+template <int TWO>
+__device__ __forceinline__ uint64_t power_sum(uint64_t e, uint64_t s) {
+    if (TWO == kFourths) e = mul2(e, e);
+    return fma2(e, e, s);
+}
+template <int TWO>
+__device__ __forceinline__ uint64_t two_powers(uint64_t f, uint64_t f1, uint64_t e) {
+    const uint64_t q = TWO == kFourths ? mul2(mul2(e, e), e) : e;
+    return mul2(fma2(f1, q, f), e);
+}
 template <int K, class T, bool HELD, int TWO, bool FEW>
 __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_constant__ RowArgs a) {
     chain_begin();
@@ -776,7 +787,7 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
                     for (int i = 0; i < P; ++i) {
                         const uint64_t d = add2(x[i], nr), e = exp2_2(mul2(d, c2));
                         s2[i & 1] = add2(s2[i & 1], e);
-                        if (TWO) t2[i & 1] = TWO == kSquares ? fma2(e, e, t2[i & 1]) : add2(t2[i & 1], exp2_2(mul2(d, l2)));
+                        if (TWO) t2[i & 1] = TWO >= kSquares ? power_sum<TWO>(e, t2[i & 1]) : add2(t2[i & 1], exp2_2(mul2(d, l2)));
                         if (kKeep > 1) kept[q][i] = e;
                     }
                 }
@@ -797,7 +808,7 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
                     for (int i = 0; i < P; ++i) {
                         const uint64_t d = add2(x[i], nr), e = exp2_2(mul2(d, c2));
                         s2 = add2(s2, e);
-                        if (TWO) t2 = TWO == kSquares ? fma2(e, e, t2) : add2(t2, exp2_2(mul2(d, l2)));
+                        if (TWO) t2 = TWO >= kSquares ? power_sum<TWO>(e, t2) : add2(t2, exp2_2(mul2(d, l2)));
                     }
                 }
                 float x, y;
@@ -842,7 +853,7 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
                 if (counts && HELD) {
                     const float f = k.dense * shrink(m_own, st.m, c);
                     const uint64_t ff = pack2(f, f);
-                    const float f1 = TWO == kSquares ? k.dense1 * shrink(m_own, st.m, kLog2e) : 0.f;
+                    const float f1 = TWO >= kSquares ? k.dense1 * shrink(m_own, st.m, kLog2e) : 0.f;
                     const uint64_t ff1 = pack2(f1, f1);
 #pragma unroll
                     for (int j = 0; j < kKeep; ++j) {
@@ -854,7 +865,7 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
                             for (int i = 0; i < P; ++i) {
                                 const uint64_t e = kept[j][i], g = mul2(ff, e);
                                 x[i] = TWO == kBoth ? fma2(dd1, exp2_2(mul2(add2(x[i], nm), l2)), g)
-                                     : TWO == kSquares ? mul2(fma2(ff1, e, ff), e) : g;
+                                     : TWO >= kSquares ? two_powers<TWO>(ff, ff1, e) : g;
                             }
                             put(v, Vec<T>::put(x));
                         }
@@ -867,7 +878,7 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
 #pragma unroll
                         for (int i = 0; i < P; ++i) {
                             const uint64_t d = add2(x[i], nm), e = exp2_2(mul2(d, c2));
-                            x[i] = TWO == kBoth ? fma2(dd1, exp2_2(mul2(d, l2)), mul2(dd, e)) : TWO == kSquares ? mul2(fma2(dd1, e, dd), e) : mul2(dd, e);
+                            x[i] = TWO == kBoth ? fma2(dd1, exp2_2(mul2(d, l2)), mul2(dd, e)) : TWO >= kSquares ? two_powers<TWO>(dd, dd1, e) : mul2(dd, e);
                         }
                         put(v, Vec<T>::put(x));
                     }
@@ -1070,17 +1081,18 @@ cudaError_t rows_launch(RowArgs a, int dtype, cudaStream_t st) {
     const size_t smem = static_cast<size_t>(a.slots) * a.slot_bytes + a.lists * list;
     const bool held = a.slot_bytes <= slot_max(most);
     const int workers = held ? static_cast<int>((a.slot_bytes / 16 + 32 * kHeld - 1) / (32 * kHeld)) : most, extra = few ? 2 : 3;
-    const int two = K != kDistill || !a.labels.p || a.hard == 0.f || a.inv_tau == 1.f ? 0 : a.inv_tau == 0.5f ? kSquares : kBoth;
+    const int two = K != kDistill || !a.labels.p || a.hard == 0.f || a.inv_tau == 1.f ? 0 : a.inv_tau == 0.5f ? kSquares : a.inv_tau == 0.25f ? kFourths : kBoth;
     auto pick = [&](auto t) {
         using T = decltype(t);
         constexpr bool D = K == kDistill;
-        constexpr int B = D ? kBoth : 0, Q = D ? kSquares : 0;
-        auto of = [&](auto f) {
-            constexpr bool F = decltype(f)::value || !D;
-            return held ? (two == kBoth ? rows_kernel<K, T, true, B, F> : two ? rows_kernel<K, T, true, Q, F> : rows_kernel<K, T, true, 0, F>)
-                        : (two == kBoth ? rows_kernel<K, T, false, B, F> : two ? rows_kernel<K, T, false, Q, F> : rows_kernel<K, T, false, 0, F>);
+        auto of = [&](auto few_entries, auto held_slots) {
+            constexpr bool F = decltype(few_entries)::value || !D, H = decltype(held_slots)::value;
+            return two == kBoth ? rows_kernel<K, T, H, D ? kBoth : 0, F>
+                 : two == kSquares ? rows_kernel<K, T, H, D ? kSquares : 0, F>
+                 : two == kFourths ? rows_kernel<K, T, H, D ? kFourths : 0, F> : rows_kernel<K, T, H, 0, F>;
         };
-        return few ? of(std::true_type()) : of(std::false_type());
+        return few ? (held ? of(std::true_type(), std::true_type()) : of(std::true_type(), std::false_type()))
+                   : (held ? of(std::false_type(), std::true_type()) : of(std::false_type(), std::false_type()));
     };
     auto kernel = dtype == GLR_BF16 ? pick(__nv_bfloat16()) : pick(float());
     if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kDynMax))) != cudaSuccess) return e;
