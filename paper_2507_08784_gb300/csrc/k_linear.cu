@@ -27,7 +27,9 @@ __device__ __forceinline__ void put(void* p, int64_t i, int dtype, float v) {
     else static_cast<float*>(p)[i] = v;
 }
 
-// One thread's vectors of a 64 x 32 slab of an operand X(i, p) = x[i si + p sp], zero past its ends.
+// One thread's elements of a 64 x 32 slab of an operand X(i, p) = x[i si + p sp], zero past its ends: vectors of 16
+// bytes along the contiguous index, or, where rows are not on 16 bytes, single elements, neighbouring threads'
+// next to each other (in a thread's own eight they would touch a sector for every two bytes).
 template <class T>
 struct Slab {
     static constexpr int V = Traits<T>::kVec, P = Traits<T>::kPitch;
@@ -35,25 +37,45 @@ struct Slab {
     T r[kPer][V];
     __device__ __forceinline__ void load(const T* x, int64_t si, int64_t sp, int64_t i0, int64_t p0, int64_t ni, int64_t np,
                                          bool wide) {
+        const bool along_p = sp == 1;
+        if (wide) {
 #pragma unroll
-        for (int u = 0; u < kPer; ++u) {
-            const int v = threadIdx.x + u * kThreads;
-            // vectors run along the contiguous index
-            const bool along_p = sp == 1;
-            const int64_t i = i0 + (along_p ? v / (kSlab / V) : v % (kTile / V) * V);
-            const int64_t p = p0 + (along_p ? v % (kSlab / V) * V : v / (kTile / V));
-            const bool in = along_p ? i < ni : p < np;
-            const int64_t left = !in ? 0 : along_p ? np - p : ni - i;
-            const T* src = x + i * si + p * sp;
-            if (wide && left >= V) {
-                *reinterpret_cast<uint4*>(r[u]) = *reinterpret_cast<const uint4*>(src);
-            } else {
+            for (int u = 0; u < kPer; ++u) {
+                const int v = threadIdx.x + u * kThreads;
+                const int64_t i = i0 + (along_p ? v / (kSlab / V) : v % (kTile / V) * V);
+                const int64_t p = p0 + (along_p ? v % (kSlab / V) * V : v / (kTile / V));
+                const bool in = along_p ? i < ni : p < np;
+                const int64_t left = !in ? 0 : along_p ? np - p : ni - i;
+                const T* src = x + i * si + p * sp;
+                if (left >= V) {
+                    *reinterpret_cast<uint4*>(r[u]) = *reinterpret_cast<const uint4*>(src);
+                } else {
 #pragma unroll
-                for (int e = 0; e < V; ++e) r[u][e] = e < left ? src[e] : T(0.f);
+                    for (int e = 0; e < V; ++e) r[u][e] = e < left ? src[e] : T(0.f);
+                }
             }
+        } else {
+            const int64_t i = i0 + (along_p ? threadIdx.x / kSlab : threadIdx.x % kTile), p = p0 + (along_p ? threadIdx.x % kSlab : threadIdx.x / kTile);
+            const int64_t di = along_p ? kThreads / kSlab : 0, dp = along_p ? 0 : kThreads / kTile;
+#pragma unroll
+            for (int u = 0; u < kPer; ++u)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const int64_t ie = i + (u * V + e) * di, pe = p + (u * V + e) * dp;
+                    r[u][e] = ie < ni && pe < np ? x[ie * si + pe * sp] : T(0.f);
+                }
         }
     }
-    __device__ __forceinline__ void store(T* s, bool along_p) const {
+    __device__ __forceinline__ void store(T* s, bool along_p, bool wide) const {
+        if (!wide) {
+            T* to = s + (along_p ? threadIdx.x / kSlab * P + threadIdx.x % kSlab : threadIdx.x % kTile * P + threadIdx.x / kTile);
+            const int step = along_p ? kThreads / kSlab * P : kThreads / kTile;
+#pragma unroll
+            for (int u = 0; u < kPer; ++u)
+#pragma unroll
+                for (int e = 0; e < V; ++e) to[(u * V + e) * step] = r[u][e];
+            return;
+        }
 #pragma unroll
         for (int u = 0; u < kPer; ++u) {
             const int v = threadIdx.x + u * kThreads;
@@ -196,8 +218,8 @@ __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant
         rb[q].load(B, p.sBj, p.sBp, j0, s * kSlab, p.N, p.K, wide_b);
     };
     auto work = [&](int q, int64_t s) {
-        ra[q].store(sa[q], p.sAp == 1);
-        rb[q].store(sb[q], p.sBp == 1);
+        ra[q].store(sa[q], p.sAp == 1, wide_a);
+        rb[q].store(sb[q], p.sBp == 1, wide_b);
         __syncthreads();
         fetch(q, s + 2);
         slab_mma(acc, sa[q] + wm * P, sb[q] + wn * P, g, t);
@@ -208,16 +230,8 @@ __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant
         work(0, s);
         if (s + 1 < last) work(1, s + 1);
     }
-    if (splits == 1) {
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-            for (int n = 0; n < 4; ++n)
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    finish(p, node, i0 + wm + 16 * m + g + 8 * (q >> 1), j0 + wn + 8 * n + 2 * t + (q & 1), acc[m][n][q]);
-        return;
-    }
+    // (always through shared memory: an epilogue in line with each of a thread's 32 results is more code than a short
+    // product has time to fetch, 54 us against 15 for 32 x 200 x 200)
     float* part = reinterpret_cast<float*>(smem);
     __syncthreads();                                  // every warp is done with the slabs
 #pragma unroll
@@ -470,10 +484,10 @@ cudaError_t any_product(const Product& p, cudaStream_t st) {
     const int64_t tiles = ((p.M + kTile - 1) / kTile) * ((p.N + kTile - 1) / kTile);
     if (tiles > 0x7fffffff) return cudaErrorInvalidValue;
     const bool wa = wide_ok(p.A, p.sAp == 1 ? p.sAi : p.sAp, p.sAb, es), wb = wide_ok(p.B, p.sBp == 1 ? p.sBj : p.sBp, p.sBb, es);
-    // CTAs a tile: as many as fill the SMs twice, as long as each keeps four slabs
+    // CTAs a tile: as many as fill the SMs, as long as each keeps two slabs
     const int64_t slabs = (p.K + kSlab - 1) / kSlab;
     int splits = 1;
-    while (splits < 8 && tiles * p.nodes * splits < 152 && slabs >= 8 * splits) splits *= 2;
+    while (splits < 8 && tiles * p.nodes * splits < 152 && slabs >= 4 * splits) splits *= 2;
     const dim3 grid(static_cast<unsigned>(tiles), splits, p.nodes);
     return p.dtype == GLR_BF16 ? launch_clusters(product_kernel<__nv_bfloat16>, grid, kThreads, splits, st, p, wa, wb)
                                : launch_clusters(product_kernel<float>, grid, kThreads, splits, st, p, wa, wb);

@@ -354,6 +354,7 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
     constexpr int CG = 2;
     constexpr bool MNA = mn_major_a(MODE), MNB = mn_major_b(MODE);
     constexpr int DT = PROMOTE ? GLR_F32 : GLR_BF16;
+    constexpr bool PLANES = PROMOTE || MODE == kGradWeight;          // bf16 gradients of fp32 matrices too
     constexpr int kEpiWarps = epi_warps(PROMOTE), kCopyA = kEpiWarps, kCopyB = kEpiWarps + 1, kIssuer = kEpiWarps + 2, kSpan = BN / (kEpiWarps / 4);
     constexpr uint32_t SB = stage_bytes<BN, CG>();
     constexpr uint32_t kCols = 2 * BN;                               // two accumulators of BN columns
@@ -401,9 +402,9 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
                     const uint32_t st = smem_u32(ring + static_cast<size_t>(s) * SB), bar = peer_addr(smem_u32(&full_bar[s]), 0);
                     if (is_a) {
                         if (rank == 0) mbar_expect_tx(smem_u32(&full_bar[s]), static_cast<uint32_t>(16384 + mine * 128) * CG);
-                        load_a<CG, MNA, PROMOTE>(a, k, m0, tl.node, st, bar);
+                        load_a<CG, MNA, PLANES>(a, k, m0, tl.node, st, bar);
                     } else {
-                        load_b<CG, MNB, PROMOTE>(a, k, n0, mine / 64, tl.node, st, bar);
+                        load_b<CG, MNB, PLANES>(a, k, n0, mine / 64, tl.node, st, bar);
                     }
                     issued |= 1u << s;
                     last = (last & ~(1u << s)) | (use << s);
@@ -688,32 +689,55 @@ __global__ void __launch_bounds__(threads_of(epi_warps(CG == 2)), CG == 2 ? 1 : 
 }
 
 // Rows of `cols` elements, ld apart, as `planes` bf16 matrices in rows of ldp (a multiple of eight), one after the
-// other: x = hi + mid + lo, each the bf16 nearest to what is left.  Bound by HBM.
+// other: x = hi + mid + lo, each the bf16 nearest to what is left.  One or two matrices a launch, eight neighbouring
+// elements a thread, 2 to 256 threads (a power of two) a row.  Bound by HBM.
 constexpr int kPackThreads = 256;
+struct PackJob {
+    const void* x; int64_t rows, cols, ld;
+    __nv_bfloat16* to; int64_t ldp;
+    int shift;                                       // log2 of the threads a row
+    int wide;                                        // 16-byte loads
+};
+struct PackArgs { PackJob job[2]; int planes; };
 template <class T>
-__global__ void __launch_bounds__(kPackThreads) pack_kernel(const T* x, int64_t rows, int64_t cols, int64_t ld, bool wide,
-                                                            __nv_bfloat16* to, int64_t ldp, int planes) {
+__global__ void __launch_bounds__(kPackThreads) pack_kernel(const __grid_constant__ PackArgs a) {
     chain_begin();
-    const int64_t per = ldp / 8, total = rows * per;
-    for (int64_t g = static_cast<int64_t>(blockIdx.x) * kPackThreads + threadIdx.x; g < total; g += static_cast<int64_t>(gridDim.x) * kPackThreads) {
-        const int64_t i = g / per, j = (g - i * per) * 8;
-        const int n = static_cast<int>(cols - j < 8 ? cols - j : 8);
-        float v[8];
-        get8(x, i * ld + j, n, wide, sizeof(T) == 2 ? GLR_BF16 : GLR_F32, v);
-        for (int p = 0; p < planes; ++p) {
-            uint32_t w[4];
+    __shared__ __align__(16) T turn[kPackThreads * 8];
+    const PackJob& x = a.job[blockIdx.y];
+    const int per = 1 << x.shift, lane = threadIdx.x & 31;
+    T* mine = turn + (threadIdx.x & ~31) * 8;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * (kPackThreads >> x.shift);
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * (kPackThreads >> x.shift) + (threadIdx.x >> x.shift); i < x.rows; i += step) {
+        const T* row = static_cast<const T*>(x.x) + i * x.ld;
+        for (int64_t j = (threadIdx.x & (per - 1)) * 8; j < x.ldp; j += per * 8) {
+            const int n = static_cast<int>(min(static_cast<int64_t>(8), x.cols - j));
+            float v[8];
+            const int64_t first = j - lane * 8;
+            if (!x.wide && per >= 32 && first + 256 <= x.ldp) {
+                // a warp's 256 elements of a row, neighbouring lanes' next to each other, turned round in shared memory
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * q], v[2 * q + 1]);
-                // what would round up to infinity is cut off instead
-                if (isinf(__low2float(h)) && isfinite(v[2 * q])) h.x = __float2bfloat16_rz(v[2 * q]);
-                if (isinf(__high2float(h)) && isfinite(v[2 * q + 1])) h.y = __float2bfloat16_rz(v[2 * q + 1]);
-                w[q] = *reinterpret_cast<const uint32_t*>(&h);
-                // an infinity or NaN is the first plane's alone
-                v[2 * q] = isfinite(v[2 * q]) ? v[2 * q] - __low2float(h) : 0.f;
-                v[2 * q + 1] = isfinite(v[2 * q + 1]) ? v[2 * q + 1] - __high2float(h) : 0.f;
+                for (int e = 0; e < 8; ++e) mine[e * 32 + lane] = first + e * 32 + lane < x.cols ? row[first + e * 32 + lane] : T(0.f);
+                __syncwarp();
+                get8(mine, lane * 8, 8, true, sizeof(T) == 2 ? GLR_BF16 : GLR_F32, v);
+                __syncwarp();
+            } else {
+                get8(row, j, n, x.wide, sizeof(T) == 2 ? GLR_BF16 : GLR_F32, v);
             }
-            *reinterpret_cast<uint4*>(to + (p * rows + i) * ldp + j) = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int p = 0; p < a.planes; ++p) {
+                uint32_t w[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * q], v[2 * q + 1]);
+                    // what would round up to infinity is cut off instead
+                    if (isinf(__low2float(h)) && isfinite(v[2 * q])) h.x = __float2bfloat16_rz(v[2 * q]);
+                    if (isinf(__high2float(h)) && isfinite(v[2 * q + 1])) h.y = __float2bfloat16_rz(v[2 * q + 1]);
+                    w[q] = *reinterpret_cast<const uint32_t*>(&h);
+                    // an infinity or NaN is the first plane's alone
+                    v[2 * q] = isfinite(v[2 * q]) ? v[2 * q] - __low2float(h) : 0.f;
+                    v[2 * q + 1] = isfinite(v[2 * q + 1]) ? v[2 * q + 1] - __high2float(h) : 0.f;
+                }
+                *reinterpret_cast<uint4*>(x.to + (p * x.rows + i) * x.ldp + j) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
         }
     }
 }
@@ -782,12 +806,17 @@ cudaError_t launch_mode(TcArgs& a, bool promote, int splits, bool paired, int sm
                    : launch(tc_product_kernel<256, MODE, false>, a, grid, dim3(2), threads_of(epi_warps(false)), smem, st);
 }
 
+// A matrix to pack: its threads a row.
+PackJob pack_job(const void* x, const Storage& s, int64_t esize, void* to) {
+    PackJob j{x, s.rows, s.cols, s.ld, static_cast<__nv_bfloat16*>(to), up8(s.cols), 1, on16(x) && s.ld * esize % 16 == 0};
+    while (j.shift < 8 && (8 << j.shift) < j.ldp) ++j.shift;
+    return j;
+}
 template <class T>
-cudaError_t pack(const void* x, const Storage& s, int planes, void* to, cudaStream_t st) {
-    const int64_t ldp = up8(s.cols), groups = (s.rows * (ldp / 8) + kPackThreads - 1) / kPackThreads;
-    const bool wide = on16(x) && s.ld * static_cast<int64_t>(sizeof(T)) % 16 == 0;
-    return launch_chain(pack_kernel<T>, static_cast<unsigned>(std::min<int64_t>(groups, 152 * 16)), kPackThreads, 0, st,
-                        static_cast<const T*>(x), s.rows, s.cols, s.ld, wide, static_cast<__nv_bfloat16*>(to), ldp, planes);
+cudaError_t pack(const PackArgs& a, int jobs, cudaStream_t st) {
+    int64_t blocks = 1;
+    for (int q = 0; q < jobs; ++q) blocks = std::max(blocks, (a.job[q].rows + (kPackThreads >> a.job[q].shift) - 1) / (kPackThreads >> a.job[q].shift));
+    return launch_chain(pack_kernel<T>, dim3(static_cast<unsigned>(std::min<int64_t>(blocks, 152 * 16)), jobs), kPackThreads, 0, st, a);
 }
 
 // Whether an operand's rows lie on 16 bytes as they are.
@@ -810,11 +839,10 @@ TcPlan tc_plan(const Product& p) {
     const Storage a = storage(p.sAi, p.sAp, p.M, p.K, p.nodes), b = storage(p.sBj, p.sBp, p.N, p.K, p.nodes);
     if (t.pack_a) t.bytes_a = (t.planes * a.rows * up8(a.cols) * 2 + 255) / 256 * 256;
     if (t.pack_b) t.bytes_b = t.planes * b.rows * up8(b.cols) * 2;
-    // Packing reads the matrices once more and launches a kernel for each: it pays where the product itself is long
-    // (bf16 rows off 16 bytes, 16 x 4096 x 4096: 76 us unpacked, 33 packed; 128 x 1500 x 1500 38 and 19; fp32 96 x 4096 x
-    // 4096 134 and 76; 64 x 1500 x 1500 unpacked 23 in either type, which is what packing it takes by itself).
+    // Packing reads the matrices once more, in a launch of its own.  any_product, the other way, takes about 2 us for every
+    // 32 contraction elements of a CTA: @@
     const double flops = 2.0 * static_cast<double>(p.M) * static_cast<double>(p.N) * static_cast<double>(p.K) * p.nodes;
-    t.ok = !(t.pack_a || t.pack_b) || flops >= 5e8;
+    t.ok = !(t.pack_a || t.pack_b) || (flops >= 5e7 && (t.planes == 1 || p.M >= 16));
     return t;
 }
 
@@ -823,17 +851,20 @@ cudaError_t tc_product(const Product& p, const TcPlan& plan, void* workspace, cu
     a.p = p;
     Product& q = a.p;
     cudaError_t e = cudaSuccess;
+    PackArgs jobs{};
+    jobs.planes = plan.planes;
+    int n = 0;
     auto packed = [&](const void*& x, int64_t& si, int64_t& sp, int64_t& sb, int64_t ni, uint8_t* to) {
         const Storage s = storage(si, sp, ni, p.K, p.nodes);
-        e = plan.planes == 3 ? pack<float>(x, s, 3, to, st) : pack<__nv_bfloat16>(x, s, 1, to, st);
+        jobs.job[n++] = pack_job(x, s, plan.planes == 3 ? 4 : 2, to);
         x = to;
         (sp == 1 ? si : sp) = up8(s.cols);
         sb = sp == 1 ? 0 : p.K * sp;
     };
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     if (plan.pack_a) packed(q.A, q.sAi, q.sAp, q.sAb, p.M, ws);
-    if (e == cudaSuccess && plan.pack_b) packed(q.B, q.sBj, q.sBp, q.sBb, p.N, ws + plan.bytes_a);
-    if (e != cudaSuccess) return e;
+    if (plan.pack_b) packed(q.B, q.sBj, q.sBp, q.sBb, p.N, ws + plan.bytes_a);
+    if (n && (e = plan.planes == 3 ? pack<float>(jobs, n, st) : pack<__nv_bfloat16>(jobs, n, st)) != cudaSuccess) return e;
     int dev = 0, sms = 0;
     if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
     if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;

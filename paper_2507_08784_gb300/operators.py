@@ -72,7 +72,7 @@ def _call(fn, args, stream) -> None:
 def _space(args, query, x: torch.Tensor, work: float, ragged: int, stream):
     """The workspace that a product asks for (float32 or rows off 16 bytes, where it is large), from PyTorch's
     allocator in the stream's own pool: its memory is reused in the order of the work that runs there."""
-    if (x.dtype == torch.bfloat16 and not ragged) or work < 5e8:
+    if (x.dtype == torch.bfloat16 and not ragged) or work < 5e7:
         return None
     need = ctypes.c_int64(0)
     _check(query(ctypes.byref(args), ctypes.byref(need)))

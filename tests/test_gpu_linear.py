@@ -367,3 +367,51 @@ def test_few_rows(rows, n, k, dt):
 def test_long_contractions_of_few_tiles(rows, n, k, dt, pad, shift):
     """Contractions that pairs of SMs or single ones share, of the product and of each gradient in turn."""
     test_large_products(rows, n, k, dt, pad, shift)
+
+
+@pytest.mark.parametrize("nodes,rows,n,k", [(2, 600, 700, 900), (1, 3000, 1000, 1032), (8, 64, 512, 1001)])
+def test_bf16_gradients_of_fp32_matrices(nodes, rows, n, k):
+    """Products of fp32 matrices large enough to be laid out in planes, rounded to bf16 once at the end."""
+    import paper_2507_08784_gb300 as glr
+    gen = torch.Generator().manual_seed(rows)
+    dZ, X = _mat(nodes * rows, n, torch.float32, gen), _mat(nodes * rows, k, torch.float32, gen)
+    dW = [torch.empty(n, k, device="cuda", dtype=torch.bfloat16) for _ in range(nodes)]
+    db = [torch.empty(n, device="cuda", dtype=torch.bfloat16) for _ in range(nodes)]
+    glr.glr_linear_grad_weight(dZ, X, dW, db=db)
+    for i in range(nodes):
+        a, b = (t[i * rows:(i + 1) * rows].double().T.contiguous().cpu() for t in (dZ, X))
+        _check(dW[i], a @ b.T, _sum_tol(a, b, rows, torch.float32), torch.bfloat16)
+        _check(db[i], a.sum(1), (rows + 8) * 2.0 ** -23 * a.abs().sum(1), torch.bfloat16)
+    glr.glr_operator_status()
+
+
+@pytest.mark.parametrize("rows,n,k", [(1, 5, 3), (20, 64, 64), (65, 130, 33), (129, 257, 200), (300, 264, 1032), (40, 1000, 2040), (384, 768, 520)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("pad", [0, 1])
+def test_c_entries_without_workspace(rows, n, k, dt, pad):
+    """All three products through the C entry points with no workspace, whatever one they would ask for."""
+    import ctypes
+    import paper_2507_08784_gb300 as glr
+    from paper_2507_08784_gb300 import _lib
+    code, dt = (0, torch.float32) if dt == "f32" else (1, torch.bfloat16)
+    assert (_lib.GLR_F32, _lib.GLR_BF16) == (0, 1)
+    gen = torch.Generator().manual_seed(rows + n)
+    X, W, Z = _mat(rows, k, dt, gen, pad), _mat(n, k, dt, gen, pad, scale=k ** -0.5), _mat(rows, n, dt, gen, pad)
+    (Y, ybuf), (D, dbuf) = _out(rows, n, dt, pad), _out(rows, k, dt, pad)
+    G = torch.empty(n, k, device="cuda", dtype=dt)
+    at = (ctypes.c_void_p * 1)(G.data_ptr())
+    lib, st = glr.load(), torch.cuda.current_stream().cuda_stream
+    p = lambda t: t.data_ptr()  # noqa: E731
+    calls = [(lib.glr_linear, _lib.GlrLinearArgs(rows, n, k, p(X), k + pad, p(W), k + pad, p(Y), n + pad, None, None, 0, None, 0, None, 0, code, 0)),
+             (lib.glr_linear_grad_input, _lib.GlrLinearGradInputArgs(rows, n, k, p(Z), n + pad, p(W), k + pad, p(D), k + pad, None, 0,
+                                                                     None, 0, None, 0, None, 0, code, 0)),
+             (lib.glr_linear_grad_weight, _lib.GlrLinearGradWeightArgs(1, rows, n, k, p(Z), n + pad, p(X), k + pad, ctypes.addressof(at),
+                                                                       None, None, 0, code, code))]
+    for fn, args in calls:
+        assert fn(ctypes.byref(args), st) == 0
+    torch.cuda.synchronize()
+    x, w, z = (t.cpu().double() for t in (X, W, Z))
+    for got, a, b in ((Y, x, w), (D, z, w.T.contiguous()), (G, z.T.contiguous(), x.T.contiguous())):
+        _check(got, a @ b.T, _sum_tol(a, b, a.shape[1], dt), dt)
+    assert _untouched(ybuf, Y) and _untouched(dbuf, D)
+    glr.glr_operator_status()
