@@ -58,6 +58,7 @@ struct TcArgs {
     int planes;                                 // 1, or 3: a slab of the contraction is six products of planes
     int chunk;                                  // slabs whose sums are kept in tensor memory (PROMOTE)
     int wide;                                   // 16-byte accesses: bit 0 out, 1 bias, 2 add, 3 pre, 4 aux
+    int columns;                                // some of them but the bias not: epilogues take columns
 };
 
 template <int BN, int CG>
@@ -144,6 +145,17 @@ __device__ __forceinline__ void tmem_load32(uint32_t ta, float (&v)[32]) {
     for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(u[j]);
 }
 
+// sum += sixteen columns (what 32 at a time would take beside the sums does not fit the registers).
+__device__ __forceinline__ void tmem_add16(uint32_t ta, float* sum) {
+    uint32_t u[16];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]),
+                   "=r"(u[8]), "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
+                 : "r"(ta));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int j = 0; j < 16; ++j) sum[j] += __uint_as_float(u[j]);
+}
 __device__ __forceinline__ void tmem_store32(uint32_t ta, const float* v) {
     uint32_t u[32];
 #pragma unroll
@@ -156,8 +168,16 @@ __device__ __forceinline__ void tmem_store32(uint32_t ta, const float* v) {
                    "r"(u[30]), "r"(u[31]), "r"(ta) : "memory");
 }
 
-// Eight elements at p (n of them in range), widened.
-__device__ __forceinline__ void get8(const void* base, int64_t at, int n, bool wide, int dtype, float (&v)[8]) {
+// Eight elements at p, `step` apart (n of them in range; wide: neighbours, on 16 bytes), widened.
+__device__ __forceinline__ void widen8(const uint4& u, float (&v)[8]) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        v[2 * q] = __uint_as_float(w[q] << 16);
+        v[2 * q + 1] = __uint_as_float(w[q] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void get8(const void* base, int64_t at, int n, bool wide, int dtype, float (&v)[8], int64_t step = 1) {
     if (dtype == GLR_F32) {
         const float* p = static_cast<const float*>(base) + at;
         if (wide && n == 8) {
@@ -165,25 +185,19 @@ __device__ __forceinline__ void get8(const void* base, int64_t at, int n, bool w
             v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = e < n ? p[e] : 0.f;
+            for (int e = 0; e < 8; ++e) v[e] = e < n ? p[e * step] : 0.f;
         }
         return;
     }
     const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(base) + at;
     if (wide && n == 8) {
-        const uint4 u = *reinterpret_cast<const uint4*>(p);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            v[2 * q] = __uint_as_float(w[q] << 16);
-            v[2 * q + 1] = __uint_as_float(w[q] & 0xffff0000u);
-        }
+        widen8(*reinterpret_cast<const uint4*>(p), v);
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = e < n ? __bfloat162float(p[e]) : 0.f;
+        for (int e = 0; e < 8; ++e) v[e] = e < n ? __bfloat162float(p[e * step]) : 0.f;
     }
 }
-__device__ __forceinline__ void put8(void* base, int64_t at, int n, bool wide, int dtype, const float (&v)[8]) {
+__device__ __forceinline__ void put8(void* base, int64_t at, int n, bool wide, int dtype, const float (&v)[8], int64_t step = 1) {
     if (dtype == GLR_F32) {
         float* p = static_cast<float*>(base) + at;
         if (wide && n == 8) {
@@ -191,7 +205,7 @@ __device__ __forceinline__ void put8(void* base, int64_t at, int n, bool wide, i
             *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) if (e < n) p[e] = v[e];
+            for (int e = 0; e < 8; ++e) if (e < n) p[e * step] = v[e];
         }
         return;
     }
@@ -206,7 +220,7 @@ __device__ __forceinline__ void put8(void* base, int64_t at, int n, bool wide, i
         *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) if (e < n) p[e] = __float2bfloat16_rn(v[e]);
+        for (int e = 0; e < 8; ++e) if (e < n) p[e * step] = __float2bfloat16_rn(v[e]);
     }
 }
 template <bool SLOPE, bool FAST>
@@ -225,48 +239,55 @@ __device__ __forceinline__ void act8(float (&v)[8], int act) {
     }
 }
 
-// The epilogue on eight neighbouring columns of a row (i, j): acc in v.
-template <int MODE, int DT>
-__device__ __forceinline__ void epilogue8(const TcArgs& a, int node, int64_t i, int64_t j, float (&v)[8]) {
+// The epilogue on eight elements: acc in v.  They are neighbouring columns of a row (i, j), or with COLUMN neighbouring
+// rows of a column, for matrices that do not lie on 16 bytes: then neighbouring lanes are neighbouring columns, and an
+// access covers whole sectors all the same (4096 x 4096 x 512 bf16, results in rows of 4099: 83 -> 40 us).
+// add and pre, unless null: the row's eight elements of either, asked for earlier.
+template <int MODE, int DT, bool COLUMN>
+__device__ __forceinline__ void epilogue8(const TcArgs& a, int node, int64_t i, int64_t j, float (&v)[8], const uint4* add = nullptr,
+                                          const uint4* pre = nullptr) {
     const Product& p = a.p;
     constexpr int dt = DT;                      // of the results, and but in kGradWeight of the inputs too
-    const int n = static_cast<int>(p.N - j < 8 ? p.N - j : 8);
+    const int64_t left = COLUMN ? p.M - i : p.N - j;
+    const int n = static_cast<int>(left < 8 ? left : 8);
+    auto get = [&](const void* x, int64_t ld, int bit, float (&f)[8]) { get8(x, i * ld + j, n, !COLUMN && (a.wide & bit), dt, f, COLUMN ? ld : 1); };
+    auto put = [&](void* x, int64_t ld, int bit, const float (&f)[8]) { put8(x, i * ld + j, n, !COLUMN && (a.wide & bit), dt, f, COLUMN ? ld : 1); };
+    auto added = [&](const float (&f)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += f[e];
+    };
     if (MODE == kGradWeight) {
-        put8(p.outs[node], i * p.N + j, n, a.wide & 1, dt, v);
+        put(p.outs[node], p.N, 1, v);
         return;
     }
     float x[8];
+    if (p.add) {
+        if (add && n == 8) widen8(*add, x);
+        else get(p.add, p.ldadd, 4, x);
+    }
     if (MODE == kForward) {
         if (p.bias) {
-            get8(p.bias, j, n, a.wide & 2, dt, x);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += x[e];
+            float b[8];
+            get8(p.bias, j, COLUMN ? 8 : n, !COLUMN && (a.wide & 2), dt, b, COLUMN ? 0 : 1);
+            added(b);
         }
-        if (p.aux) put8(p.aux, i * p.ldaux + j, n, a.wide & 16, dt, v);
+        if (p.aux) put(p.aux, p.ldaux, 16, v);
         act8<false, DT == GLR_BF16>(v, p.act);
-        if (p.add) {
-            get8(p.add, i * p.ldadd + j, n, a.wide & 4, dt, x);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += x[e];
-        }
+        if (p.add) added(x);
     } else {
-        if (p.add) {
-            get8(p.add, i * p.ldadd + j, n, a.wide & 4, dt, x);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += x[e];
-        }
-        if (p.aux) put8(p.aux, i * p.ldaux + j, n, a.wide & 16, dt, v);
+        if (p.add) added(x);
+        if (p.aux) put(p.aux, p.ldaux, 16, v);
         if (p.pre) {
-            get8(p.pre, i * p.ldpre + j, n, a.wide & 8, dt, x);
+            if (pre && n == 8) widen8(*pre, x);
+            else get(p.pre, p.ldpre, 8, x);
             act8<true, DT == GLR_BF16>(x, p.act);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] *= x[e];
         }
     }
-    put8(p.out, i * p.ldo + j, n, a.wide & 1, dt, v);
+    put(p.out, p.ldo, 1, v);
 }
 
-// A tile: its node, rows 128 CG m .., columns n0 .. n0 + bn.
 struct Tile { int node, m, n0, bn; };
 template <int BN>
 __device__ __forceinline__ Tile tile_at(const TcArgs& a, int t) {
@@ -466,13 +487,8 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
                     fence_after();
                     const uint32_t ta = tmem + static_cast<uint32_t>(b * BN + c0) + (static_cast<uint32_t>(32 * quad) << 16);
 #pragma unroll
-                    for (int c = 0; c < kSpan; c += 32) {
-                        if (c >= span) break;
-                        float v[32];
-                        tmem_load32(ta + static_cast<uint32_t>(c), v);
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) sum[c + e] += v[e];
-                    }
+                    for (int c = 0; c < kSpan; c += 16)
+                        if (c < span) tmem_add16(ta + static_cast<uint32_t>(c), sum + c);
                     if (k0 + a.chunk < a.slabs) {
                         hand_back();
                         tuse[b] ^= 1u;
@@ -494,6 +510,20 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
             const uint32_t ta = tmem + static_cast<uint32_t>(b * BN + c0) + (static_cast<uint32_t>(32 * quad) << 16);
 #pragma unroll 1
             for (int c = 0; c < span; c += 32) {
+                const int64_t j = static_cast<int64_t>(tl.n0) + c0 + c + (lane & 3) * 8;
+                // what the epilogue reads of the block, asked for before its sums are there
+                constexpr bool AHEAD = !PROMOTE && MODE != kGradWeight;
+                uint4 ahead[8];
+                if (AHEAD && !a.columns) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int64_t i = i0 + 8 * q + (lane >> 2);
+                        const bool in = i < a.p.M && j + 8 <= a.p.N;
+                        if (in && a.p.add) ahead[q] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.p.add) + i * a.p.ldadd + j);
+                        if (MODE == kGradInput && in && a.p.pre)
+                            ahead[q + 4] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.p.pre) + i * a.p.ldpre + j);
+                    }
+                }
                 float v[32];
                 tmem_load32(ta + static_cast<uint32_t>(c), v);
                 if (c + 32 >= span) hand_back();     // the last of this warp's columns
@@ -502,7 +532,17 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
                 for (int e = 0; e < 32; e += 4)
                     *reinterpret_cast<float4*>(block + lane * kBlockPitch + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
                 __syncwarp();
-                const int64_t j = static_cast<int64_t>(tl.n0) + c0 + c + (lane & 3) * 8;
+                if (a.columns) {
+#pragma unroll 1
+                    for (int q = 0; q < 4; ++q) {
+                        const int64_t j = static_cast<int64_t>(tl.n0) + c0 + c + lane;
+                        float w[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) w[e] = block[(8 * q + e) * kBlockPitch + lane];
+                        if (i0 + 8 * q < a.p.M && j < a.p.N) epilogue8<MODE, DT, true>(a, tl.node, i0 + 8 * q, j, w);
+                    }
+                    continue;
+                }
 #pragma unroll 1
                 for (int q = 0; q < 4; ++q) {
                     const int r = 8 * q + (lane >> 2);
@@ -512,7 +552,12 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_
                         const float4 x = *reinterpret_cast<const float4*>(block + r * kBlockPitch + (lane & 3) * 8 + h);
                         w[h] = x.x; w[h + 1] = x.y; w[h + 2] = x.z; w[h + 3] = x.w;
                     }
-                    if (i0 + r < a.p.M && j < a.p.N) epilogue8<MODE, DT>(a, tl.node, i0 + r, j, w);
+                    if (i0 + r < a.p.M && j < a.p.N)
+                        epilogue8<MODE, DT, false>(a, tl.node, i0 + r, j, w, AHEAD ? ahead : nullptr, AHEAD ? ahead + 4 : nullptr);
+                    if (AHEAD) {                     // the loop is kept rolled: the next ones move up
+#pragma unroll
+                        for (int u = 0; u < 3; ++u) { ahead[u] = ahead[u + 1]; ahead[u + 4] = ahead[u + 5]; }
+                    }
                 }
             }
             tuse[b] ^= 1u;
@@ -636,12 +681,8 @@ __global__ void __launch_bounds__(threads_of(epi_warps(CG == 2)), CG == 2 ? 1 : 
             if (!__all_sync(0xffffffffu, ok)) break;
             fence_after();
 #pragma unroll
-            for (int c = 0; c < kSpan; c += 32) {
-                float v[32];
-                tmem_load32(tmem + static_cast<uint32_t>(b * BN + (warp >> 2) * kSpan + c) + (static_cast<uint32_t>(32 * (warp & 3)) << 16), v);
-#pragma unroll
-                for (int e = 0; e < 32; ++e) sum[c + e] += v[e];
-            }
+            for (int c = 0; c < kSpan; c += 16)
+                tmem_add16(tmem + static_cast<uint32_t>(b * BN + (warp >> 2) * kSpan + c) + (static_cast<uint32_t>(32 * (warp & 3)) << 16), sum + c);
             hand_back<CG>(smem_u32(&tempty_bar[b]), lead);
             tuse[b] ^= 1u;
             b ^= 1;
@@ -659,7 +700,7 @@ __global__ void __launch_bounds__(threads_of(epi_warps(CG == 2)), CG == 2 ? 1 : 
     if (CG == 2 || splits > 1) cluster_sync();
     const int rows = 128 / splits;                   // this CTA's rows of the tile, eight columns a thread
     for (int e = threadIdx.x; e < rows * (BN / 8); e += kThreads) {
-        const int r = split * rows + e / (BN / 8), c = e % (BN / 8) * 8;
+        const int r = split * rows + (a.columns ? e / BN * 8 : e / (BN / 8)), c = a.columns ? e % BN : e % (BN / 8) * 8;
         const int64_t i = static_cast<int64_t>(m0) + r, j = static_cast<int64_t>(tl.n0) + c;
         if (i >= a.p.M || j >= a.p.N) continue;
         float v[8];
@@ -667,6 +708,15 @@ __global__ void __launch_bounds__(threads_of(epi_warps(CG == 2)), CG == 2 ? 1 : 
         for (int q = 0; q < 8; ++q) v[q] = 0.f;
         for (int q = 0; q < splits; ++q) {
             const uint32_t from = peer_addr(smem_u32(part + r * kPitch + c), half + CG * q);
+            if (a.columns) {
+#pragma unroll
+                for (int y = 0; y < 8; ++y) {
+                    float x;
+                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(from + 4 * kPitch * y) : "memory");
+                    v[y] += x;
+                }
+                continue;
+            }
 #pragma unroll
             for (int h = 0; h < 8; h += 4) {
                 float x[4];
@@ -676,8 +726,14 @@ __global__ void __launch_bounds__(threads_of(epi_warps(CG == 2)), CG == 2 ? 1 : 
                 for (int y = 0; y < 4; ++y) v[h + y] += x[y];
             }
         }
-        if (a.p.out_dtype == GLR_F32) epilogue8<MODE, GLR_F32>(a, tl.node, i, j, v);
-        else epilogue8<MODE, GLR_BF16>(a, tl.node, i, j, v);
+        const bool wide32 = a.p.out_dtype == GLR_F32;
+        if (a.columns) {
+            if (wide32) epilogue8<MODE, GLR_F32, true>(a, tl.node, i, j, v);
+            else epilogue8<MODE, GLR_BF16, true>(a, tl.node, i, j, v);
+        } else {
+            if (wide32) epilogue8<MODE, GLR_F32, false>(a, tl.node, i, j, v);
+            else epilogue8<MODE, GLR_BF16, false>(a, tl.node, i, j, v);
+        }
     }
     if (CG == 2 || splits > 1) cluster_sync();       // the peers are done with this CTA's shared memory
     else __syncthreads();
@@ -911,6 +967,8 @@ cudaError_t tc_product(const Product& p, const TcPlan& plan, void* workspace, cu
         a.wide = (on16(p.out) && p.ldo % per16 == 0 ? 1 : 0) | (on16(p.bias) ? 2 : 0) | (on16(p.add) && p.ldadd % per16 == 0 ? 4 : 0) |
                  (on16(p.pre) && p.ldpre % per16 == 0 ? 8 : 0) | (on16(p.aux) && p.ldaux % per16 == 0 ? 16 : 0);
     }
+    const int need = p.mode == kGradWeight ? 1 : 1 | (p.add ? 4 : 0) | (p.pre ? 8 : 0) | (p.aux ? 16 : 0);
+    a.columns = (a.wide & need) != need;
     if (!operand_map(&a.mapA, q.A, q.sAi, q.sAp, q.sAb, p.M, p.K, p.nodes, a.planes, 128) ||
         !operand_map(&a.mapB, q.B, q.sBj, q.sBp, q.sBb, p.N, p.K, p.nodes, a.planes, 64))
         return cudaErrorInvalidValue;
