@@ -20,7 +20,11 @@
 // tc_split_kernel, the sums of 256 contraction elements (64 of three planes) join the total in rounded additions by
 // the epilogue warps.
 //
-// What bounds it: the tensor pipe for contractions of about 1000 and more; below that the epilogue.  Tensor memory
+// What bounds it: the tensor pipe for contractions of about 1000 and more, 512 cycles a 256 x 256 x 64 stage (8192 x
+// 11008 x 4096 bf16: 388 us, 1905 TFLOP/s; with SiLU and pre-activation 406); below that the epilogue (8192 x 2048 x 512:
+// 29 us); for few tiles the loads' latency; with promoted sums also the reads of tensor memory, a chunk's in about the time of
+// its products (5632 x 2048 of eight nodes' 1024 rows: 117 us to bf16, 199 to fp32).  fp32: six products a slab, 4096 x
+// 4096 x 2048 328 us.  Tensor memory
 // gives a thread a row; the epilogue warps turn 32 x 32 blocks round in shared memory, so that four lanes share a
 // row and an access covers whole sectors of eight rows.
 #include <algorithm>
