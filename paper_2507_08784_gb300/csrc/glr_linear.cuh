@@ -40,6 +40,7 @@ TcPlan tc_plan(const Product& p);
 cudaError_t tc_product(const Product& p, const TcPlan& plan, void* workspace, cudaStream_t st);
 // Any strides, sizes, alignment and types, without workspace (k_linear.cu).
 cudaError_t any_product(const Product& p, cudaStream_t st);
+double any_cost(const Product& p);              // its time, us (measured fit)
 // The one of the two that the sizes, the alignment and the workspace given call for.
 cudaError_t product(const Product& p, void* workspace, int64_t workspace_bytes, cudaStream_t st);
 

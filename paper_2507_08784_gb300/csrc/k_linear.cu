@@ -462,6 +462,16 @@ cudaError_t launch_clusters(void (*kernel)(Q...), dim3 grid, int threads, int sp
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
+int64_t any_tiles(const Product& p) { return ((p.M + kTile - 1) / kTile) * ((p.N + kTile - 1) / kTile); }
+int any_splits(const Product& p) {
+    // CTAs a tile: as many as fill the SMs, as long as each keeps two slabs (100 x 300 x 200 fp32 31 -> 15 us; 64 x 64 over 2000
+    // rows 136 -> 23)
+    const int64_t slabs = (p.K + kSlab - 1) / kSlab;
+    int splits = 1;
+    while (splits < 8 && any_tiles(p) * p.nodes * splits < 152 && slabs >= 4 * splits) splits *= 2;
+    return splits;
+}
+
 // Sixteen-byte loads: the base, the row stride and the nodes' stride on 16 bytes.
 bool wide_ok(const void* base, int64_t row_stride, int64_t node_stride, int64_t esize) {
     return reinterpret_cast<uintptr_t>(base) % 16 == 0 && row_stride * esize % 16 == 0 && node_stride * esize % 16 == 0;
@@ -488,14 +498,18 @@ cudaError_t any_product(const Product& p, cudaStream_t st) {
     const int64_t tiles = ((p.M + kTile - 1) / kTile) * ((p.N + kTile - 1) / kTile);
     if (tiles > 0x7fffffff) return cudaErrorInvalidValue;
     const bool wa = wide_ok(p.A, p.sAp == 1 ? p.sAi : p.sAp, p.sAb, es), wb = wide_ok(p.B, p.sBp == 1 ? p.sBj : p.sBp, p.sBb, es);
-    // CTAs a tile: as many as fill the SMs, as long as each keeps two slabs (100 x 300 x 200 fp32 31 -> 15 us; 64 x 64 over 2000
-    // rows 136 -> 23)
-    const int64_t slabs = (p.K + kSlab - 1) / kSlab;
-    int splits = 1;
-    while (splits < 8 && tiles * p.nodes * splits < 152 && slabs >= 4 * splits) splits *= 2;
+    const int splits = any_splits(p);
     const dim3 grid(static_cast<unsigned>(tiles), splits, p.nodes);
     return p.dtype == GLR_BF16 ? launch_clusters(product_kernel<__nv_bfloat16>, grid, kThreads, splits, st, p, wa, wb)
                                : launch_clusters(product_kernel<float>, grid, kThreads, splits, st, p, wa, wb);
+}
+
+// Waves of two CTAs an SM; a slab a CTA takes about 2 us, an epilogue 4 (bf16) or 7.
+double any_cost(const Product& p) {
+    const int splits = any_splits(p);
+    const int64_t ctas = any_tiles(p) * p.nodes * splits, slabs = (p.K + kSlab - 1) / kSlab;
+    const double waves = static_cast<double>((ctas + 303) / 304), mine = static_cast<double>((slabs + splits - 1) / splits);
+    return 3 + waves * (p.dtype == GLR_BF16 ? 4 + 2.0 * mine : 7 + 2.4 * mine);
 }
 
 cudaError_t column_sums(const ColumnSums& c, cudaStream_t st) {

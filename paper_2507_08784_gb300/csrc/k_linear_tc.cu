@@ -879,6 +879,29 @@ cudaError_t pack(const PackArgs& a, int jobs, cudaStream_t st) {
     return launch_chain(pack_kernel<T>, dim3(static_cast<unsigned>(std::min<int64_t>(blocks, 152 * 16)), jobs), kPackThreads, 0, st, a);
 }
 
+int64_t big_tiles(const Product& p) { return ((p.M + 255) / 256) * ((p.N + 255) / 256) * p.nodes; }
+int64_t small_tiles(const Product& p) { return ((p.M + 127) / 128) * ((p.N + kSplitN - 1) / kSplitN) * p.nodes; }
+// One of three, by the cycles it takes (measured; a stage is a slab, or one of an fp32 slab's six products).
+// 256 x 256 tiles, one after the other on every pair: 530 a stage, 650 with promoted sums.  The same tiles, two
+// pairs sharing a contraction: 670 a stage, and more to begin and end with; 36 such clusters run at once on 152 SMs
+// (four pairs to a tile: too few clusters at once, never the fastest).  128 x 64 tiles shared by one to eight CTAs: 420 a
+// stage, 620 with two on an SM.  400 x 4096 x 4096 fp32: 176, 114 and 157 us; 1000 x 11008 x 2048 bf16: 56, 48 and 66; 200 x
+// 4096 x 4096 bf16: 27, 27 and 23; 24 rows: 27, 25 and 19.
+struct Choice { int splits; bool paired; int64_t cycles; };
+Choice choose(const Product& p, int64_t slabs, bool promote, int sms) {
+    const int64_t big = big_tiles(p), small = small_tiles(p), pairs = sms / 2;
+    const auto waves = [](int64_t n, int64_t at_once) { return (n + at_once - 1) / at_once; };
+    int64_t best = 4000 + waves(big, pairs) * slabs * (promote ? 650 : 530);
+    int splits = 0;
+    bool paired = false;
+    if (const int64_t t = 26000 + waves(big, sms * 36 / 152) * (slabs + 1) / 2 * 670; t < best && slabs >= 8) { best = t; splits = 2; paired = true; }
+    for (int q = 1; q <= 8 && (q == 1 || slabs >= 4 * q); q *= 2) {
+        const int64_t t = 2000 + waves(small * q, 2 * sms) * (6000 + waves(slabs, q) * (small * q > sms ? 620 : 420));
+        if (t < best) { best = t; splits = q; paired = false; }
+    }
+    return {splits, paired, best};
+}
+
 // Whether an operand's rows lie on 16 bytes as they are.
 bool lies_well(const void* x, int64_t si, int64_t sp, int64_t sb, int64_t ni, int64_t np, int nodes) {
     const int64_t ld = sp == 1 ? si : sp, rows = sp == 1 ? ni : np;
@@ -899,12 +922,21 @@ TcPlan tc_plan(const Product& p) {
     const Storage a = storage(p.sAi, p.sAp, p.M, p.K, p.nodes), b = storage(p.sBj, p.sBp, p.N, p.K, p.nodes);
     if (t.pack_a) t.bytes_a = (t.planes * a.rows * up8(a.cols) * 2 + 255) / 256 * 256;
     if (t.pack_b) t.bytes_b = t.planes * b.rows * up8(b.cols) * 2;
-    // Packing reads the matrices once more, in a launch of its own.  any_product, the other way, takes about 2 us for every 32
-    // contraction elements of a CTA: bf16 rows off 16 bytes, 3 x 4096 x 4096 81 us unpacked, 48 packed, 128 x 1500 x 1500
-    // 38 and 19, 64 x 500 x 500 13 and 17; fp32 16 x 4096 x 4096 91 and 74, but three rows 89 and 142; 1000 x 500 x 500 29
-    // and 25, 128 x 500 x 500 13 and 17.
+    if (!t.pack_a && !t.pack_b) {
+        t.ok = true;
+        return t;
+    }
+    // Packing reads and writes the matrices once more, in a launch of its own (2 us for a million fp32 elements, 0.9 for
+    // bf16); any_product does without.  Both times are estimated.  Rows off 16 bytes, bf16: 3 x 4096 x 4096 81 us unpacked,
+    // 48 packed, 128 x 1500 x 1500 38 and 19, 64 x 500 x 500 13 and 17; fp32: 16 x 4096 x 4096 91 and 74, 300 x 1500 x
+    // 1500 58 and 33, 32 x 8000 x 1000 44 and 52; fewer fp32 rows stay unpacked (three of 4096 x 4096 89 and 142: the few
+    // lines of their planes are read by all SMs at once).
     const double flops = 2.0 * static_cast<double>(p.M) * static_cast<double>(p.N) * static_cast<double>(p.K) * p.nodes;
-    t.ok = !(t.pack_a || t.pack_b) || (flops >= 5e7 && (t.planes == 1 || p.M >= 16));
+    if (flops < 1e7 || (t.planes == 3 && p.M < 16)) return t;
+    const int64_t slabs = (p.K + kSlab - 1) / kSlab * (t.planes == 3 ? 6 : 1);
+    const double elements = (t.pack_a ? static_cast<double>(a.rows) * a.cols : 0.0) + (t.pack_b ? static_cast<double>(b.rows) * b.cols : 0.0);
+    const double packed = (t.planes == 3 ? 13 + 2e-6 * elements : 11 + 9e-7 * elements) + choose(p, slabs, p.out_dtype == GLR_F32, 152).cycles / 1870.0;
+    t.ok = packed < any_cost(p);
     return t;
 }
 
@@ -936,24 +968,11 @@ cudaError_t tc_product(const Product& p, const TcPlan& plan, void* workspace, cu
     const int64_t slabs = (p.K + kSlab - 1) / kSlab * (plan.planes == 3 ? 6 : 1);
     if (slabs > (1 << 30)) return cudaErrorInvalidValue;
     a.slabs = static_cast<int>(slabs);
-    const int64_t big = ((p.M + 255) / 256) * ((p.N + 255) / 256) * p.nodes, pairs = sms / 2;
-    const int64_t small = ((p.M + 127) / 128) * ((p.N + kSplitN - 1) / kSplitN) * p.nodes;
+    const Choice how = choose(p, slabs, promote, sms);
+    const int64_t big = big_tiles(p), small = small_tiles(p), pairs = sms / 2;
     if (std::max(big, small) > (1 << 30)) return cudaErrorInvalidValue;
-    // One of three, by the cycles it takes (measured; a stage is a slab, or one of an fp32 slab's six products).
-    // 256 x 256 tiles, one after the other on every pair: 530 a stage, 650 with promoted sums.  The same tiles, two
-    // pairs sharing a contraction: 670 a stage, and more to begin and end with; 36 such clusters run at once on 152 SMs
-    // (four pairs to a tile: too few clusters at once, never the fastest).  128 x 64 tiles shared by one to eight CTAs: 420 a
-    // stage, 620 with two on an SM.  400 x 4096 x 4096 fp32: 176, 114 and 157 us; 1000 x 11008 x 2048 bf16: 56, 48 and 66; 200 x
-    // 4096 x 4096 bf16: 27, 27 and 23; 24 rows: 27, 25 and 19.
-    const auto waves = [](int64_t n, int64_t at_once) { return (n + at_once - 1) / at_once; };
-    int64_t best = 4000 + waves(big, pairs) * slabs * (promote ? 650 : 530);
-    int splits = 0;
-    bool paired = false;
-    if (const int64_t t = 26000 + waves(big, sms * 36 / 152) * (slabs + 1) / 2 * 670; t < best && slabs >= 8) { best = t; splits = 2; paired = true; }
-    for (int q = 1; q <= 8 && (q == 1 || slabs >= 4 * q); q *= 2) {
-        const int64_t t = 2000 + waves(small * q, 2 * sms) * (6000 + waves(slabs, q) * (small * q > sms ? 620 : 420));
-        if (t < best) { best = t; splits = q; paired = false; }
-    }
+    const int splits = how.splits;
+    const bool paired = how.paired;
     const int bm = splits && !paired ? 128 : 256, bn = splits && !paired ? kSplitN : 256;
     a.tiles_m = static_cast<int>((p.M + bm - 1) / bm);
     a.tiles_n = static_cast<int>((p.N + bn - 1) / bn);

@@ -35,7 +35,7 @@ def _mat(x: Optional[torch.Tensor], name: str, rows: int, cols: int, dtype=None)
     """Address and row stride of a rows x cols matrix argument (None: absent)."""
     if x is None:
         return None, 0
-    if x.dim() != 2 or x.shape[0] != rows or x.shape[1] != cols:
+    if x.shape != (rows, cols):
         raise ValueError(f"{name} must be {rows} x {cols}, got {tuple(x.shape)}")
     if not x.is_cuda or (dtype is not None and x.dtype != dtype):
         raise ValueError(f"{name} must be a CUDA tensor" + ("" if dtype is None else f" of {dtype}"))
@@ -72,7 +72,7 @@ def _call(fn, args, stream) -> None:
 def _space(args, query, x: torch.Tensor, work: float, ragged: int, stream):
     """The workspace that a product asks for (float32 or rows off 16 bytes, where it is large), from PyTorch's
     allocator in the stream's own pool: its memory is reused in the order of the work that runs there."""
-    if (x.dtype == torch.bfloat16 and not ragged) or work < 5e7:
+    if (x.dtype == torch.bfloat16 and not ragged) or work < 1e7:
         return None
     need = ctypes.c_int64(0)
     _check(query(ctypes.byref(args), ctypes.byref(need)))
