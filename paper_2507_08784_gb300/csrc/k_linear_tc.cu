@@ -5,15 +5,15 @@
 // ones into three bf16 planes x = hi + mid + lo (24 bits): their product is the sum of the six plane products
 // above 2^-24, one after the other in the same accumulator.
 //
-// tc_product_kernel, persistent: a CTA (CG = 1) or a pair of CTAs on two SMs (CG = 2) takes 128 CG x BN output
-// tiles in turn.  Two warps copy operand slabs of 64 contraction elements (128-byte swizzle) into a ring of
-// shared-memory stages, one thread issues tcgen05.mma.kind::f16 (of the pair's first CTA: each CTA holds its
-// 128 rows of A and half of B's, and the result's rows stay in their CTA's tensor memory), and eight warps
-// bring the finished accumulator through the epilogue while the next tile's products run into the other half
-// of tensor memory.  Stages are handed over on mbarriers; every wait is bounded: a CTA that gives up counts
-// the event, lets its copies land, frees tensor memory and returns.
-// tc_split_kernel, for few tiles: a cluster of up to eight CTAs shares a 128 x 64 tile's contraction, and adds
-// its partial tiles over distributed shared memory in the order of the contraction.
+// tc_product_kernel, persistent: a pair of CTAs on two SMs takes 256 x 256 output tiles in turn.  Two warps of each copy
+// operand slabs of 64 contraction elements (128-byte swizzle) into a ring of shared-memory stages, one thread of the
+// pair's first CTA issues tcgen05.mma.kind::f16 (each CTA holds its 128 rows of A and half of B's, and the result's rows
+// stay in their CTA's tensor memory), and eight warps (sixteen for fp32 results) bring the finished accumulator through the
+// epilogue while the next tile's products run into the other half of tensor memory.  Stages are handed over on mbarriers;
+// every wait is bounded: a CTA that gives up counts the event, lets its copies land, frees tensor memory and returns.
+// tc_split_kernel, for few tiles: a cluster of up to eight CTAs shares a 128 x 64 tile's contraction (CG = 1), or two pairs
+// a 256 x 256 one's (CG = 2), and they add their partial tiles over distributed shared memory in the order of the
+// contraction.
 //
 // The tensor cores truncate their fp32 sums (about 2^-25 of the sum for every 16 elements, always the same
 // way), which over a long contraction is far above fp32 rounding: where the result is fp32 (PROMOTE), and in

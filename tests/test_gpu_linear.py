@@ -415,3 +415,36 @@ def test_c_entries_without_workspace(rows, n, k, dt, pad):
         _check(got, a @ b.T, _sum_tol(a, b, a.shape[1], dt), dt)
     assert _untouched(ybuf, Y) and _untouched(dbuf, D)
     glr.glr_operator_status()
+
+
+@pytest.mark.parametrize("pad", [0, 1])
+def test_matrices_past_32_bits_of_elements(pad):
+    """70000 x 32768: as the input, as the input's gradient, as the weights of one row and as the weights' gradient."""
+    import paper_2507_08784_gb300 as glr
+    rows, k, n, dt = 70000, 32768, 24, torch.bfloat16
+    big = torch.empty(rows, k + pad, device="cuda", dtype=dt).normal_()[:, :k]
+    W, Z = torch.randn(n, k, device="cuda").to(dt), torch.randn(rows, n, device="cuda").to(dt)
+    at = torch.tensor([0, 1, 32767, 32768, 65535, 65536, 69999], device="cuda")
+
+    def close(got, a, b, k):
+        want, size = a @ b.T, a.abs() @ b.abs().T
+        assert ((got.double() - want).abs() <= (k + 8) * 2.0 ** -23 * size + 2.0 ** -8 * want.abs()).all()
+
+    Y = torch.empty(rows, n, device="cuda", dtype=dt)
+    glr.glr_linear(big, W, Y)
+    close(Y[at], big[at].double(), W.double(), k)
+    y = torch.empty(1, rows, device="cuda", dtype=dt)
+    glr.glr_linear(W[:1], big, y)
+    close(y[:, at], W[:1].double(), big[at].double(), k)
+    dW = torch.empty(n, k, device="cuda", dtype=dt)
+    glr.glr_linear_grad_weight(Z, big, dW)
+    close(dW[:, at % k], Z.double().T, big[:, at % k].double().T, rows)
+    out = torch.full((rows, k + pad), 7.0, device="cuda", dtype=dt)
+    glr.glr_linear_grad_input(Z, W, out[:, :k])
+    close(out[at, :k], Z[at].double(), W.double().T, n)
+    assert pad == 0 or bool((out[:, k:] == 7).all())
+    del out
+    G = torch.empty(rows, k, device="cuda", dtype=dt)
+    glr.glr_linear_grad_weight(Z.T[:8].contiguous(), W[:8].contiguous(), G)
+    close(G[at], Z.T[:8, at].double().T, W[:8].double().T, 8)
+    glr.glr_operator_status()
