@@ -271,9 +271,11 @@ __device__ __forceinline__ void widen(const uint4& u, float (&f)[8], const __nv_
 __device__ __forceinline__ void widen(const uint4& u, float (&f)[4], const float*) {
     f[0] = __uint_as_float(u.x); f[1] = __uint_as_float(u.y); f[2] = __uint_as_float(u.z); f[3] = __uint_as_float(u.w);
 }
+// Sixteen bytes past the L1.  Volatile and clobbering memory, which keeps it behind chain_begin's wait: the kernel before
+// may be writing these matrices until then, and for the same reason they are not read as constant data (.nc, __ldg).
 __device__ __forceinline__ uint4 load_once(const uint4* p) {
     uint4 u;
-    asm("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p) : "memory");
     return u;
 }
 template <class T, int R>
@@ -308,7 +310,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, 2) rows_kernel(const __grid_c
     ask(v);
     for (; v < nv; v += U * step) {
         uint4 now[U][C], row[U][EARLY ? R : 1];
-        auto row_at = [&](int u, int r) { return v + u * step < nv ? __ldg(a[r] + v + u * step) : uint4{0, 0, 0, 0}; };
+        auto row_at = [&](int u, int r) { return v + u * step < nv ? a[r][v + u * step] : uint4{0, 0, 0, 0}; };
 #pragma unroll
         for (int u = 0; u < U; ++u) {
 #pragma unroll
