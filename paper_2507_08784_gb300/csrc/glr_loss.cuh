@@ -15,6 +15,10 @@ struct Index {
     }
 };
 
+// A row of the preference loss between its passes: its maximum, log2 of the sum of exp(z - maximum) (+infinity: the row does
+// not count), and the factor of its gradient.
+struct __align__(16) RowSum { float top, log2_sum, coef, unused; };
+
 enum Kind : int { kDistill = 0, kPolicy = 1, kLogProb = 2 };
 
 struct RowArgs {
@@ -35,8 +39,7 @@ struct RowArgs {
     const float* old_logp; const float* advantage; const float* ref_logp;
     float clip_lo, clip_hi, kl;             // 1 - clip_low, 1 + clip_high
     float* logp;
-    // log-probability pass: the row's log sum exp (+infinity: the row does not count) and a zero
-    float* lse; float* coef;
+    RowSum* sums;                           // log-probability pass: one a row
     int* err;
     int cluster_shift, slots, lists; uint32_t slot_bytes;    // set by the launcher
 };
@@ -44,19 +47,19 @@ struct RowArgs {
 struct PairArgs {
     int64_t rows, pairs;
     Index offsets;
-    const float* row_logp; const float* lse; const float* ref_logp; const float* weight;
+    const float* row_logp; RowSum* sums; const float* ref_logp; const float* weight;
     float share, beta, smoothing;
     int kind, average;
-    float* pair_loss; float* seq_logp; float* coef;
+    float* pair_loss; float* seq_logp;
 };
 
 cudaError_t distill(const RowArgs& a, int dtype, cudaStream_t st);
 cudaError_t policy(const RowArgs& a, int dtype, cudaStream_t st);
-// row_logp (a.logp), a.lse and a.coef = 0 of every row
+// row_logp (a.logp) and a.sums of every row, with coefficients of 0
 cudaError_t log_prob(const RowArgs& a, int dtype, cudaStream_t st);
-// pair losses, sequence sums, and coef[t] = d loss / d row_logp[t]
+// pair losses, sequence sums, and sums[t].coef = d loss / d row_logp[t]
 cudaError_t pairs(const PairArgs& a, cudaStream_t st);
-// dz_t = coef[t] (e_token - exp(z - lse[t]))
+// dz_t = coef (e_token - exp2((z - top) log2 e - log2_sum))
 cudaError_t log_prob_grad(const RowArgs& a, int dtype, cudaStream_t st);
 // *out = sum_t w_t x_t in a fixed order, w_t = weight[t] or share; entries of weight 0 add nothing
 cudaError_t total(const float* x, const float* weight, float share, int64_t n, float* out, cudaStream_t st);

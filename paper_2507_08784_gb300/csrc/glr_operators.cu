@@ -309,12 +309,11 @@ extern "C" int glr_preference_loss(const glr_preference_args* a, void* stream) {
     r.inv_tau = 1.f;
     r.tokens = {a->tokens, a->tokens_index64};
     r.logp = a->row_logp;
-    r.lse = static_cast<float*>(a->workspace);
-    r.coef = r.lse + a->rows;
+    r.sums = static_cast<loss::RowSum*>(a->workspace);
     if (!(r.err = gave_up_counter())) return launched(who, cudaErrorNoDevice);
     loss::PairArgs p{};
     p.rows = a->rows; p.pairs = a->pairs; p.offsets = {a->offsets, a->offsets_index64};
-    p.row_logp = r.logp; p.lse = r.lse; p.coef = r.coef; p.ref_logp = a->ref_logp; p.weight = a->weight;
+    p.row_logp = r.logp; p.sums = r.sums; p.ref_logp = a->ref_logp; p.weight = a->weight;
     p.share = a->pairs ? static_cast<float>(1.0 / static_cast<double>(a->pairs)) : 0.f;
     p.beta = a->beta; p.smoothing = a->smoothing; p.kind = a->kind; p.average = a->average;
     p.pair_loss = a->pair_loss; p.seq_logp = a->seq_logp;

@@ -656,8 +656,7 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
                 if (K == kPolicy) {
                     a.row_loss[row] = k.loss;
                 } else {
-                    a.lse[row] = counts ? st.m + log_fast(st.s) : CUDART_INF_F;
-                    a.coef[row] = 0.f;
+                    a.sums[row] = RowSum{st.m, counts ? log2f(st.s) : CUDART_INF_F, 0.f, 0.f};
                 }
             }
             // ---- 4
@@ -940,7 +939,7 @@ __global__ void __launch_bounds__(kPairThreads) pairs_kernel(const PairArgs a) {
         int cnt = 0;
         for (int64_t t = b + threadIdx.x; t < e; t += kPairThreads) {
             sum = plus(sum, Pair{a.row_logp[t], 0.f});
-            cnt += a.lse[t] != CUDART_INF_F;
+            cnt += a.sums[t].log2_sum != CUDART_INF_F;
         }
         sum = block_sum(sum, scratch);
         share[h] = 1.f;
@@ -974,7 +973,7 @@ __global__ void __launch_bounds__(kPairThreads) pairs_kernel(const PairArgs a) {
     for (int s = 0; s < 2; ++s) {
         const float coef = w == 0.f ? 0.f : (s ? -slope : slope) * w * share[s];
         for (int64_t t = at[s][0] + threadIdx.x; t < at[s][1]; t += kPairThreads)
-            if (a.lse[t] != CUDART_INF_F) a.coef[t] = coef;
+            if (a.sums[t].log2_sum != CUDART_INF_F) a.sums[t].coef = coef;
     }
 }
 
@@ -988,8 +987,9 @@ __device__ __forceinline__ void store_last(void* p, const uint4& u) {
     asm volatile("st.global.cs.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(u.x), "r"(u.y), "r"(u.z), "r"(u.w) : "memory");
 }
 
-// dz = coef (e_token - exp(z - lse)): the second pass over a preference batch's rows (its factor needs the whole pair
-// first), a piece of a row a CTA.  Rows are taken from the last one back: the sums' pass ended there, and the L2 still
+// dz = coef (e_token - exp2((z - m) log2 e - log2 s)): the second pass over a preference batch's rows (its factor needs the
+// whole pair first), a piece of a row a CTA.  m and log2 s come apart from the first pass: their sum would lose the
+// latter beside an m of 1e5, and all of it at the type's lowest value.  Rows are taken from the last one back: the sums' pass ended there, and the L2 still
 // holds some 100 MB of it.  Bound by HBM: one read, one write (8 pairs of 2 x 512 rows of 32768 bf16: 225 us with the
 // sums' pass, 4.2 TB/s of one read and one write, 6.0 of the two reads that it makes).
 constexpr int kPieceVecs = 4;
@@ -1001,11 +1001,12 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const RowArgs a, int pie
     const int piece = static_cast<int>(blockIdx.x % pieces), V = static_cast<int>(a.vocab), tid = threadIdx.x;
     const T* z = static_cast<const T*>(a.z) + row * a.ldz;
     T* dz = static_cast<T*>(a.dz) + row * a.lddz;
-    const float coef = a.coef[row], lse = a.lse[row];
+    const RowSum sum = a.sums[row];
+    const float coef = sum.coef, m = sum.top, ls = sum.log2_sum;
     const int32_t tok = index_of(word_at(a.tokens, row), a.tokens.wide, V);
     const bool zero = coef == 0.f;
     auto at = [&](float x, int v) {
-        const float g = -coef * exp2_fast((x - lse) * kLog2e);
+        const float g = -coef * exp2_fast(fmaf(x - m, kLog2e, -ls));
         return v == tok ? g + coef : g;
     };
     const Span sp = span_of(z, V, 0, 0);
@@ -1021,7 +1022,7 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const RowArgs a, int pie
         for (int q = 0; q < kPieceVecs; ++q)
             if (v0 + q * kThreads < sp.nv) u[q] = load_last(z + sp.head + static_cast<int64_t>(v0 + q * kThreads) * E);
     }
-    const uint64_t nl = pack2(-lse, -lse), l2 = pack2(kLog2e, kLog2e), nc = pack2(-coef, -coef);
+    const uint64_t nm = pack2(-m, -m), nl = pack2(-ls, -ls), l2 = pack2(kLog2e, kLog2e), nc = pack2(-coef, -coef);
 #pragma unroll
     for (int q = 0; q < kPieceVecs; ++q) {
         const int v = v0 + q * kThreads, b = tok - sp.head - v * E;
@@ -1031,7 +1032,7 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const RowArgs a, int pie
             uint64_t x[P];
             Vec<T>::get(u[q], x);
 #pragma unroll
-            for (int i = 0; i < P; ++i) x[i] = mul2(nc, exp2_2(mul2(add2(x[i], nl), l2)));
+            for (int i = 0; i < P; ++i) x[i] = mul2(nc, exp2_2(fma2(add2(x[i], nm), l2, nl)));
             if (tok >= 0 && b >= 0 && b < E) {
 #pragma unroll
                 for (int i = 0; i < P; ++i) x[i] = add2(x[i], pack2(b == 2 * i ? coef : 0.f, b == 2 * i + 1 ? coef : 0.f));

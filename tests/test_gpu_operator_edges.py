@@ -1,7 +1,12 @@
 """The operators around the step at the edges of what they promise: kernels that read what the one before them wrote,
 the ends of the floating-point range, terms without a coefficient (marked gpu)."""
+import math
+
 import pytest
 import torch
+
+import _operators as ref
+from test_gpu_losses import _check_grad, _close, _dprob, _run_distill, _run_policy, _run_preference
 
 pytestmark = pytest.mark.gpu
 DT = {"f32": torch.float32, "bf16": torch.bfloat16}
@@ -44,3 +49,33 @@ def test_kernels_read_what_the_one_before_wrote(rows, dt):
 
     for (want_out, want_dw, want_db), (dw, db) in zip(run(True), run(False)):
         assert torch.equal(dw, want_dw) and torch.equal(db, want_db) and want_out.any()
+
+
+# ---------------------------------------------------------------------------------------- preference, far from zero
+
+@pytest.mark.parametrize("vocab", [777, 32769])
+@pytest.mark.parametrize("offset", [0.0, 1e4, 1e6])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_preference_gradient_of_logits_far_from_zero(vocab, offset, dt):
+    """Logits with a common offset, and rows that hold the type's lowest value throughout or but for one entry:
+    everything is a function of z - max z, so the tolerances are those of the logits' span, as for the other losses."""
+    dt = DT[dt]
+    gen = torch.Generator().manual_seed(41)
+    lengths = [4, 7, 1, 5]
+    rows = sum(lengths)
+    z = (3 * torch.randn(rows, vocab, generator=gen) + offset).to(dt)
+    span = max(float(x.max() - x.min()) for x in z.float())
+    z[2] = z[13] = torch.finfo(dt).min
+    z[6] = torch.finfo(dt).min
+    z[6, 5] = offset
+    tokens = torch.randint(0, vocab, (rows,), generator=gen)
+    tokens[6] = 5
+    offsets = torch.tensor([0] + lengths).cumsum(0)
+    want = ref.preference(z, tokens, offsets, None, None, "sigmoid", 0.1, 0.1, False)
+    loss, pair, seq, row, d = _run_preference(z.cuda(), tokens.cuda(), offsets.cuda(), None, None, "sigmoid", 0.1, 0.1)
+    rel = 2.0 ** -19 + 2.0 ** -22 * span
+    _close(row, want[3], 4 * rel)
+    _close(seq, want[2], 4 * rel)
+    grad_rel = rel + 0.1 * 4 * rel * (2 + 2 * float(want[2].abs().max()))
+    biggest = want[4].abs().max(1, keepdim=True).values
+    _check_grad(d, want[4], grad_rel, dt, biggest * (_dprob(z) + (want[4].abs() == biggest)))
