@@ -959,9 +959,11 @@ __global__ void __launch_bounds__(kPairThreads) pairs_kernel(const PairArgs a) {
         loss = e * e;
         slope = 2.f * e;
     } else {
-        // -log sigmoid(x) = max(-x, 0) + log1p(exp(-|x|))
+        // -log sigmoid(x) = max(-x, 0) + log1p(exp(-|x|)); a term whose share is 0 is left out: it may be infinite
         const float x = a.beta * h, t = log1pf(expf(-fabsf(x)));
-        loss = (1.f - a.smoothing) * (fmaxf(-x, 0.f) + t) + a.smoothing * (fmaxf(x, 0.f) + t);
+        loss = 0.f;
+        if (a.smoothing != 1.f) loss = (1.f - a.smoothing) * (fmaxf(-x, 0.f) + t);
+        if (a.smoothing != 0.f) loss += a.smoothing * (fmaxf(x, 0.f) + t);
         if (isnan(x)) loss = x;
         slope = a.beta * (a.smoothing / (1.f + expf(-x)) - (1.f - a.smoothing) / (1.f + expf(x)));
     }

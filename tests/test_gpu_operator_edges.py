@@ -79,3 +79,27 @@ def test_preference_gradient_of_logits_far_from_zero(vocab, offset, dt):
     grad_rel = rel + 0.1 * 4 * rel * (2 + 2 * float(want[2].abs().max()))
     biggest = want[4].abs().max(1, keepdim=True).values
     _check_grad(d, want[4], grad_rel, dt, biggest * (_dprob(z) + (want[4].abs() == biggest)))
+
+
+# ------------------------------------------------------------------------------- terms without a coefficient: preference
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_preference_of_a_ruled_out_answer(dt):
+    """A rejected answer with a token of logit -infinity is infinitely far behind: -log sigmoid(infinity) = 0 without
+    smoothing, and its mirror image with the smoothing at 1.  With both terms the loss is infinite."""
+    dt = DT[dt]
+    gen = torch.Generator().manual_seed(42)
+    tokens, offsets = torch.randint(0, 300, (16,), generator=gen), torch.tensor([0, 4, 8, 12, 16])
+    for smoothing, answer in ((0.0, 1), (1.0, 0), (0.1, 1)):
+        z = torch.randn(16, 300, generator=gen).to(dt)
+        banned = 4 * answer + 2
+        z[banned, tokens[banned]] = -math.inf
+        other = ref.preference(z[8:], tokens[8:], torch.tensor([0, 4, 8]), None, None, "sigmoid", 0.1, smoothing, False)
+        loss, pair, _, _, d = _run_preference(z.cuda(), tokens.cuda(), offsets.cuda(), None, None, "sigmoid", 0.1, smoothing)
+        if smoothing == 0.1:
+            assert float(pair[0]) == math.inf and float(loss) == math.inf
+            continue
+        assert float(pair[0]) == 0.0 and not d[:8].any()
+        _close(pair[1:], other[1], 2.0 ** -15)
+        _close(loss, other[0] / 2, 2.0 ** -15)
+        _check_grad(d[8:], other[4] / 2, 2.0 ** -16, dt, other[4].abs() + 1e-2)
