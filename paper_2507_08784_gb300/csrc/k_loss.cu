@@ -635,7 +635,7 @@ __global__ void __launch_bounds__((kWorkers + 2) * 32) rows_kernel(const __grid_
             if (st.s == 0.f) counts = false;
             const Coef k = coef_of<K, TWO>(a, now, st, pub, counts);
             if (D) {
-                const bool soft = counts && pub.soft;
+                const bool soft = counts && pub.soft && a.soft != 0.f;    // (the divergence may be infinite)
                 float zq = 0.f;
                 if (soft) {
 #pragma unroll 1

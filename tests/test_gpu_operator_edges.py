@@ -103,3 +103,27 @@ def test_preference_of_a_ruled_out_answer(dt):
         _close(pair[1:], other[1], 2.0 ** -15)
         _close(loss, other[0] / 2, 2.0 ** -15)
         _check_grad(d[8:], other[4] / 2, 2.0 ** -16, dt, other[4].abs() + 1e-2)
+
+
+# ----------------------------------------------------------------------------- terms without a coefficient: distillation
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("topk", [3, 100])
+def test_distillation_without_the_soft_term(dt, topk):
+    """soft = 0 and a teacher's entry that the student rules out (their divergence is infinite): the hard term alone."""
+    dt = DT[dt]
+    gen = torch.Generator().manual_seed(43)
+    z = torch.randn(5, 500, generator=gen).to(dt)
+    ids, teacher = torch.randint(0, 250, (5, topk), generator=gen), torch.randn(5, topk, generator=gen)
+    labels = torch.randint(250, 500, (5,), generator=gen)
+    z[torch.arange(5), ids[:, 1]] = -math.inf
+    for tau in (1.0, 2.0, 3.0):
+        lp = torch.log_softmax(z.double(), 1)
+        want = -0.5 * lp.gather(1, labels[:, None])[:, 0]
+        grad = 0.1 * lp.exp()
+        grad[torch.arange(5), labels] -= 0.1
+        loss, row, d = _run_distill(z.cuda(), teacher.cuda(), ids.cuda(), labels.cuda(), None, tau, 0.0, 0.5)
+        _close(row, want, 2.0 ** -16)
+        _close(loss, want.mean(), 2.0 ** -16)
+        _check_grad(d, grad, 2.0 ** -16, dt, grad.abs())
+        assert float(_run_distill(z.cuda(), teacher.cuda(), ids.cuda(), labels.cuda(), None, tau, 1.0, 0.5)[1].min()) == math.inf
