@@ -279,10 +279,11 @@ __device__ __forceinline__ Coef coef_of(const RowArgs& a, const Row& r, const St
     k.lp = (pub.zt - st.m) * a.inv_tau - log_fast(st.s);
     if (K == kPolicy) {
         const float A = r.adv, ratio = exp2_fast((k.lp - r.old) * kLog2e);
-        k.loss = -fminf(ratio * A, fminf(fmaxf(ratio, a.clip_lo), a.clip_hi) * A);
-        if (isnan(ratio * A)) k.loss = ratio * A;
-        float slope = (A > 0.f ? ratio > a.clip_hi : ratio < a.clip_lo) ? 0.f : -A * ratio;
-        if (a.ref_logp) {
+        const float gain = A == 0.f && ratio == CUDART_INF_F ? 0.f : ratio * A;      // (the ratio may leave the range)
+        k.loss = -fminf(gain, fminf(fmaxf(ratio, a.clip_lo), a.clip_hi) * A);
+        if (isnan(gain)) k.loss = gain;
+        float slope = (A > 0.f ? ratio > a.clip_hi : ratio < a.clip_lo) ? 0.f : -gain;
+        if (a.ref_logp && a.kl != 0.f) {              // (and so may exp(e))
             const float e = expm1f(r.ref - k.lp);
             k.loss += a.kl * (e - (r.ref - k.lp));
             slope -= a.kl * e;

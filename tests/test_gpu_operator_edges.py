@@ -127,3 +127,25 @@ def test_distillation_without_the_soft_term(dt, topk):
         _close(loss, want.mean(), 2.0 ** -16)
         _check_grad(d, grad, 2.0 ** -16, dt, grad.abs())
         assert float(_run_distill(z.cuda(), teacher.cuda(), ids.cuda(), labels.cuda(), None, tau, 1.0, 0.5)[1].min()) == math.inf
+
+
+# ----------------------------------------------------------------------------------- terms without a coefficient: policy
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_policy_terms_without_a_coefficient(dt):
+    """kl = 0 where exp(ref - logp) leaves the range, and an advantage of 0 where the ratio does: nothing of either."""
+    dt = DT[dt]
+    gen = torch.Generator().manual_seed(44)
+    z = torch.randn(6, 400, generator=gen).to(dt)
+    tokens, adv = torch.randint(0, 400, (6,), generator=gen).cuda(), torch.randn(6, generator=gen)
+    z[1, tokens[1]] = -160.0
+    z[2, tokens[2]] = -math.inf
+    old, refl = torch.full((6,), -5.0), torch.full((6,), -1.0)
+    a = _run_policy(z.cuda(), tokens, old.cuda(), adv.cuda(), None, None)
+    b = _run_policy(z.cuda(), tokens, old.cuda(), adv.cuda(), refl.cuda(), None, kl=0.0)
+    assert all(torch.isfinite(x).all() for x in (a[0], a[1], a[3]))
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+    adv[3], adv[4], old[3:5] = 0.0, 1.5, -120.0
+    loss, row, _, d = _run_policy(z.cuda(), tokens, old.cuda(), adv.cuda(), None, None, high=0.28)
+    assert float(row[3]) == 0.0 and not d[3:5].any()
+    assert abs(float(row[4]) + 1.28 * 1.5) < 1e-6 and torch.isfinite(loss).all()
