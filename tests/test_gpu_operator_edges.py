@@ -149,3 +149,22 @@ def test_policy_terms_without_a_coefficient(dt):
     loss, row, _, d = _run_policy(z.cuda(), tokens, old.cuda(), adv.cuda(), None, None, high=0.28)
     assert float(row[3]) == 0.0 and not d[3:5].any()
     assert abs(float(row[4]) + 1.28 * 1.5) < 1e-6 and torch.isfinite(loss).all()
+
+
+# --------------------------------------------------------------------------------------------- confident predictions
+
+@pytest.mark.parametrize("kind", ["policy", "distill"])
+def test_losses_of_confident_tokens(kind):
+    """Two fp32 logits d apart, -log p = log1p(exp(-d)): the sum 1 + exp(-d) is rounded once (2^-24) and its logarithm
+    correct to a unit in its last place or two."""
+    gap = torch.linspace(8.0, 16.0, 4096)
+    z = torch.stack([gap, torch.zeros_like(gap)], 1).contiguous()
+    want = torch.log1p(torch.exp(-gap.double()))
+    first, rows = torch.zeros(4096, dtype=torch.int64, device="cuda"), 4096
+    if kind == "policy":
+        zero = torch.zeros(rows, device="cuda")
+        got = -_run_policy(z.cuda(), first, zero, zero + 1, grad=False)[2]
+    else:
+        got = _run_distill(z.cuda(), torch.empty(rows, 0, device="cuda"), torch.empty(rows, 0, device="cuda", dtype=torch.int32), first, None,
+                           1.0, 0.0, 1.0, grad=False)[1]
+    assert ((got.double().cpu() - want).abs() <= 1.05 * 2.0 ** -24 + 2.0 ** -22 * want).all(), float((got.double().cpu() - want).abs().max())
