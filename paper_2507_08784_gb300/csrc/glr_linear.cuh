@@ -54,11 +54,10 @@ struct ColumnSums {
 cudaError_t column_sums(const ColumnSums& c, cudaStream_t st);
 
 // The activations and their slopes (GLR_ACT_*).  FAST, for results that are rounded to bf16: exponentials and
-// quotients by the hardware's approximations (a few 2^-22 relative), tanh u as 1 - 2 / (1 + exp(2 u)).
+// quotients by the hardware's approximations (a few 2^-22 relative, an exponential's more with its argument), tanh u as
+// 1 - 2 / (1 + exp(2 u)).
 template <bool FAST>
 __device__ __forceinline__ float exp_of(float x) { return FAST ? __expf(x) : expf(x); }
-template <bool FAST>
-__device__ __forceinline__ float over(float x, float y) { return FAST ? __fdividef(x, y) : x / y; }
 template <bool FAST>
 __device__ __forceinline__ float tanh_of(float u) {
     // (beyond 40 the quotient's denominator would leave the range of the fast division)
@@ -66,7 +65,10 @@ __device__ __forceinline__ float tanh_of(float u) {
 }
 template <bool FAST>
 __device__ __forceinline__ float sigmoid_of(float z) {
-    return over<FAST>(1.f, 1.f + exp_of<FAST>(FAST ? fminf(-z, 80.f) : -z));
+    if (!FAST) return 1.f / (1.f + expf(-z));
+    // from exp(-|z|): nothing leaves the fast division's range, and the value goes to 0 where exp(z) does
+    const float e = __expf(-fabsf(z));
+    return __fdividef(z >= 0.f ? 1.f : e, 1.f + e);
 }
 template <bool FAST>
 __device__ __forceinline__ float act_value(float z, int act) {

@@ -168,3 +168,48 @@ def test_losses_of_confident_tokens(kind):
         got = _run_distill(z.cuda(), torch.empty(rows, 0, device="cuda"), torch.empty(rows, 0, device="cuda", dtype=torch.int32), first, None,
                            1.0, 0.0, 1.0, grad=False)[1]
     assert ((got.double().cpu() - want).abs() <= 1.05 * 2.0 ** -24 + 2.0 ** -22 * want).all(), float((got.double().cpu() - want).abs().max())
+
+
+# ------------------------------------------------------------------------------------ ends of the range: activations
+
+# few rows; a shared contraction (bf16) or the small products (fp32); whole tiles one after the other; the same laid out first
+PATHS = [(3, 64, 64, 0), (70, 72, 64, 0), (70, 72, 64, 1), (4096, 2048, 256, 0), (4096, 2048, 256, 1)]
+
+
+def _ends(n, dt):
+    m = torch.finfo(dt).max
+    v = torch.tensor([0.0, 100.0, 1e4, 3e18, 3e19, 1e30, 1e36, m], dtype=torch.float64)
+    return torch.cat([v, -v]).to(dt).repeat(-(-n // 16))[:n]
+
+
+def _check_ends(rows, n, k, pad, act, dt):
+    import paper_2507_08784_gb300 as glr
+    dt = DT[dt]
+    z = _ends(n, dt)
+    X, W = torch.zeros(rows, k + pad, device="cuda", dtype=dt)[:, :k], torch.randn(n, k + pad, device="cuda").to(dt)[:, :k]
+    Y, P = torch.empty(rows, n + pad, device="cuda", dtype=dt)[:, :n], torch.empty(rows, n, device="cuda", dtype=dt)
+    glr.glr_linear(X, W, Y, bias=z.cuda(), act=act, preact=P)
+    zd = z.double()
+    want = zd if act == "none" else zd.clamp(min=0)
+    assert torch.equal(P.cpu(), z.expand(rows, n))
+    tol = want.abs() * 2.0 ** -20 + 1e-30
+    assert ((Y.double().cpu() - want).abs() <= tol).all(), (Y[0], want)
+
+    z = _ends(k, dt)
+    D, G = torch.zeros(rows, n + pad, device="cuda", dtype=dt)[:, :n], torch.ones(rows, k, device="cuda", dtype=dt)
+    dX = torch.empty(rows, k + pad, device="cuda", dtype=dt)[:, :k]
+    glr.glr_linear_grad_input(D, W, dX, residual=G, preact=z.cuda().expand(rows, k).contiguous(), act=act)
+    slope = (z.double() > 0).double() if act != "none" else torch.ones(k, dtype=torch.float64)
+    if act in ("gelu", "gelu_tanh", "silu"):
+        slope[z == 0] = 0.5
+    assert ((dX.double().cpu() - slope).abs() <= 2.0 ** -20).all(), (dX[0], slope)
+    glr.glr_operator_status()
+
+
+@pytest.mark.parametrize("rows,n,k,pad", PATHS)
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_activations_at_the_ends_of_the_range(rows, n, k, pad, act, dt):
+    """Pre-activations from 100 to the type's largest, of either sign: an activation is there 0 or the value itself, its
+    slope 0 or 1."""
+    _check_ends(rows, n, k, pad, act, dt)
