@@ -88,7 +88,8 @@ __device__ __forceinline__ float act_slope(float z, int act) {
             return 0.5f * (1.f + erff(z * 0.7071067811865476f)) + z * (0.3989422804014327f * exp_of<FAST>(-0.5f * z * z));
         case GLR_ACT_GELU_TANH: {
             const float t = tanh_of<FAST>(0.7978845608028654f * (z + 0.044715f * z * z * z));
-            return 0.5f * (1.f + t) + 0.5f * z * (1.f - t * t) * 0.7978845608028654f * (1.f + 3.f * 0.044715f * z * z);
+            const float z2 = fminf(z * z, 1e9f);       // (1 - t t is 0 long before)
+            return 0.5f * (1.f + t) + 0.5f * z * (1.f - t * t) * 0.7978845608028654f * (1.f + 3.f * 0.044715f * z2);
         }
         case GLR_ACT_SILU: {
             const float p = sigmoid_of<FAST>(z);

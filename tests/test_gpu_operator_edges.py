@@ -213,3 +213,11 @@ def test_activations_at_the_ends_of_the_range(rows, n, k, pad, act, dt):
     """Pre-activations from 100 to the type's largest, of either sign: an activation is there 0 or the value itself, its
     slope 0 or 1."""
     _check_ends(rows, n, k, pad, act, dt)
+
+
+# --------------------------------------------------------------------------------------------- ends of the range: gelu_tanh
+
+@pytest.mark.parametrize("rows,n,k,pad", PATHS)
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_gelu_tanh_at_the_ends_of_the_range(rows, n, k, pad, dt):
+    _check_ends(rows, n, k, pad, "gelu_tanh", dt)
