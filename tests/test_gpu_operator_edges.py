@@ -221,3 +221,38 @@ def test_activations_at_the_ends_of_the_range(rows, n, k, pad, act, dt):
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_gelu_tanh_at_the_ends_of_the_range(rows, n, k, pad, dt):
     _check_ends(rows, n, k, pad, "gelu_tanh", dt)
+
+
+# ----------------------------------------------------------------------------------------- ends of the range: fp32 products
+
+# rows, outputs and inputs of the three ways of an fp32 product: few rows, small, laid out (a shared contraction, whole tiles)
+FP32_PATHS = [(8, 200, 100), (130, 70, 90), (300, 1200, 1500), (2048, 2048, 512)]
+
+
+def _same_or_close(got, want, tol):
+    got = got.double().cpu()
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    inf = torch.isinf(want)
+    assert torch.equal(torch.isinf(got), inf) and torch.equal(got[inf], want[inf])
+    fin = torch.isfinite(want)
+    assert ((got - want).abs()[fin] <= tol[fin]).all(), float(((got - want).abs() / tol)[fin].max())
+
+
+@pytest.mark.parametrize("rows,n,k", FP32_PATHS)
+def test_extremes_in_fp32_products(rows, n, k):
+    """The type's largest values, of either sign, in single places of X and of W, against factors below 0.4."""
+    import paper_2507_08784_gb300 as glr
+    gen = torch.Generator().manual_seed(rows)
+    X, W = 0.4 * torch.rand(rows, k, generator=gen), 0.4 * torch.rand(n, k, generator=gen)
+    big = torch.finfo(torch.float32).max
+    X[1], W[7] = 0.0, 0.0
+    X[1, 3], X[2, 5], W[6, 11], W[7, 20] = big, -big, -big, big
+    want = X.double() @ W.double().T
+    tol = 2.0 ** -19 * (X.double().abs() @ W.double().abs().T) + 1e-30
+    Y, dX, dW = (torch.empty(rows, n, device="cuda") for _ in range(3))
+    glr.glr_linear(X.cuda(), W.cuda(), Y)
+    glr.glr_linear_grad_input(X.cuda(), W.T.contiguous().cuda(), dX)
+    glr.glr_linear_grad_weight(X.T.contiguous().cuda(), W.T.contiguous().cuda(), dW)
+    for got in (Y, dX, dW):
+        _same_or_close(got, want, tol)
+    glr.glr_operator_status()
