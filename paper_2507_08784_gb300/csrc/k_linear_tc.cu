@@ -749,8 +749,9 @@ __global__ void __launch_bounds__(threads_of(epi_warps(CG == 2)), CG == 2 ? 1 : 
 }
 
 // Rows of `cols` elements, ld apart, as `planes` bf16 matrices in rows of ldp (a multiple of eight), one after the
-// other: x = hi + mid + lo, each the bf16 nearest to what is left.  One or two matrices a launch, eight neighbouring
-// elements a thread, 2 to 256 threads (a power of two) a row.  Bound by HBM.
+// other: x = hi + mid + lo, each the bf16 nearest to what is left; an infinity is 1, 0 and itself, so that it meets the
+// other operand's first plane alone (times a lower one of 0, or of the other sign, an infinity would be NaN).  One or
+// two matrices a launch, eight neighbouring elements a thread, 2 to 256 threads (a power of two) a row.  Bound by HBM.
 constexpr int kPackThreads = 256;
 struct PackJob {
     const void* x; int64_t rows, cols, ld;
@@ -783,18 +784,30 @@ __global__ void __launch_bounds__(kPackThreads) pack_kernel(const __grid_constan
             } else {
                 get8(row, j, n, x.wide, sizeof(T) == 2 ? GLR_BF16 : GLR_F32, v);
             }
+            constexpr float kMost = 3.3895313892515355e38f;      // bf16's largest
+            float most = 0.f;                        // (a NaN needs no care)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[e]));
+            const bool careful = most > kMost;
             for (int p = 0; p < a.planes; ++p) {
                 uint32_t w[4];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * q], v[2 * q + 1]);
-                    // what would round up to infinity is cut off instead
-                    if (isinf(__low2float(h)) && isfinite(v[2 * q])) h.x = __float2bfloat16_rz(v[2 * q]);
-                    if (isinf(__high2float(h)) && isfinite(v[2 * q + 1])) h.y = __float2bfloat16_rz(v[2 * q + 1]);
+                    if (careful) {
+                        auto plane = [&](float x, __nv_bfloat16& to) {
+                            if (isinf(x)) {
+                                if (a.planes == 3 && p < 2) to = __float2bfloat16_rn(p == 0 ? copysignf(1.f, x) : 0.f);
+                            } else if (isinf(__bfloat162float(to))) {
+                                to = __float2bfloat16_rz(x);     // what would round up to infinity is cut off
+                            }
+                        };
+                        plane(v[2 * q], h.x);
+                        plane(v[2 * q + 1], h.y);
+                    }
                     w[q] = *reinterpret_cast<const uint32_t*>(&h);
-                    // an infinity or NaN is the first plane's alone
-                    v[2 * q] = isfinite(v[2 * q]) ? v[2 * q] - __low2float(h) : 0.f;
-                    v[2 * q + 1] = isfinite(v[2 * q + 1]) ? v[2 * q + 1] - __high2float(h) : 0.f;
+                    if (!careful || !isinf(v[2 * q])) v[2 * q] -= __low2float(h);
+                    if (!careful || !isinf(v[2 * q + 1])) v[2 * q + 1] -= __high2float(h);
                 }
                 *reinterpret_cast<uint4*>(x.to + (p * x.rows + i) * x.ldp + j) = make_uint4(w[0], w[1], w[2], w[3]);
             }

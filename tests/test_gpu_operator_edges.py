@@ -256,3 +256,41 @@ def test_extremes_in_fp32_products(rows, n, k):
     for got in (Y, dX, dW):
         _same_or_close(got, want, tol)
     glr.glr_operator_status()
+
+
+# ----------------------------------------------------------------------------------------- infinities in fp32 products
+
+@pytest.mark.parametrize("rows,n,k", FP32_PATHS)
+def test_infinities_in_fp32_products(rows, n, k):
+    """The type's largest values, infinities of either sign in X and in W, one against a zero and two against each other:
+    every result is what the definition gives, and its finite ones as close as always."""
+    import paper_2507_08784_gb300 as glr
+    gen = torch.Generator().manual_seed(rows)
+    X, W = torch.randn(rows, k, generator=gen), 3000 * torch.randn(n, k, generator=gen)
+    big = torch.finfo(torch.float32).max
+    X[1], X[2] = 0.0, 0.0
+    X[1, 3], X[2, 5], X[3, 7], X[4, k - 1], X[5, 11], X[6, 2] = big, -big, math.inf, -math.inf, math.inf, math.nan
+    W[:, 3], W[:, 5] = 0.4 * torch.rand(n, generator=gen), -0.4 * torch.rand(n, generator=gen)
+    X[3, 9] = math.inf                                      # with W's column 9 of either sign: infinite or not a number
+    W[4, 11] = 0.0
+    W[5, 13], W[6, 11] = math.inf, -math.inf
+    W[7] = 0.0
+    W[7, 20] = big
+    X[:, 20] = 0.3 * torch.rand(rows, generator=gen)
+    a, b = X.double(), W.double()
+    want = a @ b.T
+    size = torch.where(torch.isfinite(a), a, 0).abs() @ torch.where(torch.isfinite(b), b, 0).abs().T
+    want = torch.where(want.abs() > big, want.sign() * math.inf, want)
+    tol = 2.0 ** -19 * size + 1e-30
+    Y, R = (torch.empty(rows, n, device="cuda") for _ in range(2))
+    glr.glr_linear(X.cuda(), W.cuda(), Y)
+    glr.glr_linear(X.cuda(), W.cuda(), R, act="relu")
+    _same_or_close(Y, want, tol)
+    _same_or_close(R, torch.where(want <= 0, 0.0, want), tol)
+    # the same products as gradients: dZ W with dZ = X and W's transpose, and dZ^T X
+    dX, dW = torch.empty(rows, n, device="cuda"), torch.empty(rows, n, device="cuda")
+    glr.glr_linear_grad_input(X.cuda(), W.T.contiguous().cuda(), dX)
+    _same_or_close(dX, want, tol)
+    glr.glr_linear_grad_weight(X.T.contiguous().cuda(), W.T.contiguous().cuda(), dW)
+    _same_or_close(dW, want, tol)
+    glr.glr_operator_status()
