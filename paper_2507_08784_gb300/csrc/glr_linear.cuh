@@ -41,8 +41,12 @@ cudaError_t tc_product(const Product& p, const TcPlan& plan, void* workspace, cu
 // Any strides, sizes, alignment and types, without workspace (k_linear.cu).
 cudaError_t any_product(const Product& p, cudaStream_t st);
 double any_cost(const Product& p);              // its time, us (measured fit)
-// The one of the two that the sizes, the alignment and the workspace given call for.
+// Which kernels a product's sizes and alignment call for; without the workspace that `tc` asks for, kAny.
+enum class Way { kNone, kFewRows, kTensorCores, kAny };
+struct Plan { Way way; TcPlan tc; };
+Plan plan_of(const Product& p);
 cudaError_t product(const Product& p, void* workspace, int64_t workspace_bytes, cudaStream_t st);
+int sm_count();                                 // of the current device; 152 without one
 
 // sums[b][j] = sum over the rows of node b of x(i, j), x rows x n in rows of ldx
 struct ColumnSums {

@@ -173,7 +173,7 @@ int run_product(const char* who, linear::Product& p, void* workspace, int64_t by
     return launched(who, linear::product(p, workspace, bytes, st));
 }
 int product_workspace(int rc, const linear::Product& p, int64_t* bytes) {
-    if (rc == GLR_OK) *bytes = linear::tc_plan(p).bytes();
+    if (rc == GLR_OK) *bytes = linear::plan_of(p).tc.bytes();
     return rc;
 }
 

@@ -516,18 +516,25 @@ bool wide_ok(const void* base, int64_t row_stride, int64_t node_stride, int64_t 
 
 }  // namespace
 
-cudaError_t product(const Product& p, void* workspace, int64_t workspace_bytes, cudaStream_t st) {
-    if (p.M == 0 || p.N == 0) return cudaSuccess;
+Plan plan_of(const Product& p) {
+    if (p.M == 0 || p.N == 0) return {Way::kNone, {}};
     // Few rows: the tensor cores' tiles cost the same from one row to 128 (bf16 4096 x 11008: 46 us, few_rows' 25 for one row,
     // 40 for eight); fp32 ones go through any_product below 128 rows (11008 x 4096: 255 us, few_rows' 37 for one row,
     // 132 for 24).
     const int64_t es = p.dtype == GLR_BF16 ? 2 : 4;
     if (p.mode == kForward && p.M <= (p.dtype == GLR_BF16 ? 8 : 24) && p.K > 0 && p.sAp == 1 && p.sBp == 1 && wide_ok(p.A, p.M == 1 ? 0 : p.sAi, 0, es) &&
         wide_ok(p.B, p.N == 1 ? 0 : p.sBj, 0, es))
-        return p.dtype == GLR_BF16 ? few_rows<__nv_bfloat16>(p, st) : few_rows<float>(p, st);
-    const TcPlan plan = tc_plan(p);
-    const bool fits = plan.bytes() == 0 || (workspace && workspace_bytes >= plan.bytes());
-    return plan.ok && fits ? tc_product(p, plan, workspace, st) : any_product(p, st);
+        return {Way::kFewRows, {}};
+    const TcPlan tc = tc_plan(p);
+    return {tc.ok ? Way::kTensorCores : Way::kAny, tc};
+}
+
+cudaError_t product(const Product& p, void* workspace, int64_t workspace_bytes, cudaStream_t st) {
+    const Plan plan = plan_of(p);
+    if (plan.way == Way::kNone) return cudaSuccess;
+    if (plan.way == Way::kFewRows) return p.dtype == GLR_BF16 ? few_rows<__nv_bfloat16>(p, st) : few_rows<float>(p, st);
+    const bool fits = plan.tc.bytes() == 0 || (workspace && workspace_bytes >= plan.tc.bytes());
+    return plan.way == Way::kTensorCores && fits ? tc_product(p, plan.tc, workspace, st) : any_product(p, st);
 }
 
 cudaError_t any_product(const Product& p, cudaStream_t st) {

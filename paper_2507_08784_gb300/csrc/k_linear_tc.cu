@@ -923,6 +923,13 @@ bool lies_well(const void* x, int64_t si, int64_t sp, int64_t sb, int64_t ni, in
 
 }  // namespace
 
+int sm_count() {
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess) return sms;
+    cudaGetLastError();
+    return 152;
+}
+
 // Which operands a product has to have packed, and what that takes.
 TcPlan tc_plan(const Product& p) {
     TcPlan t{};
@@ -948,7 +955,7 @@ TcPlan tc_plan(const Product& p) {
     if (flops < 1e7 || (t.planes == 3 && p.M < 16)) return t;
     const int64_t slabs = (p.K + kSlab - 1) / kSlab * (t.planes == 3 ? 6 : 1);
     const double elements = (t.pack_a ? static_cast<double>(a.rows) * a.cols : 0.0) + (t.pack_b ? static_cast<double>(b.rows) * b.cols : 0.0);
-    const double packed = (t.planes == 3 ? 13 + 2e-6 * elements : 11 + 9e-7 * elements) + choose(p, slabs, p.out_dtype == GLR_F32, 152).cycles / 1870.0;
+    const double packed = (t.planes == 3 ? 13 + 2e-6 * elements : 11 + 9e-7 * elements) + choose(p, slabs, p.out_dtype == GLR_F32, sm_count()).cycles / 1870.0;
     t.ok = packed < any_cost(p);
     return t;
 }
@@ -972,9 +979,7 @@ cudaError_t tc_product(const Product& p, const TcPlan& plan, void* workspace, cu
     if (plan.pack_a) packed(q.A, q.sAi, q.sAp, q.sAb, p.M, ws);
     if (plan.pack_b) packed(q.B, q.sBj, q.sBp, q.sBb, p.N, ws + plan.bytes_a);
     if (n && (e = plan.planes == 3 ? pack<float>(jobs, n, st) : pack<__nv_bfloat16>(jobs, n, st)) != cudaSuccess) return e;
-    int dev = 0, sms = 0;
-    if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
-    if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
+    const int sms = sm_count();
     const bool promote = p.out_dtype == GLR_F32;
     a.planes = plan.planes;
     a.chunk = plan.planes == 3 ? 6 : 4;
