@@ -368,6 +368,7 @@ int glr_select_noalloc(int32_t m_prime, int32_t n_prime, int32_t r, const float*
  * backward pass starts from.  They hold no state: the caller owns every buffer, all work is enqueued
  * on `stream` without synchronisation, nothing is allocated, and a call may be captured into a
  * graph.  Common to all of them:
+ *   - The buffers lie on the current device, and `stream` is one of its streams.
  *   - Matrices are row-major with unit column stride; ld* is the row stride in elements (at least
  *     the number of columns; any value and any element-aligned address).  dtype is GLR_F32 or
  *     GLR_BF16.  Sums, statistics and epilogues are fp32; a bf16 result is rounded once.

@@ -2,6 +2,7 @@
 import ctypes
 
 import pytest
+import torch
 
 import __graft_entry__
 from paper_2507_08784_gb300 import _lib
@@ -25,3 +26,71 @@ def test_workspace_is_asked_for_where_it_is_used(lib, rows, n, k, some):
     assert (need.value > 0) == some, need.value
     args.dtype = _lib.GLR_BF16
     assert lib.glr_linear_workspace(ctypes.byref(args), ctypes.byref(need)) == 0 and need.value == 0
+
+
+class _Elsewhere:
+    """What the binding asks of a tensor on a GPU that this machine need not have."""
+    is_cuda = True
+
+    def __init__(self, *shape, dtype=torch.float32, at=0):
+        self.shape, self.dtype, self.at, self.device = torch.Size(shape), dtype, at, torch.device("cuda", at)
+
+    def stride(self):
+        return tuple(torch.empty(self.shape, device="meta").stride())
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return self.shape.numel()
+
+    def get_device(self):
+        return self.at
+
+    def data_ptr(self):
+        return P
+
+    def is_contiguous(self):
+        return True
+
+
+def _calls():
+    t, i = _Elsewhere, lambda *s: _Elsewhere(*s, dtype=torch.int64)
+    return {
+        "glr_linear": ((t(4, 8), t(6, 8), t(4, 6)), dict(bias=t(6), residual=t(4, 6), preact=t(4, 6))),
+        "glr_linear_grad_input": ((t(4, 6), t(6, 8), t(4, 8)), dict(residual=t(4, 8), preact=t(4, 8), act="silu", grad_out=t(4, 8))),
+        "glr_linear_grad_weight": ((t(4, 6), t(4, 8), [t(6, 8), t(6, 8)]), dict(db=[t(6), t(6)])),
+        "glr_distill_loss": ((t(4, 9), t(4, 2), i(4, 2)), dict(loss=t(1), row_loss=t(4), dlogits=t(4, 9), labels=i(4), weight=t(4))),
+        "glr_policy_loss": ((t(4, 9), i(4), t(4), t(4)), dict(loss=t(1), row_loss=t(4), logp=t(4), dlogits=t(4, 9), ref_logp=t(4), weight=t(4))),
+        "glr_preference_loss": ((t(4, 9), i(4), i(3)), dict(loss=t(1), pair_loss=t(1), seq_logp=t(2), row_logp=t(4), dlogits=t(4, 9),
+                                                             ref_logp=t(2), weight=t(1), workspace=t(2000))),
+    }
+
+
+@pytest.mark.parametrize("name", sorted(_calls()))
+def test_tensors_of_a_call_lie_on_the_current_device(name, monkeypatch):
+    """An argument on another device, or all of them there, never reaches the library, which takes plain addresses."""
+    from paper_2507_08784_gb300 import operators
+    reached = []
+
+    class Library:
+        def __getattr__(self, entry):
+            return lambda *a: reached.append(entry) or 0
+
+    monkeypatch.setattr(operators, "load", Library)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    fn = getattr(operators, name)
+    args, named = _calls()[name]
+    fn(*args, **named, stream=0)
+    assert reached == [name]
+    tensors = [x for a in (*args, *named.values()) for x in (a if isinstance(a, list) else [a]) if isinstance(x, _Elsewhere)]
+    for x in tensors:
+        x.at = 1
+        with pytest.raises(ValueError, match="device"):
+            fn(*args, **named, stream=0)
+        x.at = 0
+    for x in tensors:
+        x.at = 1
+    with pytest.raises(ValueError, match="device"):
+        fn(*args, **named, stream=0)
+    assert reached == [name]
