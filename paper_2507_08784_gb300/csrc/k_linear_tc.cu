@@ -15,10 +15,10 @@
 // a 256 x 256 one's (CG = 2), and they add their partial tiles over distributed shared memory in the order of the
 // contraction.
 //
-// The tensor cores truncate their fp32 sums (about 2^-25 of the sum for every 16 elements, always the same
-// way), which over a long contraction is far above fp32 rounding: where the result is fp32 (PROMOTE), and in
-// tc_split_kernel, the sums of 256 contraction elements (64 of three planes) join the total in rounded additions by
-// the epilogue warps.
+// The tensor cores truncate their fp32 sums, always the same way: 2^-25 of the sum for every 16 elements, or more, which
+// over a long contraction is far above fp32 rounding.  Where the result is fp32 (PROMOTE), and in tc_split_kernel, the
+// sums of 256 contraction elements (64 of three planes) join the total in rounded additions by the epilogue warps; where
+// it is bf16, whole tiles are summed up by truncation to kMostTruncated elements, and longer contractions are shared.
 //
 // What bounds it: the tensor pipe for contractions of about 1000 and more, 512 cycles a 256 x 256 x 64 stage (8192 x
 // 11008 x 4096 bf16: 388 us, 1905 TFLOP/s; with SiLU and pre-activation 406); below that the epilogue (8192 x 2048 x 512:
@@ -900,11 +900,16 @@ int64_t small_tiles(const Product& p) { return ((p.M + 127) / 128) * ((p.N + kSp
 // (four pairs to a tile: too few clusters at once, never the fastest).  128 x 64 tiles shared by one to eight CTAs: 420 a
 // stage, 620 with two on an SM.  400 x 4096 x 4096 fp32: 176, 114 and 157 us; 1000 x 11008 x 2048 bf16: 56, 48 and 66; 200 x
 // 4096 x 4096 bf16: 27, 27 and 23; 24 rows: 27, 25 and 19.
+// Contractions up to which sums may be truncated: of positive matrices, 32768 rows' gradients come out 2^-12.5 of their value
+// short (fp32 ones 2^-12.0), a sixteenth of the rounding to bf16, 2^20 rows' 2^-7.3.  Beyond it the sums are shared and
+// promoted, for about a tenth of the time (2048 x 2048 bf16 over 2^20 rows: 4411 us by whole tiles, 4838).
+constexpr int64_t kMostTruncated = 32768;
 struct Choice { int splits; bool paired; int64_t cycles; };
 Choice choose(const Product& p, int64_t slabs, bool promote, int sms) {
     const int64_t big = big_tiles(p), small = small_tiles(p), pairs = sms / 2;
     const auto waves = [](int64_t n, int64_t at_once) { return (n + at_once - 1) / at_once; };
-    int64_t best = 4000 + waves(big, pairs) * slabs * (promote ? 650 : 530);
+    // (whole tiles whose sums are not promoted drift with the contraction, and are not for the longest)
+    int64_t best = promote || p.K <= kMostTruncated ? 4000 + waves(big, pairs) * slabs * (promote ? 650 : 530) : INT64_MAX;
     int splits = 0;
     bool paired = false;
     if (const int64_t t = 26000 + waves(big, sms * 36 / 152) * (slabs + 1) / 2 * 670; t < best && slabs >= 8) { best = t; splits = 2; paired = true; }

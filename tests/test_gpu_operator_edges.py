@@ -294,3 +294,33 @@ def test_infinities_in_fp32_products(rows, n, k):
     glr.glr_linear_grad_weight(X.T.contiguous().cuda(), W.T.contiguous().cuda(), dW)
     _same_or_close(dW, want, tol)
     glr.glr_operator_status()
+
+
+# --------------------------------------------------------------------------------------------- very long contractions
+
+@pytest.mark.parametrize("dt,rows", [("bf16", 1 << 20), ("f32", 1 << 17)])
+def test_long_sums_rounded_to_bf16_do_not_drift(dt, rows):
+    """bf16 gradients of positive matrices of many rows.  A truncated sum is short by 2^-25 of itself or more for
+    every 16 of its terms, always the same way; roundings to bf16 (2^-8) cancel in the mean over n k / 32 results of
+    different size, to 2^-8 / sqrt(n k / 32) < 2^-16.  So the mean relative error tells them apart: below 2^-12, a sixteenth of
+    the final rounding."""
+    import paper_2507_08784_gb300 as glr
+    dt, n, k = DT[dt], 2048, 2048
+    gen = torch.Generator("cuda").manual_seed(6)
+
+    def positive(cols):
+        scale = 1 + torch.rand(cols, device="cuda", generator=gen)
+        return torch.rand(rows, cols, device="cuda", generator=gen).mul_(scale).to(dt)
+
+    dZ, X = positive(n), positive(k)
+    dW = torch.empty(n, k, device="cuda", dtype=torch.bfloat16)
+    glr.glr_linear_grad_weight(dZ, X, dW)
+    at = slice(0, n, 32)
+    want = torch.zeros(n // 32, k, device="cuda", dtype=torch.float64)
+    for i in range(0, rows, 1 << 14):
+        part = slice(i, i + (1 << 14))
+        want += dZ[part, at].double().T @ X[part].double()
+    error = (dW[at].double() - want) / want
+    assert float(error.abs().max()) <= 2.0 ** -8 + 2.0 ** -12
+    assert abs(float(error.mean())) <= 2.0 ** -12, float(error.mean())
+    glr.glr_operator_status()
