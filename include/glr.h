@@ -461,7 +461,7 @@ int glr_linear_grad_weight_workspace(const glr_linear_grad_weight_args* a, int64
  *   loss     = sum_t weight_t row_loss_t
  *   dlogits  = weight (soft / tau (p - sum_k q_k e_{id_k}) + hard (p1 - e_label))
  * labels null or a label outside [0, vocab): no hard term for the row.  No present entry (or only
- * teacher logits of -infinity): no soft term.  topk <= GLR_MAX_TOPK; tau > 0.                     */
+ * teacher logits of -infinity): no soft term.  topk <= GLR_MAX_TOPK; tau >= 1.2e-38.                    */
 #define GLR_MAX_TOPK 1024
 typedef struct glr_distill_args {
     int64_t rows, vocab, topk;
@@ -486,6 +486,7 @@ int glr_distill_loss(const glr_distill_args* a, void* stream);
  *   dlogits  = weight (d row_loss / d logp) (e_token - p) / tau
  * where the clipped branch has slope 0 (beyond 1 + clip_high for A > 0, below 1 - clip_low
  * otherwise).  A token outside [0, vocab) makes its row not count.  ref_logp null: no KL term.
+ * tau >= 1.2e-38.
  * logp (rows) receives the log-probabilities, row_loss (rows) the rows' losses.                   */
 typedef struct glr_policy_args {
     int64_t rows, vocab;
@@ -511,7 +512,7 @@ int glr_policy_loss(const glr_policy_args* a, void* stream);
  * (its mean over the tokens that count when average is 1; 0 for none) and
  * h = (seq_logp - ref_logp)_chosen - (seq_logp - ref_logp)_rejected (ref_logp null: 0):
  *   GLR_PREF_SIGMOID  pair_loss = -(1 - smoothing) log sigmoid(beta h) - smoothing log sigmoid(-beta h)
- *   GLR_PREF_IPO      pair_loss = (h - 1 / (2 beta))^2
+ *   GLR_PREF_IPO      pair_loss = (h - 1 / (2 beta))^2                    (beta >= 1.2e-38)
  *   loss = sum_p weight_p pair_loss_p (weight null: 1 / pairs each; a pair of weight 0 adds nothing
  *   and gets a zero gradient)
  *   dlogits = (d loss / d seq_logp) (d seq_logp / d row_logp) (e_token - softmax(z))

@@ -83,7 +83,7 @@ int check_layer(const char* who, int64_t rows, int64_t n, int64_t k, int dtype, 
         return refuse("%s: need 0 <= rows <= 2^30 and 0 <= n, k <= 2^24", who);
     return GLR_OK;
 }
-bool positive(float x) { return x > 0.f && x <= 3.0e38f; }
+bool positive(float x) { return x >= 1.2e-38f && x <= 3.0e38f; }       // its reciprocal too
 bool finite(float x) { return x >= -3.0e38f && x <= 3.0e38f; }
 bool flag(int v) { return v == 0 || v == 1; }
 

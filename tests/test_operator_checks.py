@@ -94,3 +94,18 @@ def test_tensors_of_a_call_lie_on_the_current_device(name, monkeypatch):
     with pytest.raises(ValueError, match="device"):
         fn(*args, **named, stream=0)
     assert reached == [name]
+
+
+@pytest.mark.parametrize("value", [1e-39, 1e-45, 3.1e38])
+def test_reciprocals_out_of_range_are_refused(lib, value):
+    """A temperature or beta whose reciprocal is not finite would make NaN of every probability."""
+    distill = _lib.GlrDistillArgs(rows=4, vocab=100, topk=3, logits=P, ld_logits=100, teacher=P, ld_teacher=3, ids=P, ld_ids=3, loss=P,
+                                  row_loss=P, temperature=value, soft=1.0)
+    policy = _lib.GlrPolicyArgs(rows=4, vocab=100, logits=P, ld_logits=100, tokens=P, old_logp=P, advantage=P, loss=P, row_loss=P, logp=P,
+                                temperature=value, clip_low=0.2, clip_high=0.2)
+    preference = _lib.GlrPreferenceArgs(rows=4, vocab=100, pairs=1, logits=P, ld_logits=100, tokens=P, offsets=P, loss=P, pair_loss=P,
+                                        seq_logp=P, row_logp=P, workspace=P, workspace_bytes=1 << 20, beta=value)
+    for name, args, says in (("glr_distill_loss", distill, "temperature"), ("glr_policy_loss", policy, "temperature"),
+                             ("glr_preference_loss", preference, "beta")):
+        assert getattr(lib, name)(ctypes.byref(args), None) == _lib.GLR_EINVAL
+        assert says in lib.glr_last_error(None).decode()
