@@ -542,8 +542,8 @@ typedef struct glr_preference_args {
 int glr_preference_loss(const glr_preference_args* a, void* stream);
 
 /* GLR_ETIMEOUT when a bounded wait inside an operator's kernel has given up on the current device
- * since the library was loaded (*gave_up such events; that call's outputs are not valid), else
- * GLR_OK.  Synchronises the device.  gave_up may be null.                                         */
+ * since this function was last called there (*gave_up such events; the outputs of the calls that they
+ * happened in are not valid), else GLR_OK.  Synchronises the device.  gave_up may be null.        */
 int glr_operator_status(int32_t* gave_up);
 
 #ifdef __cplusplus

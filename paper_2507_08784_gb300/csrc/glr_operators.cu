@@ -335,6 +335,7 @@ extern "C" int glr_operator_status(int32_t* gave_up) {
     if (e != cudaSuccess) return launched("glr_operator_status", e);
     if (gave_up) *gave_up = v;
     if (v) {
+        if ((e = cudaMemset(p, 0, sizeof(v))) != cudaSuccess) return launched("glr_operator_status", e);      // reported now
         set_global_error("a bounded wait in an operator's kernel gave up");
         return GLR_ETIMEOUT;
     }

@@ -278,7 +278,7 @@ def glr_preference_loss(logits: torch.Tensor, tokens: torch.Tensor, offsets: tor
 
 
 def glr_operator_status() -> int:
-    """Raises GlrError (GLR_ETIMEOUT) when a bounded wait in an operator's kernel has given up; else 0."""
+    """Raises GlrError (GLR_ETIMEOUT) when a bounded wait in an operator's kernel has given up since the last call; else 0."""
     n = ctypes.c_int32(0)
     _check(load().glr_operator_status(ctypes.byref(n)))
     return int(n.value)

@@ -324,3 +324,20 @@ def test_long_sums_rounded_to_bf16_do_not_drift(dt, rows):
     assert float(error.abs().max()) <= 2.0 ** -8 + 2.0 ** -12
     assert abs(float(error.mean())) <= 2.0 ** -12, float(error.mean())
     glr.glr_operator_status()
+
+
+# --------------------------------------------------------------------------------------------------- waits that gave up
+
+def test_waits_that_gave_up_are_reported_once(tmp_path):
+    """tests/operator_status_check.cu, run with the built library: a call after the report says what came since."""
+    import os
+    import shutil
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    pkg, exe = os.path.join(root, "paper_2507_08784_gb300"), str(tmp_path / "check")
+    subprocess.run([shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc", "-std=c++17", "-O1", "--expt-relaxed-constexpr",
+                    "-gencode", "arch=compute_103a,code=sm_103a", "-I", os.path.join(root, "include"), "-I",
+                    os.path.join(pkg, "csrc"), os.path.join(root, "tests", "operator_status_check.cu"), "-o", exe, "-L",
+                    os.path.join(pkg, "lib"), "-lglr", "-Xlinker", "-rpath", "-Xlinker", os.path.join(pkg, "lib")], check=True)
+    out = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert out.returncode == 0 and out.stdout.strip() == "ok", out.stdout
