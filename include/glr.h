@@ -372,6 +372,10 @@ int glr_select_noalloc(int32_t m_prime, int32_t n_prime, int32_t r, const float*
  *   - Matrices are row-major with unit column stride; ld* is the row stride in elements (at least
  *     the number of columns; any value and any element-aligned address).  dtype is GLR_F32 or
  *     GLR_BF16.  Sums, statistics and epilogues are fp32; a bf16 result is rounded once.
+ *   - fp32 products go through the tensor cores in two or three parts of each element (22 bits or more;
+ *     fewer below 2^-110), within 2^-20 of their value.  Sums of up to 32768 of them for a bf16 result may
+ *     be truncated ones (short by 2^-12 at that length); all others are rounded.  Infinities and NaN are
+ *     what the definition makes of them.
  *   - Sizes may be zero where that leaves nothing to do.  Outputs must not overlap inputs or each
  *     other unless a description says so.
  *   - The same call gives the same bits: every sum has a fixed order.
@@ -383,6 +387,7 @@ int glr_select_noalloc(int32_t m_prime, int32_t n_prime, int32_t r, const float*
 #define GLR_ACT_GELU      2   /* z Phi(z) with the error function                              */
 #define GLR_ACT_GELU_TANH 3   /* 0.5 z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3)))              */
 #define GLR_ACT_SILU      4   /* z / (1 + exp(-z))                                             */
+/* (gelu, gelu_tanh and silu of -infinity, and their slopes at an infinity, are NaN)              */
 
 /* A linear layer, Z = X W^T + b, Y = act(Z) + R: W (n x k) is the layer matrix as glr_create takes
  * it (m = n, n = k there).  bias (n, of dtype), residual (rows x n) and preact (receives Z as dtype,
@@ -516,9 +521,10 @@ int glr_policy_loss(const glr_policy_args* a, void* stream);
  *   loss = sum_p weight_p pair_loss_p (weight null: 1 / pairs each; a pair of weight 0 adds nothing
  *   and gets a zero gradient)
  *   dlogits = (d loss / d seq_logp) (d seq_logp / d row_logp) (e_token - softmax(z))
- * Rows in no sequence get a zero gradient; offsets are clamped to [0, rows].  The weights here are the
- * pairs', and a row whose token does not count is not read.  workspace: at least
- * GLR_PREFERENCE_WORKSPACE(rows, pairs) bytes of device memory, 16-byte aligned, for this call only. */
+ * Rows in no sequence get a zero gradient; offsets are clamped to [0, rows], and must not decrease (a row
+ * in two sequences would get the gradient of either).  The weights here are the pairs', and a row whose
+ * token does not count is not read.  workspace: at least GLR_PREFERENCE_WORKSPACE(rows, pairs) bytes of
+ * device memory, 16-byte aligned, for this call only.                                              */
 #define GLR_PREF_SIGMOID 0
 #define GLR_PREF_IPO     1
 #define GLR_PREFERENCE_WORKSPACE(rows, pairs) (16 * (int64_t)(rows) + 64 * (int64_t)(pairs) + 4096)

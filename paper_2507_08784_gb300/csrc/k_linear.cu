@@ -295,8 +295,8 @@ __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant
 // the contraction, its next loads in flight under the present ones' products (fp32, rounded); `ways` warps of a CTA
 // share them where they would leave SMs without warps.  Lanes' sums are exchanged by halves and added up in a fixed
 // order.  More than eight rows: CTAs for each eight.  Bound by HBM to four rows, by the products beyond.
-// One row of 2048 x 2048 bf16 8.9 us with its launch (128 x 64 tensor-core tiles: 23), of 11008 x 4096 23 us (72), of
-// 4096 x 11008 25 us (54); eight rows of the three 11, 40, 40 us (25, 64, 46).
+// One row of 2048 x 2048 bf16 8.8 us with its launch (128 x 64 tensor-core tiles: 23), of 11008 x 4096 25 us (72), of
+// 4096 x 11008 25 us (54); eight rows of the three 11, 38, 38 us (25, 64, 46).
 constexpr int kRowsCols = 4, kRowsWarps = 8;
 __device__ __forceinline__ void widen(const uint4& u, float (&f)[8], const __nv_bfloat16*) {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
@@ -519,8 +519,8 @@ bool wide_ok(const void* base, int64_t row_stride, int64_t node_stride, int64_t 
 Plan plan_of(const Product& p) {
     if (p.M == 0 || p.N == 0) return {Way::kNone, {}};
     // Few rows: the tensor cores' tiles cost the same from one row to 128 (bf16 4096 x 11008: 46 us, few_rows' 25 for one row,
-    // 40 for eight); fp32 ones go through any_product below 128 rows (11008 x 4096: 255 us, few_rows' 37 for one row,
-    // 132 for 24).
+    // 38 for eight); fp32 ones go through any_product below 128 rows (11008 x 4096: 255 us, few_rows' 37 for one row,
+    // 144 for 24).
     const int64_t es = p.dtype == GLR_BF16 ? 2 : 4;
     if (p.mode == kForward && p.M <= (p.dtype == GLR_BF16 ? 8 : 24) && p.K > 0 && p.sAp == 1 && p.sBp == 1 && wide_ok(p.A, p.M == 1 ? 0 : p.sAi, 0, es) &&
         wide_ok(p.B, p.N == 1 ? 0 : p.sBj, 0, es))

@@ -2,8 +2,8 @@
 // whose rows lie on 16 bytes, either operand contiguous along the contraction ("K-major") or along its own
 // index ("MN-major"), so that the forward product, the input's gradient and the weights' gradients all read
 // their matrices as they are.  Matrices that lie otherwise are copied into rows on 16 bytes first, and fp32
-// ones into three bf16 planes x = hi + mid + lo (24 bits): their product is the sum of the six plane products
-// above 2^-24, one after the other in the same accumulator.
+// ones into three bf16 planes x = hi + mid + lo (24 bits; below 2^-110 the lower ones leave bf16's range): their product
+// is the sum of the six plane products above 2^-24, one after the other in the same accumulator.
 //
 // tc_product_kernel, persistent: a pair of CTAs on two SMs takes 256 x 256 output tiles in turn.  Two warps of each copy
 // operand slabs of 64 contraction elements (128-byte swizzle) into a ring of shared-memory stages, one thread of the
@@ -21,12 +21,12 @@
 // it is bf16, whole tiles are summed up by truncation to kMostTruncated elements, and longer contractions are shared.
 //
 // What bounds it: the tensor pipe for contractions of about 1000 and more, 512 cycles a 256 x 256 x 64 stage (8192 x
-// 11008 x 4096 bf16: 388 us, 1905 TFLOP/s; with SiLU and pre-activation 406); below that the epilogue (8192 x 2048 x 512:
-// 29 us); for few tiles the loads' latency; with promoted sums also the reads of tensor memory, a chunk's in about the time of
-// its products (5632 x 2048 of eight nodes' 1024 rows: 117 us to bf16, 199 to fp32).  fp32: six products a slab, 4096 x
-// 4096 x 2048 328 us.  Tensor memory
-// gives a thread a row; the epilogue warps turn 32 x 32 blocks round in shared memory, so that four lanes share a
-// row and an access covers whole sectors of eight rows.
+// 11008 x 4096 bf16 with SiLU and pre-activation: 467 us among other passes, 1.58 PFLOP/s under the power cap; 408 in a
+// short row of calls, at a higher clock); below that the epilogue (8192 x 2048 x 512: 28 us); for few tiles the loads' latency; with promoted sums also the reads of tensor memory, a chunk's in about
+// the time of its products, and the sums' way back through it at the end (5632 x 2048 of eight nodes' 1024 rows: 113 us to
+// bf16, 207 to fp32).  fp32: six products a slab, 4096 x 4096 x 2048 332 to 350 us.  Tensor memory gives a thread a row;
+// the epilogue warps turn 32 x 32 blocks round in shared memory, so that four lanes share a row and an access covers
+// whole sectors of eight rows.
 #include <algorithm>
 
 #include "glr_host.cuh"

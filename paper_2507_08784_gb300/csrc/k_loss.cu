@@ -12,9 +12,10 @@
 // CTAs of a cluster exchange (m, s) over distributed shared memory.  Two service warps do everything else,
 // taking rows in turn: row data, copies, teacher entries, losses, single entries.
 //
-// Bound by HBM on many rows (8192 rows of 131071 bf16, policy loss: 637 us, 6.7 TB/s), by the copies' and barriers'
-// latency on rows of a few KiB (65536 rows of 2048 bf16: 172 us, 3.1 TB/s), and between them by both and the workers'
-// arithmetic (4096 rows of 32768 bf16: 96 to 103 us, 5.3 TB/s; without a gradient 64 us, 4.2 TB/s).
+// Bound by HBM on many rows (8192 rows of 131071 bf16, policy loss: 636 us, 6.7 TB/s), by the copies' and barriers'
+// latency on rows of a few KiB (65536 rows of 2048 bf16: 170 us, 3.2 TB/s), and between them by both and the workers'
+// arithmetic (4096 rows of 32768 bf16: 95 to 103 us, 5.3 TB/s; without a gradient 64 us, 4.2 TB/s: a slot is handed on as if
+// it were written).
 #include <math_constants.h>
 
 #include <algorithm>
@@ -312,7 +313,7 @@ constexpr int most_workers(bool few) { return few ? kWorkers : kWorkers - 1; }
 // registers for the gradient; else (rows of more than eight such slots) they are formed again.  TWO: a hard
 // term beside tau != 1, so that the sums are kept at two temperatures: kBoth takes two exponentials an element, and at
 // tau = 2 or 4 the second is the first's square or fourth power (4096 rows
-// of 32768 bf16, 64 entries, a hard term: tau = 2 126 -> 109 us, tau = 4 126 -> 111, tau = 3 126, tau = 1 103).
+// of 32768 bf16, 64 entries, a hard term: tau = 2 126 -> 107 us, tau = 4 126 -> 111, tau = 3 126, tau = 1 103).
 //
 // A worker's row is: wait for the slot, sums, one barrier, the merge of all warps' sums (and of the cluster's
 // CTAs), the gradient into the slot.  What each of up to fourteen warps would do for itself is paid that many
@@ -996,9 +997,9 @@ __device__ __forceinline__ void store_last(void* p, const uint4& u) {
 
 // dz = coef (e_token - exp2((z - m) log2 e - log2 s)): the second pass over a preference batch's rows (its factor needs the
 // whole pair first), a piece of a row a CTA.  m and log2 s come apart from the first pass: their sum would lose the
-// latter beside an m of 1e5, and all of it at the type's lowest value.  Rows are taken from the last one back: the sums' pass ended there, and the L2 still
-// holds some 100 MB of it.  Bound by HBM: one read, one write (8 pairs of 2 x 512 rows of 32768 bf16: 225 us with the
-// sums' pass, 4.2 TB/s of one read and one write, 6.0 of the two reads that it makes).
+// latter beside an m of 1e5, and all of it at the type's lowest value.  Rows are taken from the last one back: the sums'
+// pass ended there, and the L2 still holds some 100 MB of it.  Bound by HBM: one read, one write (8 pairs of 2 x 512 rows
+// of 32768 bf16: 249 us with the sums' pass, 4.3 TB/s of one read and one write, 6.5 of the two reads that it makes).
 constexpr int kPieceVecs = 4;
 template <class T>
 __global__ void __launch_bounds__(kThreads) grad_kernel(const RowArgs a, int pieces) {
