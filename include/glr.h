@@ -373,9 +373,9 @@ int glr_select_noalloc(int32_t m_prime, int32_t n_prime, int32_t r, const float*
  *     the number of columns; any value and any element-aligned address).  dtype is GLR_F32 or
  *     GLR_BF16.  Sums, statistics and epilogues are fp32; a bf16 result is rounded once.
  *   - fp32 products go through the tensor cores in two or three parts of each element (22 bits or more;
- *     fewer below 2^-110), within 2^-20 of their value.  Sums of up to 32768 of them for a bf16 result may
- *     be truncated ones (short by 2^-12 at that length); all others are rounded.  Infinities and NaN are
- *     what the definition makes of them.
+ *     fewer below 2^-110), within 2^-20 of their value.  Sums for a bf16 result may be truncated in
+ *     stretches of up to 32768 products (short by 2^-12 at that length); all others are rounded.
+ *     Infinities and NaN are what the definition makes of them.
  *   - Sizes may be zero where that leaves nothing to do.  Outputs must not overlap inputs or each
  *     other unless a description says so.
  *   - The same call gives the same bits: every sum has a fixed order.

@@ -16,17 +16,18 @@
 // contraction.
 //
 // The tensor cores truncate their fp32 sums, always the same way: 2^-25 of the sum for every 16 elements, or more, which
-// over a long contraction is far above fp32 rounding.  Where the result is fp32 (PROMOTE), and in tc_split_kernel, the
-// sums of 256 contraction elements (64 of three planes) join the total in rounded additions by the epilogue warps; where
-// it is bf16, whole tiles are summed up by truncation to kMostTruncated elements, and longer contractions are shared.
+// over a long contraction is far above fp32 rounding.  Where the result is fp32, and in tc_split_kernel, the sums of 256
+// contraction elements (64 of three planes) join the total in rounded additions by the epilogue warps (PROMOTE); where
+// it is bf16, whole tiles' sums are truncated throughout up to kMostTruncated elements, and promoted every 4096 (1024) beyond.
 //
 // What bounds it: the tensor pipe for contractions of about 1000 and more, 512 cycles a 256 x 256 x 64 stage (8192 x
 // 11008 x 4096 bf16 with SiLU and pre-activation: 467 us among other passes, 1.58 PFLOP/s under the power cap; 408 in a
-// short row of calls, at a higher clock); below that the epilogue (8192 x 2048 x 512: 28 us); for few tiles the loads' latency; with promoted sums also the reads of tensor memory, a chunk's in about
-// the time of its products, and the sums' way back through it at the end (5632 x 2048 of eight nodes' 1024 rows: 113 us to
-// bf16, 207 to fp32).  fp32: six products a slab, 4096 x 4096 x 2048 332 to 350 us.  Tensor memory gives a thread a row;
-// the epilogue warps turn 32 x 32 blocks round in shared memory, so that four lanes share a row and an access covers
-// whole sectors of eight rows.
+// short row of calls, at a higher clock); below that the epilogue (8192 x 2048 x 512: 28 us); for few tiles the loads'
+// latency; with sums promoted every 256 elements also the reads of tensor memory, a chunk's in about the time of its
+// products, and the sums' way back through it at the end (5632 x 2048 of eight nodes' 1024 rows: 113 us to bf16, 207 to
+// fp32).  fp32: six products a slab, 4096 x 4096 x 2048 332 to 350 us.  Tensor memory gives a thread a row; the epilogue
+// warps turn 32 x 32 blocks round in shared memory, so that four lanes share a row and an access covers whole sectors
+// of eight rows.
 #include <algorithm>
 
 #include "glr_host.cuh"
@@ -373,14 +374,13 @@ __device__ __forceinline__ void hand_back(uint32_t bar, uint32_t lead) {
 constexpr bool mn_major_a(int mode) { return mode == kGradWeight; }
 constexpr bool mn_major_b(int mode) { return mode != kForward; }
 
-template <int BN, int MODE, bool PROMOTE>
-__global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE)), 1) tc_product_kernel(const __grid_constant__ TcArgs a) {
+template <int BN, int MODE, bool PROMOTE, int DT>
+__global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE && DT == GLR_F32)), 1) tc_product_kernel(const __grid_constant__ TcArgs a) {
     chain_begin();
     constexpr int CG = 2;
     constexpr bool MNA = mn_major_a(MODE), MNB = mn_major_b(MODE);
-    constexpr int DT = PROMOTE ? GLR_F32 : GLR_BF16;
     constexpr bool PLANES = PROMOTE || MODE == kGradWeight;          // bf16 gradients of fp32 matrices too
-    constexpr int kEpiWarps = epi_warps(PROMOTE), kCopyA = kEpiWarps, kCopyB = kEpiWarps + 1, kIssuer = kEpiWarps + 2, kSpan = BN / (kEpiWarps / 4);
+    constexpr int kEpiWarps = epi_warps(PROMOTE && DT == GLR_F32), kCopyA = kEpiWarps, kCopyB = kEpiWarps + 1, kIssuer = kEpiWarps + 2, kSpan = BN / (kEpiWarps / 4);
     constexpr uint32_t SB = stage_bytes<BN, CG>();
     constexpr uint32_t kCols = 2 * BN;                               // two accumulators of BN columns
     extern __shared__ uint8_t dyn_smem[];
@@ -871,12 +871,15 @@ cudaError_t launch_mode(TcArgs& a, bool promote, int splits, bool paired, int sm
         return launch(tc_split_kernel<MODE, 2>, a, dim3(static_cast<unsigned>(2 * a.tiles), splits), dim3(2, splits), threads_of(epi_warps(true)), smem, st);
     }
     const uint32_t sb = stage_bytes<256, 2>();
-    const size_t blocks = epi_warps(promote) * kBlockBytes;
+    const int epi = epi_warps(a.p.out_dtype == GLR_F32);
+    const size_t blocks = epi * kBlockBytes;
     a.stages = std::min<int>(kMaxStages, static_cast<int>((kSmemBytes - 1024 - blocks) / sb));
     const size_t smem = static_cast<size_t>(a.stages) * sb + 1024 + blocks;
     const dim3 grid(static_cast<unsigned>(std::min(a.tiles, sms / 2) * 2));
-    return promote ? launch(tc_product_kernel<256, MODE, true>, a, grid, dim3(2), threads_of(epi_warps(true)), smem, st)
-                   : launch(tc_product_kernel<256, MODE, false>, a, grid, dim3(2), threads_of(epi_warps(false)), smem, st);
+    if (promote && a.p.out_dtype == GLR_BF16)
+        return launch(tc_product_kernel<256, MODE, true, GLR_BF16>, a, grid, dim3(2), threads_of(epi), smem, st);
+    return promote ? launch(tc_product_kernel<256, MODE, true, GLR_F32>, a, grid, dim3(2), threads_of(epi), smem, st)
+                   : launch(tc_product_kernel<256, MODE, false, GLR_BF16>, a, grid, dim3(2), threads_of(epi), smem, st);
 }
 
 // A matrix to pack: its threads a row.
@@ -900,16 +903,17 @@ int64_t small_tiles(const Product& p) { return ((p.M + 127) / 128) * ((p.N + kSp
 // (four pairs to a tile: too few clusters at once, never the fastest).  128 x 64 tiles shared by one to eight CTAs: 420 a
 // stage, 620 with two on an SM.  400 x 4096 x 4096 fp32: 176, 114 and 157 us; 1000 x 11008 x 2048 bf16: 56, 48 and 66; 200 x
 // 4096 x 4096 bf16: 27, 27 and 23; 24 rows: 27, 25 and 19.
-// Contractions up to which sums may be truncated: of positive matrices, 32768 rows' gradients come out 2^-12.5 of their value
-// short (fp32 ones 2^-12.0), a sixteenth of the rounding to bf16, 2^20 rows' 2^-7.3.  Beyond it the sums are shared and
-// promoted, for about a tenth of the time (2048 x 2048 bf16 over 2^20 rows: 4411 us by whole tiles, 4838).
+// Contractions up to which the sums of whole tiles for bf16 results are truncated throughout: of positive matrices, 32768 rows'
+// gradients come out 2^-12.5 of their value short (fp32 ones 2^-12.0), a sixteenth of the rounding to bf16, 2^20 rows' 2^-7.3.
+// Beyond it they are promoted too (2^-16), in chunks of sixteen times the length, whose reads of tensor memory do not show, by
+// eight warps: with sixteen a stage of the ring less (8192 x 4096 over 131072: 4.8 to 5.0 ms, truncated 4.9; with sixteen 5.4).
 constexpr int64_t kMostTruncated = 32768;
+constexpr int kLongChunk = 16;
 struct Choice { int splits; bool paired; int64_t cycles; };
 Choice choose(const Product& p, int64_t slabs, bool promote, int sms) {
     const int64_t big = big_tiles(p), small = small_tiles(p), pairs = sms / 2;
     const auto waves = [](int64_t n, int64_t at_once) { return (n + at_once - 1) / at_once; };
-    // (whole tiles whose sums are not promoted drift with the contraction, and are not for the longest)
-    int64_t best = promote || p.K <= kMostTruncated ? 4000 + waves(big, pairs) * slabs * (promote ? 650 : 530) : INT64_MAX;
+    int64_t best = 4000 + waves(big, pairs) * slabs * (promote ? 650 : 530);
     int splits = 0;
     bool paired = false;
     if (const int64_t t = 26000 + waves(big, sms * 36 / 152) * (slabs + 1) / 2 * 670; t < best && slabs >= 8) { best = t; splits = 2; paired = true; }
@@ -985,13 +989,14 @@ cudaError_t tc_product(const Product& p, const TcPlan& plan, void* workspace, cu
     if (plan.pack_b) packed(q.B, q.sBj, q.sBp, q.sBb, p.N, ws + plan.bytes_a);
     if (n && (e = plan.planes == 3 ? pack<float>(jobs, n, st) : pack<__nv_bfloat16>(jobs, n, st)) != cudaSuccess) return e;
     const int sms = sm_count();
-    const bool promote = p.out_dtype == GLR_F32;
+    const bool fp32 = p.out_dtype == GLR_F32, promote = fp32 || p.K > kMostTruncated;
     a.planes = plan.planes;
     a.chunk = plan.planes == 3 ? 6 : 4;
     const int64_t slabs = (p.K + kSlab - 1) / kSlab * (plan.planes == 3 ? 6 : 1);
     if (slabs > (1 << 30)) return cudaErrorInvalidValue;
     a.slabs = static_cast<int>(slabs);
-    const Choice how = choose(p, slabs, promote, sms);
+    const Choice how = choose(p, slabs, fp32, sms);
+    if (!fp32 && !how.splits) a.chunk *= kLongChunk;
     const int64_t big = big_tiles(p), small = small_tiles(p), pairs = sms / 2;
     if (std::max(big, small) > (1 << 30)) return cudaErrorInvalidValue;
     const int splits = how.splits;

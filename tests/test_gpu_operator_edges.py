@@ -341,3 +341,36 @@ def test_waits_that_gave_up_are_reported_once(tmp_path):
                     os.path.join(pkg, "lib"), "-lglr", "-Xlinker", "-rpath", "-Xlinker", os.path.join(pkg, "lib")], check=True)
     out = subprocess.run([exe], capture_output=True, text=True, timeout=120)
     assert out.returncode == 0 and out.stdout.strip() == "ok", out.stdout
+
+
+# ------------------------------------------------------------------------------------ epilogues of very long contractions
+
+@pytest.mark.parametrize("rows,n,k", [(2000, 2300, 33001), (2048, 2304, 40960), (300, 40, 70000)])
+@pytest.mark.parametrize("pad", [0, 3])
+def test_epilogues_of_very_long_contractions(rows, n, k, pad):
+    """bf16 layers and input gradients with everything in their epilogues, results on 16 bytes and off: sums within
+    (k + 8) 2^-23 of those of the absolute values, as in the tests of shorter ones, results within 2^-8 of their value."""
+    import paper_2507_08784_gb300 as glr
+    gen = torch.Generator("cuda").manual_seed(rows)
+
+    def mat(r, c, scale=1.0, extra=0):
+        x = torch.empty(r, -(-c // 8) * 8 + extra, device="cuda", dtype=torch.bfloat16)
+        return x.normal_(0.0, scale, generator=gen)[:, :c]
+
+    X, W, R, P = mat(rows, k), mat(n, k, k ** -0.5), mat(rows, n, extra=pad), torch.empty(rows, n, device="cuda", dtype=torch.bfloat16)
+    bias, Y = mat(1, n)[0].contiguous(), torch.empty(rows, n + pad, device="cuda", dtype=torch.bfloat16)[:, :n]
+    glr.glr_linear(X, W, Y, bias=bias, act="silu", residual=R, preact=P)
+    x, w = X.double(), W.double()
+    z, size = x @ w.T + bias.double(), x.abs() @ w.abs().T
+    tol = 1.2 * (k + 8) * 2.0 ** -23 * size + 2.0 ** -20 * (1 + z.abs())
+    for got, want in ((P, z), (Y, z * torch.sigmoid(z) + R.double())):
+        assert ((got.double() - want).abs() <= tol + 2.0 ** -8 * want.abs()).all()
+    # the same contraction as an input gradient: dZ = X, and W's transpose
+    D, G, S = torch.empty_like(Y), torch.empty(rows, n + pad, device="cuda", dtype=torch.bfloat16)[:, :n], mat(rows, n, extra=pad)
+    Wt = mat(k, n)
+    Wt.copy_(W.T)
+    glr.glr_linear_grad_input(X, Wt, D, residual=R, preact=S, act="silu", grad_out=G)
+    g, p = x @ w.T + R.double(), torch.sigmoid(S.double())
+    for got, want in ((G, g), (D, g * p * (1 + S.double() * (1 - p)))):
+        assert ((got.double() - want).abs() <= tol + 2.0 ** -20 * g.abs() * (1 + S.double().abs()) + 2.0 ** -8 * want.abs()).all()
+    glr.glr_operator_status()
