@@ -547,6 +547,183 @@ typedef struct glr_preference_args {
 } glr_preference_args;
 int glr_preference_loss(const glr_preference_args* a, void* stream);
 
+/* Embeddings.  A lookup: Y[t] = scale E[tokens[t]] (E vocab x d, Y rows x d of dtype), rounded once; a
+ * token outside [0, vocab) is padding: its row of Y is zero.  Tokens are int32, or int64 where index64
+ * is 1.  rows <= 2^30, d <= 2^20, vocab <= 2^24 - 1.                                             */
+typedef struct glr_embedding_args {
+    int64_t rows, vocab, d;
+    const void* E; int64_t lde;
+    const void* tokens;
+    void* Y; int64_t ldy;
+    int32_t dtype, index64;
+    float scale;
+    int32_t reserved;
+} glr_embedding_args;
+int glr_embedding(const glr_embedding_args* a, void* stream);
+
+/* Every node's gradient of the embedding: the rows of dY (nodes * rows x d) and of tokens are the
+ * nodes' one after the other, `rows` each, and
+ *   dE[i][v] = scale sum of dY[t] over node i's rows t with tokens[t] = v, in the order of the rows
+ * (vocab x d, contiguous, grad_dtype: what glr_step takes as G[i]), zero for tokens that do not
+ * occur; with accumulate 1 it is added to what dE[i] holds (the gradient of an output layer that
+ * shares the matrix).  dE is a host array of `nodes` device pointers to matrices that do not overlap;
+ * 1 <= nodes <= GLR_MAX_NODES, nodes * rows <= 2^30.  workspace (device memory, 16-byte aligned, for one call at a
+ * time) holds the sorted tokens: as many bytes as glr_embedding_grad_workspace says.               */
+typedef struct glr_embedding_grad_args {
+    int64_t nodes, rows, vocab, d;
+    const void* dY; int64_t lddy;
+    const void* tokens;
+    void* const* dE;
+    void* workspace; int64_t workspace_bytes;
+    int32_t dtype, grad_dtype, index64, accumulate;
+    float scale;
+    int32_t reserved;
+} glr_embedding_grad_args;
+int glr_embedding_grad(const glr_embedding_grad_args* a, void* stream);
+int glr_embedding_grad_workspace(const glr_embedding_grad_args* a, int64_t* bytes);
+
+/* Activations in 8 bits.  A row's columns fall into blocks of 32 (the last one may be shorter).  A
+ * block's scale s is the smallest power of two, at least 2^-127 and at most 2^121, with |x| <= 127 s for all
+ * its elements, kept as one byte, log2 s + 127; an element's code is the integer nearest to x / s (ties to even), at
+ * most 127, as int8.  codes is rows x cols in rows of ld_codes, scales rows x ceil(cols / 32) in rows of ld_scales.
+ * The value of a code, code * s, is exact in bf16 and fp32, within s / 2 of x (within s above 127 2^121).  A block with an infinity or a NaN
+ * has the byte 255 and stands for NaN throughout.  rows <= 2^30, cols <= 2^24.
+ * Packing: codes and scales of X (rows x cols of dtype).                                         */
+typedef struct glr_checkpoint_pack_args {
+    int64_t rows, cols;
+    const void* X; int64_t ldx;
+    void* codes; int64_t ld_codes;
+    void* scales; int64_t ld_scales;
+    int32_t dtype, reserved;
+} glr_checkpoint_pack_args;
+int glr_checkpoint_pack(const glr_checkpoint_pack_args* a, void* stream);
+/* Unpacking: Y = act(value) (rows x cols of dtype).  Scale bytes from 249 up other than 255 are not
+ * made by packing; they are read as the powers of two that they are.                             */
+typedef struct glr_checkpoint_unpack_args {
+    int64_t rows, cols;
+    const void* codes; int64_t ld_codes;
+    const void* scales; int64_t ld_scales;
+    void* Y; int64_t ldy;
+    int32_t dtype, act;
+} glr_checkpoint_unpack_args;
+int glr_checkpoint_unpack(const glr_checkpoint_unpack_args* a, void* stream);
+
+/* A layer's backward pass from the 8-bit checkpoint of its input.  codes and scales (nodes * rows x k)
+ * hold the pre-activation Z whose activation X = act(Z), rounded to dtype, was the layer's input (act
+ * GLR_ACT_NONE: the input itself).  As in glr_linear_grad_weight and glr_linear_grad_input:
+ *   dW[i] = dZ_i^T X_i, db[i] = the column sums of dZ_i          (dW null: neither; db null: not wanted)
+ *   dX    = (dZ W + residual) act'(Z)                           (dX null: not wanted, W is not read)
+ * dZ is nodes * rows x n, W n x k, residual (may be null, or dX itself) and dX nodes * rows x k, of dtype.  workspace
+ * (device memory, 16-byte aligned, for one call at a time) holds the unpacked activations: as many bytes as the
+ * query says.                                                                                     */
+typedef struct glr_linear_grad_checkpoint_args {
+    int64_t nodes, rows, n, k;
+    const void* dZ; int64_t lddz;
+    const void* W; int64_t ldw;
+    const void* codes; int64_t ld_codes;
+    const void* scales; int64_t ld_scales;
+    const void* residual; int64_t ldr;
+    void* dX; int64_t lddx;
+    void* const* dW;
+    void* const* db;
+    void* workspace; int64_t workspace_bytes;
+    int32_t dtype, grad_dtype, act, reserved;
+} glr_linear_grad_checkpoint_args;
+int glr_linear_grad_checkpoint(const glr_linear_grad_checkpoint_args* a, void* stream);
+int glr_linear_grad_checkpoint_workspace(const glr_linear_grad_checkpoint_args* a, int64_t* bytes);
+
+/* Root-mean-square norm with the residual's addition.  With S = X + residual (null: X), in fp32:
+ *   H = S, rstd = (mean_j S_j^2 + eps)^(-1/2), Y = S rstd weight (null: 1), each rounded once
+ * X, residual, H, Y are rows x n of dtype, weight n of dtype, rstd (rows) fp32.  H, rstd, Y and the pair
+ * codes, scales may be null; codes and scales receive Y, before its rounding, in 8 bits (as
+ * glr_checkpoint_pack).  H or Y may be X or residual itself, with the same ld.  1 <= n <=
+ * GLR_MAX_NORM, rows <= 2^30, eps >= 1.2e-38.                                                     */
+#define GLR_MAX_NORM 32768
+typedef struct glr_norm_args {
+    int64_t rows, n;
+    const void* X; int64_t ldx;
+    const void* residual; int64_t ldr;
+    const void* weight;
+    void* H; int64_t ldh;
+    void* Y; int64_t ldy;
+    float* rstd;
+    void* codes; int64_t ld_codes;
+    void* scales; int64_t ld_scales;
+    int32_t dtype;
+    float eps;
+} glr_norm_args;
+int glr_norm(const glr_norm_args* a, void* stream);
+
+/* Its gradients from what it left, H (X where there was no residual) and rstd.  With x = H rstd:
+ *   dX = rstd (weight dY - x mean_j(weight dY x)) + residual     (residual: the gradient that reaches H
+ *        past the norm; may be null, or dX or dY itself.  dX, which may be dY itself, is the gradient of X and of the
+ *        residual that was added; null: not wanted)
+ *   dweight[i] = the column sums of dY x over node i's rows        (n, grad_dtype; null: not wanted)
+ * The rows of all matrices (nodes * rows x n) are the nodes' one after the other; dweight is a host array of `nodes`
+ * device pointers.  workspace (device memory, 16-byte aligned, for one call at a time) is needed for dweight: as
+ * many bytes as the query says.                                                                   */
+typedef struct glr_norm_grad_args {
+    int64_t nodes, rows, n;
+    const void* dY; int64_t lddy;
+    const void* H; int64_t ldh;
+    const float* rstd;
+    const void* weight;
+    const void* residual; int64_t ldr;
+    void* dX; int64_t lddx;
+    void* const* dweight;
+    void* workspace; int64_t workspace_bytes;
+    int32_t dtype, grad_dtype;
+} glr_norm_grad_args;
+int glr_norm_grad(const glr_norm_grad_args* a, void* stream);
+int glr_norm_grad_workspace(const glr_norm_grad_args* a, int64_t* bytes);
+
+/* Log-probabilities of given tokens, what glr_policy_loss takes as old_logp and ref_logp and, with the
+ * alternatives, glr_distill_loss as a teacher's logits and ids.  With p = softmax(z / tau) over a row of
+ * logits (rows x vocab):
+ *   logp     = log p[token]; 0 where the token lies outside [0, vocab)
+ *   lse      = log sum_v exp(z_v / tau)
+ *   entropy  = -sum_v p_v log p_v
+ *   top_logp, top_ids: log p and index of the topk largest logits in descending order, equal ones by
+ *              ascending index (rows x topk, top_logp fp32, top_ids int32, or int64 where ids_index64 is 1)
+ * Each output may be null (logp and tokens both).  Logits of -infinity are entries ruled out: they are
+ * no alternatives, and where fewer than topk are left the rest is -infinity at index -1.  A row whose
+ * logits are all -infinity has logp 0, entropy 0 and lse -infinity.  A NaN or +infinity makes its row's logp, lse, entropy
+ * and top_logp NaN, a NaN counting as the largest logit.  topk <= GLR_MAX_TOPK, rows <= 2^24, tau >= 1.2e-38; logits
+ * as for the losses.                                                                              */
+typedef struct glr_token_logp_args {
+    int64_t rows, vocab, topk;
+    const void* logits; int64_t ld_logits;
+    const void* tokens;
+    float* logp;
+    float* lse;
+    float* entropy;
+    float* top_logp; int64_t ld_top_logp;
+    void* top_ids; int64_t ld_top_ids;
+    int32_t dtype, tokens_index64, ids_index64;
+    float temperature;
+} glr_token_logp_args;
+int glr_token_logp(const glr_token_logp_args* a, void* stream);
+
+/* The logits' gradient from those of logp and entropy (rows; either may be null), with lse and, for
+ * dentropy, entropy as glr_token_logp left them:
+ *   dlogits_v = (dlogp ([v = token] - p_v) - dentropy p_v (log p_v + entropy)) / tau
+ * dlogits may be logits itself with the same ld.  Rows without a distribution, and the first term of rows whose token
+ * lies outside [0, vocab), are zero; a row with neither term is not read.                         */
+typedef struct glr_token_logp_grad_args {
+    int64_t rows, vocab;
+    const void* logits; int64_t ld_logits;
+    const void* tokens;
+    const float* lse;
+    const float* entropy;
+    const float* dlogp;
+    const float* dentropy;
+    void* dlogits; int64_t ld_dlogits;
+    int32_t dtype, index64;
+    float temperature;
+    int32_t reserved;
+} glr_token_logp_grad_args;
+int glr_token_logp_grad(const glr_token_logp_grad_args* a, void* stream);
+
 /* GLR_ETIMEOUT when a bounded wait inside an operator's kernel has given up on the current device
  * since this function was last called there (*gave_up such events; the outputs of the calls that they
  * happened in are not valid), else GLR_OK.  Synchronises the device.  gave_up may be null.        */

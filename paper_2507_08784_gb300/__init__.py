@@ -23,7 +23,8 @@ __all__ = ["GlrError", "make_schedule", "glr_create", "glr_destroy", "glr_step",
            "glr_get_basis", "glr_set_basis", "glr_force_selection", "glr_test_expire_wait", "glr_profile_enable",
            "glr_profile_read", "glr_select_noalloc", "GreedyLore", "load", "glr_linear", "glr_linear_grad_input",
            "glr_linear_grad_weight", "glr_distill_loss", "glr_policy_loss", "glr_preference_loss",
-           "glr_operator_status"]
+           "glr_embedding", "glr_embedding_grad", "glr_norm", "glr_norm_grad", "glr_checkpoint_pack", "glr_checkpoint_unpack",
+           "glr_linear_grad_checkpoint", "glr_token_logp", "glr_token_logp_grad", "glr_operator_status"]
 
 
 class GlrError(RuntimeError):
@@ -336,5 +337,7 @@ class GreedyLore:
             pass
 
 
-from .operators import (glr_distill_loss, glr_linear, glr_linear_grad_input, glr_linear_grad_weight,  # noqa: E402
-                        glr_operator_status, glr_policy_loss, glr_preference_loss)
+from .operators import (glr_checkpoint_pack, glr_checkpoint_unpack, glr_distill_loss, glr_embedding,  # noqa: E402
+                        glr_embedding_grad, glr_linear, glr_linear_grad_checkpoint, glr_linear_grad_input,
+                        glr_linear_grad_weight, glr_norm, glr_norm_grad, glr_operator_status, glr_policy_loss,
+                        glr_preference_loss, glr_token_logp, glr_token_logp_grad)

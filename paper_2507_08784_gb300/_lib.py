@@ -22,6 +22,7 @@ GLR_ACT_NONE, GLR_ACT_RELU, GLR_ACT_GELU, GLR_ACT_GELU_TANH, GLR_ACT_SILU = 0, 1
 GLR_PREF_SIGMOID, GLR_PREF_IPO = 0, 1
 GLR_MAX_LOGIT_BYTES = 1572864
 GLR_MAX_TOPK = 1024
+GLR_MAX_NORM = 32768
 
 _c_void_pp = ctypes.POINTER(ctypes.c_void_p)
 _c_float_p = ctypes.c_void_p     # device/host float buffers are passed as raw addresses
@@ -107,6 +108,29 @@ GlrPreferenceArgs = _struct("GlrPreferenceArgs", "glr_preference_args",
                             "seq_logp* row_logp* dlogits* ld_dlogits workspace* workspace_bytes",
                             "dtype tokens_index64 offsets_index64 kind beta. smoothing. average reserved")
 
+GlrEmbeddingArgs = _struct("GlrEmbeddingArgs", "glr_embedding_args", "rows vocab d E* lde tokens* Y* ldy", "dtype index64 scale. reserved")
+GlrEmbeddingGradArgs = _struct("GlrEmbeddingGradArgs", "glr_embedding_grad_args",
+                               "nodes rows vocab d dY* lddy tokens* dE* workspace* workspace_bytes",
+                               "dtype grad_dtype index64 accumulate scale. reserved")
+GlrCheckpointPackArgs = _struct("GlrCheckpointPackArgs", "glr_checkpoint_pack_args",
+                                "rows cols X* ldx codes* ld_codes scales* ld_scales", "dtype reserved")
+GlrCheckpointUnpackArgs = _struct("GlrCheckpointUnpackArgs", "glr_checkpoint_unpack_args",
+                                  "rows cols codes* ld_codes scales* ld_scales Y* ldy", "dtype act")
+GlrLinearGradCheckpointArgs = _struct("GlrLinearGradCheckpointArgs", "glr_linear_grad_checkpoint_args",
+                                      "nodes rows n k dZ* lddz W* ldw codes* ld_codes scales* ld_scales residual* ldr dX* lddx "
+                                      "dW* db* workspace* workspace_bytes", "dtype grad_dtype act reserved")
+GlrNormArgs = _struct("GlrNormArgs", "glr_norm_args",
+                      "rows n X* ldx residual* ldr weight* H* ldh Y* ldy rstd* codes* ld_codes scales* ld_scales", "dtype eps.")
+GlrNormGradArgs = _struct("GlrNormGradArgs", "glr_norm_grad_args",
+                          "nodes rows n dY* lddy H* ldh rstd* weight* residual* ldr dX* lddx dweight* workspace* "
+                          "workspace_bytes", "dtype grad_dtype")
+GlrTokenLogpArgs = _struct("GlrTokenLogpArgs", "glr_token_logp_args",
+                           "rows vocab topk logits* ld_logits tokens* logp* lse* entropy* top_logp* ld_top_logp top_ids* "
+                           "ld_top_ids", "dtype tokens_index64 ids_index64 temperature.")
+GlrTokenLogpGradArgs = _struct("GlrTokenLogpGradArgs", "glr_token_logp_grad_args",
+                               "rows vocab logits* ld_logits tokens* lse* entropy* dlogp* dentropy* dlogits* ld_dlogits",
+                               "dtype index64 temperature. reserved")
+
 GLR_PHASES = 7
 PHASE_NAMES = ["prev_project", "compose", "lambda", "select", "project", "update", "refresh"]
 
@@ -160,6 +184,11 @@ _SIGNATURES = {
     "glr_distill_loss": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p]),
     "glr_policy_loss": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p]),
     "glr_preference_loss": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p]),
+    **{name: (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p])
+       for name in ("glr_embedding", "glr_embedding_grad", "glr_checkpoint_pack", "glr_checkpoint_unpack", "glr_linear_grad_checkpoint",
+                    "glr_norm", "glr_norm_grad", "glr_token_logp", "glr_token_logp_grad")},
+    **{name: (ctypes.c_int, [ctypes.c_void_p, ctypes.POINTER(ctypes.c_int64)])
+       for name in ("glr_embedding_grad_workspace", "glr_linear_grad_checkpoint_workspace", "glr_norm_grad_workspace")},
     "glr_operator_status": (ctypes.c_int, [ctypes.POINTER(ctypes.c_int32)]),
 }
 

@@ -1,31 +1,13 @@
 // Entry points of the operators around the step: linear layers and the losses on logits.  They check their arguments, fill
 // the kernels' arguments and launch; nothing is kept between calls and nothing is allocated.
-#include <cstdarg>
-#include <cstdio>
 #include <mutex>
 
+#include "glr_checks.cuh"
 #include "glr_linear.cuh"
 #include "glr_loss.cuh"
 
 namespace glr {
 namespace {
-
-int refuse(const char* fmt, ...) {
-    char msg[256];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(msg, sizeof(msg), fmt, ap);
-    va_end(ap);
-    set_global_error(msg);
-    return GLR_EINVAL;
-}
-int launched(const char* who, cudaError_t e) {
-    if (e == cudaSuccess) return GLR_OK;
-    char msg[256];
-    snprintf(msg, sizeof(msg), "%s: launch failed: %s", who, cudaGetErrorString(e));
-    set_global_error(msg);
-    return GLR_ECUDA;
-}
 
 // Bounded waits that gave up, per device (glr_operator_status).
 __device__ int g_gave_up;
@@ -44,22 +26,6 @@ int* gave_up_counter() {
     }
     return g_gave_up_addr[dev];
 }
-
-inline int64_t bytes_of(int dtype) { return dtype == GLR_BF16 ? 2 : 4; }
-inline bool dtype_ok(int dtype) { return dtype == GLR_F32 || dtype == GLR_BF16; }
-
-// A row-major matrix argument: present where it has elements, rows no closer than their length,
-// elements on their own size.
-bool matrix_ok(const void* p, int64_t ld, int64_t rows, int64_t cols, int dtype) {
-    if (rows == 0 || cols == 0) return true;
-    return p && (rows == 1 || ld >= cols) && reinterpret_cast<uintptr_t>(p) % bytes_of(dtype) == 0;
-}
-bool vector_ok(const void* p, int64_t n, int64_t bytes) {
-    return n == 0 || (p && reinterpret_cast<uintptr_t>(p) % bytes == 0);
-}
-bool optional_ok(const void* p, int64_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
-
-constexpr int64_t kMaxRows = int64_t(1) << 24;
 
 // The checks all losses share.
 int check_logits(const char* who, int64_t rows, int64_t vocab, const void* z, int64_t ldz, void* dz, int64_t lddz,
@@ -83,10 +49,6 @@ int check_layer(const char* who, int64_t rows, int64_t n, int64_t k, int dtype, 
         return refuse("%s: need 0 <= rows <= 2^30 and 0 <= n, k <= 2^24", who);
     return GLR_OK;
 }
-bool positive(float x) { return x >= 1.2e-38f && x <= 3.0e38f; }       // its reciprocal too
-bool finite(float x) { return x >= -3.0e38f && x <= 3.0e38f; }
-bool flag(int v) { return v == 0 || v == 1; }
-
 }  // namespace
 }  // namespace glr
 

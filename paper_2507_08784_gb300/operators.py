@@ -1,6 +1,6 @@
 """The operators around the step, as declared in ``include/glr.h``: a linear layer with its epilogue, the
-gradients of its input, weights and bias (the weights' per node, as ``GreedyLore.step`` takes them), and the
-losses on logits with their gradients.
+gradients of its input, weights and bias (the weights' per node, as ``GreedyLore.step`` takes them), embeddings,
+norms, activations kept in 8 bits, and the losses on logits and tokens' log-probabilities with their gradients.
 
 Every function marshals its tensors to the C entry point of its name and returns nothing: the outputs are the
 caller's tensors.  The library cannot see the tensors' shapes, so they are checked here; what it can check
@@ -275,6 +275,218 @@ def glr_preference_loss(logits: torch.Tensor, tokens: torch.Tensor, offsets: tor
                                  _vec(seq_logp, "seq_logp", dev, 2 * pairs), _vec(row_logp, "row_logp", dev, rows), d, ldd,
                                  workspace.data_ptr(), 4 * workspace.numel(), dtype, ywide, owide, PREFERENCES[kind],
                                  beta, smoothing, 1 if average else 0, 0), on)
+
+
+def _codes(codes: Optional[torch.Tensor], scales: Optional[torch.Tensor], dev: int, rows: int, cols: int):
+    """Addresses and row strides of an 8-bit matrix and its scales."""
+    if (codes is None) != (scales is None):
+        raise ValueError("codes and scales go together")
+    c, ldc = _mat(codes, "codes", dev, rows, cols, torch.int8)
+    s, lds = _mat(scales, "scales", dev, rows, (cols + 31) // 32, torch.uint8)
+    return c, ldc, s, lds
+
+
+def _nodes(grads, name: str, rows: int):
+    """The nodes' gradient tensors as a list, and the rows of each."""
+    grads = [grads] if isinstance(grads, torch.Tensor) else list(grads)
+    if len(grads) < 1 or rows % len(grads):
+        raise ValueError(f"the rows must be the same number for each of the {name}")
+    return grads, rows // len(grads)
+
+
+def _pointers(grads, name: str, dev: int, shape, dtype):
+    arr = (ctypes.c_void_p * len(grads))()
+    for i, g in enumerate(grads):
+        if tuple(g.shape) != shape:
+            raise ValueError(f"{name}[{i}] must be {' x '.join(map(str, shape))}")
+        arr[i] = _vec(g, f"{name}[{i}]", dev, g.numel(), dtype)
+    return arr
+
+
+def _scratch(args, query, device, stream):
+    """The workspace that a call needs, from PyTorch's allocator in the stream's own pool."""
+    need = ctypes.c_int64(0)
+    _check(query(ctypes.byref(args), ctypes.byref(need)))
+    if need.value == 0:
+        return None
+    space = _alloc(need.value, torch.uint8, device, stream)
+    args.workspace, args.workspace_bytes = space.data_ptr(), need.value
+    return space
+
+
+def glr_embedding(E: torch.Tensor, tokens: torch.Tensor, Y: torch.Tensor, *, scale: float = 1.0, stream=None) -> None:
+    """Y[t] = scale E[tokens[t]], zero for a token outside the vocabulary.  E vocab x d, Y rows x d."""
+    dtype, dev = _dtype(E, "E"), E.get_device()
+    (vocab, d), rows = E.shape, tokens.numel()
+    e, lde = _mat(E, "E", dev, vocab, d)
+    y, ldy = _mat(Y, "Y", dev, rows, d, E.dtype)
+    t, wide = _index(tokens, "tokens", dev, rows)
+    on = _here(dev, stream)
+    _call(load().glr_embedding, _lib.GlrEmbeddingArgs(rows, vocab, d, e, lde, t, y, ldy, dtype, wide, scale, 0), on)
+
+
+def glr_embedding_grad(dY: torch.Tensor, tokens: torch.Tensor, dE: Union[torch.Tensor, Sequence[torch.Tensor]], *,
+                       scale: float = 1.0, accumulate: bool = False, stream=None) -> None:
+    """dE[i][v] = scale times the sum of the rows of dY of token v among node i's equal share of the rows.
+
+    dE holds the nodes' vocab x d gradients (contiguous, float32 or bfloat16: the G of ``GreedyLore.step``); with
+    accumulate the sums are added to what they hold.  A tensor is one node's."""
+    dtype, dev = _dtype(dY, "dY"), dY.get_device()
+    all_rows, d = dY.shape
+    dE, rows = _nodes(dE, "dE", all_rows)
+    vocab, gd = dE[0].shape[0], dE[0].dtype
+    grad_dtype = _dtype(dE[0], "dE")
+    y, lddy = _mat(dY, "dY", dev, all_rows, d)
+    t, wide = _index(tokens, "tokens", dev, all_rows)
+    ep = _pointers(dE, "dE", dev, (vocab, d), gd)
+    lib, on = load(), _here(dev, stream)
+    args = _lib.GlrEmbeddingGradArgs(len(dE), rows, vocab, d, y, lddy, t, ctypes.addressof(ep), None, 0, dtype, grad_dtype, wide,
+                                     1 if accumulate else 0, scale, 0)
+    space = _scratch(args, lib.glr_embedding_grad_workspace, dY.device, stream)
+    _call(lib.glr_embedding_grad, args, on)
+    del space
+
+
+def glr_checkpoint_pack(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, *, stream=None) -> None:
+    """X (rows x cols) in 8 bits: codes (int8) and, for every 32 columns of a row, scales (uint8, rows x ceil(cols / 32))."""
+    dtype, dev = _dtype(X, "X"), X.get_device()
+    rows, cols = X.shape
+    x, ldx = _mat(X, "X", dev, rows, cols)
+    c, ldc, s, lds = _codes(codes, scales, dev, rows, cols)
+    on = _here(dev, stream)
+    _call(load().glr_checkpoint_pack, _lib.GlrCheckpointPackArgs(rows, cols, x, ldx, c, ldc, s, lds, dtype, 0), on)
+
+
+def glr_checkpoint_unpack(codes: torch.Tensor, scales: torch.Tensor, Y: torch.Tensor, *, act: str = "none", stream=None) -> None:
+    """Y = act of the values that codes and scales stand for."""
+    dtype, dev = _dtype(Y, "Y"), Y.get_device()
+    rows, cols = Y.shape
+    y, ldy = _mat(Y, "Y", dev, rows, cols)
+    c, ldc, s, lds = _codes(codes, scales, dev, rows, cols)
+    on = _here(dev, stream)
+    _call(load().glr_checkpoint_unpack, _lib.GlrCheckpointUnpackArgs(rows, cols, c, ldc, s, lds, y, ldy, dtype, _activation(act)), on)
+
+
+def glr_linear_grad_checkpoint(dZ: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, *, W: Optional[torch.Tensor] = None,
+                               dX: Optional[torch.Tensor] = None, dW: Union[None, torch.Tensor, Sequence[torch.Tensor]] = None,
+                               db: Union[None, torch.Tensor, Sequence[torch.Tensor]] = None, act: str = "none",
+                               residual: Optional[torch.Tensor] = None, nodes: int = 1, stream=None) -> None:
+    """A layer's backward pass from its input's checkpoint: X = act(value), dW[i] = dZ_i^T X_i, db[i] the column sums
+    of dZ_i, and dX = (dZ W + residual) act'(value); dW or dX may be left out.  The nodes are those of dW (nodes: without dW)."""
+    dtype, dev = _dtype(dZ, "dZ"), dZ.get_device()
+    all_rows, n = dZ.shape
+    k = codes.shape[1]
+    dt, grad_dtype, wp, bp = dZ.dtype, dtype, None, None
+    z, lddz = _mat(dZ, "dZ", dev, all_rows, n)
+    c, ldc, s, lds = _codes(codes, scales, dev, all_rows, k)
+    if dX is not None and W is None:
+        raise ValueError("dX needs W")
+    w, ldw = _mat(W, "W", dev, n, k, dt)
+    r, ldr = _mat(residual, "residual", dev, all_rows, k, dt)
+    x, lddx = _mat(dX, "dX", dev, all_rows, k, dt)
+    if dW is not None:
+        dW, rows = _nodes(dW, "dW", all_rows)
+        nodes, gd, grad_dtype = len(dW), dW[0].dtype, _dtype(dW[0], "dW")
+        wp = _pointers(dW, "dW", dev, (n, k), gd)
+        if db is not None:
+            db = [db] if isinstance(db, torch.Tensor) else list(db)
+            if len(db) != nodes:
+                raise ValueError("db must hold as many tensors as dW")
+            bp = _pointers(db, "db", dev, (n,), gd)
+    elif db is not None:
+        raise ValueError("db needs dW")
+    elif nodes < 1 or all_rows % nodes:
+        raise ValueError("the rows must be the same number for each of the nodes")
+    lib, on = load(), _here(dev, stream)
+    args = _lib.GlrLinearGradCheckpointArgs(nodes, all_rows // nodes, n, k, z, lddz, w, ldw, c, ldc, s, lds, r, ldr, x, lddx,
+                                            None if wp is None else ctypes.addressof(wp), None if bp is None else ctypes.addressof(bp),
+                                            None, 0, dtype, grad_dtype, _activation(act), 0)
+    space = _scratch(args, lib.glr_linear_grad_checkpoint_workspace, dZ.device, stream)
+    _call(lib.glr_linear_grad_checkpoint, args, on)
+    del space
+
+
+def glr_norm(X: torch.Tensor, Y: Optional[torch.Tensor], *, weight: Optional[torch.Tensor] = None,
+             residual: Optional[torch.Tensor] = None, H: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
+             codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, eps: float = 1e-6, stream=None) -> None:
+    """S = X + residual, H = S, rstd = (mean S^2 + eps)^(-1/2) of each row, Y = S rstd weight, codes and scales Y in 8 bits."""
+    dtype, dev = _dtype(X, "X"), X.get_device()
+    rows, n = X.shape
+    dt = X.dtype
+    x, ldx = _mat(X, "X", dev, rows, n)
+    r, ldr = _mat(residual, "residual", dev, rows, n, dt)
+    h, ldh = _mat(H, "H", dev, rows, n, dt)
+    y, ldy = _mat(Y, "Y", dev, rows, n, dt)
+    c, ldc, s, lds = _codes(codes, scales, dev, rows, n)
+    on = _here(dev, stream)
+    _call(load().glr_norm,
+          _lib.GlrNormArgs(rows, n, x, ldx, r, ldr, _vec(weight, "weight", dev, n, dt), h, ldh, y, ldy, _vec(rstd, "rstd", dev, rows),
+                           c, ldc, s, lds, dtype, eps), on)
+
+
+def glr_norm_grad(dY: torch.Tensor, H: torch.Tensor, rstd: torch.Tensor, dX: Optional[torch.Tensor], *,
+                  weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+                  dweight: Union[None, torch.Tensor, Sequence[torch.Tensor]] = None, stream=None) -> None:
+    """dX = rstd (weight dY - x mean(weight dY x)) + residual with x = H rstd, and dweight[i] = the column sums of dY x
+    over node i's equal share of the rows (vectors of n, float32 or bfloat16; a tensor is one node's)."""
+    dtype, dev = _dtype(dY, "dY"), dY.get_device()
+    all_rows, n = dY.shape
+    dt, nodes, grad_dtype, wp = dY.dtype, 1, dtype, None
+    y, lddy = _mat(dY, "dY", dev, all_rows, n)
+    h, ldh = _mat(H, "H", dev, all_rows, n, dt)
+    r, ldr = _mat(residual, "residual", dev, all_rows, n, dt)
+    x, lddx = _mat(dX, "dX", dev, all_rows, n, dt)
+    if dweight is not None:
+        dweight, _ = _nodes(dweight, "dweight", all_rows)
+        nodes, grad_dtype = len(dweight), _dtype(dweight[0], "dweight")
+        wp = _pointers(dweight, "dweight", dev, (n,), dweight[0].dtype)
+    lib, on = load(), _here(dev, stream)
+    args = _lib.GlrNormGradArgs(nodes, all_rows // nodes, n, y, lddy, h, ldh, _vec(rstd, "rstd", dev, all_rows),
+                                _vec(weight, "weight", dev, n, dt), r, ldr, x, lddx, None if wp is None else ctypes.addressof(wp),
+                                None, 0, dtype, grad_dtype)
+    space = None if wp is None else _scratch(args, lib.glr_norm_grad_workspace, dY.device, stream)
+    _call(lib.glr_norm_grad, args, on)
+    del space
+
+
+def glr_token_logp(logits: torch.Tensor, *, tokens: Optional[torch.Tensor] = None, logp: Optional[torch.Tensor] = None,
+                   lse: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                   top_logp: Optional[torch.Tensor] = None, top_ids: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                   stream=None) -> None:
+    """log softmax(logits / temperature) of every row's token, the logarithm of the sum, the entropy, and the most probable
+    alternatives (rows x topk: float32 log-probabilities, int32 or int64 ids; equal ones by ascending id; see glr.h)."""
+    dtype, dev = _dtype(logits, "logits"), logits.get_device()
+    rows, vocab = logits.shape
+    z, ldz = _mat(logits, "logits", dev, rows, vocab)
+    top = top_logp if top_logp is not None else top_ids
+    topk = 0 if top is None else top.shape[1] if top.dim() == 2 else -1
+    p, ldp = _mat(top_logp, "top_logp", dev, rows, topk, torch.float32)
+    i, ldi = _mat(top_ids, "top_ids", dev, rows, topk)
+    if top_ids is not None and top_ids.dtype not in _INDEX:
+        raise ValueError("top_ids must be int32 or int64")
+    t, wide = _index(tokens, "tokens", dev, rows)
+    on = _here(dev, stream)
+    _call(load().glr_token_logp,
+          _lib.GlrTokenLogpArgs(rows, vocab, topk, z, ldz, t, _vec(logp, "logp", dev, rows), _vec(lse, "lse", dev, rows),
+                                _vec(entropy, "entropy", dev, rows), p, ldp, i, ldi, dtype, wide,
+                                0 if top_ids is None else _INDEX[top_ids.dtype], temperature), on)
+
+
+def glr_token_logp_grad(logits: torch.Tensor, lse: torch.Tensor, dlogits: torch.Tensor, *, tokens: Optional[torch.Tensor] = None,
+                        dlogp: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                        dentropy: Optional[torch.Tensor] = None, temperature: float = 1.0, stream=None) -> None:
+    """The logits' gradient from those of the tokens' log-probabilities and of the rows' entropies, with lse and entropy as
+    glr_token_logp left them; dlogits may be logits itself."""
+    dtype, dev = _dtype(logits, "logits"), logits.get_device()
+    rows, vocab = logits.shape
+    z, ldz = _mat(logits, "logits", dev, rows, vocab)
+    d, ldd = _mat(dlogits, "dlogits", dev, rows, vocab, logits.dtype)
+    t, wide = _index(tokens, "tokens", dev, rows)
+    on = _here(dev, stream)
+    _call(load().glr_token_logp_grad,
+          _lib.GlrTokenLogpGradArgs(rows, vocab, z, ldz, t, _vec(lse, "lse", dev, rows), _vec(entropy, "entropy", dev, rows),
+                                    _vec(dlogp, "dlogp", dev, rows), _vec(dentropy, "dentropy", dev, rows), d, ldd, dtype, wide,
+                                    temperature, 0), on)
 
 
 def glr_operator_status() -> int:
