@@ -3,9 +3,20 @@
 // With x_v = (z_v - m) / tau, m the row's maximum, s = sum e^x and u = sum e^x x:
 //   lse = m / tau + log s,  logp = x_token - log s,  entropy = log s - u / s  (both terms are of one sign)
 // A thread keeps a running maximum and rescales its sums when it grows.  Entries of -infinity add nothing to either sum, and a
-// NaN reaches s.
+// NaN reaches s.  The terms of a round are added up among themselves before they join the thread's sums, which may hold a
+// term of 1 (single terms next to it: log p of a token of p = 0.8 among 131071 off by 3e-6 of itself).
+//
 // The alternatives are ordered by a 64-bit key: the logit as an integer of the same order (-0 as 0, a NaN above all) over the
-// complement of its index, so that no two are equal and equal logits go by their index.
+// complement of its index, so that no two are equal and equal logits go by their index.  They are found in the same pass.  Of the
+// CTA's W warps, the lanes of each hold 32 maxima of what they have seen; where j = ceil(topk / W), the least of the warps' j-th
+// largest maxima has topk elements at or above it, so an element below it is none of the alternatives.  This bound is set
+// after the first round, whose elements are still in registers, and raised after every doubling; what passes it (a few
+// hundred of 131071) goes to a list in shared memory that is thinned by the last bound and put in order by counting.
+// A list that runs over (many equal logits, every element above those before), a NaN or an infinity, and topk above 256 are left to
+// a radix selection of the keys, which reads the row again four to seven times.
+//
+// A row is a CTA's, or with few rows a cluster's: each CTA takes a part, and ranks its ordered alternatives among those of
+// the others, which it reads over distributed shared memory.
 #include <algorithm>
 
 #include "glr_rows.cuh"
@@ -52,29 +63,100 @@ __device__ __forceinline__ float logit_of(uint32_t order) {
 }
 __device__ __forceinline__ uint64_t key_of(float z, uint32_t index) { return static_cast<uint64_t>(order_of(z)) << 32 | ~index; }
 
+// Two fp32 values in one register pair.
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+constexpr float kInf = __builtin_huge_valf();
+
+// Eight neighbouring logits as they lie in memory.
+template <class T> struct Eight;
+template <> struct Eight<__nv_bfloat16> {
+    uint4 u;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { u = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void none() { u = make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
+    // those of [from, to) alone
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, int from, int to) {
+        const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+        uint32_t w[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t a = 2 * q >= from && 2 * q < to ? h[2 * q] : 0xff80u, b = 2 * q + 1 >= from && 2 * q + 1 < to ? h[2 * q + 1] : 0xff80u;
+            w[q] = a | b << 16;
+        }
+        u = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __device__ __forceinline__ float top() const {
+        auto h = [](uint32_t x) { return *reinterpret_cast<const __nv_bfloat162*>(&x); };
+        const __nv_bfloat162 m = __hmax2(__hmax2(h(u.x), h(u.y)), __hmax2(h(u.z), h(u.w)));
+        return fmaxf(__low2float(m), __high2float(m));
+    }
+    __device__ __forceinline__ uint64_t pair(int q) const {
+        const uint32_t w = q == 0 ? u.x : q == 1 ? u.y : q == 2 ? u.z : u.w;
+        return pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    }
+};
+template <> struct Eight<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float* p) { a = reinterpret_cast<const float4*>(p)[0]; b = reinterpret_cast<const float4*>(p)[1]; }
+    __device__ __forceinline__ void none() { a = b = make_float4(-kInf, -kInf, -kInf, -kInf); }
+    __device__ __forceinline__ void load(const float* p, int from, int to) {
+        auto at = [&](int e) { return e >= from && e < to ? p[e] : -kInf; };
+        a = make_float4(at(0), at(1), at(2), at(3));
+        b = make_float4(at(4), at(5), at(6), at(7));
+    }
+    __device__ __forceinline__ float top() const { return fmaxf(fmaxf(fmaxf(a.x, a.y), fmaxf(a.z, a.w)), fmaxf(fmaxf(b.x, b.y), fmaxf(b.z, b.w))); }
+    __device__ __forceinline__ uint64_t pair(int q) const {
+        return q == 0 ? pack2(a.x, a.y) : q == 1 ? pack2(a.z, a.w) : q == 2 ? pack2(b.x, b.y) : pack2(b.z, b.w);
+    }
+};
+
 // A row as vectors of eight that begin on 16 bytes, the first one at or before the row's first element: `skip` elements of
-// it are not the row's.  (Where elements are not on their vectors' pitch, as in rows of fp32 off 32 bytes, eight of fp32
-// begin on 16 bytes too.)
+// it are not the row's.  A CTA takes the vectors [begin, end).
 template <class T>
 struct RowVectors {
     const T* base;
     int skip;
-    int64_t vocab, count;
-    __device__ RowVectors(const T* z, int64_t v) : vocab(v) {
+    int64_t vocab, begin, end;
+    __device__ RowVectors(const T* z, int64_t v, int part, int parts) : vocab(v) {
         skip = static_cast<int>((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T));
         base = z - skip;
-        count = (skip + v + 7) / 8;
+        const int64_t count = (skip + v + 7) / 8;
+        begin = count * part / parts;
+        end = count * (part + 1) / parts;
     }
     __device__ __forceinline__ int64_t first(int64_t q) const { return q * 8 - skip; }     // index of vector q's first element
     // -infinity where there is no element
-    __device__ __forceinline__ void load(int64_t q, float (&v)[8]) const {
+    __device__ __forceinline__ void load(int64_t q, Eight<T>& v) const {
         const int64_t i = first(q);
-        if (i >= 0 && i + 8 <= vocab) {
-            load8(base + q * 8, 8, true, v);
-        } else {
+        if (q >= end) v.none();
+        else if (i >= 0 && i + 8 <= vocab) v.load(base + q * 8);
+        else v.load(base + q * 8, i < 0 ? skip : 0, vocab - i < 8 ? static_cast<int>(vocab - i) : 8);
+    }
+    __device__ __forceinline__ void load(int64_t q, float (&v)[8]) const {
+        Eight<T> x;
+        load(q, x);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = i + e >= 0 && i + e < vocab ? to_f(base[q * 8 + e]) : -__int_as_float(0x7f800000);
-        }
+        for (int e = 0; e < 4; ++e) unpack2(x.pair(e), v[2 * e], v[2 * e + 1]);
     }
 };
 
@@ -95,10 +177,10 @@ __device__ __forceinline__ void sort_keys(uint64_t* key, int n, int size) {
 
 constexpr int kMaxKeys = GLR_MAX_TOPK, kRadix = 11, kBins = 1 << kRadix;
 
-// The topk largest keys of a row, in `key` in any order: how many there are (fewer where fewer entries are left).  A radix
-// selection over the 64-bit keys: 11 bits at a time, the bin in which the topk-th key lies, as far as its ties need.
+// The topk largest keys of the CTA's part of a row, in `key` in any order: how many there are (fewer where fewer entries are
+// left).  A radix selection over the 64-bit keys: 11 bits at a time, the bin in which the topk-th key lies, as far as its ties need.
 template <class T>
-__device__ int select_keys(const RowVectors<T>& row, int topk, uint64_t* key, int* bins, int* scratch) {
+__device__ __noinline__ int select_keys(const RowVectors<T>& row, int topk, uint64_t* key, int* bins, int* scratch) {
     uint64_t prefix = 0;
     int want = topk, low = 64;                       // bits below `low` are not decided yet; keys share `prefix` above
     bool all = false;
@@ -107,7 +189,7 @@ __device__ int select_keys(const RowVectors<T>& row, int topk, uint64_t* key, in
         low -= bits;
         for (int q = threadIdx.x; q < kBins; q += kThreads) bins[q] = 0;
         __syncthreads();
-        for (int64_t q = threadIdx.x; q < row.count; q += kThreads) {
+        for (int64_t q = row.begin + threadIdx.x; q < row.end; q += kThreads) {
             float v[8];
             row.load(q, v);
 #pragma unroll
@@ -147,7 +229,7 @@ __device__ int select_keys(const RowVectors<T>& row, int topk, uint64_t* key, in
     const uint64_t least = low == 64 ? 1 : prefix << low;
     if (threadIdx.x == 0) scratch[3] = 0;
     __syncthreads();
-    for (int64_t q = threadIdx.x; q < row.count; q += kThreads) {
+    for (int64_t q = row.begin + threadIdx.x; q < row.end; q += kThreads) {
         float v[8];
         row.load(q, v);
 #pragma unroll
@@ -163,71 +245,237 @@ __device__ int select_keys(const RowVectors<T>& row, int topk, uint64_t* key, in
     return min(scratch[3], topk);
 }
 
-template <class T>
-__global__ void __launch_bounds__(kThreads) token_logp_kernel(const __grid_constant__ TokenLogp a) {
-    chain_begin();
-    __shared__ Stat parts[kWarps];
-    __shared__ uint64_t key[kMaxKeys];
-    __shared__ int bins[kBins];
-    __shared__ int scratch[4];
-    const int64_t i = blockIdx.x;
-    const T* z = static_cast<const T*>(a.z) + i * a.ldz;
-    const RowVectors<T> row(z, a.vocab);
-    const float c = kLog2e * a.inv_tau;
-    Stat t{kLowest, 0.f, 0.f};
-    for (int64_t q = threadIdx.x; q < row.count; q += kThreads) {
-        float v[8];
-        row.load(q, v);
-        float m = v[0];
+// The j-th largest of the lanes' values.
+__device__ __forceinline__ float lanes_largest(float v, int j) {
+    const int lane = threadIdx.x & 31;
 #pragma unroll
-        for (int e = 1; e < 8; ++e) m = fmaxf(m, v[e]);
+    for (int k = 2; k <= 32; k *= 2)
+#pragma unroll
+        for (int s = k / 2; s > 0; s /= 2) {
+            const float o = __shfl_xor_sync(0xffffffffu, v, s);
+            v = ((lane & s) == 0) == ((lane & k) == 0) ? fmaxf(v, o) : fminf(v, o);
+        }
+    return __shfl_sync(0xffffffffu, v, j - 1);
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t peer_addr(const void* p, uint32_t rank) {
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(static_cast<uint32_t>(__cvta_generic_to_shared(p))), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ uint64_t peer_key(const uint64_t* p, uint32_t rank) {
+    uint64_t v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(peer_addr(p, rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ float peer_float(const float* p, uint32_t rank) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(peer_addr(p, rank)) : "memory");
+    return v;
+}
+
+// Vectors a thread loads at once, the list's places, and the most alternatives that the list is used for.
+template <class T> constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;
+constexpr int kList = 2048, kCounted = 512, kListed = 32 * kWarps;
+// Entropy and alternatives or not: both cost arithmetic in every element.
+template <class T, bool ENT, bool TOP>
+__global__ void __launch_bounds__(kThreads, 5) token_logp_kernel(const __grid_constant__ TokenLogp a, int parts) {
+    chain_begin();
+    __shared__ Stat stats[kWarps + 1];
+    __shared__ float bounds[kWarps];
+    __shared__ int scratch[4];
+    __shared__ uint64_t list[TOP ? kList : 1];       // ordered in the end
+    __shared__ uint64_t thin[TOP ? kMaxKeys : 1];    // (the radix selection's bins)
+    __shared__ int count, thin_count;
+    static_assert(kBins * sizeof(int) <= kMaxKeys * sizeof(uint64_t) && kCounted <= kMaxKeys && kMaxKeys <= kList, "");
+    const int64_t i = blockIdx.x / parts;
+    const uint32_t part = parts > 1 ? cluster_rank() : 0;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const T* z = static_cast<const T*>(a.z) + i * a.ldz;
+    const RowVectors<T> row(z, a.vocab, static_cast<int>(part), parts);
+    const float c = kLog2e * a.inv_tau;
+    const uint64_t c2 = pack2(c, c);
+    const bool listed = TOP && a.topk <= kListed;
+    const int mine = listed ? (a.topk + kWarps - 1) / kWarps : 1;
+    if (TOP) {
+        if (threadIdx.x == 0) { count = 0; thin_count = 0; }
+        __syncthreads();
+    }
+    constexpr int A = kAhead<T>;
+    Stat t{kLowest, 0.f, 0.f};
+    float bound = kLowest;
+    int round = 0;
+    for (int64_t q0 = row.begin; q0 < row.end; q0 += A * kThreads, ++round) {
+        Eight<T> v[A];
+        float top[A];
+#pragma unroll
+        for (int y = 0; y < A; ++y) row.load(q0 + y * kThreads + threadIdx.x, v[y]);
+        float m = t.m;
+#pragma unroll
+        for (int y = 0; y < A; ++y) { top[y] = v[y].top(); m = fmaxf(m, top[y]); }
         if (m > t.m) {
             const float d = fmaxf((t.m - m) * c, -1e30f), x = exp2_fast(d);
             t.u = (t.u + t.s * d) * x;
             t.s *= x;
             t.m = m;
         }
+        const uint64_t neg = pack2(-t.m, -t.m);
+        uint64_t s2 = 0, u2 = 0;                     // two sums of 0.f
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float x = (v[e] - t.m) * c, p = exp2_fast(x);
-            t.s += p;
-            t.u = fmaf(p, fmaxf(x, -1e30f), t.u);
+        for (int y = 0; y < A; ++y)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float x0, x1;
+                unpack2(mul2(add2(v[y].pair(e), neg), c2), x0, x1);
+                const uint64_t p = pack2(exp2_fast(x0), exp2_fast(x1));
+                s2 = add2(s2, p);
+                // beyond 2^-126 the exponential is 0; -infinity is no factor for it
+                if (ENT) u2 = fma2(p, pack2(fmaxf(x0, -200.f), fmaxf(x1, -200.f)), u2);
+            }
+        float s0, s1;
+        unpack2(s2, s0, s1);
+        t.s += s0 + s1;
+        if (ENT) { unpack2(u2, s0, s1); t.u += s0 + s1; }
+        if (listed) {
+            if ((round & (round + 1)) == 0) {        // after 1, 2, 4, ... rounds
+                const float least = lanes_largest(t.m, mine);
+                if (lane == 0) static_cast<volatile float*>(bounds)[warp] = least;
+                if (round == 0) __syncthreads();     // from then on every warp has one; a stale one is a bound too
+                float b = static_cast<volatile float*>(bounds)[lane & (kWarps - 1)];
+#pragma unroll
+                for (int o = 1; o < kWarps; o *= 2) b = fminf(b, __shfl_xor_sync(0xffffffffu, b, o));
+                bound = fmaxf(bound, b);
+            }
+#pragma unroll
+            for (int y = 0; y < A; ++y)
+                if (top[y] >= bound) {
+                    const int64_t first = row.first(q0 + y * kThreads + threadIdx.x);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float x[2];
+                        unpack2(v[y].pair(e), x[0], x[1]);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            if (x[h] >= bound) {
+                                const int at = atomicAdd(&count, 1);
+                                if (at < kList) list[at] = key_of(x[h], static_cast<uint32_t>(first + 2 * e + h));
+                            }
+                    }
+                }
         }
     }
+    if (listed && round > 0) {
+        const float least = lanes_largest(t.m, mine);
+        if (lane == 0) bounds[warp] = least;
+    }
+    // the CTA's statistics, then the row's
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) {
         const Stat y{__shfl_xor_sync(0xffffffffu, t.m, o), __shfl_xor_sync(0xffffffffu, t.s, o), __shfl_xor_sync(0xffffffffu, t.u, o)};
         t = join(t, y, c);
     }
-    if ((threadIdx.x & 31) == 0) parts[threadIdx.x >> 5] = t;
+    if (lane == 0) stats[warp] = t;
     __syncthreads();
-    t = parts[0];
-    for (int w = 1; w < kWarps; ++w) t = join(t, parts[w], c);
+    t = stats[0];
+    for (int w = 1; w < kWarps; ++w) t = join(t, stats[w], c);
+    int n = 0;
+    if (TOP && row.begin < row.end) {
+        if (listed && count <= kList && t.s < kInf) {        // (a NaN is not below it)
+            float b = bounds[0];
+#pragma unroll
+            for (int w = 1; w < kWarps; ++w) b = fminf(b, bounds[w]);
+            const uint64_t least = static_cast<uint64_t>(order_of(b)) << 32;
+            n = count;
+            for (int q = threadIdx.x; q < n; q += kThreads)
+                if (list[q] >= least) {
+                    const int at = atomicAdd(&thin_count, 1);
+                    if (at < kCounted) thin[at] = list[q];
+                }
+            __syncthreads();
+            if (thin_count <= kCounted) {
+                n = thin_count;
+                for (int q = threadIdx.x; q < n; q += kThreads) {
+                    const uint64_t k = thin[q];
+                    int above = 0;
+                    for (int r = 0; r < n; ++r) above += thin[r] > k;
+                    list[above] = k;
+                }
+                __syncthreads();
+            } else {
+                int size = 1;
+                while (size < n) size *= 2;
+                sort_keys(list, n, size);
+            }
+        } else {
+            n = select_keys(row, a.topk, list, reinterpret_cast<int*>(thin), scratch);
+            int size = 1;
+            while (size < n) size *= 2;
+            sort_keys(list, n, size);
+        }
+        n = min(n, a.topk);
+    }
+    if (parts > 1) {
+        if (threadIdx.x == 0) { stats[kWarps] = t; scratch[3] = n; }
+        cluster_sync();
+        Stat all{kLowest, 0.f, 0.f};
+        for (int p = 0; p < parts; ++p) {
+            const float* f = &stats[kWarps].m;
+            const Stat y{peer_float(f, p), peer_float(f + 1, p), peer_float(f + 2, p)};
+            all = p ? join(all, y, c) : y;
+        }
+        t = all;
+    }
     const bool some = !(t.s == 0.f);                 // a row with a distribution, or with a NaN
-    const float log_s = logf(t.s), lse = t.m * a.inv_tau + log_s;
-    if (threadIdx.x == 0) {
-        if (a.lse) a.lse[i] = some ? lse : -__int_as_float(0x7f800000);
-        if (a.entropy) a.entropy[i] = some ? log_s - t.u * 0.6931471805599453f / t.s : 0.f;
+    const float log_s = logf(t.s);
+    if (threadIdx.x == 0 && part == 0) {
+        if (a.lse) a.lse[i] = some ? t.m * a.inv_tau + log_s : -kInf;
+        if (ENT) a.entropy[i] = some ? log_s - t.u * 0.6931471805599453f / t.s : 0.f;
         if (a.logp) {
             const int64_t y = a.tokens.at(i);
             a.logp[i] = some && y >= 0 && y < a.vocab ? (to_f(z[y]) - t.m) * a.inv_tau - log_s : 0.f;
         }
     }
-    if (a.topk == 0) return;
-    const int n = select_keys(row, a.topk, key, bins, scratch);
-    int size = 1;
-    while (size < n) size *= 2;
-    sort_keys(key, n, size);
-    for (int q = threadIdx.x; q < a.topk; q += kThreads) {
-        const uint64_t k = q < n ? key[q] : 0;
-        const int64_t id = q < n ? static_cast<int64_t>(~static_cast<uint32_t>(k)) : -1;
-        if (a.top_logp)
-            a.top_logp[i * a.ld_top_logp + q] = q < n ? (logit_of(static_cast<uint32_t>(k >> 32)) - t.m) * a.inv_tau - log_s : -__int_as_float(0x7f800000);
-        if (a.top_ids) {
-            if (a.ids_wide) static_cast<int64_t*>(a.top_ids)[i * a.ld_top_ids + q] = id;
-            else static_cast<int32_t*>(a.top_ids)[i * a.ld_top_ids + q] = static_cast<int32_t>(id);
-        }
+    if (!TOP) {
+        if (parts > 1) cluster_sync();
+        return;
     }
+    auto write = [&](int at, uint64_t k) {           // k = 0: none left
+        if (a.top_logp) a.top_logp[i * a.ld_top_logp + at] = k ? (logit_of(static_cast<uint32_t>(k >> 32)) - t.m) * a.inv_tau - log_s : -kInf;
+        if (a.top_ids) {
+            const int64_t id = k ? static_cast<int64_t>(~static_cast<uint32_t>(k)) : -1;
+            if (a.ids_wide) static_cast<int64_t*>(a.top_ids)[i * a.ld_top_ids + at] = id;
+            else static_cast<int32_t*>(a.top_ids)[i * a.ld_top_ids + at] = static_cast<int32_t>(id);
+        }
+    };
+    if (parts == 1) {
+        for (int q = threadIdx.x; q < a.topk; q += kThreads) write(q, q < n ? list[q] : 0);
+        return;
+    }
+    // each CTA's keys go where they rank among all of them
+    int total = 0;
+    for (int p = 0; p < parts; ++p) total += static_cast<int>(__float_as_int(peer_float(reinterpret_cast<const float*>(scratch + 3), p)));
+    for (int q = threadIdx.x; q < n; q += kThreads) {
+        const uint64_t k = list[q];
+        int rank = q;
+        for (int p = 1; p < parts && rank < a.topk; ++p) {
+            const uint32_t peer = (part + p) % parts;
+            int lo = 0, hi = __float_as_int(peer_float(reinterpret_cast<const float*>(scratch + 3), peer));
+            while (lo < hi) { const int mid = (lo + hi) >> 1; if (peer_key(list + mid, peer) > k) lo = mid + 1; else hi = mid; }
+            rank += lo;
+        }
+        if (rank < a.topk) write(rank, k);
+    }
+    if (part == 0)
+        for (int q = total + threadIdx.x; q < a.topk; q += kThreads) write(q, 0);
+    cluster_sync();
 }
 
 // dz_v = (dlogp (e_token - p_v) - dentropy p_v (log p_v + entropy)) / tau, with log p_v = z_v / tau - lse; the same elements by
@@ -239,7 +487,7 @@ __global__ void __launch_bounds__(kThreads) token_logp_grad_kernel(const __grid_
     const int part = static_cast<int>(blockIdx.x % parts);
     const T* z = static_cast<const T*>(a.z) + i * a.ldz;
     T* dz = static_cast<T*>(a.dz) + i * a.lddz;
-    const RowVectors<T> row(z, a.vocab);
+    const RowVectors<T> row(z, a.vocab, part, parts);
     const int64_t y = a.tokens.p ? a.tokens.at(i) : -1;
     const bool counted = y >= 0 && y < a.vocab;
     const float lse = a.lse[i];
@@ -248,7 +496,7 @@ __global__ void __launch_bounds__(kThreads) token_logp_grad_kernel(const __grid_
     const float bonus = a.dentropy && some ? a.dentropy[i] * a.inv_tau : 0.f, h = bonus != 0.f ? a.entropy[i] : 0.f;
     const float tail = a.inv_tau;
     const bool wide = (reinterpret_cast<uintptr_t>(dz) & 15) == (reinterpret_cast<uintptr_t>(z) & 15);
-    for (int64_t q = static_cast<int64_t>(part) * kThreads + threadIdx.x; q < row.count; q += static_cast<int64_t>(parts) * kThreads) {
+    for (int64_t q = row.begin + threadIdx.x; q < row.end; q += kThreads) {
         float v[8];
         row.load(q, v);
         const int64_t j = row.first(q);
@@ -275,9 +523,24 @@ __global__ void __launch_bounds__(kThreads) token_logp_grad_kernel(const __grid_
 
 cudaError_t token_logp(const TokenLogp& a, int dtype, cudaStream_t st) {
     if (a.rows == 0) return cudaSuccess;
-    const dim3 grid(static_cast<unsigned>(a.rows));
-    return dtype == GLR_BF16 ? launch_chain(token_logp_kernel<__nv_bfloat16>, grid, kThreads, 0, st, a)
-                             : launch_chain(token_logp_kernel<float>, grid, kThreads, 0, st, a);
+    // CTAs a row: a cluster where the rows leave SMs idle, each CTA with 4096 logits at least
+    int parts = 1;
+    while (parts < 8 && a.rows * parts * 2 <= 2 * 152 && a.vocab >= parts * 2 * 4096) parts *= 2;
+    cudaLaunchAttribute attr[2]{};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = parts; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(a.rows * parts)); cfg.blockDim = kThreads; cfg.stream = st;
+    cfg.attrs = attr; cfg.numAttrs = parts > 1 ? 2 : 1;
+    using H = __nv_bfloat16;
+    const auto kernel = dtype == GLR_BF16
+        ? (a.entropy ? (a.topk ? token_logp_kernel<H, true, true> : token_logp_kernel<H, true, false>)
+                     : (a.topk ? token_logp_kernel<H, false, true> : token_logp_kernel<H, false, false>))
+        : (a.entropy ? (a.topk ? token_logp_kernel<float, true, true> : token_logp_kernel<float, true, false>)
+                     : (a.topk ? token_logp_kernel<float, false, true> : token_logp_kernel<float, false, false>));
+    return cudaLaunchKernelEx(&cfg, kernel, a, parts);
 }
 
 cudaError_t token_logp_grad(const TokenLogpGrad& a, int dtype, cudaStream_t st) {
