@@ -8,12 +8,13 @@
 //
 // The alternatives are ordered by a 64-bit key: the logit as an integer of the same order (-0 as 0, a NaN above all) over the
 // complement of its index, so that no two are equal and equal logits go by their index.  They are found in the same pass.  Of the
-// CTA's W warps, the lanes of each hold 32 maxima of what they have seen; where j = ceil(topk / W), the least of the warps' j-th
-// largest maxima has topk elements at or above it, so an element below it is none of the alternatives.  This bound is set
-// after the first round, whose elements are still in registers, and raised after every doubling; what passes it (a few
-// hundred of 131071) goes to a list in shared memory that is thinned by the last bound and put in order by counting.
-// A list that runs over (many equal logits, every element above those before), a NaN or an infinity, and topk above 256 are left to
-// a radix selection of the keys, which reads the row again four to seven times.
+// CTA's W warps, the lanes of each hold 32 maxima of what they have seen (or several each, of apart vectors); where
+// j = ceil(topk / W), the least of the warps' j-th largest maxima has topk elements at or above it, so an element below it is none
+// of the alternatives.  This bound is set after the first round, whose elements are still in registers, and raised after
+// every doubling; the vectors that hold an element above it (a few hundred of 16384) go to a list in shared memory.  Those
+// above the last bound are read again, and their elements put in order by counting or a bitonic sort.
+// A list that runs over (many equal logits, every element above those before), a NaN or an infinity, and more alternatives than
+// the maxima can bound well are left to a radix selection of the keys, which reads the row again four to seven times.
 //
 // A row is a CTA's, or with few rows a cluster's: each CTA takes a part, and ranks its ordered alternatives among those of
 // the others, which it reads over distributed shared memory.
@@ -26,7 +27,7 @@ namespace rows {
 
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kThreads = 256;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;
 
@@ -114,6 +115,10 @@ template <> struct Eight<__nv_bfloat16> {
         const uint32_t w = q == 0 ? u.x : q == 1 ? u.y : q == 2 ? u.z : u.w;
         return pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
     }
+    __device__ __forceinline__ float at(int e) const {
+        const uint32_t w = e < 2 ? u.x : e < 4 ? u.y : e < 6 ? u.z : u.w;
+        return __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
+    }
 };
 template <> struct Eight<float> {
     float4 a, b;
@@ -128,6 +133,10 @@ template <> struct Eight<float> {
     __device__ __forceinline__ uint64_t pair(int q) const {
         return q == 0 ? pack2(a.x, a.y) : q == 1 ? pack2(a.z, a.w) : q == 2 ? pack2(b.x, b.y) : pack2(b.z, b.w);
     }
+    __device__ __forceinline__ float at(int e) const {
+        const float4 h = e < 4 ? a : b;
+        return (e & 3) == 0 ? h.x : (e & 3) == 1 ? h.y : (e & 3) == 2 ? h.z : h.w;
+    }
 };
 
 // A row as vectors of eight that begin on 16 bytes, the first one at or before the row's first element: `skip` elements of
@@ -135,24 +144,23 @@ template <> struct Eight<float> {
 template <class T>
 struct RowVectors {
     const T* base;
-    int skip;
-    int64_t vocab, begin, end;
-    __device__ RowVectors(const T* z, int64_t v, int part, int parts) : vocab(v) {
+    int skip, vocab, begin, end;
+    __device__ __forceinline__ RowVectors(const T* z, int v, int part, int parts) : vocab(v) {
         skip = static_cast<int>((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T));
         base = z - skip;
-        const int64_t count = (skip + v + 7) / 8;
+        const int count = (skip + v + 7) / 8;
         begin = count * part / parts;
         end = count * (part + 1) / parts;
     }
-    __device__ __forceinline__ int64_t first(int64_t q) const { return q * 8 - skip; }     // index of vector q's first element
+    __device__ __forceinline__ int first(int q) const { return q * 8 - skip; }     // index of vector q's first element
     // -infinity where there is no element
-    __device__ __forceinline__ void load(int64_t q, Eight<T>& v) const {
-        const int64_t i = first(q);
+    __device__ __forceinline__ void load(int q, Eight<T>& v) const {
+        const int i = first(q);
         if (q >= end) v.none();
         else if (i >= 0 && i + 8 <= vocab) v.load(base + q * 8);
-        else v.load(base + q * 8, i < 0 ? skip : 0, vocab - i < 8 ? static_cast<int>(vocab - i) : 8);
+        else v.load(base + q * 8, i < 0 ? skip : 0, min(8, vocab - i));
     }
-    __device__ __forceinline__ void load(int64_t q, float (&v)[8]) const {
+    __device__ __forceinline__ void load(int q, float (&v)[8]) const {
         Eight<T> x;
         load(q, x);
 #pragma unroll
@@ -160,13 +168,16 @@ struct RowVectors {
     }
 };
 
-// The CTA's keys in descending order; n <= size, a power of two; the places behind are filled with 0.
-__device__ __forceinline__ void sort_keys(uint64_t* key, int n, int size) {
-    for (int q = n + threadIdx.x; q < size; q += kThreads) key[q] = 0;
+// The CTA's keys in descending order; the places behind them, up to a power of two, are filled with 0.
+template <int NT>
+__device__ __noinline__ void sort_keys(uint64_t* key, int n) {
+    int size = 1;
+    while (size < n) size *= 2;
+    for (int q = n + threadIdx.x; q < size; q += NT) key[q] = 0;
     __syncthreads();
     for (int len = 2; len <= size; len *= 2)
         for (int gap = len / 2; gap > 0; gap /= 2) {
-            for (int q = threadIdx.x; q < size / 2; q += kThreads) {
+            for (int q = threadIdx.x; q < size / 2; q += NT) {
                 const int i = 2 * q - (q & (gap - 1)), j = i + gap;
                 const uint64_t x = key[i], y = key[j];
                 if ((x < y) == ((i & len) == 0)) { key[i] = y; key[j] = x; }
@@ -179,7 +190,7 @@ constexpr int kMaxKeys = GLR_MAX_TOPK, kRadix = 11, kBins = 1 << kRadix;
 
 // The topk largest keys of the CTA's part of a row, in `key` in any order: how many there are (fewer where fewer entries are
 // left).  A radix selection over the 64-bit keys: 11 bits at a time, the bin in which the topk-th key lies, as far as its ties need.
-template <class T>
+template <class T, int NT>
 __device__ __noinline__ int select_keys(const RowVectors<T>& row, int topk, uint64_t* key, int* bins, int* scratch) {
     uint64_t prefix = 0;
     int want = topk, low = 64;                       // bits below `low` are not decided yet; keys share `prefix` above
@@ -187,9 +198,9 @@ __device__ __noinline__ int select_keys(const RowVectors<T>& row, int topk, uint
     while (low > 0 && !all) {
         const int bits = min(kRadix, low);
         low -= bits;
-        for (int q = threadIdx.x; q < kBins; q += kThreads) bins[q] = 0;
+        for (int q = threadIdx.x; q < kBins; q += NT) bins[q] = 0;
         __syncthreads();
-        for (int64_t q = row.begin + threadIdx.x; q < row.end; q += kThreads) {
+        for (int q = row.begin + threadIdx.x; q < row.end; q += NT) {
             float v[8];
             row.load(q, v);
 #pragma unroll
@@ -229,7 +240,7 @@ __device__ __noinline__ int select_keys(const RowVectors<T>& row, int topk, uint
     const uint64_t least = low == 64 ? 1 : prefix << low;
     if (threadIdx.x == 0) scratch[3] = 0;
     __syncthreads();
-    for (int64_t q = row.begin + threadIdx.x; q < row.end; q += kThreads) {
+    for (int q = row.begin + threadIdx.x; q < row.end; q += NT) {
         float v[8];
         row.load(q, v);
 #pragma unroll
@@ -257,6 +268,24 @@ __device__ __forceinline__ float lanes_largest(float v, int j) {
         }
     return __shfl_sync(0xffffffffu, v, j - 1);
 }
+// A value that at least j of the lanes' n values each reach, j <= 32 n: ten bisections between the least and the largest of
+// them, as integers of the same order (1 is that of no logit, and below all of them).
+template <int N>
+__device__ __noinline__ float lanes_many(const float (&v)[N], int j) {
+    uint32_t o[N], lo = 0xffffffffu, hi = 0;
+#pragma unroll
+    for (int q = 0; q < N; ++q) { o[q] = order_of(v[q]); lo = min(lo, o[q]); hi = max(hi, o[q]); }
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    for (int it = 0; it < 10 && hi - lo > 1; ++it) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        int n = 0;
+#pragma unroll
+        for (int q = 0; q < N; ++q) n += __popc(__ballot_sync(0xffffffffu, o[q] >= mid));
+        if (n >= j) lo = mid; else hi = mid;
+    }
+    return fmaxf(logit_of(lo), kLowest);
+}
 
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -282,45 +311,61 @@ __device__ __forceinline__ float peer_float(const float* p, uint32_t rank) {
     return v;
 }
 
-// Vectors a thread loads at once, the list's places, and the most alternatives that the list is used for.
+// Vectors a thread loads at once (their running maxima are kept apart), and how many alternatives the list is used for: with one
+// maximum a lane, and with all.
 template <class T> constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;
-constexpr int kList = 2048, kCounted = 512, kListed = 32 * kWarps;
+constexpr int kCounted = 256;
+template <class T, int NT> constexpr int kFew = NT / 2;
+template <class T, int NT> constexpr int kListed = NT * kAhead<T> * 3 / 8;
 // Entropy and alternatives or not: both cost arithmetic in every element.
-template <class T, bool ENT, bool TOP>
-__global__ void __launch_bounds__(kThreads, 5) token_logp_kernel(const __grid_constant__ TokenLogp a, int parts) {
+template <class T, bool ENT, bool TOP, int NT>
+__global__ void __launch_bounds__(NT, 1280 / NT) token_logp_kernel(const __grid_constant__ TokenLogp a, int parts) {
     chain_begin();
-    __shared__ Stat stats[kWarps + 1];
-    __shared__ float bounds[kWarps];
+    constexpr int W = NT / 32, kWarpList = kMaxKeys * 2 / W;
+    __shared__ Stat stats[W + 1];
+    __shared__ float bounds[W];
     __shared__ int scratch[4];
-    __shared__ uint64_t list[TOP ? kList : 1];       // ordered in the end
-    __shared__ uint64_t thin[TOP ? kMaxKeys : 1];    // (the radix selection's bins)
-    __shared__ int count, thin_count;
-    static_assert(kBins * sizeof(int) <= kMaxKeys * sizeof(uint64_t) && kCounted <= kMaxKeys && kMaxKeys <= kList, "");
-    const int64_t i = blockIdx.x / parts;
+    // Each warp's vectors that hold an element above the bound, with the upper half of their maximum's order; the ordered keys in
+    // the end.  (16 KiB in all: the loads' lines in flight need the rest of the SM's memory, with 40 KiB a CTA 4096 rows took 30 us more.)
+    __shared__ __align__(16) uint64_t ordered[TOP ? kMaxKeys : 1];
+    uint32_t* list = reinterpret_cast<uint32_t*>(ordered);
+    __shared__ uint64_t thin[TOP ? kMaxKeys : 1];    // the elements above the last bound (the radix selection's bins)
+    __shared__ int over, thin_count;
+    static_assert(kBins * sizeof(int) <= kMaxKeys * sizeof(uint64_t), "");
     const uint32_t part = parts > 1 ? cluster_rank() : 0;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const T* z = static_cast<const T*>(a.z) + i * a.ldz;
-    const RowVectors<T> row(z, a.vocab, static_cast<int>(part), parts);
     const float c = kLog2e * a.inv_tau;
     const uint64_t c2 = pack2(c, c);
-    const bool listed = TOP && a.topk <= kListed;
-    const int mine = listed ? (a.topk + kWarps - 1) / kWarps : 1;
+    const bool listed = TOP && a.topk <= kListed<T, NT>, few = a.topk <= kFew<T, NT>;
+    const int mine = (a.topk + W - 1) / W;
+    constexpr int A = kAhead<T>;
+    const int64_t i = blockIdx.x / parts;
+    const T* z = static_cast<const T*>(a.z) + i * a.ldz;
+    const RowVectors<T> row(z, static_cast<int>(a.vocab), static_cast<int>(part), parts);
     if (TOP) {
-        if (threadIdx.x == 0) { count = 0; thin_count = 0; }
+        if (threadIdx.x == 0) { over = 0; thin_count = 0; }
         __syncthreads();
     }
-    constexpr int A = kAhead<T>;
     Stat t{kLowest, 0.f, 0.f};
-    float bound = kLowest;
-    int round = 0;
-    for (int64_t q0 = row.begin; q0 < row.end; q0 += A * kThreads, ++round) {
+    float bound = kLowest, most[A];
+#pragma unroll
+    for (int y = 0; y < A; ++y) most[y] = kLowest;
+    int round = 0, due = 0, entries = 0;
+    for (int q0 = row.begin; q0 < row.end; q0 += A * NT, ++round) {
         Eight<T> v[A];
         float top[A];
+        if (q0 > row.begin && q0 + A * NT < row.end) {       // whole vectors all of them
+            const T* p = row.base + (q0 + static_cast<int>(threadIdx.x)) * 8;
 #pragma unroll
-        for (int y = 0; y < A; ++y) row.load(q0 + y * kThreads + threadIdx.x, v[y]);
-        float m = t.m;
+            for (int y = 0; y < A; ++y) v[y].load(p + y * NT * 8);
+        } else {
 #pragma unroll
-        for (int y = 0; y < A; ++y) { top[y] = v[y].top(); m = fmaxf(m, top[y]); }
+            for (int y = 0; y < A; ++y) row.load(q0 + y * NT + threadIdx.x, v[y]);
+        }
+        float m_round = -kInf;
+#pragma unroll
+        for (int y = 0; y < A; ++y) { top[y] = v[y].top(); m_round = fmaxf(m_round, top[y]); if (TOP) most[y] = fmaxf(most[y], top[y]); }
+        const float m = fmaxf(t.m, m_round);
         if (m > t.m) {
             const float d = fmaxf((t.m - m) * c, -1e30f), x = exp2_fast(d);
             t.u = (t.u + t.s * d) * x;
@@ -345,36 +390,45 @@ __global__ void __launch_bounds__(kThreads, 5) token_logp_kernel(const __grid_co
         t.s += s0 + s1;
         if (ENT) { unpack2(u2, s0, s1); t.u += s0 + s1; }
         if (listed) {
-            if ((round & (round + 1)) == 0) {        // after 1, 2, 4, ... rounds
-                const float least = lanes_largest(t.m, mine);
+            // after 1, 2, 4, ... rounds, but the last
+            if (round == due && (round == 0 || q0 + A * NT < row.end)) {
+                due = 2 * due + 1;
+                const float least = few ? lanes_largest(t.m, mine) : lanes_many(most, mine);
                 if (lane == 0) static_cast<volatile float*>(bounds)[warp] = least;
                 if (round == 0) __syncthreads();     // from then on every warp has one; a stale one is a bound too
-                float b = static_cast<volatile float*>(bounds)[lane & (kWarps - 1)];
+                float b = static_cast<volatile float*>(bounds)[lane & (W - 1)];
 #pragma unroll
-                for (int o = 1; o < kWarps; o *= 2) b = fminf(b, __shfl_xor_sync(0xffffffffu, b, o));
+                for (int o = 1; o < W; o *= 2) b = fminf(b, __shfl_xor_sync(0xffffffffu, b, o));
                 bound = fmaxf(bound, b);
-            }
-#pragma unroll
-            for (int y = 0; y < A; ++y)
-                if (top[y] >= bound) {
-                    const int64_t first = row.first(q0 + y * kThreads + threadIdx.x);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float x[2];
-                        unpack2(v[y].pair(e), x[0], x[1]);
-#pragma unroll
-                        for (int h = 0; h < 2; ++h)
-                            if (x[h] >= bound) {
-                                const int at = atomicAdd(&count, 1);
-                                if (at < kList) list[at] = key_of(x[h], static_cast<uint32_t>(first + 2 * e + h));
-                            }
+                if (entries > kWarpList / 4 && entries <= kWarpList) {       // those that the new bound leaves move up
+                    const uint32_t least_order = order_of(bound) & 0xffff0000u;
+                    int kept = 0;
+                    __syncwarp();
+                    for (int q = 0; q < entries; q += 32) {
+                        const uint32_t entry = q + lane < entries ? list[warp * kWarpList + q + lane] : 0;
+                        const uint32_t some = __ballot_sync(0xffffffffu, q + lane < entries && entry >= least_order);
+                        if (some >> lane & 1) list[warp * kWarpList + kept + __popc(some & ((1u << lane) - 1))] = entry;
+                        kept += __popc(some);
+                        __syncwarp();
                     }
+                    entries = kept;
                 }
+            }
+            if (__any_sync(0xffffffffu, m_round >= bound)) {
+#pragma unroll
+                for (int y = 0; y < A; ++y) {
+                    const uint32_t some = __ballot_sync(0xffffffffu, top[y] >= bound);
+                    const int at = entries + __popc(some & ((1u << lane) - 1));
+                    if (top[y] >= bound && at < kWarpList)
+                        list[warp * kWarpList + at] = (order_of(top[y]) & 0xffff0000u) | static_cast<uint32_t>((round * A + y) * 32 + lane);
+                    entries += __popc(some);
+                }
+            }
         }
     }
-    if (listed && round > 0) {
-        const float least = lanes_largest(t.m, mine);
-        if (lane == 0) bounds[warp] = least;
+    if (listed) {
+        const float least = few ? lanes_largest(t.m, mine) : lanes_many(most, mine);
+        if (lane == 0) { bounds[warp] = least; if (entries > kWarpList) atomicAdd(&over, 1); }
     }
     // the CTA's statistics, then the row's
 #pragma unroll
@@ -385,49 +439,57 @@ __global__ void __launch_bounds__(kThreads, 5) token_logp_kernel(const __grid_co
     if (lane == 0) stats[warp] = t;
     __syncthreads();
     t = stats[0];
-    for (int w = 1; w < kWarps; ++w) t = join(t, stats[w], c);
+    for (int w = 1; w < W; ++w) t = join(t, stats[w], c);
     int n = 0;
     if (TOP && row.begin < row.end) {
-        if (listed && count <= kList && t.s < kInf) {        // (a NaN is not below it)
+        bool done = false;
+        if (listed && over == 0 && t.s < kInf) {     // (a NaN is not below it)
             float b = bounds[0];
 #pragma unroll
-            for (int w = 1; w < kWarps; ++w) b = fminf(b, bounds[w]);
-            const uint64_t least = static_cast<uint64_t>(order_of(b)) << 32;
-            n = count;
-            for (int q = threadIdx.x; q < n; q += kThreads)
-                if (list[q] >= least) {
-                    const int at = atomicAdd(&thin_count, 1);
-                    if (at < kCounted) thin[at] = list[q];
+            for (int w = 1; w < W; ++w) b = fminf(b, bounds[w]);
+            const uint32_t least = order_of(b) & 0xffff0000u;
+            for (int q = lane; q < entries; q += 32) {
+                const uint32_t entry = list[warp * kWarpList + q];
+                if (entry < least) continue;         // of a maximum below the last bound
+                const int at = row.begin + static_cast<int>(entry >> 5 & 0x7ffu) * NT + warp * 32 + static_cast<int>(entry & 31);
+                Eight<T> v;
+                row.load(at, v);
+                for (int e = 0; e < 8; ++e) {
+                    const float x = v.at(e);
+                    if (!(x >= b)) continue;
+                    const int to = atomicAdd(&thin_count, 1);
+                    if (to < kMaxKeys) thin[to] = key_of(x, static_cast<uint32_t>(row.first(at) + e));
                 }
+            }
             __syncthreads();
-            if (thin_count <= kCounted) {
-                n = thin_count;
-                for (int q = threadIdx.x; q < n; q += kThreads) {
+            n = thin_count;
+            done = n <= kMaxKeys;
+            if (n <= kCounted) {
+                for (int q = threadIdx.x; q < n; q += NT) {
                     const uint64_t k = thin[q];
                     int above = 0;
                     for (int r = 0; r < n; ++r) above += thin[r] > k;
-                    list[above] = k;
+                    ordered[above] = k;
                 }
                 __syncthreads();
-            } else {
-                int size = 1;
-                while (size < n) size *= 2;
-                sort_keys(list, n, size);
+            } else if (done) {
+                for (int q = threadIdx.x; q < n; q += NT) ordered[q] = thin[q];
+                sort_keys<NT>(ordered, n);
             }
-        } else {
-            n = select_keys(row, a.topk, list, reinterpret_cast<int*>(thin), scratch);
-            int size = 1;
-            while (size < n) size *= 2;
-            sort_keys(list, n, size);
+        }
+        if (!done) {
+            __syncthreads();
+            n = select_keys<T, NT>(row, a.topk, ordered, reinterpret_cast<int*>(thin), scratch);
+            sort_keys<NT>(ordered, n);
         }
         n = min(n, a.topk);
     }
     if (parts > 1) {
-        if (threadIdx.x == 0) { stats[kWarps] = t; scratch[3] = n; }
+        if (threadIdx.x == 0) { stats[W] = t; scratch[3] = n; }
         cluster_sync();
         Stat all{kLowest, 0.f, 0.f};
         for (int p = 0; p < parts; ++p) {
-            const float* f = &stats[kWarps].m;
+            const float* f = &stats[W].m;
             const Stat y{peer_float(f, p), peer_float(f + 1, p), peer_float(f + 2, p)};
             all = p ? join(all, y, c) : y;
         }
@@ -447,7 +509,7 @@ __global__ void __launch_bounds__(kThreads, 5) token_logp_kernel(const __grid_co
         if (parts > 1) cluster_sync();
         return;
     }
-    auto write = [&](int at, uint64_t k) {           // k = 0: none left
+    const auto write = [&](int at, uint64_t k) {           // k = 0: none left
         if (a.top_logp) a.top_logp[i * a.ld_top_logp + at] = k ? (logit_of(static_cast<uint32_t>(k >> 32)) - t.m) * a.inv_tau - log_s : -kInf;
         if (a.top_ids) {
             const int64_t id = k ? static_cast<int64_t>(~static_cast<uint32_t>(k)) : -1;
@@ -456,25 +518,25 @@ __global__ void __launch_bounds__(kThreads, 5) token_logp_kernel(const __grid_co
         }
     };
     if (parts == 1) {
-        for (int q = threadIdx.x; q < a.topk; q += kThreads) write(q, q < n ? list[q] : 0);
+        for (int q = threadIdx.x; q < a.topk; q += NT) write(q, q < n ? ordered[q] : 0);
         return;
     }
     // each CTA's keys go where they rank among all of them
     int total = 0;
-    for (int p = 0; p < parts; ++p) total += static_cast<int>(__float_as_int(peer_float(reinterpret_cast<const float*>(scratch + 3), p)));
-    for (int q = threadIdx.x; q < n; q += kThreads) {
-        const uint64_t k = list[q];
+    for (int p = 0; p < parts; ++p) total += __float_as_int(peer_float(reinterpret_cast<const float*>(scratch + 3), p));
+    for (int q = threadIdx.x; q < n; q += NT) {
+        const uint64_t k = ordered[q];
         int rank = q;
         for (int p = 1; p < parts && rank < a.topk; ++p) {
             const uint32_t peer = (part + p) % parts;
             int lo = 0, hi = __float_as_int(peer_float(reinterpret_cast<const float*>(scratch + 3), peer));
-            while (lo < hi) { const int mid = (lo + hi) >> 1; if (peer_key(list + mid, peer) > k) lo = mid + 1; else hi = mid; }
+            while (lo < hi) { const int mid = (lo + hi) >> 1; if (peer_key(ordered + mid, peer) > k) lo = mid + 1; else hi = mid; }
             rank += lo;
         }
         if (rank < a.topk) write(rank, k);
     }
     if (part == 0)
-        for (int q = total + threadIdx.x; q < a.topk; q += kThreads) write(q, 0);
+        for (int q = total + threadIdx.x; q < a.topk; q += NT) write(q, 0);
     cluster_sync();
 }
 
@@ -487,7 +549,7 @@ __global__ void __launch_bounds__(kThreads) token_logp_grad_kernel(const __grid_
     const int part = static_cast<int>(blockIdx.x % parts);
     const T* z = static_cast<const T*>(a.z) + i * a.ldz;
     T* dz = static_cast<T*>(a.dz) + i * a.lddz;
-    const RowVectors<T> row(z, a.vocab, part, parts);
+    const RowVectors<T> row(z, static_cast<int>(a.vocab), part, parts);
     const int64_t y = a.tokens.p ? a.tokens.at(i) : -1;
     const bool counted = y >= 0 && y < a.vocab;
     const float lse = a.lse[i];
@@ -496,10 +558,10 @@ __global__ void __launch_bounds__(kThreads) token_logp_grad_kernel(const __grid_
     const float bonus = a.dentropy && some ? a.dentropy[i] * a.inv_tau : 0.f, h = bonus != 0.f ? a.entropy[i] : 0.f;
     const float tail = a.inv_tau;
     const bool wide = (reinterpret_cast<uintptr_t>(dz) & 15) == (reinterpret_cast<uintptr_t>(z) & 15);
-    for (int64_t q = row.begin + threadIdx.x; q < row.end; q += kThreads) {
+    for (int q = row.begin + threadIdx.x; q < row.end; q += kThreads) {
         float v[8];
         row.load(q, v);
-        const int64_t j = row.first(q);
+        const int j = row.first(q);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float lp = v[e] * tail - lse, p = exp2_fast(lp * kLog2e);
@@ -519,6 +581,16 @@ __global__ void __launch_bounds__(kThreads) token_logp_grad_kernel(const __grid_
     }
 }
 
+template <class T, int NT>
+auto logp_kernel_of(const TokenLogp& a) {
+    return a.entropy ? (a.topk ? token_logp_kernel<T, true, true, NT> : token_logp_kernel<T, true, false, NT>)
+                     : (a.topk ? token_logp_kernel<T, false, true, NT> : token_logp_kernel<T, false, false, NT>);
+}
+template <class T>
+auto logp_kernel(const TokenLogp& a, int threads) {
+    return threads == 64 ? logp_kernel_of<T, 64>(a) : threads == 128 ? logp_kernel_of<T, 128>(a) : logp_kernel_of<T, 256>(a);
+}
+
 }  // namespace
 
 cudaError_t token_logp(const TokenLogp& a, int dtype, cudaStream_t st) {
@@ -526,21 +598,16 @@ cudaError_t token_logp(const TokenLogp& a, int dtype, cudaStream_t st) {
     // CTAs a row: a cluster where the rows leave SMs idle, each CTA with 4096 logits at least
     int parts = 1;
     while (parts < 8 && a.rows * parts * 2 <= 2 * 152 && a.vocab >= parts * 2 * 4096) parts *= 2;
+    const int threads = a.vocab <= 2048 ? 64 : a.vocab <= 4096 ? 128 : 256;
     cudaLaunchAttribute attr[2]{};
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = parts; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(static_cast<unsigned>(a.rows * parts)); cfg.blockDim = kThreads; cfg.stream = st;
+    cfg.gridDim = dim3(static_cast<unsigned>(a.rows * parts)); cfg.blockDim = threads; cfg.stream = st;
     cfg.attrs = attr; cfg.numAttrs = parts > 1 ? 2 : 1;
-    using H = __nv_bfloat16;
-    const auto kernel = dtype == GLR_BF16
-        ? (a.entropy ? (a.topk ? token_logp_kernel<H, true, true> : token_logp_kernel<H, true, false>)
-                     : (a.topk ? token_logp_kernel<H, false, true> : token_logp_kernel<H, false, false>))
-        : (a.entropy ? (a.topk ? token_logp_kernel<float, true, true> : token_logp_kernel<float, true, false>)
-                     : (a.topk ? token_logp_kernel<float, false, true> : token_logp_kernel<float, false, false>));
-    return cudaLaunchKernelEx(&cfg, kernel, a, parts);
+    return cudaLaunchKernelEx(&cfg, dtype == GLR_BF16 ? logp_kernel<__nv_bfloat16>(a, threads) : logp_kernel<float>(a, threads), a, parts);
 }
 
 cudaError_t token_logp_grad(const TokenLogpGrad& a, int dtype, cudaStream_t st) {
