@@ -568,7 +568,7 @@ int glr_embedding(const glr_embedding_args* a, void* stream);
  * occur; with accumulate 1 it is added to what dE[i] holds (the gradient of an output layer that
  * shares the matrix).  dE is a host array of `nodes` device pointers to matrices that do not overlap;
  * 1 <= nodes <= GLR_MAX_NODES, nodes * rows <= 2^30.  workspace (device memory, 16-byte aligned, for one call at a
- * time) holds the sorted tokens: as many bytes as glr_embedding_grad_workspace says.               */
+ * time) holds the sorted tokens of many rows: as many bytes as glr_embedding_grad_workspace says.   */
 typedef struct glr_embedding_grad_args {
     int64_t nodes, rows, vocab, d;
     const void* dY; int64_t lddy;

@@ -1,11 +1,11 @@
 // Embedding lookup with scaling, and every node's gradient of the embedding by sorted tokens.
 //
 // The gradient of row v is scale times the sum of the rows of dY whose token is v, in the order of the rows, so its result
-// does not depend on what runs when.  Three steps: the tokens of up to kChunk consecutive rows of a node are sorted, stably, by a
-// CTA (least significant digits first, a warp's rank among equal digits by matching lanes); where each tile of kTileRows
-// vocabulary rows begins in a chunk is written beside them; then a CTA takes a tile's rows of 256 columns, finds each row's
-// occurrences in the chunks and adds them up, one warp a row, or all its warps where there are many.  A token outside the
-// vocabulary is sorted behind all others and is nobody's.
+// does not depend on what runs when.  A CTA takes kTileRows rows of the vocabulary and up to 512 columns, puts the rows of dY that
+// belong to them in order of (token, row), and adds them up, one warp a row, or all its warps where there are many.
+// Where it finds them depends on the node's rows: up to kScan, among all of the node's tokens; beyond, in chunks of kChunk rows that a
+// kernel before has sorted by their tokens, stably, with the place where each tile begins.  Both order by ranks among equal
+// digits (warps take consecutive stretches; lanes with the same digit are matched).  A token outside the vocabulary is nobody's.
 // Bound by HBM: the gradient of the whole vocabulary is written for every node.
 #include <algorithm>
 
@@ -130,16 +130,20 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(Index tokens, int64_
         out.row[at * kChunk + q] = static_cast<int32_t>(first + from[b][q]);
     }
     // start[t] = the first place whose token lies in tile t or behind it
-    for (int q = threadIdx.x; q <= n; q += kSortThreads) {
-        const int64_t tile = q < n ? min(out.tiles, static_cast<int64_t>(key[b][q] == vocab ? out.tiles : key[b][q] / kTileRows)) : out.tiles;
-        const int64_t last = q == 0 ? -1 : key[b][q - 1] == vocab ? out.tiles : key[b][q - 1] / kTileRows;
-        for (int64_t t = last + 1; t <= tile; ++t) start[t] = q;
+    for (int64_t t = threadIdx.x; t <= out.tiles; t += kSortThreads) {
+        const int64_t least = min(t * kTileRows, static_cast<int64_t>(vocab));
+        int lo = 0, hi = n;
+        while (lo < hi) { const int m = (lo + hi) >> 1; if (key[b][m] < least) lo = m + 1; else hi = m; }
+        start[t] = lo;
     }
 }
 
 // ---- the sums ----------------------------------------------------------------------------------------------------
-constexpr int kGradWarps = 8, kSlice = 256;          // columns a CTA
+constexpr int kGradWarps = 8, kGradThreads = kGradWarps * 32, kSlice = 256;          // columns at a time
 constexpr int kMany = 64;                            // occurrences from which on all warps share a row
+constexpr int kScan = 1024;                          // a node's rows up to which its tokens are looked through
+constexpr int kBatches = 4, kPlaces = kBatches * kGradThreads;       // entries of a tile in shared memory
+constexpr int kChunksAtOnce = kGradThreads;
 
 // The lane's eight columns of a slice: neighbouring ones, or 32 apart where rows are not on 16 bytes.
 template <class T, bool WIDE>
@@ -183,12 +187,24 @@ __device__ __forceinline__ int2 find(const int32_t* token, int s, int e, int v) 
     return make_int2(from, lo);
 }
 
-// Adds up the rows of token v in the order of their chunks; `part` of `parts` takes every parts-th group of kGroup
-// occurrences (of each chunk's).  Returns how many there are.
+// Adds up the rows `row[0 .. n)` of dY: every parts-th group of kGroup of them, in their order.
 constexpr int kGroup = 8;
 template <class T, bool WIDE>
-__device__ __forceinline__ int64_t add_token(const EmbeddingGrad& a, const Sorted& s, int64_t node, int64_t tile, int v, const T* dy, int left,
-                                             bool count_only, int part, int parts, float (&sum)[8]) {
+__device__ __forceinline__ void add_rows(const T* dy, int64_t lddy, const int32_t* row, int n, int part, int parts, int left, float (&sum)[8]) {
+    const int lane = threadIdx.x & 31;
+    for (int q = part * kGroup; q < n; q += parts * kGroup) {
+        if (n - q >= kGroup) {
+#pragma unroll
+            for (int u = 0; u < kGroup; ++u) add_row<T, WIDE>(dy + row[q + u] * lddy, lane, left, sum);
+        } else {
+            for (int u = q; u < n; ++u) add_row<T, WIDE>(dy + row[u] * lddy, lane, left, sum);
+        }
+    }
+}
+// ... of token v in the chunks, one after the other, for tiles whose entries do not fit in shared memory.  Returns how many.
+template <class T, bool WIDE>
+__device__ __noinline__ int64_t add_token(const Sorted& s, int64_t node, int64_t tile, int v, const T* dy, int64_t lddy, int left, bool count_only,
+                                          int part, int parts, float (&sum)[8]) {
     const int lane = threadIdx.x & 31;
     int64_t n = 0;
     for (int64_t c0 = 0; c0 < s.chunks; c0 += 32) {
@@ -202,49 +218,148 @@ __device__ __forceinline__ int64_t add_token(const EmbeddingGrad& a, const Sorte
             const int c = __ffs(some) - 1;
             const int from = __shfl_sync(0xffffffffu, mine.x, c), to = __shfl_sync(0xffffffffu, mine.y, c);
             n += to - from;
-            if (count_only) continue;
-            const int32_t* row = s.row + s.at(node, c0 + c) * kChunk;
-            for (int q = from + part * kGroup; q < to; q += parts * kGroup) {
-                const int32_t* r = row + q;
-                const int m = min(kGroup, to - q);
-                if (m == kGroup) {
-#pragma unroll
-                    for (int u = 0; u < kGroup; ++u) add_row<T, WIDE>(dy + r[u] * a.lddy, lane, left, sum);
-                } else {
-                    for (int u = 0; u < m; ++u) add_row<T, WIDE>(dy + r[u] * a.lddy, lane, left, sum);
-                }
-            }
+            if (!count_only) add_rows<T, WIDE>(dy, lddy, s.row + s.at(node, c0 + c) * kChunk + from, to - from, part, parts, left, sum);
         }
     }
     return n;
 }
 
+// A whole tile whose entries do not fit in shared memory, each row's looked for in all chunks.
 template <class T, class G, bool WIDE>
-__global__ void __launch_bounds__(kGradWarps * 32) embedding_grad_kernel(const __grid_constant__ EmbeddingGrad a, const Sorted s) {
+__device__ __noinline__ void add_tile(const EmbeddingGrad& a, const Sorted& s, int64_t node, int64_t tile, int rows, int64_t col0, int slices,
+                                      float (*part)[kSlice]) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int64_t col = col0; col < col0 + slices * kSlice && col < a.d; col += kSlice) {
+        const int left = static_cast<int>(min(static_cast<int64_t>(kSlice), a.d - col));
+        const T* dy = static_cast<const T*>(a.dY) + node * a.rows * a.lddy + col;
+        G* de = static_cast<G*>(a.dE[node]) + col;
+        for (int r = 0; r < rows; ++r) {
+            const int v = static_cast<int>(tile * kTileRows) + r;
+            float sum[8] = {};
+            const int64_t c = add_token<T, WIDE>(s, node, tile, v, dy, a.lddy, left, false, warp, kGradWarps, sum);
+            if (c == 0 && a.accumulate) continue;    // the same for the whole CTA
+#pragma unroll
+            for (int e = 0; e < 8; ++e) part[warp][e * 32 + lane] = sum[e];
+            __syncthreads();
+            if (warp == 0) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    for (int w = 1; w < kGradWarps; ++w) sum[e] += part[w][e * 32 + lane];
+                finish_row<G, WIDE>(de + v * a.d, lane, left, a.accumulate, sum, a.scale);
+            }
+            __syncthreads();
+        }
+    }
+}
+
+// The sum over the CTA's threads before this one, and over all of them.
+__device__ __forceinline__ int2 scan_threads(int v, int* carry) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int sum = v;
+    for (int o = 1; o < 32; o *= 2) { const int y = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += y; }
+    if (lane == 31) carry[warp] = sum;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int w = 0; w < kGradWarps; ++w) { before += w < warp ? carry[w] : 0; all += carry[w]; }
+    return make_int2(before + sum - v, all);
+}
+
+template <class T, class G, bool WIDE>
+__global__ void __launch_bounds__(kGradThreads, 5) embedding_grad_kernel(const __grid_constant__ EmbeddingGrad a, const Sorted s, bool scan, int slices) {
     chain_begin();
     __shared__ float part[kGradWarps][kSlice];
-    __shared__ uint8_t many[kTileRows];
+    __shared__ int32_t list[kPlaces];
+    __shared__ int off[kTileRows + 1];
+    __shared__ uint16_t count[kGradWarps][kTileRows];
+    __shared__ int2 chunk_part[kChunksAtOnce];       // of the chunks' entries: the tile's first place, the entries before it
+    __shared__ int carry[kGradWarps];
+    __shared__ uint8_t many[kTileRows];              // rows that all warps share
+    __shared__ int some;                             // their number
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t tile = blockIdx.x, node = blockIdx.z, col = static_cast<int64_t>(blockIdx.y) * kSlice;
-    const int left = static_cast<int>(min(static_cast<int64_t>(kSlice), a.d - col));
-    const T* dy = static_cast<const T*>(a.dY) + node * a.rows * a.lddy + col;
-    G* de = static_cast<G*>(a.dE[node]) + col;
+    const int64_t tile = blockIdx.x, node = blockIdx.z;
     const int rows = static_cast<int>(min(static_cast<int64_t>(kTileRows), a.vocab - tile * kTileRows));
-    for (int r = warp; r < rows; r += kGradWarps) {
-        const int v = static_cast<int>(tile * kTileRows) + r;
-        float sum[8] = {};
-        const int64_t n = add_token<T, WIDE>(a, s, node, tile, v, dy, left, true, 0, 1, sum);
-        if (lane == 0) many[r] = n >= kMany;
-        if (n >= kMany || (n == 0 && a.accumulate)) continue;
-        if (n > 0) add_token<T, WIDE>(a, s, node, tile, v, dy, left, false, 0, 1, sum);
-        finish_row<G, WIDE>(de + v * a.d, lane, left, a.accumulate, sum, a.scale);
+    const int64_t v0 = tile * kTileRows;
+    const T* dy0 = static_cast<const T*>(a.dY) + node * a.rows * a.lddy;
+    // the tile's entries: the node's tokens, or those of the chunks one after the other
+    int n = static_cast<int>(a.rows);
+    bool fits = true;
+    if (!scan) {
+        fits = s.chunks <= kChunksAtOnce;
+        int mine = 0, from = 0;
+        if (fits && threadIdx.x < s.chunks) {
+            const int32_t* start = s.start + s.at(node, threadIdx.x) * (s.tiles + 1) + tile;
+            from = start[0];
+            mine = start[1] - from;
+        }
+        const int2 sum = scan_threads(mine, carry);
+        chunk_part[threadIdx.x] = make_int2(from, sum.x);
+        n = sum.y;
+        fits = fits && n <= kPlaces;
     }
+    for (int q = threadIdx.x; q < kGradWarps * kTileRows; q += kGradThreads) (&count[0][0])[q] = 0;
+    if (threadIdx.x == 0) some = 0;
     __syncthreads();
-    for (int r = 0; r < rows; ++r) {
-        if (!many[r]) continue;                      // the same for the whole CTA
-        const int v = static_cast<int>(tile * kTileRows) + r;
+    if (!fits) {                                     // the same for the whole CTA
+        add_tile<T, G, WIDE>(a, s, node, tile, rows, static_cast<int64_t>(blockIdx.y) * slices * kSlice, slices, part);
+        return;
+    }
+    {
+        // each warp ranks a stretch of entries; what it knows of them stays in registers
+        const int stretch = (n + kGradThreads - 1) / kGradThreads;
+        int32_t row[kBatches];
+        uint32_t rank[kBatches];                     // the token's row of the tile, and its rank among the warp's
+#pragma unroll
+        for (int u = 0; u < kBatches; ++u) {
+            rank[u] = kTileRows << 16;
+            row[u] = 0;
+            if (u < stretch) {                       // the same for the whole CTA
+                const int x = (warp * stretch + u) * 32 + lane;
+                int r = kTileRows;
+                if (x < n) {
+                    if (scan) {
+                        const int64_t t = a.tokens.at(node * a.rows + x) - v0;
+                        row[u] = x;
+                        if (t >= 0 && t < rows) r = static_cast<int>(t);
+                    } else {
+                        int c = 0, end = static_cast<int>(s.chunks);         // the last chunk that begins at x or before
+                        while (end - c > 1) { const int m = (c + end) >> 1; if (chunk_part[m].y <= x) c = m; else end = m; }
+                        const int64_t at = s.at(node, c) * kChunk + chunk_part[c].x + (x - chunk_part[c].y);
+                        row[u] = s.row[at];
+                        r = static_cast<int>(s.token[at] - v0);
+                    }
+                }
+                if (__any_sync(0xffffffffu, r < kTileRows)) {
+                    const uint32_t same = __match_any_sync(0xffffffffu, r), before = same & ((1u << lane) - 1);
+                    if (r < kTileRows) rank[u] = static_cast<uint32_t>(r) << 16 | (count[warp][r] + __popc(before));
+                    __syncwarp();
+                    if (r < kTileRows && before == 0) count[warp][r] += static_cast<uint16_t>(__popc(same));
+                    __syncwarp();
+                }
+            }
+        }
+        __syncthreads();
+        int sum = 0;
+        if (threadIdx.x < kTileRows)
+            for (int w = 0; w < kGradWarps; ++w) { const int c = count[w][threadIdx.x]; count[w][threadIdx.x] = static_cast<uint16_t>(sum); sum += c; }
+        const int2 place = scan_threads(sum, carry);
+        if (threadIdx.x < kTileRows) off[threadIdx.x] = place.x;
+        if (threadIdx.x == 0) off[kTileRows] = place.y;
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kBatches; ++u) {
+            const int r = static_cast<int>(rank[u] >> 16);
+            if (r < kTileRows) list[off[r] + count[warp][r] + (rank[u] & 0xffffu)] = row[u];
+        }
+        __syncthreads();
+    }
+    const int64_t col0 = static_cast<int64_t>(blockIdx.y) * slices * kSlice;
+    const int width = static_cast<int>(min(static_cast<int64_t>(slices) * kSlice, a.d - col0));
+    const T* dy = dy0 + col0;
+    G* de = static_cast<G*>(a.dE[node]) + v0 * a.d + col0;
+    const auto rows_of = [&](int r, int from, int parts, int c0) {
         float sum[8] = {};
-        add_token<T, WIDE>(a, s, node, tile, v, dy, left, false, warp, kGradWarps, sum);
+        add_rows<T, WIDE>(dy + c0, a.lddy, list + off[r], off[r + 1] - off[r], from, parts, width - c0, sum);
+        if (parts == 1) { finish_row<G, WIDE>(de + r * a.d + c0, lane, width - c0, a.accumulate, sum, a.scale); return; }
 #pragma unroll
         for (int e = 0; e < 8; ++e) part[warp][e * 32 + lane] = sum[e];
         __syncthreads();
@@ -252,20 +367,41 @@ __global__ void __launch_bounds__(kGradWarps * 32) embedding_grad_kernel(const _
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 for (int w = 1; w < kGradWarps; ++w) sum[e] += part[w][e * 32 + lane];
-            finish_row<G, WIDE>(de + v * a.d, lane, left, a.accumulate, sum, a.scale);
+            finish_row<G, WIDE>(de + r * a.d + c0, lane, width - c0, a.accumulate, sum, a.scale);
         }
         __syncthreads();
+    };
+    for (int r = warp; r < rows; r += kGradWarps) {
+        const int n_r = off[r + 1] - off[r];
+        if (n_r == 0) {
+            if (a.accumulate) continue;
+            if (WIDE) {
+                constexpr int kPer = 16 / sizeof(G);
+                for (int j = lane * kPer; j < width; j += 32 * kPer) *reinterpret_cast<uint4*>(de + r * a.d + j) = make_uint4(0, 0, 0, 0);
+            } else {
+                for (int j = lane; j < width; j += 32) put(de + r * a.d + j, 0.f);
+            }
+        } else if (n_r >= kMany) {
+            if (lane == 0) many[atomicAdd(&some, 1)] = static_cast<uint8_t>(r);
+        } else {
+            for (int c0 = 0; c0 < width; c0 += kSlice) rows_of(r, 0, 1, c0);
+        }
     }
+    __syncthreads();
+    for (int q = 0; q < some; ++q)
+        for (int c0 = 0; c0 < width; c0 += kSlice) rows_of(many[q], warp, kGradWarps, c0);
 }
 
 bool on16(const void* p, int64_t ld_bytes) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld_bytes % 16 == 0; }
 
 template <class T, class G>
-cudaError_t launch_grad(const EmbeddingGrad& a, const Sorted& s, bool wide, cudaStream_t st) {
-    const int64_t slices = (a.d + kSlice - 1) / kSlice;
-    const dim3 grid(static_cast<unsigned>(s.tiles), static_cast<unsigned>(slices), static_cast<unsigned>(a.nodes));
-    return wide ? launch_chain(embedding_grad_kernel<T, G, true>, grid, kGradWarps * 32, 0, st, a, s)
-                : launch_chain(embedding_grad_kernel<T, G, false>, grid, kGradWarps * 32, 0, st, a, s);
+cudaError_t launch_grad(const EmbeddingGrad& a, const Sorted& s, bool scan, bool wide, cudaStream_t st) {
+    // columns a CTA: one slice where that takes all, or where two would leave SMs idle
+    const int64_t all = (a.d + kSlice - 1) / kSlice;
+    const int slices = all > 1 && s.tiles * a.nodes * ((all + 1) / 2) >= 152 * 8 ? 2 : 1;
+    const dim3 grid(static_cast<unsigned>(s.tiles), static_cast<unsigned>((all + slices - 1) / slices), static_cast<unsigned>(a.nodes));
+    return wide ? launch_chain(embedding_grad_kernel<T, G, true>, grid, kGradThreads, 0, st, a, s, scan, slices)
+                : launch_chain(embedding_grad_kernel<T, G, false>, grid, kGradThreads, 0, st, a, s, scan, slices);
 }
 
 }  // namespace
@@ -282,6 +418,7 @@ cudaError_t lookup(const Lookup& a, int dtype, cudaStream_t st) {
 }
 
 int64_t embedding_grad_bytes(int64_t nodes, int64_t rows, int64_t vocab) {
+    if (rows <= kScan) return 0;
     const Sorted s = sorted_of(nodes, rows, vocab, nullptr);
     return nodes * s.chunks * (2 * kChunk + s.tiles + 1) * 4;
 }
@@ -289,7 +426,8 @@ int64_t embedding_grad_bytes(int64_t nodes, int64_t rows, int64_t vocab) {
 cudaError_t embedding_grad(const EmbeddingGrad& a, int dtype, int grad_dtype, cudaStream_t st) {
     if (a.vocab == 0 || a.d == 0) return cudaSuccess;
     const Sorted s = sorted_of(a.nodes, a.rows, a.vocab, a.workspace);
-    if (s.chunks > 0) {
+    const bool scan = a.rows <= kScan;
+    if (!scan) {
         int bits = 0;
         while ((int64_t{1} << bits) <= a.vocab) ++bits;          // of the largest key, vocab
         constexpr int kBytes = kChunk * 2 * (4 + 2);
@@ -298,15 +436,15 @@ cudaError_t embedding_grad(const EmbeddingGrad& a, int dtype, int grad_dtype, cu
             e = launch_chain(sort_kernel, dim3(static_cast<unsigned>(s.chunks), static_cast<unsigned>(a.nodes)), kSortThreads, kBytes, st,
                              a.tokens, a.rows, static_cast<int>(a.vocab), bits, s);
         if (e != cudaSuccess) return e;
-    } else if (a.accumulate) {
+    } else if (a.rows == 0 && a.accumulate) {
         return cudaSuccess;
     }
     const int64_t es = dtype == GLR_BF16 ? 2 : 4, gs = grad_dtype == GLR_BF16 ? 2 : 4;
     bool wide = on16(a.dY, a.nodes * a.rows > 1 ? a.lddy * es : 0) && a.d % 8 == 0;
     for (int64_t i = 0; i < a.nodes; ++i) wide = wide && on16(a.dE[i], a.d * gs);
     if (dtype == GLR_BF16)
-        return grad_dtype == GLR_BF16 ? launch_grad<__nv_bfloat16, __nv_bfloat16>(a, s, wide, st) : launch_grad<__nv_bfloat16, float>(a, s, wide, st);
-    return grad_dtype == GLR_BF16 ? launch_grad<float, __nv_bfloat16>(a, s, wide, st) : launch_grad<float, float>(a, s, wide, st);
+        return grad_dtype == GLR_BF16 ? launch_grad<__nv_bfloat16, __nv_bfloat16>(a, s, scan, wide, st) : launch_grad<__nv_bfloat16, float>(a, s, scan, wide, st);
+    return grad_dtype == GLR_BF16 ? launch_grad<float, __nv_bfloat16>(a, s, scan, wide, st) : launch_grad<float, float>(a, s, scan, wide, st);
 }
 
 }  // namespace rows

@@ -268,7 +268,7 @@ __device__ __forceinline__ float lanes_largest(float v, int j) {
         }
     return __shfl_sync(0xffffffffu, v, j - 1);
 }
-// A value that at least j of the lanes' n values each reach, j <= 32 n: ten bisections between the least and the largest of
+// A value that at least j of the lanes' n values each reach, j <= 32 n: sixteen bisections between the least and the largest of
 // them, as integers of the same order (1 is that of no logit, and below all of them).
 template <int N>
 __device__ __noinline__ float lanes_many(const float (&v)[N], int j) {
@@ -277,7 +277,7 @@ __device__ __noinline__ float lanes_many(const float (&v)[N], int j) {
     for (int q = 0; q < N; ++q) { o[q] = order_of(v[q]); lo = min(lo, o[q]); hi = max(hi, o[q]); }
     lo = __reduce_min_sync(0xffffffffu, lo);
     hi = __reduce_max_sync(0xffffffffu, hi);
-    for (int it = 0; it < 10 && hi - lo > 1; ++it) {
+    for (int it = 0; it < 16 && hi - lo > 1; ++it) {
         const uint32_t mid = lo + (hi - lo) / 2;
         int n = 0;
 #pragma unroll

@@ -87,8 +87,8 @@ GOOD = {
     ("glr_embedding_grad", dict(accumulate=2), "accumulate"), ("glr_embedding_grad", dict(dE=None), "dE is null"),
     ("glr_embedding_grad", dict(dE=A(HOLE)), "dE[1]"), ("glr_embedding_grad", dict(dE=A(TWICE)), "twice"),
     ("glr_embedding_grad", dict(lddy=7), "dY null"), ("glr_embedding_grad", dict(scale=float("nan")), "scale"),
-    ("glr_embedding_grad", dict(workspace=None), "workspace"), ("glr_embedding_grad", dict(workspace_bytes=100), "workspace"),
-    ("glr_embedding_grad", dict(workspace=P + 8), "workspace"), ("glr_embedding_grad", dict(vocab=-1), "vocab"),
+    ("glr_embedding_grad", dict(rows=5000, workspace=None), "workspace"), ("glr_embedding_grad", dict(rows=5000, workspace_bytes=100), "workspace"),
+    ("glr_embedding_grad", dict(rows=5000, workspace=P + 8), "workspace"), ("glr_embedding_grad", dict(vocab=-1), "vocab"),
     ("glr_checkpoint_pack", dict(dtype=-1), "unknown dtype"), ("glr_checkpoint_pack", dict(cols=1 << 25), "cols"),
     ("glr_checkpoint_pack", dict(X=None), "X null"), ("glr_checkpoint_pack", dict(codes=None), "codes"),
     ("glr_checkpoint_pack", dict(scales=None), "scales"), ("glr_checkpoint_pack", dict(ld_codes=32), "ld <"),
@@ -147,7 +147,7 @@ def test_workspace_queries(lib):
         assert getattr(lib, name + "_workspace")(ctypes.byref(cls(**{**good, **change})), ctypes.byref(n)) == 0
         return n.value
 
-    assert need("glr_embedding_grad") > 0 and need("glr_embedding_grad", rows=0) == 0 and need("glr_embedding_grad", d=0) == 0
+    assert need("glr_embedding_grad", rows=5000) > 0 and need("glr_embedding_grad", rows=0) == 0 and need("glr_embedding_grad", rows=5000, d=0) == 0
     assert need("glr_norm_grad") > 0 and need("glr_norm_grad", dweight=None) == 0
     both = need("glr_linear_grad_checkpoint")
     assert both >= 2 * 8 * 33 * 4
