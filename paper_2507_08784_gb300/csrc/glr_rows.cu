@@ -61,7 +61,7 @@ int check_embedding_grad(const char* who, const glr_embedding_grad_args* a) {
     return GLR_OK;
 }
 int64_t embedding_grad_need(const glr_embedding_grad_args* a) {
-    return a->vocab && a->d ? rows::embedding_grad_bytes(a->nodes, a->rows, a->vocab) : 0;
+    return a->vocab && a->d ? rows::embedding_grad_bytes(a->nodes, a->rows, a->vocab, a->d) : 0;
 }
 
 int check_norm_grad(const char* who, const glr_norm_grad_args* a) {

@@ -151,7 +151,7 @@ struct EmbeddingGrad {
     void* dE[GLR_MAX_NODES];
     void* workspace;
 };
-int64_t embedding_grad_bytes(int64_t nodes, int64_t rows, int64_t vocab);
+int64_t embedding_grad_bytes(int64_t nodes, int64_t rows, int64_t vocab, int64_t d);
 cudaError_t embedding_grad(const EmbeddingGrad& a, int dtype, int grad_dtype, cudaStream_t st);
 
 constexpr int kMaxNorm = GLR_MAX_NORM;

@@ -1,11 +1,12 @@
 // Embedding lookup with scaling, and every node's gradient of the embedding by sorted tokens.
 //
 // The gradient of row v is scale times the sum of the rows of dY whose token is v, in the order of the rows, so its result
-// does not depend on what runs when.  A CTA takes kTileRows rows of the vocabulary and up to 512 columns, puts the rows of dY that
-// belong to them in order of (token, row), and adds them up, one warp a row, or all its warps where there are many.
-// Where it finds them depends on the node's rows: up to kScan, among all of the node's tokens; beyond, in chunks of kChunk rows that a
-// kernel before has sorted by their tokens, stably, with the place where each tile begins.  Both order by ranks among equal
-// digits (warps take consecutive stretches; lanes with the same digit are matched).  A token outside the vocabulary is nobody's.
+// does not depend on what runs when.  A CTA takes 64 or 256 rows of the vocabulary and 256 columns and adds up the rows of dY that
+// belong to them, one warp a row, or all its warps where there are many.
+// Where it finds them depends on the node's rows: up to kScan it looks through the node's tokens and puts its own in order of
+// (token, row); beyond, chunks of kChunk rows have been sorted by their tokens, stably, by a kernel before, with the place where each
+// tile begins.  Both order by ranks among equal digits: warps take consecutive stretches, lanes with the same digit are matched.
+// A token outside the vocabulary is nobody's.
 // Bound by HBM: the gradient of the whole vocabulary is written for every node.
 #include <algorithm>
 
@@ -41,19 +42,25 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const __grid_con
 
 // ---- the tokens in order ---------------------------------------------------------------------------------------
 constexpr int kChunk = 4096, kSortThreads = 512, kSortWarps = kSortThreads / 32, kMine = kChunk / kSortThreads;
-constexpr int kTileRows = 64;
 constexpr int kDigit = 8, kDigits = 1 << kDigit;
 
 // A chunk's sorted tokens, the rows (of its node) that they come from, and where each tile's begin.
 struct Sorted {
     int32_t* token; int32_t* row; int32_t* start;
     int64_t chunks, tiles;                           // a node's
+    int tile_rows;
     __host__ __device__ int64_t at(int64_t node, int64_t chunk) const { return node * chunks + chunk; }
 };
-Sorted sorted_of(int64_t nodes, int64_t rows, int64_t vocab, void* workspace) {
+// A tile's rows: few where the tiles would leave SMs idle, and where a table of many would not have room for the chunks.
+constexpr int kFewRows = 64, kManyRows = 256;
+int tile_rows(int64_t nodes, int64_t rows, int64_t vocab, int64_t d) {
+    return rows <= 8 * kChunk && (vocab + kManyRows - 1) / kManyRows * nodes * ((d + 255) / 256) >= 152 * 5 ? kManyRows : kFewRows;
+}
+Sorted sorted_of(int64_t nodes, int64_t rows, int64_t vocab, int64_t d, void* workspace) {
     Sorted s{};
     s.chunks = (rows + kChunk - 1) / kChunk;
-    s.tiles = (vocab + kTileRows - 1) / kTileRows;
+    s.tile_rows = tile_rows(nodes, rows, vocab, d);
+    s.tiles = (vocab + s.tile_rows - 1) / s.tile_rows;
     const int64_t all = nodes * s.chunks;
     s.token = static_cast<int32_t*>(workspace);
     s.row = s.token + all * kChunk;
@@ -131,7 +138,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(Index tokens, int64_
     }
     // start[t] = the first place whose token lies in tile t or behind it
     for (int64_t t = threadIdx.x; t <= out.tiles; t += kSortThreads) {
-        const int64_t least = min(t * kTileRows, static_cast<int64_t>(vocab));
+        const int64_t least = min(t * out.tile_rows, static_cast<int64_t>(vocab));
         int lo = 0, hi = n;
         while (lo < hi) { const int m = (lo + hi) >> 1; if (key[b][m] < least) lo = m + 1; else hi = m; }
         start[t] = lo;
@@ -142,8 +149,6 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(Index tokens, int64_
 constexpr int kGradWarps = 8, kGradThreads = kGradWarps * 32, kSlice = 256;          // columns at a time
 constexpr int kMany = 64;                            // occurrences from which on all warps share a row
 constexpr int kScan = 1024;                          // a node's rows up to which its tokens are looked through
-constexpr int kBatches = 4, kPlaces = kBatches * kGradThreads;       // entries of a tile in shared memory
-constexpr int kChunksAtOnce = kGradThreads;
 
 // The lane's eight columns of a slice: neighbouring ones, or 32 apart where rows are not on 16 bytes.
 template <class T, bool WIDE>
@@ -177,14 +182,10 @@ __device__ __forceinline__ void finish_row(G* to, int lane, int left, bool accum
     }
 }
 
-// Where token v lies in the part [s, e) of a chunk.
-__device__ __forceinline__ int2 find(const int32_t* token, int s, int e, int v) {
-    int lo = s, hi = e;
-    while (lo < hi) { const int m = (lo + hi) >> 1; if (token[m] < v) lo = m + 1; else hi = m; }
-    const int from = lo;
-    hi = e;
-    while (lo < hi) { const int m = (lo + hi) >> 1; if (token[m] <= v) lo = m + 1; else hi = m; }
-    return make_int2(from, lo);
+// The first place of [s, e) whose token is v or a later one.
+__device__ __forceinline__ int first_at(const int32_t* token, int s, int e, int v) {
+    while (s < e) { const int m = (s + e) >> 1; if (token[m] < v) s = m + 1; else e = m; }
+    return s;
 }
 
 // Adds up the rows `row[0 .. n)` of dY: every parts-th group of kGroup of them, in their order.
@@ -201,165 +202,37 @@ __device__ __forceinline__ void add_rows(const T* dy, int64_t lddy, const int32_
         }
     }
 }
-// ... of token v in the chunks, one after the other, for tiles whose entries do not fit in shared memory.  Returns how many.
-template <class T, bool WIDE>
-__device__ __noinline__ int64_t add_token(const Sorted& s, int64_t node, int64_t tile, int v, const T* dy, int64_t lddy, int left, bool count_only,
-                                          int part, int parts, float (&sum)[8]) {
-    const int lane = threadIdx.x & 31;
-    int64_t n = 0;
-    for (int64_t c0 = 0; c0 < s.chunks; c0 += 32) {
-        int2 mine = make_int2(0, 0);
-        if (c0 + lane < s.chunks) {
-            const int64_t at = s.at(node, c0 + lane);
-            const int32_t* start = s.start + at * (s.tiles + 1) + tile;
-            mine = find(s.token + at * kChunk, start[0], start[1], v);
-        }
-        for (uint32_t some = __ballot_sync(0xffffffffu, mine.x < mine.y); some; some &= some - 1) {
-            const int c = __ffs(some) - 1;
-            const int from = __shfl_sync(0xffffffffu, mine.x, c), to = __shfl_sync(0xffffffffu, mine.y, c);
-            n += to - from;
-            if (!count_only) add_rows<T, WIDE>(dy, lddy, s.row + s.at(node, c0 + c) * kChunk + from, to - from, part, parts, left, sum);
-        }
-    }
-    return n;
-}
-
-// A whole tile whose entries do not fit in shared memory, each row's looked for in all chunks.
-template <class T, class G, bool WIDE>
-__device__ __noinline__ void add_tile(const EmbeddingGrad& a, const Sorted& s, int64_t node, int64_t tile, int rows, int64_t col0, int slices,
-                                      float (*part)[kSlice]) {
+// A tile's rows, one warp each, then those that all warps share.  of(r) is how many rows of dY the tile's row r has;
+// add(r, part, parts, sum) adds up every parts-th group of them.
+template <class G, bool WIDE, class Of, class Add>
+__device__ __forceinline__ void sum_rows(const EmbeddingGrad& a, G* de, int rows, int left, float (*part)[kSlice], uint16_t* many, int* some,
+                                         const Of& of, const Add& add) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int64_t col = col0; col < col0 + slices * kSlice && col < a.d; col += kSlice) {
-        const int left = static_cast<int>(min(static_cast<int64_t>(kSlice), a.d - col));
-        const T* dy = static_cast<const T*>(a.dY) + node * a.rows * a.lddy + col;
-        G* de = static_cast<G*>(a.dE[node]) + col;
-        for (int r = 0; r < rows; ++r) {
-            const int v = static_cast<int>(tile * kTileRows) + r;
+    for (int r = warp; r < rows; r += kGradWarps) {
+        const int n = of(r);
+        if (n == 0) {
+            if (a.accumulate) continue;
+            if (WIDE) {
+                constexpr int kPer = 16 / sizeof(G);
+#pragma unroll
+                for (int j = lane * kPer; j < kSlice; j += 32 * kPer)
+                    if (j < left) *reinterpret_cast<uint4*>(de + r * a.d + j) = make_uint4(0, 0, 0, 0);
+            } else {
+                for (int j = lane; j < left; j += 32) put(de + r * a.d + j, 0.f);
+            }
+        } else if (n >= kMany) {
+            if (lane == 0) many[atomicAdd(some, 1)] = static_cast<uint16_t>(r);
+        } else {
             float sum[8] = {};
-            const int64_t c = add_token<T, WIDE>(s, node, tile, v, dy, a.lddy, left, false, warp, kGradWarps, sum);
-            if (c == 0 && a.accumulate) continue;    // the same for the whole CTA
-#pragma unroll
-            for (int e = 0; e < 8; ++e) part[warp][e * 32 + lane] = sum[e];
-            __syncthreads();
-            if (warp == 0) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    for (int w = 1; w < kGradWarps; ++w) sum[e] += part[w][e * 32 + lane];
-                finish_row<G, WIDE>(de + v * a.d, lane, left, a.accumulate, sum, a.scale);
-            }
-            __syncthreads();
+            add(r, 0, 1, sum);
+            finish_row<G, WIDE>(de + r * a.d, lane, left, a.accumulate, sum, a.scale);
         }
     }
-}
-
-// The sum over the CTA's threads before this one, and over all of them.
-__device__ __forceinline__ int2 scan_threads(int v, int* carry) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int sum = v;
-    for (int o = 1; o < 32; o *= 2) { const int y = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += y; }
-    if (lane == 31) carry[warp] = sum;
     __syncthreads();
-    int before = 0, all = 0;
-    for (int w = 0; w < kGradWarps; ++w) { before += w < warp ? carry[w] : 0; all += carry[w]; }
-    return make_int2(before + sum - v, all);
-}
-
-template <class T, class G, bool WIDE>
-__global__ void __launch_bounds__(kGradThreads, 5) embedding_grad_kernel(const __grid_constant__ EmbeddingGrad a, const Sorted s, bool scan, int slices) {
-    chain_begin();
-    __shared__ float part[kGradWarps][kSlice];
-    __shared__ int32_t list[kPlaces];
-    __shared__ int off[kTileRows + 1];
-    __shared__ uint16_t count[kGradWarps][kTileRows];
-    __shared__ int2 chunk_part[kChunksAtOnce];       // of the chunks' entries: the tile's first place, the entries before it
-    __shared__ int carry[kGradWarps];
-    __shared__ uint8_t many[kTileRows];              // rows that all warps share
-    __shared__ int some;                             // their number
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t tile = blockIdx.x, node = blockIdx.z;
-    const int rows = static_cast<int>(min(static_cast<int64_t>(kTileRows), a.vocab - tile * kTileRows));
-    const int64_t v0 = tile * kTileRows;
-    const T* dy0 = static_cast<const T*>(a.dY) + node * a.rows * a.lddy;
-    // the tile's entries: the node's tokens, or those of the chunks one after the other
-    int n = static_cast<int>(a.rows);
-    bool fits = true;
-    if (!scan) {
-        fits = s.chunks <= kChunksAtOnce;
-        int mine = 0, from = 0;
-        if (fits && threadIdx.x < s.chunks) {
-            const int32_t* start = s.start + s.at(node, threadIdx.x) * (s.tiles + 1) + tile;
-            from = start[0];
-            mine = start[1] - from;
-        }
-        const int2 sum = scan_threads(mine, carry);
-        chunk_part[threadIdx.x] = make_int2(from, sum.x);
-        n = sum.y;
-        fits = fits && n <= kPlaces;
-    }
-    for (int q = threadIdx.x; q < kGradWarps * kTileRows; q += kGradThreads) (&count[0][0])[q] = 0;
-    if (threadIdx.x == 0) some = 0;
-    __syncthreads();
-    if (!fits) {                                     // the same for the whole CTA
-        add_tile<T, G, WIDE>(a, s, node, tile, rows, static_cast<int64_t>(blockIdx.y) * slices * kSlice, slices, part);
-        return;
-    }
-    {
-        // each warp ranks a stretch of entries; what it knows of them stays in registers
-        const int stretch = (n + kGradThreads - 1) / kGradThreads;
-        int32_t row[kBatches];
-        uint32_t rank[kBatches];                     // the token's row of the tile, and its rank among the warp's
-#pragma unroll
-        for (int u = 0; u < kBatches; ++u) {
-            rank[u] = kTileRows << 16;
-            row[u] = 0;
-            if (u < stretch) {                       // the same for the whole CTA
-                const int x = (warp * stretch + u) * 32 + lane;
-                int r = kTileRows;
-                if (x < n) {
-                    if (scan) {
-                        const int64_t t = a.tokens.at(node * a.rows + x) - v0;
-                        row[u] = x;
-                        if (t >= 0 && t < rows) r = static_cast<int>(t);
-                    } else {
-                        int c = 0, end = static_cast<int>(s.chunks);         // the last chunk that begins at x or before
-                        while (end - c > 1) { const int m = (c + end) >> 1; if (chunk_part[m].y <= x) c = m; else end = m; }
-                        const int64_t at = s.at(node, c) * kChunk + chunk_part[c].x + (x - chunk_part[c].y);
-                        row[u] = s.row[at];
-                        r = static_cast<int>(s.token[at] - v0);
-                    }
-                }
-                if (__any_sync(0xffffffffu, r < kTileRows)) {
-                    const uint32_t same = __match_any_sync(0xffffffffu, r), before = same & ((1u << lane) - 1);
-                    if (r < kTileRows) rank[u] = static_cast<uint32_t>(r) << 16 | (count[warp][r] + __popc(before));
-                    __syncwarp();
-                    if (r < kTileRows && before == 0) count[warp][r] += static_cast<uint16_t>(__popc(same));
-                    __syncwarp();
-                }
-            }
-        }
-        __syncthreads();
-        int sum = 0;
-        if (threadIdx.x < kTileRows)
-            for (int w = 0; w < kGradWarps; ++w) { const int c = count[w][threadIdx.x]; count[w][threadIdx.x] = static_cast<uint16_t>(sum); sum += c; }
-        const int2 place = scan_threads(sum, carry);
-        if (threadIdx.x < kTileRows) off[threadIdx.x] = place.x;
-        if (threadIdx.x == 0) off[kTileRows] = place.y;
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < kBatches; ++u) {
-            const int r = static_cast<int>(rank[u] >> 16);
-            if (r < kTileRows) list[off[r] + count[warp][r] + (rank[u] & 0xffffu)] = row[u];
-        }
-        __syncthreads();
-    }
-    const int64_t col0 = static_cast<int64_t>(blockIdx.y) * slices * kSlice;
-    const int width = static_cast<int>(min(static_cast<int64_t>(slices) * kSlice, a.d - col0));
-    const T* dy = dy0 + col0;
-    G* de = static_cast<G*>(a.dE[node]) + v0 * a.d + col0;
-    const auto rows_of = [&](int r, int from, int parts, int c0) {
+    for (int q = 0; q < *some; ++q) {
+        const int r = many[q];
         float sum[8] = {};
-        add_rows<T, WIDE>(dy + c0, a.lddy, list + off[r], off[r + 1] - off[r], from, parts, width - c0, sum);
-        if (parts == 1) { finish_row<G, WIDE>(de + r * a.d + c0, lane, width - c0, a.accumulate, sum, a.scale); return; }
+        add(r, warp, kGradWarps, sum);
 #pragma unroll
         for (int e = 0; e < 8; ++e) part[warp][e * 32 + lane] = sum[e];
         __syncthreads();
@@ -367,41 +240,144 @@ __global__ void __launch_bounds__(kGradThreads, 5) embedding_grad_kernel(const _
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 for (int w = 1; w < kGradWarps; ++w) sum[e] += part[w][e * 32 + lane];
-            finish_row<G, WIDE>(de + r * a.d + c0, lane, width - c0, a.accumulate, sum, a.scale);
+            finish_row<G, WIDE>(de + r * a.d, lane, left, a.accumulate, sum, a.scale);
         }
         __syncthreads();
-    };
-    for (int r = warp; r < rows; r += kGradWarps) {
-        const int n_r = off[r + 1] - off[r];
-        if (n_r == 0) {
-            if (a.accumulate) continue;
-            if (WIDE) {
-                constexpr int kPer = 16 / sizeof(G);
-                for (int j = lane * kPer; j < width; j += 32 * kPer) *reinterpret_cast<uint4*>(de + r * a.d + j) = make_uint4(0, 0, 0, 0);
-            } else {
-                for (int j = lane; j < width; j += 32) put(de + r * a.d + j, 0.f);
-            }
-        } else if (n_r >= kMany) {
-            if (lane == 0) many[atomicAdd(&some, 1)] = static_cast<uint8_t>(r);
-        } else {
-            for (int c0 = 0; c0 < width; c0 += kSlice) rows_of(r, 0, 1, c0);
+    }
+}
+
+// Up to kScan rows a node: the CTA looks through the node's tokens.
+template <class T, class G, bool WIDE, int R>
+__global__ void __launch_bounds__(kGradThreads, 5) scan_grad_kernel(const __grid_constant__ EmbeddingGrad a) {
+    chain_begin();
+    __shared__ float part[kGradWarps][kSlice];
+    __shared__ int32_t list[kScan];                  // the tile's rows of dY in order of (token, row)
+    __shared__ int off[R + 1];                       // where each of its tokens begins
+    __shared__ uint16_t count[kGradWarps][R];
+    __shared__ int carry[kGradWarps];
+    __shared__ uint16_t many[R];
+    __shared__ int some;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t node = blockIdx.z, v0 = static_cast<int64_t>(blockIdx.x) * R, col = static_cast<int64_t>(blockIdx.y) * kSlice;
+    const int rows = static_cast<int>(min(static_cast<int64_t>(R), a.vocab - v0)), left = static_cast<int>(min(static_cast<int64_t>(kSlice), a.d - col));
+    // each warp takes a stretch of rows: their tokens' places in the tile (R: none), then the ranks among the warp's too
+    constexpr int kBatches = kScan / kGradThreads;
+    const int n = static_cast<int>(a.rows), stretch = (n + kGradThreads - 1) / kGradThreads;
+    uint32_t rank[kBatches];
+#pragma unroll
+    for (int u = 0; u < kBatches; ++u) {
+        const int x = (warp * stretch + u) * 32 + lane;
+        rank[u] = R;
+        if (u < stretch && x < n) {
+            const int64_t t = a.tokens.at(node * a.rows + x) - v0;
+            if (t >= 0 && t < rows) rank[u] = static_cast<uint32_t>(t);
+        }
+    }
+    for (int q = threadIdx.x; q < kGradWarps * R / 2; q += kGradThreads) reinterpret_cast<uint32_t*>(&count[0][0])[q] = 0;
+    if (threadIdx.x == 0) some = 0;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kBatches; ++u) {
+        const int r = static_cast<int>(rank[u]);
+        rank[u] = static_cast<uint32_t>(r) << 16;
+        if (__any_sync(0xffffffffu, r < R)) {
+            const uint32_t same = __match_any_sync(0xffffffffu, r), before = same & ((1u << lane) - 1);
+            if (r < R) rank[u] |= count[warp][r] + __popc(before);
+            __syncwarp();
+            if (r < R && before == 0) count[warp][r] += static_cast<uint16_t>(__popc(same));
+            __syncwarp();
         }
     }
     __syncthreads();
-    for (int q = 0; q < some; ++q)
-        for (int c0 = 0; c0 < width; c0 += kSlice) rows_of(many[q], warp, kGradWarps, c0);
+    int sum = 0;
+    if (threadIdx.x < R)
+        for (int w = 0; w < kGradWarps; ++w) { const int c = count[w][threadIdx.x]; count[w][threadIdx.x] = static_cast<uint16_t>(sum); sum += c; }
+    int before = sum;                                // of the threads up to this one, then before it
+    for (int o = 1; o < 32; o *= 2) { const int y = __shfl_up_sync(0xffffffffu, before, o); if (lane >= o) before += y; }
+    if (lane == 31) carry[warp] = before;
+    __syncthreads();
+    before -= sum;
+    for (int w = 0; w < warp; ++w) before += carry[w];
+    if (threadIdx.x < R) off[threadIdx.x] = before;
+    if (threadIdx.x == R - 1) off[R] = before + sum;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kBatches; ++u) {
+        const int r = static_cast<int>(rank[u] >> 16);
+        if (r < R) list[off[r] + count[warp][r] + (rank[u] & 0xffffu)] = (warp * stretch + u) * 32 + lane;
+    }
+    __syncthreads();
+    const T* dy = static_cast<const T*>(a.dY) + node * a.rows * a.lddy + col;
+    sum_rows<G, WIDE>(a, static_cast<G*>(a.dE[node]) + v0 * a.d + col, rows, left, part, many, &some,
+                      [&](int r) { return off[r + 1] - off[r]; },
+                      [&](int r, int from, int parts, float (&s)[8]) { add_rows<T, WIDE>(dy, a.lddy, list + off[r], off[r + 1] - off[r], from, parts, left, s); });
+}
+
+// Beyond: the tile's part of every sorted chunk, with a table of where each row begins in each chunk (TABLE), or, of more
+// chunks than it has room for, looked for row by row.
+constexpr int kTable = 2080;
+template <class T, class G, bool WIDE, int R, bool TABLE>
+__global__ void __launch_bounds__(kGradThreads, 5) sorted_grad_kernel(const __grid_constant__ EmbeddingGrad a, const Sorted s) {
+    chain_begin();
+    __shared__ float part[kGradWarps][kSlice];
+    __shared__ int32_t table[TABLE ? kTable : 1];
+    __shared__ uint16_t many[R];
+    __shared__ int some;
+    const int lane = threadIdx.x & 31;
+    const int64_t tile = blockIdx.x, node = blockIdx.z, v0 = tile * R, col = static_cast<int64_t>(blockIdx.y) * kSlice;
+    const int rows = static_cast<int>(min(static_cast<int64_t>(R), a.vocab - v0)), left = static_cast<int>(min(static_cast<int64_t>(kSlice), a.d - col));
+    const auto part_of = [&](int64_t chunk) {
+        const int32_t* start = s.start + s.at(node, chunk) * (s.tiles + 1) + tile;
+        return make_int2(start[0], start[1]);
+    };
+    if (threadIdx.x == 0) some = 0;
+    if (TABLE)
+        for (int q = threadIdx.x; q < static_cast<int>(s.chunks) * (R + 1); q += kGradThreads) {
+            const int chunk = q / (R + 1), r = q % (R + 1);
+            const int2 p = part_of(chunk);
+            table[q] = r == 0 ? p.x : r == R ? p.y : first_at(s.token + s.at(node, chunk) * kChunk, p.x, p.y, static_cast<int>(v0) + r);
+        }
+    __syncthreads();
+    const T* dy = static_cast<const T*>(a.dY) + node * a.rows * a.lddy + col;
+    // the part of chunk c0 + lane that is row r's
+    const auto mine = [&](int64_t c0, int r) {
+        if (c0 + lane >= s.chunks) return make_int2(0, 0);
+        if (TABLE) return make_int2(table[lane * (R + 1) + r], table[lane * (R + 1) + r + 1]);
+        const int2 p = part_of(c0 + lane);
+        const int32_t* token = s.token + s.at(node, c0 + lane) * kChunk;
+        return make_int2(first_at(token, p.x, p.y, static_cast<int>(v0) + r), first_at(token, p.x, p.y, static_cast<int>(v0) + r + 1));
+    };
+    sum_rows<G, WIDE>(a, static_cast<G*>(a.dE[node]) + v0 * a.d + col, rows, left, part, many, &some,
+        [&](int r) {
+            int n = 0;
+            for (int64_t c0 = 0; c0 < s.chunks; c0 += 32) { const int2 m = mine(c0, r); n += m.y - m.x; }
+            return __reduce_add_sync(0xffffffffu, n);
+        },
+        [&](int r, int from, int parts, float (&sum)[8]) {
+            for (int64_t c0 = 0; c0 < s.chunks; c0 += 32) {
+                const int2 m = mine(c0, r);
+                for (uint32_t some_of = __ballot_sync(0xffffffffu, m.x < m.y); some_of; some_of &= some_of - 1) {
+                    const int c = __ffs(some_of) - 1;
+                    const int begin = __shfl_sync(0xffffffffu, m.x, c), end = __shfl_sync(0xffffffffu, m.y, c);
+                    add_rows<T, WIDE>(dy, a.lddy, s.row + s.at(node, c0 + c) * kChunk + begin, end - begin, from, parts, left, sum);
+                }
+            }
+        });
 }
 
 bool on16(const void* p, int64_t ld_bytes) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld_bytes % 16 == 0; }
 
+template <class T, class G, bool WIDE, int R>
+cudaError_t launch_tiles(const EmbeddingGrad& a, const Sorted& s, cudaStream_t st) {
+    const dim3 grid(static_cast<unsigned>(s.tiles), static_cast<unsigned>((a.d + kSlice - 1) / kSlice), static_cast<unsigned>(a.nodes));
+    if (a.rows <= kScan) return launch_chain(scan_grad_kernel<T, G, WIDE, R>, grid, kGradThreads, 0, st, a);
+    return s.chunks * (R + 1) <= kTable ? launch_chain(sorted_grad_kernel<T, G, WIDE, R, true>, grid, kGradThreads, 0, st, a, s)
+                                        : launch_chain(sorted_grad_kernel<T, G, WIDE, R, false>, grid, kGradThreads, 0, st, a, s);
+}
 template <class T, class G>
-cudaError_t launch_grad(const EmbeddingGrad& a, const Sorted& s, bool scan, bool wide, cudaStream_t st) {
-    // columns a CTA: one slice where that takes all, or where two would leave SMs idle
-    const int64_t all = (a.d + kSlice - 1) / kSlice;
-    const int slices = all > 1 && s.tiles * a.nodes * ((all + 1) / 2) >= 152 * 8 ? 2 : 1;
-    const dim3 grid(static_cast<unsigned>(s.tiles), static_cast<unsigned>((all + slices - 1) / slices), static_cast<unsigned>(a.nodes));
-    return wide ? launch_chain(embedding_grad_kernel<T, G, true>, grid, kGradThreads, 0, st, a, s, scan, slices)
-                : launch_chain(embedding_grad_kernel<T, G, false>, grid, kGradThreads, 0, st, a, s, scan, slices);
+cudaError_t launch_grad(const EmbeddingGrad& a, const Sorted& s, bool wide, cudaStream_t st) {
+    if (s.tile_rows == kFewRows) return wide ? launch_tiles<T, G, true, kFewRows>(a, s, st) : launch_tiles<T, G, false, kFewRows>(a, s, st);
+    return wide ? launch_tiles<T, G, true, kManyRows>(a, s, st) : launch_tiles<T, G, false, kManyRows>(a, s, st);
 }
 
 }  // namespace
@@ -417,17 +393,16 @@ cudaError_t lookup(const Lookup& a, int dtype, cudaStream_t st) {
                              : launch_chain(lookup_kernel<float>, grid, kLookupThreads, 0, st, a, shift, wide_e, wide_y);
 }
 
-int64_t embedding_grad_bytes(int64_t nodes, int64_t rows, int64_t vocab) {
+int64_t embedding_grad_bytes(int64_t nodes, int64_t rows, int64_t vocab, int64_t d) {
     if (rows <= kScan) return 0;
-    const Sorted s = sorted_of(nodes, rows, vocab, nullptr);
+    const Sorted s = sorted_of(nodes, rows, vocab, d, nullptr);
     return nodes * s.chunks * (2 * kChunk + s.tiles + 1) * 4;
 }
 
 cudaError_t embedding_grad(const EmbeddingGrad& a, int dtype, int grad_dtype, cudaStream_t st) {
     if (a.vocab == 0 || a.d == 0) return cudaSuccess;
-    const Sorted s = sorted_of(a.nodes, a.rows, a.vocab, a.workspace);
-    const bool scan = a.rows <= kScan;
-    if (!scan) {
+    const Sorted s = sorted_of(a.nodes, a.rows, a.vocab, a.d, a.workspace);
+    if (a.rows > kScan) {
         int bits = 0;
         while ((int64_t{1} << bits) <= a.vocab) ++bits;          // of the largest key, vocab
         constexpr int kBytes = kChunk * 2 * (4 + 2);
@@ -443,8 +418,8 @@ cudaError_t embedding_grad(const EmbeddingGrad& a, int dtype, int grad_dtype, cu
     bool wide = on16(a.dY, a.nodes * a.rows > 1 ? a.lddy * es : 0) && a.d % 8 == 0;
     for (int64_t i = 0; i < a.nodes; ++i) wide = wide && on16(a.dE[i], a.d * gs);
     if (dtype == GLR_BF16)
-        return grad_dtype == GLR_BF16 ? launch_grad<__nv_bfloat16, __nv_bfloat16>(a, s, scan, wide, st) : launch_grad<__nv_bfloat16, float>(a, s, scan, wide, st);
-    return grad_dtype == GLR_BF16 ? launch_grad<float, __nv_bfloat16>(a, s, scan, wide, st) : launch_grad<float, float>(a, s, scan, wide, st);
+        return grad_dtype == GLR_BF16 ? launch_grad<__nv_bfloat16, __nv_bfloat16>(a, s, wide, st) : launch_grad<__nv_bfloat16, float>(a, s, wide, st);
+    return grad_dtype == GLR_BF16 ? launch_grad<float, __nv_bfloat16>(a, s, wide, st) : launch_grad<float, float>(a, s, wide, st);
 }
 
 }  // namespace rows
