@@ -150,20 +150,47 @@ constexpr int kGradWarps = 8, kGradThreads = kGradWarps * 32, kSlice = 256;     
 constexpr int kMany = 64;                            // occurrences from which on all warps share a row
 constexpr int kScan = 1024;                          // a node's rows up to which its tokens are looked through
 
-// The lane's eight columns of a slice: neighbouring ones, or 32 apart where rows are not on 16 bytes.
-template <class T, bool WIDE>
-__device__ __forceinline__ void add_row(const T* row, int lane, int left, float (&sum)[8]) {
-    if (WIDE) {
+// The lane's eight columns of a slice of a row, as they lie in memory: neighbouring ones, or 32 apart where rows are not on 16
+// bytes (0 beyond the last one).
+template <class T, bool WIDE> struct Columns;
+template <> struct Columns<__nv_bfloat16, true> {
+    static constexpr int kAhead = 8;                 // rows loaded before the first one is added
+    uint4 u;
+    __device__ __forceinline__ void load(const __nv_bfloat16* row, int lane, int left) {
+        u = lane * 8 < left ? *reinterpret_cast<const uint4*>(row + lane * 8) : make_uint4(0, 0, 0, 0);
+    }
+    __device__ __forceinline__ void add(float (&sum)[8]) const {
         float v[8];
-        load8(row + lane * 8, left - lane * 8, true, v);
+        widen8(u, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum[e] += v[e];
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e * 32 + lane < left) sum[e] += to_f(row[e * 32 + lane]);
     }
-}
+};
+template <> struct Columns<float, true> {
+    static constexpr int kAhead = 4;
+    float4 a, b;
+    __device__ __forceinline__ void load(const float* row, int lane, int left) {
+        const float4* p = reinterpret_cast<const float4*>(row + lane * 8);
+        const bool in = lane * 8 < left;
+        a = in ? p[0] : make_float4(0.f, 0.f, 0.f, 0.f);
+        b = in ? p[1] : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    __device__ __forceinline__ void add(float (&sum)[8]) const {
+        sum[0] += a.x; sum[1] += a.y; sum[2] += a.z; sum[3] += a.w; sum[4] += b.x; sum[5] += b.y; sum[6] += b.z; sum[7] += b.w;
+    }
+};
+template <class T> struct Columns<T, false> {
+    static constexpr int kAhead = 2;
+    T x[8];
+    __device__ __forceinline__ void load(const T* row, int lane, int left) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = e * 32 + lane < left ? row[e * 32 + lane] : T(0.f);
+    }
+    __device__ __forceinline__ void add(float (&sum)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += to_f(x[e]);
+    }
+};
 template <class G, bool WIDE>
 __device__ __forceinline__ void finish_row(G* to, int lane, int left, bool accumulate, const float (&sum)[8], float scale) {
     float v[8];
@@ -188,20 +215,31 @@ __device__ __forceinline__ int first_at(const int32_t* token, int s, int e, int 
     return s;
 }
 
-// Adds up the rows `row[0 .. n)` of dY: every parts-th group of kGroup of them, in their order.
-constexpr int kGroup = 8;
+// Adds up the rows `row[0 .. n)` of dY: every parts-th group of 32 of them, in their order.
 template <class T, bool WIDE>
 __device__ __forceinline__ void add_rows(const T* dy, int64_t lddy, const int32_t* row, int n, int part, int parts, int left, float (&sum)[8]) {
+    using C = Columns<T, WIDE>;
     const int lane = threadIdx.x & 31;
-    for (int q = part * kGroup; q < n; q += parts * kGroup) {
-        if (n - q >= kGroup) {
+    for (int q = part * 32; q < n; q += parts * 32) {
+        const int mine = q + lane < n ? row[q + lane] : 0, m = min(32, n - q);
+        int u = 0;
+        for (; u + C::kAhead <= m; u += C::kAhead) {
+            C c[C::kAhead];
 #pragma unroll
-            for (int u = 0; u < kGroup; ++u) add_row<T, WIDE>(dy + row[q + u] * lddy, lane, left, sum);
-        } else {
-            for (int u = q; u < n; ++u) add_row<T, WIDE>(dy + row[u] * lddy, lane, left, sum);
+            for (int k = 0; k < C::kAhead; ++k) c[k].load(dy + __shfl_sync(0xffffffffu, mine, u + k) * lddy, lane, left);
+#pragma unroll
+            for (int k = 0; k < C::kAhead; ++k) c[k].add(sum);
+        }
+        for (; u < m; u += 2) {
+            C c[2];
+            c[0].load(dy + __shfl_sync(0xffffffffu, mine, u) * lddy, lane, left);
+            c[1].load(dy + __shfl_sync(0xffffffffu, mine, min(u + 1, m - 1)) * lddy, lane, left);
+            c[0].add(sum);
+            if (u + 1 < m) c[1].add(sum);
         }
     }
 }
+
 // A tile's rows, one warp each, then those that all warps share.  of(r) is how many rows of dY the tile's row r has;
 // add(r, part, parts, sum) adds up every parts-th group of them.
 template <class G, bool WIDE, class Of, class Add>
@@ -248,7 +286,7 @@ __device__ __forceinline__ void sum_rows(const EmbeddingGrad& a, G* de, int rows
 
 // Up to kScan rows a node: the CTA looks through the node's tokens.
 template <class T, class G, bool WIDE, int R>
-__global__ void __launch_bounds__(kGradThreads, 5) scan_grad_kernel(const __grid_constant__ EmbeddingGrad a) {
+__global__ void __launch_bounds__(kGradThreads, 4) scan_grad_kernel(const __grid_constant__ EmbeddingGrad a) {
     chain_begin();
     __shared__ float part[kGradWarps][kSlice];
     __shared__ int32_t list[kScan];                  // the tile's rows of dY in order of (token, row)
@@ -317,7 +355,7 @@ __global__ void __launch_bounds__(kGradThreads, 5) scan_grad_kernel(const __grid
 // chunks than it has room for, looked for row by row.
 constexpr int kTable = 2080;
 template <class T, class G, bool WIDE, int R, bool TABLE>
-__global__ void __launch_bounds__(kGradThreads, 5) sorted_grad_kernel(const __grid_constant__ EmbeddingGrad a, const Sorted s) {
+__global__ void __launch_bounds__(kGradThreads, 4) sorted_grad_kernel(const __grid_constant__ EmbeddingGrad a, const Sorted s) {
     chain_begin();
     __shared__ float part[kGradWarps][kSlice];
     __shared__ int32_t table[TABLE ? kTable : 1];
