@@ -20,7 +20,7 @@ namespace {
 constexpr int kLookupThreads = 256;
 
 template <class T>
-__global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const __grid_constant__ Lookup a, int shift, bool wide_e, bool wide_y) {
+__global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const __grid_constant__ Lookup a, int shift) {
     chain_begin();
     const int per = 1 << shift;
     const int64_t step = static_cast<int64_t>(gridDim.x) * (kLookupThreads >> shift);
@@ -32,11 +32,27 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const __grid_con
         for (int64_t j = (threadIdx.x & (per - 1)) * 8; j < a.d; j += per * 8) {
             const int n = static_cast<int>(min(static_cast<int64_t>(8), a.d - j));
             float v[8];
-            load8(e + j, in ? n : 0, wide_e, v);
+            load8(e + j, in ? n : 0, true, v);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] = in ? v[q] * a.scale : 0.f;
-            store8(y + j, n, wide_y, v);
+            for (int q = 0; q < 8; ++q) v[q] *= a.scale;        // (0 for padding)
+            store8(y + j, n, true, v);
         }
+    }
+}
+
+// Rows off 16 bytes: 256 columns a warp.
+template <class T>
+__global__ void __launch_bounds__(kLookupThreads) lookup_apart_kernel(const __grid_constant__ Lookup a, int64_t parts) {
+    chain_begin();
+    const int64_t warps = static_cast<int64_t>(gridDim.x) * (kLookupThreads / 32);
+    for (int64_t q = static_cast<int64_t>(blockIdx.x) * (kLookupThreads / 32) + (threadIdx.x >> 5); q < a.rows * parts; q += warps) {
+        const int64_t i = q / parts, first = (q - i * parts) * 256, t = a.tokens.at(i);
+        const bool in = t >= 0 && t < a.vocab;
+        float v[8];
+        load_apart(static_cast<const T*>(a.E) + (in ? t : 0) * a.lde, first, in ? a.d : 0, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= a.scale;
+        store_apart(static_cast<T*>(a.Y) + i * a.ldy, first, a.d, v);
     }
 }
 
@@ -422,13 +438,19 @@ cudaError_t launch_grad(const EmbeddingGrad& a, const Sorted& s, bool wide, cuda
 
 cudaError_t lookup(const Lookup& a, int dtype, cudaStream_t st) {
     if (a.rows == 0 || a.d == 0) return cudaSuccess;
+    const int64_t es = dtype == GLR_BF16 ? 2 : 4;
+    if (!on16(a.E, a.vocab > 1 ? a.lde * es : 0) || !on16(a.Y, a.rows > 1 ? a.ldy * es : 0)) {
+        const int64_t parts = (a.d + 255) / 256, warps = kLookupThreads / 32;
+        const dim3 grid(static_cast<unsigned>(std::min<int64_t>((a.rows * parts + warps - 1) / warps, 152 * 32)));
+        return dtype == GLR_BF16 ? launch_chain(lookup_apart_kernel<__nv_bfloat16>, grid, kLookupThreads, 0, st, a, parts)
+                                 : launch_chain(lookup_apart_kernel<float>, grid, kLookupThreads, 0, st, a, parts);
+    }
     int shift = 0;
     while (shift < 8 && (8LL << shift) < a.d) ++shift;
-    const int64_t per = kLookupThreads >> shift, es = dtype == GLR_BF16 ? 2 : 4;
+    const int64_t per = kLookupThreads >> shift;
     const dim3 grid(static_cast<unsigned>(std::min<int64_t>((a.rows + per - 1) / per, 152 * 32)));
-    const bool wide_e = on16(a.E, a.vocab > 1 ? a.lde * es : 0), wide_y = on16(a.Y, a.rows > 1 ? a.ldy * es : 0);
-    return dtype == GLR_BF16 ? launch_chain(lookup_kernel<__nv_bfloat16>, grid, kLookupThreads, 0, st, a, shift, wide_e, wide_y)
-                             : launch_chain(lookup_kernel<float>, grid, kLookupThreads, 0, st, a, shift, wide_e, wide_y);
+    return dtype == GLR_BF16 ? launch_chain(lookup_kernel<__nv_bfloat16>, grid, kLookupThreads, 0, st, a, shift)
+                             : launch_chain(lookup_kernel<float>, grid, kLookupThreads, 0, st, a, shift);
 }
 
 int64_t embedding_grad_bytes(int64_t nodes, int64_t rows, int64_t vocab, int64_t d) {
