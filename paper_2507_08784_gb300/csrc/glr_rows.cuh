@@ -108,24 +108,26 @@ __device__ __forceinline__ uint32_t block_scale(const float (&v)[8]) {
     m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
     return scale_of(m);
 }
+// The nearest integer to a product of at most 127 stands in the low bits of its sum with 1.5 2^23.
 __device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float d, uint32_t scale) {
     if (scale == kNoScale) return 0;
-    const float inv = inverse_scale(scale);
-    int q[4] = {__float2int_rn(a * inv), __float2int_rn(b * inv), __float2int_rn(c * inv), __float2int_rn(d * inv)};
-    if (scale == kTopScale)
+    const float inv = inverse_scale(scale), half = 12582912.f;
+    int q[4] = {__float_as_int(fmaf(a, inv, half)), __float_as_int(fmaf(b, inv, half)), __float_as_int(fmaf(c, inv, half)),
+                __float_as_int(fmaf(d, inv, half))};
+    if (scale == kTopScale) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) q[e] = max(-127, min(127, q[e]));
-    return (static_cast<uint32_t>(q[0]) & 0xffu) | (static_cast<uint32_t>(q[1]) & 0xffu) << 8 | (static_cast<uint32_t>(q[2]) & 0xffu) << 16 |
-           static_cast<uint32_t>(q[3]) << 24;
+        for (int e = 0; e < 4; ++e) q[e] = max(0x4b400000 - 127, min(0x4b400000 + 127, q[e]));
+    }
+    return __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
 }
 __device__ __forceinline__ uint2 block_codes(const float (&v)[8], uint32_t scale) {
     return make_uint2(four_codes(v[0], v[1], v[2], v[3], scale), four_codes(v[4], v[5], v[6], v[7], scale));
 }
 __device__ __forceinline__ void code_values(uint2 c, uint32_t scale, float (&v)[8]) {
     const float s = scale_value(scale);
-    const uint32_t w[2] = {c.x, c.y};
+    const uint32_t w[2] = {c.x ^ 0x80808080u, c.y ^ 0x80808080u};        // codes + 128, each the low byte of 2^23 + code + 128
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(static_cast<int8_t>(w[e / 4] >> (8 * (e % 4)))) * s;
+    for (int e = 0; e < 8; ++e) v[e] = (__uint_as_float(__byte_perm(w[e / 4], 0x4b000000u, 0x7650 + e % 4)) - 8388736.f) * s;
 }
 __device__ __forceinline__ void store_codes(int8_t* p, int n, bool wide, uint2 c) {
     if (wide && n >= 8) {

@@ -12,46 +12,109 @@ namespace {
 
 constexpr int kThreads = 256;
 
+// Sixteen or 32 bytes of a row as they lie in memory.
+template <class T> struct Raw;
+template <> struct Raw<__nv_bfloat16> {
+    uint4 u;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, int n, bool wide) {
+        if (wide && n >= 8) { u = *reinterpret_cast<const uint4*>(p); return; }
+        const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+        uint32_t w[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) w[q] = (2 * q < n ? h[2 * q] : 0u) | (2 * q + 1 < n ? h[2 * q + 1] : 0u) << 16;
+        u = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const { widen8(u, v); }
+    // the largest |x|, as an fp32 value's bits
+    __device__ __forceinline__ uint32_t most() const {
+        constexpr uint32_t m = 0x7fff7fffu;
+        const uint32_t x = __vmaxu2(__vmaxu2(u.x & m, u.y & m), __vmaxu2(u.z & m, u.w & m));
+        return max(x << 16, x & 0xffff0000u);
+    }
+};
+template <> struct Raw<float> {
+    float v[8];
+    __device__ __forceinline__ void load(const float* p, int n, bool wide) { load8(p, n, wide, v); }
+    __device__ __forceinline__ void get(float (&to)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) to[e] = v[e];
+    }
+    __device__ __forceinline__ uint32_t most() const {
+        uint32_t m = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(v[e]) & 0x7fffffffu);
+        return m;
+    }
+};
+
+// Two vectors of eight columns a thread at a time: of a row, or, where a row has no more than one for each thread, of two rows.
+struct Pair {
+    int64_t i[2], j[2];
+    int n[2];
+    __device__ __forceinline__ Pair(int64_t row, int64_t next, bool one, int64_t col, int64_t per8, int64_t rows, int64_t cols) {
+        i[0] = row; i[1] = one ? next : row;
+        j[0] = col; j[1] = one ? col : col + per8;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) n[u] = i[u] < rows ? static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(8), cols - j[u]))) : 0;
+    }
+};
+
 template <class T>
 __global__ void __launch_bounds__(kThreads) pack_kernel(const __grid_constant__ Pack a, int shift, bool wide, bool wide_codes) {
     chain_begin();
-    const int per = 1 << shift, at = threadIdx.x & (per - 1);
-    const int64_t up = (a.cols + kBlock - 1) / kBlock * kBlock, step = static_cast<int64_t>(gridDim.x) * (kThreads >> shift);
-    // a warp's lanes may hold several rows: all of them stay until the last one's row is done
-    for (int64_t first = static_cast<int64_t>(blockIdx.x) * (kThreads >> shift); first < a.rows; first += step) {
-        const int64_t i = first + (threadIdx.x >> shift);
-        const bool here = i < a.rows;
-        const T* x = static_cast<const T*>(a.X) + (here ? i : 0) * a.ldx;
-        for (int64_t j = at * 8; j - at * 8 < up; j += per * 8) {
-            const int n = here ? static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(8), a.cols - j))) : 0;
-            float v[8];
-            load8(x + j, n, wide, v);
-            const uint32_t s = block_scale(v);
-            const uint2 c = block_codes(v, s);
-            if (n > 0) {
-                store_codes(a.codes + i * a.ld_codes + j, n, wide_codes, c);
-                if ((at & 3) == 0) a.scales[i * a.ld_scales + j / kBlock] = static_cast<uint8_t>(s);
+    const int64_t per8 = 8LL << shift, col = (threadIdx.x & ((1 << shift) - 1)) * 8, own = threadIdx.x >> shift, group = kThreads >> shift;
+    const bool one = a.cols <= per8;
+    const int64_t step = gridDim.x * group;
+    // all lanes of a block are there: the loops go by the CTA's first row and the row's stretches
+    for (int64_t first = blockIdx.x * group; first < a.rows; first += one ? 2 * step : step)
+        for (int64_t c = 0; c < a.cols; c += 2 * per8) {
+            const Pair at(first + own, first + step + own, one, c + col, per8, a.rows, a.cols);
+            Raw<T> x[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) x[u].load(static_cast<const T*>(a.X) + at.i[u] * a.ldx + at.j[u], at.n[u], wide);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                uint32_t m = x[u].most();
+                m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+                const uint32_t s = scale_of(m);
+                if (at.n[u] <= 0) continue;
+                float v[8];
+                x[u].get(v);
+                store_codes(a.codes + at.i[u] * a.ld_codes + at.j[u], at.n[u], wide_codes, block_codes(v, s));
+                if ((threadIdx.x & 3) == 0) a.scales[at.i[u] * a.ld_scales + at.j[u] / kBlock] = static_cast<uint8_t>(s);
             }
         }
-    }
 }
 
 template <class T>
 __global__ void __launch_bounds__(kThreads) unpack_kernel(const __grid_constant__ Unpack a, int shift) {
     chain_begin();
-    const int per = 1 << shift;
-    const int64_t step = static_cast<int64_t>(gridDim.x) * (kThreads >> shift);
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * (kThreads >> shift) + (threadIdx.x >> shift); i < a.rows; i += step)
-        for (int64_t j = (threadIdx.x & (per - 1)) * 8; j < a.cols; j += per * 8) {
-            const int n = static_cast<int>(min(static_cast<int64_t>(8), a.cols - j));
-            float v[8];
-            code_values(load_codes(a.codes + i * a.ld_codes + j, n, true), a.scales[i * a.ld_scales + j / kBlock], v);
-            if (a.Z) store8(static_cast<T*>(a.Z) + i * a.ldz + j, n, true, v);
-            if (!a.Y) continue;
-            if (a.act != GLR_ACT_NONE)
+    const int64_t per8 = 8LL << shift, col = (threadIdx.x & ((1 << shift) - 1)) * 8, own = threadIdx.x >> shift, group = kThreads >> shift;
+    const bool one = a.cols <= per8;
+    const int64_t step = gridDim.x * group;
+    for (int64_t first = blockIdx.x * group; first < a.rows; first += one ? 2 * step : step)
+        for (int64_t c = 0; c < a.cols; c += 2 * per8) {
+            const Pair at(first + own, first + step + own, one, c + col, per8, a.rows, a.cols);
+            uint2 codes[2];
+            uint32_t s[2];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = linear::act_value<sizeof(T) == 2>(v[e], a.act);
-            store8(static_cast<T*>(a.Y) + i * a.ldy + j, n, true, v);
+            for (int u = 0; u < 2; ++u) {
+                codes[u] = load_codes(a.codes + at.i[u] * a.ld_codes + at.j[u], at.n[u], true);
+                s[u] = at.n[u] > 0 ? a.scales[at.i[u] * a.ld_scales + at.j[u] / kBlock] : 0;
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if (at.n[u] <= 0) continue;
+                float v[8];
+                code_values(codes[u], s[u], v);
+                if (a.Z) store8(static_cast<T*>(a.Z) + at.i[u] * a.ldz + at.j[u], at.n[u], true, v);
+                if (!a.Y) continue;
+                if (a.act != GLR_ACT_NONE)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = linear::act_value<sizeof(T) == 2>(v[e], a.act);
+                store8(static_cast<T*>(a.Y) + at.i[u] * a.ldy + at.j[u], at.n[u], true, v);
+            }
         }
 }
 
