@@ -24,6 +24,8 @@ struct Product {
     const void* bias;
     const void* add; int64_t ldadd;
     const void* pre; int64_t ldpre;
+    const int8_t* pre_codes; int64_t ldpc;      // kGradInput: pre in 8 bits (glr_rows.cuh), in place of pre
+    const uint8_t* pre_scales; int64_t ldps;
     void* aux; int64_t ldaux;
     void* outs[GLR_MAX_NODES];              // kGradWeight: each node's M x N result, contiguous
     int* err;
@@ -47,6 +49,10 @@ struct Plan { Way way; TcPlan tc; };
 Plan plan_of(const Product& p);
 cudaError_t product(const Product& p, void* workspace, int64_t workspace_bytes, cudaStream_t st);
 int sm_count();                                 // of the current device; 152 without one
+
+// glr_linear_grad_input with the pre-activation in 8 bits; the arguments' preact and act are not looked at.
+int grad_input_packed(const char* who, const glr_linear_grad_input_args& a, const int8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds,
+                      int act, cudaStream_t st);
 
 // sums[b][j] = sum over the rows of node b of x(i, j), x rows x n in rows of ldx
 struct ColumnSums {

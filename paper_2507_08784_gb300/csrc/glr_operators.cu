@@ -141,6 +141,18 @@ int product_workspace(int rc, const linear::Product& p, int64_t* bytes) {
 
 }  // namespace
 
+int glr::linear::grad_input_packed(const char* who, const glr_linear_grad_input_args& a, const int8_t* codes, int64_t ldc, const uint8_t* scales,
+                                   int64_t lds, int act, cudaStream_t st) {
+    linear::Product p;
+    glr_linear_grad_input_args plain = a;
+    plain.act = GLR_ACT_NONE;
+    plain.preact = nullptr;
+    if (int rc = grad_input_product(who, &plain, p)) return rc;
+    p.act = act;
+    if (act != GLR_ACT_NONE) { p.pre_codes = codes; p.ldpc = ldc; p.pre_scales = scales; p.ldps = lds; }
+    return run_product(who, p, a.workspace, a.workspace_bytes, st);
+}
+
 extern "C" int glr_linear(const glr_linear_args* a, void* stream) {
     linear::Product p;
     const int rc = linear_product("glr_linear", a, p);

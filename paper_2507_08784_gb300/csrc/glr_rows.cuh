@@ -233,13 +233,12 @@ struct Pack {
     uint8_t* scales; int64_t ld_scales;
 };
 cudaError_t pack(const Pack& a, int dtype, cudaStream_t st);
-// Y (may be null) receives act(value), Z (may be null) the values themselves.
+// Y receives act(value).
 struct Unpack {
     int64_t rows, cols;
     const int8_t* codes; int64_t ld_codes;
     const uint8_t* scales; int64_t ld_scales;
     void* Y; int64_t ldy;
-    void* Z; int64_t ldz;
     int act;
 };
 cudaError_t unpack(const Unpack& a, int dtype, cudaStream_t st);

@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(kThreads) pack_kernel(const __grid_constant__ 
         }
 }
 
-template <class T>
+template <class T, int ACT>
 __global__ void __launch_bounds__(kThreads) unpack_kernel(const __grid_constant__ Unpack a, int shift) {
     chain_begin();
     const int64_t per8 = 8LL << shift, col = (threadIdx.x & ((1 << shift) - 1)) * 8, own = threadIdx.x >> shift, group = kThreads >> shift;
@@ -108,11 +108,8 @@ __global__ void __launch_bounds__(kThreads) unpack_kernel(const __grid_constant_
                 if (at.n[u] <= 0) continue;
                 float v[8];
                 code_values(codes[u], s[u], v);
-                if (a.Z) store8(static_cast<T*>(a.Z) + at.i[u] * a.ldz + at.j[u], at.n[u], true, v);
-                if (!a.Y) continue;
-                if (a.act != GLR_ACT_NONE)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = linear::act_value<sizeof(T) == 2>(v[e], a.act);
+                for (int e = 0; e < 8; ++e) v[e] = linear::act_value<sizeof(T) == 2>(v[e], ACT);
                 store8(static_cast<T*>(a.Y) + at.i[u] * a.ldy + at.j[u], at.n[u], true, v);
             }
         }
@@ -127,8 +124,6 @@ __global__ void __launch_bounds__(kThreads) unpack_apart_kernel(const __grid_con
         const int64_t i = q / parts, first = (q - i * parts) * 256;
         float v[8];
         load_blocks(a.codes + i * a.ld_codes, a.scales + i * a.ld_scales, first, a.cols, v);
-        if (a.Z) store_apart(static_cast<T*>(a.Z) + i * a.ldz, first, a.cols, v);
-        if (!a.Y) continue;
         if (a.act != GLR_ACT_NONE)
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = linear::act_value<sizeof(T) == 2>(v[e], a.act);
@@ -147,6 +142,12 @@ unsigned blocks_of(int64_t rows, int shift) {
     return static_cast<unsigned>(std::min<int64_t>((rows + (kThreads >> shift) - 1) / (kThreads >> shift), 152 * 32));
 }
 
+template <class T>
+auto unpack_of(int act) {
+    return act == GLR_ACT_RELU ? unpack_kernel<T, GLR_ACT_RELU> : act == GLR_ACT_GELU ? unpack_kernel<T, GLR_ACT_GELU>
+         : act == GLR_ACT_GELU_TANH ? unpack_kernel<T, GLR_ACT_GELU_TANH> : act == GLR_ACT_SILU ? unpack_kernel<T, GLR_ACT_SILU>
+                                    : unpack_kernel<T, GLR_ACT_NONE>;
+}
 unsigned apart_blocks(int64_t tasks) { return static_cast<unsigned>(std::min<int64_t>((tasks + kThreads / 32 - 1) / (kThreads / 32), 152 * 32)); }
 
 }  // namespace
@@ -162,17 +163,17 @@ cudaError_t pack(const Pack& a, int dtype, cudaStream_t st) {
 }
 
 cudaError_t unpack(const Unpack& a, int dtype, cudaStream_t st) {
-    if (a.rows == 0 || a.cols == 0 || (!a.Y && !a.Z)) return cudaSuccess;
+    if (a.rows == 0 || a.cols == 0) return cudaSuccess;
     const int64_t es = dtype == GLR_BF16 ? 2 : 4, several = a.rows > 1;
-    if ((a.Y && !on(a.Y, several * a.ldy * es, 16)) || (a.Z && !on(a.Z, several * a.ldz * es, 16)) || !on(a.codes, several * a.ld_codes, 8)) {
+    if (!on(a.Y, several * a.ldy * es, 16) || !on(a.codes, several * a.ld_codes, 8)) {
         const int64_t parts = (a.cols + 255) / 256;
         return dtype == GLR_BF16 ? launch_chain(unpack_apart_kernel<__nv_bfloat16>, apart_blocks(a.rows * parts), kThreads, 0, st, a, parts)
                                  : launch_chain(unpack_apart_kernel<float>, apart_blocks(a.rows * parts), kThreads, 0, st, a, parts);
     }
     const int shift = threads_shift(a.cols);
     const dim3 grid(blocks_of(a.rows, shift));
-    return dtype == GLR_BF16 ? launch_chain(unpack_kernel<__nv_bfloat16>, grid, kThreads, 0, st, a, shift)
-                             : launch_chain(unpack_kernel<float>, grid, kThreads, 0, st, a, shift);
+    return dtype == GLR_BF16 ? launch_chain(unpack_of<__nv_bfloat16>(a.act), grid, kThreads, 0, st, a, shift)
+                             : launch_chain(unpack_of<float>(a.act), grid, kThreads, 0, st, a, shift);
 }
 
 }  // namespace rows

@@ -7,6 +7,7 @@
 // bf16 operands go through mma.sync.m16n8k16; fp32 ones through m16n8k8 in the 3xTF32 form
 // (x = hi + lo, a b ~ hi hi + hi lo + lo hi, a few 2^-21 relative a product), accumulated in fp32.
 #include "glr_linear.cuh"
+#include "glr_rows.cuh"
 
 namespace glr {
 namespace linear {
@@ -188,7 +189,10 @@ __device__ __forceinline__ void finish(const Product& p, int node, int64_t i, in
         put(p.out, i * p.ldo + j, p.dtype, y);
     } else {
         const float g = p.add ? acc + get(p.add, i * p.ldadd + j, p.dtype) : acc;
-        const float d = p.pre ? g * act_slope<false>(get(p.pre, i * p.ldpre + j, p.dtype), p.act) : g;
+        const float z = p.pre_codes ? static_cast<float>(p.pre_codes[i * p.ldpc + j]) * rows::scale_value(p.pre_scales[i * p.ldps + j / rows::kBlock])
+                      : p.pre       ? get(p.pre, i * p.ldpre + j, p.dtype)
+                                    : 0.f;
+        const float d = p.pre || p.pre_codes ? g * act_slope<false>(z, p.act) : g;
         if (p.aux) put(p.aux, i * p.ldaux + j, p.dtype, g);
         put(p.out, i * p.ldo + j, p.dtype, d);
     }

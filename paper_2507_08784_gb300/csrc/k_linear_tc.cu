@@ -33,6 +33,7 @@
 #include "glr_host.cuh"
 #include "glr_linear.cuh"
 #include "glr_ptx.cuh"
+#include "glr_rows.cuh"
 
 namespace glr {
 namespace linear {
@@ -244,6 +245,16 @@ __device__ __forceinline__ void act8(float (&v)[8], int act) {
     }
 }
 
+// Eight pre-activations kept in 8 bits, n of them there, one by one.
+template <bool COLUMN>
+__device__ __forceinline__ void codes8(const Product& p, int64_t i, int64_t j, int n, float (&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int64_t row = COLUMN ? i + e : i, col = COLUMN ? j : j + e;
+        x[e] = e < n ? static_cast<float>(p.pre_codes[row * p.ldpc + col]) * rows::scale_value(p.pre_scales[row * p.ldps + col / rows::kBlock]) : 0.f;
+    }
+}
+
 // The epilogue on eight elements: acc in v.  They are neighbouring columns of a row (i, j), or with COLUMN neighbouring
 // rows of a column, for matrices that do not lie on 16 bytes: then neighbouring lanes are neighbouring columns, and an
 // access covers whole sectors all the same (4096 x 4096 x 512 bf16, results in rows of 4099: 83 -> 40 us).
@@ -282,8 +293,11 @@ __device__ __forceinline__ void epilogue8(const TcArgs& a, int node, int64_t i, 
     } else {
         if (p.add) added(x);
         if (p.aux) put(p.aux, p.ldaux, 16, v);
-        if (p.pre) {
-            if (pre && n == 8) widen8(*pre, x);
+        if (p.pre || p.pre_codes) {
+            if (p.pre_codes) {
+                if (pre && n == 8 && (a.wide & 8)) rows::code_values(make_uint2(pre->x, pre->y), pre->z, x);
+                else codes8<COLUMN>(p, i, j, n, x);
+            } else if (pre && n == 8) widen8(*pre, x);
             else get(p.pre, p.ldpre, 8, x);
             act8<true, DT == GLR_BF16>(x, p.act);
 #pragma unroll
@@ -526,6 +540,10 @@ __global__ void __launch_bounds__(threads_of(epi_warps(PROMOTE && DT == GLR_F32)
                         if (in && a.p.add) ahead[q] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.p.add) + i * a.p.ldadd + j);
                         if (MODE == kGradInput && in && a.p.pre)
                             ahead[q + 4] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.p.pre) + i * a.p.ldpre + j);
+                        if (MODE == kGradInput && in && a.p.pre_codes && (a.wide & 8)) {
+                            const uint2 c = *reinterpret_cast<const uint2*>(a.p.pre_codes + i * a.p.ldpc + j);
+                            ahead[q + 4] = make_uint4(c.x, c.y, a.p.pre_scales[i * a.p.ldps + j / rows::kBlock], 0);
+                        }
                     }
                 }
                 float v[32];
@@ -1016,7 +1034,8 @@ cudaError_t tc_product(const Product& p, const TcPlan& plan, void* workspace, cu
         for (int i = 0; i < p.nodes; ++i) a.wide = a.wide && on16(p.outs[i]);
     } else {
         a.wide = (on16(p.out) && p.ldo % per16 == 0 ? 1 : 0) | (on16(p.bias) ? 2 : 0) | (on16(p.add) && p.ldadd % per16 == 0 ? 4 : 0) |
-                 (on16(p.pre) && p.ldpre % per16 == 0 ? 8 : 0) | (on16(p.aux) && p.ldaux % per16 == 0 ? 16 : 0);
+                 (p.pre_codes ? (reinterpret_cast<uintptr_t>(p.pre_codes) % 8 == 0 && p.ldpc % 8 == 0 ? 8 : 0)
+                              : on16(p.pre) && p.ldpre % per16 == 0 ? 8 : 0) | (on16(p.aux) && p.ldaux % per16 == 0 ? 16 : 0);
     }
     const int need = p.mode == kGradWeight ? 1 : 1 | (p.add ? 4 : 0) | (p.pre ? 8 : 0) | (p.aux ? 16 : 0);
     a.columns = (a.wide & need) != need;

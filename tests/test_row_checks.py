@@ -150,9 +150,8 @@ def test_workspace_queries(lib):
     assert need("glr_embedding_grad", rows=5000) > 0 and need("glr_embedding_grad", rows=0) == 0 and need("glr_embedding_grad", rows=5000, d=0) == 0
     assert need("glr_norm_grad") > 0 and need("glr_norm_grad", dweight=None) == 0
     both = need("glr_linear_grad_checkpoint")
-    assert both >= 2 * 8 * 33 * 4
-    assert need("glr_linear_grad_checkpoint", dX=None) < both and need("glr_linear_grad_checkpoint", dW=None, db=None) < both
-    assert need("glr_linear_grad_checkpoint", act=0) < both
+    assert both >= 8 * 33 * 4
+    assert need("glr_linear_grad_checkpoint", dX=None) <= both and need("glr_linear_grad_checkpoint", dW=None, db=None) < both
 
 
 def _calls():
