@@ -258,15 +258,13 @@ __device__ __noinline__ int select_keys(const RowVectors<T>& row, int topk, uint
 
 // The j-th largest of the lanes' values.
 __device__ __forceinline__ float lanes_largest(float v, int j) {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int k = 2; k <= 32; k *= 2)
-#pragma unroll
-        for (int s = k / 2; s > 0; s /= 2) {
-            const float o = __shfl_xor_sync(0xffffffffu, v, s);
-            v = ((lane & s) == 0) == ((lane & k) == 0) ? fmaxf(v, o) : fminf(v, o);
-        }
-    return __shfl_sync(0xffffffffu, v, j - 1);
+    uint32_t o = order_of(v), most = 0;
+    for (int left = j; left > 0;) {
+        most = __reduce_max_sync(0xffffffffu, o);
+        left -= __popc(__ballot_sync(0xffffffffu, o == most));       // equal ones at once
+        if (o == most) o = 0;
+    }
+    return most == 0 ? kLowest : fmaxf(logit_of(most), kLowest);
 }
 // A value that at least j of the lanes' n values each reach, j <= 32 n: sixteen bisections between the least and the largest of
 // them, as integers of the same order (1 is that of no logit, and below all of them).
@@ -286,6 +284,9 @@ __device__ __noinline__ float lanes_many(const float (&v)[N], int j) {
     }
     return fmaxf(logit_of(lo), kLowest);
 }
+
+// The order of an entry's maximum, of which it has the upper half: no less than the upper half of the maximum's own order.
+__device__ __forceinline__ uint32_t entry_order(uint32_t entry) { return order_of(__uint_as_float(entry & 0xffff0000u)); }
 
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -325,8 +326,8 @@ __global__ void __launch_bounds__(NT, 1280 / NT) token_logp_kernel(const __grid_
     __shared__ Stat stats[W + 1];
     __shared__ float bounds[W];
     __shared__ int scratch[4];
-    // Each warp's vectors that hold an element above the bound, with the upper half of their maximum's order; the ordered keys in
-    // the end.  (16 KiB in all: the loads' lines in flight need the rest of the SM's memory, with 40 KiB a CTA 4096 rows took 30 us more.)
+    // Each warp's vectors that hold an element above the bound, with the upper half of their maximum; the ordered keys in the
+    // end.  (16 KiB in all: the loads' lines in flight need the rest of the SM's memory, with 40 KiB a CTA 4096 rows took 30 us more.)
     __shared__ __align__(16) uint64_t ordered[TOP ? kMaxKeys : 1];
     uint32_t* list = reinterpret_cast<uint32_t*>(ordered);
     __shared__ uint64_t thin[TOP ? kMaxKeys : 1];    // the elements above the last bound (the radix selection's bins)
@@ -351,6 +352,8 @@ __global__ void __launch_bounds__(NT, 1280 / NT) token_logp_kernel(const __grid_
 #pragma unroll
     for (int y = 0; y < A; ++y) most[y] = kLowest;
     int round = 0, due = 0, entries = 0;
+    const uint32_t before = (1u << lane) - 1;
+    uint32_t* mine_list = list + warp * kWarpList;
     for (int q0 = row.begin; q0 < row.end; q0 += A * NT, ++round) {
         Eight<T> v[A];
         float top[A];
@@ -364,7 +367,11 @@ __global__ void __launch_bounds__(NT, 1280 / NT) token_logp_kernel(const __grid_
         }
         float m_round = -kInf;
 #pragma unroll
-        for (int y = 0; y < A; ++y) { top[y] = v[y].top(); m_round = fmaxf(m_round, top[y]); if (TOP) most[y] = fmaxf(most[y], top[y]); }
+        for (int y = 0; y < A; ++y) { top[y] = v[y].top(); m_round = fmaxf(m_round, top[y]); }
+        if (TOP && !few) {
+#pragma unroll
+            for (int y = 0; y < A; ++y) most[y] = fmaxf(most[y], top[y]);
+        }
         const float m = fmaxf(t.m, m_round);
         if (m > t.m) {
             const float d = fmaxf((t.m - m) * c, -1e30f), x = exp2_fast(d);
@@ -394,9 +401,9 @@ __global__ void __launch_bounds__(NT, 1280 / NT) token_logp_kernel(const __grid_
             if (round == due && (round == 0 || q0 + A * NT < row.end)) {
                 due = 2 * due + 1;
                 const float least = few ? lanes_largest(t.m, mine) : lanes_many(most, mine);
-                if (lane == 0) static_cast<volatile float*>(bounds)[warp] = least;
-                if (round == 0) __syncthreads();     // from then on every warp has one; a stale one is a bound too
-                float b = static_cast<volatile float*>(bounds)[lane & (W - 1)];
+                if (lane == 0) bounds[warp] = least;
+                __syncthreads();                     // a warp far behind would keep the bound down for all
+                float b = bounds[lane & (W - 1)];       // (a later one is a bound too)
 #pragma unroll
                 for (int o = 1; o < W; o *= 2) b = fminf(b, __shfl_xor_sync(0xffffffffu, b, o));
                 bound = fmaxf(bound, b);
@@ -405,9 +412,9 @@ __global__ void __launch_bounds__(NT, 1280 / NT) token_logp_kernel(const __grid_
                     int kept = 0;
                     __syncwarp();
                     for (int q = 0; q < entries; q += 32) {
-                        const uint32_t entry = q + lane < entries ? list[warp * kWarpList + q + lane] : 0;
-                        const uint32_t some = __ballot_sync(0xffffffffu, q + lane < entries && entry >= least_order);
-                        if (some >> lane & 1) list[warp * kWarpList + kept + __popc(some & ((1u << lane) - 1))] = entry;
+                        const uint32_t entry = q + lane < entries ? mine_list[q + lane] : 0;
+                        const uint32_t some = __ballot_sync(0xffffffffu, q + lane < entries && entry_order(entry) >= least_order);
+                        if (some >> lane & 1) mine_list[kept + __popc(some & before)] = entry;
                         kept += __popc(some);
                         __syncwarp();
                     }
@@ -415,12 +422,13 @@ __global__ void __launch_bounds__(NT, 1280 / NT) token_logp_kernel(const __grid_
                 }
             }
             if (__any_sync(0xffffffffu, m_round >= bound)) {
+                const uint32_t place = static_cast<uint32_t>(round * A * 32 + lane);
 #pragma unroll
                 for (int y = 0; y < A; ++y) {
                     const uint32_t some = __ballot_sync(0xffffffffu, top[y] >= bound);
-                    const int at = entries + __popc(some & ((1u << lane) - 1));
-                    if (top[y] >= bound && at < kWarpList)
-                        list[warp * kWarpList + at] = (order_of(top[y]) & 0xffff0000u) | static_cast<uint32_t>((round * A + y) * 32 + lane);
+                    if (some == 0) continue;
+                    const int at = entries + __popc(some & before);
+                    if (top[y] >= bound && at < kWarpList) mine_list[at] = (__float_as_uint(top[y]) & 0xffff0000u) | (place + y * 32);
                     entries += __popc(some);
                 }
             }
@@ -449,8 +457,8 @@ __global__ void __launch_bounds__(NT, 1280 / NT) token_logp_kernel(const __grid_
             for (int w = 1; w < W; ++w) b = fminf(b, bounds[w]);
             const uint32_t least = order_of(b) & 0xffff0000u;
             for (int q = lane; q < entries; q += 32) {
-                const uint32_t entry = list[warp * kWarpList + q];
-                if (entry < least) continue;         // of a maximum below the last bound
+                const uint32_t entry = mine_list[q];
+                if (entry_order(entry) < least) continue;        // of a maximum below the last bound
                 const int at = row.begin + static_cast<int>(entry >> 5 & 0x7ffu) * NT + warp * 32 + static_cast<int>(entry & 31);
                 Eight<T> v;
                 row.load(at, v);
@@ -541,42 +549,67 @@ __global__ void __launch_bounds__(NT, 1280 / NT) token_logp_kernel(const __grid_
 }
 
 // dz_v = (dlogp (e_token - p_v) - dentropy p_v (log p_v + entropy)) / tau, with log p_v = z_v / tau - lse; the same elements by
-// the same thread, so dz may be z.
-template <class T>
+// the same thread, so dz may be z.  Bound by HBM: 6000 x 65536 bf16 with both terms 238 us, 6.6 TB/s
+// (one vector's load at a time 293).
+template <class T> constexpr int kGradAhead = sizeof(T) == 2 ? 4 : 2;
+template <class T, bool ENT>
 __global__ void __launch_bounds__(kThreads) token_logp_grad_kernel(const __grid_constant__ TokenLogpGrad a, int parts) {
     chain_begin();
+    constexpr int A = kGradAhead<T>;
     const int64_t i = blockIdx.x / parts;
     const int part = static_cast<int>(blockIdx.x % parts);
     const T* z = static_cast<const T*>(a.z) + i * a.ldz;
     T* dz = static_cast<T*>(a.dz) + i * a.lddz;
     const RowVectors<T> row(z, static_cast<int>(a.vocab), part, parts);
-    const int64_t y = a.tokens.p ? a.tokens.at(i) : -1;
-    const bool counted = y >= 0 && y < a.vocab;
+    const int64_t y64 = a.tokens.p ? a.tokens.at(i) : -1;
+    const int y = y64 >= 0 && y64 < a.vocab ? static_cast<int>(y64) : -8;
     const float lse = a.lse[i];
-    const bool some = lse != -__int_as_float(0x7f800000);
-    const float coef = a.dlogp && counted && some ? a.dlogp[i] * a.inv_tau : 0.f;
-    const float bonus = a.dentropy && some ? a.dentropy[i] * a.inv_tau : 0.f, h = bonus != 0.f ? a.entropy[i] : 0.f;
-    const float tail = a.inv_tau;
+    const bool some = lse != -kInf;
+    const float coef = a.dlogp && y >= 0 && some ? a.dlogp[i] * a.inv_tau : 0.f;
+    const float bonus = ENT && some ? a.dentropy[i] * a.inv_tau : 0.f;
+    const bool read = coef != 0.f || bonus != 0.f;   // (a NaN among them too)
+    // the factor of p: -coef - bonus (log p + entropy)
+    const float base = -(bonus != 0.f ? fmaf(bonus, a.entropy[i], coef) : coef);
     const bool wide = (reinterpret_cast<uintptr_t>(dz) & 15) == (reinterpret_cast<uintptr_t>(z) & 15);
-    for (int q = row.begin + threadIdx.x; q < row.end; q += kThreads) {
-        float v[8];
-        row.load(q, v);
-        const int j = row.first(q);
+    for (int q0 = row.begin; q0 < row.end; q0 += A * kThreads) {
+        Eight<T> x[A];
+        const bool inside = q0 > row.begin && q0 + A * kThreads < row.end;   // whole vectors all of them
+        if (!read) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float lp = v[e] * tail - lse, p = exp2_fast(lp * kLog2e);
-            float d = -coef * p;
-            if (bonus != 0.f) d -= p != 0.f ? bonus * p * (lp + h) : 0.f;
-            if (j + e == y) d += coef;
-            v[e] = some && (coef != 0.f || bonus != 0.f) ? d : 0.f;
-        }
-        T* to = dz + j;
-        if (wide && j >= 0 && j + 8 <= a.vocab) {
-            store8(to, 8, true, v);
+            for (int u = 0; u < A; ++u) x[u].none();
+        } else if (inside) {
+            const T* p = row.base + (q0 + static_cast<int>(threadIdx.x)) * 8;
+#pragma unroll
+            for (int u = 0; u < A; ++u) x[u].load(p + u * kThreads * 8);
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (j + e >= 0 && j + e < a.vocab) put(to + e, v[e]);
+            for (int u = 0; u < A; ++u) row.load(q0 + u * kThreads + threadIdx.x, x[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < A; ++u) {
+            const int q = q0 + u * kThreads + threadIdx.x, j = row.first(q);
+            if (q >= row.end) continue;
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) unpack2(x[u].pair(e), v[2 * e], v[2 * e + 1]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float lp = fmaf(v[e], a.inv_tau, -lse), p = exp2_fast(lp * kLog2e);
+                // (below 2^-126 p is 0, and a log p of -infinity no factor for it)
+                v[e] = !read ? 0.f : ENT ? p * fmaf(-bonus, fmaxf(lp, -200.f), base) : p * base;
+            }
+            if (y >= j && y < j + 8) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += j + e == y ? coef : 0.f;
+            }
+            T* to = dz + j;
+            if (wide && j >= 0 && j + 8 <= a.vocab) {
+                store8(to, 8, true, v);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (j + e >= 0 && j + e < a.vocab) put(to + e, v[e]);
+            }
         }
     }
 }
@@ -616,8 +649,10 @@ cudaError_t token_logp_grad(const TokenLogpGrad& a, int dtype, cudaStream_t st) 
     const int64_t most = std::max<int64_t>(1, a.vocab / (8 * 4 * kThreads));
     const int parts = static_cast<int>(std::min(most, std::max<int64_t>(1, 152 * 8 / a.rows)));
     const dim3 grid(static_cast<unsigned>(a.rows * parts));
-    return dtype == GLR_BF16 ? launch_chain(token_logp_grad_kernel<__nv_bfloat16>, grid, kThreads, 0, st, a, parts)
-                             : launch_chain(token_logp_grad_kernel<float>, grid, kThreads, 0, st, a, parts);
+    using H = __nv_bfloat16;
+    return launch_chain(dtype == GLR_BF16 ? (a.dentropy ? token_logp_grad_kernel<H, true> : token_logp_grad_kernel<H, false>)
+                                          : (a.dentropy ? token_logp_grad_kernel<float, true> : token_logp_grad_kernel<float, false>),
+                        grid, kThreads, 0, st, a, parts);
 }
 
 }  // namespace rows
