@@ -47,72 +47,77 @@ template <> struct Raw<float> {
     }
 };
 
-// Two vectors of eight columns a thread at a time: of a row, or, where a row has no more than one for each thread, of two rows.
+// Tasks of up to 32 threads (1 << shift), two vectors of eight columns each: `chunks` of a row, or two rows where a row has no more
+// than one vector for each thread.
+struct Tasks {
+    int shift;
+    int64_t chunks, all;
+};
 struct Pair {
     int64_t i[2], j[2];
     int n[2];
-    __device__ __forceinline__ Pair(int64_t row, int64_t next, bool one, int64_t col, int64_t per8, int64_t rows, int64_t cols) {
-        i[0] = row; i[1] = one ? next : row;
-        j[0] = col; j[1] = one ? col : col + per8;
+    __device__ __forceinline__ Pair(const Tasks& t, int64_t q, int64_t rows, int64_t cols) {
+        const int64_t per8 = 8LL << t.shift, col = (threadIdx.x & ((1 << t.shift) - 1)) * 8;
+        const bool one = cols <= per8;
+        int64_t row = one ? 2 * q : q;
+        if (t.chunks > 1) row = t.all <= 0x7fffffff ? static_cast<uint32_t>(q) / static_cast<uint32_t>(t.chunks) : q / t.chunks;
+        i[0] = row; i[1] = one ? row + 1 : row;
+        j[0] = one ? col : (q - row * t.chunks) * 2 * per8 + col;
+        j[1] = one ? col : j[0] + per8;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) n[u] = i[u] < rows ? static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(8), cols - j[u]))) : 0;
+        for (int u = 0; u < 2; ++u)
+            n[u] = q < t.all && i[u] < rows ? static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(8), cols - j[u]))) : 0;
     }
 };
 
 template <class T>
-__global__ void __launch_bounds__(kThreads) pack_kernel(const __grid_constant__ Pack a, int shift, bool wide, bool wide_codes) {
+__global__ void __launch_bounds__(kThreads) pack_kernel(const __grid_constant__ Pack a, const Tasks t, bool wide, bool wide_codes) {
     chain_begin();
-    const int64_t per8 = 8LL << shift, col = (threadIdx.x & ((1 << shift) - 1)) * 8, own = threadIdx.x >> shift, group = kThreads >> shift;
-    const bool one = a.cols <= per8;
-    const int64_t step = gridDim.x * group;
-    // all lanes of a block are there: the loops go by the CTA's first row and the row's stretches
-    for (int64_t first = blockIdx.x * group; first < a.rows; first += one ? 2 * step : step)
-        for (int64_t c = 0; c < a.cols; c += 2 * per8) {
-            const Pair at(first + own, first + step + own, one, c + col, per8, a.rows, a.cols);
-            Raw<T> x[2];
+    const int64_t group = kThreads >> t.shift;
+    // all lanes of a block are there: the loop goes by the CTA's first task
+    for (int64_t first = blockIdx.x * group; first < t.all; first += gridDim.x * group) {
+        const Pair at(t, first + (threadIdx.x >> t.shift), a.rows, a.cols);
+        Raw<T> x[2];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) x[u].load(static_cast<const T*>(a.X) + at.i[u] * a.ldx + at.j[u], at.n[u], wide);
+        for (int u = 0; u < 2; ++u) x[u].load(static_cast<const T*>(a.X) + at.i[u] * a.ldx + at.j[u], at.n[u], wide);
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                uint32_t m = x[u].most();
-                m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-                m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-                const uint32_t s = scale_of(m);
-                if (at.n[u] <= 0) continue;
-                float v[8];
-                x[u].get(v);
-                store_codes(a.codes + at.i[u] * a.ld_codes + at.j[u], at.n[u], wide_codes, block_codes(v, s));
-                if ((threadIdx.x & 3) == 0) a.scales[at.i[u] * a.ld_scales + at.j[u] / kBlock] = static_cast<uint8_t>(s);
-            }
+        for (int u = 0; u < 2; ++u) {
+            uint32_t m = x[u].most();
+            m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+            m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+            const uint32_t s = scale_of(m);
+            if (at.n[u] <= 0) continue;
+            float v[8];
+            x[u].get(v);
+            store_codes(a.codes + at.i[u] * a.ld_codes + at.j[u], at.n[u], wide_codes, block_codes(v, s));
+            if ((threadIdx.x & 3) == 0) a.scales[at.i[u] * a.ld_scales + at.j[u] / kBlock] = static_cast<uint8_t>(s);
         }
+    }
 }
 
 template <class T, int ACT>
-__global__ void __launch_bounds__(kThreads) unpack_kernel(const __grid_constant__ Unpack a, int shift) {
+__global__ void __launch_bounds__(kThreads) unpack_kernel(const __grid_constant__ Unpack a, const Tasks t) {
     chain_begin();
-    const int64_t per8 = 8LL << shift, col = (threadIdx.x & ((1 << shift) - 1)) * 8, own = threadIdx.x >> shift, group = kThreads >> shift;
-    const bool one = a.cols <= per8;
-    const int64_t step = gridDim.x * group;
-    for (int64_t first = blockIdx.x * group; first < a.rows; first += one ? 2 * step : step)
-        for (int64_t c = 0; c < a.cols; c += 2 * per8) {
-            const Pair at(first + own, first + step + own, one, c + col, per8, a.rows, a.cols);
-            uint2 codes[2];
-            uint32_t s[2];
+    const int64_t group = kThreads >> t.shift;
+    for (int64_t first = blockIdx.x * group; first < t.all; first += gridDim.x * group) {
+        const Pair at(t, first + (threadIdx.x >> t.shift), a.rows, a.cols);
+        uint2 codes[2];
+        uint32_t s[2];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                codes[u] = load_codes(a.codes + at.i[u] * a.ld_codes + at.j[u], at.n[u], true);
-                s[u] = at.n[u] > 0 ? a.scales[at.i[u] * a.ld_scales + at.j[u] / kBlock] : 0;
-            }
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                if (at.n[u] <= 0) continue;
-                float v[8];
-                code_values(codes[u], s[u], v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = linear::act_value<sizeof(T) == 2>(v[e], ACT);
-                store8(static_cast<T*>(a.Y) + at.i[u] * a.ldy + at.j[u], at.n[u], true, v);
-            }
+        for (int u = 0; u < 2; ++u) {
+            codes[u] = load_codes(a.codes + at.i[u] * a.ld_codes + at.j[u], at.n[u], true);
+            s[u] = at.n[u] > 0 ? a.scales[at.i[u] * a.ld_scales + at.j[u] / kBlock] : 0;
         }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            if (at.n[u] <= 0) continue;
+            float v[8];
+            code_values(codes[u], s[u], v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = linear::act_value<sizeof(T) == 2>(v[e], ACT);
+            store8(static_cast<T*>(a.Y) + at.i[u] * a.ldy + at.j[u], at.n[u], true, v);
+        }
+    }
 }
 
 // Rows off 16 bytes (codes off 8): 256 columns a warp.
@@ -133,15 +138,18 @@ __global__ void __launch_bounds__(kThreads) unpack_apart_kernel(const __grid_con
 
 bool on(const void* p, int64_t ld_bytes, int64_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0 && ld_bytes % to == 0; }
 
-int threads_shift(int64_t cols) {
-    int shift = 2;
-    while (shift < 8 && (8LL << shift) < cols) ++shift;
-    return shift;
+Tasks tasks_of(int64_t rows, int64_t cols) {
+    Tasks t{2, 1, 0};
+    while (t.shift < 5 && (8LL << t.shift) < cols) ++t.shift;
+    if (cols <= (8LL << t.shift)) { t.all = (rows + 1) / 2; return t; }
+    t.chunks = (cols + (16LL << t.shift) - 1) / (16LL << t.shift);
+    t.all = rows * t.chunks;
+    return t;
 }
-unsigned blocks_of(int64_t rows, int shift) {
-    return static_cast<unsigned>(std::min<int64_t>((rows + (kThreads >> shift) - 1) / (kThreads >> shift), 152 * 32));
+unsigned blocks_of(const Tasks& t) {
+    const int64_t group = kThreads >> t.shift;
+    return static_cast<unsigned>(std::min<int64_t>((t.all + group - 1) / group, 152 * 32));
 }
-
 template <class T>
 auto unpack_of(int act) {
     return act == GLR_ACT_RELU ? unpack_kernel<T, GLR_ACT_RELU> : act == GLR_ACT_GELU ? unpack_kernel<T, GLR_ACT_GELU>
@@ -156,10 +164,10 @@ cudaError_t pack(const Pack& a, int dtype, cudaStream_t st) {
     if (a.rows == 0 || a.cols == 0) return cudaSuccess;
     const int64_t es = dtype == GLR_BF16 ? 2 : 4;
     const bool wide = on(a.X, a.rows > 1 ? a.ldx * es : 0, 16), wide_codes = on(a.codes, a.rows > 1 ? a.ld_codes : 0, 8);
-    const int shift = threads_shift(a.cols);
-    const dim3 grid(blocks_of(a.rows, shift));
-    return dtype == GLR_BF16 ? launch_chain(pack_kernel<__nv_bfloat16>, grid, kThreads, 0, st, a, shift, wide, wide_codes)
-                             : launch_chain(pack_kernel<float>, grid, kThreads, 0, st, a, shift, wide, wide_codes);
+    const Tasks t = tasks_of(a.rows, a.cols);
+    const dim3 grid(blocks_of(t));
+    return dtype == GLR_BF16 ? launch_chain(pack_kernel<__nv_bfloat16>, grid, kThreads, 0, st, a, t, wide, wide_codes)
+                             : launch_chain(pack_kernel<float>, grid, kThreads, 0, st, a, t, wide, wide_codes);
 }
 
 cudaError_t unpack(const Unpack& a, int dtype, cudaStream_t st) {
@@ -170,10 +178,10 @@ cudaError_t unpack(const Unpack& a, int dtype, cudaStream_t st) {
         return dtype == GLR_BF16 ? launch_chain(unpack_apart_kernel<__nv_bfloat16>, apart_blocks(a.rows * parts), kThreads, 0, st, a, parts)
                                  : launch_chain(unpack_apart_kernel<float>, apart_blocks(a.rows * parts), kThreads, 0, st, a, parts);
     }
-    const int shift = threads_shift(a.cols);
-    const dim3 grid(blocks_of(a.rows, shift));
-    return dtype == GLR_BF16 ? launch_chain(unpack_of<__nv_bfloat16>(a.act), grid, kThreads, 0, st, a, shift)
-                             : launch_chain(unpack_of<float>(a.act), grid, kThreads, 0, st, a, shift);
+    const Tasks t = tasks_of(a.rows, a.cols);
+    const dim3 grid(blocks_of(t));
+    return dtype == GLR_BF16 ? launch_chain(unpack_of<__nv_bfloat16>(a.act), grid, kThreads, 0, st, a, t)
+                             : launch_chain(unpack_of<float>(a.act), grid, kThreads, 0, st, a, t);
 }
 
 }  // namespace rows
