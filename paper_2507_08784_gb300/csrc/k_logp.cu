@@ -495,13 +495,17 @@ __global__ void __launch_bounds__(NT, 1280 / NT) token_logp_kernel(const __grid_
     if (parts > 1) {
         if (threadIdx.x == 0) { stats[W] = t; scratch[3] = n; }
         cluster_sync();
-        Stat all{kLowest, 0.f, 0.f};
-        for (int p = 0; p < parts; ++p) {
+        // a CTA's statistics a lane, joined in the same order everywhere
+        t = Stat{kLowest, 0.f, 0.f};
+        if (lane < parts) {
             const float* f = &stats[W].m;
-            const Stat y{peer_float(f, p), peer_float(f + 1, p), peer_float(f + 2, p)};
-            all = p ? join(all, y, c) : y;
+            t = Stat{peer_float(f, lane), peer_float(f + 1, lane), peer_float(f + 2, lane)};
         }
-        t = all;
+        for (int o = 1; o < parts; o *= 2) {
+            const Stat y{__shfl_down_sync(0xffffffffu, t.m, o), __shfl_down_sync(0xffffffffu, t.s, o), __shfl_down_sync(0xffffffffu, t.u, o)};
+            t = join(t, y, c);
+        }
+        t = Stat{__shfl_sync(0xffffffffu, t.m, 0), __shfl_sync(0xffffffffu, t.s, 0), __shfl_sync(0xffffffffu, t.u, 0)};
     }
     const bool some = !(t.s == 0.f);                 // a row with a distribution, or with a NaN
     const float log_s = logf(t.s);
@@ -529,20 +533,23 @@ __global__ void __launch_bounds__(NT, 1280 / NT) token_logp_kernel(const __grid_
         for (int q = threadIdx.x; q < a.topk; q += NT) write(q, q < n ? ordered[q] : 0);
         return;
     }
-    // each CTA's keys go where they rank among all of them
-    int total = 0;
-    for (int p = 0; p < parts; ++p) total += __float_as_int(peer_float(reinterpret_cast<const float*>(scratch + 3), p));
-    for (int q = threadIdx.x; q < n; q += NT) {
-        const uint64_t k = ordered[q];
-        int rank = q;
-        for (int p = 1; p < parts && rank < a.topk; ++p) {
-            const uint32_t peer = (part + p) % parts;
-            int lo = 0, hi = __float_as_int(peer_float(reinterpret_cast<const float*>(scratch + 3), peer));
-            while (lo < hi) { const int mid = (lo + hi) >> 1; if (peer_key(ordered + mid, peer) > k) lo = mid + 1; else hi = mid; }
-            rank += lo;
-        }
-        if (rank < a.topk) write(rank, k);
+    // each CTA's keys go where they rank among all of them: a thread counts those of one peer above one key
+    const auto keys_of = [&](uint32_t rank) { return __float_as_int(peer_float(reinterpret_cast<const float*>(scratch + 3), rank)); };
+    const int total = __reduce_add_sync(0xffffffffu, lane < parts ? keys_of(lane) : 0);
+    int* above = reinterpret_cast<int*>(thin);
+    for (int q = threadIdx.x; q < n; q += NT) above[q] = q;
+    __syncthreads();
+    for (int q = threadIdx.x; q < n * (parts - 1); q += NT) {
+        const int own = q % n;
+        const uint32_t peer = (part + 1 + q / n) % parts;
+        const uint64_t k = ordered[own];
+        int lo = 0, hi = keys_of(peer);
+        while (lo < hi) { const int mid = (lo + hi) >> 1; if (peer_key(ordered + mid, peer) > k) lo = mid + 1; else hi = mid; }
+        if (lo) atomicAdd(&above[own], lo);
     }
+    __syncthreads();
+    for (int q = threadIdx.x; q < n; q += NT)
+        if (above[q] < a.topk) write(above[q], ordered[q]);
     if (part == 0)
         for (int q = total + threadIdx.x; q < a.topk; q += NT) write(q, 0);
     cluster_sync();
