@@ -23,40 +23,28 @@ def lookup(E, tokens, scale):
 def embedding_grad(dY, tokens, nodes, vocab, scale):
     """The gradients, and for each element the sum of absolute terms and the number of terms."""
     rows = dY.shape[0] // nodes
-    G = torch.zeros(nodes, vocab, dY.shape[1], dtype=torch.float64)
-    A, N = torch.zeros_like(G), torch.zeros(nodes, vocab, 1, dtype=torch.float64)
-    for t, v in enumerate(tokens.tolist()):
-        if 0 <= v < vocab:
-            G[t // rows, v] += scale * dY[t].double()
-            A[t // rows, v] += abs(scale) * dY[t].double().abs()
-            N[t // rows, v] += 1
-    return G, A, N
+    ok = (tokens >= 0) & (tokens < vocab)
+    at = (tokens.long() + vocab * (torch.arange(len(tokens)) // max(1, rows)))[ok]
+    add = lambda x: torch.zeros(nodes * vocab, x.shape[1], dtype=torch.float64).index_add_(0, at, x[ok]).view(nodes, vocab, -1)  # noqa: E731
+    d = dY.double()
+    return add(scale * d), add(abs(scale) * d.abs()), add(torch.ones(len(tokens), 1, dtype=torch.float64))
 
 
 def pack(X):
     """Codes, scale bytes and values of a matrix (float32 or bfloat16; exact in 64 bits)."""
-    X = X.double()
     rows, cols = X.shape
-    codes = torch.zeros(rows, cols, dtype=torch.int8)
-    scales = torch.zeros(rows, (cols + 31) // 32, dtype=torch.uint8)
-    values = torch.zeros(rows, cols, dtype=torch.float64)
-    for i in range(rows):
-        for b in range((cols + 31) // 32):
-            x = X[i, 32 * b:32 * b + 32]
-            if not torch.isfinite(x).all():
-                scales[i, b] = 255
-                values[i, 32 * b:32 * b + 32] = math.nan
-                continue
-            most, p = float(x.abs().max()), -127
-            if most > 0:
-                p = max(-127, math.frexp(most / 127)[1] - 2)
-                while most > 127 * 2.0 ** p:
-                    p += 1
-                p = min(p, 121)
-            codes[i, 32 * b:32 * b + 32] = torch.round(x * 2.0 ** -p).clamp(-127, 127).to(torch.int8)        # ties to even
-            scales[i, b] = p + 127
-            values[i, 32 * b:32 * b + 32] = codes[i, 32 * b:32 * b + 32].double() * 2.0 ** p
-    return codes, scales, values
+    blocks = (cols + 31) // 32
+    x = torch.nn.functional.pad(X.double(), (0, 32 * blocks - cols)).view(rows, blocks, 32)
+    finite = torch.isfinite(x).all(2, keepdim=True)
+    x = torch.where(finite, x, 0.0)
+    # the smallest p with 2^p >= most / 127, a quotient that no rounding takes to a power of two from above
+    part, p = torch.frexp(x.abs().amax(2, keepdim=True) / 127)
+    p = torch.where(part == 0.5, p - 1, p)
+    p = torch.where(part == 0, -127, p).clamp(-127, 121)
+    codes = torch.round(x * 2.0 ** -p.double()).clamp(-127, 127)                    # ties to even
+    values = torch.where(finite, codes * 2.0 ** p.double(), math.nan)
+    flat = lambda t: t.reshape(rows, -1)[:, :cols]  # noqa: E731
+    return flat(codes).to(torch.int8), torch.where(finite, p + 127, 255)[:, :, 0].to(torch.uint8), flat(values)
 
 
 def norm(X, residual, weight, eps):

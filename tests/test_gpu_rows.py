@@ -134,6 +134,15 @@ def test_embedding_grad_distributions(glr, kind, accumulate, d):
     assert torch.equal(got, again)
 
 
+@pytest.mark.parametrize("rows,vocab,d", [(135000, 300, 8), (40000, 70000, 16)])
+def test_embedding_grad_of_many_chunks(glr, rows, vocab, d):
+    """More sorted chunks than a tile's table holds, and tiles of many rows with a table of several chunks."""
+    gen = torch.Generator().manual_seed(5)
+    tokens = (torch.rand(rows, generator=gen) ** 3 * vocab).long()
+    tokens[::1000] = -1
+    _embedding_grad(glr, 1, rows, vocab, d, torch.float32, torch.float32, tokens, scale=0.25)
+
+
 def test_embedding_grad_of_no_rows(glr):
     dE = [torch.full((9, 16), 5.0, device="cuda") for _ in range(2)]
     args = (torch.empty(0, 16, device="cuda"), torch.empty(0, device="cuda", dtype=torch.int32), dE)
@@ -211,7 +220,7 @@ def test_codes_of_what_is_not_finite(glr, bad):
 
 @pytest.mark.parametrize("rows,cols,pad,shift", [
     (1, 1, 0, 0), (2, 31, 1, 1), (3, 32, 0, 0), (5, 33, 0, 3), (7, 64, 8, 8), (4, 255, 1, 0), (3, 2048, 0, 0), (2, 2049, 0, 1), (600, 40, 0, 0),
-    (2, 5000, 3, 5), (5000, 8, 0, 0),
+    (2, 5000, 3, 5), (5000, 8, 0, 0), (1500, 520, 0, 0), (3, 40000, 0, 0),
 ])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_pack_and_unpack(glr, rows, cols, pad, shift, dt):
@@ -300,7 +309,7 @@ NORM_SIZES = [(1, 1, 0, 0), (3, 5, 1, 1), (9, 32, 0, 0), (5, 33, 3, 5), (70, 64,
               (4, 2048, 0, 0), (3, 2049, 7, 3), (5, 4096, 0, 0), (2, 8200, 8, 0), (3, 16384, 0, 0), (2, 16385, 0, 1), (2, 32768, 0, 0)]
 
 
-@pytest.mark.parametrize("rows,n,pad,shift", NORM_SIZES)
+@pytest.mark.parametrize("rows,n,pad,shift", NORM_SIZES + [(5000, 136, 0, 0), (1400, 4096, 0, 0), (700, 4100, 0, 0), (2000, 515, 0, 0)])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("full", [True, False])
 def test_norm(glr, rows, n, pad, shift, dt, full):
@@ -501,6 +510,29 @@ def test_token_logp(glr, rows, vocab, topk, pad, shift, dt, tau):
     wide = rows % 2 == 1
     _check_logp(glr, z.t, tokens.to(torch.int64 if wide else torch.int32), tau, topk, torch.int64 if wide else torch.int32)
     z.check()
+
+
+@pytest.mark.parametrize("rows,vocab,topk", [(330, 20000, 48), (900, 9001, 200), (2000, 1500, 90), (400, 40000, 300), (500, 3000, 128)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_token_logp_of_many_rows(glr, rows, vocab, topk, dt):
+    """A CTA a row: alternatives as a stable sort orders them, log-probabilities as log_softmax in 64 bits."""
+    gen = torch.Generator().manual_seed(rows)
+    z = _logits(rows, vocab, DT[dt], 0, 0, gen, 2.0).t
+    z[:, ::97] = -math.inf
+    tokens = torch.randint(0, vocab, (rows,), generator=gen)
+    tokens[tokens % 97 == 0] += 1
+    logp, lse, ent, top, ids = _run_logp(glr, z, tokens.cuda(), 0.9, topk)
+    lp = torch.log_softmax(z.double() / 0.9, 1).cpu()
+    tol = _logp_tol(z.cpu(), 0.9) + 4 * U * 40
+    order = torch.sort(z.cpu(), dim=1, descending=True, stable=True).indices[:, :topk]
+    assert torch.equal(ids.cpu().long(), order)
+    _near(top, lp.gather(1, order), tol)
+    _near(logp, lp.gather(1, tokens.clamp(max=vocab - 1)[:, None])[:, 0], tol)
+    _near(lse, torch.logsumexp(z.double().cpu() / 0.9, 1), tol)
+    w_ent = -torch.where(lp > -math.inf, lp.exp() * torch.where(lp > -math.inf, lp, 0.0), 0.0).sum(1)
+    _near(ent, w_ent, (2 * tol + 2.0 ** -18) * (1 + w_ent))
+    again = _run_logp(glr, z, tokens.cuda(), 0.9, topk)
+    assert all(torch.equal(a, b) for a, b in zip((logp, lse, ent, top, ids), again))
 
 
 @pytest.mark.parametrize("vocab", [50, 5000, 70000])
