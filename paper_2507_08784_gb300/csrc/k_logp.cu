@@ -638,7 +638,12 @@ cudaError_t token_logp(const TokenLogp& a, int dtype, cudaStream_t st) {
     // CTAs a row: a cluster where the rows leave SMs idle, each CTA with 4096 logits at least
     int parts = 1;
     while (parts < 8 && a.rows * parts * 2 <= 2 * 152 && a.vocab >= parts * 2 * 4096) parts *= 2;
-    const int threads = a.vocab <= 2048 ? 64 : a.vocab <= 4096 ? 128 : 256;
+    // Threads a CTA: smaller ones are more in turn at a row's end (4096 x 131071 bf16, 64 alternatives: 263 us with 128, 279 with 256,
+    // 352 with 64; 16384 x 5003 without alternatives 66 with 128, 51 with 64), but bound fewer alternatives, and share fewer keys'
+    // ordering in a cluster (one row of 32768, 64 alternatives: 15 with 128, 11 with 256).
+    const auto listed = [&](int threads) { return threads * (dtype == GLR_BF16 ? kAhead<__nv_bfloat16> : kAhead<float>) * 3 / 8; };
+    int threads = a.vocab <= (a.topk ? 2048 : 8192) && a.topk <= listed(64) ? 64 : 128;
+    if (threads == 128 && (a.topk > std::min(128, listed(128)) || (parts > 1 && a.topk > 32))) threads = 256;
     cudaLaunchAttribute attr[2]{};
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
