@@ -364,8 +364,9 @@ int glr_select_noalloc(int32_t m_prime, int32_t n_prime, int32_t r, const float*
 /* ---- operators around the step ----------------------------------------------------------- */
 
 /* What makes the gradients that a step takes: the layers' products with their epilogues and
- * gradients, and the losses on the logits of the last layer, each with the gradient that the
- * backward pass starts from.  They hold no state: the caller owns every buffer, all work is enqueued
+ * gradients, embeddings and norms with theirs, activations kept in 8 bits between the passes, and the
+ * losses and log-probabilities of the logits of the last layer, with the gradient that the backward
+ * pass starts from.  They hold no state: the caller owns every buffer, all work is enqueued
  * on `stream` without synchronisation, nothing is allocated, and a call may be captured into a
  * graph.  Common to all of them:
  *   - The buffers lie on the current device, and `stream` is one of its streams.

@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_apart_kernel(const __gr
 
 // ---- the tokens in order ---------------------------------------------------------------------------------------
 constexpr int kChunk = 4096, kSortThreads = 512, kSortWarps = kSortThreads / 32, kMine = kChunk / kSortThreads;
-constexpr int kDigit = 8, kDigits = 1 << kDigit;
+constexpr int kDigit = 9, kDigits = 1 << kDigit;        // two passes for up to 2^18 - 1 tokens
 
 // A chunk's sorted tokens, the rows (of its node) that they come from, and where each tile's begin.
 struct Sorted {

@@ -296,6 +296,8 @@ __device__ __forceinline__ void epilogue8(const TcArgs& a, int node, int64_t i, 
         if (p.pre || p.pre_codes) {
             if (p.pre_codes) {
                 if (pre && n == 8 && (a.wide & 8)) rows::code_values(make_uint2(pre->x, pre->y), pre->z, x);
+                else if (!COLUMN && n == 8 && (a.wide & 8))
+                    rows::code_values(*reinterpret_cast<const uint2*>(p.pre_codes + i * p.ldpc + j), p.pre_scales[i * p.ldps + j / rows::kBlock], x);
                 else codes8<COLUMN>(p, i, j, n, x);
             } else if (pre && n == 8) widen8(*pre, x);
             else get(p.pre, p.ldpre, 8, x);
