@@ -162,14 +162,15 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(Index tokens, int64_
 }
 
 // ---- the sums ----------------------------------------------------------------------------------------------------
-constexpr int kGradWarps = 8, kGradThreads = kGradWarps * 32, kSlice = 256;          // columns at a time
+constexpr int kGradWarps = 8, kGradThreads = kGradWarps * 32;
 constexpr int kMany = 64;                            // occurrences from which on all warps share a row
 constexpr int kScan = 1024;                          // a node's rows up to which its tokens are looked through
 
-// The lane's eight columns of a slice of a row, as they lie in memory: neighbouring ones, or 32 apart where rows are not on 16
+// L lanes take a row of dY, 8 L columns of it; with L = 8 a warp adds up four rows at once.
+// The lane's eight columns of a slice of a row, as they lie in memory: neighbouring ones, or L apart where rows are not on 16
 // bytes (0 beyond the last one).
-template <class T, bool WIDE> struct Columns;
-template <> struct Columns<__nv_bfloat16, true> {
+template <class T, bool WIDE, int L> struct Columns;
+template <int L> struct Columns<__nv_bfloat16, true, L> {
     static constexpr int kAhead = 8;                 // rows loaded before the first one is added
     uint4 u;
     __device__ __forceinline__ void load(const __nv_bfloat16* row, int lane, int left) {
@@ -182,7 +183,7 @@ template <> struct Columns<__nv_bfloat16, true> {
         for (int e = 0; e < 8; ++e) sum[e] += v[e];
     }
 };
-template <> struct Columns<float, true> {
+template <int L> struct Columns<float, true, L> {
     static constexpr int kAhead = 4;
     float4 a, b;
     __device__ __forceinline__ void load(const float* row, int lane, int left) {
@@ -195,19 +196,19 @@ template <> struct Columns<float, true> {
         sum[0] += a.x; sum[1] += a.y; sum[2] += a.z; sum[3] += a.w; sum[4] += b.x; sum[5] += b.y; sum[6] += b.z; sum[7] += b.w;
     }
 };
-template <class T> struct Columns<T, false> {
+template <class T, int L> struct Columns<T, false, L> {
     static constexpr int kAhead = 2;
     T x[8];
     __device__ __forceinline__ void load(const T* row, int lane, int left) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = e * 32 + lane < left ? row[e * 32 + lane] : T(0.f);
+        for (int e = 0; e < 8; ++e) x[e] = e * L + lane < left ? row[e * L + lane] : T(0.f);
     }
     __device__ __forceinline__ void add(float (&sum)[8]) const {
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum[e] += to_f(x[e]);
     }
 };
-template <class G, bool WIDE>
+template <class G, bool WIDE, int L>
 __device__ __forceinline__ void finish_row(G* to, int lane, int left, bool accumulate, const float (&sum)[8], float scale) {
     float v[8];
     if (WIDE) {
@@ -218,8 +219,8 @@ __device__ __forceinline__ void finish_row(G* to, int lane, int left, bool accum
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            if (e * 32 + lane < left) {
-                G* p = to + e * 32 + lane;
+            if (e * L + lane < left) {
+                G* p = to + e * L + lane;
                 put(p, accumulate ? fmaf(sum[e], scale, to_f(*p)) : sum[e] * scale);
             }
     }
@@ -231,37 +232,49 @@ __device__ __forceinline__ int first_at(const int32_t* token, int s, int e, int 
     return s;
 }
 
-// Adds up the rows `row[0 .. n)` of dY: every parts-th group of 32 of them, in their order.
-template <class T, bool WIDE>
+// Adds up the rows `row[0 .. n)` of dY: every parts-th group of 32 of them, in their order; the lanes have a sum for each of
+// their 32 / L groups.
+template <class T, bool WIDE, int L>
 __device__ __forceinline__ void add_rows(const T* dy, int64_t lddy, const int32_t* row, int n, int part, int parts, int left, float (&sum)[8]) {
-    using C = Columns<T, WIDE>;
-    const int lane = threadIdx.x & 31;
+    using C = Columns<T, WIDE, L>;
+    constexpr int kAtOnce = 32 / L;
+    const int lane = threadIdx.x & 31, own = lane & (L - 1), group = lane / L;
     for (int q = part * 32; q < n; q += parts * 32) {
         const int mine = q + lane < n ? row[q + lane] : 0, m = min(32, n - q);
         int u = 0;
-        for (; u + C::kAhead <= m; u += C::kAhead) {
+        for (; u + C::kAhead * kAtOnce <= m; u += C::kAhead * kAtOnce) {
             C c[C::kAhead];
 #pragma unroll
-            for (int k = 0; k < C::kAhead; ++k) c[k].load(dy + __shfl_sync(0xffffffffu, mine, u + k) * lddy, lane, left);
+            for (int k = 0; k < C::kAhead; ++k) c[k].load(dy + __shfl_sync(0xffffffffu, mine, u + k * kAtOnce + group) * lddy, own, left);
 #pragma unroll
             for (int k = 0; k < C::kAhead; ++k) c[k].add(sum);
         }
-        for (; u < m; u += 2) {
+        for (; u < m; u += 2 * kAtOnce) {
             C c[2];
-            c[0].load(dy + __shfl_sync(0xffffffffu, mine, u) * lddy, lane, left);
-            c[1].load(dy + __shfl_sync(0xffffffffu, mine, min(u + 1, m - 1)) * lddy, lane, left);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int x = u + k * kAtOnce + group;
+                c[k].load(dy + __shfl_sync(0xffffffffu, mine, min(x, 31)) * lddy, own, x < m ? left : 0);
+            }
             c[0].add(sum);
-            if (u + 1 < m) c[1].add(sum);
+            c[1].add(sum);
         }
     }
 }
 
 // A tile's rows, one warp each, then those that all warps share.  of(r) is how many rows of dY the tile's row r has;
 // add(r, part, parts, sum) adds up every parts-th group of them.
-template <class G, bool WIDE, class Of, class Add>
-__device__ __forceinline__ void sum_rows(const EmbeddingGrad& a, G* de, int rows, int left, float (*part)[kSlice], uint16_t* many, int* some,
+template <class G, bool WIDE, int L, class Of, class Add>
+__device__ __forceinline__ void sum_rows(const EmbeddingGrad& a, G* de, int rows, int left, float (*part)[8 * L], uint16_t* many, int* some,
                                          const Of& of, const Add& add) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const auto total = [&](int r, int from, int parts, float (&sum)[8]) {
+        add(r, from, parts, sum);
+#pragma unroll
+        for (int o = L; o < 32; o *= 2)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], o);
+    };
     for (int r = warp; r < rows; r += kGradWarps) {
         const int n = of(r);
         if (n == 0) {
@@ -269,7 +282,7 @@ __device__ __forceinline__ void sum_rows(const EmbeddingGrad& a, G* de, int rows
             if (WIDE) {
                 constexpr int kPer = 16 / sizeof(G);
 #pragma unroll
-                for (int j = lane * kPer; j < kSlice; j += 32 * kPer)
+                for (int j = lane * kPer; j < 8 * L; j += 32 * kPer)
                     if (j < left) *reinterpret_cast<uint4*>(de + r * a.d + j) = make_uint4(0, 0, 0, 0);
             } else {
                 for (int j = lane; j < left; j += 32) put(de + r * a.d + j, 0.f);
@@ -278,33 +291,35 @@ __device__ __forceinline__ void sum_rows(const EmbeddingGrad& a, G* de, int rows
             if (lane == 0) many[atomicAdd(some, 1)] = static_cast<uint16_t>(r);
         } else {
             float sum[8] = {};
-            add(r, 0, 1, sum);
-            finish_row<G, WIDE>(de + r * a.d, lane, left, a.accumulate, sum, a.scale);
+            total(r, 0, 1, sum);
+            if (lane < L) finish_row<G, WIDE, L>(de + r * a.d, lane, left, a.accumulate, sum, a.scale);
         }
     }
     __syncthreads();
     for (int q = 0; q < *some; ++q) {
         const int r = many[q];
         float sum[8] = {};
-        add(r, warp, kGradWarps, sum);
+        total(r, warp, kGradWarps, sum);
+        if (lane < L) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) part[warp][e * 32 + lane] = sum[e];
+            for (int e = 0; e < 8; ++e) part[warp][e * L + lane] = sum[e];
+        }
         __syncthreads();
-        if (warp == 0) {
+        if (warp == 0 && lane < L) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                for (int w = 1; w < kGradWarps; ++w) sum[e] += part[w][e * 32 + lane];
-            finish_row<G, WIDE>(de + r * a.d, lane, left, a.accumulate, sum, a.scale);
+                for (int w = 1; w < kGradWarps; ++w) sum[e] += part[w][e * L + lane];
+            finish_row<G, WIDE, L>(de + r * a.d, lane, left, a.accumulate, sum, a.scale);
         }
         __syncthreads();
     }
 }
 
 // Up to kScan rows a node: the CTA looks through the node's tokens.
-template <class T, class G, bool WIDE, int R>
+template <class T, class G, bool WIDE, int R, int L>
 __global__ void __launch_bounds__(kGradThreads, 4) scan_grad_kernel(const __grid_constant__ EmbeddingGrad a) {
     chain_begin();
-    __shared__ float part[kGradWarps][kSlice];
+    __shared__ float part[kGradWarps][8 * L];
     __shared__ int32_t list[kScan];                  // the tile's rows of dY in order of (token, row)
     __shared__ int off[R + 1];                       // where each of its tokens begins
     __shared__ uint16_t count[kGradWarps][R];
@@ -312,8 +327,8 @@ __global__ void __launch_bounds__(kGradThreads, 4) scan_grad_kernel(const __grid
     __shared__ uint16_t many[R];
     __shared__ int some;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t node = blockIdx.z, v0 = static_cast<int64_t>(blockIdx.x) * R, col = static_cast<int64_t>(blockIdx.y) * kSlice;
-    const int rows = static_cast<int>(min(static_cast<int64_t>(R), a.vocab - v0)), left = static_cast<int>(min(static_cast<int64_t>(kSlice), a.d - col));
+    const int64_t node = blockIdx.z, v0 = static_cast<int64_t>(blockIdx.x) * R, col = static_cast<int64_t>(blockIdx.y) * (8 * L);
+    const int rows = static_cast<int>(min(static_cast<int64_t>(R), a.vocab - v0)), left = static_cast<int>(min(static_cast<int64_t>(8 * L), a.d - col));
     // each warp takes a stretch of rows: their tokens' places in the tile (R: none), then the ranks among the warp's too
     constexpr int kBatches = kScan / kGradThreads;
     const int n = static_cast<int>(a.rows), stretch = (n + kGradThreads - 1) / kGradThreads;
@@ -362,24 +377,24 @@ __global__ void __launch_bounds__(kGradThreads, 4) scan_grad_kernel(const __grid
     }
     __syncthreads();
     const T* dy = static_cast<const T*>(a.dY) + node * a.rows * a.lddy + col;
-    sum_rows<G, WIDE>(a, static_cast<G*>(a.dE[node]) + v0 * a.d + col, rows, left, part, many, &some,
+    sum_rows<G, WIDE, L>(a, static_cast<G*>(a.dE[node]) + v0 * a.d + col, rows, left, part, many, &some,
                       [&](int r) { return off[r + 1] - off[r]; },
-                      [&](int r, int from, int parts, float (&s)[8]) { add_rows<T, WIDE>(dy, a.lddy, list + off[r], off[r + 1] - off[r], from, parts, left, s); });
+                      [&](int r, int from, int parts, float (&s)[8]) { add_rows<T, WIDE, L>(dy, a.lddy, list + off[r], off[r + 1] - off[r], from, parts, left, s); });
 }
 
 // Beyond: the tile's part of every sorted chunk, with a table of where each row begins in each chunk (TABLE), or, of more
 // chunks than it has room for, looked for row by row.
 constexpr int kTable = 2080;
-template <class T, class G, bool WIDE, int R, bool TABLE>
+template <class T, class G, bool WIDE, int R, int L, bool TABLE>
 __global__ void __launch_bounds__(kGradThreads, 4) sorted_grad_kernel(const __grid_constant__ EmbeddingGrad a, const Sorted s) {
     chain_begin();
-    __shared__ float part[kGradWarps][kSlice];
+    __shared__ float part[kGradWarps][8 * L];
     __shared__ int32_t table[TABLE ? kTable : 1];
     __shared__ uint16_t many[R];
     __shared__ int some;
     const int lane = threadIdx.x & 31;
-    const int64_t tile = blockIdx.x, node = blockIdx.z, v0 = tile * R, col = static_cast<int64_t>(blockIdx.y) * kSlice;
-    const int rows = static_cast<int>(min(static_cast<int64_t>(R), a.vocab - v0)), left = static_cast<int>(min(static_cast<int64_t>(kSlice), a.d - col));
+    const int64_t tile = blockIdx.x, node = blockIdx.z, v0 = tile * R, col = static_cast<int64_t>(blockIdx.y) * (8 * L);
+    const int rows = static_cast<int>(min(static_cast<int64_t>(R), a.vocab - v0)), left = static_cast<int>(min(static_cast<int64_t>(8 * L), a.d - col));
     const auto part_of = [&](int64_t chunk) {
         const int32_t* start = s.start + s.at(node, chunk) * (s.tiles + 1) + tile;
         return make_int2(start[0], start[1]);
@@ -401,7 +416,7 @@ __global__ void __launch_bounds__(kGradThreads, 4) sorted_grad_kernel(const __gr
         const int32_t* token = s.token + s.at(node, c0 + lane) * kChunk;
         return make_int2(first_at(token, p.x, p.y, static_cast<int>(v0) + r), first_at(token, p.x, p.y, static_cast<int>(v0) + r + 1));
     };
-    sum_rows<G, WIDE>(a, static_cast<G*>(a.dE[node]) + v0 * a.d + col, rows, left, part, many, &some,
+    sum_rows<G, WIDE, L>(a, static_cast<G*>(a.dE[node]) + v0 * a.d + col, rows, left, part, many, &some,
         [&](int r) {
             int n = 0;
             for (int64_t c0 = 0; c0 < s.chunks; c0 += 32) { const int2 m = mine(c0, r); n += m.y - m.x; }
@@ -413,7 +428,7 @@ __global__ void __launch_bounds__(kGradThreads, 4) sorted_grad_kernel(const __gr
                 for (uint32_t some_of = __ballot_sync(0xffffffffu, m.x < m.y); some_of; some_of &= some_of - 1) {
                     const int c = __ffs(some_of) - 1;
                     const int begin = __shfl_sync(0xffffffffu, m.x, c), end = __shfl_sync(0xffffffffu, m.y, c);
-                    add_rows<T, WIDE>(dy, a.lddy, s.row + s.at(node, c0 + c) * kChunk + begin, end - begin, from, parts, left, sum);
+                    add_rows<T, WIDE, L>(dy, a.lddy, s.row + s.at(node, c0 + c) * kChunk + begin, end - begin, from, parts, left, sum);
                 }
             }
         });
@@ -421,17 +436,23 @@ __global__ void __launch_bounds__(kGradThreads, 4) sorted_grad_kernel(const __gr
 
 bool on16(const void* p, int64_t ld_bytes) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld_bytes % 16 == 0; }
 
-template <class T, class G, bool WIDE, int R>
+template <class T, class G, bool WIDE, int R, int L>
 cudaError_t launch_tiles(const EmbeddingGrad& a, const Sorted& s, cudaStream_t st) {
-    const dim3 grid(static_cast<unsigned>(s.tiles), static_cast<unsigned>((a.d + kSlice - 1) / kSlice), static_cast<unsigned>(a.nodes));
-    if (a.rows <= kScan) return launch_chain(scan_grad_kernel<T, G, WIDE, R>, grid, kGradThreads, 0, st, a);
-    return s.chunks * (R + 1) <= kTable ? launch_chain(sorted_grad_kernel<T, G, WIDE, R, true>, grid, kGradThreads, 0, st, a, s)
-                                        : launch_chain(sorted_grad_kernel<T, G, WIDE, R, false>, grid, kGradThreads, 0, st, a, s);
+    const dim3 grid(static_cast<unsigned>(s.tiles), static_cast<unsigned>((a.d + 8 * L - 1) / (8 * L)), static_cast<unsigned>(a.nodes));
+    if (a.rows <= kScan) return launch_chain(scan_grad_kernel<T, G, WIDE, R, L>, grid, kGradThreads, 0, st, a);
+    return s.chunks * (R + 1) <= kTable ? launch_chain(sorted_grad_kernel<T, G, WIDE, R, L, true>, grid, kGradThreads, 0, st, a, s)
+                                        : launch_chain(sorted_grad_kernel<T, G, WIDE, R, L, false>, grid, kGradThreads, 0, st, a, s);
+}
+template <class T, class G, bool WIDE>
+cudaError_t launch_wide(const EmbeddingGrad& a, const Sorted& s, cudaStream_t st) {
+    if (s.tile_rows == kManyRows) return launch_tiles<T, G, WIDE, kManyRows, 32>(a, s, st);
+    // narrow slices where wide ones would leave SMs idle: a token of many rows then keeps fewer columns waiting
+    return s.tiles * a.nodes * ((a.d + 255) / 256) < 152 * 4 ? launch_tiles<T, G, WIDE, kFewRows, 8>(a, s, st)
+                                                             : launch_tiles<T, G, WIDE, kFewRows, 32>(a, s, st);
 }
 template <class T, class G>
 cudaError_t launch_grad(const EmbeddingGrad& a, const Sorted& s, bool wide, cudaStream_t st) {
-    if (s.tile_rows == kFewRows) return wide ? launch_tiles<T, G, true, kFewRows>(a, s, st) : launch_tiles<T, G, false, kFewRows>(a, s, st);
-    return wide ? launch_tiles<T, G, true, kManyRows>(a, s, st) : launch_tiles<T, G, false, kManyRows>(a, s, st);
+    return wide ? launch_wide<T, G, true>(a, s, st) : launch_wide<T, G, false>(a, s, st);
 }
 
 }  // namespace
