@@ -1,5 +1,7 @@
-// Activations in 8 bits with a scale for every 32 columns, and back (the format is in glr_rows.cuh): bound by HBM.  A row
-// has 4 to 256 threads (a power of two) with eight neighbouring elements each, so that four lanes hold a block.
+// Activations in 8 bits with a scale for every 32 columns, and back (the format is in glr_rows.cuh).  Four lanes hold a block,
+// eight neighbouring columns each; a task of 32 threads is 512 columns of a row, two vectors a thread on their way at once.
+// Bound by HBM (8192 x 5632 bf16 packed 26 us, unpacked 22, floor 21 each), unpacking with SiLU by its exponentials and
+// reciprocals (31).
 #include <algorithm>
 
 #include "glr_linear.cuh"

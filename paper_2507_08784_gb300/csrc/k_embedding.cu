@@ -7,7 +7,9 @@
 // (token, row); beyond, chunks of kChunk rows have been sorted by their tokens, stably, by a kernel before, with the place where each
 // tile begins.  Both order by ranks among equal digits: warps take consecutive stretches, lanes with the same digit are matched.
 // A token outside the vocabulary is nobody's.
-// Bound by HBM: the gradient of the whole vocabulary is written for every node.
+// Bound by HBM: the gradient of the whole vocabulary is written for every node (8 nodes x 1024 rows, 32768 x 2048 bf16, 1.1 GB:
+// 179 us, 6.2 TB/s; lookups of 16384 rows of 4096 bf16 34 us).  Tiles of 64 rows instead of 256 took 256 us: what a CTA does before
+// it writes costs as much as its writes.  Eight rows of dY are loaded before the first is added (one at a time: 200 us).
 #include <algorithm>
 
 #include "glr_rows.cuh"
