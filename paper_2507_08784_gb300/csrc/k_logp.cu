@@ -373,6 +373,20 @@ __global__ void __launch_bounds__(NT, 1280 / NT) token_logp_kernel(const __grid_
     int round = 0, due = 0, entries = 0;
     const uint32_t before = (1u << lane) - 1;
     uint32_t* mine_list = list + warp * kWarpList;
+    // the warp's entries that a new bound leaves move up
+    const auto thin_out = [&](float b) {
+        const uint32_t least = order_of(b) & 0xffff0000u;
+        int kept = 0;
+        __syncwarp();
+        for (int q = 0; q < entries; q += 32) {
+            const uint32_t entry = q + lane < entries ? mine_list[q + lane] : 0;
+            const uint32_t some = __ballot_sync(0xffffffffu, q + lane < entries && entry_order(entry) >= least);
+            if (some >> lane & 1) mine_list[kept + __popc(some & before)] = entry;
+            kept += __popc(some);
+            __syncwarp();
+        }
+        entries = kept;
+    };
     for (int q0 = row.begin; q0 < row.end; q0 += A * NT, ++round) {
         Eight<T> v[A];
         float top[A];
@@ -426,19 +440,7 @@ __global__ void __launch_bounds__(NT, 1280 / NT) token_logp_kernel(const __grid_
 #pragma unroll
                 for (int o = 1; o < W; o *= 2) b = fminf(b, __shfl_xor_sync(0xffffffffu, b, o));
                 bound = fmaxf(bound, b);
-                if (entries > kWarpList / 4 && entries <= kWarpList) {       // those that the new bound leaves move up
-                    const uint32_t least_order = order_of(bound) & 0xffff0000u;
-                    int kept = 0;
-                    __syncwarp();
-                    for (int q = 0; q < entries; q += 32) {
-                        const uint32_t entry = q + lane < entries ? mine_list[q + lane] : 0;
-                        const uint32_t some = __ballot_sync(0xffffffffu, q + lane < entries && entry_order(entry) >= least_order);
-                        if (some >> lane & 1) mine_list[kept + __popc(some & before)] = entry;
-                        kept += __popc(some);
-                        __syncwarp();
-                    }
-                    entries = kept;
-                }
+                if (entries > kWarpList / 4 && entries <= kWarpList) thin_out(bound);
             }
             if (__any_sync(0xffffffffu, m_round >= bound)) {
                 const uint32_t place = static_cast<uint32_t>(round * A * 32 + lane);
@@ -475,10 +477,9 @@ __global__ void __launch_bounds__(NT, 1280 / NT) token_logp_kernel(const __grid_
         for (int w = 1; w < W; ++w) b = fminf(b, bounds[w]);
         const bool ordinary = t.s < kInf;            // no NaN and no infinity in this part
         if (listed && over == 0 && ordinary) {
-            const uint32_t least = order_of(b) & 0xffff0000u;
+            thin_out(b);                             // first, so that most are read again at once
             for (int q = lane; q < entries; q += 32) {
                 const uint32_t entry = mine_list[q];
-                if (entry_order(entry) < least) continue;        // of a maximum below the last bound
                 const int at = row.begin + static_cast<int>(entry >> 5 & 0x7ffu) * NT + warp * 32 + static_cast<int>(entry & 31);
                 Eight<T> v;
                 row.load(at, v);
