@@ -285,8 +285,8 @@ __device__ __forceinline__ float lanes_largest(float v, int j) {
     }
     return most == 0 ? kLowest : fmaxf(logit_of(most), kLowest);
 }
-// A value that at least j of the lanes' n values each reach, j <= 32 n: sixteen bisections between the least and the largest of
-// them, as integers of the same order (1 is that of no logit, and below all of them).
+// A value that at least j of the lanes' n values each reach, j <= 32 n: at most sixteen bisections between the least and the
+// largest of them, as integers of the same order (1 is that of no logit, and below all of them).
 template <int N>
 __device__ __noinline__ float lanes_many(const float (&v)[N], int j) {
     uint32_t o[N], lo = 0xffffffffu, hi = 0;
@@ -300,6 +300,7 @@ __device__ __noinline__ float lanes_many(const float (&v)[N], int j) {
 #pragma unroll
         for (int q = 0; q < N; ++q) n += __popc(__ballot_sync(0xffffffffu, o[q] >= mid));
         if (n >= j) lo = mid; else hi = mid;
+        if (n == j) break;                           // (8192 x 8192 bf16, 128 alternatives 146 us without, 142 so)
     }
     return fmaxf(logit_of(lo), kLowest);
 }
@@ -455,10 +456,13 @@ __global__ void __launch_bounds__(NT, 1280 / NT) token_logp_kernel(const __grid_
             }
         }
     }
-    if (TOP) {
+    // a part of one round: its first bound is the last one (16384 x 2048 bf16, 64 alternatives 126 us with both, 103 with one)
+    const bool current = listed && round == 1;
+    if (TOP && !current) {
         const float least = few ? lanes_largest(t.m, mine) : mine <= 32 * A ? lanes_many(most, mine) : kLowest;
-        if (lane == 0) { bounds[warp] = least; if (entries > kWarpList) atomicAdd(&over, 1); }
+        if (lane == 0) bounds[warp] = least;
     }
+    if (TOP && lane == 0 && entries > kWarpList) atomicAdd(&over, 1);
     // the CTA's statistics, then the row's
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) {
@@ -477,7 +481,7 @@ __global__ void __launch_bounds__(NT, 1280 / NT) token_logp_kernel(const __grid_
         for (int w = 1; w < W; ++w) b = fminf(b, bounds[w]);
         const bool ordinary = t.s < kInf;            // no NaN and no infinity in this part
         if (listed && over == 0 && ordinary) {
-            thin_out(b);                             // first, so that most are read again at once
+            if (!current) thin_out(b);               // first, so that most are read again at once
             for (int q = lane; q < entries; q += 32) {
                 const uint32_t entry = mine_list[q];
                 const int at = row.begin + static_cast<int>(entry >> 5 & 0x7ffu) * NT + warp * 32 + static_cast<int>(entry & 31);
