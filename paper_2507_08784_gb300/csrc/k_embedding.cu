@@ -169,10 +169,11 @@ constexpr int kMany = 64;                            // occurrences from which o
 constexpr int kScan = 1024;                          // a node's rows up to which its tokens are looked through
 
 // L lanes take a row of dY, 8 L columns of it; with L = 8 a warp adds up four rows at once.
-// The lane's eight columns of a slice of a row, as they lie in memory: neighbouring ones, or L apart where rows are not on 16
-// bytes (0 beyond the last one).
-template <class T, bool WIDE, int L> struct Columns;
-template <int L> struct Columns<__nv_bfloat16, true, L> {
+// The lane's eight columns of a slice of a row, as they lie in memory (0 beyond the last one): neighbouring ones (WIDE 1), also
+// where dE's rows are on 16 bytes and only dY's are not (2: 8 x 1024 rows with a stride of 2049, 32768 x 2048 bf16 189 us; as 0
+// 251), else L apart (0).  Of rows off 16 bytes four are loaded at once (two: 4 x 6639 rows into 3062 x 989 bf16 100 us, now 79).
+template <class T, int WIDE, int L> struct Columns;
+template <int L> struct Columns<__nv_bfloat16, 1, L> {
     static constexpr int kAhead = 8;                 // rows loaded before the first one is added
     uint4 u;
     __device__ __forceinline__ void load(const __nv_bfloat16* row, int lane, int left) {
@@ -185,7 +186,7 @@ template <int L> struct Columns<__nv_bfloat16, true, L> {
         for (int e = 0; e < 8; ++e) sum[e] += v[e];
     }
 };
-template <int L> struct Columns<float, true, L> {
+template <int L> struct Columns<float, 1, L> {
     static constexpr int kAhead = 4;
     float4 a, b;
     __device__ __forceinline__ void load(const float* row, int lane, int left) {
@@ -198,8 +199,8 @@ template <int L> struct Columns<float, true, L> {
         sum[0] += a.x; sum[1] += a.y; sum[2] += a.z; sum[3] += a.w; sum[4] += b.x; sum[5] += b.y; sum[6] += b.z; sum[7] += b.w;
     }
 };
-template <class T, int L> struct Columns<T, false, L> {
-    static constexpr int kAhead = 2;
+template <class T, int L> struct Columns<T, 0, L> {
+    static constexpr int kAhead = 4;
     T x[8];
     __device__ __forceinline__ void load(const T* row, int lane, int left) {
 #pragma unroll
@@ -210,7 +211,19 @@ template <class T, int L> struct Columns<T, false, L> {
         for (int e = 0; e < 8; ++e) sum[e] += to_f(x[e]);
     }
 };
-template <class G, bool WIDE, int L>
+template <class T, int L> struct Columns<T, 2, L> {
+    static constexpr int kAhead = 4;
+    T x[8];
+    __device__ __forceinline__ void load(const T* row, int lane, int left) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = lane * 8 < left ? row[lane * 8 + e] : T(0.f);
+    }
+    __device__ __forceinline__ void add(float (&sum)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += to_f(x[e]);
+    }
+};
+template <class G, int WIDE, int L>
 __device__ __forceinline__ void finish_row(G* to, int lane, int left, bool accumulate, const float (&sum)[8], float scale) {
     float v[8];
     if (WIDE) {
@@ -236,7 +249,7 @@ __device__ __forceinline__ int first_at(const int32_t* token, int s, int e, int 
 
 // Adds up the rows `row[0 .. n)` of dY: every parts-th group of 32 of them, in their order; the lanes have a sum for each of
 // their 32 / L groups.
-template <class T, bool WIDE, int L>
+template <class T, int WIDE, int L>
 __device__ __forceinline__ void add_rows(const T* dy, int64_t lddy, const int32_t* row, int n, int part, int parts, int left, float (&sum)[8]) {
     using C = Columns<T, WIDE, L>;
     constexpr int kAtOnce = 32 / L;
@@ -266,7 +279,7 @@ __device__ __forceinline__ void add_rows(const T* dy, int64_t lddy, const int32_
 
 // A tile's rows, one warp each, then those that all warps share.  of(r) is how many rows of dY the tile's row r has;
 // add(r, part, parts, sum) adds up every parts-th group of them.
-template <class G, bool WIDE, int L, class Of, class Add>
+template <class G, int WIDE, int L, class Of, class Add>
 __device__ __forceinline__ void sum_rows(const EmbeddingGrad& a, G* de, int rows, int left, float (*part)[8 * L], uint16_t* many, int* some,
                                          const Of& of, const Add& add) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -318,7 +331,7 @@ __device__ __forceinline__ void sum_rows(const EmbeddingGrad& a, G* de, int rows
 }
 
 // Up to kScan rows a node: the CTA looks through the node's tokens.
-template <class T, class G, bool WIDE, int R, int L>
+template <class T, class G, int WIDE, int R, int L>
 __global__ void __launch_bounds__(kGradThreads, 4) scan_grad_kernel(const __grid_constant__ EmbeddingGrad a) {
     chain_begin();
     __shared__ float part[kGradWarps][8 * L];
@@ -387,7 +400,7 @@ __global__ void __launch_bounds__(kGradThreads, 4) scan_grad_kernel(const __grid
 // Beyond: the tile's part of every sorted chunk, with a table of where each row begins in each chunk (TABLE), or, of more
 // chunks than it has room for, looked for row by row.
 constexpr int kTable = 2080;
-template <class T, class G, bool WIDE, int R, int L, bool TABLE>
+template <class T, class G, int WIDE, int R, int L, bool TABLE>
 __global__ void __launch_bounds__(kGradThreads, 4) sorted_grad_kernel(const __grid_constant__ EmbeddingGrad a, const Sorted s) {
     chain_begin();
     __shared__ float part[kGradWarps][8 * L];
@@ -438,14 +451,14 @@ __global__ void __launch_bounds__(kGradThreads, 4) sorted_grad_kernel(const __gr
 
 bool on16(const void* p, int64_t ld_bytes) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld_bytes % 16 == 0; }
 
-template <class T, class G, bool WIDE, int R, int L>
+template <class T, class G, int WIDE, int R, int L>
 cudaError_t launch_tiles(const EmbeddingGrad& a, const Sorted& s, cudaStream_t st) {
     const dim3 grid(static_cast<unsigned>(s.tiles), static_cast<unsigned>((a.d + 8 * L - 1) / (8 * L)), static_cast<unsigned>(a.nodes));
     if (a.rows <= kScan) return launch_chain(scan_grad_kernel<T, G, WIDE, R, L>, grid, kGradThreads, 0, st, a);
     return s.chunks * (R + 1) <= kTable ? launch_chain(sorted_grad_kernel<T, G, WIDE, R, L, true>, grid, kGradThreads, 0, st, a, s)
                                         : launch_chain(sorted_grad_kernel<T, G, WIDE, R, L, false>, grid, kGradThreads, 0, st, a, s);
 }
-template <class T, class G, bool WIDE>
+template <class T, class G, int WIDE>
 cudaError_t launch_wide(const EmbeddingGrad& a, const Sorted& s, cudaStream_t st) {
     if (s.tile_rows == kManyRows) return launch_tiles<T, G, WIDE, kManyRows, 32>(a, s, st);
     // narrow slices where wide ones would leave SMs idle: a token of many rows then keeps fewer columns waiting
@@ -453,8 +466,8 @@ cudaError_t launch_wide(const EmbeddingGrad& a, const Sorted& s, cudaStream_t st
                                                              : launch_tiles<T, G, WIDE, kFewRows, 32>(a, s, st);
 }
 template <class T, class G>
-cudaError_t launch_grad(const EmbeddingGrad& a, const Sorted& s, bool wide, cudaStream_t st) {
-    return wide ? launch_wide<T, G, true>(a, s, st) : launch_wide<T, G, false>(a, s, st);
+cudaError_t launch_grad(const EmbeddingGrad& a, const Sorted& s, int wide, cudaStream_t st) {
+    return wide == 0 ? launch_wide<T, G, 0>(a, s, st) : wide == 1 ? launch_wide<T, G, 1>(a, s, st) : launch_wide<T, G, 2>(a, s, st);
 }
 
 }  // namespace
@@ -498,8 +511,9 @@ cudaError_t embedding_grad(const EmbeddingGrad& a, int dtype, int grad_dtype, cu
         return cudaSuccess;
     }
     const int64_t es = dtype == GLR_BF16 ? 2 : 4, gs = grad_dtype == GLR_BF16 ? 2 : 4;
-    bool wide = on16(a.dY, a.nodes * a.rows > 1 ? a.lddy * es : 0) && a.d % 8 == 0;
-    for (int64_t i = 0; i < a.nodes; ++i) wide = wide && on16(a.dE[i], a.d * gs);
+    bool whole = a.d % 8 == 0;
+    for (int64_t i = 0; i < a.nodes; ++i) whole = whole && on16(a.dE[i], a.d * gs);
+    const int wide = !whole ? 0 : on16(a.dY, a.nodes * a.rows > 1 ? a.lddy * es : 0) ? 1 : 2;
     if (dtype == GLR_BF16)
         return grad_dtype == GLR_BF16 ? launch_grad<__nv_bfloat16, __nv_bfloat16>(a, s, wide, st) : launch_grad<__nv_bfloat16, float>(a, s, wide, st);
     return grad_dtype == GLR_BF16 ? launch_grad<float, __nv_bfloat16>(a, s, wide, st) : launch_grad<float, float>(a, s, wide, st);
