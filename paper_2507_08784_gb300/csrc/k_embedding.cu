@@ -170,7 +170,7 @@ constexpr int kScan = 1024;                          // a node's rows up to whic
 
 // L lanes take a row of dY, 8 L columns of it; with L = 8 a warp adds up four rows at once.
 // The lane's eight columns of a slice of a row, as they lie in memory (0 beyond the last one): neighbouring ones (WIDE 1), also
-// where dE's rows are on 16 bytes and only dY's are not (2: 8 x 1024 rows with a stride of 2049, 32768 x 2048 bf16 189 us; as 0
+// where dE's rows are on 16 bytes and only dY's are not (2: 8 x 1024 rows with a stride of 2049, 32768 x 2048 bf16 188 us; as 0
 // 251), else L apart (0).  Of rows off 16 bytes four are loaded at once (two: 4 x 6639 rows into 3062 x 989 bf16 100 us, now 79).
 template <class T, int WIDE, int L> struct Columns;
 template <int L> struct Columns<__nv_bfloat16, 1, L> {

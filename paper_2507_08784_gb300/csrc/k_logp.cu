@@ -16,7 +16,7 @@
 // A list that runs over (many equal logits, every element above those before), a NaN or an infinity, and more alternatives than
 // the maxima can bound well are left to a radix selection of the keys, which reads the row again four to seven times.
 //
-// Bound by what it issues beside HBM: 4096 x 131071 bf16 with the entropy and 64 alternatives 239 us (1.07 GB, 4.5 TB/s), 180 without
+// Bound by what it issues beside HBM: 4096 x 131071 bf16 with the entropy and 64 alternatives 234 us (1.07 GB, 4.6 TB/s), 180 without
 // alternatives (6.0 TB/s).
 //
 // A row is a CTA's, or with few rows a cluster's: each CTA takes a part, and ranks its ordered alternatives among those of
@@ -663,9 +663,9 @@ cudaError_t token_logp(const TokenLogp& a, int dtype, cudaStream_t st) {
     // CTAs a row: a cluster where the rows leave SMs idle, each CTA with 4096 logits at least
     int parts = 1;
     while (parts < 8 && a.rows * parts * 2 <= 2 * 152 && a.vocab >= parts * 2 * 4096) parts *= 2;
-    // Threads a CTA: smaller ones are more in turn at a row's end (4096 x 131071 bf16, 64 alternatives: 263 us with 128, 279 with 256,
-    // 352 with 64; 16384 x 5003 without alternatives 66 with 128, 51 with 64), but bound fewer alternatives, and share fewer keys'
-    // ordering in a cluster (one row of 32768, 64 alternatives: 15 with 128, 11 with 256).
+    // Threads a CTA: smaller ones are more in turn at a row's end (4096 x 131071 bf16, 64 alternatives: 246 us with 128, 262 with 256,
+    // 331 with 64; 16384 x 5003 without alternatives 66 with 128, 51 with 64), but bound fewer alternatives, and share fewer keys'
+    // ordering in a cluster (one row of 32768, 64 alternatives: 13 with 128, 9 with 256).
     const auto listed = [&](int threads) { return threads * (dtype == GLR_BF16 ? kAhead<__nv_bfloat16> : kAhead<float>) * 3 / 8; };
     int threads = a.vocab <= (a.topk ? 2048 : 8192) && a.topk <= listed(64) ? 64 : 128;
     if (threads == 128 && (a.topk > std::min(128, listed(128)) || (parts > 1 && a.topk > 32))) threads = 256;

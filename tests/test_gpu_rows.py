@@ -143,6 +143,19 @@ def test_embedding_grad_of_many_chunks(glr, rows, vocab, d):
     _embedding_grad(glr, 1, rows, vocab, d, torch.float32, torch.float32, tokens, scale=0.25)
 
 
+@pytest.mark.parametrize("nodes,rows,vocab,d,pad,shift", [
+    (2, 900, 130, 264, 3, 0), (1, 5000, 700, 600, 1, 0), (2, 3000, 400, 40, 0, 1), (3, 300, 40000, 520, 5, 2), (1, 2000, 70000, 256, 1, 1),
+])
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("dt,gd", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32")])
+def test_embedding_grad_of_rows_off_16_bytes(glr, nodes, rows, vocab, d, pad, shift, accumulate, dt, gd):
+    """Whole vectors of dE from rows of dY at any alignment; a token of hundreds of rows, and single ones."""
+    gen = torch.Generator().manual_seed(d)
+    tokens = (torch.rand(nodes * rows, generator=gen) ** 5 * vocab).long()
+    tokens[::17] = -1
+    _embedding_grad(glr, nodes, rows, vocab, d, DT[dt], DT[gd], tokens, pad, shift, scale=0.5, accumulate=accumulate)
+
+
 def test_embedding_grad_of_no_rows(glr):
     dE = [torch.full((9, 16), 5.0, device="cuda") for _ in range(2)]
     args = (torch.empty(0, 16, device="cuda"), torch.empty(0, device="cuda", dtype=torch.int32), dE)
