@@ -213,7 +213,7 @@ __device__ __noinline__ int select_keys(const RowVectors<T>& row, int topk, floa
             for (int u = 0; u < 4; ++u) row.load(q0 + u * NT + threadIdx.x, v[u]);
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                if (!(v[u].top() >= floor)) continue;
+                if (v[u].top() < floor) continue;    // (false of eight NaNs, whose maximum is one)
                 for (int e = 0; e < 8; ++e) {
                     const float x = v[u].at(e);
                     const int index = row.first(q0 + u * NT + threadIdx.x) + e;
@@ -259,7 +259,7 @@ __device__ __noinline__ int select_keys(const RowVectors<T>& row, int topk, floa
         if (bin < 0) { every = true; break; }        // fewer than topk entries: all of them (first digit only)
         prefix = prefix << bits | static_cast<uint64_t>(bin);
         want -= above;
-        // the bin's least entry is a better floor (a NaN or an infinity among them is none: all vectors are looked at then)
+        // the bin's least entry is a better floor (not where a NaN or an infinity may be it: all vectors are looked at then)
         if (most != 0xffffffffu) floor = fmaxf(floor, logit_of(least_order + static_cast<uint32_t>((prefix << low) >> index_bits)));
         if (inside == want) break;                   // the whole bin is wanted: its lower bits need no decision
     }
