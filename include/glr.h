@@ -708,6 +708,8 @@ int glr_token_logp(const glr_token_logp_args* a, void* stream);
 /* The logits' gradient from those of logp and entropy (rows; either may be null), with lse and, for
  * dentropy, entropy as glr_token_logp left them:
  *   dlogits_v = (dlogp ([v = token] - p_v) - dentropy p_v (log p_v + entropy)) / tau
+ * Up to |lse| = 64 p is formed from lse, whose rounding leaves it within 2^-16 of itself.  Rows further from zero (an lse that left
+ * the range among them, -infinity) are read once more for their maximum and sum, and are as exact as logp.
  * dlogits may be logits itself with the same ld.  Rows without a distribution, and the first term of rows whose token
  * lies outside [0, vocab), are zero; a row with neither term is not read.                         */
 typedef struct glr_token_logp_grad_args {

@@ -581,9 +581,43 @@ __global__ void __launch_bounds__(NT, 1280 / NT) token_logp_kernel(const __grid_
 }
 
 // dz_v = (dlogp (e_token - p_v) - dentropy p_v (log p_v + entropy)) / tau, with log p_v = z_v / tau - lse; the same elements by
-// the same thread, so dz may be z.  Bound by HBM: 6000 x 65536 bf16 with both terms 238 us, 6.6 TB/s
+// the same thread, so dz may be z.  Bound by HBM: 6000 x 65536 bf16 with both terms 232 us, 6.8 TB/s
 // (one vector's load at a time 293).
 template <class T> constexpr int kGradAhead = sizeof(T) == 2 ? 4 : 2;
+
+// lse is one fp32 number, off by up to |lse| 2^-24, and z / tau by as much: up to 64 that leaves every p within 2^-16 of itself.
+// Beyond (logits far from zero, rows of the type's lowest value, an m / tau that leaves the range) the row's maximum and sum
+// are formed again, and log p_v = (z_v - m) / tau - log s (6000 x 65536 bf16, all rows such: 378 us; one of 131072 18, in place 30).
+constexpr float kFar = 64.f;
+
+// The CTA's Stat (without u) of a whole row.  Not inlined: few rows need it, and its registers would be every row's.
+template <class T>
+__device__ __noinline__ Stat row_stat(const T* z, int vocab, float c) {
+    __shared__ Stat stats[kThreads / 32];
+    constexpr int A = kGradAhead<T>;
+    const RowVectors<T> row(z, vocab, 0, 1);
+    Stat t{kLowest, 0.f, 0.f};
+    for (int q0 = row.begin; q0 < row.end; q0 += A * kThreads) {
+        Eight<T> x[A];
+        float m = t.m, s = 0.f;
+#pragma unroll
+        for (int u = 0; u < A; ++u) { row.load(q0 + u * kThreads + threadIdx.x, x[u]); m = fmaxf(m, x[u].top()); }
+#pragma unroll
+        for (int u = 0; u < A; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s += exp2_fast((x[u].at(e) - m) * c);
+        t.s = fmaf(t.s, exp2_fast((t.m - m) * c), s);
+        t.m = m;
+    }
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) t = join(t, Stat{__shfl_xor_sync(0xffffffffu, t.m, o), __shfl_xor_sync(0xffffffffu, t.s, o), 0.f}, c);
+    if ((threadIdx.x & 31) == 0) stats[threadIdx.x >> 5] = t;
+    __syncthreads();
+    t = stats[0];
+    for (int w = 1; w < kThreads / 32; ++w) t = join(t, stats[w], c);
+    return t;
+}
+
 template <class T, bool ENT>
 __global__ void __launch_bounds__(kThreads) token_logp_grad_kernel(const __grid_constant__ TokenLogpGrad a, int parts) {
     chain_begin();
@@ -592,14 +626,24 @@ __global__ void __launch_bounds__(kThreads) token_logp_grad_kernel(const __grid_
     const int part = static_cast<int>(blockIdx.x % parts);
     const T* z = static_cast<const T*>(a.z) + i * a.ldz;
     T* dz = static_cast<T*>(a.dz) + i * a.lddz;
-    const RowVectors<T> row(z, static_cast<int>(a.vocab), part, parts);
+    RowVectors<T> row(z, static_cast<int>(a.vocab), part, parts);
     const int64_t y64 = a.tokens.p ? a.tokens.at(i) : -1;
     const int y = y64 >= 0 && y64 < a.vocab ? static_cast<int>(y64) : -8;
-    const float lse = a.lse[i];
-    const bool some = lse != -kInf;
-    const float coef = a.dlogp && y >= 0 && some ? a.dlogp[i] * a.inv_tau : 0.f;
-    const float bonus = ENT && some ? a.dentropy[i] * a.inv_tau : 0.f;
-    const bool read = coef != 0.f || bonus != 0.f;   // (a NaN among them too)
+    float lse = a.lse[i], m = 0.f;
+    float coef = a.dlogp && y >= 0 ? a.dlogp[i] * a.inv_tau : 0.f;
+    float bonus = ENT ? a.dentropy[i] * a.inv_tau : 0.f;
+    bool read = coef != 0.f || bonus != 0.f;         // (a NaN among them too)
+    const bool far = read && fabsf(lse) > kFar;      // the same for all CTAs of a row
+    if (far) {
+        if (a.dz == a.z) {                           // one CTA for all of it: another would read what it has written
+            if (part) return;
+            row = RowVectors<T>(z, static_cast<int>(a.vocab), 0, 1);
+        }
+        const Stat t = row_stat(z, static_cast<int>(a.vocab), kLog2e * a.inv_tau);
+        m = t.m;
+        lse = logf(t.s);
+        if (t.s == 0.f) { read = false; coef = bonus = 0.f; }        // no distribution
+    }
     // the factor of p: -coef - bonus (log p + entropy)
     const float base = -(bonus != 0.f ? fmaf(bonus, a.entropy[i], coef) : coef);
     const bool wide = (reinterpret_cast<uintptr_t>(dz) & 15) == (reinterpret_cast<uintptr_t>(z) & 15);
@@ -624,6 +668,10 @@ __global__ void __launch_bounds__(kThreads) token_logp_grad_kernel(const __grid_
             float v[8];
 #pragma unroll
             for (int e = 0; e < 4; ++e) unpack2(x[u].pair(e), v[2 * e], v[2 * e + 1]);
+            if (far) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] -= m;
+            }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float lp = fmaf(v[e], a.inv_tau, -lse), p = exp2_fast(lp * kLog2e);
