@@ -564,9 +564,10 @@ int glr_embedding(const glr_embedding_args* a, void* stream);
 
 /* Every node's gradient of the embedding: the rows of dY (nodes * rows x d) and of tokens are the
  * nodes' one after the other, `rows` each, and
- *   dE[i][v] = scale sum of dY[t] over node i's rows t with tokens[t] = v, in the order of the rows
+ *   dE[i][v] = scale sum of dY[t] over node i's rows t with tokens[t] = v
  * (vocab x d, contiguous, grad_dtype: what glr_step takes as G[i]), zero for tokens that do not
- * occur; with accumulate 1 it is added to what dE[i] holds (the gradient of an output layer that
+ * occur.  The sum is of several partial ones, its order a function of nodes, rows, vocab, d and tokens alone (so a node's
+ * bits by itself may be others than together with more).  With accumulate 1 it is added to what dE[i] holds (the gradient of an output layer that
  * shares the matrix).  dE is a host array of `nodes` device pointers to matrices that do not overlap;
  * 1 <= nodes <= GLR_MAX_NODES, nodes * rows <= 2^30.  workspace (device memory, 16-byte aligned, for one call at a
  * time) holds the sorted tokens of many rows: as many bytes as glr_embedding_grad_workspace says.   */

@@ -1,8 +1,9 @@
 // Embedding lookup with scaling, and every node's gradient of the embedding by sorted tokens.
 //
-// The gradient of row v is scale times the sum of the rows of dY whose token is v, in the order of the rows, so its result
-// does not depend on what runs when.  A CTA takes 64 or 256 rows of the vocabulary and 256 columns and adds up the rows of dY that
-// belong to them, one warp a row, or all its warps where there are many.
+// The gradient of row v is scale times the sum of the rows of dY whose token is v.  They are put in the order of the rows and
+// added up in partial sums that the sizes and the tokens fix (a warp's groups of lanes take rows in turn, and from kMany rows on
+// the warps groups of 32), so that the result does not depend on what runs when.  A CTA takes 64 or 256 rows of the vocabulary
+// and 64 or 256 columns and adds up the rows of dY that belong to them, one warp a row, or all its warps where there are many.
 // Where it finds them depends on the node's rows: up to kScan it looks through the node's tokens and puts its own in order of
 // (token, row); beyond, chunks of kChunk rows have been sorted by their tokens, stably, by a kernel before, with the place where each
 // tile begins.  Both order by ranks among equal digits: warps take consecutive stretches, lanes with the same digit are matched.

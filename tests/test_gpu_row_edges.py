@@ -1,5 +1,5 @@
-"""The row operators at the edges of what they promise: alternatives of rows that hold NaNs, gradients of log-probabilities
-of logits far from zero (marked gpu)."""
+"""The row operators at the edges of what they promise: the order of an embedding gradient's sums, alternatives of rows that
+hold NaNs, gradients of log-probabilities of logits far from zero (marked gpu)."""
 import math
 
 import pytest
@@ -23,6 +23,34 @@ def _lib():
 def glr(_lib):
     import paper_2507_08784_gb300
     return paper_2507_08784_gb300
+
+
+# ---------------------------------------------------------------------------------------------------- embeddings
+
+# narrow and wide slices, looked through and sorted
+@pytest.mark.parametrize("nodes,rows,vocab,d", [(2, 700, 90, 48), (4, 1000, 40000, 512), (1, 6000, 300, 264), (8, 2000, 32000, 256)])
+@pytest.mark.parametrize("gd", ["f32", "bf16"])
+def test_order_of_the_sums(glr, nodes, rows, vocab, d, gd):
+    """It is fixed by the sizes and the tokens: strides, alignment, the tokens' type, the type of equal values and a run
+    beside other work change no bit."""
+    gen = torch.Generator().manual_seed(d)
+    n = nodes * rows
+    tokens = ((torch.rand(n, generator=gen) ** 5 * (vocab + 40)).long() - 20).cuda()
+    value = torch.randn(n, d, generator=gen).bfloat16()
+
+    def run(dt, pad, shift, index, stream=None):
+        dY = Guarded(n, d, dt, pad, shift, value=value)
+        dE = [torch.empty(vocab, d, device="cuda", dtype=DT[gd]) for _ in range(nodes)]
+        torch.cuda.synchronize()
+        glr.glr_embedding_grad(dY.t, tokens.to(index), dE, scale=1.25, stream=stream)
+        torch.cuda.synchronize()
+        return torch.stack(dE)
+
+    want = run(torch.bfloat16, 0, 0, torch.int64)
+    side = torch.cuda.Stream()
+    for dt, pad, shift, index, stream in ((torch.bfloat16, 1, 0, torch.int32, None), (torch.bfloat16, 8, 3, torch.int64, side),
+                                          (torch.float32, 0, 0, torch.int32, None), (torch.float32, 3, 1, torch.int64, side)):
+        assert torch.equal(run(dt, pad, shift, index, stream), want)
 
 
 # ------------------------------------------------------------------------------------------- log-probabilities
