@@ -290,8 +290,8 @@ extern "C" int glr_linear_grad_checkpoint(const glr_linear_grad_checkpoint_args*
         if (int rc = linear::grad_input_packed(who, g, codes, a->ld_codes, scales, a->ld_scales, a->act, st)) return rc;
     }
     if (a->dW) {
-        // (The epilogue of dX, which has the pre-activation in hand, could write it too: 320 us of 8192 x 5632 to 2048 bf16 with SiLU
-        // instead of 313, and other input gradients 8 us slower.)
+        // (The epilogue of dX, which has the pre-activation in hand, could write it too: 8192 x 5632 to 2048 bf16 with SiLU, 318 us, took
+        // 7 us more so, and other input gradients 8.)
         rows::Unpack u{};
         u.rows = a->nodes * a->rows; u.cols = a->k;
         u.codes = codes; u.ld_codes = a->ld_codes; u.scales = scales; u.ld_scales = a->ld_scales;

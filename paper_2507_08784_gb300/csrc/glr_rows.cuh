@@ -65,7 +65,7 @@ __device__ __forceinline__ void store8(T* p, int n, bool wide, const float (&v)[
 
 // Where rows do not lie on 16 bytes, a warp takes 256 columns with each lane's eight 32 apart, so that neighbouring lanes
 // touch neighbouring elements (each lane's eight next to each other cost four times the L1's cycles: a norm of 8192 x 4095 bf16
-// with a residual and 8-bit output 182 us instead of 84).
+// 87 us instead of 49, its gradient 227 instead of 109).
 template <class T>
 __device__ __forceinline__ void load_apart(const T* row, int64_t first, int64_t cols, float (&v)[8]) {
     const int64_t j = first + (threadIdx.x & 31);

@@ -5,8 +5,9 @@
 // (h beyond 1e19) the sum is formed again of h 2^-72.
 // The gradient, dx = rstd (w dy - x^ mean(w dy x^)) + d with x^ = h rstd, needs one sum a row; dw_j = sum_t dy x^ is summed by
 // each CTA over its rows of one node in registers, and over the CTAs by a second kernel in their order.
-// Both are bound by HBM: 8192 x 4096 bf16 with residual and 8-bit output 53 us (303 MB, 5.7 TB/s), gradient with residual 45 us
-// (268 MB, 6.0 TB/s) and 5 for the weights' sums.  A row a CTA at a time, without the ring of rows on their way, took 69 and 127.
+// Both are bound by HBM: 8192 x 4096 bf16 with residual and 8-bit output 54 us (303 MB, 5.6 TB/s), gradient of eight nodes with
+// residual 57 us (268 MB, 4.7 TB/s), 4 of them the second kernel's.  A row a CTA at a time, without the ring of rows on their way,
+// took 72 and 122.
 #include <algorithm>
 
 #include "glr_rows.cuh"
